@@ -60,6 +60,7 @@ extern "C" {
 #define LUQ_STATUS_BOUNDS 8    /* only from the checking build of the library (compiled with -DLUQ_DEBUG, see
                                   luq_debug_build): an address a kernel formed lay outside its region; that access
                                   was skipped (never a trap), outputs unspecified */
+#define LUQ_STATUS_OFFSETS 16 /* group offsets that decrease or leave [0, M]: taken as their running maximum, clamped */
 
 /* options for luq_set_option */
 #define LUQ_OPT_MMA_KIND 1 /* 0: tcgen05 kind::f8f6f4 on e4m3 operands (operand bytes passed to a GEMM are then
@@ -375,6 +376,78 @@ int luq_gemm_wgrad(luq_ctx* ctx, const uint8_t* d_g_codes, const float* d_alpha,
 int luq_gemm_wgrad_static(const uint8_t* d_g_codes, const float* d_alpha, int n_samples,
                           const uint8_t* d_a_codes, const float* d_sa,
                           float* d_dw, int64_t M, int64_t N, int64_t K, void* stream);
+
+/* ---- layer norm, and answering in 8 bits -----------------------------------------------------------
+ * What a Transformer block needs around the products above, and the integer form in which a trained
+ * layer answers (the paper trains; it has no counterpart of these).  Rows are tokens.  Row strides
+ * ("ld_*") are in elements and at least the row's length; x, dy, y, dx and z need the alignment of
+ * their element type only (rows that start at multiples of 16 bytes are faster), int8 codes a 16-byte
+ * aligned base and a row stride that is a multiple of 16 (bytes between a row's end and the next row
+ * are neither read nor written).  d_gamma / d_beta / d_bias and all scales are fp32.  rows or M = 0 is a
+ * no-op; a row length (cols, K) below 1 is LUQ_ERR_ARG.  Inputs and outputs must not overlap.
+ *
+ * Layer norm: y = (x - mean) * rstd * gamma + beta with mean and variance over the row (the variance
+ * divides by cols), rstd = (variance + eps)^-1/2.  d_gamma / d_beta may be NULL (ones / zeros); d_mean
+ * and d_rstd [rows] may be NULL, the backward pass needs them.  Inf or NaN in a row makes that row NaN. */
+int luq_layer_norm(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int64_t cols, int64_t ld_x,
+                   const float* d_gamma, const float* d_beta, float eps,
+                   void* d_y, int64_t ld_y, float* d_mean, float* d_rstd, void* stream);
+
+/* Backward pass of luq_layer_norm: with xhat = (x - mean) * rstd and g = dy * gamma
+ *   dx = rstd * (g - mean_c(g) - xhat * mean_c(g * xhat)),  dgamma = sum_r dy * xhat,  dbeta = sum_r dy.
+ * d_dx, d_dgamma, d_dbeta: each may be NULL (not needed).  dy, x and dx have the element type `dtype`,
+ * the others are fp32.  The sums over rows are made in a fixed order (results repeat bit for bit); their
+ * partial sums use the context's workspace.  rows = 0 gives zero dgamma and dbeta. */
+int luq_layer_norm_bwd(luq_ctx* ctx, const void* d_dy, int64_t ld_dy, const void* d_x, int64_t ld_x, int dtype,
+                       int64_t rows, int64_t cols, const float* d_gamma, const float* d_mean, const float* d_rstd,
+                       void* d_dx, int64_t ld_dx, float* d_dgamma, float* d_dbeta, void* stream);
+
+/* int8 codes with a scale for each row (token): scale = max|x| / 127, q = rint(x * fl(127 / max|x|)), ties to
+ * even, value q * scale.  A row of zeros: zero codes and scale.  A non-zero maximum below 2^-100: the same, and
+ * LUQ_STATUS_RANGE.  A row with Inf or NaN: zero codes and a NaN scale (its products are NaN, other rows'
+ * are not), and LUQ_STATUS_NONFINITE. */
+int luq_quant_int8_rows(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int64_t cols, int64_t ld_x,
+                        int8_t* d_codes, int64_t ld_codes, float* d_scale, void* stream);
+/* luq_layer_norm followed by luq_quant_int8_rows in one pass; the norm's result is quantized as the fp32
+ * numbers it is computed in, not rounded to the type of x first. */
+int luq_layer_norm_int8(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int64_t cols, int64_t ld_x,
+                        const float* d_gamma, const float* d_beta, float eps,
+                        int8_t* d_codes, int64_t ld_codes, float* d_scale, void* stream);
+
+/* Z[t,n] = sx[t] * sw[n] * sum_k X[t,k] * W[n,k] + bias[n]: x_codes [M x K] with a scale per token, w_codes
+ * [N x K] with a scale per output channel (quantize W with luq_quant_int8_rows), any int8 codes.
+ * z_dtype: LUQ_F32 or LUQ_BF16.  Any M, N >= 0, 1 <= K <= 131071 (the int32 sums are exact up to there,
+ * LUQ_ERR_UNSUPPORTED beyond).  d_bias may be NULL. */
+int luq_gemm_int8(luq_ctx* ctx, const int8_t* d_x_codes, int64_t ld_x, const float* d_sx,
+                  const int8_t* d_w_codes, int64_t ld_w, const float* d_sw, const float* d_bias,
+                  void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream);
+
+/* The same grouped by expert: rows d_offsets[e] .. d_offsets[e+1]-1 are multiplied with w_codes[e] (w_stride
+ * bytes apart, a multiple of 16), sw[e*N + n] and bias[e*N + n].  d_offsets: groups + 1 int32 in DEVICE memory,
+ * non-decreasing; groups may be empty; 1 <= groups <= LUQ_MAX_GROUPS.  Rows before the first or from the last
+ * offset on belong to no group and are not written.  Offsets that decrease or leave [0, M] raise
+ * LUQ_STATUS_OFFSETS and are taken as their running maximum, clamped. */
+#define LUQ_MAX_GROUPS 1024
+int luq_gemm_int8_grouped(luq_ctx* ctx, const int8_t* d_x_codes, int64_t ld_x, const float* d_sx,
+                          const int32_t* d_offsets, int groups,
+                          const int8_t* d_w_codes, int64_t ld_w, int64_t w_stride, const float* d_sw, const float* d_bias,
+                          void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream);
+
+/* Quantizer and product in one call, from the high-precision tokens x [M x K]: luq_quant_int8_rows then
+ * luq_gemm_int8 / luq_gemm_int8_grouped, or luq_layer_norm_int8 then luq_gemm_int8, with the same results bit
+ * for bit.  The tokens' codes and scales stay in the context's workspace: M * (16 * ceil(K / 16) + 4) bytes,
+ * LUQ_ERR_WORKSPACE beyond 96 MiB (make the two calls, or more calls with fewer rows). */
+int luq_quant_int8_gemm(luq_ctx* ctx, const void* d_x, int dtype, int64_t ld_x,
+                        const int8_t* d_w_codes, int64_t ld_w, const float* d_sw, const float* d_bias,
+                        void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream);
+int luq_layer_norm_int8_gemm(luq_ctx* ctx, const void* d_x, int dtype, int64_t ld_x,
+                             const float* d_gamma, const float* d_beta, float eps,
+                             const int8_t* d_w_codes, int64_t ld_w, const float* d_sw, const float* d_bias,
+                             void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream);
+int luq_quant_int8_gemm_grouped(luq_ctx* ctx, const void* d_x, int dtype, int64_t ld_x,
+                                const int32_t* d_offsets, int groups,
+                                const int8_t* d_w_codes, int64_t ld_w, int64_t w_stride, const float* d_sw, const float* d_bias,
+                                void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream);
 
 /* 1 if this library was compiled with -DLUQ_DEBUG: every shared-memory, tensor-memory and global
  * address that the converters, epilogues and streaming loops form is checked against its region

@@ -1,6 +1,6 @@
 """In-tree build of the sm_100a C-ABI library (``libluq_b200.so``) with nvcc.
 
-``python -m paper_2112_10769_b200.build`` compiles the three translation units
+``python -m paper_2112_10769_b200.build`` compiles the translation units
 and links one shared library next to this file.  nvcc cross-compiles without a
 GPU.  The quantizer file is compiled without FMA contraction; nothing is built
 with fast-math, flush-to-zero or approximate division.
@@ -21,7 +21,7 @@ ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 COMMON = ["-std=c++17", "-O3", "-lineinfo", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"),
           "-I", CSRC, "--expt-relaxed-constexpr",
           "-diag-suppress", "177"]   # 177: a static member that one instantiation of a configuration struct does not use
-UNITS = {"quant.cu": ["-fmad=false"], "gemm.cu": [], "api.cu": []}
+UNITS = {"quant.cu": ["-fmad=false"], "gemm.cu": [], "rows.cu": [], "gemm_int8.cu": [], "api.cu": []}
 
 
 def _digest(paths, extra=()) -> str:

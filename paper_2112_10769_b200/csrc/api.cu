@@ -494,6 +494,178 @@ int luq_gemm_wgrad(luq_ctx* ctx, const uint8_t* d_g_codes, const float* d_alpha,
   return cuda_rc(luq_launch_gemm(ctx, a, as_stream(stream)));
 }
 
+// ---- layer norm, and answering in 8 bits ---------------------------------------------------------------
+
+namespace {
+
+constexpr int64_t kMaxExtent = (1ll << 31) - 4096;   // tile counts and rounded-up extents stay in int32
+
+bool element_type(int dtype) { return dtype == LUQ_F32 || dtype == LUQ_BF16; }
+// a tensor of rows x cols elements of `dtype` with a row stride: present if needed, aligned to its elements
+bool tensor_ok(const void* p, int dtype, int64_t rows, int64_t cols, int64_t ld, bool needed) {
+  if (!p) return !needed || rows == 0;
+  return (reinterpret_cast<uintptr_t>(p) & (dtype == LUQ_BF16 ? 1u : 3u)) == 0 && (rows <= 1 || ld >= cols);
+}
+bool floats_ok(const void* p, bool needed) { return p ? (reinterpret_cast<uintptr_t>(p) & 3u) == 0 : !needed; }
+bool codes_ok(const void* p, int64_t rows, int64_t cols, int64_t ld) {
+  return rows == 0 || (p && aligned16(p) && ld >= cols && ld % 16 == 0 && ld < (1ll << 40));
+}
+bool rows_ok(int64_t rows, int64_t cols) { return rows >= 0 && cols >= 1 && rows <= kMaxExtent && cols <= kMaxExtent; }
+
+int int8_args_ok(const luq_int8_args& a, int z_dtype, bool grouped) {
+  if (!element_type(z_dtype) || a.M < 0 || a.N < 0 || a.K < 1 || a.M > kMaxExtent || a.N > kMaxExtent) return LUQ_ERR_ARG;
+  if (a.K > 131071) return LUQ_ERR_UNSUPPORTED;
+  if (grouped && (a.groups < 1 || a.groups > LUQ_MAX_GROUPS || (a.M && a.N && !a.offsets))) return LUQ_ERR_ARG;
+  if (grouped && ((reinterpret_cast<uintptr_t>(a.offsets) & 3u) || a.w_stride % 16 || a.w_stride >= (1ll << 40) ||
+                  (a.groups > 1 && a.N && a.w_stride < (a.N - 1) * a.ld_w + a.K))) return LUQ_ERR_ARG;
+  if (a.M == 0 || a.N == 0) return LUQ_OK;
+  if (!codes_ok(a.w_codes, a.N, a.K, a.ld_w)) return LUQ_ERR_ARG;
+  if (!floats_ok(a.sw, true) || !floats_ok(a.bias, false)) return LUQ_ERR_ARG;
+  return tensor_ok(a.z, z_dtype, a.M, a.N, a.ld_z, true) ? LUQ_OK : LUQ_ERR_ARG;
+}
+
+// the product, from codes (x == null) or from high-precision rows that are quantized into the workspace first
+int int8_product(luq_ctx* ctx, luq_int8_args a, int z_dtype, bool grouped, const void* x, int dtype, int64_t ld_x, bool norm,
+                 const float* gamma, const float* beta, float eps, bool from_codes, void* stream) {
+  if (!ctx) return LUQ_ERR_ARG;
+  const int rc = int8_args_ok(a, z_dtype, grouped);
+  if (rc) return rc;
+  a.out_bf16 = z_dtype == LUQ_BF16;
+  if (!grouped) { a.offsets = nullptr; a.groups = 1; a.w_stride = a.ld_w * a.N; }
+  if (from_codes) {
+    if (!codes_ok(a.x_codes, a.M, a.K, a.ld_x) || !floats_ok(a.sx, a.M > 0)) return LUQ_ERR_ARG;
+  } else {
+    if (!element_type(dtype) || !tensor_ok(x, dtype, a.M, a.K, ld_x, true)) return LUQ_ERR_ARG;
+    if (!floats_ok(gamma, false) || !floats_ok(beta, false) || !(eps >= 0.0f)) return LUQ_ERR_ARG;
+  }
+  if (a.M == 0 || a.N == 0) return LUQ_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return LUQ_ERR_CUDA;
+  if (!from_codes) {
+    a.ld_x = (a.K + 15) / 16 * 16;
+    const size_t codes = static_cast<size_t>(a.M) * static_cast<size_t>(a.ld_x);
+    if (codes + static_cast<size_t>(a.M) * sizeof(float) > ctx->workspace_bytes) return LUQ_ERR_WORKSPACE;
+    int8_t* const q = reinterpret_cast<int8_t*>(ctx->d_workspace);
+    float* const s = reinterpret_cast<float*>(q + codes);
+    const int e = cuda_rc(luq_launch_int8_rows(ctx, x, dtype, a.M, static_cast<int>(a.K), ld_x, norm, gamma, beta, eps, q,
+                                               a.ld_x, s, as_stream(stream)));
+    if (e) return e;
+    a.x_codes = q;
+    a.sx = s;
+  }
+  return cuda_rc(luq_launch_gemm_int8(ctx, a, as_stream(stream)));
+}
+
+luq_int8_args int8_args(const int8_t* x, int64_t ld_x, const float* sx, const int32_t* offsets, int groups, const int8_t* w,
+                        int64_t ld_w, int64_t w_stride, const float* sw, const float* bias, void* z, int64_t ld_z, int64_t M,
+                        int64_t N, int64_t K) {
+  luq_int8_args a{};
+  a.x_codes = x; a.ld_x = ld_x; a.sx = sx; a.offsets = offsets; a.groups = groups;
+  a.w_codes = w; a.ld_w = ld_w; a.w_stride = w_stride; a.sw = sw; a.bias = bias;
+  a.z = z; a.ld_z = ld_z; a.M = M; a.N = N; a.K = K;
+  return a;
+}
+
+}  // namespace
+
+int luq_layer_norm(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int64_t cols, int64_t ld_x,
+                   const float* d_gamma, const float* d_beta, float eps, void* d_y, int64_t ld_y, float* d_mean,
+                   float* d_rstd, void* stream) {
+  if (!ctx || !element_type(dtype) || !rows_ok(rows, cols) || !(eps >= 0.0f)) return LUQ_ERR_ARG;
+  if (!tensor_ok(d_x, dtype, rows, cols, ld_x, true) || !tensor_ok(d_y, dtype, rows, cols, ld_y, true)) return LUQ_ERR_ARG;
+  if (!floats_ok(d_gamma, false) || !floats_ok(d_beta, false) || !floats_ok(d_mean, false) || !floats_ok(d_rstd, false))
+    return LUQ_ERR_ARG;
+  if (rows == 0) return LUQ_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return LUQ_ERR_CUDA;
+  return cuda_rc(luq_launch_layer_norm(ctx, d_x, dtype, rows, static_cast<int>(cols), ld_x, d_gamma, d_beta, eps, d_y, ld_y,
+                                       d_mean, d_rstd, as_stream(stream)));
+}
+
+int luq_layer_norm_bwd(luq_ctx* ctx, const void* d_dy, int64_t ld_dy, const void* d_x, int64_t ld_x, int dtype, int64_t rows,
+                       int64_t cols, const float* d_gamma, const float* d_mean, const float* d_rstd, void* d_dx,
+                       int64_t ld_dx, float* d_dgamma, float* d_dbeta, void* stream) {
+  if (!ctx || !element_type(dtype) || !rows_ok(rows, cols)) return LUQ_ERR_ARG;
+  if (!tensor_ok(d_dy, dtype, rows, cols, ld_dy, true) || !tensor_ok(d_x, dtype, rows, cols, ld_x, true) ||
+      !tensor_ok(d_dx, dtype, rows, cols, ld_dx, false)) return LUQ_ERR_ARG;
+  if (!floats_ok(d_gamma, false) || !floats_ok(d_mean, rows > 0) || !floats_ok(d_rstd, rows > 0) ||
+      !floats_ok(d_dgamma, false) || !floats_ok(d_dbeta, false)) return LUQ_ERR_ARG;
+  if (!d_dx && !d_dgamma && !d_dbeta) return LUQ_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return LUQ_ERR_CUDA;
+  if (rows == 0) {                                    // the sums over nothing
+    const size_t bytes = static_cast<size_t>(cols) * sizeof(float);
+    if (d_dgamma && cudaMemsetAsync(d_dgamma, 0, bytes, as_stream(stream)) != cudaSuccess) return LUQ_ERR_CUDA;
+    if (d_dbeta && cudaMemsetAsync(d_dbeta, 0, bytes, as_stream(stream)) != cudaSuccess) return LUQ_ERR_CUDA;
+    return LUQ_OK;
+  }
+  return cuda_rc(luq_launch_layer_norm_bwd(ctx, d_dy, ld_dy, d_x, ld_x, dtype, rows, static_cast<int>(cols), d_gamma, d_mean,
+                                           d_rstd, d_dx, ld_dx, d_dgamma, d_dbeta, as_stream(stream)));
+}
+
+static int int8_rows(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int64_t cols, int64_t ld_x, bool norm,
+                     const float* d_gamma, const float* d_beta, float eps, int8_t* d_codes, int64_t ld_codes, float* d_scale,
+                     void* stream) {
+  if (!ctx || !element_type(dtype) || !rows_ok(rows, cols) || !(eps >= 0.0f)) return LUQ_ERR_ARG;
+  if (!tensor_ok(d_x, dtype, rows, cols, ld_x, true) || !codes_ok(d_codes, rows, cols, ld_codes)) return LUQ_ERR_ARG;
+  if (!floats_ok(d_gamma, false) || !floats_ok(d_beta, false) || !floats_ok(d_scale, rows > 0)) return LUQ_ERR_ARG;
+  if (rows == 0) return LUQ_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return LUQ_ERR_CUDA;
+  return cuda_rc(luq_launch_int8_rows(ctx, d_x, dtype, rows, static_cast<int>(cols), ld_x, norm, d_gamma, d_beta, eps, d_codes,
+                                      ld_codes, d_scale, as_stream(stream)));
+}
+
+int luq_quant_int8_rows(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int64_t cols, int64_t ld_x, int8_t* d_codes,
+                        int64_t ld_codes, float* d_scale, void* stream) {
+  return int8_rows(ctx, d_x, dtype, rows, cols, ld_x, false, nullptr, nullptr, 0.0f, d_codes, ld_codes, d_scale, stream);
+}
+
+int luq_layer_norm_int8(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int64_t cols, int64_t ld_x,
+                        const float* d_gamma, const float* d_beta, float eps, int8_t* d_codes, int64_t ld_codes,
+                        float* d_scale, void* stream) {
+  return int8_rows(ctx, d_x, dtype, rows, cols, ld_x, true, d_gamma, d_beta, eps, d_codes, ld_codes, d_scale, stream);
+}
+
+int luq_gemm_int8(luq_ctx* ctx, const int8_t* d_x_codes, int64_t ld_x, const float* d_sx, const int8_t* d_w_codes, int64_t ld_w,
+                  const float* d_sw, const float* d_bias, void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K,
+                  void* stream) {
+  return int8_product(ctx, int8_args(d_x_codes, ld_x, d_sx, nullptr, 1, d_w_codes, ld_w, 0, d_sw, d_bias, d_z, ld_z, M, N, K),
+                      z_dtype, false, nullptr, 0, 0, false, nullptr, nullptr, 0.0f, true, stream);
+}
+
+int luq_gemm_int8_grouped(luq_ctx* ctx, const int8_t* d_x_codes, int64_t ld_x, const float* d_sx, const int32_t* d_offsets,
+                          int groups, const int8_t* d_w_codes, int64_t ld_w, int64_t w_stride, const float* d_sw,
+                          const float* d_bias, void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K,
+                          void* stream) {
+  return int8_product(ctx, int8_args(d_x_codes, ld_x, d_sx, d_offsets, groups, d_w_codes, ld_w, w_stride, d_sw, d_bias, d_z,
+                                     ld_z, M, N, K),
+                      z_dtype, true, nullptr, 0, 0, false, nullptr, nullptr, 0.0f, true, stream);
+}
+
+int luq_quant_int8_gemm(luq_ctx* ctx, const void* d_x, int dtype, int64_t ld_x, const int8_t* d_w_codes, int64_t ld_w,
+                        const float* d_sw, const float* d_bias, void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N,
+                        int64_t K, void* stream) {
+  return int8_product(ctx, int8_args(nullptr, 0, nullptr, nullptr, 1, d_w_codes, ld_w, 0, d_sw, d_bias, d_z, ld_z, M, N, K),
+                      z_dtype, false, d_x, dtype, ld_x, false, nullptr, nullptr, 0.0f, false, stream);
+}
+
+int luq_layer_norm_int8_gemm(luq_ctx* ctx, const void* d_x, int dtype, int64_t ld_x, const float* d_gamma, const float* d_beta,
+                             float eps, const int8_t* d_w_codes, int64_t ld_w, const float* d_sw, const float* d_bias,
+                             void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream) {
+  return int8_product(ctx, int8_args(nullptr, 0, nullptr, nullptr, 1, d_w_codes, ld_w, 0, d_sw, d_bias, d_z, ld_z, M, N, K),
+                      z_dtype, false, d_x, dtype, ld_x, true, d_gamma, d_beta, eps, false, stream);
+}
+
+int luq_quant_int8_gemm_grouped(luq_ctx* ctx, const void* d_x, int dtype, int64_t ld_x, const int32_t* d_offsets, int groups,
+                                const int8_t* d_w_codes, int64_t ld_w, int64_t w_stride, const float* d_sw,
+                                const float* d_bias, void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K,
+                                void* stream) {
+  return int8_product(ctx, int8_args(nullptr, 0, nullptr, d_offsets, groups, d_w_codes, ld_w, w_stride, d_sw, d_bias, d_z,
+                                     ld_z, M, N, K),
+                      z_dtype, true, d_x, dtype, ld_x, false, nullptr, nullptr, 0.0f, false, stream);
+}
+
 int luq_status(luq_ctx* ctx, void* stream, int* host_flags) {
   if (!ctx || !host_flags) return LUQ_ERR_ARG;
   DeviceGuard guard(ctx->device);

@@ -99,6 +99,29 @@ int luq_launch_quant_fwd(luq_ctx* ctx, const void* d_a, int dtype, const float* 
                          float* d_z, int64_t M, int64_t N, int64_t K, cudaStream_t st, float* d_estimate = nullptr,
                          float eta = 0.0f, float* d_measured = nullptr);
 
+// rows.cu: layer norm and the row-wise int8 quantizer (row strides ld_* in elements)
+int luq_launch_layer_norm(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int cols, int64_t ld_x,
+                          const float* d_gamma, const float* d_beta, float eps, void* d_y, int64_t ld_y, float* d_mean,
+                          float* d_rstd, cudaStream_t st);
+int luq_launch_layer_norm_bwd(luq_ctx* ctx, const void* d_dy, int64_t ld_dy, const void* d_x, int64_t ld_x, int dtype,
+                              int64_t rows, int cols, const float* d_gamma, const float* d_mean, const float* d_rstd,
+                              void* d_dx, int64_t ld_dx, float* d_dgamma, float* d_dbeta, cudaStream_t st);
+// norm: the codes are those of the layer norm's result, not of x
+int luq_launch_int8_rows(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int cols, int64_t ld_x, bool norm,
+                         const float* d_gamma, const float* d_beta, float eps, int8_t* d_codes, int64_t ld_codes,
+                         float* d_scale, cudaStream_t st);
+
+// gemm_int8.cu: Z[t, n] = sx[t] sw[e, n] sum_k X[t, k] W[e, n, k] + bias[e, n], e = the group of row t
+struct luq_int8_args {
+  const int8_t* x_codes; int64_t ld_x; const float* sx;
+  const int* offsets; int groups;                       // offsets null: one group
+  const int8_t* w_codes; int64_t ld_w; int64_t w_stride;
+  const float* sw; const float* bias;
+  void* z; int out_bf16; int64_t ld_z;
+  int64_t M, N, K;
+};
+int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, cudaStream_t st);
+
 #ifdef __CUDACC__
 
 // Launch helper.  LUQ_LAUNCH_COOPERATIVE: all blocks of the grid are resident at once (the kernel
