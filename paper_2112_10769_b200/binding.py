@@ -8,6 +8,8 @@ paper_2112_10769_b200.build``) or no sm_100 GPU is present, calls raise.
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import os
 
 import torch
@@ -15,6 +17,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 # LUQ_LIB selects another build of the same library, e.g. the bounds-checking one (libluq_b200_debug.so)
 LIB_PATH = os.environ.get("LUQ_LIB") or os.path.join(_HERE, "libluq_b200.so")
+NATIVE_PATH = os.path.join(_HERE, "_calls.so")
 
 LUQ_F32, LUQ_BF16 = 0, 1
 STATUS_NONFINITE, STATUS_RANGE, STATUS_TIMEOUT, STATUS_BOUNDS = 1, 2, 4, 8
@@ -108,6 +111,34 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError("inputs are float32 or bfloat16")
 
 
+def _dtype_value(dtype: torch.dtype) -> int:
+    if dtype is torch.float32:
+        return LUQ_F32
+    if dtype is torch.bfloat16:
+        return LUQ_BF16
+    raise TypeError("outputs are float32 or bfloat16")
+
+
+_native = None
+_NATIVE_ENTRIES = ("luq_layer_norm", "luq_layer_norm_bwd", "luq_layer_norm_int8", "luq_quant_int8_rows", "luq_gemm_int8",
+                   "luq_gemm_int8_grouped", "luq_quant_int8_gemm", "luq_layer_norm_int8_gemm", "luq_quant_int8_gemm_grouped")
+
+
+def native():
+    """The native argument handling of the 8-bit operators, bound to the loaded library; raises if it is missing."""
+    global _native
+    if _native is None:
+        L = load()
+        if not os.path.exists(NATIVE_PATH):
+            raise RuntimeError(f"{NATIVE_PATH} not found: build it with `python -m paper_2112_10769_b200.build`")
+        loader = importlib.machinery.ExtensionFileLoader("_calls", NATIVE_PATH)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_calls", loader))
+        loader.exec_module(module)
+        module.bind(LuqError, *(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in _NATIVE_ENTRIES))
+        _native = module
+    return _native
+
+
 def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
@@ -136,6 +167,7 @@ class Context:
         h = ctypes.c_void_p()
         _check(load().luq_create(ctypes.byref(h), device), "luq_create")
         self.handle = h
+        self._address, self._native = h.value, native()
 
     def close(self):
         if getattr(self, "handle", None):
@@ -413,188 +445,66 @@ class Context:
         return out
 
     # ---- layer norm, and answering in 8 bits ----------------------------------------------------
-    # Tokens are rows: 2-D tensors (leading dimensions are flattened) whose rows are contiguous; other layouts
-    # and broadcast rows are copied first.  int8 codes are [rows, cols] views of rows that start at
-    # multiples of 16 bytes (new_codes makes them).
-    def _tokens(self, t: torch.Tensor, what: str) -> torch.Tensor:
-        if t.get_device() != self.device:
-            raise TypeError(f"{what}: tensor on cuda:{self.device} expected, got {t.device}")
-        if t.dim() != 2:
-            t = t.reshape(-1, t.shape[-1])
-        if (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-            t = t.contiguous()
-        return t
-
-    def _floats(self, t, numel: int, what: str):
-        """Pointer of an optional float32 tensor (None -> NULL), size, type and place checked."""
-        if t is None:
-            return None
-        if t.dtype != torch.float32 or t.numel() != numel or not t.is_contiguous() or t.get_device() != self.device:
-            raise TypeError(f"{what}: contiguous float32 tensor of {numel} elements on cuda:{self.device} expected")
-        return t.data_ptr()
-
-    def _codes(self, t: torch.Tensor, shape, what: str) -> int:
-        """Row stride of an int8 tensor of codes after checking it."""
-        if t.dtype != torch.int8 or tuple(t.shape) != tuple(shape) or t.get_device() != self.device:
-            raise TypeError(f"{what}: int8 tensor of shape {tuple(shape)} on cuda:{self.device} expected")
-        cols = shape[-1]
-        ld = t.stride(-2) if shape[-2] > 1 else -(-cols // 16) * 16
-        if (t.stride(-1) != 1 and cols > 1) or ld % 16 or ld < cols or t.data_ptr() % 16:
-            raise TypeError(f"{what}: rows have to start at multiples of 16 bytes (see new_codes)")
-        return ld
-
+    # Tokens are rows: tensors whose rows are contiguous (leading dimensions are flattened); other layouts and
+    # broadcast rows are copied first.  int8 codes are [rows, cols] views of rows that start at multiples of
+    # 16 bytes (new_codes makes them).  Types, shapes and devices are checked in native code (_calls), which
+    # raises TypeError; the C entry points' own refusals raise LuqError.
     def new_codes(self, rows: int, cols: int) -> torch.Tensor:
         """Uninitialised int8 codes [rows, cols] in the layout the products read."""
         return torch.empty((rows, -(-cols // 16) * 16), dtype=torch.int8, device=f"cuda:{self.device}")[:, :cols]
 
-    def _z(self, out, rows: int, cols: int, dtype, x: torch.Tensor):
-        if out is None:
-            return torch.empty((rows, cols), dtype=dtype, device=x.device)
-        if tuple(out.shape) != (rows, cols) or (out.stride(1) != 1 and cols > 1) or \
-                (rows > 1 and out.stride(0) < cols) or out.get_device() != self.device:
-            raise TypeError(f"output: {rows} x {cols} tensor with contiguous rows on cuda:{self.device} expected")
-        return out
-
     def layer_norm(self, x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
                    eps: float = 1e-5, out: torch.Tensor | None = None):
         """(y, mean, rstd): layer norm over the last dimension; mean and 1/std of every row for the backward pass."""
-        shape, x = x.shape, self._tokens(x, "x")
-        rows, cols = x.shape
-        y = self._z(out, rows, cols, x.dtype, x)
-        if y.dtype != x.dtype:
-            raise TypeError("layer norm's result has the type of its input")
-        mean = torch.empty(rows, dtype=torch.float32, device=x.device)
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-        _check(load().luq_layer_norm(self.handle, x.data_ptr(), _dtype_code(x), rows, cols, x.stride(0) if rows > 1 else cols,
-                                     self._floats(weight, cols, "weight"), self._floats(bias, cols, "bias"), eps,
-                                     y.data_ptr(), y.stride(0) if rows > 1 else cols, mean.data_ptr(), rstd.data_ptr(),
-                                     _stream()), "luq_layer_norm")
-        return (y if out is not None or len(shape) == 2 else y.reshape(shape)), mean, rstd
+        return self._native.layer_norm(self._address, self.device, x, weight, bias, eps, out)
 
     def layer_norm_bwd(self, dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
                        weight: torch.Tensor | None = None, need_dx: bool = True, need_dweight: bool = True,
                        need_dbias: bool = True):
         """(dx, dweight, dbias) of layer_norm; what is not needed is None and not computed."""
-        if dy.shape != x.shape or dy.dtype != x.dtype:
-            raise TypeError("dy has the shape and type of x")
-        shape, x, dy = x.shape, self._tokens(x, "x"), self._tokens(dy, "dy")
-        rows, cols = x.shape
-        dx = torch.empty((rows, cols), dtype=x.dtype, device=x.device) if need_dx else None
-        dw = torch.empty(cols, dtype=torch.float32, device=x.device) if need_dweight else None
-        db = torch.empty(cols, dtype=torch.float32, device=x.device) if need_dbias else None
-        _check(load().luq_layer_norm_bwd(self.handle, dy.data_ptr(), dy.stride(0) if rows > 1 else cols, x.data_ptr(),
-                                         x.stride(0) if rows > 1 else cols, _dtype_code(x), rows, cols,
-                                         self._floats(weight, cols, "weight"), self._floats(mean, rows, "mean"),
-                                         self._floats(rstd, rows, "rstd"), dx.data_ptr() if need_dx else None, cols,
-                                         dw.data_ptr() if need_dweight else None, db.data_ptr() if need_dbias else None,
-                                         _stream()), "luq_layer_norm_bwd")
-        return (dx if dx is None or len(shape) == 2 else dx.reshape(shape)), dw, db
+        return self._native.layer_norm_bwd(self._address, self.device, dy, x, mean, rstd, weight, need_dx, need_dweight,
+                                           need_dbias)
 
     def layer_norm_int8(self, x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
                         eps: float = 1e-5):
         """(codes, scale): layer norm, its result as int8 codes with a scale for each row, in one pass."""
-        x = self._tokens(x, "x")
-        rows, cols = x.shape
-        codes = self.new_codes(rows, cols)
-        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
-        _check(load().luq_layer_norm_int8(self.handle, x.data_ptr(), _dtype_code(x), rows, cols,
-                                          x.stride(0) if rows > 1 else cols, self._floats(weight, cols, "weight"),
-                                          self._floats(bias, cols, "bias"), eps, codes.data_ptr(), -(-cols // 16) * 16,
-                                          scale.data_ptr(), _stream()), "luq_layer_norm_int8")
-        return codes, scale
+        return self._native.layer_norm_int8(self._address, self.device, x, weight, bias, eps)
 
     def quant_int8_rows(self, x: torch.Tensor):
         """(codes, scale): int8 codes with a scale for each row - tokens, or the output channels of a weight."""
-        x = self._tokens(x, "x")
-        rows, cols = x.shape
-        codes = self.new_codes(rows, cols)
-        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
-        _check(load().luq_quant_int8_rows(self.handle, x.data_ptr(), _dtype_code(x), rows, cols,
-                                          x.stride(0) if rows > 1 else cols, codes.data_ptr(), -(-cols // 16) * 16,
-                                          scale.data_ptr(), _stream()), "luq_quant_int8_rows")
-        return codes, scale
-
-    def _weights(self, w: torch.Tensor, K: int, grouped: bool):
-        """(groups, N, row stride, expert stride) of weight codes [N, K] or, grouped, [groups, N, K]."""
-        if w.dim() != (3 if grouped else 2) or w.shape[-1] != K:
-            raise TypeError(f"weight codes: {'[groups, N, K]' if grouped else '[N, K]'} with K = {K} expected")
-        groups, N = (w.shape[0], w.shape[1]) if grouped else (1, w.shape[0])
-        ld = self._codes(w, w.shape, "weight codes")
-        return groups, N, ld, (w.stride(0) if grouped and groups > 1 else N * ld)
-
-    def _offsets(self, t: torch.Tensor, groups: int) -> int:
-        if t.dtype != torch.int32 or t.numel() != groups + 1 or not t.is_contiguous() or t.get_device() != self.device:
-            raise TypeError(f"offsets: contiguous int32 tensor of {groups + 1} elements on cuda:{self.device} expected")
-        return t.data_ptr()
+        return self._native.quant_int8_rows(self._address, self.device, x)
 
     def gemm_int8(self, codes: torch.Tensor, scale: torch.Tensor, w_codes: torch.Tensor, w_scale: torch.Tensor,
                   bias: torch.Tensor | None = None, out: torch.Tensor | None = None, out_dtype=torch.float32):
         """Z[t, n] = scale[t] * w_scale[n] * sum_k codes[t, k] * w_codes[n, k] (+ bias[n])."""
-        M, K = codes.shape
-        ld_x = self._codes(codes, codes.shape, "token codes")
-        _, N, ld_w, _ = self._weights(w_codes, K, False)
-        z = self._z(out, M, N, out_dtype, codes)
-        _check(load().luq_gemm_int8(self.handle, codes.data_ptr(), ld_x, self._floats(scale, M, "scale"), w_codes.data_ptr(), ld_w,
-                                    self._floats(w_scale, N, "w_scale"), self._floats(bias, N, "bias"), z.data_ptr(),
-                                    _dtype_code(z), z.stride(0) if M > 1 else N, M, N, K, _stream()), "luq_gemm_int8")
-        return z
+        return self._native.gemm_int8(self._address, self.device, codes, scale, w_codes, w_scale, bias, out,
+                                      _dtype_value(out_dtype))
 
     def gemm_int8_grouped(self, codes: torch.Tensor, scale: torch.Tensor, offsets: torch.Tensor, w_codes: torch.Tensor,
                           w_scale: torch.Tensor, bias: torch.Tensor | None = None, out: torch.Tensor | None = None,
                           out_dtype=torch.float32):
         """gemm_int8 with one weight per expert: rows offsets[e] .. offsets[e + 1] - 1 with w_codes[e].  `offsets` is on
         the device; rows that belong to no expert are not written."""
-        M, K = codes.shape
-        ld_x = self._codes(codes, codes.shape, "token codes")
-        E, N, ld_w, w_stride = self._weights(w_codes, K, True)
-        z = self._z(out, M, N, out_dtype, codes)
-        _check(load().luq_gemm_int8_grouped(self.handle, codes.data_ptr(), ld_x, self._floats(scale, M, "scale"),
-                                            self._offsets(offsets, E), E, w_codes.data_ptr(), ld_w, w_stride,
-                                            self._floats(w_scale, E * N, "w_scale"), self._floats(bias, E * N, "bias"),
-                                            z.data_ptr(), _dtype_code(z), z.stride(0) if M > 1 else N, M, N, K, _stream()),
-               "luq_gemm_int8_grouped")
-        return z
+        return self._native.gemm_int8_grouped(self._address, self.device, codes, scale, offsets, w_codes, w_scale, bias, out,
+                                              _dtype_value(out_dtype))
 
     def quant_int8_gemm(self, x: torch.Tensor, w_codes: torch.Tensor, w_scale: torch.Tensor, bias: torch.Tensor | None = None,
                         out: torch.Tensor | None = None, out_dtype=None):
         """quant_int8_rows(x) and gemm_int8 in one call; the result has the type of x unless said otherwise."""
-        x = self._tokens(x, "x")
-        M, K = x.shape
-        _, N, ld_w, _ = self._weights(w_codes, K, False)
-        z = self._z(out, M, N, out_dtype or x.dtype, x)
-        _check(load().luq_quant_int8_gemm(self.handle, x.data_ptr(), _dtype_code(x), x.stride(0) if M > 1 else K, w_codes.data_ptr(),
-                                          ld_w, self._floats(w_scale, N, "w_scale"), self._floats(bias, N, "bias"),
-                                          z.data_ptr(), _dtype_code(z), z.stride(0) if M > 1 else N, M, N, K, _stream()),
-               "luq_quant_int8_gemm")
-        return z
+        return self._native.quant_int8_gemm(self._address, self.device, x, w_codes, w_scale, bias, out,
+                                            -1 if out_dtype is None else _dtype_value(out_dtype))
 
     def layer_norm_int8_gemm(self, x: torch.Tensor, weight, bias, eps: float, w_codes: torch.Tensor, w_scale: torch.Tensor,
                              w_bias: torch.Tensor | None = None, out: torch.Tensor | None = None, out_dtype=None):
         """layer_norm_int8(x, weight, bias, eps) and gemm_int8 in one call."""
-        x = self._tokens(x, "x")
-        M, K = x.shape
-        _, N, ld_w, _ = self._weights(w_codes, K, False)
-        z = self._z(out, M, N, out_dtype or x.dtype, x)
-        _check(load().luq_layer_norm_int8_gemm(self.handle, x.data_ptr(), _dtype_code(x), x.stride(0) if M > 1 else K,
-                                               self._floats(weight, K, "weight"), self._floats(bias, K, "bias"), eps,
-                                               w_codes.data_ptr(), ld_w, self._floats(w_scale, N, "w_scale"),
-                                               self._floats(w_bias, N, "w_bias"), z.data_ptr(), _dtype_code(z),
-                                               z.stride(0) if M > 1 else N, M, N, K, _stream()), "luq_layer_norm_int8_gemm")
-        return z
+        return self._native.layer_norm_int8_gemm(self._address, self.device, x, weight, bias, eps, w_codes, w_scale, w_bias, out,
+                                                 -1 if out_dtype is None else _dtype_value(out_dtype))
 
     def quant_int8_gemm_grouped(self, x: torch.Tensor, offsets: torch.Tensor, w_codes: torch.Tensor, w_scale: torch.Tensor,
                                 bias: torch.Tensor | None = None, out: torch.Tensor | None = None, out_dtype=None):
         """quant_int8_rows(x) and gemm_int8_grouped in one call."""
-        x = self._tokens(x, "x")
-        M, K = x.shape
-        E, N, ld_w, w_stride = self._weights(w_codes, K, True)
-        z = self._z(out, M, N, out_dtype or x.dtype, x)
-        _check(load().luq_quant_int8_gemm_grouped(self.handle, x.data_ptr(), _dtype_code(x), x.stride(0) if M > 1 else K,
-                                                  self._offsets(offsets, E), E, w_codes.data_ptr(), ld_w, w_stride,
-                                                  self._floats(w_scale, E * N, "w_scale"), self._floats(bias, E * N, "bias"),
-                                                  z.data_ptr(), _dtype_code(z), z.stride(0) if M > 1 else N, M, N, K,
-                                                  _stream()), "luq_quant_int8_gemm_grouped")
-        return z
+        return self._native.quant_int8_gemm_grouped(self._address, self.device, x, offsets, w_codes, w_scale, bias, out,
+                                                    -1 if out_dtype is None else _dtype_value(out_dtype))
 
     def status(self) -> int:
         """Synchronises the current stream; returns and clears the device status bits."""

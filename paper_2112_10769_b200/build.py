@@ -16,6 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libluq_b200.so")
+NATIVE = os.path.join(HERE, "_calls.so")                 # argument handling of the 8-bit operators (a Python extension)
 LIB_DEBUG = os.path.join(HERE, "libluq_b200_debug.so")   # the same sources with -DLUQ_DEBUG (bounds-checking build)
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 COMMON = ["-std=c++17", "-O3", "-lineinfo", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"),
@@ -48,6 +49,26 @@ def _stamp(target: str, digest: str) -> None:
         f.write(digest)
 
 
+def build_native(force: bool = False) -> str:
+    """Compiles the Python extension that checks the 8-bit operators' arguments (host code only)."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    src = os.path.join(CSRC, "torch_calls.cpp")
+    digest = _digest([src, os.path.join(ROOT, "include", "luq.h")], [torch.__version__, sys.version])
+    if force or _stale(NATIVE, digest):
+        lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
+        includes = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(ROOT, "include"),
+                                                    os.path.join(cpp_extension.CUDA_HOME or "/usr/local/cuda", "include")]
+        cmd = ["g++", "-std=c++20", "-O2", "-fPIC", "-shared", "-fvisibility=hidden",
+               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", src, "-o", NATIVE]
+        cmd += [f"-isystem{d}" for d in includes] + [f"-L{lib_dir}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+        subprocess.run(cmd, check=True)
+        _stamp(NATIVE, digest)
+    return NATIVE
+
+
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
     """Compiles the library; debug=True compiles the bounds-checking variant (-DLUQ_DEBUG) next to it."""
     nvcc = os.environ.get("NVCC", "nvcc")
@@ -74,6 +95,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     if force or _stale(lib, link_digest):
         subprocess.run([nvcc] + ARCH + ["-shared", "-o", lib] + objs, check=True)
         _stamp(lib, link_digest)
+    build_native(force)
     return lib
 
 

@@ -16,7 +16,8 @@ struct DeviceGuard {
   bool ok = true;
   explicit DeviceGuard(int dev) {
     if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+    if (prev == dev) { prev = -1; return; }          // nothing to restore
+    if (cudaSetDevice(dev) != cudaSuccess) ok = false;
   }
   ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
 };
