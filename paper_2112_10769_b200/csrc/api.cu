@@ -554,7 +554,7 @@ int int8_product(luq_ctx* ctx, luq_int8_args a, int z_dtype, bool grouped, const
     a.x_codes = q;
     a.sx = s;
   }
-  return cuda_rc(luq_launch_gemm_int8(ctx, a, as_stream(stream)));
+  return cuda_rc(luq_launch_gemm_int8(ctx, a, !from_codes, as_stream(stream)));
 }
 
 luq_int8_args int8_args(const int8_t* x, int64_t ld_x, const float* sx, const int32_t* offsets, int groups, const int8_t* w,

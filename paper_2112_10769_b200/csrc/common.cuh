@@ -120,7 +120,8 @@ struct luq_int8_args {
   void* z; int out_bf16; int64_t ld_z;
   int64_t M, N, K;
 };
-int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, cudaStream_t st);
+// early: the preceding kernel of the stream is this call's quantizer, which writes x_codes and sx only
+int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, bool early, cudaStream_t st);
 
 #ifdef __CUDACC__
 

@@ -29,9 +29,8 @@ using namespace luqdev;
 constexpr int kCh = 128;                  // output channels per tile (tensor-memory lanes)
 constexpr int kBk = 128;                  // contraction elements per stage
 constexpr int kSlab = kCh * kBk;          // bytes of W per stage
-constexpr int kThreads = 192;
 constexpr int kFirstEpiWarp = 2;
-constexpr int kBox = 32 * 32 * 4;         // one 32 x 32 fp32 store box (half of it for bf16)
+constexpr int kWarpStaging = 32 * 32 * 4; // a warp's store boxes: one of 32 x 32 fp32, or two of bf16
 constexpr int kBand = 8;                  // token tiles that walk the channels together
 
 struct Int8Params {
@@ -46,26 +45,32 @@ struct Int8Params {
   int groups;
   int num_kb;
   int tiles_n;              // channel tiles
-  int out_bf16;
+  int early;                // everything but the tokens' codes and scales was there before the preceding kernel
   int z_tma;                // the output can be addressed by TMA
   long long tma_cols;       // a store copy writes whole 16-byte pieces: boxes up to this column end on one
 };
 
-template <int BT>
+// One tile: kCh channels (twice that on a CTA pair) by up to BT tokens.  EW epilogue warps, two per quarter of
+// the lanes where a tile has more than one step of 32 tokens.
+template <int BT, bool PAIR>
 struct Cfg {
-  static constexpr int x_bytes = BT * kBk;
-  static constexpr int stage_bytes = kSlab + x_bytes;
-  static constexpr int stages = BT == 256 ? 3 : BT == 128 ? 5 : BT == 64 ? 7 : BT == 32 ? 8 : 9;
+  static constexpr int epi_warps = BT <= 32 ? 4 : 8;
+  static constexpr int threads = 32 * (kFirstEpiWarp + epi_warps);
+  static constexpr int x_rows = PAIR ? BT / 2 : BT;               // token rows this CTA holds of a tile
+  static constexpr int box_rows = BT < 32 ? BT : 32;              // token rows per copy
+  static constexpr int stage_bytes = kSlab + x_rows * kBk;
+  static constexpr int stages = BT == 16 ? 10 : BT == 64 ? 7 : 5;
   static constexpr int chunk = BT < 32 ? BT : 32;                 // tokens per epilogue step
   static constexpr int tmem_cols = 2 * BT;
-  static constexpr int staging = stages * stage_bytes;            // 4 warps x 2 boxes
-  static constexpr int token_scales = staging + 4 * 2 * kBox;     // 4 warps x 32 floats
-  static constexpr int barriers = token_scales + 4 * 128;
+  static constexpr int staging = stages * stage_bytes;            // store boxes, or a split's partial tile
+  static constexpr int token_scales = staging + (BT == 16 ? 8192 : epi_warps * kWarpStaging);   // two tiles' scales
+  static constexpr int barriers = token_scales + 2 * BT * 4;
   static constexpr int num_barriers = 2 * stages + 4;
   static constexpr int tmem_slot = barriers + 8 * num_barriers;
   static constexpr int abort_flag = tmem_slot + 4;
   static constexpr int groups = abort_flag + 4;                   // group ends, then tile prefix: 2 x (groups + 1) ints
-  static int smem_bytes(int n_groups) { return groups + 8 * (n_groups + 1) + 1024; }
+  static constexpr int smem_bytes(int n_groups) { return groups + 8 * (n_groups + 1) + 1024; }
+  static_assert(groups + 8 * (LUQ_MAX_GROUPS + 1) + 1024 <= 232448, "exceeds the 227 KB of shared memory a CTA may use");
 };
 
 __device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[16]) {
@@ -76,6 +81,16 @@ __device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[16])
         "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr)
       : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_nctarank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ int ld_shared_cluster(uint32_t cluster_addr) {
+  int v;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(cluster_addr) : "memory");
+  return v;
 }
 template <int CHUNK>
 __device__ __forceinline__ void load_chunk(uint32_t taddr, uint32_t (&r)[CHUNK]) {
@@ -136,7 +151,8 @@ struct Unit {
 };
 // Units walk the channel tiles in bands of kBand token tiles, tokens fastest: what runs together shares
 // both operands' tiles in L2.
-__device__ __forceinline__ Unit find_unit(long long u, const Int8Params& p, int tile_rows, const int* hi, const int* first_tile) {
+__device__ __forceinline__ Unit find_unit(long long u, const Int8Params& p, int tile_rows, int tile_ch, const int* hi,
+                                          const int* first_tile) {
   const int token_tiles = first_tile[p.groups];
   const long long per_band = static_cast<long long>(kBand) * p.tiles_n;
   const int band = static_cast<int>(u / per_band);
@@ -153,15 +169,107 @@ __device__ __forceinline__ Unit find_unit(long long u, const Int8Params& p, int 
   v.group = lo;
   v.row0 = hi[lo] + (j - first_tile[lo]) * tile_rows;
   v.rows = min(tile_rows, hi[lo + 1] - v.row0);
-  v.ch0 = c * kCh;
+  v.ch0 = c * tile_ch;
   return v;
 }
 
-template <int BT>
-__global__ void __launch_bounds__(kThreads, 1)
+__device__ __forceinline__ void store_z(void* z, long long at, float v, bool bf16) {
+  if (bf16) static_cast<__nv_bfloat16*>(z)[at] = __float2bfloat16_rn(v);
+  else static_cast<float*>(z)[at] = v;
+}
+
+// Takes a tile's accumulators out of tensor memory, scales them and writes them: this warp's quarter of the
+// lanes (32 channels), every second step of 32 tokens where two warps share a quarter.
+// A full step goes through a staged box [token][channel] and one copy; a step that holds rows of another
+// group, or an output the copies cannot address, is written element by element (32 channels in a row).
+template <typename C, bool BF16>
+__device__ __forceinline__ void write_tile(const Int8Params& p, const void* tm_z, const Unit& v, uint32_t taddr, int warp_e,
+                                           int lane, uint32_t staging, uint8_t* gen, const float* scales, uint32_t& box_it) {
+  constexpr int CH = C::chunk, kStep = C::epi_warps / 4 * CH;
+  constexpr int kBoxes = BF16 ? 2 : 1, kBoxBytes = kWarpStaging / kBoxes;
+  const int quarter = (warp_e + kFirstEpiWarp) & 3;
+  const int ch_first = v.ch0 + quarter * 32, ch = ch_first + lane;
+  if (ch_first >= p.N) return;                         // warp-uniform
+  const bool ch_in = ch < p.N;
+  const long long wi = static_cast<long long>(v.group) * p.N + ch;
+  const float sw = ch_in ? __ldg(p.sw + wi) : 0.0f;
+  const float bias = ch_in && p.bias ? __ldg(p.bias + wi) : 0.0f;
+  const bool boxes = CH == 32 && p.z_tma && (ch_first + 32 <= p.N || p.tma_cols == p.N);
+
+  auto emit = [&](const uint32_t (&r)[CH], int c0) {
+    const int left = v.rows - c0;                      // token rows of this step that exist
+    auto value = [&](int i, float s) { return fmaf(static_cast<float>(static_cast<int>(r[i])) * sw, s, bias); };
+    if (boxes && left >= 32) {
+      const uint32_t slot = static_cast<uint32_t>(warp_e) * kWarpStaging + (box_it & (kBoxes - 1)) * kBoxBytes;
+      ++box_it;
+      if (lane == 0) bulk_wait_read<kBoxes - 1>();     // the store that last read this box is done
+      __syncwarp();
+      uint8_t* const box = gen + C::staging + slot;
+#pragma unroll
+      for (int i = 0; i < CH; i += 4) {
+        const float4 s4 = *reinterpret_cast<const float4*>(scales + c0 + i);
+        const float z[4] = {value(i, s4.x), value(i + 1, s4.y), value(i + 2, s4.z), value(i + 3, s4.w)};
+        if constexpr (BF16) {
+          // a lane has one channel of two tokens, a word is two channels of one: neighbours swap halves, the
+          // even lane keeps the first token's word, the odd lane the second's
+#pragma unroll
+          for (int j = 0; j < 4; j += 2) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(z[j], z[j + 1]);
+            const uint32_t own = *reinterpret_cast<const uint32_t*>(&h);
+            const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, own, 1);
+            const uint32_t word = __byte_perm(own, other, lane & 1 ? 0x3276 : 0x5410);
+            uint8_t* const at = box + (i + j + (lane & 1)) * 64 + (lane >> 1) * 4;
+            if (smem_in(at, gen, C::staging, C::token_scales, 4, p.status)) *reinterpret_cast<uint32_t*>(at) = word;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint8_t* const at = box + (i + j) * 128 + lane * 4;
+            if (smem_in(at, gen, C::staging, C::token_scales, 4, p.status)) *reinterpret_cast<float*>(at) = z[j];
+          }
+        }
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) {
+        tma_store_2d(tm_z, staging + slot, ch_first, v.row0 + c0);
+        bulk_commit();
+      }
+    } else if (ch_in) {
+      const long long z0 = (static_cast<long long>(v.row0) + c0) * p.ld_z + ch;
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+        if (i < left) store_z(p.z, z0 + i * p.ld_z, value(i, scales[c0 + i]), BF16);
+    }
+  };
+
+  // two register sets: the next step's accumulators are on their way while this one's are written
+  uint32_t r0[CH], r1[CH];
+  int c = (warp_e >> 2) * CH;
+  if (c < v.rows) load_chunk<CH>(taddr + c, r0);
+#pragma unroll 1
+  for (; c < v.rows; c += 2 * kStep) {
+    tmem_ld_wait();
+    if (c + kStep < v.rows) load_chunk<CH>(taddr + c + kStep, r1);
+    emit(r0, c);
+    if (c + kStep < v.rows) {
+      tmem_ld_wait();
+      if (c + 2 * kStep < v.rows) load_chunk<CH>(taddr + c + 2 * kStep, r0);
+      emit(r1, c + kStep);
+    }
+  }
+}
+
+// SPLIT: the CTAs of a cluster share a tile and take a share of its contraction each (few tokens: too few tiles
+// for the SMs); partial tiles meet through distributed shared memory, as integers, in any order exact.
+// PAIR: the two CTAs of a cluster compute a tile of 256 channels together (cta_group::2), each fetches half of
+// the tokens' rows.
+template <int BT, bool PAIR, bool SPLIT, bool BF16>
+__global__ void __launch_bounds__((Cfg<BT, PAIR>::threads), 1)
 int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x,
                  const __grid_constant__ CUtensorMap tm_z, const Int8Params p) {
-  using C = Cfg<BT>;
+  static_assert(!(PAIR && SPLIT), "one use of the cluster at a time");
+  using C = Cfg<BT, PAIR>;
   constexpr int ES = C::stages;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -179,9 +287,12 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   int* const first_tile = hi + p.groups + 1;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = PAIR || SPLIT ? cluster_ctarank() : 0u;
+  const uint32_t cluster = PAIR ? 2u : (SPLIT ? cluster_nctarank() : 1u);
   if (threadIdx.x == 0) {
+    // on a pair the leader's barriers count both CTAs
     for (int s = 0; s < ES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), 4); }
+    for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), (PAIR ? 2 : 1) * C::epi_warps); }
     *abort_flag = 0;
     fence_barrier_init();
     fence_proxy_async();
@@ -189,154 +300,219 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     if (p.z_tma) tma_prefetch_desc(&tm_z);
   }
   if (warp == 1) {
-    tmem_alloc(base + C::tmem_slot, C::tmem_cols);
-    tmem_relinquish();
+    if constexpr (PAIR) { tmem_alloc_pair(base + C::tmem_slot, C::tmem_cols); tmem_relinquish_pair(); }
+    else { tmem_alloc(base + C::tmem_slot, C::tmem_cols); tmem_relinquish(); }
   }
-  pdl_wait();
+  // weights, offsets and channel scales may be read before the preceding kernel has ended when that kernel is
+  // this call's own quantizer (which started after all earlier ones had ended); its codes and scales may not
+  if (!p.early) pdl_wait();
   pdl_trigger();
   if (warp == kFirstEpiWarp) find_groups(p, BT, hi, first_tile, blockIdx.x == 0);
   tc_fence_before();
-  __syncthreads();
+  if constexpr (PAIR || SPLIT) cluster_sync_all();     // both CTAs' barriers are set up
+  else __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  // units of this cluster: every cluster-th
   const long long units = static_cast<long long>(first_tile[p.groups]) * p.tiles_n;
+  const long long u_first = blockIdx.x / cluster, u_step = gridDim.x / cluster;
+  // this CTA's share of a tile's contraction
+  const int kb_first = SPLIT ? static_cast<int>(static_cast<long long>(p.num_kb) * rank / cluster) : 0;
+  const int kb_end = SPLIT ? static_cast<int>(static_cast<long long>(p.num_kb) * (rank + 1) / cluster) : p.num_kb;
 
-  if (warp == 0) {
-    // ---------------------------------------------------------------- producer
-    if (lane == 0) {
-      uint32_t issued = 0, stage = 0, phase = 0;
-      bool ok = true;
-      for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
-        const Unit v = find_unit(u, p, BT, hi, first_tile);
-        for (int kb = 0; kb < p.num_kb; ++kb) {
-          if (!mbar_wait(empty(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
-          const uint32_t dst = base + stage * C::stage_bytes;
-          mbar_arrive_expect_tx(full(stage), C::stage_bytes);
-          tma_load_3d(dst, &tm_w, full(stage), kb * kBk, v.ch0, v.group);
-          tma_load_2d(dst + kSlab, &tm_x, full(stage), kb * kBk, v.row0);
-          ++issued;
-          if (++stage == static_cast<uint32_t>(ES)) { stage = 0; phase ^= 1u; }
-        }
+  // ---- the roles, a unit at a time; state lives across units ----
+  uint32_t stage = 0, phase = 0, issued = 0, it = 0, box_it = 0;
+  bool ok = true, waited = !p.early;
+
+  auto produce = [&](const Unit& v) {                  // one thread
+    // token rows of this CTA: all of the tile's, or on a pair its half of the instruction's extent
+    const int half = (v.rows + 31) / 32 * 16;
+    const int x_row0 = v.row0 + (PAIR ? static_cast<int>(rank) * half : 0);
+    const int boxes = ((PAIR ? half : v.rows) + C::box_rows - 1) / C::box_rows;
+    const uint32_t bytes = kSlab + boxes * C::box_rows * kBk;
+    const int ch0 = v.ch0 + (PAIR ? static_cast<int>(rank) * kCh : 0);
+    auto w_copy = [&](int kb, uint32_t s) {
+      const uint32_t dst = base + s * C::stage_bytes;
+      if constexpr (PAIR) {
+        if (rank == 0) mbar_arrive_expect_tx(full(s), 2 * bytes);   // both CTAs' bytes
+        tma_pair_load_3d(dst, &tm_w, mapa_shared(full(s), 0), kb * kBk, ch0, v.group);
+      } else {
+        mbar_arrive_expect_tx(full(s), bytes);
+        tma_load_3d(dst, &tm_w, full(s), kb * kBk, ch0, v.group);
       }
-      // every copy must have landed before the CTA may exit
-      for (int s = 0; s < ES; ++s)
-        if (issued > static_cast<uint32_t>(s)) mbar_wait(full(s), ((issued - 1 - s) / ES) & 1u, abort_flag);
+    };
+    auto x_copy = [&](int kb, uint32_t s) {
+      const uint32_t dst = base + s * C::stage_bytes + kSlab;
+      for (int b = 0; b < boxes; ++b) {
+        if constexpr (PAIR) tma_pair_load_2d(dst + b * C::box_rows * kBk, &tm_x, mapa_shared(full(s), 0), kb * kBk, x_row0 + b * C::box_rows);
+        else tma_load_2d(dst + b * C::box_rows * kBk, &tm_x, full(s), kb * kBk, x_row0 + b * C::box_rows);
+      }
+    };
+    int kb = kb_first;
+    if (!waited) {
+      // the first stages' weights, then the wait for the quantizer, then their tokens
+      const int ahead = min(kb_end - kb, ES);
+      for (int i = 0; i < ahead; ++i) w_copy(kb + i, i);
+      pdl_wait();
+      waited = true;
+      for (int i = 0; i < ahead; ++i) x_copy(kb + i, i);
+      kb += ahead;
+      issued = ahead;
+      stage = ahead == ES ? 0 : ahead;
+      phase = ahead == ES ? 1 : 0;
     }
-  } else if (warp == 1) {
-    // -------------------------------------------------------------- MMA issuer
-    if (lane == 0) {
-      // S32 accumulator, signed 8-bit A and B, both K-major, M = 128; N per tile
-      constexpr uint32_t idesc0 = (2u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kCh >> 4) << 24);
-      const uint64_t da0 = umma_desc_sw128(base, 16, 1024), db0 = umma_desc_sw128(base + kSlab, 16, 1024);
-      constexpr uint64_t kStageStep = C::stage_bytes >> 4;
-      uint32_t stage = 0, phase = 0, it = 0;
-      bool ok = true;
-      for (long long u = blockIdx.x; ok && u < units; u += gridDim.x, ++it) {
-        const Unit v = find_unit(u, p, BT, hi, first_tile);
-        const uint32_t idesc = idesc0 | (static_cast<uint32_t>((v.rows + 15) / 16 * 2) << 17);
-        const uint32_t buf = it & 1u;
-        if (!mbar_wait(acc_empty(buf), ((it >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t tmem_d = tmem_base + buf * BT;
-        uint32_t accumulate = 0;
-        for (int kb = 0; kb < p.num_kb; ++kb) {
-          if (!mbar_wait(full(stage), phase, abort_flag)) { ok = false; break; }
-          tc_fence_after();
-          const uint64_t da = da0 + stage * kStageStep, db = db0 + stage * kStageStep;
-#pragma unroll
-          for (int kk = 0; kk < kBk / 32; ++kk) {
-            tc_mma<1>(tmem_d, da + kk * 2, db + kk * 2, idesc, accumulate);
-            accumulate = 1;
-          }
-          tc_commit(empty(stage));
-          if (++stage == static_cast<uint32_t>(ES)) { stage = 0; phase ^= 1u; }
-        }
-        if (ok) tc_commit(acc_full(buf));
+    for (; kb < kb_end; ++kb) {
+      if (!mbar_wait(empty(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
+      w_copy(kb, stage);
+      x_copy(kb, stage);
+      ++issued;
+      if (++stage == static_cast<uint32_t>(ES)) { stage = 0; phase ^= 1u; }
+    }
+  };
+  auto drain = [&]() {                                 // every copy must have landed before the CTA may exit
+    if (PAIR && rank != 0) return;                     // the leader's barriers count both CTAs' copies
+    for (int s = 0; s < ES; ++s)
+      if (issued > static_cast<uint32_t>(s)) {
+        if constexpr (PAIR) mbar_wait_cluster(full(s), ((issued - 1 - s) / ES) & 1u, abort_flag);
+        else mbar_wait(full(s), ((issued - 1 - s) / ES) & 1u, abort_flag);
       }
+  };
+  auto multiply = [&](const Unit& v) {                 // one thread (of the leader)
+    // S32 accumulator, signed 8-bit A and B, both K-major; N covers the tile's tokens
+    const uint32_t n8 = PAIR ? (v.rows + 31) / 32 * 4 : (v.rows + 15) / 16 * 2;
+    const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | (n8 << 17) | (static_cast<uint32_t>((PAIR ? 2 : 1) * kCh >> 4) << 24);
+    const uint64_t da0 = umma_desc_sw128(base, 16, 1024), db0 = umma_desc_sw128(base + kSlab, 16, 1024);
+    constexpr uint64_t kStageStep = C::stage_bytes >> 4;
+    const uint32_t buf = it & 1u;
+    const bool free = PAIR ? mbar_wait_cluster(acc_empty(buf), ((it >> 1) & 1u) ^ 1u, abort_flag)
+                           : mbar_wait(acc_empty(buf), ((it >> 1) & 1u) ^ 1u, abort_flag);
+    if (!free) { ok = false; return; }
+    tc_fence_after();
+    const uint32_t tmem_d = tmem_base + buf * BT;
+    uint32_t accumulate = 0;
+    for (int kb = kb_first; kb < kb_end; ++kb) {
+      const bool there = PAIR ? mbar_wait_cluster(full(stage), phase, abort_flag) : mbar_wait(full(stage), phase, abort_flag);
+      if (!there) { ok = false; return; }
+      tc_fence_after();
+      const uint64_t da = da0 + stage * kStageStep, db = db0 + stage * kStageStep;
+#pragma unroll
+      for (int kk = 0; kk < kBk / 32; ++kk) {
+        if constexpr (PAIR) tc_mma_pair<1>(tmem_d, da + kk * 2, db + kk * 2, idesc, accumulate);
+        else tc_mma<1>(tmem_d, da + kk * 2, db + kk * 2, idesc, accumulate);
+        accumulate = 1;
+      }
+      if constexpr (PAIR) tc_commit_pair(empty(stage));
+      else tc_commit(empty(stage));
+      if (++stage == static_cast<uint32_t>(ES)) { stage = 0; phase ^= 1u; }
+    }
+    if constexpr (PAIR) tc_commit_pair(acc_full(buf));
+    else tc_commit(acc_full(buf));
+  };
+
+  const int warp_e = warp - kFirstEpiWarp;
+  const uint32_t lane_base = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+  auto scales_of = [&](uint32_t i) { return reinterpret_cast<float*>(gen + C::token_scales) + (i & 1u) * BT; };
+  // the tile's token scales, fetched before its accumulators are awaited; the tile two before has been
+  // written by all warps once this one meets them here
+  auto fetch_scales = [&](const Unit& v) {
+    if (!waited) { pdl_wait(); waited = true; }
+    float* const s = scales_of(it);
+    for (int t = threadIdx.x - 32 * kFirstEpiWarp; t < v.rows; t += 32 * C::epi_warps) s[t] = __ldg(p.sx + v.row0 + t);
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * C::epi_warps) : "memory");
+  };
+
+  if constexpr (!SPLIT) {
+    if (warp == 0) {
+      if (lane == 0) {
+        for (long long u = u_first; ok && u < units; u += u_step) produce(find_unit(u, p, BT, PAIR ? 2 * kCh : kCh, hi, first_tile));
+        drain();
+      }
+    } else if (warp == 1) {
+      if (lane == 0 && rank == 0)
+        for (long long u = u_first; ok && u < units; u += u_step, ++it) multiply(find_unit(u, p, BT, PAIR ? 2 * kCh : kCh, hi, first_tile));
+    } else {
+      for (long long u = u_first; u < units; u += u_step, ++it) {
+        Unit v = find_unit(u, p, BT, PAIR ? 2 * kCh : kCh, hi, first_tile);
+        if (PAIR) v.ch0 += static_cast<int>(rank) * kCh;
+        fetch_scales(v);
+        const uint32_t buf = it & 1u;
+        // after a wait that ran out the loop goes on without touching the tile: the warps keep meeting
+        ok = ok && mbar_wait(acc_full(buf), (it >> 1) & 1u, abort_flag);
+        if (ok) {
+          tc_fence_after();
+          write_tile<C, BF16>(p, &tm_z, v, lane_base + buf * BT, warp_e, lane, base + C::staging, gen, scales_of(it), box_it);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (PAIR) mbar_arrive_cluster(mapa_shared(acc_empty(buf), 0));
+          else mbar_arrive(acc_empty(buf));
+        }
+      }
+      if (lane == 0) bulk_wait<0>();   // all stores of this warp are complete before the CTA exits
     }
   } else {
-    // ---------------------------------------------------------------- epilogue
-    const int quarter = warp & 3;                      // tensor-memory lanes this warp may read
-    const uint32_t stage0 = base + C::staging + (warp - kFirstEpiWarp) * 2 * kBox;
-    uint8_t* const stage0_gen = gen + C::staging + (warp - kFirstEpiWarp) * 2 * kBox;
-    float* const scales = reinterpret_cast<float*>(gen + C::token_scales + (warp - kFirstEpiWarp) * 128);
-    uint32_t it = 0, box_it = 0;
-    for (long long u = blockIdx.x; u < units; u += gridDim.x, ++it) {
-      const Unit v = find_unit(u, p, BT, hi, first_tile);
-      const int ch_first = v.ch0 + quarter * 32;
-      const int ch = ch_first + lane;
-      const bool ch_in = ch < p.N;
-      const long long wi = static_cast<long long>(v.group) * p.N + ch;
-      const float sw = ch_in ? __ldg(p.sw + wi) : 0.0f;
-      const float bias = ch_in && p.bias ? __ldg(p.bias + wi) : 0.0f;
-      const uint32_t buf = it & 1u;
-      if (!mbar_wait(acc_full(buf), (it >> 1) & 1u, abort_flag)) break;
-      tc_fence_after();
-      const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + buf * BT;
-      if (ch_first < p.N) {                            // warp-uniform
-#pragma unroll 1
-        for (int c0 = 0; c0 < v.rows; c0 += C::chunk) {
-          const int left = v.rows - c0;                // token rows of this step that exist
+    int* const partial = reinterpret_cast<int*>(gen + C::staging);      // [token][channel]
+    for (long long u = u_first; u < units; u += u_step, ++it) {
+      const Unit v = find_unit(u, p, BT, kCh, hi, first_tile);
+      if (warp == 0) {
+        if (lane == 0 && ok) produce(v);
+      } else if (warp == 1) {
+        if (lane == 0 && ok) multiply(v);
+      } else {
+        fetch_scales(v);
+        const uint32_t buf = it & 1u;
+        ok = ok && mbar_wait(acc_full(buf), (it >> 1) & 1u, abort_flag);
+        tc_fence_after();
+        for (int c = (warp_e >> 2) * C::chunk; ok && c < v.rows; c += C::epi_warps / 4 * C::chunk) {
           uint32_t r[C::chunk];
-          load_chunk<C::chunk>(taddr + c0, r);
-          __syncwarp();                                // the previous step's scales have been read
-          scales[lane] = lane < left ? __ldg(p.sx + v.row0 + c0 + lane) : 0.0f;
-          __syncwarp();
+          load_chunk<C::chunk>(lane_base + buf * BT + c, r);
           tmem_ld_wait();
-          auto value = [&](int i, float s) { return fmaf(static_cast<float>(static_cast<int>(r[i])) * sw, s, bias); };
-          if (C::chunk == 32 && p.z_tma && left >= 32 && (ch_first + 32 <= p.N || p.tma_cols == p.N)) {
-            const uint32_t b = box_it & 1u;
-            ++box_it;
-            if (lane == 0) bulk_wait_read<1>();        // the store that last read this box is done
-            __syncwarp();
-            uint8_t* const box = stage0_gen + b * kBox;
 #pragma unroll
-            for (int i = 0; i < C::chunk; i += 4) {
-              const float4 s4 = *reinterpret_cast<const float4*>(scales + i);
-              const float s[4] = {s4.x, s4.y, s4.z, s4.w};
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const float z = value(i + j, s[j]);
-                uint8_t* const at = box + (p.out_bf16 ? (i + j) * 64 + lane * 2 : (i + j) * 128 + lane * 4);
-                if (smem_in(at, gen, C::staging, C::token_scales, 4, p.status)) {
-                  if (p.out_bf16) *reinterpret_cast<__nv_bfloat16*>(at) = __float2bfloat16_rn(z);
-                  else *reinterpret_cast<float*>(at) = z;
-                }
-              }
-            }
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) {
-              tma_store_2d(&tm_z, stage0 + b * kBox, ch_first, v.row0 + c0);
-              bulk_commit();
-            }
-          } else if (ch_in) {
-            const long long z0 = (static_cast<long long>(v.row0) + c0) * p.ld_z + ch;
-#pragma unroll
-            for (int i = 0; i < C::chunk; ++i) {
-              if (i < left) {
-                const float z = value(i, scales[i]);
-                const long long at = z0 + i * p.ld_z;
-                if (p.out_bf16) static_cast<__nv_bfloat16*>(p.z)[at] = __float2bfloat16_rn(z);
-                else static_cast<float*>(p.z)[at] = z;
-              }
-            }
-          }
+          for (int i = 0; i < C::chunk; ++i)
+            if (smem_in(partial + (c + i) * kCh + (warp & 3) * 32 + lane, gen, C::staging, C::token_scales, 4, p.status))
+              partial[(c + i) * kCh + (warp & 3) * 32 + lane] = static_cast<int>(r[i]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(acc_empty(buf));
+      }
+      __syncwarp();
+      cluster_sync_all();              // every CTA's partial tile is there
+      if (warp >= kFirstEpiWarp) {
+        // a token's 128 channels at a time, tokens dealt out over the CTAs
+        const float* const s = scales_of(it);
+        const int ch = v.ch0 + (warp & 3) * 32 + lane;
+        const bool ch_in = ch < p.N;
+        const long long wi = static_cast<long long>(v.group) * p.N + ch;
+        const float sw = ch_in ? __ldg(p.sw + wi) : 0.0f;
+        const float bias = ch_in && p.bias ? __ldg(p.bias + wi) : 0.0f;
+        for (int t = static_cast<int>(rank) + (warp_e >> 2) * static_cast<int>(cluster); t < v.rows;
+             t += static_cast<int>(cluster) * (C::epi_warps / 4)) {
+          const uint32_t at = smem_u32(partial + t * kCh + (warp & 3) * 32 + lane);
+          int sum = 0;
+          for (uint32_t q = 0; q < cluster; ++q) sum += ld_shared_cluster(mapa_shared(at, q));
+          if (ch_in)
+            store_z(p.z, (static_cast<long long>(v.row0) + t) * p.ld_z + ch, fmaf(static_cast<float>(sum) * sw, s[t], bias), BF16);
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(acc_empty(buf));
+      cluster_sync_all();              // and has been read by all
     }
-    if (lane == 0) bulk_wait<0>();   // all stores of this warp are complete before the CTA exits
+    if (warp == 0 && lane == 0) drain();
   }
 
+  // a CTA without tiles has waited for nothing yet: what comes after this kernel relies on the preceding one
+  // having ended too
+  if (p.early) pdl_wait();
   tc_fence_before();
-  __syncthreads();
+  __syncwarp();
+  if constexpr (PAIR) cluster_sync_all();              // neither CTA leaves while the other's copies or arrivals need it
+  else __syncthreads();
   if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, LUQ_STATUS_TIMEOUT);
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem_base, C::tmem_cols);
+    if constexpr (PAIR) tmem_dealloc_pair(tmem_base, C::tmem_cols);
+    else tmem_dealloc(tmem_base, C::tmem_cols);
   }
 }
 
@@ -369,33 +545,37 @@ int encode_z(void* fn, CUtensorMap* map, void* ptr, int64_t cols, int64_t rows, 
                                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS;
 }
 
-template <int BT>
-int launch(luq_ctx* ctx, const luq_int8_args& a, const Int8Params& p, const CUtensorMap& tw, const CUtensorMap& tz,
-           cudaStream_t st) {
+template <int BT, bool PAIR, bool SPLIT, bool BF16>
+int launch(luq_ctx* ctx, const luq_int8_args& a, const Int8Params& p, long long units, int cluster, const CUtensorMap& tw,
+           const CUtensorMap& tz, cudaStream_t st) {
+  using C = Cfg<BT, PAIR>;
   CUtensorMap tx;
-  if (encode_codes(ctx->encode_tiled, &tx, a.x_codes, a.K, a.M, a.ld_x, 0, 0, BT)) return LUQ_ERR_CUDA;
-  auto kernel = int8_gemm_kernel<BT>;
-  const int smem = Cfg<BT>::smem_bytes(p.groups);
-  const cudaError_t attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (encode_codes(ctx->encode_tiled, &tx, a.x_codes, a.K, a.M, a.ld_x, 0, 0, C::box_rows)) return LUQ_ERR_CUDA;
+  auto kernel = int8_gemm_kernel<BT, PAIR, SPLIT, BF16>;
+  const cudaError_t attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem_bytes(LUQ_MAX_GROUPS));
   if (attr != cudaSuccess) return static_cast<int>(attr);
-  // token tiles: at most one partial tile per group that has rows
-  const long long partial = p.groups < a.M ? p.groups : a.M;
-  const long long most = (a.M / BT + partial) * p.tiles_n;
   const int sms = (ctx->sm_limit > 0 && ctx->sm_limit < ctx->sm_count) ? ctx->sm_limit : ctx->sm_count;
-  const int grid = static_cast<int>(most < sms ? most : sms);
-  const cudaError_t e = luq_launch_kernel(kernel, grid, kThreads, static_cast<size_t>(smem), st, LUQ_LAUNCH_EARLY, 1, tw, tx, tz, p);
+  const long long most = sms / cluster > 0 ? sms / cluster : 1;
+  const int grid = static_cast<int>(units < most ? units : most) * cluster;
+  const cudaError_t e = luq_launch_kernel(kernel, grid, C::threads, static_cast<size_t>(C::smem_bytes(p.groups)), st,
+                                          LUQ_LAUNCH_EARLY, static_cast<unsigned>(cluster), tw, tx, tz, p);
   if (e == cudaSuccess) ctx->launches += 1;
   return static_cast<int>(e);
+}
+template <int BT, bool PAIR, bool SPLIT>
+int launch_out(luq_ctx* ctx, const luq_int8_args& a, const Int8Params& p, long long units, int cluster, const CUtensorMap& tw,
+               const CUtensorMap& tz, cudaStream_t st) {
+  return a.out_bf16 ? launch<BT, PAIR, SPLIT, true>(ctx, a, p, units, cluster, tw, tz, st)
+                    : launch<BT, PAIR, SPLIT, false>(ctx, a, p, units, cluster, tw, tz, st);
 }
 
 }  // namespace
 
-int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, cudaStream_t st) {
+int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, bool early, cudaStream_t st) {
   Int8Params p{};
   p.sx = a.sx; p.sw = a.sw; p.bias = a.bias; p.offsets = a.offsets; p.z = a.z; p.ld_z = a.ld_z; p.status = ctx->d_status;
-  p.M = a.M; p.N = a.N; p.groups = a.groups; p.out_bf16 = a.out_bf16;
+  p.M = a.M; p.N = a.N; p.groups = a.groups; p.early = early;
   p.num_kb = static_cast<int>((a.K + kBk - 1) / kBk);
-  p.tiles_n = static_cast<int>((a.N + kCh - 1) / kCh);
   const int64_t esize = a.out_bf16 ? 2 : 4;
   p.z_tma = (reinterpret_cast<uintptr_t>(a.z) & 15u) == 0 && (a.ld_z * esize) % 16 == 0;
   p.tma_cols = a.N / (16 / esize) * (16 / esize);
@@ -406,11 +586,23 @@ int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, cudaStream_t st) 
   } else {
     tz = tw;                                          // not used
   }
-  // tokens a group has on average decide the tile: one tile holds them where it can
-  const long long mean_rows = (a.M + a.groups - 1) / a.groups;
-  if (mean_rows <= 16) return launch<16>(ctx, a, p, tw, tz, st);
-  if (mean_rows <= 32) return launch<32>(ctx, a, p, tw, tz, st);
-  if (mean_rows <= 64) return launch<64>(ctx, a, p, tw, tz, st);
-  if (mean_rows <= 512) return launch<128>(ctx, a, p, tw, tz, st);
-  return launch<256>(ctx, a, p, tw, tz, st);
+  // most tiles there can be: at most one partial token tile per group that has rows
+  const long long used = p.groups < a.M ? p.groups : a.M;
+  auto units = [&](int tile_rows, int tile_ch) {
+    p.tiles_n = static_cast<int>((a.N + tile_ch - 1) / tile_ch);
+    return (p.groups == 1 ? (a.M + tile_rows - 1) / tile_rows : a.M / tile_rows + used) * p.tiles_n;
+  };
+  const int sms = (ctx->sm_limit > 0 && ctx->sm_limit < ctx->sm_count) ? ctx->sm_limit : ctx->sm_count;
+  const long long mean_rows = (a.M + used - 1) / used;
+  long long n = units(256, 2 * kCh);
+  if (sms >= 2 && mean_rows >= 192 && n >= sms / 2) return launch_out<256, true, false>(ctx, a, p, n, 2, tw, tz, st);
+  n = units(128, kCh);
+  if (mean_rows > 64 && n >= sms) return launch_out<128, false, false>(ctx, a, p, n, 1, tw, tz, st);
+  const bool narrow = mean_rows <= 16;
+  n = narrow ? units(16, kCh) : units(64, kCh);
+  int split = 1;
+  while (split < 8 && n * split * 2 <= sms && split * 2 <= p.num_kb) split *= 2;
+  if (split > 1) return narrow ? launch_out<16, false, true>(ctx, a, p, n, split, tw, tz, st)
+                               : launch_out<64, false, true>(ctx, a, p, n, split, tw, tz, st);
+  return narrow ? launch_out<16, false, false>(ctx, a, p, n, 1, tw, tz, st) : launch_out<64, false, false>(ctx, a, p, n, 1, tw, tz, st);
 }
