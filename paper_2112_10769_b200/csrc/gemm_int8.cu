@@ -50,11 +50,12 @@ struct Int8Params {
   long long tma_cols;       // a store copy writes whole 16-byte pieces: boxes up to this column end on one
 };
 
-// One tile: kCh channels (twice that on a CTA pair) by up to BT tokens.  EW epilogue warps, two per quarter of
-// the lanes where a tile has more than one step of 32 tokens.
+// One tile: kCh channels (twice that on a CTA pair) by up to BT tokens.  The epilogue's warps come in groups of
+// four (one per quarter of the lanes, 32 channels each); a group takes `span` tokens of the tile.
 template <int BT, bool PAIR>
 struct Cfg {
-  static constexpr int epi_warps = BT <= 32 ? 4 : 8;
+  static constexpr int epi_warps = BT == 16 ? 4 : 8;
+  static constexpr int span = BT / (epi_warps / 4);
   static constexpr int threads = 32 * (kFirstEpiWarp + epi_warps);
   static constexpr int x_rows = PAIR ? BT / 2 : BT;               // token rows this CTA holds of a tile
   static constexpr int box_rows = BT < 32 ? BT : 32;              // token rows per copy
@@ -149,114 +150,137 @@ __device__ __forceinline__ void find_groups(const Int8Params& p, int tile_rows, 
 struct Unit {
   int group, row0, rows, ch0;
 };
-// Units walk the channel tiles in bands of kBand token tiles, tokens fastest: what runs together shares
-// both operands' tiles in L2.
-__device__ __forceinline__ Unit find_unit(long long u, const Int8Params& p, int tile_rows, int tile_ch, const int* hi,
-                                          const int* first_tile) {
-  const int token_tiles = first_tile[p.groups];
-  const long long per_band = static_cast<long long>(kBand) * p.tiles_n;
-  const int band = static_cast<int>(u / per_band);
-  const int in_band = static_cast<int>(u - band * per_band);
-  const int width = min(kBand, token_tiles - band * kBand);
-  const int c = in_band / width;
-  const int j = band * kBand + (in_band - c * width);
-  int lo = 0, up = p.groups;                       // the last group whose first tile is <= j
-  while (up - lo > 1) {
-    const int mid = (lo + up) >> 1;
-    if (first_tile[mid] <= j) lo = mid; else up = mid;
+// The tiles of one CTA (or cluster), in order.  Tiles walk the channels in bands of kBand token tiles, tokens
+// fastest: what runs together shares both operands' tiles in L2.  Every role and every epilogue warp walks for
+// itself, so a step has no division but in the last band.  (There are less than 2^31 tiles: they would need more
+// outputs than memory holds.)
+struct Walk {
+  int u, step, units, band, in_band, per_band, token_tiles;
+  __device__ __forceinline__ Walk(const Int8Params& p, int tiles, int first, int by)
+      : u(first), step(by), units(tiles * p.tiles_n), band(first / (kBand * p.tiles_n)), per_band(kBand * p.tiles_n), token_tiles(tiles) {
+    in_band = first - band * per_band;
   }
-  Unit v;
-  v.group = lo;
-  v.row0 = hi[lo] + (j - first_tile[lo]) * tile_rows;
-  v.rows = min(tile_rows, hi[lo + 1] - v.row0);
-  v.ch0 = c * tile_ch;
-  return v;
-}
+  __device__ __forceinline__ bool more() const { return u < units; }
+  __device__ __forceinline__ void next() {
+    u += step;
+    in_band += step;
+    while (in_band >= per_band) { in_band -= per_band; ++band; }
+  }
+  __device__ __forceinline__ Unit unit(const Int8Params& p, int tile_rows, int tile_ch, const int* hi, const int* first_tile) const {
+    const int width = min(kBand, token_tiles - band * kBand);
+    const int c = width == kBand ? in_band / kBand : in_band / width;
+    const int j = band * kBand + in_band - c * width;
+    int lo = 0, up = p.groups;                     // the last group whose first tile is <= j
+    while (up - lo > 1) {
+      const int mid = (lo + up) >> 1;
+      if (first_tile[mid] <= j) lo = mid; else up = mid;
+    }
+    Unit v;
+    v.group = lo;
+    v.row0 = hi[lo] + (j - first_tile[lo]) * tile_rows;
+    v.rows = min(tile_rows, hi[lo + 1] - v.row0);
+    v.ch0 = c * tile_ch;
+    return v;
+  }
+};
 
 __device__ __forceinline__ void store_z(void* z, long long at, float v, bool bf16) {
   if (bf16) static_cast<__nv_bfloat16*>(z)[at] = __float2bfloat16_rn(v);
   else static_cast<float*>(z)[at] = v;
 }
+// two products and two sums of neighbouring tokens: z = (acc * sw) * s + bias
+__device__ __forceinline__ float2 scale2(uint32_t a0, uint32_t a1, float2 sw, float2 s, float2 bias) {
+  const float2 acc = make_float2(static_cast<float>(static_cast<int>(a0)), static_cast<float>(static_cast<int>(a1)));
+  return __ffma2_rn(__fmul2_rn(acc, sw), s, bias);
+}
 
 // Takes a tile's accumulators out of tensor memory, scales them and writes them: this warp's quarter of the
-// lanes (32 channels), every second step of 32 tokens where two warps share a quarter.
-// A full step goes through a staged box [token][channel] and one copy; a step that holds rows of another
+// lanes (32 channels) and its group's span of tokens, in steps of 32.
+// A full step goes through a staged box [token][channel] and a copy; a step that holds rows of another
 // group, or an output the copies cannot address, is written element by element (32 channels in a row).
+// One fence serves all boxes a warp has (two of bf16, one of fp32).
 template <typename C, bool BF16>
-__device__ __forceinline__ void write_tile(const Int8Params& p, const void* tm_z, const Unit& v, uint32_t taddr, int warp_e,
-                                           int lane, uint32_t staging, uint8_t* gen, const float* scales, uint32_t& box_it) {
-  constexpr int CH = C::chunk, kStep = C::epi_warps / 4 * CH;
+__device__ __forceinline__ void write_tile(const Int8Params& p, const void* tm_z, const Unit& v, float sw, float bias,
+                                           uint32_t taddr, int warp_e, int lane, uint32_t staging, uint8_t* gen,
+                                           const float* scales) {
+  constexpr int CH = C::chunk, kSteps = C::span / CH, kPair = kSteps < 2 ? kSteps : 2;
   constexpr int kBoxes = BF16 ? 2 : 1, kBoxBytes = kWarpStaging / kBoxes;
   const int quarter = (warp_e + kFirstEpiWarp) & 3;
   const int ch_first = v.ch0 + quarter * 32, ch = ch_first + lane;
-  if (ch_first >= p.N) return;                         // warp-uniform
-  const bool ch_in = ch < p.N;
-  const long long wi = static_cast<long long>(v.group) * p.N + ch;
-  const float sw = ch_in ? __ldg(p.sw + wi) : 0.0f;
-  const float bias = ch_in && p.bias ? __ldg(p.bias + wi) : 0.0f;
+  const int c_first = (warp_e >> 2) * C::span;
+  if (ch_first >= p.N || c_first >= v.rows) return;    // warp-uniform
   const bool boxes = CH == 32 && p.z_tma && (ch_first + 32 <= p.N || p.tma_cols == p.N);
+  const float2 sw2 = make_float2(sw, sw), bias2 = make_float2(bias, bias);
+  const uint32_t slot = static_cast<uint32_t>(warp_e) * kWarpStaging;
+  uint8_t* const box0 = gen + C::staging + slot;
 
-  auto emit = [&](const uint32_t (&r)[CH], int c0) {
-    const int left = v.rows - c0;                      // token rows of this step that exist
-    auto value = [&](int i, float s) { return fmaf(static_cast<float>(static_cast<int>(r[i])) * sw, s, bias); };
-    if (boxes && left >= 32) {
-      const uint32_t slot = static_cast<uint32_t>(warp_e) * kWarpStaging + (box_it & (kBoxes - 1)) * kBoxBytes;
-      ++box_it;
-      if (lane == 0) bulk_wait_read<kBoxes - 1>();     // the store that last read this box is done
-      __syncwarp();
-      uint8_t* const box = gen + C::staging + slot;
+  int staged = 0, first_staged = c_first;
+  auto flush = [&]() {                                 // hands the staged boxes to the copy engine
+    fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) {
+      for (int i = 0; i < staged; ++i) tma_store_2d(tm_z, staging + slot + i * kBoxBytes, ch_first, v.row0 + first_staged + 32 * i);
+      bulk_commit();
+    }
+    staged = 0;
+  };
+#pragma unroll 1
+  for (int pair = 0; pair < kSteps && c_first + pair * CH < v.rows; pair += kPair) {
+    uint32_t r[kPair][CH];
 #pragma unroll
-      for (int i = 0; i < CH; i += 4) {
-        const float4 s4 = *reinterpret_cast<const float4*>(scales + c0 + i);
-        const float z[4] = {value(i, s4.x), value(i + 1, s4.y), value(i + 2, s4.z), value(i + 3, s4.w)};
-        if constexpr (BF16) {
-          // a lane has one channel of two tokens, a word is two channels of one: neighbours swap halves, the
-          // even lane keeps the first token's word, the odd lane the second's
+    for (int i = 0; i < kPair; ++i)
+      if (c_first + (pair + i) * CH < v.rows) load_chunk<CH>(taddr + c_first + (pair + i) * CH, r[i]);
+    tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 4; j += 2) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(z[j], z[j + 1]);
-            const uint32_t own = *reinterpret_cast<const uint32_t*>(&h);
-            const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, own, 1);
-            const uint32_t word = __byte_perm(own, other, lane & 1 ? 0x3276 : 0x5410);
-            uint8_t* const at = box + (i + j + (lane & 1)) * 64 + (lane >> 1) * 4;
-            if (smem_in(at, gen, C::staging, C::token_scales, 4, p.status)) *reinterpret_cast<uint32_t*>(at) = word;
+    for (int step = 0; step < kPair; ++step) {
+      const int c0 = c_first + (pair + step) * CH, left = v.rows - c0;
+      if (boxes && left >= 32) {
+        if (staged == 0) {                               // (first of its pair) the stores that last read this warp's boxes are done
+          if (lane == 0) bulk_wait_read<0>();
+          __syncwarp();
+        }
+        if (staged == 0) first_staged = c0;
+        uint8_t* const box = box0 + staged * kBoxBytes;
+        ++staged;
+#pragma unroll
+        for (int i = 0; i < CH; i += 4) {
+          const float4 s4 = *reinterpret_cast<const float4*>(scales + c0 + i);
+          const float2 z[2] = {scale2(r[step][i], r[step][i + 1], sw2, make_float2(s4.x, s4.y), bias2),
+                               scale2(r[step][i + 2], r[step][i + 3], sw2, make_float2(s4.z, s4.w), bias2)};
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            if constexpr (BF16) {
+              // a lane has one channel of two tokens, a word is two channels of one: neighbours swap halves, the
+              // even lane keeps the first token's word, the odd lane the second's
+              const __nv_bfloat162 h = __floats2bfloat162_rn(z[j].x, z[j].y);
+              const uint32_t own = *reinterpret_cast<const uint32_t*>(&h);
+              const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, own, 1);
+              const uint32_t word = __byte_perm(own, other, lane & 1 ? 0x3276 : 0x5410);
+              uint8_t* const at = box + (i + 2 * j + (lane & 1)) * 64 + (lane >> 1) * 4;
+              if (smem_in(at, gen, C::staging, C::token_scales, 4, p.status)) *reinterpret_cast<uint32_t*>(at) = word;
+            } else {
+              uint8_t* const at = box + (i + 2 * j) * 128 + lane * 4;
+              if (smem_in(at, gen, C::staging, C::token_scales, 132, p.status)) {
+                *reinterpret_cast<float*>(at) = z[j].x;
+                *reinterpret_cast<float*>(at + 128) = z[j].y;
+              }
+            }
           }
-        } else {
+        }
+        if (staged == kBoxes) flush();
+      } else if (left > 0 && ch < p.N) {
+        const long long z0 = (static_cast<long long>(v.row0) + c0) * p.ld_z + ch;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint8_t* const at = box + (i + j) * 128 + lane * 4;
-            if (smem_in(at, gen, C::staging, C::token_scales, 4, p.status)) *reinterpret_cast<float*>(at) = z[j];
+        for (int i = 0; i < CH; i += 2) {
+          if (i < left) {
+            const float2 z = scale2(r[step][i], r[step][i + 1], sw2, make_float2(scales[c0 + i], scales[c0 + i + 1]), bias2);
+            store_z(p.z, z0 + i * p.ld_z, z.x, BF16);
+            if (i + 1 < left) store_z(p.z, z0 + (i + 1) * p.ld_z, z.y, BF16);
           }
         }
       }
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) {
-        tma_store_2d(tm_z, staging + slot, ch_first, v.row0 + c0);
-        bulk_commit();
-      }
-    } else if (ch_in) {
-      const long long z0 = (static_cast<long long>(v.row0) + c0) * p.ld_z + ch;
-#pragma unroll
-      for (int i = 0; i < CH; ++i)
-        if (i < left) store_z(p.z, z0 + i * p.ld_z, value(i, scales[c0 + i]), BF16);
     }
-  };
-
-  // two register sets: the next step's accumulators are on their way while this one's are written
-  uint32_t r0[CH], r1[CH];
-  int c = (warp_e >> 2) * CH;
-  if (c < v.rows) load_chunk<CH>(taddr + c, r0);
-#pragma unroll 1
-  for (; c < v.rows; c += 2 * kStep) {
-    tmem_ld_wait();
-    if (c + kStep < v.rows) load_chunk<CH>(taddr + c + kStep, r1);
-    emit(r0, c);
-    if (c + kStep < v.rows) {
-      tmem_ld_wait();
-      if (c + 2 * kStep < v.rows) load_chunk<CH>(taddr + c + 2 * kStep, r0);
-      emit(r1, c + kStep);
-    }
+    if (staged) flush();
   }
 }
 
@@ -313,15 +337,15 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   else __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  // units of this cluster: every cluster-th
-  const long long units = static_cast<long long>(first_tile[p.groups]) * p.tiles_n;
-  const long long u_first = blockIdx.x / cluster, u_step = gridDim.x / cluster;
+  // the tiles of this cluster: every (number of clusters)-th
+  Walk walk(p, first_tile[p.groups], static_cast<int>(blockIdx.x / cluster), static_cast<int>(gridDim.x / cluster));
+  auto unit_of = [&](const Walk& w) { return w.unit(p, BT, PAIR ? 2 * kCh : kCh, hi, first_tile); };
   // this CTA's share of a tile's contraction
   const int kb_first = SPLIT ? static_cast<int>(static_cast<long long>(p.num_kb) * rank / cluster) : 0;
   const int kb_end = SPLIT ? static_cast<int>(static_cast<long long>(p.num_kb) * (rank + 1) / cluster) : p.num_kb;
 
   // ---- the roles, a unit at a time; state lives across units ----
-  uint32_t stage = 0, phase = 0, issued = 0, it = 0, box_it = 0;
+  uint32_t stage = 0, phase = 0, issued = 0, it = 0;
   bool ok = true, waited = !p.early;
 
   auto produce = [&](const Unit& v) {                  // one thread
@@ -412,35 +436,56 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   const int warp_e = warp - kFirstEpiWarp;
   const uint32_t lane_base = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
   auto scales_of = [&](uint32_t i) { return reinterpret_cast<float*>(gen + C::token_scales) + (i & 1u) * BT; };
-  // the tile's token scales, fetched before its accumulators are awaited; the tile two before has been
-  // written by all warps once this one meets them here
-  auto fetch_scales = [&](const Unit& v) {
+  // What a tile's epilogue needs from global memory, one tile ahead: this thread's token scale (the warps share
+  // them through shared memory) and its channel's scale and bias.
+  float s_ahead = 0.0f, sw_ahead = 0.0f, bias_ahead = 0.0f;
+  auto look_ahead = [&](const Unit& v) {
+    const int ch = v.ch0 + (warp & 3) * 32 + lane;
+    const bool ch_in = ch < p.N;
+    const long long wi = static_cast<long long>(v.group) * p.N + ch;
+    sw_ahead = ch_in ? __ldg(p.sw + wi) : 0.0f;
+    bias_ahead = ch_in && p.bias ? __ldg(p.bias + wi) : 0.0f;
     if (!waited) { pdl_wait(); waited = true; }
-    float* const s = scales_of(it);
-    for (int t = threadIdx.x - 32 * kFirstEpiWarp; t < v.rows; t += 32 * C::epi_warps) s[t] = __ldg(p.sx + v.row0 + t);
+    const int t = threadIdx.x - 32 * kFirstEpiWarp;
+    if (t < v.rows) s_ahead = __ldg(p.sx + v.row0 + t);
+  };
+  // the tile two before has been written by all warps once this one meets them here
+  auto share_scales = [&]() {
+    const int t = threadIdx.x - 32 * kFirstEpiWarp;
+    if (t < BT) scales_of(it)[t] = s_ahead;
     asm volatile("bar.sync 1, %0;" ::"n"(32 * C::epi_warps) : "memory");
   };
+  static_assert(32 * C::epi_warps >= BT, "a thread fetches one token's scale");
 
   if constexpr (!SPLIT) {
     if (warp == 0) {
       if (lane == 0) {
-        for (long long u = u_first; ok && u < units; u += u_step) produce(find_unit(u, p, BT, PAIR ? 2 * kCh : kCh, hi, first_tile));
+        for (; ok && walk.more(); walk.next()) produce(unit_of(walk));
         drain();
       }
     } else if (warp == 1) {
       if (lane == 0 && rank == 0)
-        for (long long u = u_first; ok && u < units; u += u_step, ++it) multiply(find_unit(u, p, BT, PAIR ? 2 * kCh : kCh, hi, first_tile));
+        for (; ok && walk.more(); walk.next(), ++it) multiply(unit_of(walk));
     } else {
-      for (long long u = u_first; u < units; u += u_step, ++it) {
-        Unit v = find_unit(u, p, BT, PAIR ? 2 * kCh : kCh, hi, first_tile);
-        if (PAIR) v.ch0 += static_cast<int>(rank) * kCh;
-        fetch_scales(v);
+      Unit next{};
+      auto ahead = [&]() {
+        next = unit_of(walk);
+        if (PAIR) next.ch0 += static_cast<int>(rank) * kCh;
+        look_ahead(next);
+      };
+      if (walk.more()) ahead();
+      while (walk.more()) {
+        const Unit v = next;
+        const float sw = sw_ahead, bias = bias_ahead;
+        share_scales();
+        walk.next();
+        if (walk.more()) ahead();
         const uint32_t buf = it & 1u;
         // after a wait that ran out the loop goes on without touching the tile: the warps keep meeting
         ok = ok && mbar_wait(acc_full(buf), (it >> 1) & 1u, abort_flag);
         if (ok) {
           tc_fence_after();
-          write_tile<C, BF16>(p, &tm_z, v, lane_base + buf * BT, warp_e, lane, base + C::staging, gen, scales_of(it), box_it);
+          write_tile<C, BF16>(p, &tm_z, v, sw, bias, lane_base + buf * BT, warp_e, lane, base + C::staging, gen, scales_of(it));
         }
         tc_fence_before();
         __syncwarp();
@@ -448,19 +493,21 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
           if constexpr (PAIR) mbar_arrive_cluster(mapa_shared(acc_empty(buf), 0));
           else mbar_arrive(acc_empty(buf));
         }
+        ++it;
       }
       if (lane == 0) bulk_wait<0>();   // all stores of this warp are complete before the CTA exits
     }
   } else {
     int* const partial = reinterpret_cast<int*>(gen + C::staging);      // [token][channel]
-    for (long long u = u_first; u < units; u += u_step, ++it) {
-      const Unit v = find_unit(u, p, BT, kCh, hi, first_tile);
+    for (; walk.more(); walk.next(), ++it) {
+      const Unit v = unit_of(walk);
       if (warp == 0) {
         if (lane == 0 && ok) produce(v);
       } else if (warp == 1) {
         if (lane == 0 && ok) multiply(v);
       } else {
-        fetch_scales(v);
+        look_ahead(v);
+        share_scales();
         const uint32_t buf = it & 1u;
         ok = ok && mbar_wait(acc_full(buf), (it >> 1) & 1u, abort_flag);
         tc_fence_after();
@@ -483,17 +530,14 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         // a token's 128 channels at a time, tokens dealt out over the CTAs
         const float* const s = scales_of(it);
         const int ch = v.ch0 + (warp & 3) * 32 + lane;
-        const bool ch_in = ch < p.N;
-        const long long wi = static_cast<long long>(v.group) * p.N + ch;
-        const float sw = ch_in ? __ldg(p.sw + wi) : 0.0f;
-        const float bias = ch_in && p.bias ? __ldg(p.bias + wi) : 0.0f;
         for (int t = static_cast<int>(rank) + (warp_e >> 2) * static_cast<int>(cluster); t < v.rows;
              t += static_cast<int>(cluster) * (C::epi_warps / 4)) {
           const uint32_t at = smem_u32(partial + t * kCh + (warp & 3) * 32 + lane);
           int sum = 0;
           for (uint32_t q = 0; q < cluster; ++q) sum += ld_shared_cluster(mapa_shared(at, q));
-          if (ch_in)
-            store_z(p.z, (static_cast<long long>(v.row0) + t) * p.ld_z + ch, fmaf(static_cast<float>(sum) * sw, s[t], bias), BF16);
+          if (ch < p.N)
+            store_z(p.z, (static_cast<long long>(v.row0) + t) * p.ld_z + ch,
+                    fmaf(static_cast<float>(sum) * sw_ahead, s[t], bias_ahead), BF16);
         }
       }
       cluster_sync_all();              // and has been read by all

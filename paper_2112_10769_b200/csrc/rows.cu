@@ -35,10 +35,13 @@ struct RowParams {
   long long ld_codes;
   float* scale;
   unsigned int* status;
+  bool vec_params, vec_y;   // gamma and beta, and the rows of y, are 16-byte aligned
 };
 
 __device__ __forceinline__ float load1(const float* p) { return __ldg(p); }
 __device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float load1_any(const float* p) { return *p; }              // shared or global memory
+__device__ __forceinline__ float load1_any(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
@@ -76,20 +79,28 @@ __device__ __forceinline__ void finish_stats(float d1, float d2, float eps, floa
   rstd = rsqrtf(var + eps);
 }
 
-// Factor and scale of a row with the maximum |v| whose bit pattern is `top` (NaN patterns are above
-// Inf's, Inf's above every number's).  Inf/NaN: zero codes and a NaN scale, so that what is made of the row is NaN
-// and of the others is not; a maximum below 2^-100 (127 / max would overflow): zero codes, zero scale.
-__device__ __forceinline__ float row_factor(unsigned int top, float& scale, unsigned int& flags) {
-  const float m = __uint_as_float(top);
-  if (top >= 0x7F800000u) { scale = __uint_as_float(0x7FC00000u); flags = LUQ_STATUS_NONFINITE; return 0.0f; }
-  if (m < 0x1p-100f) { scale = 0.0f; flags = top ? LUQ_STATUS_RANGE : 0u; return 0.0f; }
-  scale = __fdiv_rn(m, 127.0f);
-  flags = 0u;
-  return __fdiv_rn(127.0f, m);
+// What a row whose maximum |v| has the bit pattern `top` is multiplied with (NaN patterns are above Inf's, Inf's
+// above every number's).  Zero: all codes are zero - a row of zeros; a row with Inf or NaN, which gets a NaN
+// scale, so that what is made of it is NaN and of the others is not; a maximum below 2^-100, where 127 / max would
+// overflow, which gets a zero scale.
+__device__ __forceinline__ float row_factor(unsigned int top) {
+  return top >= 0x7F800000u || top < 0x0D800000u ? 0.0f : __fdiv_rn(127.0f, __uint_as_float(top));
 }
-__device__ __forceinline__ int quantize1(float v, float factor) {
-  // a zero factor also serves rows that hold Inf or NaN: their products are not looked at
-  return factor == 0.0f ? 0 : __float2int_rn(__fmul_rn(v, factor));
+__device__ __forceinline__ void store_scale(unsigned int top, float* scale, unsigned int* status) {
+  const bool bad = top >= 0x7F800000u, tiny = top < 0x0D800000u;   // 2^-100
+  *scale = bad ? __uint_as_float(0x7FC00000u) : tiny ? 0.0f : __fdiv_rn(__uint_as_float(top), 127.0f);
+  if (bad || (tiny && top)) atomicOr(status, bad ? LUQ_STATUS_NONFINITE : LUQ_STATUS_RANGE);
+}
+// max(a, |b|), NaN if either is
+__device__ __forceinline__ float max_abs(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+  return r;
+}
+// rint(v * factor) in the low byte: the sum's last mantissa bit is worth 1, so it is rounded to the nearest whole
+// number, ties to even, and holds it in two's complement (|v * factor| <= 127)
+__device__ __forceinline__ uint32_t quantize1(float v, float factor) {
+  return __float_as_uint(__fadd_rn(__fmul_rn(v, factor), 12582912.0f));
 }
 
 // Any width, any alignment: one block per row, the row is read again for every pass (from L2).  Serves the
@@ -135,24 +146,28 @@ __global__ void __launch_bounds__(512) row_loop_kernel(const RowParams p) {
       unsigned int top = 0u;
       for (int c = threadIdx.x; c < C; c += blockDim.x) top = max(top, __float_as_uint(value(c)) & 0x7FFFFFFFu);
       top = block_max(top, reinterpret_cast<unsigned int*>(box));
-      float scale;
-      unsigned int flags;
-      const float factor = row_factor(top, scale, flags);
+      const float factor = row_factor(top);
       int8_t* const q = p.codes + r * p.ld_codes;
-      for (int c = threadIdx.x; c < C; c += blockDim.x) q[c] = static_cast<int8_t>(quantize1(value(c), factor));
-      if (threadIdx.x == 0) {
-        p.scale[r] = scale;
-        if (flags) atomicOr(p.status, flags);
-      }
+      for (int c = threadIdx.x; c < C; c += blockDim.x) q[c] = factor == 0.0f ? 0 : static_cast<int8_t>(quantize1(value(c), factor));
+      if (threadIdx.x == 0) store_scale(top, p.scale + r, p.status);
     }
   }
 }
 
 // ---- rows held in registers ----------------------------------------------------------------------------
-// A thread holds EPT elements of a row in pieces of 16 bytes, piece j at (thread + j * threads) * V: one pass
-// over memory.  Where rows do not start at multiples of 16 bytes (VEC false) a warp moves the same 512 bytes
-// element by element, coalesced, through 512 bytes of shared memory: every element has the same owner, so
-// sums are made in the same order and results do not depend on strides and alignment.
+// A group of G threads takes a row: G = 1 .. 32 lanes of a warp (NARROW, rows up to 512 elements: several rows per
+// warp), or several warps.  A thread holds EPT elements in pieces of 16 bytes, piece j at (thread + j * G) * V, so
+// a row is read once; 16 of them share what a row costs beside its elements (reductions, divisions, loop).
+// How the pieces get there:
+//   kRing    many wide rows: every group has a ring of whole rows in shared memory, filled by bulk copies several
+//            rows ahead - what an SM can stream is the bytes it has in flight, and registers hold too few.  Rows
+//            that start inside a 16-byte piece are copied with the pieces around them and shifted into place.
+//   kDirect  16-byte loads into registers, one row ahead
+//   kBounce  the same for rows that do not start at multiples of 16 bytes: element by element, coalesced,
+//            and through 512 bytes of shared memory per warp to their owners
+// An element has the same owner in all three, and sums are made in the same order: results do not depend on
+// strides, alignment or the number of rows.
+constexpr int kRing = 0, kDirect = 1, kBounce = 2;
 
 template <typename T>
 struct Piece {
@@ -182,62 +197,13 @@ __device__ __forceinline__ uint4 pack(const float* v, const __nv_bfloat16*) {
 __device__ __forceinline__ float zero_of(const float*) { return 0.0f; }
 __device__ __forceinline__ __nv_bfloat16 zero_of(const __nv_bfloat16*) { return __float2bfloat16_rn(0.0f); }
 
-// elements c .. c + V - 1 of a row of `cols`, zero beyond its end; `wbuf`: the warp's 32 x 16 bytes (VEC false).
-// All lanes of a warp call it, with consecutive pieces.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load_piece(const T* row, int c, int cols, uint4* wbuf, float* v) {
-  constexpr int V = Piece<T>::V;
-  if constexpr (VEC) {
-    if (c + V <= cols) {
-      unpack(__ldg(reinterpret_cast<const uint4*>(row + c)), row, v);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = c + i < cols ? load1(row + c + i) : 0.0f;
-    }
-  } else {
-    const int lane = threadIdx.x & 31, c0 = c - lane * V;
-    T* const b = reinterpret_cast<T*>(wbuf);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int e = i * 32 + lane;
-      b[e] = c0 + e < cols ? row[c0 + e] : zero_of(row);
-    }
-    __syncwarp();
-    unpack(wbuf[lane], row, v);
-    __syncwarp();
-  }
-}
-template <typename T, bool VEC>
-__device__ __forceinline__ void store_piece(T* row, int c, int cols, uint4* wbuf, const float* v) {
-  constexpr int V = Piece<T>::V;
-  if constexpr (VEC) {
-    if (c + V <= cols) {
-      *reinterpret_cast<uint4*>(row + c) = pack(v, row);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (c + i < cols) store1(row + c + i, v[i]);
-    }
-  } else {
-    const int lane = threadIdx.x & 31, c0 = c - lane * V;
-    const T* const b = reinterpret_cast<const T*>(wbuf);
-    wbuf[lane] = pack(v, row);
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int e = i * 32 + lane;
-      if (c0 + e < cols) row[c0 + e] = b[e];
-    }
-    __syncwarp();
-  }
-}
-// V parameters, `other` where there are none
-template <int V, bool VEC>
-__device__ __forceinline__ void load_params(const float* g, int c, int cols, float other, float* v) {
-  if (g == nullptr) {
+// V parameters, `other` where there are none; `vec`: 16-byte aligned
+template <int V, bool FULL>
+__device__ __forceinline__ void load_params(const float* g, bool vec, int c, int cols, float other, float* v) {
+  if (!FULL && g == nullptr) {
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = other;
-  } else if (VEC && c + V <= cols) {
+  } else if (FULL || (vec && c + V <= cols)) {
 #pragma unroll
     for (int i = 0; i < V; i += 4) {
       const float4 f = __ldg(reinterpret_cast<const float4*>(g + c + i));
@@ -249,124 +215,421 @@ __device__ __forceinline__ void load_params(const float* g, int c, int cols, flo
   }
 }
 
-// sums and maxima over the threads of a row: a warp (WARP), or the block
-template <bool WARP>
-__device__ __forceinline__ float row_sum(float v, float* box) {
-  v = warp_sum(v);
-  if (WARP) return v;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  if (lane == 0) box[warp] = v;
-  __syncthreads();
-  return warp_sum(lane < warps ? box[lane] : 0.0f);
-}
-template <bool WARP>
-__device__ __forceinline__ float2 row_sum2(float a, float b, float2* box) {
-  a = warp_sum(a);
-  b = warp_sum(b);
-  if (WARP) return make_float2(a, b);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  if (lane == 0) box[warp] = make_float2(a, b);
-  __syncthreads();
-  const float2 v = lane < warps ? box[lane] : make_float2(0.0f, 0.0f);
-  return make_float2(warp_sum(v.x), warp_sum(v.y));
-}
-template <bool WARP>
-__device__ __forceinline__ unsigned int row_max(unsigned int v, unsigned int* box) {
-  v = __reduce_max_sync(0xFFFFFFFFu, v);
-  if (WARP) return v;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  if (lane == 0) box[warp] = v;
-  __syncthreads();
-  return __reduce_max_sync(0xFFFFFFFFu, lane < warps ? box[lane] : 0u);
+// A group, its barrier, and sums and maxima over its threads, with the result in all of them.  `box` has slots for
+// each warp of the group; consecutive reductions of a group use different boxes, so each costs one barrier.
+template <bool NARROW>
+struct Group {
+  int index, tid, G, warps;
+  __device__ __forceinline__ explicit Group(int threads) : G(threads) {
+    index = threadIdx.x / G;
+    tid = threadIdx.x - index * G;
+    warps = NARROW ? 1 : G >> 5;
+  }
+  __device__ __forceinline__ void sync() const { asm volatile("bar.sync %0, %1;" ::"r"(1 + index), "r"(G) : "memory"); }
+  __device__ __forceinline__ int sub() const { return NARROW ? (threadIdx.x & 31) / G : 0; }   // row within the warp
+  __device__ __forceinline__ float sum(float v, float* box) const {
+    if constexpr (NARROW) {
+      for (int o = G >> 1; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+      return v;
+    }
+    const int lane = threadIdx.x & 31;
+    v = warp_sum(v);
+    if (lane == 0) box[tid >> 5] = v;
+    sync();
+    v = (lane & 15) < warps ? box[lane & 15] : 0.0f;
+#pragma unroll
+    for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+  }
+  // two sums; over whole warps for the price of one: after the first exchange the lower half of the lanes carries
+  // a, the upper b
+  __device__ __forceinline__ float2 sum2(float a, float b, float* box) const {
+    if constexpr (NARROW) {
+      for (int o = G >> 1; o; o >>= 1) {
+        a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+        b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
+      }
+      return make_float2(a, b);
+    }
+    const int lane = threadIdx.x & 31;
+    const bool upper = lane & 16;
+    float v = (upper ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, upper ? a : b, 16);
+#pragma unroll
+    for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    if ((lane & 15) == 0) box[2 * (tid >> 5) + (lane >> 4)] = v;
+    sync();
+    v = (lane & 15) < warps ? box[2 * (lane & 15) + (lane >> 4)] : 0.0f;
+#pragma unroll
+    for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    const float other = __shfl_xor_sync(0xFFFFFFFFu, v, 16);
+    return upper ? make_float2(other, v) : make_float2(v, other);
+  }
+  __device__ __forceinline__ unsigned int max(unsigned int v, unsigned int* box) const {
+    if constexpr (NARROW) {
+      for (int o = G >> 1; o; o >>= 1) {
+        const unsigned int w = __shfl_xor_sync(0xFFFFFFFFu, v, o);
+        v = v > w ? v : w;
+      }
+      return v;
+    }
+    v = __reduce_max_sync(0xFFFFFFFFu, v);
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) box[tid >> 5] = v;
+    sync();
+    return __reduce_max_sync(0xFFFFFFFFu, lane < warps ? box[lane] : 0u);
+  }
+};
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar) : "memory");
 }
 
-template <typename T, int MODE, int EPT, bool VEC, bool WARP>
-__global__ void __launch_bounds__(WARP ? 256 : 512) row_kernel(const RowParams p) {
-  constexpr int V = Piece<T>::V, VPT = EPT / V;
-  // one box per reduction of a row, so that a row costs one barrier per reduction; the next row's first write to
-  // a box comes after a later barrier than the last read of it
-  __shared__ float sum_box[16];
-  __shared__ float2 sum2_box[16];
-  __shared__ unsigned int max_box[2][16];
-  __shared__ uint4 move[VEC ? 1 : (WARP ? 8 : 16)][32];
-  uint4* const wbuf = move[VEC ? 0 : threadIdx.x >> 5];
-  pdl_wait();
-  pdl_trigger();
-  const int C = p.cols;
-  const int G = WARP ? 32 : static_cast<int>(blockDim.x);
-  const int tid = WARP ? static_cast<int>(threadIdx.x & 31) : static_cast<int>(threadIdx.x);
-  const long long first = WARP ? static_cast<long long>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
-  const long long step = WARP ? static_cast<long long>(gridDim.x) * (blockDim.x >> 5) : gridDim.x;
-  const float inv_c = 1.0f / C;
-  int parity = 0;
-  for (long long r = first; r < p.rows; r += step, parity ^= 1) {
-    const T* const x = static_cast<const T*>(p.x) + r * p.ld_x;
-    float v[EPT];
+// The rows of one to two tensors on their way into a group's registers.
+//   start(r)   before the first row, after the wait for the preceding kernel
+//   take(r, v) row r's elements, zero beyond its end; rows come in the order first, first + step, ...
+//   release(r) kRing: once every thread of the group has taken row r (a barrier lies between), the stage is
+//              filled again
+// kRing waits are bounded; when one runs out the group goes on without writing anything (ok() is false), so that
+// its barriers still meet, and finish() waits for the copies under way and raises the status.
+template <typename T, int TENSORS, int EPT, int LOAD, bool FULL, bool NARROW>
+struct Rows {
+  static constexpr int V = Piece<T>::V, VPT = EPT / V;
+  const T* base[2];
+  long long ld[2];
+  long long rows, step;
+  int cols, tid, G;
+  // kRing
+  uint32_t bars = 0, data = 0, phase = 0;
+  uint8_t* held = nullptr;
+  int depth = 0, row_bytes = 0, stage = 0, issued = 0;
+  volatile uint32_t* abort_flag = nullptr;
+  bool fine = true;
+  // kDirect, kBounce: the next row, as it lies in memory or element by element
+  uint4 raw[TENSORS][LOAD == kDirect ? VPT : 1];
+  T single[TENSORS][LOAD == kBounce ? EPT : 1];
+  uint4* wbuf = nullptr;
+
+  static int ring_row_bytes(int cols) { return (cols * static_cast<int>(sizeof(T)) + 32 + 127) / 128 * 128; }
+  // shared memory of a block's rings: [groups][depth] barriers, the abort word, then [groups][depth][TENSORS] rows
+  static int ring_head(int groups, int depth) { return (groups * depth * 8 + 4 + 127) / 128 * 128; }
+  static int ring_bytes(int groups, int depth, int cols) {
+    return ring_head(groups, depth) + groups * depth * TENSORS * ring_row_bytes(cols);
+  }
+
+  __device__ __forceinline__ void init_ring(uint8_t* smem, int groups, int group, int n) {   // all threads; a barrier follows
+    depth = n;
+    row_bytes = (cols * static_cast<int>(sizeof(T)) + 32 + 127) / 128 * 128;
+    const int head = (groups * depth * 8 + 4 + 127) / 128 * 128;
+    bars = smem_u32(smem) + group * depth * 8;
+    abort_flag = reinterpret_cast<volatile uint32_t*>(smem + groups * depth * 8);
+    held = smem + head + group * depth * TENSORS * row_bytes;
+    data = smem_u32(held);
+    if (tid == 0)
+      for (int s = 0; s < depth; ++s) mbar_init(bars + 8 * s, 1);
+    if (threadIdx.x == 0) *abort_flag = 0;
+    fence_barrier_init();
+  }
+  // A row's bytes lie at (address & 15) in its stage.  Rows at the tensor's ends are copied without the pieces that
+  // reach beyond it (take() fetches such a row element by element).
+  __device__ __forceinline__ void fill(int s, long long r) {
+    const int bytes = cols * static_cast<int>(sizeof(T));
+    uint32_t total = 0, lo[TENSORS], n[TENSORS];
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) load_piece<T, VEC>(x, (tid + j * G) * V, C, wbuf, v + j * V);
-    if (MODE != kInt8) {
-      float s = 0.0f;
+    for (int t = 0; t < TENSORS; ++t) {
+      const uint32_t m = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base[t] + r * ld[t]) & 15u);
+      lo[t] = r == 0 && m ? 16u : 0u;
+      n[t] = (r + 1 < rows ? (m + bytes + 15u) & ~15u : (m + bytes) & ~15u) - lo[t];
+      total += n[t];
+    }
+    mbar_arrive_expect_tx(bars + 8 * s, total);
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) s += v[i];
-      const float mean0 = row_sum<WARP>(s, sum_box) * inv_c;
-      float s1 = 0.0f, s2 = 0.0f;
+    for (int t = 0; t < TENSORS; ++t) {
+      const uintptr_t from = reinterpret_cast<uintptr_t>(base[t] + r * ld[t]) & ~static_cast<uintptr_t>(15);
+      bulk_load(data + (s * TENSORS + t) * row_bytes + lo[t], reinterpret_cast<const void*>(from + lo[t]), n[t], bars + 8 * s);
+    }
+    ++issued;
+  }
+  // elements c .. c + V - 1 of tensor t's row in the present stage, m = the row's address & 15
+  __device__ __forceinline__ void ring_piece(int t, uint32_t m, int c, float* v) const {
+    const uint4* const q = reinterpret_cast<const uint4*>(held + (stage * TENSORS + t) * row_bytes) + c / V;
+    const uint4 a = q[0];
+    if (FULL || m == 0) { unpack(a, base[0], v); return; }
+    const uint4 b = q[1];
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (m & 8) {
 #pragma unroll
-      for (int j = 0; j < VPT; ++j) {
-        const int left = C - (tid + j * G) * V;          // elements of this piece that exist
+      for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (m & 4) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float d = i < left ? v[j * V + i] - mean0 : 0.0f;
-          v[j * V + i] = d;
-          s1 += d;
-          s2 = fmaf(d, d, s2);
+      for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    if (m & 2) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+    unpack(make_uint4(w[0], w[1], w[2], w[3]), base[0], v);
+  }
+  __device__ __forceinline__ uint32_t skew(int t, long long r) const {
+    return FULL ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base[t] + r * ld[t]) & 15u);
+  }
+  // a row whose stage lacks elements that lie at the tensor's ends
+  __device__ __forceinline__ bool at_end(int t, long long r) const {
+    const uint32_t m = skew(t, r);
+    return !FULL && ((r == 0 && m) || (r + 1 == rows && ((m + cols * sizeof(T)) & 15u)));
+  }
+  __device__ __forceinline__ void fetch(long long r) {
+#pragma unroll
+    for (int t = 0; t < TENSORS; ++t) {
+      const T* const row = base[t] + r * ld[t];
+      if constexpr (LOAD == kDirect) {
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+          const int c = (tid + j * G) * V;
+          raw[t][j] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < rows) {
+            if (FULL || c + V <= cols) {
+              raw[t][j] = __ldg(reinterpret_cast<const uint4*>(row + c));
+            } else {
+              float v[V];
+#pragma unroll
+              for (int i = 0; i < V; ++i) v[i] = c + i < cols ? load1(row + c + i) : 0.0f;
+              raw[t][j] = pack(v, row);                // exact: the values are of type T
+            }
+          }
+        }
+      } else if constexpr (LOAD == kBounce) {
+        const int width = NARROW ? G : 32, l = threadIdx.x & (width - 1);
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+          const int c0 = (tid - l + j * G) * V;          // the lanes' common range of elements
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const int c = c0 + i * width + l;
+            single[t][j * V + i] = r < rows && c < cols ? row[c] : zero_of(row);
+          }
         }
       }
-      const float2 t = row_sum2<WARP>(s1, s2, sum2_box);
+    }
+  }
+  __device__ __forceinline__ void start(long long first) {
+    if constexpr (LOAD == kRing) {
+      if (tid == 0)
+        for (int s = 0; s < depth; ++s)
+          if (first + s * step < rows) fill(s, first + s * step);
+    } else {
+      fetch(first);
+    }
+  }
+  // (in a narrow group's warp, r may lie beyond the rows)
+  __device__ __forceinline__ void take(long long r, float (*v)[EPT]) {
+    if constexpr (LOAD == kRing) {
+      fine = fine && mbar_wait(bars + 8 * stage, phase, abort_flag);
+#pragma unroll
+      for (int t = 0; t < TENSORS; ++t) {
+        const uint32_t m = skew(t, r);
+        if (at_end(t, r)) {
+          const T* const row = base[t] + r * ld[t];
+#pragma unroll
+          for (int j = 0; j < VPT; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+              const int c = (tid + j * G) * V + i;
+              v[t][j * V + i] = c < cols ? load1(row + c) : 0.0f;
+            }
+        } else {
+#pragma unroll
+          for (int j = 0; j < VPT; ++j) {
+            const int c = (tid + j * G) * V;
+            if (FULL || c < cols) ring_piece(t, m, c, v[t] + j * V);
+            if (!FULL && c + V > cols) {
+#pragma unroll
+              for (int i = 0; i < V; ++i)
+                if (c + i >= cols) v[t][j * V + i] = 0.0f;
+            }
+          }
+        }
+      }
+    } else if constexpr (LOAD == kDirect) {
+#pragma unroll
+      for (int t = 0; t < TENSORS; ++t)
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) unpack(raw[t][j], base[0], v[t] + j * V);
+      fetch(r + step);
+    } else {
+      const int lane = threadIdx.x & 31, width = NARROW ? G : 32, l = lane & (width - 1);
+      T* const b = reinterpret_cast<T*>(wbuf) + (lane - l) * V;
+#pragma unroll
+      for (int t = 0; t < TENSORS; ++t)
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) b[i * width + l] = single[t][j * V + i];
+          __syncwarp();
+          unpack(wbuf[lane], base[0], v[t] + j * V);
+          __syncwarp();
+        }
+      fetch(r + step);
+    }
+  }
+  __device__ __forceinline__ void release(long long r) {
+    if constexpr (LOAD == kRing) {
+      const long long next = r + depth * step;
+      if (tid == 0 && next < rows) fill(stage, next);
+      if (++stage == depth) { stage = 0; phase ^= 1u; }
+    }
+  }
+  __device__ __forceinline__ bool ok() const { return LOAD != kRing || fine; }
+  __device__ __forceinline__ void finish(unsigned int* status) const {
+    if constexpr (LOAD == kRing) {
+      if (tid != 0 || !*abort_flag) return;
+      for (int s = 0; s < depth; ++s)
+        if (issued > s) mbar_wait(bars + 8 * s, ((issued - 1 - s) / depth) & 1u, abort_flag);
+      atomicOr(status, LUQ_STATUS_TIMEOUT);
+    }
+  }
+};
+
+// writes V elements of a row; `vec`: the row starts at a multiple of 16 bytes (else through the warp's 512 bytes)
+template <typename T, bool FULL, bool NARROW>
+__device__ __forceinline__ void store_piece(T* row, bool exists, bool vec, int tid, int G, int j, int cols, uint4* wbuf,
+                                            const float* v) {
+  constexpr int V = Piece<T>::V;
+  const int c = (tid + j * G) * V;
+  if (FULL || vec) {
+    if (!exists) return;
+    if (FULL || c + V <= cols) {
+      *reinterpret_cast<uint4*>(row + c) = pack(v, row);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (c + i < cols) store1(row + c + i, v[i]);
+    }
+  } else {
+    const int lane = threadIdx.x & 31, width = NARROW ? G : 32, l = lane & (width - 1);
+    const T* const b = reinterpret_cast<const T*>(wbuf) + (lane - l) * V;
+    const int c0 = (tid - l + j * G) * V;
+    wbuf[lane] = pack(v, row);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (exists && c0 + i * width + l < cols) row[c0 + i * width + l] = b[i * width + l];
+    __syncwarp();
+  }
+}
+
+// FULL: every thread has EPT elements, and all is aligned and there: no test per piece (a third of the instructions)
+template <typename T, int MODE, int EPT, int LOAD, bool FULL, bool NARROW>
+__global__ void __launch_bounds__(512, EPT == 16 ? 2 : 1) row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
+  constexpr int V = Piece<T>::V, VPT = EPT / V;
+  // one box per reduction of a row; without the norm a row has one reduction only and uses two in turn
+  __shared__ float sum_box[16];
+  __shared__ float sum2_box[32];
+  __shared__ unsigned int max_box[2][16];
+  __shared__ uint4 move[FULL ? 1 : 16][32];
+  extern __shared__ __align__(128) uint8_t ring_smem[];
+  const Group<NARROW> g(threads_per_row);
+  const int groups = blockDim.x / g.G, slot = g.index * g.warps, tid = g.tid, G = g.G, C = p.cols;
+  uint4* const wbuf = move[FULL ? 0 : threadIdx.x >> 5];
+  Rows<T, 1, EPT, LOAD, FULL, NARROW> in;
+  in.base[0] = static_cast<const T*>(p.x); in.ld[0] = p.ld_x; in.rows = p.rows; in.cols = C; in.tid = tid; in.G = G;
+  in.step = static_cast<long long>(gridDim.x) * groups;
+  in.wbuf = wbuf;
+  if constexpr (LOAD == kRing) {
+    in.init_ring(ring_smem, groups, g.index, ring_depth);
+    __syncthreads();
+  }
+  pdl_wait();
+  pdl_trigger();
+  const long long first = static_cast<long long>(blockIdx.x) * groups + g.index;
+  in.start(first);
+  if (LOAD != kRing && MODE != kInt8) {                // few rows: the parameters arrive with the row
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      const int c = (tid + j * G) * V;
+      if (c < C && p.gamma) asm volatile("prefetch.global.L1 [%0];" ::"l"(p.gamma + c));
+      if (c < C && p.beta) asm volatile("prefetch.global.L1 [%0];" ::"l"(p.beta + c));
+    }
+  }
+  const float inv_c = 1.0f / C;
+  int parity = 0;
+  for (long long r = first; r - g.sub() < p.rows; r += in.step, parity ^= 1) {
+    float row[1][EPT];
+    in.take(r, row);
+    float (&v)[EPT] = row[0];
+    const bool exists = in.ok() && (!NARROW || r < p.rows);
+    if (MODE != kInt8) {
+      // four strands of additions: a single one would be as long as the loads
+      float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) s[i & 3] += v[i];
+      const float mean0 = g.sum((s[0] + s[1]) + (s[2] + s[3]), sum_box + slot) * inv_c;
+      in.release(r);
+      float s1[2] = {0.0f, 0.0f}, s2[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        const int c = (tid + j * G) * V;
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[j * V + i] -= mean0;
+        if (!FULL && c + V > C) {                        // elements that do not exist
+#pragma unroll
+          for (int i = 0; i < V; ++i)
+            if (c + i >= C) v[j * V + i] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          s1[i & 1] += v[j * V + i];
+          s2[i & 1] = fmaf(v[j * V + i], v[j * V + i], s2[i & 1]);
+        }
+      }
+      const float2 t = g.sum2(s1[0] + s1[1], s2[0] + s2[1], sum2_box + 2 * slot);
       float shift, rstd;
       finish_stats(t.x * inv_c, t.y * inv_c, p.eps, mean0, shift, rstd);
+      const float minus = -shift * rstd;
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
         const int c = (tid + j * G) * V;
         float w[V], b[V];
-        load_params<V, VEC>(p.gamma, c, C, 1.0f, w);
-        load_params<V, VEC>(p.beta, c, C, 0.0f, b);
+        load_params<V, FULL>(p.gamma, p.vec_params, c, C, 1.0f, w);
+        load_params<V, FULL>(p.beta, p.vec_params, c, C, 0.0f, b);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[j * V + i] = fmaf((v[j * V + i] - shift) * rstd, w[i], b[i]);
-        if (MODE == kNorm) store_piece<T, VEC>(static_cast<T*>(p.y) + r * p.ld_y, c, C, wbuf, v + j * V);
+        for (int i = 0; i < V; ++i) v[j * V + i] = fmaf(fmaf(v[j * V + i], rstd, minus), w[i], b[i]);
+        if (MODE == kNorm) store_piece<T, FULL, NARROW>(static_cast<T*>(p.y) + r * p.ld_y, exists, p.vec_y, tid, G, j, C, wbuf, v + j * V);
+        if (MODE != kNorm && !FULL && c + V > C) {
+#pragma unroll
+          for (int i = 0; i < V; ++i)
+            if (c + i >= C) v[j * V + i] = 0.0f;
+        }
       }
-      if (MODE == kNorm && tid == 0) {
+      if (MODE == kNorm && tid == 0 && exists) {
         if (p.mean) p.mean[r] = mean0 + shift;
         if (p.rstd) p.rstd[r] = rstd;
       }
     }
     if (MODE != kNorm) {
-      unsigned int top = 0u;
+      float m[2] = {0.0f, 0.0f};
 #pragma unroll
-      for (int j = 0; j < VPT; ++j) {
-        const int left = C - (tid + j * G) * V;
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (i < left) top = max(top, __float_as_uint(v[j * V + i]) & 0x7FFFFFFFu);
-      }
-      // (without the norm this is the only reduction of a row: two boxes in turn)
-      top = row_max<WARP>(top, max_box[parity]);
-      float scale;
-      unsigned int flags;
-      const float factor = row_factor(top, scale, flags);
+      for (int i = 0; i < EPT; ++i) m[i & 1] = max_abs(m[i & 1], v[i]);
+      const unsigned int top = g.max(__float_as_uint(max_abs(m[0], m[1])), max_box[parity] + slot);
+      if (MODE == kInt8) in.release(r);
+      const float factor = row_factor(top);
       int8_t* const q = p.codes + r * p.ld_codes;
+      if (factor == 0.0f) {                              // products with Inf and NaN are not looked at
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) v[i] = 0.0f;
+      }
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
         const int c = (tid + j * G) * V;
-        uint32_t word[V / 4];                       // codes' rows always start at multiples of 16 bytes
+        uint32_t word[V / 4];                            // codes' rows always start at multiples of 16 bytes
 #pragma unroll
-        for (int i = 0; i < V; i += 4) {
-          const uint32_t a = static_cast<uint32_t>(quantize1(v[j * V + i], factor)) & 0xFFu;
-          const uint32_t b = static_cast<uint32_t>(quantize1(v[j * V + i + 1], factor)) & 0xFFu;
-          const uint32_t d = static_cast<uint32_t>(quantize1(v[j * V + i + 2], factor)) & 0xFFu;
-          const uint32_t e = static_cast<uint32_t>(quantize1(v[j * V + i + 3], factor)) & 0xFFu;
-          word[i / 4] = a | (b << 8) | (d << 16) | (e << 24);
-        }
-        if (c + V <= C) {
+        for (int i = 0; i < V; i += 4)
+          word[i / 4] = __byte_perm(__byte_perm(quantize1(v[j * V + i], factor), quantize1(v[j * V + i + 1], factor), 0x0040),
+                                    __byte_perm(quantize1(v[j * V + i + 2], factor), quantize1(v[j * V + i + 3], factor), 0x0040),
+                                    0x5410);
+        if (!exists) continue;
+        if (FULL || c + V <= C) {
           if constexpr (V == 8) *reinterpret_cast<uint2*>(q + c) = make_uint2(word[0], word[1]);
           else *reinterpret_cast<uint32_t*>(q + c) = word[0];
         } else {
@@ -375,12 +638,10 @@ __global__ void __launch_bounds__(WARP ? 256 : 512) row_kernel(const RowParams p
             if (c + i < C) q[c + i] = static_cast<int8_t>(word[i / 4] >> (8 * (i & 3)));
         }
       }
-      if (tid == 0) {
-        p.scale[r] = scale;
-        if (flags) atomicOr(p.status, flags);
-      }
+      if (tid == 0 && exists) store_scale(top, p.scale + r, p.status);
     }
   }
+  in.finish(p.status);
 }
 
 struct NormBwdParams {
@@ -396,6 +657,8 @@ struct NormBwdParams {
   float* partial;        // workspace: [chunks][2][cols] partial dgamma / dbeta
   int chunks;
   long long rows_per_chunk;
+  unsigned int* status;
+  bool vec_gamma, vec_dx;
 };
 
 // mean_c(g) and mean_c(g xhat) of every row
@@ -448,108 +711,183 @@ __global__ void __launch_bounds__(256) norm_bwd_columns_kernel(const NormBwdPara
   p.partial[(2 * chunk + 1) * p.cols + c] = dbeta;
 }
 
-// Rows in registers: a block is several groups of G threads, a group takes every gridDim.x * groups-th row
-// and keeps its columns' sums of dgamma and dbeta in registers over all of them; at the end the block adds its
-// groups' sums (in order, through shared memory) into one row of partial sums.  One pass over x and dy; the
-// next row's pieces are loaded before this row's reduction waits.
-template <typename T, int EPT, bool VEC>
-__global__ void __launch_bounds__(1024) norm_bwd_kernel(const NormBwdParams p, int G) {
+// Rows in registers: a group takes every gridDim.x * groups-th row and keeps its columns' sums of dgamma and
+// dbeta in registers over all of them; at the end the block adds its groups' sums (in order) into one row of partial
+// sums.  One pass over x and dy.  Rows wider than 8192 elements (EPT 32: 64 sums a thread leave no room for the row)
+// stay in the ring's stage and are read from there twice.
+template <typename T, int EPT, int LOAD, bool FULL, bool NARROW>
+__global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, int threads_per_row, int ring_depth) {
   constexpr int V = Piece<T>::V, VPT = EPT / V;
-  __shared__ float2 box[2][32];
-  __shared__ uint4 move[VEC ? 1 : 32][32];
-  extern __shared__ float sums[];                    // [2][cols], only with more than one group
+  constexpr bool TWICE = EPT == 32;
+  static_assert(!TWICE || LOAD == kRing, "a row that is read twice stays in the ring");
+  __shared__ float box[2][32];
+  __shared__ uint4 move[FULL ? 1 : 16][32];
+  extern __shared__ __align__(128) uint8_t ring_smem[];   // the ring; at the end [2][cols] sums
+  const Group<NARROW> g(threads_per_row);
+  const int groups = blockDim.x / g.G, group = g.index, slot = g.index * g.warps, tid = g.tid, G = g.G, C = p.cols;
+  uint4* const wbuf = move[FULL ? 0 : threadIdx.x >> 5];
+  Rows<T, 2, TWICE ? V : EPT, LOAD, FULL, NARROW> in;
+  in.base[0] = static_cast<const T*>(p.x); in.ld[0] = p.ld_x;
+  in.base[1] = static_cast<const T*>(p.dy); in.ld[1] = p.ld_dy;
+  in.rows = p.rows; in.cols = C; in.tid = tid; in.G = G; in.wbuf = wbuf;
+  in.step = static_cast<long long>(gridDim.x) * groups;
+  if constexpr (LOAD == kRing) {
+    in.init_ring(ring_smem, groups, group, ring_depth);
+    __syncthreads();
+  }
   pdl_wait();
   pdl_trigger();
-  const int C = p.cols;
-  const int groups = blockDim.x / G, group = threadIdx.x / G, tid = threadIdx.x - group * G;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int warps = G >> 5, first_warp = group * warps;
-  uint4* const wbuf = move[VEC ? 0 : warp];
-  const long long step = static_cast<long long>(gridDim.x) * groups;
+  const long long first = static_cast<long long>(blockIdx.x) * groups + group, step = in.step;
+  in.start(first);
   const float inv_c = 1.0f / C;
-  float dgamma[EPT], dbeta[EPT], w[EPT];
+  float dgamma[EPT], dbeta[EPT], w[TWICE ? 1 : EPT];
+  if constexpr (!TWICE) {
 #pragma unroll
-  for (int j = 0; j < VPT; ++j) load_params<V, VEC>(p.gamma, (tid + j * G) * V, C, 1.0f, w + j * V);
+    for (int j = 0; j < VPT; ++j) load_params<V, FULL>(p.gamma, p.vec_gamma, (tid + j * G) * V, C, 1.0f, w + j * V);
+  }
 #pragma unroll
   for (int i = 0; i < EPT; ++i) dgamma[i] = dbeta[i] = 0.0f;
-  long long r = static_cast<long long>(blockIdx.x) * groups + group;
   int parity = 0;
-  for (; r < p.rows; r += step, parity ^= 1) {
-    const float mean = __ldg(p.mean + r), rstd = __ldg(p.rstd + r);
-    float x[EPT], dy[EPT];
+  float mean = 0.0f, rstd = 0.0f;
+  if (first < p.rows) { mean = __ldg(p.mean + first); rstd = __ldg(p.rstd + first); }
+  for (long long r = first; r - g.sub() < p.rows; r += step, parity ^= 1) {
+    // the next row's mean and 1/std are on their way while this row is worked on
+    const long long after = r + step;
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    if (after < p.rows) { next_mean = __ldg(p.mean + after); next_rstd = __ldg(p.rstd + after); }
+    float s1[2] = {0.0f, 0.0f}, s2[2] = {0.0f, 0.0f};
+    // beyond a row's end dy is zero: nothing is added
+    auto gather = [&](float& x, float& dy, float weight, float& dg, float& db, int i) {
+      x = (x - mean) * rstd;
+      dg = fmaf(dy, x, dg);
+      db += dy;
+      dy *= weight;
+      s1[i & 1] += dy;
+      s2[i & 1] = fmaf(dy, x, s2[i & 1]);
+    };
+    T* const dx = static_cast<T*>(p.dx) + r * p.ld_dx;
+    if constexpr (!TWICE) {
+      float row[2][EPT];
+      in.take(r, row);
+      float (&x)[EPT] = row[0], (&dy)[EPT] = row[1];
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-      load_piece<T, VEC>(static_cast<const T*>(p.x) + r * p.ld_x, (tid + j * G) * V, C, wbuf, x + j * V);
-      load_piece<T, VEC>(static_cast<const T*>(p.dy) + r * p.ld_dy, (tid + j * G) * V, C, wbuf, dy + j * V);
-    }
-    float s1 = 0.0f, s2 = 0.0f;
+      for (int i = 0; i < EPT; ++i) gather(x[i], dy[i], w[i], dgamma[i], dbeta[i], i);
+      if (p.dx) {
+        const float2 t = g.sum2(s1[0] + s1[1], s2[0] + s2[1], box[parity] + 2 * slot);   // two boxes in turn: one barrier per row
+        in.release(r);
+        const bool exists = in.ok() && (!NARROW || r < p.rows);
+        const float m1 = -t.x * inv_c * rstd, m2 = t.y * inv_c;
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) {                  // beyond the row's end dy is zero: nothing is added
-      x[i] = (x[i] - mean) * rstd;
-      dgamma[i] = fmaf(dy[i], x[i], dgamma[i]);
-      dbeta[i] += dy[i];
-      dy[i] *= w[i];
-      s1 += dy[i];
-      s2 = fmaf(dy[i], x[i], s2);
-    }
-    if (p.dx) {
-      s1 = warp_sum(s1);
-      s2 = warp_sum(s2);
-      if (warps > 1) {
-        // the two boxes in turn: one barrier per row
-        if (lane == 0) box[parity][warp] = make_float2(s1, s2);
-        asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(G) : "memory");
-        const float2 t = lane < warps ? box[parity][first_warp + lane] : make_float2(0.0f, 0.0f);
-        s1 = warp_sum(t.x);
-        s2 = warp_sum(t.y);
+        for (int i = 0; i < EPT; ++i) dy[i] = fmaf(fmaf(-x[i], m2, dy[i]), rstd, m1);
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) store_piece<T, FULL, NARROW>(dx, exists, p.vec_dx, tid, G, j, C, wbuf, dy + j * V);
       }
-      s1 *= inv_c;
-      s2 *= inv_c;
+    } else {
+      in.fine = in.fine && mbar_wait(in.bars + 8 * in.stage, in.phase, in.abort_flag);
+      const bool end0 = in.at_end(0, r), end1 = in.at_end(1, r);
+      auto piece = [&](int t, int c, float* v) {
+        if (t ? end1 : end0) {
+          const T* const row = in.base[t] + r * in.ld[t];
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) dy[i] = rstd * (fmaf(-x[i], s2, dy[i]) - s1);
+          for (int i = 0; i < V; ++i) v[i] = c + i < C ? load1(row + c + i) : 0.0f;
+        } else {
+          if (c < C) in.ring_piece(t, in.skew(t, r), c, v);
+          if (c + V > C) {
 #pragma unroll
-      for (int j = 0; j < VPT; ++j)
-        store_piece<T, VEC>(static_cast<T*>(p.dx) + r * p.ld_dx, (tid + j * G) * V, C, wbuf, dy + j * V);
+            for (int i = 0; i < V; ++i)
+              if (c + i >= C) v[i] = 0.0f;
+          }
+        }
+      };
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        const int c = (tid + j * G) * V;
+        float x[V], dy[V], weight[V];
+        piece(0, c, x);
+        piece(1, c, dy);
+        load_params<V, FULL>(p.gamma, p.vec_gamma, c, C, 1.0f, weight);
+#pragma unroll
+        for (int i = 0; i < V; ++i) gather(x[i], dy[i], weight[i], dgamma[j * V + i], dbeta[j * V + i], i);
+      }
+      const float2 t = g.sum2(s1[0] + s1[1], s2[0] + s2[1], box[parity] + 2 * slot);
+      const float m1 = -t.x * inv_c * rstd, m2 = t.y * inv_c;
+      if (p.dx) {
+#pragma unroll 1
+        for (int j = 0; j < VPT; ++j) {
+          const int c = (tid + j * G) * V;
+          float x[V], dy[V], weight[V];
+          piece(0, c, x);
+          piece(1, c, dy);
+          load_params<V, FULL>(p.gamma, p.vec_gamma, c, C, 1.0f, weight);
+#pragma unroll
+          for (int i = 0; i < V; ++i) dy[i] = fmaf(fmaf(-((x[i] - mean) * rstd), m2, dy[i] * weight[i]), rstd, m1);
+          store_piece<T, FULL, NARROW>(dx, in.ok(), p.vec_dx, tid, G, j, C, wbuf, dy);
+        }
+      }
+      g.sync();                                        // everyone has read the stage
+      in.release(r);
     }
+    mean = next_mean;
+    rstd = next_rstd;
   }
+  in.finish(p.status);
   if (p.partial == nullptr) return;
   float* const out = p.partial + 2ll * blockIdx.x * C;
-  for (int g = 0; g < groups; ++g) {
-    if (group == g) {
-      float* const to = g == groups - 1 ? out : sums;
+  float* const sums = reinterpret_cast<float*>(ring_smem);
+  // a narrow warp's rows first, then the block's warps (or groups) in order
+  if constexpr (NARROW) {
+    for (int o = G; o < 32; o <<= 1) {
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) {
+        dgamma[i] += __shfl_xor_sync(0xFFFFFFFFu, dgamma[i], o);
+        dbeta[i] += __shfl_xor_sync(0xFFFFFFFFu, dbeta[i], o);
+      }
+    }
+  }
+  const int turns = NARROW ? blockDim.x >> 5 : groups, mine = NARROW ? threadIdx.x >> 5 : group;
+  if (turns > 1) __syncthreads();                      // the ring is done with
+  for (int k = 0; k < turns; ++k) {
+    if (mine == k && g.sub() == 0) {
+      float* const to = k == turns - 1 ? out : sums;
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           const int c = (tid + j * G) * V + i;
           if (c < C) {
-            to[c] = g ? sums[c] + dgamma[j * V + i] : dgamma[j * V + i];
-            to[C + c] = g ? sums[C + c] + dbeta[j * V + i] : dbeta[j * V + i];
+            to[c] = k ? sums[c] + dgamma[j * V + i] : dgamma[j * V + i];
+            to[C + c] = k ? sums[C + c] + dbeta[j * V + i] : dbeta[j * V + i];
           }
         }
       }
     }
-    if (groups > 1) __syncthreads();
+    if (turns > 1) __syncthreads();
   }
 }
 
-// adds the chunks' partial sums in a fixed order: 32 columns by 8 strands per block
-__global__ void __launch_bounds__(256) norm_bwd_reduce_kernel(const float* __restrict__ partial, int chunks, int cols,
-                                                              float* dgamma, float* dbeta) {
-  __shared__ float box[8][33];
+// adds the chunks' partial sums in a fixed order: 32 columns by 32 strands per block, four loads in flight each
+__global__ void __launch_bounds__(1024) norm_bwd_reduce_kernel(const float* __restrict__ partial, int chunks, int cols,
+                                                               float* dgamma, float* dbeta) {
+  __shared__ float box[32][33];
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5;
   const long long total = 2ll * cols;
   const long long j = static_cast<long long>(blockIdx.x) * 32 + lane;    // column of [dgamma | dbeta]
   float s = 0.0f;
-  if (j < total)
-    for (int k = strand; k < chunks; k += 8) s += partial[k * total + j];
+  if (j < total) {
+    for (int k = strand; k < chunks; k += 128) {
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = k + 32 * i < chunks ? __ldcg(partial + (k + 32ll * i) * total + j) : 0.0f;
+      s += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+  }
   box[strand][lane] = s;
   __syncthreads();
   if (strand == 0 && j < total) {
 #pragma unroll
-    for (int k = 1; k < 8; ++k) s += box[k][lane];
+    for (int k = 1; k < 32; ++k) s += box[k][lane];
     if (j < cols) { if (dgamma) dgamma[j] = s; }
     else if (dbeta) dbeta[j - cols] = s;
   }
@@ -559,64 +897,115 @@ bool aligned(const void* p, long long ld, int size) {
   return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld * size) % 16 == 0;
 }
 
-template <typename T, int MODE, int EPT, bool VEC, bool WARP>
-cudaError_t launch_row(luq_ctx* ctx, const RowParams& p, int block, long long blocks, cudaStream_t st) {
-  // enough blocks to fill the SMs, each walking its rows
-  const long long cap = static_cast<long long>(ctx->sm_count) * (2048 / block);
-  return luq_launch_kernel(row_kernel<T, MODE, EPT, VEC, WARP>, static_cast<int>(blocks < cap ? blocks : cap), block, 0, st,
-                           LUQ_LAUNCH_EARLY, 1, p);
+constexpr int kRingBytes = 100 * 1024;     // of a block of the forward kernels: two blocks share an SM
+constexpr int kRingBytesAlone = 190 * 1024;
+
+template <typename K>
+cudaError_t allow_smem(K kernel) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+}
+// stages of a ring: as many as fit, eight at most, two if two do fit an SM (one row of x and dy may be 128 KB)
+int ring_depth_for(int groups, int stage_bytes, int budget) {
+  int d = budget / (groups * (stage_bytes + 8));
+  if (d < 2) d = 2 * groups * (stage_bytes + 8) <= kRingBytesAlone ? 2 : 1;
+  return d > 8 ? 8 : d;
+}
+// threads of a row: a power of two of lanes up to a warp, whole warps beyond
+int threads_of_row(int cols, int ept) {
+  if (cols <= 512) {
+    int g = 1;
+    while (g * ept < cols) g <<= 1;
+    return g;
+  }
+  return (cols + 32 * ept - 1) / (32 * ept) * 32;
 }
 
-template <typename T, int MODE, bool VEC>
-cudaError_t launch_row_width(luq_ctx* ctx, const RowParams& p, cudaStream_t st) {
-  const int C = p.cols;
-  const int warps = p.rows >= 8ll * ctx->sm_count ? 8 : 1;           // rows per block while every SM has some
-  const long long blocks = (p.rows + warps - 1) / warps;
-  if (C <= 256) return launch_row<T, MODE, 8, VEC, true>(ctx, p, 32 * warps, blocks, st);
-  if (C <= 1024) return launch_row<T, MODE, 32, VEC, true>(ctx, p, 32 * warps, blocks, st);
-  if (C <= 4096) return launch_row<T, MODE, 8, VEC, false>(ctx, p, (C + 255) / 256 * 32, p.rows, st);
-  if (C <= 8192) return launch_row<T, MODE, 16, VEC, false>(ctx, p, (C + 511) / 512 * 32, p.rows, st);
-  return launch_row<T, MODE, 32, VEC, false>(ctx, p, (C + 1023) / 1024 * 32, p.rows, st);
+template <typename T, int MODE, int EPT, int LOAD, bool NARROW>
+cudaError_t launch_row(luq_ctx* ctx, const RowParams& p, bool vec, cudaStream_t st) {
+  const int G = threads_of_row(p.cols, EPT);
+  // groups share a block while every SM has some; a block has whole warps
+  int groups = 512 / G;
+  while (groups > 1 && G * groups > 32 && p.rows < static_cast<long long>(groups) * ctx->sm_count) groups >>= 1;
+  const int row_bytes = Rows<T, 1, EPT, LOAD, false, NARROW>::ring_row_bytes(p.cols);
+  const int depth = LOAD == kRing ? ring_depth_for(groups, row_bytes, kRingBytes) : 0;
+  const size_t smem = LOAD == kRing ? static_cast<size_t>(Rows<T, 1, EPT, LOAD, false, NARROW>::ring_bytes(groups, depth, p.cols)) : 0;
+  const bool full = LOAD != kBounce && vec && p.cols == G * EPT && (MODE == kInt8 || (p.gamma && p.beta));
+  auto kernel = full ? row_kernel<T, MODE, EPT, LOAD, LOAD != kBounce, NARROW> : row_kernel<T, MODE, EPT, LOAD, false, NARROW>;
+  if (LOAD == kRing) {
+    const cudaError_t e = allow_smem(kernel);
+    if (e != cudaSuccess) return e;
+  }
+  const long long blocks = (p.rows + groups - 1) / groups;
+  const long long cap = static_cast<long long>(ctx->sm_count) * (LOAD == kRing ? (EPT == 32 || smem > kRingBytes + 4096 ? 1 : 2)
+                                                                               : 1024 / (G * groups));
+  return luq_launch_kernel(kernel, static_cast<int>(blocks < cap ? blocks : cap), G * groups, smem, st, LUQ_LAUNCH_EARLY, 1, p, G, depth);
 }
 
 template <typename T, int MODE>
-int launch_rows(luq_ctx* ctx, const RowParams& p, cudaStream_t st) {
+int launch_rows(luq_ctx* ctx, RowParams p, cudaStream_t st) {
   cudaError_t e;
+  p.vec_params = aligned(p.gamma, 0, 4) && aligned(p.beta, 0, 4);
+  p.vec_y = MODE != kNorm || aligned(p.y, p.ld_y, sizeof(T));
+  const bool vec_x = aligned(p.x, p.ld_x, sizeof(T)), vec = vec_x && p.vec_params && p.vec_y;
+  // the ring pays where every group has several rows
+  const bool many = p.rows >= 8ll * ctx->sm_count;
   if (p.cols > 16384) {
     const long long cap = 4ll * ctx->sm_count;
     e = luq_launch_kernel(row_loop_kernel<T, MODE>, static_cast<int>(p.rows < cap ? p.rows : cap), 512, 0, st, LUQ_LAUNCH_EARLY, 1, p);
+  } else if (p.cols > 8192) {
+    e = many ? launch_row<T, MODE, 32, kRing, false>(ctx, p, vec, st)
+             : vec_x ? launch_row<T, MODE, 32, kDirect, false>(ctx, p, vec, st) : launch_row<T, MODE, 32, kBounce, false>(ctx, p, vec, st);
+  } else if (p.cols > 512) {
+    e = many ? launch_row<T, MODE, 16, kRing, false>(ctx, p, vec, st)
+             : vec_x ? launch_row<T, MODE, 16, kDirect, false>(ctx, p, vec, st) : launch_row<T, MODE, 16, kBounce, false>(ctx, p, vec, st);
   } else {
-    const bool vec = aligned(p.x, p.ld_x, sizeof(T)) && aligned(p.gamma, 0, 4) && aligned(p.beta, 0, 4) &&
-                     (MODE != kNorm || aligned(p.y, p.ld_y, sizeof(T)));
-    e = vec ? launch_row_width<T, MODE, true>(ctx, p, st) : launch_row_width<T, MODE, false>(ctx, p, st);
+    e = vec_x ? launch_row<T, MODE, 16, kDirect, true>(ctx, p, vec, st) : launch_row<T, MODE, 16, kBounce, true>(ctx, p, vec, st);
   }
   if (e == cudaSuccess) ctx->launches += 1;
   return static_cast<int>(e);
 }
 
-template <typename T, bool VEC>
-cudaError_t launch_norm_bwd_rows(const NormBwdParams& p, int G, int block, int grid, cudaStream_t st) {
-  const size_t smem = block > G ? 2 * sizeof(float) * static_cast<size_t>(p.cols) : 0;
-  return luq_launch_kernel(norm_bwd_kernel<T, 8, VEC>, grid, block, smem, st, LUQ_LAUNCH_EARLY, 1, p, G);
+template <typename T, int EPT, int LOAD, bool NARROW>
+cudaError_t launch_norm_bwd_rows(const NormBwdParams& p, bool vec, int G, int block, int grid, cudaStream_t st) {
+  const int groups = block / G;
+  using R = Rows<T, 2, 16, LOAD, false, NARROW>;
+  const int depth = LOAD == kRing ? ring_depth_for(groups, 2 * R::ring_row_bytes(p.cols), kRingBytesAlone) : 0;
+  const size_t sums = block > G ? 2 * sizeof(float) * static_cast<size_t>(p.cols) : 0;
+  const size_t ring = LOAD == kRing ? static_cast<size_t>(R::ring_bytes(groups, depth, p.cols)) : 0;
+  constexpr bool can = LOAD != kBounce && EPT == 16;
+  const bool full = can && vec && p.cols == G * EPT && p.gamma;
+  auto kernel = full ? norm_bwd_kernel<T, EPT, LOAD, can, NARROW> : norm_bwd_kernel<T, EPT, LOAD, false, NARROW>;
+  const cudaError_t e = allow_smem(kernel);
+  if (e != cudaSuccess) return e;
+  return luq_launch_kernel(kernel, grid, block, ring > sums ? ring : sums, st, LUQ_LAUNCH_EARLY, 1, p, G, depth);
 }
 
 template <typename T>
 int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, cudaStream_t st) {
   const size_t per_chunk = 2 * sizeof(float) * static_cast<size_t>(p.cols);
   cudaError_t e = cudaSuccess;
-  if (p.cols <= 8192) {
-    // eight elements of a row per thread; groups of threads that share a block while there are rows for them
-    const int G = (p.cols + 255) / 256 * 32;
-    int groups = G <= 256 ? 512 / G : 1;
-    while (groups > 1 && static_cast<long long>(groups) * ctx->sm_count > 2 * p.rows) groups >>= 1;
+  p.vec_gamma = aligned(p.gamma, 0, 4);
+  p.vec_dx = aligned(p.dx, p.ld_dx, sizeof(T));
+  const bool vec_in = aligned(p.x, p.ld_x, sizeof(T)) && aligned(p.dy, p.ld_dy, sizeof(T)), vec = vec_in && p.vec_gamma && p.vec_dx;
+  // a row of x and one of dy have to fit the ring
+  if (p.cols <= 16384 && Rows<T, 2, 16, kRing, false, false>::ring_bytes(1, 1, p.cols) <= 200 * 1024) {
+    // as many sums of both kinds per thread as elements of a row; groups share a block while there are rows for them
+    const int ept = p.cols > 8192 ? 32 : 16;
+    const int G = threads_of_row(p.cols, ept);
+    int groups = 512 / G;
+    while (groups > 1 && G * groups > 32 && static_cast<long long>(groups) * ctx->sm_count > p.rows) groups >>= 1;
     const int block = G * groups;
-    long long blocks = static_cast<long long>(ctx->sm_count) * (block > 512 ? 1 : 1024 / block);
+    long long blocks = ctx->sm_count;
     if (blocks * groups > p.rows) blocks = (p.rows + groups - 1) / groups;
     p.partial = dgamma || dbeta ? ctx->d_workspace : nullptr;
     p.chunks = static_cast<int>(blocks);
-    const bool vec = aligned(p.x, p.ld_x, sizeof(T)) && aligned(p.dy, p.ld_dy, sizeof(T)) && aligned(p.dx, p.ld_dx, sizeof(T)) &&
-                     aligned(p.gamma, 0, 4);
-    e = vec ? launch_norm_bwd_rows<T, true>(p, G, block, p.chunks, st) : launch_norm_bwd_rows<T, false>(p, G, block, p.chunks, st);
+    const bool ring = p.dx != nullptr && p.rows >= 4 * blocks * groups;
+    if (ept == 32) e = launch_norm_bwd_rows<T, 32, kRing, false>(p, vec, G, block, p.chunks, st);
+    else if (p.cols <= 512) e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, true>(p, vec, G, block, p.chunks, st)
+                                       : launch_norm_bwd_rows<T, 16, kBounce, true>(p, vec, G, block, p.chunks, st);
+    else if (ring) e = launch_norm_bwd_rows<T, 16, kRing, false>(p, vec, G, block, p.chunks, st);
+    else e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, false>(p, vec, G, block, p.chunks, st)
+                    : launch_norm_bwd_rows<T, 16, kBounce, false>(p, vec, G, block, p.chunks, st);
   } else {
     // workspace: two floats per row, then the chunks' partial sums
     const size_t means = ((static_cast<size_t>(p.rows) * sizeof(float2) + 255) / 256) * 256;
@@ -642,7 +1031,7 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
   if (e != cudaSuccess) return static_cast<int>(e);
   ctx->launches += 1;
   if (dgamma || dbeta) {
-    e = luq_launch_kernel(norm_bwd_reduce_kernel, static_cast<int>((2ll * p.cols + 31) / 32), 256, 0, st, LUQ_LAUNCH_EARLY, 1,
+    e = luq_launch_kernel(norm_bwd_reduce_kernel, static_cast<int>((2ll * p.cols + 31) / 32), 1024, 0, st, LUQ_LAUNCH_EARLY, 1,
                           p.partial, p.chunks, p.cols, dgamma, dbeta);
     if (e == cudaSuccess) ctx->launches += 1;
   }
@@ -675,7 +1064,7 @@ int luq_launch_layer_norm_bwd(luq_ctx* ctx, const void* d_dy, int64_t ld_dy, con
                               void* d_dx, int64_t ld_dx, float* d_dgamma, float* d_dbeta, cudaStream_t st) {
   NormBwdParams p{};
   p.dy = d_dy; p.x = d_x; p.rows = rows; p.cols = cols; p.ld_dy = ld_dy; p.ld_x = ld_x; p.ld_dx = ld_dx;
-  p.gamma = d_gamma; p.mean = d_mean; p.rstd = d_rstd; p.dx = d_dx;
+  p.gamma = d_gamma; p.mean = d_mean; p.rstd = d_rstd; p.dx = d_dx; p.status = ctx->d_status;
   return dtype == LUQ_BF16 ? launch_norm_bwd<__nv_bfloat16>(ctx, p, d_dgamma, d_dbeta, st)
                            : launch_norm_bwd<float>(ctx, p, d_dgamma, d_dbeta, st);
 }
