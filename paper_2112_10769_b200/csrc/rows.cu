@@ -721,7 +721,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
   static_assert(!TWICE || LOAD == kRing, "a row that is read twice stays in the ring");
   __shared__ float box[2][32];
   __shared__ uint4 move[FULL ? 1 : 16][32];
-  extern __shared__ __align__(128) uint8_t ring_smem[];   // the ring; at the end [2][cols] sums
+  extern __shared__ __align__(128) uint8_t ring_smem[];   // the ring; at the end [groups][2][cols] sums
   const Group<NARROW> g(threads_per_row);
   const int groups = blockDim.x / g.G, group = g.index, slot = g.index * g.warps, tid = g.tid, G = g.G, C = p.cols;
   uint4* const wbuf = move[FULL ? 0 : threadIdx.x >> 5];
@@ -832,8 +832,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
   in.finish(p.status);
   if (p.partial == nullptr) return;
   float* const out = p.partial + 2ll * blockIdx.x * C;
-  float* const sums = reinterpret_cast<float*>(ring_smem);
-  // a narrow warp's rows first, then the block's warps (or groups) in order
+  // a narrow warp's rows first, then the block's warps (or groups) in order, each thread a column
   if constexpr (NARROW) {
     for (int o = G; o < 32; o <<= 1) {
 #pragma unroll
@@ -844,23 +843,29 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
     }
   }
   const int turns = NARROW ? blockDim.x >> 5 : groups, mine = NARROW ? threadIdx.x >> 5 : group;
+  float* const sums = reinterpret_cast<float*>(ring_smem);
+  float* const to = turns == 1 ? out : sums + 2 * mine * C;
   if (turns > 1) __syncthreads();                      // the ring is done with
-  for (int k = 0; k < turns; ++k) {
-    if (mine == k && g.sub() == 0) {
-      float* const to = k == turns - 1 ? out : sums;
+  if (g.sub() == 0) {
 #pragma unroll
-      for (int j = 0; j < VPT; ++j) {
+    for (int j = 0; j < VPT; ++j) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const int c = (tid + j * G) * V + i;
-          if (c < C) {
-            to[c] = k ? sums[c] + dgamma[j * V + i] : dgamma[j * V + i];
-            to[C + c] = k ? sums[C + c] + dbeta[j * V + i] : dbeta[j * V + i];
-          }
+      for (int i = 0; i < V; ++i) {
+        const int c = (tid + j * G) * V + i;
+        if (c < C) {
+          to[c] = dgamma[j * V + i];
+          to[C + c] = dbeta[j * V + i];
         }
       }
     }
-    if (turns > 1) __syncthreads();
+  }
+  if (turns > 1) {
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * C; c += blockDim.x) {
+      float s = sums[c];
+      for (int k = 1; k < turns; ++k) s += sums[2 * k * C + c];
+      out[c] = s;
+    }
   }
 }
 
@@ -969,7 +974,8 @@ cudaError_t launch_norm_bwd_rows(const NormBwdParams& p, bool vec, int G, int bl
   const int groups = block / G;
   using R = Rows<T, 2, 16, LOAD, false, NARROW>;
   const int depth = LOAD == kRing ? ring_depth_for(groups, 2 * R::ring_row_bytes(p.cols), kRingBytesAlone) : 0;
-  const size_t sums = block > G ? 2 * sizeof(float) * static_cast<size_t>(p.cols) : 0;
+  const int turns = NARROW ? block / 32 : groups;
+  const size_t sums = turns > 1 ? 2 * sizeof(float) * static_cast<size_t>(p.cols) * turns : 0;
   const size_t ring = LOAD == kRing ? static_cast<size_t>(R::ring_bytes(groups, depth, p.cols)) : 0;
   constexpr bool can = LOAD != kBounce && EPT == 16;
   const bool full = can && vec && p.cols == G * EPT && p.gamma;
