@@ -11,9 +11,10 @@
 // a group's last, partial tile and a handful of tokens of a model that answers alike.
 //
 // One persistent CTA per SM, warp-specialised:
-//   warp 0     TMA producer: 128 x 128 bytes of W and the tile's token rows x 128 bytes, 128-byte swizzle
+//   warp 0     TMA producer of W, 128 x 128 bytes per stage, 128-byte swizzle
 //   warp 1     one thread issues tcgen05.mma kind::i8; owns the tensor-memory allocation (two accumulators)
-//   warps 2-5  epilogue: tcgen05.ld -> scales, bias -> staged 32 x 32 boxes -> TMA store; token rows
+//   warp 2     TMA producer of the tile's token rows x 128 bytes
+//   warps 3..  epilogue: tcgen05.ld -> scales, bias -> staged 32 x 32 boxes -> TMA store; token rows
 //              that share a box with another group's, and outputs TMA cannot address, are stored directly
 // All waits are bounded; on expiry the CTA flags LUQ_STATUS_TIMEOUT, drains its copies, frees its
 // tensor memory and returns.
@@ -29,7 +30,8 @@ using namespace luqdev;
 constexpr int kCh = 128;                  // output channels per tile (tensor-memory lanes)
 constexpr int kBk = 128;                  // contraction elements per stage
 constexpr int kSlab = kCh * kBk;          // bytes of W per stage
-constexpr int kFirstEpiWarp = 2;
+constexpr int kXWarp = 2;
+constexpr int kFirstEpiWarp = 3;
 constexpr int kWarpStaging = 32 * 32 * 4; // a warp's store boxes: one of 32 x 32 fp32, or two of bf16
 constexpr int kBand = 8;                  // token tiles that walk the channels together
 
@@ -58,7 +60,7 @@ struct Cfg {
   static constexpr int span = BT / (epi_warps / 4);
   static constexpr int threads = 32 * (kFirstEpiWarp + epi_warps);
   static constexpr int x_rows = PAIR ? BT / 2 : BT;               // token rows this CTA holds of a tile
-  static constexpr int box_rows = BT < 32 ? BT : 32;              // token rows per copy
+  static constexpr int part_rows = BT < 32 ? BT : 32;             // token rows per copy of a tile that is not full
   static constexpr int stage_bytes = kSlab + x_rows * kBk;
   static constexpr int stages = BT == 16 ? 10 : BT == 64 ? 7 : 5;
   static constexpr int chunk = BT < 32 ? BT : 32;                 // tokens per epilogue step
@@ -300,7 +302,7 @@ __device__ __forceinline__ void write_tile(const Int8Params& p, const void* tm_z
 template <int BT, bool PAIR, bool SPLIT, bool BF16>
 __global__ void __launch_bounds__((Cfg<BT, PAIR>::threads), 1)
 int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x,
-                 const __grid_constant__ CUtensorMap tm_z, const Int8Params p) {
+                 const __grid_constant__ CUtensorMap tm_x_part, const __grid_constant__ CUtensorMap tm_z, const Int8Params p) {
   static_assert(!(PAIR && SPLIT), "one use of the cluster at a time");
   using C = Cfg<BT, PAIR>;
   constexpr int ES = C::stages;
@@ -330,6 +332,7 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     fence_barrier_init();
     fence_proxy_async();
     tma_prefetch_desc(&tm_w); tma_prefetch_desc(&tm_x);
+    if (C::part_rows < C::x_rows) tma_prefetch_desc(&tm_x_part);
     if (p.z_tma) tma_prefetch_desc(&tm_z);
   }
   if (warp == 1) {
@@ -357,48 +360,37 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   uint32_t stage = 0, phase = 0, issued = 0, it = 0;
   bool ok = true, waited = !p.early;
 
-  auto produce = [&](const Unit& v) {                  // one thread
+  // one thread fetches the weights, another the tokens (two threads pull more than one); the first counts both
+  // on the stage's barrier
+  auto produce = [&](const Unit& v, bool tokens) {
     // token rows of this CTA: all of the tile's, or on a pair its half of the instruction's extent
     const int half = (v.rows + 31) / 32 * 16;
     const int x_row0 = v.row0 + (PAIR ? static_cast<int>(rank) * half : 0);
-    const int boxes = ((PAIR ? half : v.rows) + C::box_rows - 1) / C::box_rows;
-    const uint32_t bytes = kSlab + boxes * C::box_rows * kBk;
+    // one copy for a full tile's rows (a quarter of the size is a quarter slower), else as many as it takes
+    const int parts = ((PAIR ? half : v.rows) + C::part_rows - 1) / C::part_rows;
+    const bool whole = parts * C::part_rows == C::x_rows;
+    const uint32_t bytes = kSlab + parts * C::part_rows * kBk;
     const int ch0 = v.ch0 + (PAIR ? static_cast<int>(rank) * kCh : 0);
-    auto w_copy = [&](int kb, uint32_t s) {
-      const uint32_t dst = base + s * C::stage_bytes;
-      if constexpr (PAIR) {
-        if (rank == 0) mbar_arrive_expect_tx(full(s), 2 * bytes);   // both CTAs' bytes
-        tma_pair_load_3d(dst, &tm_w, mapa_shared(full(s), 0), kb * kBk, ch0, v.group);
-      } else {
-        mbar_arrive_expect_tx(full(s), bytes);
-        tma_load_3d(dst, &tm_w, full(s), kb * kBk, ch0, v.group);
-      }
-    };
-    auto x_copy = [&](int kb, uint32_t s) {
-      const uint32_t dst = base + s * C::stage_bytes + kSlab;
-      for (int b = 0; b < boxes; ++b) {
-        if constexpr (PAIR) tma_pair_load_2d(dst + b * C::box_rows * kBk, &tm_x, mapa_shared(full(s), 0), kb * kBk, x_row0 + b * C::box_rows);
-        else tma_load_2d(dst + b * C::box_rows * kBk, &tm_x, full(s), kb * kBk, x_row0 + b * C::box_rows);
-      }
-    };
-    int kb = kb_first;
-    if (!waited) {
-      // the first stages' weights, then the wait for the quantizer, then their tokens
-      const int ahead = min(kb_end - kb, ES);
-      for (int i = 0; i < ahead; ++i) w_copy(kb + i, i);
-      pdl_wait();
-      waited = true;
-      for (int i = 0; i < ahead; ++i) x_copy(kb + i, i);
-      kb += ahead;
-      issued = ahead;
-      stage = ahead == ES ? 0 : ahead;
-      phase = ahead == ES ? 1 : 0;
-    }
-    for (; kb < kb_end; ++kb) {
+    for (int kb = kb_first; kb < kb_end; ++kb) {
       if (!mbar_wait(empty(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
-      w_copy(kb, stage);
-      x_copy(kb, stage);
-      ++issued;
+      const uint32_t dst = base + stage * C::stage_bytes;
+      const uint32_t bar = PAIR ? mapa_shared(full(stage), 0) : full(stage);
+      if (!tokens) {
+        if (!PAIR) mbar_arrive_expect_tx(bar, bytes);
+        else if (rank == 0) mbar_arrive_expect_tx(full(stage), 2 * bytes);   // both CTAs' bytes
+        if constexpr (PAIR) tma_pair_load_3d(dst, &tm_w, bar, kb * kBk, ch0, v.group);
+        else tma_load_3d(dst, &tm_w, bar, kb * kBk, ch0, v.group);
+        ++issued;
+      } else if (whole) {
+        if constexpr (PAIR) tma_pair_load_2d(dst + kSlab, &tm_x, bar, kb * kBk, x_row0);
+        else tma_load_2d(dst + kSlab, &tm_x, bar, kb * kBk, x_row0);
+      } else {
+        for (int b = 0; b < parts; ++b) {
+          const int off = b * C::part_rows;
+          if constexpr (PAIR) tma_pair_load_2d(dst + kSlab + off * kBk, &tm_x_part, bar, kb * kBk, x_row0 + off);
+          else tma_load_2d(dst + kSlab + off * kBk, &tm_x_part, bar, kb * kBk, x_row0 + off);
+        }
+      }
       if (++stage == static_cast<uint32_t>(ES)) { stage = 0; phase ^= 1u; }
     }
   };
@@ -467,10 +459,11 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   static_assert(32 * C::epi_warps >= BT, "a thread fetches one token's scale");
 
   if constexpr (!SPLIT) {
-    if (warp == 0) {
+    if (warp == 0 || warp == kXWarp) {
       if (lane == 0) {
-        for (; ok && walk.more(); walk.next()) produce(unit_of(walk));
-        drain();
+        if (warp == kXWarp && !waited) pdl_wait();
+        for (; ok && walk.more(); walk.next()) produce(unit_of(walk), warp == kXWarp);
+        if (warp == 0) drain();
       }
     } else if (warp == 1) {
       if (lane == 0 && rank == 0)
@@ -510,8 +503,11 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     int* const partial = reinterpret_cast<int*>(gen + C::staging);      // [token][channel]
     for (; walk.more(); walk.next(), ++it) {
       const Unit v = unit_of(walk);
-      if (warp == 0) {
-        if (lane == 0 && ok) produce(v);
+      if (warp == 0 || warp == kXWarp) {
+        if (lane == 0 && ok) {
+          if (warp == kXWarp && !waited) { pdl_wait(); waited = true; }
+          produce(v, warp == kXWarp);
+        }
       } else if (warp == 1) {
         if (lane == 0 && ok) multiply(v);
       } else {
@@ -602,8 +598,10 @@ template <int BT, bool PAIR, bool SPLIT, bool BF16>
 int launch(luq_ctx* ctx, const luq_int8_args& a, const Int8Params& p, long long units, int cluster, const CUtensorMap& tw,
            const CUtensorMap& tz, cudaStream_t st) {
   using C = Cfg<BT, PAIR>;
-  CUtensorMap tx;
-  if (encode_codes(ctx->encode_tiled, &tx, a.x_codes, a.K, a.M, a.ld_x, 0, 0, C::box_rows)) return LUQ_ERR_CUDA;
+  CUtensorMap tx, tx_part;
+  if (encode_codes(ctx->encode_tiled, &tx, a.x_codes, a.K, a.M, a.ld_x, 0, 0, C::x_rows)) return LUQ_ERR_CUDA;
+  if (C::part_rows == C::x_rows) tx_part = tx;
+  else if (encode_codes(ctx->encode_tiled, &tx_part, a.x_codes, a.K, a.M, a.ld_x, 0, 0, C::part_rows)) return LUQ_ERR_CUDA;
   auto kernel = int8_gemm_kernel<BT, PAIR, SPLIT, BF16>;
   const cudaError_t attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem_bytes(LUQ_MAX_GROUPS));
   if (attr != cudaSuccess) return static_cast<int>(attr);
@@ -611,7 +609,7 @@ int launch(luq_ctx* ctx, const luq_int8_args& a, const Int8Params& p, long long 
   const long long most = sms / cluster > 0 ? sms / cluster : 1;
   const int grid = static_cast<int>(units < most ? units : most) * cluster;
   const cudaError_t e = luq_launch_kernel(kernel, grid, C::threads, static_cast<size_t>(C::smem_bytes(p.groups)), st,
-                                          LUQ_LAUNCH_EARLY, static_cast<unsigned>(cluster), tw, tx, tz, p);
+                                          LUQ_LAUNCH_EARLY, static_cast<unsigned>(cluster), tw, tx, tx_part, tz, p);
   if (e == cudaSuccess) ctx->launches += 1;
   return static_cast<int>(e);
 }
