@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "luq.h"
 
 #define LUQ_KMAX 4  // default level count: alpha = max / 2^LUQ_KMAX (Eq. alpha with b = 3)
@@ -166,6 +168,19 @@ cudaError_t luq_launch_kernel(void (*kernel)(KArgs...), int grid, int block, siz
   cfg.numAttrs = n;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
+
+// Runs a call that has to be made once per device (a kernel's attribute): a static of the launching function.
+struct luq_once_per_device {
+  std::atomic<unsigned long long> done{0};
+  template <typename F>
+  cudaError_t operator()(F&& call, int device) {
+    const unsigned long long bit = device >= 0 && device < 64 ? 1ull << device : 0ull;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    const cudaError_t e = call();
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+  }
+};
 
 // Checking build (-DLUQ_DEBUG): LUQ_IN_BOUNDS(cond, status) is `cond`, and a false one raises
 // LUQ_STATUS_BOUNDS in the status word; callers skip the access.  In the normal build it is `true`

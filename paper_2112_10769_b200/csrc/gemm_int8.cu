@@ -33,6 +33,7 @@ constexpr int kSlab = kCh * kBk;          // bytes of W per stage
 constexpr int kXWarp = 2;
 constexpr int kFirstEpiWarp = 3;
 constexpr int kWarpStaging = 32 * 32 * 4; // a warp's store boxes: one of 32 x 32 fp32, or two of bf16
+constexpr int kMaxSplit = 8;              // CTAs that share a tile's contraction (a portable cluster)
 constexpr int kBand = 8;                  // token tiles that walk the channels together
 
 struct Int8Params {
@@ -95,6 +96,10 @@ __device__ __forceinline__ uint32_t cluster_nctarank() {
 __device__ __forceinline__ void mbar_arrive_leader(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
+// meets the other CTAs without waiting for this one's stores to global memory
+__device__ __forceinline__ void cluster_sync_relaxed() {
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 __device__ __forceinline__ int ld_shared_cluster(uint32_t cluster_addr) {
   int v;
   asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(cluster_addr) : "memory");
@@ -112,19 +117,11 @@ __device__ __forceinline__ void load_chunk(uint32_t taddr, uint32_t (&r)[CHUNK])
 __device__ __forceinline__ void find_groups(const Int8Params& p, int tile_rows, int* hi, int* first_tile, bool report) {
   const int lane = threadIdx.x & 31;
   const int M = static_cast<int>(p.M);
-  if (p.offsets == nullptr) {
-    if (lane == 0) {
-      hi[0] = 0; hi[1] = M;
-      first_tile[0] = 0; first_tile[1] = (M + tile_rows - 1) / tile_rows;
-    }
-    __syncwarp();
-    return;
-  }
   int carry = 0;
   bool bad = false;
   for (int e0 = 0; e0 <= p.groups; e0 += 32) {
     const int e = e0 + lane;
-    const int raw = e <= p.groups ? __ldg(p.offsets + e) : 0;
+    const int raw = e <= p.groups ? *(p.offsets + e) : 0;
     int v = min(max(raw, 0), M);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -177,6 +174,10 @@ struct Walk {
     const int width = min(kBand, token_tiles - band * kBand);
     const int c = width == kBand ? in_band / kBand : in_band / width;
     const int j = band * kBand + in_band - c * width;
+    if (p.offsets == nullptr) {
+      const int row0 = j * tile_rows;
+      return Unit{0, row0, min(tile_rows, static_cast<int>(p.M) - row0), c * tile_ch};
+    }
     int lo = 0, up = p.groups;                     // the last group whose first tile is <= j
     while (up - lo > 1) {
       const int mid = (lo + up) >> 1;
@@ -324,73 +325,101 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = PAIR || SPLIT ? cluster_ctarank() : 0u;
   const uint32_t cluster = PAIR ? 2u : (SPLIT ? cluster_nctarank() : 1u);
-  if (threadIdx.x == 0) {
-    // on a pair the leader's barriers count both CTAs
-    for (int s = 0; s < ES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), (PAIR ? 2 : 1) * C::epi_warps); }
-    *abort_flag = 0;
-    fence_barrier_init();
-    fence_proxy_async();
-    tma_prefetch_desc(&tm_w); tma_prefetch_desc(&tm_x);
-    if (C::part_rows < C::x_rows) tma_prefetch_desc(&tm_x_part);
-    if (p.z_tma) tma_prefetch_desc(&tm_z);
-  }
-  if (warp == 1) {
+  // this CTA's share of a tile's contraction
+  const int kb_first = SPLIT ? static_cast<int>(static_cast<long long>(p.num_kb) * rank / cluster) : 0;
+  const int kb_end = SPLIT ? static_cast<int>(static_cast<long long>(p.num_kb) * (rank + 1) / cluster) : p.num_kb;
+  const int by = static_cast<int>(gridDim.x / cluster), first = static_cast<int>(blockIdx.x / cluster);
+  auto unit_of = [&](const Walk& w) { return w.unit(p, BT, PAIR ? 2 * kCh : kCh, hi, first_tile); };
+  // copies of the tokens that a tile takes (one for a full tile: a quarter of the size is a quarter slower), and
+  // the bytes of a stage of this CTA
+  auto token_parts = [&](const Unit& v) {
+    return ((PAIR ? (v.rows + 31) / 32 * 16 : v.rows) + C::part_rows - 1) / C::part_rows;
+  };
+  // the weights of a stage; counts the bytes of its tokens too
+  auto w_copy = [&](const Unit& v, int kb, uint32_t s) {
+    const uint32_t bytes = kSlab + token_parts(v) * C::part_rows * kBk;
+    const uint32_t dst = base + s * C::stage_bytes;
+    if constexpr (PAIR) {
+      if (rank == 0) mbar_arrive_expect_tx(full(s), 2 * bytes);        // both CTAs' bytes
+      tma_pair_load_3d(dst, &tm_w, mapa_shared(full(s), 0), kb * kBk, v.ch0 + static_cast<int>(rank) * kCh, v.group);
+    } else {
+      mbar_arrive_expect_tx(full(s), bytes);
+      tma_load_3d(dst, &tm_w, full(s), kb * kBk, v.ch0, v.group);
+    }
+  };
+
+  // (Loads in this file are plain ones: a load marked as read-only may be moved ahead of the wait for the kernel
+  // that writes what it reads.)
+  // Weights, offsets and channel scales may be read before the preceding kernel has ended when that kernel is
+  // this call's own quantizer (which started after all earlier ones had ended); its codes and scales may not
+  int w_ahead = 0;             // stages of the first tile whose weights are on their way already
+  if (!p.early) pdl_wait();
+  if (warp == 0) {
+    if (lane == 0) {
+      // on a pair the leader's barriers count both CTAs
+      for (int s = 0; s < ES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+      for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), (PAIR ? 2 : 1) * C::epi_warps); }
+      *abort_flag = 0;
+      fence_barrier_init();
+      fence_proxy_async();
+      // a single group needs no search: the weights start before the rest of the CTA is set up
+      if (!PAIR && p.offsets == nullptr) {
+        const Walk w(p, static_cast<int>((p.M + BT - 1) / BT), first, by);
+        if (w.more()) {
+          const Unit v = unit_of(w);
+          w_ahead = min(kb_end - kb_first, ES);
+          for (int i = 0; i < w_ahead; ++i) w_copy(v, kb_first + i, i);
+        }
+      }
+    }
+  } else if (warp == 1) {
     if constexpr (PAIR) { tmem_alloc_pair(base + C::tmem_slot, C::tmem_cols); tmem_relinquish_pair(); }
     else { tmem_alloc(base + C::tmem_slot, C::tmem_cols); tmem_relinquish(); }
+  } else if (warp == kFirstEpiWarp) {
+    if (p.offsets) find_groups(p, BT, hi, first_tile, blockIdx.x == 0);
+    if (lane == 0 && p.z_tma) tma_prefetch_desc(&tm_z);
   }
-  // weights, offsets and channel scales may be read before the preceding kernel has ended when that kernel is
-  // this call's own quantizer (which started after all earlier ones had ended); its codes and scales may not
-  if (!p.early) pdl_wait();
   pdl_trigger();
-  if (warp == kFirstEpiWarp) find_groups(p, BT, hi, first_tile, blockIdx.x == 0);
   tc_fence_before();
-  if constexpr (PAIR || SPLIT) cluster_sync_all();     // both CTAs' barriers are set up
+  __syncwarp();
+  if constexpr (PAIR) cluster_sync_all();              // both CTAs' barriers are set up
   else __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   // the tiles of this cluster: every (number of clusters)-th
-  Walk walk(p, first_tile[p.groups], static_cast<int>(blockIdx.x / cluster), static_cast<int>(gridDim.x / cluster));
-  auto unit_of = [&](const Walk& w) { return w.unit(p, BT, PAIR ? 2 * kCh : kCh, hi, first_tile); };
-  // this CTA's share of a tile's contraction
-  const int kb_first = SPLIT ? static_cast<int>(static_cast<long long>(p.num_kb) * rank / cluster) : 0;
-  const int kb_end = SPLIT ? static_cast<int>(static_cast<long long>(p.num_kb) * (rank + 1) / cluster) : p.num_kb;
+  Walk walk(p, p.offsets ? first_tile[p.groups] : static_cast<int>((p.M + BT - 1) / BT), first, by);
+  const bool idle = !walk.more();
 
   // ---- the roles, a unit at a time; state lives across units ----
   uint32_t stage = 0, phase = 0, issued = 0, it = 0;
   bool ok = true, waited = !p.early;
 
-  // one thread fetches the weights, another the tokens (two threads pull more than one); the first counts both
-  // on the stage's barrier
+  // one thread fetches the weights, another the tokens (two threads pull more than one)
   auto produce = [&](const Unit& v, bool tokens) {
     // token rows of this CTA: all of the tile's, or on a pair its half of the instruction's extent
-    const int half = (v.rows + 31) / 32 * 16;
-    const int x_row0 = v.row0 + (PAIR ? static_cast<int>(rank) * half : 0);
-    // one copy for a full tile's rows (a quarter of the size is a quarter slower), else as many as it takes
-    const int parts = ((PAIR ? half : v.rows) + C::part_rows - 1) / C::part_rows;
+    const int x_row0 = v.row0 + (PAIR ? static_cast<int>(rank) * ((v.rows + 31) / 32 * 16) : 0);
+    const int parts = token_parts(v);
     const bool whole = parts * C::part_rows == C::x_rows;
-    const uint32_t bytes = kSlab + parts * C::part_rows * kBk;
-    const int ch0 = v.ch0 + (PAIR ? static_cast<int>(rank) * kCh : 0);
     for (int kb = kb_first; kb < kb_end; ++kb) {
       if (!mbar_wait(empty(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
-      const uint32_t dst = base + stage * C::stage_bytes;
-      const uint32_t bar = PAIR ? mapa_shared(full(stage), 0) : full(stage);
       if (!tokens) {
-        if (!PAIR) mbar_arrive_expect_tx(bar, bytes);
-        else if (rank == 0) mbar_arrive_expect_tx(full(stage), 2 * bytes);   // both CTAs' bytes
-        if constexpr (PAIR) tma_pair_load_3d(dst, &tm_w, bar, kb * kBk, ch0, v.group);
-        else tma_load_3d(dst, &tm_w, bar, kb * kBk, ch0, v.group);
-        ++issued;
-      } else if (whole) {
-        if constexpr (PAIR) tma_pair_load_2d(dst + kSlab, &tm_x, bar, kb * kBk, x_row0);
-        else tma_load_2d(dst + kSlab, &tm_x, bar, kb * kBk, x_row0);
+        if (w_ahead > 0) --w_ahead;
+        else w_copy(v, kb, stage);
       } else {
-        for (int b = 0; b < parts; ++b) {
-          const int off = b * C::part_rows;
-          if constexpr (PAIR) tma_pair_load_2d(dst + kSlab + off * kBk, &tm_x_part, bar, kb * kBk, x_row0 + off);
-          else tma_load_2d(dst + kSlab + off * kBk, &tm_x_part, bar, kb * kBk, x_row0 + off);
+        const uint32_t dst = base + stage * C::stage_bytes + kSlab;
+        const uint32_t bar = PAIR ? mapa_shared(full(stage), 0) : full(stage);
+        if (whole) {
+          if constexpr (PAIR) tma_pair_load_2d(dst, &tm_x, bar, kb * kBk, x_row0);
+          else tma_load_2d(dst, &tm_x, bar, kb * kBk, x_row0);
+        } else {
+          for (int b = 0; b < parts; ++b) {
+            const int off = b * C::part_rows;
+            if constexpr (PAIR) tma_pair_load_2d(dst + off * kBk, &tm_x_part, bar, kb * kBk, x_row0 + off);
+            else tma_load_2d(dst + off * kBk, &tm_x_part, bar, kb * kBk, x_row0 + off);
+          }
         }
       }
+      ++issued;
       if (++stage == static_cast<uint32_t>(ES)) { stage = 0; phase ^= 1u; }
     }
   };
@@ -444,11 +473,11 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     const int ch = v.ch0 + (warp & 3) * 32 + lane;
     const bool ch_in = ch < p.N;
     const long long wi = static_cast<long long>(v.group) * p.N + ch;
-    sw_ahead = ch_in ? __ldg(p.sw + wi) : 0.0f;
-    bias_ahead = ch_in && p.bias ? __ldg(p.bias + wi) : 0.0f;
+    sw_ahead = ch_in ? *(p.sw + wi) : 0.0f;
+    bias_ahead = ch_in && p.bias ? *(p.bias + wi) : 0.0f;
     if (!waited) { pdl_wait(); waited = true; }
     const int t = threadIdx.x - 32 * kFirstEpiWarp;
-    if (t < v.rows) s_ahead = __ldg(p.sx + v.row0 + t);
+    if (t < v.rows) s_ahead = *(p.sx + v.row0 + t);
   };
   // the tile two before has been written by all warps once this one meets them here
   auto share_scales = [&]() {
@@ -537,22 +566,26 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         const int ch = v.ch0 + (warp & 3) * 32 + lane;
         for (int t = static_cast<int>(rank) + (warp_e >> 2) * static_cast<int>(cluster); t < v.rows;
              t += static_cast<int>(cluster) * (C::epi_warps / 4)) {
+          if (ch >= p.N) continue;     // every load below is used, and so has ended, before the meeting after it
           const uint32_t at = smem_u32(partial + t * kCh + (warp & 3) * 32 + lane);
+          int part[kMaxSplit];         // all on their way at once
+#pragma unroll
+          for (int q = 0; q < kMaxSplit; ++q) part[q] = q < static_cast<int>(cluster) ? ld_shared_cluster(mapa_shared(at, q)) : 0;
           int sum = 0;
-          for (uint32_t q = 0; q < cluster; ++q) sum += ld_shared_cluster(mapa_shared(at, q));
-          if (ch < p.N)
-            store_z(p.z, (static_cast<long long>(v.row0) + t) * p.ld_z + ch,
-                    fmaf(static_cast<float>(sum) * sw_ahead, s[t], bias_ahead), BF16);
+#pragma unroll
+          for (int q = 0; q < kMaxSplit; ++q) sum += part[q];
+          store_z(p.z, (static_cast<long long>(v.row0) + t) * p.ld_z + ch, fmaf(static_cast<float>(sum) * sw_ahead, s[t], bias_ahead), BF16);
         }
       }
-      cluster_sync_all();              // and has been read by all
+      __syncwarp();
+      cluster_sync_relaxed();          // and has been read by all
     }
     if (warp == 0 && lane == 0) drain();
   }
 
   // a CTA without tiles has waited for nothing yet: what comes after this kernel relies on the preceding one
   // having ended too
-  if (p.early) pdl_wait();
+  if (p.early && idle) pdl_wait();
   tc_fence_before();
   __syncwarp();
   if constexpr (PAIR) cluster_sync_all();              // neither CTA leaves while the other's copies or arrivals need it
@@ -595,15 +628,19 @@ int encode_z(void* fn, CUtensorMap* map, void* ptr, int64_t cols, int64_t rows, 
 }
 
 template <int BT, bool PAIR, bool SPLIT, bool BF16>
-int launch(luq_ctx* ctx, const luq_int8_args& a, const Int8Params& p, long long units, int cluster, const CUtensorMap& tw,
+int launch(luq_ctx* ctx, const luq_int8_args& a, const Int8Params& p, long long units, int cluster,
            const CUtensorMap& tz, cudaStream_t st) {
   using C = Cfg<BT, PAIR>;
-  CUtensorMap tx, tx_part;
+  CUtensorMap tw, tx, tx_part;
+  if (encode_codes(ctx->encode_tiled, &tw, a.w_codes, a.K, a.N, a.ld_w, a.groups, a.w_stride, kCh)) return LUQ_ERR_CUDA;
   if (encode_codes(ctx->encode_tiled, &tx, a.x_codes, a.K, a.M, a.ld_x, 0, 0, C::x_rows)) return LUQ_ERR_CUDA;
   if (C::part_rows == C::x_rows) tx_part = tx;
   else if (encode_codes(ctx->encode_tiled, &tx_part, a.x_codes, a.K, a.M, a.ld_x, 0, 0, C::part_rows)) return LUQ_ERR_CUDA;
   auto kernel = int8_gemm_kernel<BT, PAIR, SPLIT, BF16>;
-  const cudaError_t attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem_bytes(LUQ_MAX_GROUPS));
+  static luq_once_per_device allowed;
+  const cudaError_t attr = allowed([&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem_bytes(LUQ_MAX_GROUPS));
+  }, ctx->device);
   if (attr != cudaSuccess) return static_cast<int>(attr);
   const int sms = (ctx->sm_limit > 0 && ctx->sm_limit < ctx->sm_count) ? ctx->sm_limit : ctx->sm_count;
   const long long most = sms / cluster > 0 ? sms / cluster : 1;
@@ -614,10 +651,10 @@ int launch(luq_ctx* ctx, const luq_int8_args& a, const Int8Params& p, long long 
   return static_cast<int>(e);
 }
 template <int BT, bool PAIR, bool SPLIT>
-int launch_out(luq_ctx* ctx, const luq_int8_args& a, const Int8Params& p, long long units, int cluster, const CUtensorMap& tw,
+int launch_out(luq_ctx* ctx, const luq_int8_args& a, const Int8Params& p, long long units, int cluster,
                const CUtensorMap& tz, cudaStream_t st) {
-  return a.out_bf16 ? launch<BT, PAIR, SPLIT, true>(ctx, a, p, units, cluster, tw, tz, st)
-                    : launch<BT, PAIR, SPLIT, false>(ctx, a, p, units, cluster, tw, tz, st);
+  return a.out_bf16 ? launch<BT, PAIR, SPLIT, true>(ctx, a, p, units, cluster, tz, st)
+                    : launch<BT, PAIR, SPLIT, false>(ctx, a, p, units, cluster, tz, st);
 }
 
 }  // namespace
@@ -630,13 +667,8 @@ int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, bool early, cudaS
   const int64_t esize = a.out_bf16 ? 2 : 4;
   p.z_tma = (reinterpret_cast<uintptr_t>(a.z) & 15u) == 0 && (a.ld_z * esize) % 16 == 0;
   p.tma_cols = a.N / (16 / esize) * (16 / esize);
-  CUtensorMap tw, tz;
-  if (encode_codes(ctx->encode_tiled, &tw, a.w_codes, a.K, a.N, a.ld_w, a.groups, a.w_stride, kCh)) return LUQ_ERR_CUDA;
-  if (p.z_tma) {
-    if (encode_z(ctx->encode_tiled, &tz, a.z, a.N, a.M, a.ld_z, a.out_bf16 != 0)) return LUQ_ERR_CUDA;
-  } else {
-    tz = tw;                                          // not used
-  }
+  CUtensorMap tz{};                                   // not used where copies cannot address the output
+  if (p.z_tma && encode_z(ctx->encode_tiled, &tz, a.z, a.N, a.M, a.ld_z, a.out_bf16 != 0)) return LUQ_ERR_CUDA;
   // most tiles there can be: at most one partial token tile per group that has rows
   const long long used = p.groups < a.M ? p.groups : a.M;
   auto units = [&](int tile_rows, int tile_ch) {
@@ -646,14 +678,14 @@ int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, bool early, cudaS
   const int sms = (ctx->sm_limit > 0 && ctx->sm_limit < ctx->sm_count) ? ctx->sm_limit : ctx->sm_count;
   const long long mean_rows = (a.M + used - 1) / used;
   long long n = units(256, 2 * kCh);
-  if (sms >= 2 && mean_rows >= 192 && n >= sms / 2) return launch_out<256, true, false>(ctx, a, p, n, 2, tw, tz, st);
+  if (sms >= 2 && mean_rows >= 192 && n >= sms / 2) return launch_out<256, true, false>(ctx, a, p, n, 2, tz, st);
   n = units(128, kCh);
-  if (mean_rows > 64 && n >= sms) return launch_out<128, false, false>(ctx, a, p, n, 1, tw, tz, st);
+  if (mean_rows > 64 && n >= sms) return launch_out<128, false, false>(ctx, a, p, n, 1, tz, st);
   const bool narrow = mean_rows <= 16;
   n = narrow ? units(16, kCh) : units(64, kCh);
   int split = 1;
-  while (split < 8 && n * split * 2 <= sms && split * 2 <= p.num_kb) split *= 2;
-  if (split > 1) return narrow ? launch_out<16, false, true>(ctx, a, p, n, split, tw, tz, st)
-                               : launch_out<64, false, true>(ctx, a, p, n, split, tw, tz, st);
-  return narrow ? launch_out<16, false, false>(ctx, a, p, n, 1, tw, tz, st) : launch_out<64, false, false>(ctx, a, p, n, 1, tw, tz, st);
+  while (split < kMaxSplit && n * split * 2 <= sms && split * 2 <= p.num_kb) split *= 2;
+  if (split > 1) return narrow ? launch_out<16, false, true>(ctx, a, p, n, split, tz, st)
+                               : launch_out<64, false, true>(ctx, a, p, n, split, tz, st);
+  return narrow ? launch_out<16, false, false>(ctx, a, p, n, 1, tz, st) : launch_out<64, false, false>(ctx, a, p, n, 1, tz, st);
 }

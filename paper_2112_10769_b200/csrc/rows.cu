@@ -38,7 +38,7 @@ struct RowParams {
   bool vec_params, vec_y;   // gamma and beta, and the rows of y, are 16-byte aligned
 };
 
-__device__ __forceinline__ float load1(const float* p) { return __ldg(p); }
+__device__ __forceinline__ float load1(const float* p) { return *(p); }
 __device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ float load1_any(const float* p) { return *p; }              // shared or global memory
 __device__ __forceinline__ float load1_any(const __nv_bfloat16* p) { return __bfloat162float(*p); }
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(512) row_loop_kernel(const RowParams p) {
       float v = load1(x + c);
       if (MODE != kInt8) {
         v = ((v - mean0) - shift) * rstd;
-        v = fmaf(v, p.gamma ? __ldg(p.gamma + c) : 1.0f, p.beta ? __ldg(p.beta + c) : 0.0f);
+        v = fmaf(v, p.gamma ? *(p.gamma + c) : 1.0f, p.beta ? *(p.beta + c) : 0.0f);
       }
       return v;
     };
@@ -206,12 +206,12 @@ __device__ __forceinline__ void load_params(const float* g, bool vec, int c, int
   } else if (FULL || (vec && c + V <= cols)) {
 #pragma unroll
     for (int i = 0; i < V; i += 4) {
-      const float4 f = __ldg(reinterpret_cast<const float4*>(g + c + i));
+      const float4 f = *(reinterpret_cast<const float4*>(g + c + i));
       v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = c + i < cols ? __ldg(g + c + i) : 0.0f;
+    for (int i = 0; i < V; ++i) v[i] = c + i < cols ? *(g + c + i) : 0.0f;
   }
 }
 
@@ -390,7 +390,7 @@ struct Rows {
           raw[t][j] = make_uint4(0u, 0u, 0u, 0u);
           if (r < rows) {
             if (FULL || c + V <= cols) {
-              raw[t][j] = __ldg(reinterpret_cast<const uint4*>(row + c));
+              raw[t][j] = *(reinterpret_cast<const uint4*>(row + c));
             } else {
               float v[V];
 #pragma unroll
@@ -669,10 +669,10 @@ __global__ void __launch_bounds__(512) norm_bwd_means_kernel(const NormBwdParams
   for (long long r = blockIdx.x; r < p.rows; r += gridDim.x) {
     const T* const x = static_cast<const T*>(p.x) + r * p.ld_x;
     const T* const dy = static_cast<const T*>(p.dy) + r * p.ld_dy;
-    const float mean = __ldg(p.mean + r), rstd = __ldg(p.rstd + r);
+    const float mean = *(p.mean + r), rstd = *(p.rstd + r);
     float s1 = 0.0f, s2 = 0.0f;
     for (int c = threadIdx.x; c < p.cols; c += blockDim.x) {
-      const float g = load1(dy + c) * (p.gamma ? __ldg(p.gamma + c) : 1.0f);
+      const float g = load1(dy + c) * (p.gamma ? *(p.gamma + c) : 1.0f);
       s1 += g;
       s2 = fmaf(g, (load1(x + c) - mean) * rstd, s2);
     }
@@ -691,12 +691,12 @@ __global__ void __launch_bounds__(256) norm_bwd_columns_kernel(const NormBwdPara
   const long long chunk = blockIdx.x / column_tiles;
   if (c64 >= p.cols) return;
   const int c = static_cast<int>(c64);
-  const float w = p.gamma ? __ldg(p.gamma + c) : 1.0f;
+  const float w = p.gamma ? *(p.gamma + c) : 1.0f;
   const long long r0 = chunk * p.rows_per_chunk;
   const long long r1 = r0 + p.rows_per_chunk < p.rows ? r0 + p.rows_per_chunk : p.rows;
   float dgamma = 0.0f, dbeta = 0.0f;
   for (long long r = r0; r < r1; ++r) {
-    const float mean = __ldg(p.mean + r), rstd = __ldg(p.rstd + r);
+    const float mean = *(p.mean + r), rstd = *(p.rstd + r);
     const float dy = load1(static_cast<const T*>(p.dy) + r * p.ld_dy + c);
     const float xhat = (load1(static_cast<const T*>(p.x) + r * p.ld_x + c) - mean) * rstd;
     dgamma = fmaf(dy, xhat, dgamma);
@@ -748,12 +748,12 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
   for (int i = 0; i < EPT; ++i) dgamma[i] = dbeta[i] = 0.0f;
   int parity = 0;
   float mean = 0.0f, rstd = 0.0f;
-  if (first < p.rows) { mean = __ldg(p.mean + first); rstd = __ldg(p.rstd + first); }
+  if (first < p.rows) { mean = *(p.mean + first); rstd = *(p.rstd + first); }
   for (long long r = first; r - g.sub() < p.rows; r += step, parity ^= 1) {
     // the next row's mean and 1/std are on their way while this row is worked on
     const long long after = r + step;
     float next_mean = 0.0f, next_rstd = 0.0f;
-    if (after < p.rows) { next_mean = __ldg(p.mean + after); next_rstd = __ldg(p.rstd + after); }
+    if (after < p.rows) { next_mean = *(p.mean + after); next_rstd = *(p.rstd + after); }
     float s1[2] = {0.0f, 0.0f}, s2[2] = {0.0f, 0.0f};
     // beyond a row's end dy is zero: nothing is added
     auto gather = [&](float& x, float& dy, float weight, float& dg, float& db, int i) {
@@ -870,7 +870,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
 }
 
 // adds the chunks' partial sums in a fixed order: 32 columns by 32 strands per block, four loads in flight each
-__global__ void __launch_bounds__(1024) norm_bwd_reduce_kernel(const float* __restrict__ partial, int chunks, int cols,
+__global__ void __launch_bounds__(1024) norm_bwd_reduce_kernel(const float* partial, int chunks, int cols,
                                                                float* dgamma, float* dbeta) {
   __shared__ float box[32][33];
   pdl_wait();
@@ -905,8 +905,8 @@ constexpr int kRingBytes = 66 * 1024;      // of a block of the forward kernels:
 constexpr int kRingBytesAlone = 190 * 1024;
 
 template <typename K>
-cudaError_t allow_smem(K kernel) {
-  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+cudaError_t allow_smem(K kernel, luq_once_per_device& once, int device) {
+  return once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024); }, device);
 }
 // stages of a ring: as many as fit, eight at most, two if two do fit an SM (one row of x and dy may be 128 KB)
 int ring_depth_for(int groups, int stage_bytes, int budget) {
@@ -936,7 +936,8 @@ cudaError_t launch_row(luq_ctx* ctx, const RowParams& p, bool vec, cudaStream_t 
   const bool full = LOAD != kBounce && vec && p.cols == G * EPT && (MODE == kInt8 || (p.gamma && p.beta));
   auto kernel = full ? row_kernel<T, MODE, EPT, LOAD, LOAD != kBounce, NARROW> : row_kernel<T, MODE, EPT, LOAD, false, NARROW>;
   if (LOAD == kRing) {
-    const cudaError_t e = allow_smem(kernel);
+    static luq_once_per_device once[2];
+    const cudaError_t e = allow_smem(kernel, once[full], ctx->device);
     if (e != cudaSuccess) return e;
   }
   const long long blocks = (p.rows + groups - 1) / groups;
@@ -970,7 +971,7 @@ int launch_rows(luq_ctx* ctx, RowParams p, cudaStream_t st) {
 }
 
 template <typename T, int EPT, int LOAD, bool NARROW>
-cudaError_t launch_norm_bwd_rows(const NormBwdParams& p, bool vec, int G, int block, int grid, cudaStream_t st) {
+cudaError_t launch_norm_bwd_rows(int device, const NormBwdParams& p, bool vec, int G, int block, int grid, cudaStream_t st) {
   const int groups = block / G;
   using R = Rows<T, 2, 16, LOAD, false, NARROW>;
   const int depth = LOAD == kRing ? ring_depth_for(groups, 2 * R::ring_row_bytes(p.cols), kRingBytesAlone) : 0;
@@ -980,7 +981,8 @@ cudaError_t launch_norm_bwd_rows(const NormBwdParams& p, bool vec, int G, int bl
   constexpr bool can = LOAD != kBounce && EPT == 16;
   const bool full = can && vec && p.cols == G * EPT && p.gamma;
   auto kernel = full ? norm_bwd_kernel<T, EPT, LOAD, can, NARROW> : norm_bwd_kernel<T, EPT, LOAD, false, NARROW>;
-  const cudaError_t e = allow_smem(kernel);
+  static luq_once_per_device once[2];
+  const cudaError_t e = allow_smem(kernel, once[full], device);
   if (e != cudaSuccess) return e;
   return luq_launch_kernel(kernel, grid, block, ring > sums ? ring : sums, st, LUQ_LAUNCH_EARLY, 1, p, G, depth);
 }
@@ -1005,12 +1007,12 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
     p.partial = dgamma || dbeta ? ctx->d_workspace : nullptr;
     p.chunks = static_cast<int>(blocks);
     const bool ring = p.dx != nullptr && p.rows >= 4 * blocks * groups;
-    if (ept == 32) e = launch_norm_bwd_rows<T, 32, kRing, false>(p, vec, G, block, p.chunks, st);
-    else if (p.cols <= 512) e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, true>(p, vec, G, block, p.chunks, st)
-                                       : launch_norm_bwd_rows<T, 16, kBounce, true>(p, vec, G, block, p.chunks, st);
-    else if (ring) e = launch_norm_bwd_rows<T, 16, kRing, false>(p, vec, G, block, p.chunks, st);
-    else e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, false>(p, vec, G, block, p.chunks, st)
-                    : launch_norm_bwd_rows<T, 16, kBounce, false>(p, vec, G, block, p.chunks, st);
+    if (ept == 32) e = launch_norm_bwd_rows<T, 32, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
+    else if (p.cols <= 512) e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, true>(ctx->device, p, vec, G, block, p.chunks, st)
+                                       : launch_norm_bwd_rows<T, 16, kBounce, true>(ctx->device, p, vec, G, block, p.chunks, st);
+    else if (ring) e = launch_norm_bwd_rows<T, 16, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
+    else e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, false>(ctx->device, p, vec, G, block, p.chunks, st)
+                    : launch_norm_bwd_rows<T, 16, kBounce, false>(ctx->device, p, vec, G, block, p.chunks, st);
   } else {
     // workspace: two floats per row, then the chunks' partial sums
     const size_t means = ((static_cast<size_t>(p.rows) * sizeof(float2) + 255) / 256) * 256;
