@@ -354,6 +354,7 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   // this call's own quantizer (which started after all earlier ones had ended); its codes and scales may not
   int w_ahead = 0;             // stages of the first tile whose weights are on their way already
   if (!p.early) pdl_wait();
+  pdl_trigger();
   if (warp == 0) {
     if (lane == 0) {
       // on a pair the leader's barriers count both CTAs
@@ -379,7 +380,6 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     if (p.offsets) find_groups(p, BT, hi, first_tile, blockIdx.x == 0);
     if (lane == 0 && p.z_tma) tma_prefetch_desc(&tm_z);
   }
-  pdl_trigger();
   tc_fence_before();
   __syncwarp();
   if constexpr (PAIR) cluster_sync_all();              // both CTAs' barriers are set up

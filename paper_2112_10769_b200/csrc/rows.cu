@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(512) row_loop_kernel(const RowParams p) {
 //            that start inside a 16-byte piece are copied with the pieces around them and shifted into place.
 //   kDirect  16-byte loads into registers, one row ahead
 //   kBounce  the same for rows that do not start at multiples of 16 bytes: element by element, coalesced,
-//            and through 512 bytes of shared memory per warp to their owners
+//            and through shared memory to their owners in the same warp
 // An element has the same owner in all three, and sums are made in the same order: results do not depend on
 // strides, alignment or the number of rows.
 constexpr int kRing = 0, kDirect = 1, kBounce = 2;
@@ -173,6 +173,9 @@ template <typename T>
 struct Piece {
   static constexpr int V = 16 / static_cast<int>(sizeof(T));
 };
+// pieces per thread that pass through a warp's shared memory together (16 elements: 2 KB of fp32, 1 KB of bf16)
+template <typename T>
+constexpr int kBouncePieces = 16 / Piece<T>::V;
 __device__ __forceinline__ void unpack(const uint4& w, const float*, float* v) {
   v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
 }
@@ -415,9 +418,9 @@ struct Rows {
   }
   __device__ __forceinline__ void start(long long first) {
     if constexpr (LOAD == kRing) {
-      if (tid == 0)
-        for (int s = 0; s < depth; ++s)
-          if (first + s * step < rows) fill(s, first + s * step);
+      if (tid < depth && first + tid * step < rows) fill(tid, first + tid * step);
+      issued = 0;
+      while (issued < depth && first + issued * step < rows) ++issued;
     } else {
       fetch(first);
     }
@@ -461,15 +464,19 @@ struct Rows {
       const int lane = threadIdx.x & 31, width = NARROW ? G : 32, l = lane & (width - 1);
       T* const b = reinterpret_cast<T*>(wbuf) + (lane - l) * V;
 #pragma unroll
-      for (int t = 0; t < TENSORS; ++t)
+      for (int t = 0; t < TENSORS; ++t) {
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) {
+        for (int j0 = 0; j0 < VPT; j0 += kBouncePieces<T>) {
 #pragma unroll
-          for (int i = 0; i < V; ++i) b[i * width + l] = single[t][j * V + i];
+          for (int j = 0; j < kBouncePieces<T>; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) b[j * 32 * V + i * width + l] = single[t][(j0 + j) * V + i];
           __syncwarp();
-          unpack(wbuf[lane], base[0], v[t] + j * V);
+#pragma unroll
+          for (int j = 0; j < kBouncePieces<T>; ++j) unpack(wbuf[j * 32 + lane], base[0], v[t] + (j0 + j) * V);
           __syncwarp();
         }
+      }
       fetch(r + step);
     }
   }
@@ -491,47 +498,63 @@ struct Rows {
   }
 };
 
-// writes V elements of a row; `vec`: the row starts at a multiple of 16 bytes (else through the warp's 512 bytes)
-template <typename T, bool FULL, bool NARROW>
-__device__ __forceinline__ void store_piece(T* row, bool exists, bool vec, int tid, int G, int j, int cols, uint4* wbuf,
-                                            const float* v) {
-  constexpr int V = Piece<T>::V;
-  const int c = (tid + j * G) * V;
+// writes a thread's elements of a row; `vec`: the row starts at a multiple of 16 bytes (else through the warp's
+// shared memory, as kBounce reads)
+template <typename T, int EPT, bool FULL, bool NARROW>
+__device__ __forceinline__ void store_row(T* row, bool exists, bool vec, int tid, int G, int cols, uint4* wbuf, const float* v) {
+  constexpr int V = Piece<T>::V, VPT = EPT / V;
   if (FULL || vec) {
     if (!exists) return;
-    if (FULL || c + V <= cols) {
-      *reinterpret_cast<uint4*>(row + c) = pack(v, row);
-    } else {
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (c + i < cols) store1(row + c + i, v[i]);
+    for (int j = 0; j < VPT; ++j) {
+      const int c = (tid + j * G) * V;
+      if (FULL || c + V <= cols) {
+        *reinterpret_cast<uint4*>(row + c) = pack(v + j * V, row);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (c + i < cols) store1(row + c + i, v[j * V + i]);
+      }
     }
   } else {
+    constexpr int P = VPT < kBouncePieces<T> ? VPT : kBouncePieces<T>;
     const int lane = threadIdx.x & 31, width = NARROW ? G : 32, l = lane & (width - 1);
     const T* const b = reinterpret_cast<const T*>(wbuf) + (lane - l) * V;
-    const int c0 = (tid - l + j * G) * V;
-    wbuf[lane] = pack(v, row);
-    __syncwarp();
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (exists && c0 + i * width + l < cols) row[c0 + i * width + l] = b[i * width + l];
-    __syncwarp();
+    for (int j0 = 0; j0 < VPT; j0 += P) {
+#pragma unroll
+      for (int j = 0; j < P; ++j) wbuf[j * 32 + lane] = pack(v + (j0 + j) * V, row);
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < P; ++j) {
+        const int c0 = (tid - l + (j0 + j) * G) * V + l;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (exists && c0 + i * width < cols) row[c0 + i * width] = b[j * 32 * V + i * width + l];
+      }
+      __syncwarp();
+    }
   }
 }
 
+// blocks of a row kernel that share an SM, by the registers they need without spilling
+template <int MODE, int EPT, int LOAD, bool FULL>
+constexpr int kRowBlocks = EPT == 32 ? 1 : FULL || MODE == kInt8 || (MODE == kNormInt8 && LOAD == kRing) ? 3 : 2;
+
 // FULL: every thread has EPT elements, and all is aligned and there: no test per piece (a third of the instructions)
 template <typename T, int MODE, int EPT, int LOAD, bool FULL, bool NARROW>
-__global__ void __launch_bounds__(EPT == 16 ? 256 : 512, EPT == 16 ? 3 : 1) row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
+__global__ void __launch_bounds__(EPT == 16 ? 256 : 512, kRowBlocks<MODE, EPT, LOAD, FULL>) row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
   constexpr int V = Piece<T>::V, VPT = EPT / V;
   // one box per reduction of a row; without the norm a row has one reduction only and uses two in turn
   __shared__ float sum_box[16];
   __shared__ float sum2_box[32];
   __shared__ unsigned int max_box[2][16];
-  __shared__ uint4 move[FULL ? 1 : (EPT == 16 ? 8 : 16)][32];
+  constexpr bool MOVES = !FULL && (MODE == kNorm || LOAD == kBounce);
+  __shared__ uint4 move[MOVES ? (EPT == 16 ? 8 : 16) : 1][MOVES ? 32 * kBouncePieces<T> : 1];
   extern __shared__ __align__(128) uint8_t ring_smem[];
   const Group<NARROW> g(threads_per_row);
   const int groups = blockDim.x / g.G, slot = g.index * g.warps, tid = g.tid, G = g.G, C = p.cols;
-  uint4* const wbuf = move[FULL ? 0 : threadIdx.x >> 5];
+  uint4* const wbuf = move[MOVES ? threadIdx.x >> 5 : 0];
   Rows<T, 1, EPT, LOAD, FULL, NARROW> in;
   in.base[0] = static_cast<const T*>(p.x); in.ld[0] = p.ld_x; in.rows = p.rows; in.cols = C; in.tid = tid; in.G = G;
   in.step = static_cast<long long>(gridDim.x) * groups;
@@ -594,13 +617,15 @@ __global__ void __launch_bounds__(EPT == 16 ? 256 : 512, EPT == 16 ? 3 : 1) row_
         const int c = (tid + j * G) * V;
 #pragma unroll
         for (int i = 0; i < V; ++i) v[j * V + i] = fmaf(fmaf(v[j * V + i], rstd, minus), w[j * V + i], b[j * V + i]);
-        if (MODE == kNorm) store_piece<T, FULL, NARROW>(static_cast<T*>(p.y) + r * p.ld_y, exists, p.vec_y, tid, G, j, C, wbuf, v + j * V);
+        // (a full row piece by piece: its stores leave while the next piece is computed)
+        if (MODE == kNorm && FULL && exists) *reinterpret_cast<uint4*>(static_cast<T*>(p.y) + r * p.ld_y + c) = pack(v + j * V, static_cast<const T*>(nullptr));
         if (MODE != kNorm && !FULL && c + V > C) {
 #pragma unroll
           for (int i = 0; i < V; ++i)
             if (c + i >= C) v[j * V + i] = 0.0f;
         }
       }
+      if (MODE == kNorm && !FULL) store_row<T, EPT, FULL, NARROW>(static_cast<T*>(p.y) + r * p.ld_y, exists, p.vec_y, tid, G, C, wbuf, v);
       if (MODE == kNorm && tid == 0 && exists) {
         if (p.mean) p.mean[r] = mean0 + shift;
         if (p.rstd) p.rstd[r] = rstd;
@@ -720,7 +745,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
   constexpr bool TWICE = EPT == 32;
   static_assert(!TWICE || LOAD == kRing, "a row that is read twice stays in the ring");
   __shared__ float box[2][32];
-  __shared__ uint4 move[FULL ? 1 : 16][32];
+  __shared__ uint4 move[FULL ? 1 : 16][FULL ? 1 : 32 * kBouncePieces<T>];
   extern __shared__ __align__(128) uint8_t ring_smem[];   // the ring; at the end [groups][2][cols] sums
   const Group<NARROW> g(threads_per_row);
   const int groups = blockDim.x / g.G, group = g.index, slot = g.index * g.warps, tid = g.tid, G = g.G, C = p.cols;
@@ -737,8 +762,9 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
   pdl_wait();
   pdl_trigger();
   const long long first = static_cast<long long>(blockIdx.x) * groups + group, step = in.step;
-  in.start(first);
   const float inv_c = 1.0f / C;
+  float mean = 0.0f, rstd = 0.0f;
+  if (first < p.rows) { mean = *(p.mean + first); rstd = *(p.rstd + first); }
   float dgamma[EPT], dbeta[EPT], w[TWICE ? 1 : EPT];
   if constexpr (!TWICE) {
 #pragma unroll
@@ -746,9 +772,8 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
   }
 #pragma unroll
   for (int i = 0; i < EPT; ++i) dgamma[i] = dbeta[i] = 0.0f;
+  in.start(first);
   int parity = 0;
-  float mean = 0.0f, rstd = 0.0f;
-  if (first < p.rows) { mean = *(p.mean + first); rstd = *(p.rstd + first); }
   for (long long r = first; r - g.sub() < p.rows; r += step, parity ^= 1) {
     // the next row's mean and 1/std are on their way while this row is worked on
     const long long after = r + step;
@@ -778,8 +803,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
         const float m1 = -t.x * inv_c * rstd, m2 = t.y * inv_c;
 #pragma unroll
         for (int i = 0; i < EPT; ++i) dy[i] = fmaf(fmaf(-x[i], m2, dy[i]), rstd, m1);
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) store_piece<T, FULL, NARROW>(dx, exists, p.vec_dx, tid, G, j, C, wbuf, dy + j * V);
+        store_row<T, EPT, FULL, NARROW>(dx, exists, p.vec_dx, tid, G, C, wbuf, dy);
       }
     } else {
       in.fine = in.fine && mbar_wait(in.bars + 8 * in.stage, in.phase, in.abort_flag);
@@ -820,7 +844,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
           load_params<V, FULL>(p.gamma, p.vec_gamma, c, C, 1.0f, weight);
 #pragma unroll
           for (int i = 0; i < V; ++i) dy[i] = fmaf(fmaf(-((x[i] - mean) * rstd), m2, dy[i] * weight[i]), rstd, m1);
-          store_piece<T, FULL, NARROW>(dx, in.ok(), p.vec_dx, tid, G, j, C, wbuf, dy);
+          store_row<T, V, FULL, NARROW>(dx + j * G * V, in.ok(), p.vec_dx, tid, G, C - j * G * V, wbuf, dy);
         }
       }
       g.sync();                                        // everyone has read the stage
@@ -844,28 +868,36 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
   }
   const int turns = NARROW ? blockDim.x >> 5 : groups, mine = NARROW ? threadIdx.x >> 5 : group;
   float* const sums = reinterpret_cast<float*>(ring_smem);
-  float* const to = turns == 1 ? out : sums + 2 * mine * C;
-  if (turns > 1) __syncthreads();                      // the ring is done with
+  const int Cp = (C + 3) & ~3;                         // a row of sums in shared memory
+  if (turns == 1) {
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) {
+      const int c = (tid + i / V * G) * V + i % V;
+      if (c < C) {
+        out[c] = dgamma[i];
+        out[C + c] = dbeta[i];
+      }
+    }
+    return;
+  }
+  __syncthreads();                                     // the ring is done with
   if (g.sub() == 0) {
+    float* const to = sums + 2 * mine * Cp;
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int c = (tid + j * G) * V + i;
-        if (c < C) {
-          to[c] = dgamma[j * V + i];
-          to[C + c] = dbeta[j * V + i];
-        }
+    for (int i = 0; i < EPT; i += 4) {
+      const int c = (tid + i / V * G) * V + i % V;
+      if (c < Cp) {
+        *reinterpret_cast<float4*>(to + c) = make_float4(dgamma[i], dgamma[i + 1], dgamma[i + 2], dgamma[i + 3]);
+        *reinterpret_cast<float4*>(to + Cp + c) = make_float4(dbeta[i], dbeta[i + 1], dbeta[i + 2], dbeta[i + 3]);
       }
     }
   }
-  if (turns > 1) {
-    __syncthreads();
-    for (int c = threadIdx.x; c < 2 * C; c += blockDim.x) {
-      float s = sums[c];
-      for (int k = 1; k < turns; ++k) s += sums[2 * k * C + c];
-      out[c] = s;
-    }
+  __syncthreads();
+  for (int c = threadIdx.x; c < 2 * C; c += blockDim.x) {
+    const int at = c < C ? c : Cp + c - C;
+    float s = sums[at];
+    for (int k = 1; k < turns; ++k) s += sums[2 * k * Cp + at];
+    out[c] = s;
   }
 }
 
@@ -901,12 +933,12 @@ bool aligned(const void* p, long long ld, int size) {
   return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld * size) % 16 == 0;
 }
 
-constexpr int kRingBytes = 66 * 1024;      // of a block of the forward kernels: three blocks share an SM
+constexpr int kRingBytes = 66 * 1024;      // of a block of the forward kernels: two or three blocks share an SM
 constexpr int kRingBytesAlone = 190 * 1024;
 
 template <typename K>
 cudaError_t allow_smem(K kernel, luq_once_per_device& once, int device) {
-  return once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024); }, device);
+  return once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 192 * 1024); }, device);
 }
 // stages of a ring: as many as fit, eight at most, two if two do fit an SM (one row of x and dy may be 128 KB)
 int ring_depth_for(int groups, int stage_bytes, int budget) {
@@ -930,10 +962,11 @@ cudaError_t launch_row(luq_ctx* ctx, const RowParams& p, bool vec, cudaStream_t 
   // groups share a block while every SM has some; a block has whole warps
   int groups = (EPT == 16 ? 256 : 512) / G;
   while (groups > 1 && G * groups > 32 && p.rows < static_cast<long long>(groups) * ctx->sm_count) groups >>= 1;
+  const bool full = LOAD != kBounce && vec && p.cols == G * EPT && (MODE == kInt8 || (p.gamma && p.beta));
+  const int per_sm = full ? kRowBlocks<MODE, EPT, LOAD, true> : kRowBlocks<MODE, EPT, LOAD, false>;
   const int row_bytes = Rows<T, 1, EPT, LOAD, false, NARROW>::ring_row_bytes(p.cols);
   const int depth = LOAD == kRing ? ring_depth_for(groups, row_bytes, EPT == 16 ? kRingBytes : kRingBytesAlone) : 0;
   const size_t smem = LOAD == kRing ? static_cast<size_t>(Rows<T, 1, EPT, LOAD, false, NARROW>::ring_bytes(groups, depth, p.cols)) : 0;
-  const bool full = LOAD != kBounce && vec && p.cols == G * EPT && (MODE == kInt8 || (p.gamma && p.beta));
   auto kernel = full ? row_kernel<T, MODE, EPT, LOAD, LOAD != kBounce, NARROW> : row_kernel<T, MODE, EPT, LOAD, false, NARROW>;
   if (LOAD == kRing) {
     static luq_once_per_device once[2];
@@ -941,7 +974,7 @@ cudaError_t launch_row(luq_ctx* ctx, const RowParams& p, bool vec, cudaStream_t 
     if (e != cudaSuccess) return e;
   }
   const long long blocks = (p.rows + groups - 1) / groups;
-  const long long cap = static_cast<long long>(ctx->sm_count) * (EPT == 16 ? 3 : 1) *
+  const long long cap = static_cast<long long>(ctx->sm_count) * per_sm *
                         (LOAD == kRing ? 1 : (EPT == 16 ? 256 : 512) / (G * groups));
   return luq_launch_kernel(kernel, static_cast<int>(blocks < cap ? blocks : cap), G * groups, smem, st, LUQ_LAUNCH_EARLY, 1, p, G, depth);
 }
@@ -976,7 +1009,7 @@ cudaError_t launch_norm_bwd_rows(int device, const NormBwdParams& p, bool vec, i
   using R = Rows<T, 2, 16, LOAD, false, NARROW>;
   const int depth = LOAD == kRing ? ring_depth_for(groups, 2 * R::ring_row_bytes(p.cols), kRingBytesAlone) : 0;
   const int turns = NARROW ? block / 32 : groups;
-  const size_t sums = turns > 1 ? 2 * sizeof(float) * static_cast<size_t>(p.cols) * turns : 0;
+  const size_t sums = turns > 1 ? 2 * sizeof(float) * static_cast<size_t>((p.cols + 3) & ~3) * turns : 0;
   const size_t ring = LOAD == kRing ? static_cast<size_t>(R::ring_bytes(groups, depth, p.cols)) : 0;
   constexpr bool can = LOAD != kBounce && EPT == 16;
   const bool full = can && vec && p.cols == G * EPT && p.gamma;
@@ -995,7 +1028,7 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
   p.vec_dx = aligned(p.dx, p.ld_dx, sizeof(T));
   const bool vec_in = aligned(p.x, p.ld_x, sizeof(T)) && aligned(p.dy, p.ld_dy, sizeof(T)), vec = vec_in && p.vec_gamma && p.vec_dx;
   // a row of x and one of dy have to fit the ring
-  if (p.cols <= 16384 && Rows<T, 2, 16, kRing, false, false>::ring_bytes(1, 1, p.cols) <= 200 * 1024) {
+  if (p.cols <= 16384 && Rows<T, 2, 16, kRing, false, false>::ring_bytes(1, 1, p.cols) <= 192 * 1024) {
     // as many sums of both kinds per thread as elements of a row; groups share a block while there are rows for them
     const int ept = p.cols > 8192 ? 32 : 16;
     const int G = threads_of_row(p.cols, ept);
@@ -1006,7 +1039,7 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
     if (blocks * groups > p.rows) blocks = (p.rows + groups - 1) / groups;
     p.partial = dgamma || dbeta ? ctx->d_workspace : nullptr;
     p.chunks = static_cast<int>(blocks);
-    const bool ring = p.dx != nullptr && p.rows >= 4 * blocks * groups;
+    const bool ring = p.dx != nullptr && p.rows >= 2 * blocks * groups;
     if (ept == 32) e = launch_norm_bwd_rows<T, 32, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
     else if (p.cols <= 512) e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, true>(ctx->device, p, vec, G, block, p.chunks, st)
                                        : launch_norm_bwd_rows<T, 16, kBounce, true>(ctx->device, p, vec, G, block, p.chunks, st);
