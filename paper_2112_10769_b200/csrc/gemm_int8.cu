@@ -352,34 +352,24 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   // that writes what it reads.)
   // Weights, offsets and channel scales may be read before the preceding kernel has ended when that kernel is
   // this call's own quantizer (which started after all earlier ones had ended); its codes and scales may not
-  int w_ahead = 0;             // stages of the first tile whose weights are on their way already
-  if (!p.early) pdl_wait();
-  pdl_trigger();
-  if (warp == 0) {
-    if (lane == 0) {
-      // on a pair the leader's barriers count both CTAs
-      for (int s = 0; s < ES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-      for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), (PAIR ? 2 : 1) * C::epi_warps); }
-      *abort_flag = 0;
-      fence_barrier_init();
-      fence_proxy_async();
-      // a single group needs no search: the weights start before the rest of the CTA is set up
-      if (!PAIR && p.offsets == nullptr) {
-        const Walk w(p, static_cast<int>((p.M + BT - 1) / BT), first, by);
-        if (w.more()) {
-          const Unit v = unit_of(w);
-          w_ahead = min(kb_end - kb_first, ES);
-          for (int i = 0; i < w_ahead; ++i) w_copy(v, kb_first + i, i);
-        }
-      }
-    }
-  } else if (warp == 1) {
+  if (threadIdx.x == 0) {
+    // on a pair the leader's barriers count both CTAs
+    for (int s = 0; s < ES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), (PAIR ? 2 : 1) * C::epi_warps); }
+    *abort_flag = 0;
+    fence_barrier_init();
+    fence_proxy_async();
+    tma_prefetch_desc(&tm_w); tma_prefetch_desc(&tm_x);
+    if (C::part_rows < C::x_rows) tma_prefetch_desc(&tm_x_part);
+    if (p.z_tma) tma_prefetch_desc(&tm_z);
+  }
+  if (warp == 1) {
     if constexpr (PAIR) { tmem_alloc_pair(base + C::tmem_slot, C::tmem_cols); tmem_relinquish_pair(); }
     else { tmem_alloc(base + C::tmem_slot, C::tmem_cols); tmem_relinquish(); }
-  } else if (warp == kFirstEpiWarp) {
-    if (p.offsets) find_groups(p, BT, hi, first_tile, blockIdx.x == 0);
-    if (lane == 0 && p.z_tma) tma_prefetch_desc(&tm_z);
   }
+  if (!p.early) pdl_wait();
+  pdl_trigger();
+  if (warp == kFirstEpiWarp && p.offsets) find_groups(p, BT, hi, first_tile, blockIdx.x == 0);
   tc_fence_before();
   __syncwarp();
   if constexpr (PAIR) cluster_sync_all();              // both CTAs' barriers are set up
@@ -403,8 +393,7 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     for (int kb = kb_first; kb < kb_end; ++kb) {
       if (!mbar_wait(empty(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
       if (!tokens) {
-        if (w_ahead > 0) --w_ahead;
-        else w_copy(v, kb, stage);
+        w_copy(v, kb, stage);
       } else {
         const uint32_t dst = base + stage * C::stage_bytes + kSlab;
         const uint32_t bar = PAIR ? mapa_shared(full(stage), 0) : full(stage);
