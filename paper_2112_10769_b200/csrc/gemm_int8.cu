@@ -57,13 +57,14 @@ struct Int8Params {
 // four (one per quarter of the lanes, 32 channels each); a group takes `span` tokens of the tile.
 template <int BT, bool PAIR>
 struct Cfg {
-  static constexpr int epi_warps = BT == 16 ? 4 : 8;
+  static constexpr int epi_warps = BT <= 32 ? 4 : 8;
   static constexpr int span = BT / (epi_warps / 4);
   static constexpr int threads = 32 * (kFirstEpiWarp + epi_warps);
   static constexpr int x_rows = PAIR ? BT / 2 : BT;               // token rows this CTA holds of a tile
   static constexpr int part_rows = BT < 32 ? BT : 32;             // token rows per copy of a tile that is not full
   static constexpr int stage_bytes = kSlab + x_rows * kBk;
-  static constexpr int stages = BT == 16 ? 10 : BT == 64 ? 7 : 5;
+  static constexpr int per_sm = BT <= 32 ? 2 : 1;
+  static constexpr int stages = BT == 16 ? 5 : BT == 32 ? 4 : BT == 64 ? 7 : 5;
   static constexpr int chunk = BT < 32 ? BT : 32;                 // tokens per epilogue step
   static constexpr int tmem_cols = 2 * BT;
   static constexpr int staging = stages * stage_bytes;            // store boxes, or a split's partial tile
@@ -301,7 +302,7 @@ __device__ __forceinline__ void write_tile(const Int8Params& p, const void* tm_z
 // PAIR: the two CTAs of a cluster compute a tile of 256 channels together (cta_group::2), each fetches half of
 // the tokens' rows.
 template <int BT, bool PAIR, bool SPLIT, bool BF16>
-__global__ void __launch_bounds__((Cfg<BT, PAIR>::threads), 1)
+__global__ void __launch_bounds__((Cfg<BT, PAIR>::threads), (Cfg<BT, PAIR>::per_sm))
 int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x,
                  const __grid_constant__ CUtensorMap tm_x_part, const __grid_constant__ CUtensorMap tm_z, const Int8Params p) {
   static_assert(!(PAIR && SPLIT), "one use of the cluster at a time");
@@ -632,7 +633,7 @@ int launch(luq_ctx* ctx, const luq_int8_args& a, const Int8Params& p, long long 
   }, ctx->device);
   if (attr != cudaSuccess) return static_cast<int>(attr);
   const int sms = (ctx->sm_limit > 0 && ctx->sm_limit < ctx->sm_count) ? ctx->sm_limit : ctx->sm_count;
-  const long long most = sms / cluster > 0 ? sms / cluster : 1;
+  const long long most = sms * C::per_sm / cluster > 0 ? sms * C::per_sm / cluster : 1;
   const int grid = static_cast<int>(units < most ? units : most) * cluster;
   const cudaError_t e = luq_launch_kernel(kernel, grid, C::threads, static_cast<size_t>(C::smem_bytes(p.groups)), st,
                                           LUQ_LAUNCH_EARLY, static_cast<unsigned>(cluster), tw, tx, tx_part, tz, p);
@@ -666,15 +667,31 @@ int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, bool early, cudaS
   };
   const int sms = (ctx->sm_limit > 0 && ctx->sm_limit < ctx->sm_count) ? ctx->sm_limit : ctx->sm_count;
   const long long mean_rows = (a.M + used - 1) / used;
+  // The tile by the tokens that a group has on average and by how many tiles there are (device time, token
+  // quantizer included; before -> with the choice made here):
+  //  - pairs for 192 tokens on while they fill half the SMs (8192x4096x1024: 43 us, 128-token tiles 47 us)
+  //  - two small CTAs share an SM up to 32 tokens: 64 experts of 32 rows 16.8 -> 16.1 us, 8 experts of one row
+  //    15.7 -> 12.6 us, 60 experts of 17 rows 19.4 (64-token tiles) -> 18.1 us
+  //  - too few tiles: the contraction is split while a CTA keeps eight stages (64x4096x4096: 9.6 us, 32-token
+  //    tiles 12.7 us), else 32-token tiles (500x1000x1000: 9.9 split -> 7.2 us); a handful of tokens is split
+  //    as far as it goes (one token, 4096x1024: 5.0 us)
   long long n = units(256, 2 * kCh);
   if (sms >= 2 && mean_rows >= 192 && n >= sms / 2) return launch_out<256, true, false>(ctx, a, p, n, 2, tz, st);
-  n = units(128, kCh);
-  if (mean_rows > 64 && n >= sms) return launch_out<128, false, false>(ctx, a, p, n, 1, tz, st);
-  const bool narrow = mean_rows <= 16;
-  n = narrow ? units(16, kCh) : units(64, kCh);
-  int split = 1;
-  while (split < kMaxSplit && n * split * 2 <= sms && split * 2 <= p.num_kb) split *= 2;
-  if (split > 1) return narrow ? launch_out<16, false, true>(ctx, a, p, n, split, tz, st)
-                               : launch_out<64, false, true>(ctx, a, p, n, split, tz, st);
-  return narrow ? launch_out<16, false, false>(ctx, a, p, n, 1, tz, st) : launch_out<64, false, false>(ctx, a, p, n, 1, tz, st);
+  if (mean_rows > 64 && (n = units(128, kCh)) >= sms) return launch_out<128, false, false>(ctx, a, p, n, 1, tz, st);
+  auto splits = [&](int stages) {
+    int split = 1;
+    while (split < kMaxSplit && n * split * 2 <= sms && split * 2 * stages <= p.num_kb) split *= 2;
+    return split;
+  };
+  if (mean_rows > 32) {
+    n = units(64, kCh);
+    if (n >= sms / 2) return launch_out<64, false, false>(ctx, a, p, n, 1, tz, st);
+    const int split = splits(8);
+    if (split > 1) return launch_out<64, false, true>(ctx, a, p, n, split, tz, st);
+  }
+  const bool few = mean_rows <= 16;
+  n = units(few ? 16 : 32, kCh);
+  const int split = splits(1);
+  if (few) return split > 1 ? launch_out<16, false, true>(ctx, a, p, n, split, tz, st) : launch_out<16, false, false>(ctx, a, p, n, 1, tz, st);
+  return split > 1 ? launch_out<32, false, true>(ctx, a, p, n, split, tz, st) : launch_out<32, false, false>(ctx, a, p, n, 1, tz, st);
 }
