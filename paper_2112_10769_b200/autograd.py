@@ -1,4 +1,4 @@
-"""A linear layer trained with the 4-bit path, as a ``torch.autograd.Function``.
+"""A linear layer trained with the 4-bit path, as a ``torch.autograd.Function``, and the layer norm between such layers.
 
 Argument marshalling only: every step runs in the library's kernels (Sec. 3, Eqs. Forward /
 Backward / Update; Sec. 4 LUQ; Sec. 5.1 SMP).
@@ -134,3 +134,42 @@ class LuqLinear(torch.nn.Module):
         super()._load_from_state_dict(state_dict, prefix, *args, **kwargs)
         if prefix + "estimates" in state_dict:
             self._primed[:] = [bool(v > 0) for v in self.estimates.tolist()]
+
+
+class LayerNormFunction(torch.autograd.Function):
+    """Layer norm over the last dimension: forward and backward pass in the library's kernels.  The mean and
+    1/std of every row are kept for the backward pass beside x."""
+
+    @staticmethod
+    def forward(ctx, x: torch.Tensor, weight: torch.Tensor | None, bias: torch.Tensor | None, eps: float):
+        lib = context(x.device)
+        y, mean, rstd = lib.layer_norm(x, weight, bias, eps)
+        ctx.save_for_backward(x, mean, rstd, weight)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy: torch.Tensor):
+        x, mean, rstd, weight = ctx.saved_tensors
+        need_dx, need_dweight, need_dbias, _ = ctx.needs_input_grad
+        dx, dweight, dbias = context(x.device).layer_norm_bwd(dy, x, mean, rstd, weight, need_dx, need_dweight, need_dbias)
+        return dx, dweight, dbias, None
+
+
+def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+               eps: float = 1e-5) -> torch.Tensor:
+    """``torch.nn.functional.layer_norm`` over the last dimension.  x is float32 or bfloat16, weight and bias are
+    float32 (or None); the result has the type of x."""
+    return LayerNormFunction.apply(x, weight, bias, eps)
+
+
+class LayerNorm(torch.nn.Module):
+    """``torch.nn.LayerNorm`` over the last dimension, with float32 parameters whatever the type of its input."""
+
+    def __init__(self, features: int, eps: float = 1e-5, bias: bool = True, device=None):
+        super().__init__()
+        self.normalized_shape, self.eps = (features,), eps
+        self.weight = torch.nn.Parameter(torch.ones(features, device=device, dtype=torch.float32))
+        self.bias = torch.nn.Parameter(torch.zeros(features, device=device, dtype=torch.float32)) if bias else None
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        return layer_norm(x, self.weight, self.bias, self.eps)
