@@ -402,7 +402,8 @@ int luq_layer_norm_bwd(luq_ctx* ctx, const void* d_dy, int64_t ld_dy, const void
                        int64_t rows, int64_t cols, const float* d_gamma, const float* d_mean, const float* d_rstd,
                        void* d_dx, int64_t ld_dx, float* d_dgamma, float* d_dbeta, void* stream);
 
-/* int8 codes with a scale for each row (token): scale = max|x| / 127, q = rint(x * fl(127 / max|x|)), ties to
+/* int8 codes with a scale for each row (token): scale = max|x| / 127, q = rint(x * f), f = 127 * fl(1 / max|x|) - every
+ * operation rounded to binary32, the form in which a tensor library evaluates 127 / max - ties to
  * even, value q * scale.  A row of zeros: zero codes and scale.  A non-zero maximum below 2^-100: the same, and
  * LUQ_STATUS_RANGE.  A row with Inf or NaN: zero codes and a NaN scale (its products are NaN, other rows'
  * are not), and LUQ_STATUS_NONFINITE. */

@@ -5,7 +5,7 @@
 //   y_c  = (x_c - mean) rstd gamma_c + beta_c
 //   backward, with xhat = (x - mean) rstd and g = dy gamma:
 //   dx_c = rstd (g_c - 1/C sum g - xhat_c 1/C sum g xhat)   dgamma_c = sum_r dy xhat   dbeta_c = sum_r dy
-//   int8: scale = max_c |v_c| / 127, q_c = rint(v_c * fl32(127 / max)), ties to even
+//   int8: scale = max_c |v_c| / 127, q_c = rint(v_c * fl32(127 * fl32(1 / max))), ties to even
 //
 // All statistics and sums are binary32 and summed in a fixed order (no atomics on sums), so a call
 // repeats bit for bit.  The mean is corrected once by the sum of the centred values, and values are centred with
@@ -81,10 +81,10 @@ __device__ __forceinline__ void finish_stats(float d1, float d2, float eps, floa
 
 // What a row whose maximum |v| has the bit pattern `top` is multiplied with (NaN patterns are above Inf's, Inf's
 // above every number's).  Zero: all codes are zero - a row of zeros; a row with Inf or NaN, which gets a NaN
-// scale, so that what is made of it is NaN and of the others is not; a maximum below 2^-100, where 127 / max would
+// scale, so that what is made of it is NaN and of the others is not; a maximum below 2^-100, where 127 / max could
 // overflow, which gets a zero scale.
 __device__ __forceinline__ float row_factor(unsigned int top) {
-  return top >= 0x7F800000u || top < 0x0D800000u ? 0.0f : __fdiv_rn(127.0f, __uint_as_float(top));
+  return top >= 0x7F800000u || top < 0x0D800000u ? 0.0f : __fmul_rn(127.0f, __frcp_rn(__uint_as_float(top)));
 }
 __device__ __forceinline__ void store_scale(unsigned int top, float* scale, unsigned int* status) {
   const bool bad = top >= 0x7F800000u, tiny = top < 0x0D800000u;   // 2^-100

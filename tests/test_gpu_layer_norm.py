@@ -214,11 +214,11 @@ def test_more_than_2_to_31_elements(ctx):
 # ---- int8 rows -----------------------------------------------------------------------------------------------
 
 def codes32(x):
-    """The definition, in binary32 with numpy: scale = max / 127, q = rint(x * (127 / max))."""
+    """The definition, in binary32 with numpy: scale = max / 127, q = rint(x * (127 * (1 / max)))."""
     x = x.float().cpu().numpy()
     top = np.abs(x).max(1)
     with np.errstate(divide="ignore"):
-        factor = np.where(top > 0, np.float32(127) / top, np.float32(0)).astype(np.float32)
+        factor = np.where(top > 0, np.float32(127) * (np.float32(1) / top), np.float32(0)).astype(np.float32)
     return np.rint(x * factor[:, None]).astype(np.int8), (top / np.float32(127)).astype(np.float32)
 
 
