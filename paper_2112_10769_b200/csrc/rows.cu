@@ -469,11 +469,14 @@ struct Rows {
         for (int j0 = 0; j0 < VPT; j0 += kBouncePieces<T>) {
 #pragma unroll
           for (int j = 0; j < kBouncePieces<T>; ++j)
+            if (j0 + j < VPT) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) b[j * 32 * V + i * width + l] = single[t][(j0 + j) * V + i];
+              for (int i = 0; i < V; ++i) b[j * 32 * V + i * width + l] = single[t][(j0 + j) * V + i];
+            }
           __syncwarp();
 #pragma unroll
-          for (int j = 0; j < kBouncePieces<T>; ++j) unpack(wbuf[j * 32 + lane], base[0], v[t] + (j0 + j) * V);
+          for (int j = 0; j < kBouncePieces<T>; ++j)
+            if (j0 + j < VPT) unpack(wbuf[j * 32 + lane], base[0], v[t] + (j0 + j) * V);
           __syncwarp();
         }
       }
@@ -523,10 +526,12 @@ __device__ __forceinline__ void store_row(T* row, bool exists, bool vec, int tid
 #pragma unroll
     for (int j0 = 0; j0 < VPT; j0 += P) {
 #pragma unroll
-      for (int j = 0; j < P; ++j) wbuf[j * 32 + lane] = pack(v + (j0 + j) * V, row);
+      for (int j = 0; j < P; ++j)
+        if (j0 + j < VPT) wbuf[j * 32 + lane] = pack(v + (j0 + j) * V, row);
       __syncwarp();
 #pragma unroll
       for (int j = 0; j < P; ++j) {
+        if (j0 + j >= VPT) continue;
         const int c0 = (tid - l + (j0 + j) * G) * V + l;
 #pragma unroll
         for (int i = 0; i < V; ++i)
@@ -537,20 +542,24 @@ __device__ __forceinline__ void store_row(T* row, bool exists, bool vec, int tid
   }
 }
 
-// blocks of a row kernel that share an SM, by the registers they need without spilling
-template <int MODE, int EPT, int LOAD, bool FULL>
-constexpr int kRowBlocks = EPT == 32 ? 1 : FULL || MODE == kInt8 || (MODE == kNormInt8 && LOAD == kRing) ? 3 : 2;
+// threads of a row kernel's block (at most), and blocks that share an SM, by the registers they need without spilling
+template <int EPT, bool NARROW>
+constexpr int kRowThreads = EPT == 32 && !NARROW ? 512 : 256;
+template <int MODE, int EPT, int LOAD, bool FULL, bool NARROW>
+constexpr int kRowBlocks = EPT == 32 && !NARROW ? 1
+                           : MODE == kInt8 || (EPT == 16 && (FULL || (MODE == kNormInt8 && LOAD == kRing))) ? 3 : 2;
 
 // FULL: every thread has EPT elements, and all is aligned and there: no test per piece (a third of the instructions)
 template <typename T, int MODE, int EPT, int LOAD, bool FULL, bool NARROW>
-__global__ void __launch_bounds__(EPT == 16 ? 256 : 512, kRowBlocks<MODE, EPT, LOAD, FULL>) row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
+__global__ void __launch_bounds__((kRowThreads<EPT, NARROW>), (kRowBlocks<MODE, EPT, LOAD, FULL, NARROW>))
+row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
   constexpr int V = Piece<T>::V, VPT = EPT / V;
   // one box per reduction of a row; without the norm a row has one reduction only and uses two in turn
   __shared__ float sum_box[16];
   __shared__ float sum2_box[32];
   __shared__ unsigned int max_box[2][16];
   constexpr bool MOVES = !FULL && (MODE == kNorm || LOAD == kBounce);
-  __shared__ uint4 move[MOVES ? (EPT == 16 ? 8 : 16) : 1][MOVES ? 32 * kBouncePieces<T> : 1];
+  __shared__ uint4 move[MOVES ? kRowThreads<EPT, NARROW> / 32 : 1][MOVES ? 32 * kBouncePieces<T> : 1];
   extern __shared__ __align__(128) uint8_t ring_smem[];
   const Group<NARROW> g(threads_per_row);
   const int groups = blockDim.x / g.G, slot = g.index * g.warps, tid = g.tid, G = g.G, C = p.cols;
@@ -678,7 +687,9 @@ struct NormBwdParams {
   const float* rstd;
   void* dx;              // may be null
   float2* row_means;     // workspace: mean of g and of g xhat, per row
-  float* partial;        // workspace: [chunks][2][cols] partial dgamma / dbeta
+  float* partial;        // workspace: [chunks][2][cols] partial dgamma / dbeta; null if neither is wanted
+  float* dgamma;         // the results, written directly by a grid of one block
+  float* dbeta;
   int chunks;
   long long rows_per_chunk;
   unsigned int* status;
@@ -867,19 +878,11 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
     }
   }
   const int turns = NARROW ? blockDim.x >> 5 : groups, mine = NARROW ? threadIdx.x >> 5 : group;
+  // (one block: these are the results)
+  float* const out_gamma = gridDim.x == 1 ? p.dgamma : out;
+  float* const out_beta = gridDim.x == 1 ? p.dbeta : out + C;
   float* const sums = reinterpret_cast<float*>(ring_smem);
   const int Cp = (C + 3) & ~3;                         // a row of sums in shared memory
-  if (turns == 1) {
-#pragma unroll
-    for (int i = 0; i < EPT; ++i) {
-      const int c = (tid + i / V * G) * V + i % V;
-      if (c < C) {
-        out[c] = dgamma[i];
-        out[C + c] = dbeta[i];
-      }
-    }
-    return;
-  }
   __syncthreads();                                     // the ring is done with
   if (g.sub() == 0) {
     float* const to = sums + 2 * mine * Cp;
@@ -893,11 +896,14 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
     }
   }
   __syncthreads();
-  for (int c = threadIdx.x; c < 2 * C; c += blockDim.x) {
-    const int at = c < C ? c : Cp + c - C;
-    float s = sums[at];
-    for (int k = 1; k < turns; ++k) s += sums[2 * k * Cp + at];
-    out[c] = s;
+  for (int c = threadIdx.x; c < C; c += blockDim.x) {
+    float sg = sums[c], sb = sums[Cp + c];
+    for (int k = 1; k < turns; ++k) {
+      sg += sums[2 * k * Cp + c];
+      sb += sums[(2 * k + 1) * Cp + c];
+    }
+    if (out_gamma) out_gamma[c] = sg;
+    if (out_beta) out_beta[c] = sb;
   }
 }
 
@@ -948,7 +954,7 @@ int ring_depth_for(int groups, int stage_bytes, int budget) {
 }
 // threads of a row: a power of two of lanes up to a warp, whole warps beyond
 int threads_of_row(int cols, int ept) {
-  if (cols <= 512) {
+  if (cols <= 32 * ept) {
     int g = 1;
     while (g * ept < cols) g <<= 1;
     return g;
@@ -960,12 +966,13 @@ template <typename T, int MODE, int EPT, int LOAD, bool NARROW>
 cudaError_t launch_row(luq_ctx* ctx, const RowParams& p, bool vec, cudaStream_t st) {
   const int G = threads_of_row(p.cols, EPT);
   // groups share a block while every SM has some; a block has whole warps
-  int groups = (EPT == 16 ? 256 : 512) / G;
+  int groups = (G > 256 ? 512 : 256) / G;
   while (groups > 1 && G * groups > 32 && p.rows < static_cast<long long>(groups) * ctx->sm_count) groups >>= 1;
   const bool full = LOAD != kBounce && vec && p.cols == G * EPT && (MODE == kInt8 || (p.gamma && p.beta));
-  const int per_sm = full ? kRowBlocks<MODE, EPT, LOAD, true> : kRowBlocks<MODE, EPT, LOAD, false>;
+  int per_sm = full ? kRowBlocks<MODE, EPT, LOAD, true, NARROW> : kRowBlocks<MODE, EPT, LOAD, false, NARROW>;
+  if (kRowThreads<EPT, NARROW> == 512 && G <= 256) per_sm = 2;
   const int row_bytes = Rows<T, 1, EPT, LOAD, false, NARROW>::ring_row_bytes(p.cols);
-  const int depth = LOAD == kRing ? ring_depth_for(groups, row_bytes, EPT == 16 ? kRingBytes : kRingBytesAlone) : 0;
+  const int depth = LOAD == kRing ? ring_depth_for(groups, row_bytes, per_sm > 1 ? kRingBytes : kRingBytesAlone) : 0;
   const size_t smem = LOAD == kRing ? static_cast<size_t>(Rows<T, 1, EPT, LOAD, false, NARROW>::ring_bytes(groups, depth, p.cols)) : 0;
   auto kernel = full ? row_kernel<T, MODE, EPT, LOAD, LOAD != kBounce, NARROW> : row_kernel<T, MODE, EPT, LOAD, false, NARROW>;
   if (LOAD == kRing) {
@@ -975,8 +982,40 @@ cudaError_t launch_row(luq_ctx* ctx, const RowParams& p, bool vec, cudaStream_t 
   }
   const long long blocks = (p.rows + groups - 1) / groups;
   const long long cap = static_cast<long long>(ctx->sm_count) * per_sm *
-                        (LOAD == kRing ? 1 : (EPT == 16 ? 256 : 512) / (G * groups));
+                        (LOAD == kRing ? 1 : (G > 256 ? 512 : 256) / (G * groups));
   return luq_launch_kernel(kernel, static_cast<int>(blocks < cap ? blocks : cap), G * groups, smem, st, LUQ_LAUNCH_EARLY, 1, p, G, depth);
+}
+
+template <typename T, int MODE, int EPT, bool NARROW>
+cudaError_t launch_row_from(luq_ctx* ctx, const RowParams& p, bool vec_x, bool vec, bool ring, cudaStream_t st) {
+  if (ring) return launch_row<T, MODE, EPT, kRing, NARROW>(ctx, p, vec, st);
+  return vec_x ? launch_row<T, MODE, EPT, kDirect, NARROW>(ctx, p, vec, st) : launch_row<T, MODE, EPT, kBounce, NARROW>(ctx, p, vec, st);
+}
+template <typename T, int MODE, int EPT>
+cudaError_t launch_row_load(luq_ctx* ctx, const RowParams& p, bool vec_x, bool vec, bool many, cudaStream_t st) {
+  if (p.cols > 32 * EPT) return launch_row_from<T, MODE, EPT, false>(ctx, p, vec_x, vec, many, st);
+  // rows of less than a warp: the ring's copies would be too small
+  return launch_row_from<T, MODE, EPT, true>(ctx, p, vec_x, vec, many && p.cols > 512, st);
+}
+
+// Elements per thread by the width alone (what a row becomes must not depend on where it lies).  What counts is the
+// share of a block's 256 x elements that a row's groups use, and how much of a row's fixed cost an element bears
+// (16 -> chosen, norm / norm to int8 / int8, us):
+//   32  whole multiples of 1024: 16384x4096 bf16 57 -> 47 / 70 -> 57 / 37; to int8 also widths that 32 fits as well as
+//       16 does: 5223x3830 bf16 35 -> 31.5 / 20.6 -> 18.1
+//   24  where it fits better: 41582x704 bf16 55 -> 45 / 63 -> 50 / 35 -> 27, 5000x6000 bf16 41 (32) -> 32.5;
+//       norms of odd widths stay at 16, whose rows are rarely aligned and need the registers (60000x700: 86, 24: 131)
+int elements_per_thread(int mode, int cols) {
+  if (cols <= 512) return 16;
+  if (cols > 8192) return 32;
+  auto fit = [&](int ept) {
+    const int G = threads_of_row(cols, ept);
+    return G > 256 ? 0.0f : static_cast<float>(cols) / (G * ept) * (G * (256 / G)) / 256.0f;
+  };
+  const float f16 = fit(16), f24 = fit(24), f32 = fit(32);
+  if (cols > 1024 && (cols % 1024 == 0 || (cols > 2048 && mode != kNorm && f32 >= f16 && f32 >= f24))) return 32;
+  if (f24 >= f16 && f24 > 0.0f && (mode != kNorm || cols % 8 == 0 || f16 == 0.0f)) return 24;
+  return f16 > 0.0f ? 16 : 32;
 }
 
 template <typename T, int MODE>
@@ -990,14 +1029,12 @@ int launch_rows(luq_ctx* ctx, RowParams p, cudaStream_t st) {
   if (p.cols > 16384) {
     const long long cap = 4ll * ctx->sm_count;
     e = luq_launch_kernel(row_loop_kernel<T, MODE>, static_cast<int>(p.rows < cap ? p.rows : cap), 512, 0, st, LUQ_LAUNCH_EARLY, 1, p);
-  } else if (p.cols > 4096) {
-    e = many ? launch_row<T, MODE, 32, kRing, false>(ctx, p, vec, st)
-             : vec_x ? launch_row<T, MODE, 32, kDirect, false>(ctx, p, vec, st) : launch_row<T, MODE, 32, kBounce, false>(ctx, p, vec, st);
-  } else if (p.cols > 512) {
-    e = many ? launch_row<T, MODE, 16, kRing, false>(ctx, p, vec, st)
-             : vec_x ? launch_row<T, MODE, 16, kDirect, false>(ctx, p, vec, st) : launch_row<T, MODE, 16, kBounce, false>(ctx, p, vec, st);
   } else {
-    e = vec_x ? launch_row<T, MODE, 16, kDirect, true>(ctx, p, vec, st) : launch_row<T, MODE, 16, kBounce, true>(ctx, p, vec, st);
+    switch (elements_per_thread(MODE, p.cols)) {
+      case 16: e = launch_row_load<T, MODE, 16>(ctx, p, vec_x, vec, many, st); break;
+      case 24: e = launch_row_load<T, MODE, 24>(ctx, p, vec_x, vec, many, st); break;
+      default: e = launch_row_load<T, MODE, 32>(ctx, p, vec_x, vec, many, st);
+    }
   }
   if (e == cudaSuccess) ctx->launches += 1;
   return static_cast<int>(e);
@@ -1009,7 +1046,7 @@ cudaError_t launch_norm_bwd_rows(int device, const NormBwdParams& p, bool vec, i
   using R = Rows<T, 2, 16, LOAD, false, NARROW>;
   const int depth = LOAD == kRing ? ring_depth_for(groups, 2 * R::ring_row_bytes(p.cols), kRingBytesAlone) : 0;
   const int turns = NARROW ? block / 32 : groups;
-  const size_t sums = turns > 1 ? 2 * sizeof(float) * static_cast<size_t>((p.cols + 3) & ~3) * turns : 0;
+  const size_t sums = 2 * sizeof(float) * static_cast<size_t>((p.cols + 3) & ~3) * turns;
   const size_t ring = LOAD == kRing ? static_cast<size_t>(R::ring_bytes(groups, depth, p.cols)) : 0;
   constexpr bool can = LOAD != kBounce && EPT == 16;
   const bool full = can && vec && p.cols == G * EPT && p.gamma;
@@ -1025,6 +1062,9 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
   const size_t per_chunk = 2 * sizeof(float) * static_cast<size_t>(p.cols);
   cudaError_t e = cudaSuccess;
   p.vec_gamma = aligned(p.gamma, 0, 4);
+  p.dgamma = dgamma;
+  p.dbeta = dbeta;
+  bool reduced = false;
   p.vec_dx = aligned(p.dx, p.ld_dx, sizeof(T));
   const bool vec_in = aligned(p.x, p.ld_x, sizeof(T)) && aligned(p.dy, p.ld_dy, sizeof(T)), vec = vec_in && p.vec_gamma && p.vec_dx;
   // a row of x and one of dy have to fit the ring
@@ -1039,6 +1079,7 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
     if (blocks * groups > p.rows) blocks = (p.rows + groups - 1) / groups;
     p.partial = dgamma || dbeta ? ctx->d_workspace : nullptr;
     p.chunks = static_cast<int>(blocks);
+    reduced = blocks == 1;
     const bool ring = p.dx != nullptr && p.rows >= 2 * blocks * groups;
     if (ept == 32) e = launch_norm_bwd_rows<T, 32, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
     else if (p.cols <= 512) e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, true>(ctx->device, p, vec, G, block, p.chunks, st)
@@ -1070,7 +1111,7 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
   }
   if (e != cudaSuccess) return static_cast<int>(e);
   ctx->launches += 1;
-  if (dgamma || dbeta) {
+  if ((dgamma || dbeta) && !reduced) {
     e = luq_launch_kernel(norm_bwd_reduce_kernel, static_cast<int>((2ll * p.cols + 31) / 32), 1024, 0, st, LUQ_LAUNCH_EARLY, 1,
                           p.partial, p.chunks, p.cols, dgamma, dbeta);
     if (e == cudaSuccess) ctx->launches += 1;
