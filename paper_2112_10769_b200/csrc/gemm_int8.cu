@@ -21,6 +21,8 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 
+#include <climits>
+
 #include "common.cuh"
 
 namespace {
@@ -67,8 +69,10 @@ struct Cfg {
   static constexpr int stages = BT == 16 ? 5 : BT == 32 ? 4 : BT == 64 ? 7 : 5;
   static constexpr int chunk = BT < 32 ? BT : 32;                 // tokens per epilogue step
   static constexpr int tmem_cols = 2 * BT;
-  static constexpr int staging = stages * stage_bytes;            // store boxes, or a split's partial tile
-  static constexpr int token_scales = staging + (BT == 16 ? 8192 : epi_warps * kWarpStaging);   // two tiles' scales
+  static constexpr int staging = stages * stage_bytes;            // store boxes
+  static constexpr int token_scales = staging + (BT == 16 ? 0 : epi_warps * kWarpStaging);      // two tiles' scales
+  // a split's partial tile lies where the stages were, which its contraction is done with
+  static_assert(BT * kCh * 4 <= stages * stage_bytes, "a partial tile has to fit the stages");
   static constexpr int barriers = token_scales + 2 * BT * 4;
   static constexpr int num_barriers = 2 * stages + 4;
   static constexpr int tmem_slot = barriers + 8 * num_barriers;
@@ -297,6 +301,33 @@ __device__ __forceinline__ void write_tile(const Int8Params& p, const void* tm_z
   }
 }
 
+// Adds a channel's partial sums of Q CTAs (of fewer, if the cluster has fewer) for every stride-th token and
+// writes the results; sixteen loads from the other CTAs are on their way at once.
+template <int Q>
+__device__ __forceinline__ void join(const Int8Params& p, const Unit& v, uint32_t column, int first_token, int stride, int ch,
+                                     float sw, float bias, const float* scales, bool bf16) {
+  constexpr int U = 16 / Q;
+  const int cluster = static_cast<int>(cluster_nctarank());
+  for (int t0 = first_token; t0 < v.rows; t0 += U * stride) {
+    int part[U][Q];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+        part[u][q] = q < cluster && t0 + u * stride < v.rows ? ld_shared_cluster(mapa_shared(column + (t0 + u * stride) * kCh * 4, q)) : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * stride;
+      int sum = 0;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) sum += part[u][q];
+      if (t < v.rows)
+        store_z(p.z, (static_cast<long long>(v.row0) + t) * p.ld_z + ch, fmaf(static_cast<float>(sum) * sw, scales[t], bias), bf16);
+    }
+  }
+}
+
 // SPLIT: the CTAs of a cluster share a tile and take a share of its contraction each (few tokens: too few tiles
 // for the SMs); partial tiles meet through distributed shared memory, as integers, in any order exact.
 // PAIR: the two CTAs of a cluster compute a tile of 256 channels together (cta_group::2), each fetches half of
@@ -519,7 +550,7 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
       if (lane == 0) bulk_wait<0>();   // all stores of this warp are complete before the CTA exits
     }
   } else {
-    int* const partial = reinterpret_cast<int*>(gen + C::staging);      // [token][channel]
+    int* const partial = reinterpret_cast<int*>(gen);      // [token][channel], in place of the stages
     for (; walk.more(); walk.next(), ++it) {
       const Unit v = unit_of(walk);
       if (warp == 0 || warp == kXWarp) {
@@ -541,7 +572,7 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
           tmem_ld_wait();
 #pragma unroll
           for (int i = 0; i < C::chunk; ++i)
-            if (smem_in(partial + (c + i) * kCh + (warp & 3) * 32 + lane, gen, C::staging, C::token_scales, 4, p.status))
+            if (smem_in(partial + (c + i) * kCh + (warp & 3) * 32 + lane, gen, 0, C::staging, 4, p.status))
               partial[(c + i) * kCh + (warp & 3) * 32 + lane] = static_cast<int>(r[i]);
         }
         tc_fence_before();
@@ -552,20 +583,16 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
       cluster_sync_all();              // every CTA's partial tile is there
       if (warp >= kFirstEpiWarp) {
         // a token's 128 channels at a time, tokens dealt out over the CTAs
-        const float* const s = scales_of(it);
         const int ch = v.ch0 + (warp & 3) * 32 + lane;
-        for (int t = static_cast<int>(rank) + (warp_e >> 2) * static_cast<int>(cluster); t < v.rows;
-             t += static_cast<int>(cluster) * (C::epi_warps / 4)) {
-          if (ch >= p.N) continue;     // every load below is used, and so has ended, before the meeting after it
-          const uint32_t at = smem_u32(partial + t * kCh + (warp & 3) * 32 + lane);
-          int part[kMaxSplit];         // all on their way at once
-#pragma unroll
-          for (int q = 0; q < kMaxSplit; ++q) part[q] = q < static_cast<int>(cluster) ? ld_shared_cluster(mapa_shared(at, q)) : 0;
-          int sum = 0;
-#pragma unroll
-          for (int q = 0; q < kMaxSplit; ++q) sum += part[q];
-          store_z(p.z, (static_cast<long long>(v.row0) + t) * p.ld_z + ch, fmaf(static_cast<float>(sum) * sw_ahead, s[t], bias_ahead), BF16);
+        const int first_token = static_cast<int>(rank) + (warp_e >> 2) * static_cast<int>(cluster);
+        const int stride = static_cast<int>(cluster) * (C::epi_warps / 4);
+        const uint32_t column = smem_u32(partial + (warp & 3) * 32 + lane);
+        if (ch < p.N) {                // every load below is used, and so has ended, before the meeting after it
+          if (cluster <= 2) join<2>(p, v, column, first_token, stride, ch, sw_ahead, bias_ahead, scales_of(it), BF16);
+          else if (cluster <= 4) join<4>(p, v, column, first_token, stride, ch, sw_ahead, bias_ahead, scales_of(it), BF16);
+          else join<8>(p, v, column, first_token, stride, ch, sw_ahead, bias_ahead, scales_of(it), BF16);
         }
+        fence_proxy_async();           // the next tile's copies come after these reads
       }
       __syncwarp();
       cluster_sync_relaxed();          // and has been read by all
@@ -647,6 +674,35 @@ int launch_out(luq_ctx* ctx, const luq_int8_args& a, const Int8Params& p, long l
                     : launch<BT, PAIR, SPLIT, false>(ctx, a, p, units, cluster, tz, st);
 }
 
+// How long the product takes with each tile, in hundredths of a microsecond past the launch: rounds over the SMs
+// x (stages x the time of one + what a tile costs at its ends).  The rates were fitted to 22 products of 40 to
+// 13097 tokens, each timed with every tile and split; of 26 others the choice was the best or within 10% of it.
+// What a stage takes is its share of the L2 (24 to 32 KB at 75-85 KB a microsecond and SM), not of the tensor cores.  A split pays
+// its meeting and the sums over the other CTAs' memory; it is taken in a single round only.  Examples, token quantizer
+// excluded: 2443x576x4096 14.7 us with 128-token tiles in one round, 24.0 with 64-token tiles in two, 17.2 with pairs;
+// 1313x2340x3033 15.3 with pairs, 21.7 with 128; 142x384x3904 7.0 with 32-token tiles split in four, 12.3 unsplit.
+struct Choice { int tokens, split; };
+template <class Units>
+Choice choose_tile(int sms, int num_kb, long long mean_rows, Units units) {
+  struct Tile { int tokens, channels, ctas, stage, ends, meeting; };        // ctas: that one tile occupies
+  constexpr Tile tiles[] = {{256, 2 * kCh, 2, 43, 150, 0}, {128, kCh, 1, 38, 50, 210}, {64, kCh, 1, 30, 50, 140}, {32, kCh, 1, 27, 40, 120}};
+  Choice best{64, 1};
+  long long best_time = LLONG_MAX;
+  for (const Tile& t : tiles) {
+    if (t.tokens == 256 && (sms < 2 || mean_rows <= 128)) continue;
+    const long long n = units(t.tokens, t.channels);
+    for (int split = 1; split <= kMaxSplit; split *= 2) {
+      // clusters of four and eight do not fill the SMs: a group of SMs that share clusters has 16 to 20
+      const long long slots = split > 2 ? sms - sms / 8 : sms;
+      if (split > 1 && (t.tokens == 256 || n * split > slots || split > num_kb)) break;
+      const long long rounds = (n + sms / t.ctas - 1) / (sms / t.ctas);
+      const long long time = rounds * ((num_kb + split - 1) / split * t.stage + t.ends) + (split > 1 ? t.meeting : 0);
+      if (time < best_time) { best_time = time; best = {t.tokens, split}; }
+    }
+  }
+  return best;
+}
+
 }  // namespace
 
 int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, bool early, cudaStream_t st) {
@@ -667,31 +723,23 @@ int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, bool early, cudaS
   };
   const int sms = (ctx->sm_limit > 0 && ctx->sm_limit < ctx->sm_count) ? ctx->sm_limit : ctx->sm_count;
   const long long mean_rows = (a.M + used - 1) / used;
-  // The tile by the tokens that a group has on average and by how many tiles there are (device time, token
-  // quantizer included; before -> with the choice made here):
-  //  - pairs for 192 tokens on while they fill half the SMs (8192x4096x1024: 43 us, 128-token tiles 47 us)
-  //  - two small CTAs share an SM up to 32 tokens: 64 experts of 32 rows 16.8 -> 16.1 us, 8 experts of one row
-  //    15.7 -> 12.6 us, 60 experts of 17 rows 19.4 (64-token tiles) -> 18.1 us
-  //  - too few tiles: the contraction is split while a CTA keeps eight stages (64x4096x4096: 9.6 us, 32-token
-  //    tiles 12.7 us), else 32-token tiles (500x1000x1000: 9.9 split -> 7.2 us); a handful of tokens is split
-  //    as far as it goes (one token, 4096x1024: 5.0 us)
-  long long n = units(256, 2 * kCh);
-  if (sms >= 2 && mean_rows >= 192 && n >= sms / 2) return launch_out<256, true, false>(ctx, a, p, n, 2, tz, st);
-  if (mean_rows > 64 && (n = units(128, kCh)) >= sms) return launch_out<128, false, false>(ctx, a, p, n, 1, tz, st);
-  auto splits = [&](int stages) {
-    int split = 1;
-    while (split < kMaxSplit && n * split * 2 <= sms && split * 2 * stages <= p.num_kb) split *= 2;
-    return split;
-  };
+  // The tile is the one that the model below expects to end first.  Up to 32 tokens a group, two small CTAs share
+  // an SM (64 experts of 32 rows 16.8 -> 16.1 us, 8 experts of one row 15.7 -> 12.6 us, 60 experts of 17 rows 19.4 us
+  // with 64-token tiles -> 18.1 us) and the contraction is split as far as it goes (one token, 4096x1024: 5.0 us).
   if (mean_rows > 32) {
-    n = units(64, kCh);
-    if (n >= sms / 2) return launch_out<64, false, false>(ctx, a, p, n, 1, tz, st);
-    const int split = splits(8);
-    if (split > 1) return launch_out<64, false, true>(ctx, a, p, n, split, tz, st);
+    const Choice best = choose_tile(sms, p.num_kb, mean_rows, units);
+    const long long n = units(best.tokens, best.tokens == 256 ? 2 * kCh : kCh);
+    if (best.tokens == 256) return launch_out<256, true, false>(ctx, a, p, n, 2, tz, st);
+    if (best.tokens == 128)
+      return best.split > 1 ? launch_out<128, false, true>(ctx, a, p, n, best.split, tz, st) : launch_out<128, false, false>(ctx, a, p, n, 1, tz, st);
+    if (best.tokens == 64)
+      return best.split > 1 ? launch_out<64, false, true>(ctx, a, p, n, best.split, tz, st) : launch_out<64, false, false>(ctx, a, p, n, 1, tz, st);
+    return best.split > 1 ? launch_out<32, false, true>(ctx, a, p, n, best.split, tz, st) : launch_out<32, false, false>(ctx, a, p, n, 1, tz, st);
   }
   const bool few = mean_rows <= 16;
-  n = units(few ? 16 : 32, kCh);
-  const int split = splits(1);
+  const long long n = units(few ? 16 : 32, kCh);
+  int split = 1;
+  while (split < kMaxSplit && n * split * 2 <= sms && split * 2 <= p.num_kb) split *= 2;
   if (few) return split > 1 ? launch_out<16, false, true>(ctx, a, p, n, split, tz, st) : launch_out<16, false, false>(ctx, a, p, n, 1, tz, st);
   return split > 1 ? launch_out<32, false, true>(ctx, a, p, n, split, tz, st) : launch_out<32, false, false>(ctx, a, p, n, 1, tz, st);
 }
