@@ -200,13 +200,24 @@ __device__ __forceinline__ uint4 pack(const float* v, const __nv_bfloat16*) {
 __device__ __forceinline__ float zero_of(const float*) { return 0.0f; }
 __device__ __forceinline__ __nv_bfloat16 zero_of(const __nv_bfloat16*) { return __float2bfloat16_rn(0.0f); }
 
-// V parameters, `other` where there are none; `vec`: 16-byte aligned
-template <int V, bool FULL>
+// What a row consists of: kFull, every thread has EPT elements; kWhole, whole pieces; kRagged, anything.  The first
+// two also mean that all tensors are there and aligned.
+constexpr int kRagged = 0, kWhole = 1, kFull = 2;
+template <typename T>
+int fit_of(int cols, int full) { return cols == full ? kFull : cols % Piece<T>::V == 0 ? kWhole : kRagged; }
+// do all elements of the piece at c exist?
+template <int FIT, int V>
+__device__ __forceinline__ bool piece_exists(int c, int cols) {
+  return FIT == kFull || (FIT == kWhole ? c < cols : c + V <= cols);
+}
+
+// V parameters, `other` where there are none, zero beyond the row's end; `vec`: 16-byte aligned
+template <int V, int FIT>
 __device__ __forceinline__ void load_params(const float* g, bool vec, int c, int cols, float other, float* v) {
-  if (!FULL && g == nullptr) {
+  if (FIT == kRagged && g == nullptr) {
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = other;
-  } else if (FULL || (vec && c + V <= cols)) {
+  } else if (piece_exists<FIT, V>(c, cols) && (FIT != kRagged || vec)) {
 #pragma unroll
     for (int i = 0; i < V; i += 4) {
       const float4 f = *(reinterpret_cast<const float4*>(g + c + i));
@@ -228,7 +239,10 @@ struct Group {
     tid = threadIdx.x - index * G;
     warps = NARROW ? 1 : G >> 5;
   }
-  __device__ __forceinline__ void sync() const { asm volatile("bar.sync %0, %1;" ::"r"(1 + index), "r"(G) : "memory"); }
+  __device__ __forceinline__ void sync() const {
+    if (NARROW) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + index), "r"(G) : "memory");
+  }
   __device__ __forceinline__ int sub() const { return NARROW ? (threadIdx.x & 31) / G : 0; }   // row within the warp
   __device__ __forceinline__ float sum(float v, float* box) const {
     if constexpr (NARROW) {
@@ -295,7 +309,7 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 //              filled again
 // kRing waits are bounded; when one runs out the group goes on without writing anything (ok() is false), so that
 // its barriers still meet, and finish() waits for the copies under way and raises the status.
-template <typename T, int TENSORS, int EPT, int LOAD, bool FULL, bool NARROW>
+template <typename T, int TENSORS, int EPT, int LOAD, int FIT, bool NARROW>
 struct Rows {
   static constexpr int V = Piece<T>::V, VPT = EPT / V;
   const T* base[2];
@@ -334,7 +348,7 @@ struct Rows {
     fence_barrier_init();
   }
   // A row's bytes lie at (address & 15) in its stage.  Rows at the tensor's ends are copied without the pieces that
-  // reach beyond it (take() fetches such a row element by element).
+  // reach beyond it (await() fetches what they hold).
   __device__ __forceinline__ void fill(int s, long long r) {
     const int bytes = cols * static_cast<int>(sizeof(T));
     uint32_t total = 0, lo[TENSORS], n[TENSORS];
@@ -357,7 +371,7 @@ struct Rows {
   __device__ __forceinline__ void ring_piece(int t, uint32_t m, int c, float* v) const {
     const uint4* const q = reinterpret_cast<const uint4*>(held + (stage * TENSORS + t) * row_bytes) + c / V;
     const uint4 a = q[0];
-    if (FULL || m == 0) { unpack(a, base[0], v); return; }
+    if (FIT != kRagged || m == 0) { unpack(a, base[0], v); return; }
     const uint4 b = q[1];
     uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     if (m & 8) {
@@ -375,12 +389,25 @@ struct Rows {
     unpack(make_uint4(w[0], w[1], w[2], w[3]), base[0], v);
   }
   __device__ __forceinline__ uint32_t skew(int t, long long r) const {
-    return FULL ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base[t] + r * ld[t]) & 15u);
+    return FIT != kRagged ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base[t] + r * ld[t]) & 15u);
   }
-  // a row whose stage lacks elements that lie at the tensor's ends
-  __device__ __forceinline__ bool at_end(int t, long long r) const {
-    const uint32_t m = skew(t, r);
-    return !FULL && ((r == 0 && m) || (r + 1 == rows && ((m + cols * sizeof(T)) & 15u)));
+  // Waits for row r's stage.  In the tensor's first and last row the elements in the pieces that reach beyond it were
+  // not copied: a lane each puts them there.
+  __device__ __forceinline__ void await(const Group<NARROW>& g, long long r) {
+    fine = fine && mbar_wait(bars + 8 * stage, phase, abort_flag);
+    if (FIT != kRagged || (r != 0 && r + 1 != rows)) return;
+    if (tid < V) {
+#pragma unroll
+      for (int t = 0; t < TENSORS; ++t) {
+        const T* const row = base[t] + r * ld[t];
+        const int m = static_cast<int>(skew(t, r)) / static_cast<int>(sizeof(T)), tail = (m + cols) % V;
+        T* const to = reinterpret_cast<T*>(held + (stage * TENSORS + t) * row_bytes) + m;
+        if (r == 0 && m && tid < V - m && tid < cols) to[tid] = row[tid];
+        if (r + 1 == rows && tid < tail && tid < cols) to[cols - 1 - tid] = row[cols - 1 - tid];
+      }
+      fence_proxy_async();               // before the stage's next copy
+    }
+    g.sync();
   }
   __device__ __forceinline__ void fetch(long long r) {
 #pragma unroll
@@ -392,9 +419,9 @@ struct Rows {
           const int c = (tid + j * G) * V;
           raw[t][j] = make_uint4(0u, 0u, 0u, 0u);
           if (r < rows) {
-            if (FULL || c + V <= cols) {
+            if (piece_exists<FIT, V>(c, cols)) {
               raw[t][j] = *(reinterpret_cast<const uint4*>(row + c));
-            } else {
+            } else if (FIT == kRagged) {
               float v[V];
 #pragma unroll
               for (int i = 0; i < V; ++i) v[i] = c + i < cols ? load1(row + c + i) : 0.0f;
@@ -421,36 +448,30 @@ struct Rows {
       if (tid < depth && first + tid * step < rows) fill(tid, first + tid * step);
       issued = 0;
       while (issued < depth && first + issued * step < rows) ++issued;
-    } else {
-      fetch(first);
+    } else {                               // the first turn of the loop, one step before the first row, fetches it
+#pragma unroll
+      for (int t = 0; t < TENSORS; ++t) {
+        for (uint4& w : raw[t]) w = make_uint4(0u, 0u, 0u, 0u);
+        for (T& w : single[t]) w = zero_of(base[0]);
+      }
     }
   }
+  static constexpr bool AHEAD = LOAD != kRing;   // a turn of the loop comes before the first row
   // (in a narrow group's warp, r may lie beyond the rows)
-  __device__ __forceinline__ void take(long long r, float (*v)[EPT]) {
+  __device__ __forceinline__ void take(const Group<NARROW>& g, long long r, float (*v)[EPT]) {
     if constexpr (LOAD == kRing) {
-      fine = fine && mbar_wait(bars + 8 * stage, phase, abort_flag);
+      await(g, r);
 #pragma unroll
       for (int t = 0; t < TENSORS; ++t) {
         const uint32_t m = skew(t, r);
-        if (at_end(t, r)) {
-          const T* const row = base[t] + r * ld[t];
 #pragma unroll
-          for (int j = 0; j < VPT; ++j)
+        for (int j = 0; j < VPT; ++j) {
+          const int c = (tid + j * G) * V;
+          if (FIT == kFull || c < cols) ring_piece(t, m, c, v[t] + j * V);
+          if (!piece_exists<FIT, V>(c, cols)) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-              const int c = (tid + j * G) * V + i;
-              v[t][j * V + i] = c < cols ? load1(row + c) : 0.0f;
-            }
-        } else {
-#pragma unroll
-          for (int j = 0; j < VPT; ++j) {
-            const int c = (tid + j * G) * V;
-            if (FULL || c < cols) ring_piece(t, m, c, v[t] + j * V);
-            if (!FULL && c + V > cols) {
-#pragma unroll
-              for (int i = 0; i < V; ++i)
-                if (c + i >= cols) v[t][j * V + i] = 0.0f;
-            }
+            for (int i = 0; i < V; ++i)
+              if (FIT != kRagged || c + i >= cols) v[t][j * V + i] = 0.0f;
           }
         }
       }
@@ -503,17 +524,17 @@ struct Rows {
 
 // writes a thread's elements of a row; `vec`: the row starts at a multiple of 16 bytes (else through the warp's
 // shared memory, as kBounce reads)
-template <typename T, int EPT, bool FULL, bool NARROW>
+template <typename T, int EPT, int FIT, bool NARROW>
 __device__ __forceinline__ void store_row(T* row, bool exists, bool vec, int tid, int G, int cols, uint4* wbuf, const float* v) {
   constexpr int V = Piece<T>::V, VPT = EPT / V;
-  if (FULL || vec) {
+  if (FIT != kRagged || vec) {
     if (!exists) return;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
       const int c = (tid + j * G) * V;
-      if (FULL || c + V <= cols) {
+      if (piece_exists<FIT, V>(c, cols)) {
         *reinterpret_cast<uint4*>(row + c) = pack(v + j * V, row);
-      } else {
+      } else if (FIT == kRagged) {
 #pragma unroll
         for (int i = 0; i < V; ++i)
           if (c + i < cols) store1(row + c + i, v[j * V + i]);
@@ -545,26 +566,26 @@ __device__ __forceinline__ void store_row(T* row, bool exists, bool vec, int tid
 // threads of a row kernel's block (at most), and blocks that share an SM, by the registers they need without spilling
 template <int EPT, bool NARROW>
 constexpr int kRowThreads = EPT == 32 && !NARROW ? 512 : 256;
-template <int MODE, int EPT, int LOAD, bool FULL, bool NARROW>
+template <int MODE, int EPT, int LOAD, int FIT, bool NARROW>
 constexpr int kRowBlocks = EPT == 32 && !NARROW ? 1
-                           : MODE == kInt8 || (EPT == 16 && (FULL || (MODE == kNormInt8 && LOAD == kRing))) ? 3 : 2;
+                           : MODE == kInt8 || (EPT == 16 && (FIT != kRagged || (MODE == kNormInt8 && LOAD == kRing))) ? 3 : 2;
 
-// FULL: every thread has EPT elements, and all is aligned and there: no test per piece (a third of the instructions)
-template <typename T, int MODE, int EPT, int LOAD, bool FULL, bool NARROW>
-__global__ void __launch_bounds__((kRowThreads<EPT, NARROW>), (kRowBlocks<MODE, EPT, LOAD, FULL, NARROW>))
+// FIT, for rows of 16384 x 4096 bf16 / 41582 x 704 bf16: 46 / - us with kFull, 57 / 31 with kWhole, - / 45 with kRagged
+template <typename T, int MODE, int EPT, int LOAD, int FIT, bool NARROW>
+__global__ void __launch_bounds__((kRowThreads<EPT, NARROW>), (kRowBlocks<MODE, EPT, LOAD, FIT, NARROW>))
 row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
   constexpr int V = Piece<T>::V, VPT = EPT / V;
   // one box per reduction of a row; without the norm a row has one reduction only and uses two in turn
   __shared__ float sum_box[16];
   __shared__ float sum2_box[32];
   __shared__ unsigned int max_box[2][16];
-  constexpr bool MOVES = !FULL && (MODE == kNorm || LOAD == kBounce);
+  constexpr bool MOVES = FIT == kRagged && (MODE == kNorm || LOAD == kBounce);
   __shared__ uint4 move[MOVES ? kRowThreads<EPT, NARROW> / 32 : 1][MOVES ? 32 * kBouncePieces<T> : 1];
   extern __shared__ __align__(128) uint8_t ring_smem[];
   const Group<NARROW> g(threads_per_row);
   const int groups = blockDim.x / g.G, slot = g.index * g.warps, tid = g.tid, G = g.G, C = p.cols;
   uint4* const wbuf = move[MOVES ? threadIdx.x >> 5 : 0];
-  Rows<T, 1, EPT, LOAD, FULL, NARROW> in;
+  Rows<T, 1, EPT, LOAD, FIT, NARROW> in;
   in.base[0] = static_cast<const T*>(p.x); in.ld[0] = p.ld_x; in.rows = p.rows; in.cols = C; in.tid = tid; in.G = G;
   in.step = static_cast<long long>(gridDim.x) * groups;
   in.wbuf = wbuf;
@@ -582,15 +603,17 @@ row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
   if constexpr (MODE != kInt8) {
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-      load_params<V, FULL>(p.gamma, p.vec_params, (tid + j * G) * V, C, 1.0f, w + j * V);
-      load_params<V, FULL>(p.beta, p.vec_params, (tid + j * G) * V, C, 0.0f, b + j * V);
+      load_params<V, FIT>(p.gamma, p.vec_params, (tid + j * G) * V, C, 1.0f, w + j * V);
+      load_params<V, FIT>(p.beta, p.vec_params, (tid + j * G) * V, C, 0.0f, b + j * V);
     }
   }
   const float inv_c = 1.0f / C;
   int parity = 0;
-  for (long long r = first; r - g.sub() < p.rows; r += in.step, parity ^= 1) {
+#pragma unroll 1
+  for (long long r = in.AHEAD ? first - in.step : first; r - g.sub() < p.rows; r += in.step, parity ^= 1) {
     float row[1][EPT];
-    in.take(r, row);
+    in.take(g, r, row);
+    if (in.AHEAD && r < first) continue;
     float (&v)[EPT] = row[0];
     const bool exists = in.ok() && (!NARROW || r < p.rows);
     if (MODE != kInt8) {
@@ -605,8 +628,8 @@ row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
       for (int j = 0; j < VPT; ++j) {
         const int c = (tid + j * G) * V;
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[j * V + i] -= mean0;
-        if (!FULL && c + V > C) {                        // elements that do not exist
+        for (int i = 0; i < V; ++i) v[j * V + i] -= FIT == kWhole && c >= C ? 0.0f : mean0;
+        if (FIT == kRagged && c + V > C) {                        // elements that do not exist
 #pragma unroll
           for (int i = 0; i < V; ++i)
             if (c + i >= C) v[j * V + i] = 0.0f;
@@ -627,14 +650,14 @@ row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
 #pragma unroll
         for (int i = 0; i < V; ++i) v[j * V + i] = fmaf(fmaf(v[j * V + i], rstd, minus), w[j * V + i], b[j * V + i]);
         // (a full row piece by piece: its stores leave while the next piece is computed)
-        if (MODE == kNorm && FULL && exists) *reinterpret_cast<uint4*>(static_cast<T*>(p.y) + r * p.ld_y + c) = pack(v + j * V, static_cast<const T*>(nullptr));
-        if (MODE != kNorm && !FULL && c + V > C) {
+        if (MODE == kNorm && FIT != kRagged && exists && piece_exists<FIT, V>(c, C)) *reinterpret_cast<uint4*>(static_cast<T*>(p.y) + r * p.ld_y + c) = pack(v + j * V, static_cast<const T*>(nullptr));
+        if (MODE != kNorm && FIT == kRagged && c + V > C) {
 #pragma unroll
           for (int i = 0; i < V; ++i)
             if (c + i >= C) v[j * V + i] = 0.0f;
         }
       }
-      if (MODE == kNorm && !FULL) store_row<T, EPT, FULL, NARROW>(static_cast<T*>(p.y) + r * p.ld_y, exists, p.vec_y, tid, G, C, wbuf, v);
+      if (MODE == kNorm && FIT == kRagged) store_row<T, EPT, FIT, NARROW>(static_cast<T*>(p.y) + r * p.ld_y, exists, p.vec_y, tid, G, C, wbuf, v);
       if (MODE == kNorm && tid == 0 && exists) {
         if (p.mean) p.mean[r] = mean0 + shift;
         if (p.rstd) p.rstd[r] = rstd;
@@ -662,10 +685,10 @@ row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
                                     __byte_perm(quantize1(v[j * V + i + 2], factor), quantize1(v[j * V + i + 3], factor), 0x0040),
                                     0x5410);
         if (!exists) continue;
-        if (FULL || c + V <= C) {
+        if (piece_exists<FIT, V>(c, C)) {
           if constexpr (V == 8) *reinterpret_cast<uint2*>(q + c) = make_uint2(word[0], word[1]);
           else *reinterpret_cast<uint32_t*>(q + c) = word[0];
-        } else {
+        } else if (FIT == kRagged) {
 #pragma unroll
           for (int i = 0; i < V; ++i)
             if (c + i < C) q[c + i] = static_cast<int8_t>(word[i / 4] >> (8 * (i & 3)));
@@ -750,18 +773,18 @@ __global__ void __launch_bounds__(256) norm_bwd_columns_kernel(const NormBwdPara
 // dbeta in registers over all of them; at the end the block adds its groups' sums (in order) into one row of partial
 // sums.  One pass over x and dy.  Rows wider than 8192 elements (EPT 32: 64 sums a thread leave no room for the row)
 // stay in the ring's stage and are read from there twice.
-template <typename T, int EPT, int LOAD, bool FULL, bool NARROW>
+template <typename T, int EPT, int LOAD, int FIT, bool NARROW>
 __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, int threads_per_row, int ring_depth) {
   constexpr int V = Piece<T>::V, VPT = EPT / V;
   constexpr bool TWICE = EPT == 32;
   static_assert(!TWICE || LOAD == kRing, "a row that is read twice stays in the ring");
   __shared__ float box[2][32];
-  __shared__ uint4 move[FULL ? 1 : 16][FULL ? 1 : 32 * kBouncePieces<T>];
+  __shared__ uint4 move[FIT != kRagged ? 1 : 16][FIT != kRagged ? 1 : 32 * kBouncePieces<T>];
   extern __shared__ __align__(128) uint8_t ring_smem[];   // the ring; at the end [groups][2][cols] sums
   const Group<NARROW> g(threads_per_row);
   const int groups = blockDim.x / g.G, group = g.index, slot = g.index * g.warps, tid = g.tid, G = g.G, C = p.cols;
-  uint4* const wbuf = move[FULL ? 0 : threadIdx.x >> 5];
-  Rows<T, 2, TWICE ? V : EPT, LOAD, FULL, NARROW> in;
+  uint4* const wbuf = move[FIT != kRagged ? 0 : threadIdx.x >> 5];
+  Rows<T, 2, TWICE ? V : EPT, LOAD, FIT, NARROW> in;
   in.base[0] = static_cast<const T*>(p.x); in.ld[0] = p.ld_x;
   in.base[1] = static_cast<const T*>(p.dy); in.ld[1] = p.ld_dy;
   in.rows = p.rows; in.cols = C; in.tid = tid; in.G = G; in.wbuf = wbuf;
@@ -775,17 +798,18 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
   const long long first = static_cast<long long>(blockIdx.x) * groups + group, step = in.step;
   const float inv_c = 1.0f / C;
   float mean = 0.0f, rstd = 0.0f;
-  if (first < p.rows) { mean = *(p.mean + first); rstd = *(p.rstd + first); }
+  if (!in.AHEAD && first < p.rows) { mean = *(p.mean + first); rstd = *(p.rstd + first); }
   float dgamma[EPT], dbeta[EPT], w[TWICE ? 1 : EPT];
   if constexpr (!TWICE) {
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) load_params<V, FULL>(p.gamma, p.vec_gamma, (tid + j * G) * V, C, 1.0f, w + j * V);
+    for (int j = 0; j < VPT; ++j) load_params<V, FIT>(p.gamma, p.vec_gamma, (tid + j * G) * V, C, 1.0f, w + j * V);
   }
 #pragma unroll
   for (int i = 0; i < EPT; ++i) dgamma[i] = dbeta[i] = 0.0f;
   in.start(first);
   int parity = 0;
-  for (long long r = first; r - g.sub() < p.rows; r += step, parity ^= 1) {
+#pragma unroll 1
+  for (long long r = in.AHEAD ? first - step : first; r - g.sub() < p.rows; r += step, parity ^= 1) {
     // the next row's mean and 1/std are on their way while this row is worked on
     const long long after = r + step;
     float next_mean = 0.0f, next_rstd = 0.0f;
@@ -803,7 +827,8 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
     T* const dx = static_cast<T*>(p.dx) + r * p.ld_dx;
     if constexpr (!TWICE) {
       float row[2][EPT];
-      in.take(r, row);
+      in.take(g, r, row);
+      if (in.AHEAD && r < first) { mean = next_mean; rstd = next_rstd; continue; }
       float (&x)[EPT] = row[0], (&dy)[EPT] = row[1];
 #pragma unroll
       for (int i = 0; i < EPT; ++i) gather(x[i], dy[i], w[i], dgamma[i], dbeta[i], i);
@@ -814,23 +839,16 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
         const float m1 = -t.x * inv_c * rstd, m2 = t.y * inv_c;
 #pragma unroll
         for (int i = 0; i < EPT; ++i) dy[i] = fmaf(fmaf(-x[i], m2, dy[i]), rstd, m1);
-        store_row<T, EPT, FULL, NARROW>(dx, exists, p.vec_dx, tid, G, C, wbuf, dy);
+        store_row<T, EPT, FIT, NARROW>(dx, exists, p.vec_dx, tid, G, C, wbuf, dy);
       }
     } else {
-      in.fine = in.fine && mbar_wait(in.bars + 8 * in.stage, in.phase, in.abort_flag);
-      const bool end0 = in.at_end(0, r), end1 = in.at_end(1, r);
+      in.await(g, r);
       auto piece = [&](int t, int c, float* v) {
-        if (t ? end1 : end0) {
-          const T* const row = in.base[t] + r * in.ld[t];
+        if (FIT == kFull || c < C) in.ring_piece(t, in.skew(t, r), c, v);
+        if (!piece_exists<FIT, V>(c, C)) {
 #pragma unroll
-          for (int i = 0; i < V; ++i) v[i] = c + i < C ? load1(row + c + i) : 0.0f;
-        } else {
-          if (c < C) in.ring_piece(t, in.skew(t, r), c, v);
-          if (c + V > C) {
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-              if (c + i >= C) v[i] = 0.0f;
-          }
+          for (int i = 0; i < V; ++i)
+            if (FIT != kRagged || c + i >= C) v[i] = 0.0f;
         }
       };
 #pragma unroll
@@ -839,7 +857,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
         float x[V], dy[V], weight[V];
         piece(0, c, x);
         piece(1, c, dy);
-        load_params<V, FULL>(p.gamma, p.vec_gamma, c, C, 1.0f, weight);
+        load_params<V, FIT>(p.gamma, p.vec_gamma, c, C, 1.0f, weight);
 #pragma unroll
         for (int i = 0; i < V; ++i) gather(x[i], dy[i], weight[i], dgamma[j * V + i], dbeta[j * V + i], i);
       }
@@ -852,10 +870,10 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
           float x[V], dy[V], weight[V];
           piece(0, c, x);
           piece(1, c, dy);
-          load_params<V, FULL>(p.gamma, p.vec_gamma, c, C, 1.0f, weight);
+          load_params<V, FIT>(p.gamma, p.vec_gamma, c, C, 1.0f, weight);
 #pragma unroll
           for (int i = 0; i < V; ++i) dy[i] = fmaf(fmaf(-((x[i] - mean) * rstd), m2, dy[i] * weight[i]), rstd, m1);
-          store_row<T, V, FULL, NARROW>(dx + j * G * V, in.ok(), p.vec_dx, tid, G, C - j * G * V, wbuf, dy);
+          store_row<T, V, FIT, NARROW>(dx + j * G * V, in.ok(), p.vec_dx, tid, G, C - j * G * V, wbuf, dy);
         }
       }
       g.sync();                                        // everyone has read the stage
@@ -968,16 +986,20 @@ cudaError_t launch_row(luq_ctx* ctx, const RowParams& p, bool vec, cudaStream_t 
   // groups share a block while every SM has some; a block has whole warps
   int groups = (G > 256 ? 512 : 256) / G;
   while (groups > 1 && G * groups > 32 && p.rows < static_cast<long long>(groups) * ctx->sm_count) groups >>= 1;
-  const bool full = LOAD != kBounce && vec && p.cols == G * EPT && (MODE == kInt8 || (p.gamma && p.beta));
-  int per_sm = full ? kRowBlocks<MODE, EPT, LOAD, true, NARROW> : kRowBlocks<MODE, EPT, LOAD, false, NARROW>;
+  const int fit = LOAD == kBounce || !vec || (MODE != kInt8 && !(p.gamma && p.beta)) ? kRagged : fit_of<T>(p.cols, G * EPT);
+  int per_sm = fit == kRagged ? kRowBlocks<MODE, EPT, LOAD, kRagged, NARROW> : kRowBlocks<MODE, EPT, LOAD, kWhole, NARROW>;
   if (kRowThreads<EPT, NARROW> == 512 && G <= 256) per_sm = 2;
-  const int row_bytes = Rows<T, 1, EPT, LOAD, false, NARROW>::ring_row_bytes(p.cols);
+  const int row_bytes = Rows<T, 1, EPT, LOAD, kRagged, NARROW>::ring_row_bytes(p.cols);
   const int depth = LOAD == kRing ? ring_depth_for(groups, row_bytes, per_sm > 1 ? kRingBytes : kRingBytesAlone) : 0;
-  const size_t smem = LOAD == kRing ? static_cast<size_t>(Rows<T, 1, EPT, LOAD, false, NARROW>::ring_bytes(groups, depth, p.cols)) : 0;
-  auto kernel = full ? row_kernel<T, MODE, EPT, LOAD, LOAD != kBounce, NARROW> : row_kernel<T, MODE, EPT, LOAD, false, NARROW>;
+  const size_t smem = LOAD == kRing ? static_cast<size_t>(Rows<T, 1, EPT, LOAD, kRagged, NARROW>::ring_bytes(groups, depth, p.cols)) : 0;
+  auto kernel = row_kernel<T, MODE, EPT, LOAD, kRagged, NARROW>;
+  if constexpr (LOAD != kBounce) {
+    if (fit == kWhole) kernel = row_kernel<T, MODE, EPT, LOAD, kWhole, NARROW>;
+    if (fit == kFull) kernel = row_kernel<T, MODE, EPT, LOAD, kFull, NARROW>;
+  }
   if (LOAD == kRing) {
-    static luq_once_per_device once[2];
-    const cudaError_t e = allow_smem(kernel, once[full], ctx->device);
+    static luq_once_per_device once[3];
+    const cudaError_t e = allow_smem(kernel, once[fit], ctx->device);
     if (e != cudaSuccess) return e;
   }
   const long long blocks = (p.rows + groups - 1) / groups;
@@ -988,8 +1010,10 @@ cudaError_t launch_row(luq_ctx* ctx, const RowParams& p, bool vec, cudaStream_t 
 
 template <typename T, int MODE, int EPT, bool NARROW>
 cudaError_t launch_row_from(luq_ctx* ctx, const RowParams& p, bool vec_x, bool vec, bool ring, cudaStream_t st) {
-  if (ring) return launch_row<T, MODE, EPT, kRing, NARROW>(ctx, p, vec, st);
-  return vec_x ? launch_row<T, MODE, EPT, kDirect, NARROW>(ctx, p, vec, st) : launch_row<T, MODE, EPT, kBounce, NARROW>(ctx, p, vec, st);
+  if (ring || (!NARROW && !vec_x)) return launch_row<T, MODE, EPT, kRing, NARROW>(ctx, p, vec, st);
+  if constexpr (NARROW)
+    if (!vec_x) return launch_row<T, MODE, EPT, kBounce, NARROW>(ctx, p, vec, st);
+  return launch_row<T, MODE, EPT, kDirect, NARROW>(ctx, p, vec, st);
 }
 template <typename T, int MODE, int EPT>
 cudaError_t launch_row_load(luq_ctx* ctx, const RowParams& p, bool vec_x, bool vec, bool many, cudaStream_t st) {
@@ -1043,18 +1067,22 @@ int launch_rows(luq_ctx* ctx, RowParams p, cudaStream_t st) {
 template <typename T, int EPT, int LOAD, bool NARROW>
 cudaError_t launch_norm_bwd_rows(int device, const NormBwdParams& p, bool vec, int G, int block, int grid, cudaStream_t st) {
   const int groups = block / G;
-  using R = Rows<T, 2, 16, LOAD, false, NARROW>;
+  using R = Rows<T, 2, 16, LOAD, kRagged, NARROW>;
   const int depth = LOAD == kRing ? ring_depth_for(groups, 2 * R::ring_row_bytes(p.cols), kRingBytesAlone) : 0;
   const int turns = NARROW ? block / 32 : groups;
   const size_t sums = 2 * sizeof(float) * static_cast<size_t>((p.cols + 3) & ~3) * turns;
   const size_t ring = LOAD == kRing ? static_cast<size_t>(R::ring_bytes(groups, depth, p.cols)) : 0;
-  constexpr bool can = LOAD != kBounce && EPT == 16;
-  const bool full = can && vec && p.cols == G * EPT && p.gamma;
-  auto kernel = full ? norm_bwd_kernel<T, EPT, LOAD, can, NARROW> : norm_bwd_kernel<T, EPT, LOAD, false, NARROW>;
-  static luq_once_per_device once[2];
-  const cudaError_t e = allow_smem(kernel, once[full], device);
+  const int fit = LOAD == kBounce || !vec || !p.gamma ? kRagged : fit_of<T>(p.cols, EPT == 16 ? G * EPT : 0);
+  auto kernel = norm_bwd_kernel<T, EPT, LOAD, kRagged, NARROW>;
+  if constexpr (LOAD != kBounce) {
+    if (fit == kWhole) kernel = norm_bwd_kernel<T, EPT, LOAD, kWhole, NARROW>;
+    if constexpr (EPT == 16)
+      if (fit == kFull) kernel = norm_bwd_kernel<T, EPT, LOAD, kFull, NARROW>;
+  }
+  static luq_once_per_device once[3];
+  const cudaError_t e = allow_smem(kernel, once[fit], device);
   if (e != cudaSuccess) return e;
-  return luq_launch_kernel(kernel, grid, block, ring > sums ? ring : sums, st, LUQ_LAUNCH_EARLY, 1, p, G, depth);
+  return luq_launch_kernel(kernel, grid, block, LOAD == kRing && ring > sums ? ring : sums, st, LUQ_LAUNCH_EARLY, 1, p, G, depth);
 }
 
 template <typename T>
@@ -1068,7 +1096,7 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
   p.vec_dx = aligned(p.dx, p.ld_dx, sizeof(T));
   const bool vec_in = aligned(p.x, p.ld_x, sizeof(T)) && aligned(p.dy, p.ld_dy, sizeof(T)), vec = vec_in && p.vec_gamma && p.vec_dx;
   // a row of x and one of dy have to fit the ring
-  if (p.cols <= 16384 && Rows<T, 2, 16, kRing, false, false>::ring_bytes(1, 1, p.cols) <= 192 * 1024) {
+  if (p.cols <= 16384 && Rows<T, 2, 16, kRing, kRagged, false>::ring_bytes(1, 1, p.cols) <= 192 * 1024) {
     // as many sums of both kinds per thread as elements of a row; groups share a block while there are rows for them
     const int ept = p.cols > 8192 ? 32 : 16;
     const int G = threads_of_row(p.cols, ept);
@@ -1084,7 +1112,7 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
     if (ept == 32) e = launch_norm_bwd_rows<T, 32, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
     else if (p.cols <= 512) e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, true>(ctx->device, p, vec, G, block, p.chunks, st)
                                        : launch_norm_bwd_rows<T, 16, kBounce, true>(ctx->device, p, vec, G, block, p.chunks, st);
-    else if (ring) e = launch_norm_bwd_rows<T, 16, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
+    else if (ring || (p.dx != nullptr && !vec_in)) e = launch_norm_bwd_rows<T, 16, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
     else e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, false>(ctx->device, p, vec, G, block, p.chunks, st)
                     : launch_norm_bwd_rows<T, 16, kBounce, false>(ctx->device, p, vec, G, block, p.chunks, st);
   } else {
