@@ -448,15 +448,10 @@ struct Rows {
       if (tid < depth && first + tid * step < rows) fill(tid, first + tid * step);
       issued = 0;
       while (issued < depth && first + issued * step < rows) ++issued;
-    } else {                               // the first turn of the loop, one step before the first row, fetches it
-#pragma unroll
-      for (int t = 0; t < TENSORS; ++t) {
-        for (uint4& w : raw[t]) w = make_uint4(0u, 0u, 0u, 0u);
-        for (T& w : single[t]) w = zero_of(base[0]);
-      }
+    } else {
+      fetch(first);
     }
   }
-  static constexpr bool AHEAD = LOAD != kRing;   // a turn of the loop comes before the first row
   // (in a narrow group's warp, r may lie beyond the rows)
   __device__ __forceinline__ void take(const Group<NARROW>& g, long long r, float (*v)[EPT]) {
     if constexpr (LOAD == kRing) {
@@ -609,11 +604,9 @@ row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
   }
   const float inv_c = 1.0f / C;
   int parity = 0;
-#pragma unroll 1
-  for (long long r = in.AHEAD ? first - in.step : first; r - g.sub() < p.rows; r += in.step, parity ^= 1) {
+  for (long long r = first; r - g.sub() < p.rows; r += in.step, parity ^= 1) {
     float row[1][EPT];
     in.take(g, r, row);
-    if (in.AHEAD && r < first) continue;
     float (&v)[EPT] = row[0];
     const bool exists = in.ok() && (!NARROW || r < p.rows);
     if (MODE != kInt8) {
@@ -773,8 +766,12 @@ __global__ void __launch_bounds__(256) norm_bwd_columns_kernel(const NormBwdPara
 // dbeta in registers over all of them; at the end the block adds its groups' sums (in order) into one row of partial
 // sums.  One pass over x and dy.  Rows wider than 8192 elements (EPT 32: 64 sums a thread leave no room for the row)
 // stay in the ring's stage and are read from there twice.
+// Threads of a block (at most): narrow rows that are fetched element by element need more than the 128 registers of
+// 512 threads - what they spill waits for its load (1032 rows of 187 fp32:
+// 19.8 us with 512 threads, 8.8; 65536 x 128 fp32 29.8 -> 22.3, bf16, which spills little, 15.5 -> 16.0.
+constexpr int bwd_threads(bool narrow) { return narrow ? 384 : 512; }
 template <typename T, int EPT, int LOAD, int FIT, bool NARROW>
-__global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, int threads_per_row, int ring_depth) {
+__global__ void __launch_bounds__(bwd_threads(NARROW)) norm_bwd_kernel(const NormBwdParams p, int threads_per_row, int ring_depth) {
   constexpr int V = Piece<T>::V, VPT = EPT / V;
   constexpr bool TWICE = EPT == 32;
   static_assert(!TWICE || LOAD == kRing, "a row that is read twice stays in the ring");
@@ -798,7 +795,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
   const long long first = static_cast<long long>(blockIdx.x) * groups + group, step = in.step;
   const float inv_c = 1.0f / C;
   float mean = 0.0f, rstd = 0.0f;
-  if (!in.AHEAD && first < p.rows) { mean = *(p.mean + first); rstd = *(p.rstd + first); }
+  if (first < p.rows) { mean = *(p.mean + first); rstd = *(p.rstd + first); }
   float dgamma[EPT], dbeta[EPT], w[TWICE ? 1 : EPT];
   if constexpr (!TWICE) {
 #pragma unroll
@@ -808,8 +805,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
   for (int i = 0; i < EPT; ++i) dgamma[i] = dbeta[i] = 0.0f;
   in.start(first);
   int parity = 0;
-#pragma unroll 1
-  for (long long r = in.AHEAD ? first - step : first; r - g.sub() < p.rows; r += step, parity ^= 1) {
+  for (long long r = first; r - g.sub() < p.rows; r += step, parity ^= 1) {
     // the next row's mean and 1/std are on their way while this row is worked on
     const long long after = r + step;
     float next_mean = 0.0f, next_rstd = 0.0f;
@@ -828,7 +824,6 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p, in
     if constexpr (!TWICE) {
       float row[2][EPT];
       in.take(g, r, row);
-      if (in.AHEAD && r < first) { mean = next_mean; rstd = next_rstd; continue; }
       float (&x)[EPT] = row[0], (&dy)[EPT] = row[1];
 #pragma unroll
       for (int i = 0; i < EPT; ++i) gather(x[i], dy[i], w[i], dgamma[i], dbeta[i], i);
@@ -1018,8 +1013,9 @@ cudaError_t launch_row_from(luq_ctx* ctx, const RowParams& p, bool vec_x, bool v
 template <typename T, int MODE, int EPT>
 cudaError_t launch_row_load(luq_ctx* ctx, const RowParams& p, bool vec_x, bool vec, bool many, cudaStream_t st) {
   if (p.cols > 32 * EPT) return launch_row_from<T, MODE, EPT, false>(ctx, p, vec_x, vec, many, st);
-  // rows of less than a warp: the ring's copies would be too small
-  return launch_row_from<T, MODE, EPT, true>(ctx, p, vec_x, vec, many && p.cols > 512, st);
+  // rows of up to a warp: the ring's copies are small, and pay for rows that fill it and are unaligned only (20000 x
+  // 301 fp32 44 -> 24 us, norm backward 78 -> 38; aligned, 20000 x 320 bf16 backward: 17 us, 23 from the ring)
+  return launch_row_from<T, MODE, EPT, true>(ctx, p, vec_x, vec, (many && p.cols > 512) || (!vec_x && p.cols > 16 * EPT), st);
 }
 
 // Elements per thread by the width alone (what a row becomes must not depend on where it lies).  What counts is the
@@ -1100,8 +1096,15 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
     // as many sums of both kinds per thread as elements of a row; groups share a block while there are rows for them
     const int ept = p.cols > 8192 ? 32 : 16;
     const int G = threads_of_row(p.cols, ept);
+    // (narrow rows: whole warps of them)
     int groups = 512 / G;
-    while (groups > 1 && G * groups > 32 && static_cast<long long>(groups) * ctx->sm_count > p.rows) groups >>= 1;
+    if (p.cols <= 512) {
+      const int per_warp = 32 / G;
+      const long long warps = p.rows / (static_cast<long long>(per_warp) * ctx->sm_count);
+      groups = per_warp * static_cast<int>(warps < 1 ? 1 : warps > bwd_threads(true) / 32 ? bwd_threads(true) / 32 : warps);
+    } else {
+      while (groups > 1 && static_cast<long long>(groups) * ctx->sm_count > p.rows) groups >>= 1;
+    }
     const int block = G * groups;
     long long blocks = ctx->sm_count;
     if (blocks * groups > p.rows) blocks = (p.rows + groups - 1) / groups;
@@ -1109,10 +1112,12 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
     p.chunks = static_cast<int>(blocks);
     reduced = blocks == 1;
     const bool ring = p.dx != nullptr && p.rows >= 2 * blocks * groups;
+    const bool whole = vec && p.gamma && p.cols % Piece<T>::V == 0;
     if (ept == 32) e = launch_norm_bwd_rows<T, 32, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
+    else if (p.cols > 256 && p.cols <= 512 && p.dx != nullptr && !vec_in) e = launch_norm_bwd_rows<T, 16, kRing, true>(ctx->device, p, vec, G, block, p.chunks, st);
     else if (p.cols <= 512) e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, true>(ctx->device, p, vec, G, block, p.chunks, st)
                                        : launch_norm_bwd_rows<T, 16, kBounce, true>(ctx->device, p, vec, G, block, p.chunks, st);
-    else if (ring || (p.dx != nullptr && !vec_in)) e = launch_norm_bwd_rows<T, 16, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
+    else if (ring || (p.dx != nullptr && !whole)) e = launch_norm_bwd_rows<T, 16, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
     else e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, false>(ctx->device, p, vec, G, block, p.chunks, st)
                     : launch_norm_bwd_rows<T, 16, kBounce, false>(ctx->device, p, vec, G, block, p.chunks, st);
   } else {
