@@ -161,9 +161,11 @@ __global__ void __launch_bounds__(512) row_loop_kernel(const RowParams p) {
 // How the pieces get there:
 //   kRing    many wide rows: every group has a ring of whole rows in shared memory, filled by bulk copies several
 //            rows ahead - what an SM can stream is the bytes it has in flight, and registers hold too few.  Rows
-//            that start inside a 16-byte piece are copied with the pieces around them and shifted into place.
+//            that start inside a 16-byte piece are copied with the pieces around them and shifted into place, and
+//            take this way however few they are (890 x 7161 norm: bf16 17 us, fp32 30; fetched element by element
+//            54 and 60)
 //   kDirect  16-byte loads into registers, one row ahead
-//   kBounce  the same for rows that do not start at multiples of 16 bytes: element by element, coalesced,
+//   kBounce  the same for narrow rows that do not start at multiples of 16 bytes: element by element, coalesced,
 //            and through shared memory to their owners in the same warp
 // An element has the same owner in all three, and sums are made in the same order: results do not depend on
 // strides, alignment or the number of rows.
@@ -565,7 +567,9 @@ template <int MODE, int EPT, int LOAD, int FIT, bool NARROW>
 constexpr int kRowBlocks = EPT == 32 && !NARROW ? 1
                            : MODE == kInt8 || (EPT == 16 && (FIT != kRagged || (MODE == kNormInt8 && LOAD == kRing))) ? 3 : 2;
 
-// FIT, for rows of 16384 x 4096 bf16 / 41582 x 704 bf16: 46 / - us with kFull, 57 / 31 with kWhole, - / 45 with kRagged
+// What bounds it: many rows, HBM (16384 x 4096 bf16 norm 46 us, 5.8 TB/s; 8192 x 1024 fp32 13.1 us, 5.1 TB/s); rows
+// that do not fill their threads or are narrow, the instructions per element; few rows, the latency of one row (1.9 us).
+// FIT, norm of 16384 x 4096 bf16: 46 us with kFull, 58 with kWhole; of 41582 x 704 bf16: 31 with kWhole, 45 with kRagged.
 template <typename T, int MODE, int EPT, int LOAD, int FIT, bool NARROW>
 __global__ void __launch_bounds__((kRowThreads<EPT, NARROW>), (kRowBlocks<MODE, EPT, LOAD, FIT, NARROW>))
 row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
@@ -1021,10 +1025,12 @@ cudaError_t launch_row_load(luq_ctx* ctx, const RowParams& p, bool vec_x, bool v
 // Elements per thread by the width alone (what a row becomes must not depend on where it lies).  What counts is the
 // share of a block's 256 x elements that a row's groups use, and how much of a row's fixed cost an element bears
 // (16 -> chosen, norm / norm to int8 / int8, us):
-//   32  whole multiples of 1024: 16384x4096 bf16 57 -> 47 / 70 -> 57 / 37; to int8 also widths that 32 fits as well as
-//       16 does: 5223x3830 bf16 35 -> 31.5 / 20.6 -> 18.1
-//   24  where it fits better: 41582x704 bf16 55 -> 45 / 63 -> 50 / 35 -> 27, 5000x6000 bf16 41 (32) -> 32.5;
-//       norms of odd widths stay at 16, whose rows are rarely aligned and need the registers (60000x700: 86, 24: 131)
+//   32  whole multiples of 1024 that fit 24 no better: 16384x4096 bf16 57 -> 46 / 70 -> 57 / 37; to int8 also widths that
+//       it fits as well as the others: 5223x3830 bf16 35 -> 33 / 21 -> 19.  Unaligned norms it costs dear (10000x1311
+//       fp32 32 -> 61 / 36 -> 44 / 21 -> 23)
+//   24  where it fits better: 41582x704 bf16 41 -> 32 / 48 -> 40 / 26 -> 22, 10000x1311 bf16 27 -> 23 / 32 -> 26 / 19 -> 15,
+//       5000x6144 bf16 (32) 26.7 -> 25.4 / 31.5 -> 30.8 / 21 -> 18; norms of odd widths of up to a warp stay at 16
+//       (60000x700 bf16: 84, 24: 124)
 int elements_per_thread(int mode, int cols) {
   if (cols <= 512) return 16;
   if (cols > 8192) return 32;
@@ -1033,8 +1039,8 @@ int elements_per_thread(int mode, int cols) {
     return G > 256 ? 0.0f : static_cast<float>(cols) / (G * ept) * (G * (256 / G)) / 256.0f;
   };
   const float f16 = fit(16), f24 = fit(24), f32 = fit(32);
-  if (cols > 1024 && (cols % 1024 == 0 || (cols > 2048 && mode != kNorm && f32 >= f16 && f32 >= f24))) return 32;
-  if (f24 >= f16 && f24 > 0.0f && (mode != kNorm || cols % 8 == 0 || f16 == 0.0f)) return 24;
+  if (cols > 1024 && f32 >= f24 && (cols % 1024 == 0 || (cols > 2048 && mode != kNorm && f32 >= f16))) return 32;
+  if (f24 >= f16 && f24 > 0.0f && (mode != kNorm || cols % 8 == 0 || cols > 768)) return 24;
   return f16 > 0.0f ? 16 : 32;
 }
 
