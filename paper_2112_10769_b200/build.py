@@ -1,8 +1,8 @@
 """In-tree build of the sm_100a C-ABI library (``libluq_b200.so``) with nvcc.
 
 ``python -m paper_2112_10769_b200.build`` compiles the translation units
-and links one shared library next to this file.  nvcc cross-compiles without a
-GPU.  The quantizer file is compiled without FMA contraction; nothing is built
+and links one shared library next to this file, and a Python extension (``_calls.so``, host code only)
+that checks the 8-bit operators' arguments.  nvcc cross-compiles without a GPU.  The quantizer file is compiled without FMA contraction; nothing is built
 with fast-math, flush-to-zero or approximate division.
 """
 from __future__ import annotations

@@ -18,6 +18,11 @@
 //              that share a box with another group's, and outputs TMA cannot address, are stored directly
 // All waits are bounded; on expiry the CTA flags LUQ_STATUS_TIMEOUT, drains its copies, frees its
 // tensor memory and returns.
+//
+// What bounds it: many tokens, the L2's delivery of operands next to the tensor cores (16384x4096x4096 175 us, 3.1 POP/s;
+// 8192x4096x1024 32.8 us, 2.1 POP/s, where a tile's contraction is hardly longer than its epilogue); few tokens, the
+// weights' bytes (32 tokens over 64 experts of 2048x1024 14.2 us) or, for one layer, the latency of a launch and one
+// trip through memory (5 tokens, 4096x4096 6.0 us).
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -677,9 +682,9 @@ int launch_out(luq_ctx* ctx, const luq_int8_args& a, const Int8Params& p, long l
 // How long the product takes with each tile, in hundredths of a microsecond past the launch: rounds over the SMs
 // x (stages x the time of one + what a tile costs at its ends).  The rates were fitted to 22 products of 40 to
 // 13097 tokens, each timed with every tile and split; of 26 others the choice was the best or within 10% of it.
-// What a stage takes is its share of the L2 (24 to 32 KB at 75-85 KB a microsecond and SM), not of the tensor cores.  A split pays
-// its meeting and the sums over the other CTAs' memory; it is taken in a single round only.  Examples, token quantizer
-// excluded: 2443x576x4096 14.7 us with 128-token tiles in one round, 24.0 with 64-token tiles in two, 17.2 with pairs;
+// What a stage takes is its share of the L2 (24 to 32 KB at 75-85 KB a microsecond and SM), not of the tensor cores.  A
+// split pays its meeting and the sums over the other CTAs' memory; it is taken in a single round only.  Product
+// alone: 2443x576x4096 14.7 us with 128-token tiles in one round, 24.0 with 64-token tiles in two, 17.2 with pairs;
 // 1313x2340x3033 15.3 with pairs, 21.7 with 128; 142x384x3904 7.0 with 32-token tiles split in four, 12.3 unsplit.
 struct Choice { int tokens, split; };
 template <class Units>
