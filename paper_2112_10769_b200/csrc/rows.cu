@@ -840,6 +840,9 @@ __global__ void __launch_bounds__(bwd_threads(NARROW)) norm_bwd_kernel(const Nor
 #pragma unroll
         for (int i = 0; i < EPT; ++i) dy[i] = fmaf(fmaf(-x[i], m2, dy[i]), rstd, m1);
         store_row<T, EPT, FIT, NARROW>(dx, exists, p.vec_dx, tid, G, C, wbuf, dy);
+      } else if constexpr (LOAD == kRing) {
+        g.sync();                                      // everyone has read the stage
+        in.release(r);
       }
     } else {
       in.await(g, r);
@@ -925,9 +928,11 @@ __global__ void __launch_bounds__(bwd_threads(NARROW)) norm_bwd_kernel(const Nor
   }
 }
 
-// adds the chunks' partial sums in a fixed order: 32 columns by 32 strands per block, four loads in flight each
+// adds the chunks' partial sums in a fixed order: 32 columns by 32 strands per block, five loads in flight each (a
+// chunk for every SM then takes one trip)
 __global__ void __launch_bounds__(1024) norm_bwd_reduce_kernel(const float* partial, int chunks, int cols,
                                                                float* dgamma, float* dbeta) {
+  constexpr int U = 5;
   __shared__ float box[32][33];
   pdl_wait();
   pdl_trigger();
@@ -936,11 +941,12 @@ __global__ void __launch_bounds__(1024) norm_bwd_reduce_kernel(const float* part
   const long long j = static_cast<long long>(blockIdx.x) * 32 + lane;    // column of [dgamma | dbeta]
   float s = 0.0f;
   if (j < total) {
-    for (int k = strand; k < chunks; k += 128) {
-      float v[4];
+    for (int k = strand; k < chunks; k += 32 * U) {
+      float v[U];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = k + 32 * i < chunks ? __ldcg(partial + (k + 32ll * i) * total + j) : 0.0f;
-      s += (v[0] + v[1]) + (v[2] + v[3]);
+      for (int i = 0; i < U; ++i) v[i] = k + 32 * i < chunks ? __ldcg(partial + (k + 32ll * i) * total + j) : 0.0f;
+#pragma unroll
+      for (int i = 0; i < U; ++i) s += v[i];
     }
   }
   box[strand][lane] = s;
@@ -1076,7 +1082,8 @@ cudaError_t launch_norm_bwd_rows(int device, const NormBwdParams& p, bool vec, i
   const size_t sums = 2 * sizeof(float) * static_cast<size_t>((p.cols + 3) & ~3) * turns;
   const size_t ring = LOAD == kRing ? static_cast<size_t>(R::ring_bytes(groups, depth, p.cols)) : 0;
   const int fit = LOAD == kBounce || !vec || !p.gamma ? kRagged : fit_of<T>(p.cols, EPT == 16 ? G * EPT : 0);
-  auto kernel = norm_bwd_kernel<T, EPT, LOAD, kRagged, NARROW>;
+  constexpr int least = LOAD == kDirect && !NARROW ? kWhole : kRagged;     // (such rows take the ring)
+  auto kernel = norm_bwd_kernel<T, EPT, LOAD, least, NARROW>;
   if constexpr (LOAD != kBounce) {
     if (fit == kWhole) kernel = norm_bwd_kernel<T, EPT, LOAD, kWhole, NARROW>;
     if constexpr (EPT == 16)
@@ -1118,15 +1125,14 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
     p.partial = dgamma || dbeta ? ctx->d_workspace : nullptr;
     p.chunks = static_cast<int>(blocks);
     reduced = blocks == 1;
-    const bool ring = p.dx != nullptr && p.rows >= 2 * blocks * groups;
+    const bool ring = p.rows >= 2 * blocks * groups;
     const bool whole = vec && p.gamma && p.cols % Piece<T>::V == 0;
     if (ept == 32) e = launch_norm_bwd_rows<T, 32, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
-    else if (p.cols > 256 && p.cols <= 512 && p.dx != nullptr && !vec_in) e = launch_norm_bwd_rows<T, 16, kRing, true>(ctx->device, p, vec, G, block, p.chunks, st);
+    else if (p.cols > 256 && p.cols <= 512 && !vec_in) e = launch_norm_bwd_rows<T, 16, kRing, true>(ctx->device, p, vec, G, block, p.chunks, st);
     else if (p.cols <= 512) e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, true>(ctx->device, p, vec, G, block, p.chunks, st)
                                        : launch_norm_bwd_rows<T, 16, kBounce, true>(ctx->device, p, vec, G, block, p.chunks, st);
-    else if (ring || (p.dx != nullptr && !whole)) e = launch_norm_bwd_rows<T, 16, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
-    else e = vec_in ? launch_norm_bwd_rows<T, 16, kDirect, false>(ctx->device, p, vec, G, block, p.chunks, st)
-                    : launch_norm_bwd_rows<T, 16, kBounce, false>(ctx->device, p, vec, G, block, p.chunks, st);
+    else if (ring || !whole) e = launch_norm_bwd_rows<T, 16, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
+    else e = launch_norm_bwd_rows<T, 16, kDirect, false>(ctx->device, p, vec, G, block, p.chunks, st);
   } else {
     // workspace: two floats per row, then the chunks' partial sums
     const size_t means = ((static_cast<size_t>(p.rows) * sizeof(float2) + 255) / 256) * 256;
