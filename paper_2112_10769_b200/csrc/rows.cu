@@ -370,10 +370,11 @@ struct Rows {
     ++issued;
   }
   // elements c .. c + V - 1 of tensor t's row in the present stage, m = the row's address & 15
+  template <bool ALIGNED>
   __device__ __forceinline__ void ring_piece(int t, uint32_t m, int c, float* v) const {
     const uint4* const q = reinterpret_cast<const uint4*>(held + (stage * TENSORS + t) * row_bytes) + c / V;
     const uint4 a = q[0];
-    if (FIT != kRagged || m == 0) { unpack(a, base[0], v); return; }
+    if (ALIGNED) { unpack(a, base[0], v); return; }
     const uint4 b = q[1];
     uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     if (m & 8) {
@@ -461,10 +462,19 @@ struct Rows {
 #pragma unroll
       for (int t = 0; t < TENSORS; ++t) {
         const uint32_t m = skew(t, r);
+        // (aligned rows apart: a test for each piece would keep the next one's load waiting)
+        if (m == 0) {
+#pragma unroll
+          for (int j = 0; j < VPT; ++j)
+            if (FIT == kFull || (tid + j * G) * V < cols) ring_piece<true>(t, 0u, (tid + j * G) * V, v[t] + j * V);
+        } else {
+#pragma unroll
+          for (int j = 0; j < VPT; ++j)
+            if ((tid + j * G) * V < cols) ring_piece<false>(t, m, (tid + j * G) * V, v[t] + j * V);
+        }
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
           const int c = (tid + j * G) * V;
-          if (FIT == kFull || c < cols) ring_piece(t, m, c, v[t] + j * V);
           if (!piece_exists<FIT, V>(c, cols)) {
 #pragma unroll
             for (int i = 0; i < V; ++i)
@@ -847,7 +857,10 @@ __global__ void __launch_bounds__(bwd_threads(NARROW)) norm_bwd_kernel(const Nor
     } else {
       in.await(g, r);
       auto piece = [&](int t, int c, float* v) {
-        if (FIT == kFull || c < C) in.ring_piece(t, in.skew(t, r), c, v);
+        if (FIT == kFull || c < C) {
+          if (in.skew(t, r) == 0) in.template ring_piece<true>(t, 0u, c, v);
+          else in.template ring_piece<false>(t, in.skew(t, r), c, v);
+        }
         if (!piece_exists<FIT, V>(c, C)) {
 #pragma unroll
           for (int i = 0; i < V; ++i)
