@@ -777,14 +777,14 @@ __global__ void __launch_bounds__(256) norm_bwd_columns_kernel(const NormBwdPara
 }
 
 // Threads of a block (at most): narrow rows that are fetched element by element need more than the 128 registers of
-// 512 threads - what they spill waits for its load (1032 x 187 fp32 19.8 us with 512 threads, 8.8 with 384; 65536 x 128
-// fp32 29.8 -> 22.1, bf16, which spills little, 15.5 -> 16.1).
+// 512 threads - what they spill waits for its load (1032 x 187 fp32 19.8 us with 512 threads, 8.4 with 384; 65536 x 128
+// fp32 29.8 -> 21.6, bf16, which spills little, 15.5 -> 15.4).
 constexpr int bwd_threads(bool narrow) { return narrow ? 384 : 512; }
 // Rows in registers: a group takes every gridDim.x * groups-th row and keeps its columns' sums of dgamma and
 // dbeta in registers over all of them; at the end the block adds its groups' sums (in order) into one row of partial
 // sums.  One pass over x and dy.  Rows wider than 8192 elements (EPT 32: 64 sums a thread leave no room for the row)
 // stay in the ring's stage and are read from there twice.  16384 x 4096 bf16 72 us (5.6 TB/s, HBM); 4099 x 771 fp32 of
-// pitch 776 17.6 us, the latency of four rows a group and the second kernel's 3 us.
+// pitch 776 16.3 us, the latency of four rows a group and the second kernel's 2.7 us.
 template <typename T, int EPT, int LOAD, int FIT, bool NARROW>
 __global__ void __launch_bounds__(bwd_threads(NARROW)) norm_bwd_kernel(const NormBwdParams p, int threads_per_row, int ring_depth) {
   constexpr int V = Piece<T>::V, VPT = EPT / V;
