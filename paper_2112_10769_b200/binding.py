@@ -172,7 +172,7 @@ class Context:
     def close(self):
         if getattr(self, "handle", None):
             load().luq_destroy(self.handle)
-            self.handle = None
+            self.handle, self._address = None, 0       # (null: every call refuses it)
 
     def __del__(self):  # pragma: no cover
         try:

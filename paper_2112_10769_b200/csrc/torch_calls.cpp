@@ -58,6 +58,7 @@ struct Args {
     if (given != wanted) type_error("wrong number of arguments");
     ctx = static_cast<luq_ctx*>(PyLong_AsVoidPtr(*at++));
     if (PyErr_Occurred()) throw Raised{};
+    if (!ctx) check(LUQ_ERR_ARG, "the context is closed");
     device = integer();
   }
   int64_t integer() {

@@ -1,0 +1,39 @@
+"""The host side of layer norm and the 8-bit operators: contexts, modules and their buffers.  No GPU needed."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2112_10769_b200 import binding
+from paper_2112_10769_b200 import build as libbuild
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    libbuild.build()
+    return binding.load()
+
+
+def test_a_closed_context_is_refused(monkeypatch):
+    # what a closed context owned has been freed: its address must not reach the library any more
+    destroyed = []
+
+    class Library:
+        @staticmethod
+        def luq_destroy(handle):
+            destroyed.append(handle.value)
+
+    ctx = binding.Context.__new__(binding.Context)
+    ctx.device, ctx.handle, ctx._address, ctx._native = 0, ctypes.c_void_p(4096), 4096, binding.native()
+    with monkeypatch.context() as m:
+        m.setattr(binding, "load", lambda: Library)
+        ctx.close()
+    assert destroyed == [4096]
+    x = torch.zeros(2, 16)
+    for call in (lambda: ctx.layer_norm(x), lambda: ctx.layer_norm_bwd(x, x, x, x), lambda: ctx.layer_norm_int8(x),
+                 lambda: ctx.quant_int8_rows(x), lambda: ctx.gemm_int8(x, x, x, x), lambda: ctx.gemm_int8_grouped(x, x, x, x, x),
+                 lambda: ctx.quant_int8_gemm(x, x, x), lambda: ctx.layer_norm_int8_gemm(x, None, None, 1e-5, x, x),
+                 lambda: ctx.quant_int8_gemm_grouped(x, x, x, x)):
+        with pytest.raises(binding.LuqError) as e:
+            call()
+        assert e.value.code == binding.ERR_ARG
