@@ -436,8 +436,9 @@ int luq_gemm_int8_grouped(luq_ctx* ctx, const int8_t* d_x_codes, int64_t ld_x, c
 
 /* Quantizer and product in one call, from the high-precision tokens x [M x K]: luq_quant_int8_rows then
  * luq_gemm_int8 / luq_gemm_int8_grouped, or luq_layer_norm_int8 then luq_gemm_int8, with the same results bit
- * for bit.  The tokens' codes and scales stay in the context's workspace: M * (16 * ceil(K / 16) + 4) bytes,
- * LUQ_ERR_WORKSPACE beyond 96 MiB (make the two calls, or more calls with fewer rows). */
+ * for bit.  The tokens' codes and scales stay in the context's workspace, M * (16 * ceil(K / 16) + 4) bytes; where
+ * that is more than its 96 MiB, the call works through the rows in chunks of at least 1024, and for K > 98288, where
+ * 1024 rows do not fit, it returns LUQ_ERR_WORKSPACE (make the two calls). */
 int luq_quant_int8_gemm(luq_ctx* ctx, const void* d_x, int dtype, int64_t ld_x,
                         const int8_t* d_w_codes, int64_t ld_w, const float* d_sw, const float* d_bias,
                         void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream);

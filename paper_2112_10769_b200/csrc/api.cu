@@ -42,7 +42,7 @@ const char* luq_strerror(int code) {
     case LUQ_ERR_ARG: return "invalid argument (null or misaligned pointer, bad size or sample count)";
     case LUQ_ERR_CUDA: return "a CUDA call failed";
     case LUQ_ERR_UNSUPPORTED: return "unsupported device or option";
-    case LUQ_ERR_WORKSPACE: return "split workspace too small for this problem";
+    case LUQ_ERR_WORKSPACE: return "workspace too small for this problem";
     default: return "unknown error";
   }
 }
@@ -501,6 +501,8 @@ namespace {
 
 constexpr int64_t kMaxExtent = (1ll << 31) - 4096;   // tile counts and rounded-up extents stay in int32
 
+constexpr int64_t kLeastChunk = 1024;                // rows of a chunk of the one-call products
+
 bool element_type(int dtype) { return dtype == LUQ_F32 || dtype == LUQ_BF16; }
 // a tensor of rows x cols elements of `dtype` with a row stride: present if needed, aligned to its elements
 bool tensor_ok(const void* p, int dtype, int64_t rows, int64_t cols, int64_t ld, bool needed) {
@@ -542,19 +544,34 @@ int int8_product(luq_ctx* ctx, luq_int8_args a, int z_dtype, bool grouped, const
   if (a.M == 0 || a.N == 0) return LUQ_OK;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return LUQ_ERR_CUDA;
-  if (!from_codes) {
-    a.ld_x = (a.K + 15) / 16 * 16;
-    const size_t codes = static_cast<size_t>(a.M) * static_cast<size_t>(a.ld_x);
-    if (codes + static_cast<size_t>(a.M) * sizeof(float) > ctx->workspace_bytes) return LUQ_ERR_WORKSPACE;
-    int8_t* const q = reinterpret_cast<int8_t*>(ctx->d_workspace);
-    float* const s = reinterpret_cast<float*>(q + codes);
-    const int e = cuda_rc(luq_launch_int8_rows(ctx, x, dtype, a.M, static_cast<int>(a.K), ld_x, norm, gamma, beta, eps, q,
-                                               a.ld_x, s, as_stream(stream)));
-    if (e) return e;
-    a.x_codes = q;
-    a.sx = s;
+  a.row0 = 0;
+  a.all_rows = a.M;
+  if (from_codes) return cuda_rc(luq_launch_gemm_int8(ctx, a, false, as_stream(stream)));
+  // Rows whose codes do not fit the workspace together are taken in equal chunks, one after the other.  Every chunk
+  // reads the weights again: one of less than kLeastChunk rows (K > 98288) would be bound by them.
+  a.ld_x = (a.K + 15) / 16 * 16;
+  int64_t chunk = a.M;
+  const int64_t fit = static_cast<int64_t>(ctx->workspace_bytes / (static_cast<size_t>(a.ld_x) + sizeof(float)));
+  if (fit < a.M) {
+    if (fit < kLeastChunk) return LUQ_ERR_WORKSPACE;
+    const int64_t most = fit / 256 * 256, chunks = (a.M + most - 1) / most;      // whole tiles of any size
+    chunk = ((a.M + chunks - 1) / chunks + 255) / 256 * 256;
   }
-  return cuda_rc(luq_launch_gemm_int8(ctx, a, !from_codes, as_stream(stream)));
+  const char* const rows = static_cast<const char*>(x);
+  char* const z = static_cast<char*>(a.z);
+  int8_t* const q = reinterpret_cast<int8_t*>(ctx->d_workspace);
+  float* const s = reinterpret_cast<float*>(q + chunk * a.ld_x);
+  a.x_codes = q;
+  a.sx = s;
+  for (; a.row0 < a.all_rows; a.row0 += chunk) {
+    a.M = a.all_rows - a.row0 < chunk ? a.all_rows - a.row0 : chunk;
+    a.z = z + a.row0 * a.ld_z * (z_dtype == LUQ_BF16 ? 2 : 4);
+    int e = cuda_rc(luq_launch_int8_rows(ctx, rows + a.row0 * ld_x * (dtype == LUQ_BF16 ? 2 : 4), dtype, a.M, static_cast<int>(a.K),
+                                         ld_x, norm, gamma, beta, eps, q, a.ld_x, s, as_stream(stream)));
+    if (!e) e = cuda_rc(luq_launch_gemm_int8(ctx, a, true, as_stream(stream)));
+    if (e) return e;
+  }
+  return LUQ_OK;
 }
 
 luq_int8_args int8_args(const int8_t* x, int64_t ld_x, const float* sx, const int32_t* offsets, int groups, const int8_t* w,

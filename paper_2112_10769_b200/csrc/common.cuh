@@ -121,6 +121,7 @@ struct luq_int8_args {
   const float* sw; const float* bias;
   void* z; int out_bf16; int64_t ld_z;
   int64_t M, N, K;
+  int64_t row0, all_rows;                               // the M rows are row0 .. of the all_rows that the offsets count
 };
 // early: the preceding kernel of the stream is this call's quantizer, which writes x_codes and sx only
 int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, bool early, cudaStream_t st);

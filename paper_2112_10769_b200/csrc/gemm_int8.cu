@@ -52,6 +52,7 @@ struct Int8Params {
   long long ld_z;
   unsigned int* status;
   long long M, N;
+  int row0, all_rows;       // these M rows are row0 .. of the rows that the offsets count
   int groups;
   int num_kb;
   int tiles_n;              // channel tiles
@@ -121,9 +122,9 @@ __device__ __forceinline__ void load_chunk(uint32_t taddr, uint32_t (&r)[CHUNK])
   else tmem_ld_32x16(taddr, r);
 }
 
-// Row ranges of the groups and the running count of their token tiles, by one warp.  Offsets are taken
-// as their running maximum clamped to [0, M]: whatever they hold, every row belongs to one group at most and no
-// address leaves the tensors; offsets that had to be changed raise LUQ_STATUS_OFFSETS.
+// Row ranges of the groups among this launch's rows and the running count of their token tiles, by one warp.  Offsets
+// are taken as their running maximum clamped to [0, all_rows]: whatever they hold, every row belongs to one group at
+// most and no address leaves the tensors; offsets that had to be changed raise LUQ_STATUS_OFFSETS.
 __device__ __forceinline__ void find_groups(const Int8Params& p, int tile_rows, int* hi, int* first_tile, bool report) {
   const int lane = threadIdx.x & 31;
   const int M = static_cast<int>(p.M);
@@ -132,14 +133,14 @@ __device__ __forceinline__ void find_groups(const Int8Params& p, int tile_rows, 
   for (int e0 = 0; e0 <= p.groups; e0 += 32) {
     const int e = e0 + lane;
     const int raw = e <= p.groups ? *(p.offsets + e) : 0;
-    int v = min(max(raw, 0), M);
+    int v = min(max(raw, 0), p.all_rows);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int up = __shfl_up_sync(0xFFFFFFFFu, v, o);
       if (lane >= o) v = max(v, up);
     }
     v = max(v, carry);
-    if (e <= p.groups) { hi[e] = v; bad |= v != raw; }
+    if (e <= p.groups) { hi[e] = min(max(v - p.row0, 0), M); bad |= v != raw; }
     carry = __shfl_sync(0xFFFFFFFFu, v, 31);
   }
   if (report && __any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicOr(p.status, LUQ_STATUS_OFFSETS);
@@ -714,6 +715,7 @@ int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, bool early, cudaS
   Int8Params p{};
   p.sx = a.sx; p.sw = a.sw; p.bias = a.bias; p.offsets = a.offsets; p.z = a.z; p.ld_z = a.ld_z; p.status = ctx->d_status;
   p.M = a.M; p.N = a.N; p.groups = a.groups; p.early = early;
+  p.row0 = static_cast<int>(a.row0); p.all_rows = static_cast<int>(a.all_rows);
   p.num_kb = static_cast<int>((a.K + kBk - 1) / kBk);
   const int64_t esize = a.out_bf16 ? 2 : 4;
   p.z_tma = (reinterpret_cast<uintptr_t>(a.z) & 15u) == 0 && (a.ld_z * esize) % 16 == 0;
