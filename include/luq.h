@@ -30,7 +30,8 @@
  *     luq_status(): outputs stay defined (zero codes and a zero scale for a
  *     non-finite or out-of-range max; unspecified values after a TIMEOUT).
  *   - A context serves one stream at a time; calls that overlap on the GPU
- *     through the same context race on its workspace.
+ *     through the same context race on its workspace.  With luq_set_allocator
+ *     layer norm and the 8-bit calls have no workspace in common and may.
  */
 #ifndef LUQ_H_
 #define LUQ_H_
@@ -377,6 +378,16 @@ int luq_gemm_wgrad_static(const uint8_t* d_g_codes, const float* d_alpha, int n_
                           const uint8_t* d_a_codes, const float* d_sa,
                           float* d_dw, int64_t M, int64_t N, int64_t K, void* stream);
 
+/* Where layer norm's backward pass and the one-call 8-bit products take their workspace from: alloc(user, bytes, stream)
+ * returns device memory of at least `bytes` bytes (at most 96 MiB; 256-byte aligned, on the context's device, which is
+ * current) whose earlier users on `stream` may still be running, NULL if there is none (the call then returns
+ * LUQ_ERR_WORKSPACE); release(user, ptr, stream) takes it back while the call's kernels may still be running on `stream`:
+ * the next user has to come after them in that stream.  Both are called on the thread of the call and must not
+ * throw.  alloc = NULL: the context's own workspace (default). */
+typedef void* (*luq_alloc_fn)(void* user, size_t bytes, void* stream);
+typedef void (*luq_release_fn)(void* user, void* ptr, void* stream);
+int luq_set_allocator(luq_ctx* ctx, luq_alloc_fn alloc, luq_release_fn release, void* user);
+
 /* ---- layer norm, and answering in 8 bits -----------------------------------------------------------
  * What a Transformer block needs around the products above, and the integer form in which a trained
  * layer answers (the paper trains; it has no counterpart of these).  Rows are tokens.  Row strides
@@ -397,7 +408,7 @@ int luq_layer_norm(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int64
  *   dx = rstd * (g - mean_c(g) - xhat * mean_c(g * xhat)),  dgamma = sum_r dy * xhat,  dbeta = sum_r dy.
  * d_dx, d_dgamma, d_dbeta: each may be NULL (not needed).  dy, x and dx have the element type `dtype`,
  * the others are fp32.  The sums over rows are made in a fixed order (results repeat bit for bit); their
- * partial sums use the context's workspace.  rows = 0 gives zero dgamma and dbeta. */
+ * partial sums use a workspace.  rows = 0 gives zero dgamma and dbeta. */
 int luq_layer_norm_bwd(luq_ctx* ctx, const void* d_dy, int64_t ld_dy, const void* d_x, int64_t ld_x, int dtype,
                        int64_t rows, int64_t cols, const float* d_gamma, const float* d_mean, const float* d_rstd,
                        void* d_dx, int64_t ld_dx, float* d_dgamma, float* d_dbeta, void* stream);
@@ -436,8 +447,8 @@ int luq_gemm_int8_grouped(luq_ctx* ctx, const int8_t* d_x_codes, int64_t ld_x, c
 
 /* Quantizer and product in one call, from the high-precision tokens x [M x K]: luq_quant_int8_rows then
  * luq_gemm_int8 / luq_gemm_int8_grouped, or luq_layer_norm_int8 then luq_gemm_int8, with the same results bit
- * for bit.  The tokens' codes and scales stay in the context's workspace, M * (16 * ceil(K / 16) + 4) bytes; where
- * that is more than its 96 MiB, the call works through the rows in chunks of at least 1024, and for K > 98288, where
+ * for bit.  The tokens' codes and scales stay in a workspace, M * (16 * ceil(K / 16) + 4) bytes; where
+ * that is more than 96 MiB, the call works through the rows in chunks of at least 1024, and for K > 98288, where
  * 1024 rows do not fit, it returns LUQ_ERR_WORKSPACE (make the two calls). */
 int luq_quant_int8_gemm(luq_ctx* ctx, const void* d_x, int dtype, int64_t ld_x,
                         const int8_t* d_w_codes, int64_t ld_w, const float* d_sw, const float* d_bias,

@@ -26,7 +26,8 @@ _contexts: dict[int, binding.Context] = {}
 
 
 def context(device: torch.device) -> binding.Context:
-    """One library context per device, created on first use."""
+    """One library context per device, created on first use.  Layer norm and the 8-bit modules may use it on several streams
+    at once; the 4-bit layers share its workspace and run on one at a time."""
     index = device.index if device.index is not None else torch.cuda.current_device()
     if index not in _contexts:
         _contexts[index] = binding.Context(index)

@@ -34,7 +34,7 @@ SYMBOLS = ("luq_create", "luq_destroy", "luq_set_option", "luq_kmax", "luq_debug
            "luq_amax_multi", "luq_quant_int4_multi", "luq_quant_int4_hindsight_gemm_fwd", "luq_quant_uint4", "luq_amax_quant_int4", "luq_quant_int4_hindsight", "luq_quant_grad", "luq_amax_quant_grad", "luq_quant_grad_nearest", "luq_quant_grad_ablation", "luq_quant_grad_pw2",
            "luq_quant_grad_hindsight", "luq_debug_quotient", "luq_debug_expire_wait", "luq_debug_bounds_probe", "luq_gemm_fwd", "luq_quant_int4_gemm_fwd", "luq_gemm_bwd", "luq_gemm_wgrad",
            "luq_layer_norm", "luq_layer_norm_bwd", "luq_layer_norm_int8", "luq_quant_int8_rows", "luq_gemm_int8",
-           "luq_gemm_int8_grouped", "luq_quant_int8_gemm", "luq_layer_norm_int8_gemm", "luq_quant_int8_gemm_grouped",
+           "luq_gemm_int8_grouped", "luq_quant_int8_gemm", "luq_layer_norm_int8_gemm", "luq_quant_int8_gemm_grouped", "luq_set_allocator",
            "luq_gemm_wgrad_static", "luq_status", "luq_launch_count", "luq_strerror")
 
 _lib = None
@@ -94,6 +94,7 @@ def load() -> ctypes.CDLL:
         L.luq_quant_int8_gemm.argtypes = [vp, vp, ci, i64, vp, i64, vp, vp] + product
         L.luq_layer_norm_int8_gemm.argtypes = [vp, vp, ci, i64, vp, vp, cf, vp, i64, vp, vp] + product
         L.luq_quant_int8_gemm_grouped.argtypes = [vp, vp, ci, i64, vp, ci, vp, i64, i64, vp, vp] + product
+        L.luq_set_allocator.argtypes = [vp, vp, vp, vp]
         L.luq_status.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int)]
         L.luq_launch_count.argtypes = [vp]
         L.luq_launch_count.restype = i64
@@ -121,7 +122,8 @@ def _dtype_value(dtype: torch.dtype) -> int:
 
 _native = None
 _NATIVE_ENTRIES = ("luq_layer_norm", "luq_layer_norm_bwd", "luq_layer_norm_int8", "luq_quant_int8_rows", "luq_gemm_int8",
-                   "luq_gemm_int8_grouped", "luq_quant_int8_gemm", "luq_layer_norm_int8_gemm", "luq_quant_int8_gemm_grouped")
+                   "luq_gemm_int8_grouped", "luq_quant_int8_gemm", "luq_layer_norm_int8_gemm", "luq_quant_int8_gemm_grouped",
+                   "luq_set_allocator")
 
 
 def native():
@@ -158,7 +160,8 @@ def _check(rc: int, what: str):
 
 
 class Context:
-    """Owns one luq_ctx (status word + split workspace) on a device."""
+    """Owns one luq_ctx (status word + split workspace) on a device.  One stream at a time uses it, but for layer norm and
+    the 8-bit calls."""
 
     def __init__(self, device: int = 0):
         if not torch.cuda.is_available():
@@ -168,6 +171,7 @@ class Context:
         _check(load().luq_create(ctypes.byref(h), device), "luq_create")
         self.handle = h
         self._address, self._native = h.value, native()
+        self._native.attach(self._address)
 
     def close(self):
         if getattr(self, "handle", None):
@@ -448,7 +452,8 @@ class Context:
     # Tokens are rows: tensors whose rows are contiguous (leading dimensions are flattened); other layouts and
     # broadcast rows are copied first.  int8 codes are [rows, cols] views of rows that start at multiples of
     # 16 bytes (new_codes makes them).  Types, shapes and devices are checked in native code (_calls), which
-    # raises TypeError; the C entry points' own refusals raise LuqError.
+    # raises TypeError; the C entry points' own refusals raise LuqError.  These calls may overlap on several streams:
+    # what they need beside their outputs is torch's memory of the stream they run on.
     def new_codes(self, rows: int, cols: int) -> torch.Tensor:
         """Uninitialised int8 codes [rows, cols] in the layout the products read."""
         return torch.empty((rows, -(-cols // 16) * 16), dtype=torch.int8, device=f"cuda:{self.device}")[:, :cols]

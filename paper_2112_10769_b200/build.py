@@ -63,7 +63,7 @@ def build_native(force: bool = False) -> str:
                                                     os.path.join(cpp_extension.CUDA_HOME or "/usr/local/cuda", "include")]
         cmd = ["g++", "-std=c++20", "-O2", "-fPIC", "-shared", "-fvisibility=hidden",
                f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", src, "-o", NATIVE]
-        cmd += [f"-isystem{d}" for d in includes] + [f"-L{lib_dir}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+        cmd += [f"-isystem{d}" for d in includes] + [f"-L{lib_dir}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"]
         subprocess.run(cmd, check=True)
         _stamp(NATIVE, digest)
     return NATIVE

@@ -495,6 +495,14 @@ int luq_gemm_wgrad(luq_ctx* ctx, const uint8_t* d_g_codes, const float* d_alpha,
   return cuda_rc(luq_launch_gemm(ctx, a, as_stream(stream)));
 }
 
+int luq_set_allocator(luq_ctx* ctx, luq_alloc_fn alloc, luq_release_fn release, void* user) {
+  if (!ctx || (alloc && !release)) return LUQ_ERR_ARG;
+  ctx->alloc = alloc;
+  ctx->release = release;
+  ctx->alloc_user = user;
+  return LUQ_OK;
+}
+
 // ---- layer norm, and answering in 8 bits ---------------------------------------------------------------
 
 namespace {
@@ -559,7 +567,9 @@ int int8_product(luq_ctx* ctx, luq_int8_args a, int z_dtype, bool grouped, const
   }
   const char* const rows = static_cast<const char*>(x);
   char* const z = static_cast<char*>(a.z);
-  int8_t* const q = reinterpret_cast<int8_t*>(ctx->d_workspace);
+  luq_call_workspace workspace(ctx, stream);
+  int8_t* const q = static_cast<int8_t*>(workspace.get(static_cast<size_t>(chunk) * (static_cast<size_t>(a.ld_x) + sizeof(float))));
+  if (!q) return LUQ_ERR_WORKSPACE;
   float* const s = reinterpret_cast<float*>(q + chunk * a.ld_x);
   a.x_codes = q;
   a.sx = s;

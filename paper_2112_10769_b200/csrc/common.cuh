@@ -29,6 +29,22 @@ struct luq_ctx {
   int kmax;                 // LUQ levels alpha * 2^0 .. alpha * 2^kmax (1..6, default LUQ_KMAX)
   int64_t launches;
   void* encode_tiled;       // cuTensorMapEncodeTiled, resolved at create
+  luq_alloc_fn alloc;       // luq_set_allocator; null: d_workspace
+  luq_release_fn release;
+  void* alloc_user;
+};
+
+// The workspace of one call of the row and 8-bit operators: the caller's allocator's, or the context's own.
+struct luq_call_workspace {
+  luq_ctx* const ctx;
+  void* const stream;
+  void* ptr = nullptr;
+  luq_call_workspace(luq_ctx* c, void* s) : ctx(c), stream(s) {}
+  luq_call_workspace(const luq_call_workspace&) = delete;
+  luq_call_workspace& operator=(const luq_call_workspace&) = delete;
+  // bytes <= ctx->workspace_bytes; null: there is none
+  void* get(size_t bytes) { return ptr = ctx->alloc ? ctx->alloc(ctx->alloc_user, bytes, stream) : ctx->d_workspace; }
+  ~luq_call_workspace() { if (ctx->alloc && ptr) ctx->release(ctx->alloc_user, ptr, stream); }
 };
 
 // internal launchers (defined in quant.cu / gemm.cu); return a cudaError_t as int

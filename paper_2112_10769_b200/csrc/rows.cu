@@ -717,8 +717,8 @@ struct NormBwdParams {
   const float* rstd;
   void* dx;              // may be null
   float2* row_means;     // workspace: mean of g and of g xhat, per row
-  float* partial;        // workspace: [chunks][2][cols] partial dgamma / dbeta; null if neither is wanted
-  float* dgamma;         // the results, written directly by a grid of one block
+  float* partial;        // workspace: [chunks][2][cols] partial dgamma / dbeta
+  float* dgamma;         // the results (may be null), written directly by a grid of one block
   float* dbeta;
   int chunks;
   long long rows_per_chunk;
@@ -899,7 +899,7 @@ __global__ void __launch_bounds__(bwd_threads(NARROW)) norm_bwd_kernel(const Nor
     rstd = next_rstd;
   }
   in.finish(p.status);
-  if (p.partial == nullptr) return;
+  if (!p.dgamma && !p.dbeta) return;
   float* const out = p.partial + 2ll * blockIdx.x * C;
   // a narrow warp's rows first, then the block's warps (or groups) in order, each thread a column
   if constexpr (NARROW) {
@@ -1112,6 +1112,7 @@ template <typename T>
 int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, cudaStream_t st) {
   const size_t per_chunk = 2 * sizeof(float) * static_cast<size_t>(p.cols);
   cudaError_t e = cudaSuccess;
+  luq_call_workspace workspace(ctx, st);
   p.vec_gamma = aligned(p.gamma, 0, 4);
   p.dgamma = dgamma;
   p.dbeta = dbeta;
@@ -1135,9 +1136,12 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
     const int block = G * groups;
     long long blocks = ctx->sm_count;
     if (blocks * groups > p.rows) blocks = (p.rows + groups - 1) / groups;
-    p.partial = dgamma || dbeta ? ctx->d_workspace : nullptr;
     p.chunks = static_cast<int>(blocks);
     reduced = blocks == 1;
+    if ((dgamma || dbeta) && !reduced) {                 // (at most 16384 columns and a block for every SM: 20 MB)
+      p.partial = static_cast<float*>(workspace.get(per_chunk * static_cast<size_t>(blocks)));
+      if (!p.partial) return LUQ_ERR_WORKSPACE;
+    }
     const bool ring = p.rows >= 2 * blocks * groups;
     const bool whole = vec && p.gamma && p.cols % Piece<T>::V == 0;
     if (ept == 32) e = launch_norm_bwd_rows<T, 32, kRing, false>(ctx->device, p, vec, G, block, p.chunks, st);
@@ -1150,8 +1154,6 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
     // workspace: two floats per row, then the chunks' partial sums
     const size_t means = ((static_cast<size_t>(p.rows) * sizeof(float2) + 255) / 256) * 256;
     if (means + per_chunk > ctx->workspace_bytes) return LUQ_ERR_WORKSPACE;
-    p.row_means = reinterpret_cast<float2*>(ctx->d_workspace);
-    p.partial = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(ctx->d_workspace) + means);
     const long long column_tiles = (p.cols + 255) / 256;
     long long chunks = (8ll * ctx->sm_count + column_tiles - 1) / column_tiles;
     const long long room = static_cast<long long>((ctx->workspace_bytes - means) / per_chunk);
@@ -1159,6 +1161,10 @@ int launch_norm_bwd(luq_ctx* ctx, NormBwdParams p, float* dgamma, float* dbeta, 
     if (chunks > p.rows) chunks = p.rows;
     p.rows_per_chunk = (p.rows + chunks - 1) / chunks;
     p.chunks = static_cast<int>((p.rows + p.rows_per_chunk - 1) / p.rows_per_chunk);
+    uint8_t* const w = static_cast<uint8_t*>(workspace.get(means + per_chunk * static_cast<size_t>(p.chunks)));
+    if (!w) return LUQ_ERR_WORKSPACE;
+    p.row_means = reinterpret_cast<float2*>(w);
+    p.partial = reinterpret_cast<float*>(w + means);
     if (p.dx) {
       const long long cap = 4ll * ctx->sm_count;
       e = luq_launch_kernel(norm_bwd_means_kernel<T>, static_cast<int>(p.rows < cap ? p.rows : cap), 512, 0, st,

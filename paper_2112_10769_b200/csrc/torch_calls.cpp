@@ -10,11 +10,16 @@
 
 #include <ATen/ATen.h>
 #include <ATen/core/LegacyTypeDispatch.h>
+#include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
+#include <exception>
+#include <optional>
 #include <string>
+#include <utility>
 
 #include "luq.h"
 
@@ -30,6 +35,7 @@ struct Entry {
   decltype(&luq_quant_int8_gemm) quant_int8_gemm;
   decltype(&luq_layer_norm_int8_gemm) layer_norm_int8_gemm;
   decltype(&luq_quant_int8_gemm_grouped) quant_int8_gemm_grouped;
+  decltype(&luq_set_allocator) set_allocator;
 } lib{};
 PyObject* error_class = nullptr;   // binding.LuqError(code, what)
 
@@ -39,8 +45,12 @@ struct Raised {};
   PyErr_SetString(PyExc_TypeError, what.c_str());
   throw Raised{};
 }
+// What the workspace's allocation threw: it must not pass the library's C entry points, and leaves here.
+thread_local std::exception_ptr thrown;
+
 void check(int rc, const char* what) {
   if (rc == LUQ_OK) return;
+  if (thrown) std::rethrow_exception(std::exchange(thrown, nullptr));
   PyObject* e = PyObject_CallFunction(error_class, "is", rc, what);
   if (e) {
     PyErr_SetObject(error_class, e);
@@ -58,6 +68,7 @@ struct Args {
     if (given != wanted) type_error("wrong number of arguments");
     ctx = static_cast<luq_ctx*>(PyLong_AsVoidPtr(*at++));
     if (PyErr_Occurred()) throw Raised{};
+    thrown = nullptr;
     if (!ctx) check(LUQ_ERR_ARG, "the context is closed");
     device = integer();
   }
@@ -157,8 +168,9 @@ const int32_t* offsets_of(const at::Tensor& t, int64_t groups) {
   return static_cast<const int32_t*>(t.data_ptr());
 }
 
+// (past the dispatcher: it costs as much as the workspace's allocation)
 at::Tensor make(at::IntArrayRef size, at::ScalarType type, int64_t device) {
-  return at::empty(size, at::TensorOptions().dtype(type).device(at::kCUDA, static_cast<at::DeviceIndex>(device)));
+  return at::detail::empty_cuda(size, type, at::Device(at::kCUDA, static_cast<at::DeviceIndex>(device)), std::nullopt);
 }
 // the caller's output (checked), or a new one of type `code`
 at::Tensor output(const at::Tensor* out, int64_t rows, int64_t cols, int64_t code, int64_t device) {
@@ -335,6 +347,31 @@ PyObject* layer_norm_int8_gemm(PyObject* const* args, Py_ssize_t n) {
   return wrap(z);
 }
 
+// A call's workspace is torch's memory of the call's stream: calls on several streams, and graphs, each have their own.
+void* workspace_alloc(void*, size_t bytes, void* stream) {
+  try {
+    return c10::cuda::CUDACachingAllocator::raw_alloc_with_stream(bytes, static_cast<cudaStream_t>(stream));
+  } catch (...) {
+    thrown = std::current_exception();
+    return nullptr;
+  }
+}
+void workspace_release(void*, void* ptr, void*) {
+  try {
+    c10::cuda::CUDACachingAllocator::raw_delete(ptr);
+  } catch (...) {                                        // (the memory is lost, the call's results are there)
+  }
+}
+// attach(ctx): a new context takes its workspaces from torch
+PyObject* attach(PyObject* const* args, Py_ssize_t n) {
+  if (n != 1) type_error("wrong number of arguments");
+  luq_ctx* const ctx = static_cast<luq_ctx*>(PyLong_AsVoidPtr(args[0]));
+  if (PyErr_Occurred()) throw Raised{};
+  thrown = nullptr;
+  check(lib.set_allocator(ctx, workspace_alloc, workspace_release, nullptr), "luq_set_allocator");
+  return Py_NewRef(Py_None);
+}
+
 // bind(error class, addresses of the entry points in the order of Entry)
 PyObject* bind(PyObject* const* args, Py_ssize_t n) {
   constexpr Py_ssize_t count = sizeof(Entry) / sizeof(void*);
@@ -352,6 +389,7 @@ PyObject* bind(PyObject* const* args, Py_ssize_t n) {
 
 #define CALL(name, body) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<body>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CALL("bind", bind),
+                         CALL("attach", attach),
                          CALL("layer_norm", layer_norm),
                          CALL("layer_norm_bwd", layer_norm_bwd),
                          CALL("layer_norm_int8", layer_norm_int8),

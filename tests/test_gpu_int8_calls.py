@@ -1,4 +1,4 @@
-"""The one-call 8-bit products as programs use them: more tokens than the workspace holds."""
+"""The one-call 8-bit products as programs use them: more tokens than the workspace holds, several streams, graphs."""
 import pytest
 import torch
 
@@ -66,3 +66,83 @@ def test_modules_answer_a_long_prompt():
     z = Int8Experts(w)(x, torch.tensor([0, 5000, M], dtype=torch.int32, device="cuda"))
     assert torch.equal(z[:5000], Int8Linear(w[0])(x[:5000])) and torch.equal(z[5000:], Int8Linear(w[1])(x[5000:]))
     assert autograd.context(x.device).status() == 0
+
+
+def test_streams_answer_side_by_side():
+    # two streams through the modules of one device, nothing waits for anything: neither sees the other's codes,
+    # scales or partial sums.  The first calls' results, made one at a time, are the reference
+    from paper_2112_10769_b200.int8 import Int8Experts, Int8Linear
+    g = torch.Generator("cuda").manual_seed(1)
+    K, N, E = 1024, 512, 4
+    w = torch.randn(E, N, K, device="cuda", generator=g)
+    dense, normed, experts = Int8Linear(w[0]), Int8Linear(w[1], norm=torch.nn.LayerNorm(K, device="cuda")), Int8Experts(w)
+    gamma = torch.rand(K, device="cuda", generator=g) + 0.5
+    lib = autograd.context(w.device)
+
+    def calls(x, offsets):
+        _, mean, rstd = lib.layer_norm(x, gamma)
+        return (dense(x), normed(x), experts(x, offsets), *lib.layer_norm_bwd(x.flip(0), x, mean, rstd, gamma))
+
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    inputs, want = [], []
+    for i, rows in enumerate((700, 3000)):
+        x = torch.randn(rows, K, device="cuda", generator=g) * 10.0 ** (2 * i)
+        offsets = torch.tensor([0, rows // 5, rows // 2, rows // 2, rows], dtype=torch.int32, device="cuda")
+        inputs.append((x, offsets))
+        want.append(calls(x, offsets))
+        torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(40):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(calls(*inputs[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for result in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(result, want[i]))
+    assert lib.status() == 0
+
+
+def test_a_graph_has_a_workspace_of_its_own(ctx):
+    # a captured call is replayed while the stream it was captured from goes on with other tokens
+    x, other = (torch.randn(2000, 1024, device="cuda") * f for f in (1, 100))
+    w, sw = ctx.quant_int8_rows(torch.randn(256, 1024, device="cuda"))
+    want, want_other = ctx.quant_int8_gemm(x, w, sw), ctx.quant_int8_gemm(other, w, sw)
+    out = torch.empty_like(want)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        for _ in range(20):
+            ctx.quant_int8_gemm(x, w, sw, out=out)
+    replay = torch.cuda.Stream()
+    for _ in range(10):
+        with torch.cuda.stream(replay):
+            out.zero_()
+            graph.replay()
+        with torch.cuda.stream(stream):
+            got = [ctx.quant_int8_gemm(other, w, sw) for _ in range(20)]
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and all(torch.equal(z, want_other) for z in got)
+    assert ctx.status() == 0
+
+
+def test_no_memory_for_a_workspace_is_torchs_error(ctx):
+    # (a limit of torch's allocator, not of the device: nothing is filled up)
+    M, N, K = 12000, 64, 8192
+    x = torch.randn(M, K, device="cuda")
+    w, sw = ctx.quant_int8_rows(torch.randn(N, K, device="cuda"))
+    want, out = ctx.quant_int8_gemm(x, w, sw), torch.zeros(M, N, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    parts = [b["size"] for s in torch.cuda.memory_snapshot() for b in s["blocks"] if b["state"] == "inactive"]
+    assert max(parts, default=0) < M * K                 # no part of a segment in use would do
+    try:
+        torch.cuda.set_per_process_memory_fraction(1e-6)
+        launches = ctx.launches
+        with pytest.raises(torch.OutOfMemoryError):
+            ctx.quant_int8_gemm(x, w, sw, out=out)
+        assert ctx.launches == launches
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    ctx.quant_int8_gemm(x, w, sw, out=out)
+    assert torch.equal(out, want) and ctx.status() == 0

@@ -37,3 +37,10 @@ def test_a_closed_context_is_refused(monkeypatch):
         with pytest.raises(binding.LuqError) as e:
             call()
         assert e.value.code == binding.ERR_ARG
+
+
+def test_a_context_takes_its_workspaces_from_torch(lib):
+    # what lets calls on several streams share a context (the native half of Context.__init__)
+    assert lib.luq_set_allocator(None, None, None, None) == binding.ERR_ARG
+    with pytest.raises(binding.LuqError):
+        binding.native().attach(0)
