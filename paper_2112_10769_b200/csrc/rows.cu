@@ -74,7 +74,8 @@ __device__ __forceinline__ unsigned int block_max(unsigned int v, unsigned int* 
 // first sum is the more exact one (the rounding of the centred values outweighs what it lost), above it the correction
 // is (a mean 1e4 times the spread: 1e-3 of the spread without it).
 __device__ __forceinline__ void finish_stats(float d1, float d2, float eps, float mean0, float& shift, float& rstd) {
-  const float var = fmaxf(d2 - d1 * d1, 0.0f);
+  float var;                                             // at least zero; NaN, of a row with Inf or NaN, stays NaN
+  asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(var) : "f"(d2 - d1 * d1));
   shift = mean0 * mean0 > var ? d1 : 0.0f;
   rstd = rsqrtf(var + eps);
 }
