@@ -139,7 +139,7 @@ class LuqLinear(torch.nn.Module):
 
 class LayerNormFunction(torch.autograd.Function):
     """Layer norm over the last dimension: forward and backward pass in the library's kernels.  The mean and
-    1/std of every row are kept for the backward pass beside x."""
+    1/std of every row are kept for the backward pass beside x.  There is no second derivative: asking for it raises."""
 
     @staticmethod
     def forward(ctx, x: torch.Tensor, weight: torch.Tensor | None, bias: torch.Tensor | None, eps: float):
@@ -151,15 +151,28 @@ class LayerNormFunction(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy: torch.Tensor):
         x, mean, rstd, weight = ctx.saved_tensors
-        need_dx, need_dweight, need_dbias, _ = ctx.needs_input_grad
-        dx, dweight, dbias = context(x.device).layer_norm_bwd(dy, x, mean, rstd, weight, need_dx, need_dweight, need_dbias)
-        return dx, dweight, dbias, None
+        need = ctx.needs_input_grad[:3]
+        # (with a graph of the gradient asked for, dy or x or the weight may lead to a second derivative)
+        grads = LayerNormGradient.apply if torch.is_grad_enabled() else context(x.device).layer_norm_bwd
+        return *grads(dy, x, mean, rstd, weight, *need), None
+
+
+class LayerNormGradient(torch.autograd.Function):
+    """The backward pass where a graph of it is recorded: differentiating it raises instead of leaving it out."""
+
+    @staticmethod
+    def forward(ctx, dy, x, mean, rstd, weight, *need):
+        return context(x.device).layer_norm_bwd(dy, x, mean, rstd, weight, *need)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("layer_norm is differentiable once: its backward pass has no derivative")
 
 
 def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
                eps: float = 1e-5) -> torch.Tensor:
     """``torch.nn.functional.layer_norm`` over the last dimension.  x is float32 or bfloat16, weight and bias are
-    float32 (or None); the result has the type of x."""
+    float32 (or None); the result has the type of x.  Differentiable once."""
     return LayerNormFunction.apply(x, weight, bias, eps)
 
 

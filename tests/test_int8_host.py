@@ -44,3 +44,35 @@ def test_a_context_takes_its_workspaces_from_torch(lib):
     assert lib.luq_set_allocator(None, None, None, None) == binding.ERR_ARG
     with pytest.raises(binding.LuqError):
         binding.native().attach(0)
+
+
+def test_a_second_derivative_of_layer_norm_is_refused(monkeypatch):
+    # the backward pass is a kernel call that records nothing: differentiating through it has to raise, not to leave
+    # the norm's part out.  The library's calls are played by the formulas here
+    from paper_2112_10769_b200 import autograd
+
+    class Formulas:
+        @staticmethod
+        def layer_norm(x, weight, bias, eps):
+            with torch.no_grad():
+                mean, rstd = x.mean(-1), (x.var(-1, unbiased=False) + eps).rsqrt()
+                return (x - mean[:, None]) * rstd[:, None] * weight + bias, mean, rstd
+
+        @staticmethod
+        def layer_norm_bwd(dy, x, mean, rstd, weight, *need):
+            with torch.no_grad():
+                xhat, g = (x - mean[:, None]) * rstd[:, None], dy * weight
+                dx = rstd[:, None] * (g - g.mean(-1, keepdim=True) - xhat * (g * xhat).mean(-1, keepdim=True))
+                return dx, (dy * xhat).sum(0), dy.sum(0)
+
+    monkeypatch.setattr(autograd, "context", lambda device: Formulas)
+    x = torch.randn(3, 8, requires_grad=True)
+    w, b = torch.rand(8, requires_grad=True), torch.zeros(8, requires_grad=True)
+    for loss in (lambda y: y.square().sum(), lambda y: (y * torch.arange(8.0)).sum()):      # dy has a graph; has none
+        for of in (x, w):
+            first = torch.autograd.grad(loss(autograd.layer_norm(x, w, b)), of, create_graph=True)[0]
+            with pytest.raises(RuntimeError, match="differentiable once"):
+                (first.square().sum() + x.sum()).backward()
+    x.grad = None
+    autograd.layer_norm(x, w, b).square().sum().backward()          # one derivative as ever
+    assert torch.allclose(x.grad, torch.autograd.grad(torch.nn.functional.layer_norm(x, (8,), w, b).square().sum(), x)[0], atol=1e-4)
