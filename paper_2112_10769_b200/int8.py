@@ -26,6 +26,11 @@ def quantize_weight(w: torch.Tensor):
     return codes.as_strided(w.shape, (w.shape[-2] * ld, ld, 1)), scale.view(w.shape[:-1])
 
 
+def _snapshot(t: torch.Tensor | None):
+    """A parameter as it is now, in 32 bits and in memory of its own."""
+    return None if t is None else t.detach().to(torch.float32, copy=True).contiguous()
+
+
 class Int8Linear(torch.nn.Module):
     """``torch.nn.Linear`` in 8 bits.  ``norm``: a layer norm module (``autograd.LayerNorm`` or
     ``torch.nn.LayerNorm`` over the last dimension) that is applied to the tokens first, in the same call."""
@@ -35,14 +40,14 @@ class Int8Linear(torch.nn.Module):
         codes, scale = quantize_weight(weight)
         self.register_buffer("codes", codes)
         self.register_buffer("scale", scale)
-        self.register_buffer("bias", None if bias is None else bias.detach().float())
+        self.register_buffer("bias", _snapshot(bias))
         self.eps = None
         if norm is not None:
             if tuple(norm.normalized_shape) != (weight.shape[-1],):
                 raise ValueError("the layer norm has to run over the inputs of the layer")
             self.eps = float(norm.eps)
-            self.register_buffer("norm_weight", None if norm.weight is None else norm.weight.detach().float())
-            self.register_buffer("norm_bias", None if norm.bias is None else norm.bias.detach().float())
+            self.register_buffer("norm_weight", _snapshot(norm.weight))
+            self.register_buffer("norm_bias", _snapshot(norm.bias))
 
     @classmethod
     def of(cls, layer: torch.nn.Module, norm: torch.nn.Module | None = None) -> "Int8Linear":
@@ -67,7 +72,7 @@ class Int8Experts(torch.nn.Module):
         codes, scale = quantize_weight(weight)
         self.register_buffer("codes", codes)
         self.register_buffer("scale", scale)
-        self.register_buffer("bias", None if bias is None else bias.detach().float())
+        self.register_buffer("bias", _snapshot(bias))
 
     def forward(self, x: torch.Tensor, offsets: torch.Tensor) -> torch.Tensor:
         return autograd.context(x.device).quant_int8_gemm_grouped(x, offsets, self.codes, self.scale, self.bias)

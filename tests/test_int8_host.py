@@ -76,3 +76,34 @@ def test_a_second_derivative_of_layer_norm_is_refused(monkeypatch):
     x.grad = None
     autograd.layer_norm(x, w, b).square().sum().backward()          # one derivative as ever
     assert torch.allclose(x.grad, torch.autograd.grad(torch.nn.functional.layer_norm(x, (8,), w, b).square().sum(), x)[0], atol=1e-4)
+
+
+@pytest.fixture
+def int8_modules(monkeypatch):
+    """The modules of int8.py with the quantizer played by its formula, codes in rows of a multiple of 16 bytes."""
+    from paper_2112_10769_b200 import int8
+
+    class Formulas:
+        @staticmethod
+        def quant_int8_rows(w):
+            codes = torch.zeros(w.shape[0], -(-w.shape[1] // 16) * 16, dtype=torch.int8)[:, :w.shape[1]]
+            scale = w.abs().amax(1) / 127
+            codes.copy_((w / scale[:, None]).round())
+            return codes, scale
+
+    monkeypatch.setattr(int8.autograd, "context", lambda device: Formulas)
+    return int8
+
+
+def test_the_modules_answer_as_of_their_making(int8_modules):
+    # codes and scales are a snapshot of the weight, so the other parameters have to be one too
+    lin, norm = torch.nn.Linear(40, 24), torch.nn.LayerNorm(40)
+    bias = torch.zeros(2, 24)
+    layers = int8_modules.Int8Linear.of(lin, norm=norm), int8_modules.Int8Experts(torch.randn(2, 24, 40), bias)
+    before = [{k: v.clone() for k, v in layer.state_dict().items()} for layer in layers]
+    with torch.no_grad():
+        for p in (*lin.parameters(), *norm.parameters(), bias):
+            p.add_(1)
+    for layer, state in zip(layers, before):
+        for k, v in layer.state_dict().items():
+            assert torch.equal(v, state[k]), k
