@@ -176,7 +176,29 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     return LayerNormFunction.apply(x, weight, bias, eps)
 
 
-class LayerNorm(torch.nn.Module):
+class KeepsFloat32(torch.nn.Module):
+    """A module whose parameters and buffers the kernels read as float32: casting it (``model.bfloat16()``) or loading
+    tensors of another type into it leaves them so, moving it moves them."""
+
+    def _kept(self, t: torch.Tensor) -> torch.Tensor:
+        return t.float() if t.is_floating_point() else t
+
+    def _apply(self, fn, recurse=True):
+        def move(t):
+            moved = fn(t)
+            return self._kept(moved if moved.dtype == t.dtype else t.to(moved.device))
+        return super()._apply(move, recurse)
+
+    def _load_from_state_dict(self, state_dict, prefix, *args, **kwargs):
+        super()._load_from_state_dict(state_dict, prefix, *args, **kwargs)
+        with torch.no_grad():                              # (what was assigned rather than copied)
+            for own in (self._parameters, self._buffers):
+                for name, t in own.items():
+                    if t is not None and self._kept(t) is not t:
+                        own[name] = torch.nn.Parameter(self._kept(t), t.requires_grad) if own is self._parameters else self._kept(t)
+
+
+class LayerNorm(KeepsFloat32):
     """``torch.nn.LayerNorm`` over the last dimension, with float32 parameters whatever the type of its input."""
 
     def __init__(self, features: int, eps: float = 1e-5, bias: bool = True, device=None):

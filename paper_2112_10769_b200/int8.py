@@ -31,7 +31,18 @@ def _snapshot(t: torch.Tensor | None):
     return None if t is None else t.detach().to(torch.float32, copy=True).contiguous()
 
 
-class Int8Linear(torch.nn.Module):
+class _Int8Module(autograd.KeepsFloat32):
+    """Codes keep rows that start at multiples of 16 bytes: a move or a copy packs them."""
+
+    def _kept(self, t: torch.Tensor) -> torch.Tensor:
+        t = super()._kept(t)
+        if t.dtype != torch.int8 or (t.stride(-1) == 1 and all(s % 16 == 0 for s in t.stride()[:-1]) and t.data_ptr() % 16 == 0):
+            return t
+        rows = torch.empty((*t.shape[:-1], -(-t.shape[-1] // 16) * 16), dtype=torch.int8, device=t.device)[..., :t.shape[-1]]
+        return rows.copy_(t)
+
+
+class Int8Linear(_Int8Module):
     """``torch.nn.Linear`` in 8 bits.  ``norm``: a layer norm module (``autograd.LayerNorm`` or
     ``torch.nn.LayerNorm`` over the last dimension) that is applied to the tokens first, in the same call."""
 
@@ -63,7 +74,7 @@ class Int8Linear(torch.nn.Module):
         return z if x.dim() == 2 else z.reshape(*x.shape[:-1], z.shape[-1])
 
 
-class Int8Experts(torch.nn.Module):
+class Int8Experts(_Int8Module):
     """One weight per expert, ``[E, N, K]``.  ``forward(x, offsets)``: rows ``offsets[e] .. offsets[e + 1] - 1`` of x
     belong to expert e (``offsets``: int32 on the device, E + 1 numbers)."""
 

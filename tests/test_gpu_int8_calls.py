@@ -146,3 +146,18 @@ def test_no_memory_for_a_workspace_is_torchs_error(ctx):
         torch.cuda.set_per_process_memory_fraction(1.0)
     ctx.quant_int8_gemm(x, w, sw, out=out)
     assert torch.equal(out, want) and ctx.status() == 0
+
+
+def test_modules_answer_the_same_after_a_move_and_a_cast():
+    import copy
+    from paper_2112_10769_b200.int8 import Int8Experts, Int8Linear
+    K = 200                                               # rows of codes with eight bytes between them
+    x, offsets = torch.randn(9, K, device="cuda"), torch.tensor([0, 4, 9], dtype=torch.int32, device="cuda")
+    dense = Int8Linear(torch.randn(72, K, device="cuda"), torch.randn(72, device="cuda"), torch.nn.LayerNorm(K, device="cuda"))
+    experts = Int8Experts(torch.randn(2, 72, K, device="cuda"))
+    norm = autograd.LayerNorm(K, device="cuda")
+    want = dense(x), experts(x, offsets), norm(x)
+    for moved in (lambda m: m.cpu().cuda(), lambda m: m.bfloat16(), lambda m: m.half(), copy.deepcopy):
+        got = moved(dense)(x), moved(experts)(x, offsets), moved(norm)(x)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert norm(x.bfloat16()).dtype == torch.bfloat16

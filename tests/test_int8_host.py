@@ -107,3 +107,36 @@ def test_the_modules_answer_as_of_their_making(int8_modules):
     for layer, state in zip(layers, before):
         for k, v in layer.state_dict().items():
             assert torch.equal(v, state[k]), k
+
+
+def rows_fit_the_products(codes):
+    return codes.stride(-1) == 1 and all(s % 16 == 0 for s in codes.stride()[:-1]) and codes.data_ptr() % 16 == 0
+
+
+@pytest.mark.parametrize("how", ["bfloat16", "half", "double", "clone", "pickle", "assign"])
+def test_the_modules_can_be_moved_and_cast(int8_modules, how):
+    # the calls read float32 scales and parameters, and codes whose rows start at multiples of 16 bytes: a cast, a move
+    # (which packs rows of 40 codes tightly, like clone) and loaded tensors have to leave both
+    import io
+    from paper_2112_10769_b200 import autograd
+    layers = (int8_modules.Int8Linear.of(torch.nn.Linear(40, 24), norm=torch.nn.LayerNorm(40)),
+              int8_modules.Int8Experts(torch.randn(2, 24, 40), torch.randn(2, 24)), autograd.LayerNorm(40))
+    for layer in layers:
+        before = {k: v.clone() for k, v in layer.state_dict().items()}
+        if how == "clone":
+            layer._apply(lambda t: t.clone(memory_format=torch.contiguous_format))
+        elif how == "pickle":
+            file = io.BytesIO()
+            torch.save(layer.state_dict(), file)
+            file.seek(0)
+            layer.load_state_dict(torch.load(file))
+        elif how == "assign":
+            layer.load_state_dict({k: v.contiguous() if v.dtype == torch.int8 else v.double() for k, v in before.items()}, assign=True)
+        else:
+            getattr(layer, how)()
+        after = layer.state_dict()
+        assert list(after) == list(before)
+        for k, v in after.items():
+            assert v.dtype == before[k].dtype and v.shape == before[k].shape and torch.equal(v, before[k]), k
+            assert v.dtype != torch.int8 or rows_fit_the_products(v), k
+        assert all(p.requires_grad for p in layer.parameters())
