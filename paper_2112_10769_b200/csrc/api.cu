@@ -542,7 +542,8 @@ int int8_product(luq_ctx* ctx, luq_int8_args a, int z_dtype, bool grouped, const
   const int rc = int8_args_ok(a, z_dtype, grouped);
   if (rc) return rc;
   a.out_bf16 = z_dtype == LUQ_BF16;
-  if (!grouped) { a.offsets = nullptr; a.groups = 1; a.w_stride = a.ld_w * a.N; }
+  if (!grouped) { a.offsets = nullptr; a.groups = 1; }
+  if (a.groups == 1) a.w_stride = a.ld_w * a.N;         // (there is nothing between one group and the next)
   if (from_codes) {
     if (!codes_ok(a.x_codes, a.M, a.K, a.ld_x) || !floats_ok(a.sx, a.M > 0)) return LUQ_ERR_ARG;
   } else {

@@ -161,3 +161,17 @@ def test_modules_answer_the_same_after_a_move_and_a_cast():
         got = moved(dense)(x), moved(experts)(x, offsets), moved(norm)(x)
         assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert norm(x.bfloat16()).dtype == torch.bfloat16
+
+
+def test_the_stride_between_groups_means_nothing_for_one_group(ctx):
+    M, N, K = 20, 48, 64
+    x, w = (torch.randint(-127, 128, (n, K), device="cuda", dtype=torch.int8) for n in (M, N))
+    sx, sw = torch.rand(M, device="cuda"), torch.rand(N, device="cuda")
+    offsets = torch.tensor([0, M], dtype=torch.int32, device="cuda")
+    want = ctx.gemm_int8(x, sx, w, sw)
+    for stride in (N * K, 0, -16, 16):
+        z = torch.zeros(M, N, device="cuda")
+        rc = binding.load().luq_gemm_int8_grouped(ctx.handle, x.data_ptr(), K, sx.data_ptr(), offsets.data_ptr(), 1, w.data_ptr(), K, stride,
+                                                  sw.data_ptr(), None, z.data_ptr(), 0, N, M, N, K, torch.cuda.current_stream().cuda_stream)
+        assert rc == 0 and torch.equal(z, want), stride
+    assert ctx.status() == 0
