@@ -572,17 +572,17 @@ __device__ __forceinline__ void store_row(T* row, bool exists, bool vec, int tid
 }
 
 // threads of a row kernel's block (at most), and blocks that share an SM, by the registers they need without spilling
-template <int EPT, bool NARROW>
-constexpr int kRowThreads = EPT == 32 && !NARROW ? 512 : 256;
-template <int MODE, int EPT, int LOAD, int FIT, bool NARROW>
-constexpr int kRowBlocks = EPT == 32 && !NARROW ? 1
+template <int EPT>
+constexpr int kRowThreads = EPT == 32 ? 512 : 256;
+template <int MODE, int EPT, int LOAD, int FIT>
+constexpr int kRowBlocks = EPT == 32 ? 1
                            : MODE == kInt8 || (EPT == 16 && (FIT != kRagged || (MODE == kNormInt8 && LOAD == kRing))) ? 3 : 2;
 
 // What bounds it: many rows, HBM (16384 x 4096 bf16 norm 46 us, 5.8 TB/s; 8192 x 1024 fp32 13.1 us, 5.1 TB/s); rows
 // that do not fill their threads or are narrow, the instructions per element; few rows, the latency of one row (1.9 us).
 // FIT, norm of 16384 x 4096 bf16: 46 us with kFull, 58 with kWhole; of 41582 x 704 bf16: 31 with kWhole, 45 with kRagged.
 template <typename T, int MODE, int EPT, int LOAD, int FIT, bool NARROW>
-__global__ void __launch_bounds__((kRowThreads<EPT, NARROW>), (kRowBlocks<MODE, EPT, LOAD, FIT, NARROW>))
+__global__ void __launch_bounds__((kRowThreads<EPT>), (kRowBlocks<MODE, EPT, LOAD, FIT>))
 row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
   constexpr int V = Piece<T>::V, VPT = EPT / V;
   // one box per reduction of a row; without the norm a row has one reduction only and uses two in turn
@@ -590,7 +590,7 @@ row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
   __shared__ float sum2_box[32];
   __shared__ unsigned int max_box[2][16];
   constexpr bool MOVES = FIT == kRagged && (MODE == kNorm || LOAD == kBounce);
-  __shared__ uint4 move[MOVES ? kRowThreads<EPT, NARROW> / 32 : 1][MOVES ? 32 * kBouncePieces<T> : 1];
+  __shared__ uint4 move[MOVES ? kRowThreads<EPT> / 32 : 1][MOVES ? 32 * kBouncePieces<T> : 1];
   extern __shared__ __align__(128) uint8_t ring_smem[];
   const Group<NARROW> g(threads_per_row);
   const int groups = blockDim.x / g.G, slot = g.index * g.warps, tid = g.tid, G = g.G, C = p.cols;
@@ -1007,13 +1007,14 @@ cudaError_t launch_row(luq_ctx* ctx, const RowParams& p, bool vec, cudaStream_t 
   int groups = (G > 256 ? 512 : 256) / G;
   while (groups > 1 && G * groups > 32 && p.rows < static_cast<long long>(groups) * ctx->sm_count) groups >>= 1;
   const int fit = LOAD == kBounce || !vec || (MODE != kInt8 && !(p.gamma && p.beta)) ? kRagged : fit_of<T>(p.cols, G * EPT);
-  int per_sm = fit == kRagged ? kRowBlocks<MODE, EPT, LOAD, kRagged, NARROW> : kRowBlocks<MODE, EPT, LOAD, kWhole, NARROW>;
-  if (kRowThreads<EPT, NARROW> == 512 && G <= 256) per_sm = 2;
+  int per_sm = fit == kRagged ? kRowBlocks<MODE, EPT, LOAD, kRagged> : kRowBlocks<MODE, EPT, LOAD, kWhole>;
+  if (kRowThreads<EPT> == 512 && G <= 256) per_sm = 2;
   const int row_bytes = Rows<T, 1, EPT, LOAD, kRagged, NARROW>::ring_row_bytes(p.cols);
   const int depth = LOAD == kRing ? ring_depth_for(groups, row_bytes, per_sm > 1 ? kRingBytes : kRingBytesAlone) : 0;
   const size_t smem = LOAD == kRing ? static_cast<size_t>(Rows<T, 1, EPT, LOAD, kRagged, NARROW>::ring_bytes(groups, depth, p.cols)) : 0;
   auto kernel = row_kernel<T, MODE, EPT, LOAD, kRagged, NARROW>;
-  if constexpr (LOAD != kBounce) {
+  // (narrow rows of 16 elements a thread take the ring where they are unaligned only)
+  if constexpr (LOAD == kDirect || (LOAD == kRing && !(NARROW && EPT == 16))) {
     if (fit == kWhole) kernel = row_kernel<T, MODE, EPT, LOAD, kWhole, NARROW>;
     if (fit == kFull) kernel = row_kernel<T, MODE, EPT, LOAD, kFull, NARROW>;
   }
@@ -1031,16 +1032,17 @@ cudaError_t launch_row(luq_ctx* ctx, const RowParams& p, bool vec, cudaStream_t 
 template <typename T, int MODE, int EPT, bool NARROW>
 cudaError_t launch_row_from(luq_ctx* ctx, const RowParams& p, bool vec_x, bool vec, bool ring, cudaStream_t st) {
   if (ring || (!NARROW && !vec_x)) return launch_row<T, MODE, EPT, kRing, NARROW>(ctx, p, vec, st);
-  if constexpr (NARROW)
+  if constexpr (NARROW && EPT == 16)                     // (with 24 all unaligned ones take the ring)
     if (!vec_x) return launch_row<T, MODE, EPT, kBounce, NARROW>(ctx, p, vec, st);
   return launch_row<T, MODE, EPT, kDirect, NARROW>(ctx, p, vec, st);
 }
 template <typename T, int MODE, int EPT>
 cudaError_t launch_row_load(luq_ctx* ctx, const RowParams& p, bool vec_x, bool vec, bool many, cudaStream_t st) {
-  if (p.cols > 32 * EPT) return launch_row_from<T, MODE, EPT, false>(ctx, p, vec_x, vec, many, st);
+  if constexpr (EPT == 32) return launch_row_from<T, MODE, EPT, false>(ctx, p, vec_x, vec, many, st);   // above 1024 columns only
+  else if (p.cols > 32 * EPT) return launch_row_from<T, MODE, EPT, false>(ctx, p, vec_x, vec, many, st);
   // rows of up to a warp: the ring's copies are small, and pay for rows that fill it and are unaligned only (20000 x
   // 301 fp32 44 -> 24 us, norm backward 78 -> 38; aligned, 20000 x 320 bf16 backward: 17 us, 23 from the ring)
-  return launch_row_from<T, MODE, EPT, true>(ctx, p, vec_x, vec, (many && p.cols > 512) || (!vec_x && p.cols > 16 * EPT), st);
+  else return launch_row_from<T, MODE, EPT, true>(ctx, p, vec_x, vec, (many && p.cols > 512) || (!vec_x && p.cols > 16 * EPT), st);
 }
 
 // Elements per thread by the width alone (what a row becomes must not depend on where it lies).  What counts is the
@@ -1098,7 +1100,7 @@ cudaError_t launch_norm_bwd_rows(int device, const NormBwdParams& p, bool vec, i
   const int fit = LOAD == kBounce || !vec || !p.gamma ? kRagged : fit_of<T>(p.cols, EPT == 16 ? G * EPT : 0);
   constexpr int least = LOAD == kDirect && !NARROW ? kWhole : kRagged;     // (such rows take the ring)
   auto kernel = norm_bwd_kernel<T, EPT, LOAD, least, NARROW>;
-  if constexpr (LOAD != kBounce) {
+  if constexpr (LOAD == kDirect || (LOAD == kRing && !NARROW)) {           // (narrow rows take the ring where they are unaligned only)
     if (fit == kWhole) kernel = norm_bwd_kernel<T, EPT, LOAD, kWhole, NARROW>;
     if constexpr (EPT == 16)
       if (fit == kFull) kernel = norm_bwd_kernel<T, EPT, LOAD, kFull, NARROW>;
