@@ -106,6 +106,9 @@ extern "C" {
                               return it too.  Set it on the quantizing and on the multiplying context alike.
                               0 (default): one plane per sample.  The paper states SMP as repeated products;
                               it has no counterpart of this shortcut. */
+#define LUQ_OPT_CHECK_SLACK 10 /* checking build only (LUQ_ERR_UNSUPPORTED in the normal one): the checks of layer norm and the
+                              8-bit kernels take rows as n elements (0..64) shorter than they are, so that accesses
+                              to the last n, which are sound, are reported and skipped: a test of the checks.  0 (default) */
 #define LUQ_OPT_LEVELS 4   /* kmax of the gradient quantizers, 1..6 (default luq_kmax() = 4): levels
                               alpha * 2^0 .. alpha * 2^kmax with alpha = max / 2^kmax, codes 0..kmax+1.  The
                               other grids of the paper from the same kernels: kmax = 2 is the FP2 grid of
@@ -463,7 +466,7 @@ int luq_quant_int8_gemm_grouped(luq_ctx* ctx, const void* d_x, int dtype, int64_
                                 void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream);
 
 /* 1 if this library was compiled with -DLUQ_DEBUG: every shared-memory, tensor-memory and global
- * address that the converters, epilogues and streaming loops form is checked against its region
+ * address that the converters, epilogues, row kernels and streaming loops form is checked against its region
  * before use; a violation raises LUQ_STATUS_BOUNDS and skips the access.  (The pool this library
  * was developed on offers no compute-sanitizer; this build stands in for it.)  0 otherwise. */
 int luq_debug_build(void);

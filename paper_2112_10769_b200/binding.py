@@ -26,6 +26,7 @@ MAX_GROUPS = 1024
 OPT_MMA_KIND, OPT_SPLITS, OPT_PAIRS, OPT_LEVELS, OPT_UNSIGNED_ACTIVATIONS, OPT_OUTPUT_BF16 = 1, 2, 3, 4, 5, 6
 OPT_GRADIENT_INT4 = 7
 OPT_SM_LIMIT = 8
+OPT_CHECK_SLACK = 10
 OPT_SUM_SAMPLES = 9
 SCHEME_FP4, SCHEME_FP4_SR, SCHEME_FP4_SU, SCHEME_LUQ, SCHEME_INT4_SR = 0, 1, 2, 3, 4
 ERR_ARG, ERR_CUDA, ERR_UNSUPPORTED, ERR_WORKSPACE = -1, -2, -3, -4

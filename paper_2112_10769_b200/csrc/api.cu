@@ -136,6 +136,12 @@ int luq_set_option(luq_ctx* ctx, int option, int value) {
       if (value < 0 || value > 2) return LUQ_ERR_ARG;
       ctx->use_pairs = value;
       return LUQ_OK;
+#ifdef LUQ_DEBUG
+    case LUQ_OPT_CHECK_SLACK:
+      if (value < 0 || value > 64) return LUQ_ERR_ARG;
+      ctx->check_slack = value;
+      return LUQ_OK;
+#endif
     default:
       return LUQ_ERR_UNSUPPORTED;
   }

@@ -29,6 +29,7 @@ struct luq_ctx {
   int kmax;                 // LUQ levels alpha * 2^0 .. alpha * 2^kmax (1..6, default LUQ_KMAX)
   int64_t launches;
   void* encode_tiled;       // cuTensorMapEncodeTiled, resolved at create
+  int check_slack;          // checking build: LUQ_OPT_CHECK_SLACK
   luq_alloc_fn alloc;       // luq_set_allocator; null: d_workspace
   luq_release_fn release;
   void* alloc_user;
@@ -217,12 +218,12 @@ __device__ __forceinline__ bool smem_in(const void* p, const void* base, int lo,
   (void)off; (void)lo; (void)hi; (void)bytes; (void)status;
   return LUQ_IN_BOUNDS(off >= lo && off + bytes <= hi, status);
 }
-// do the 32 accumulator columns read at `taddr` lie inside the `cols` columns allocated at `tmem_base`?
-__device__ __forceinline__ bool tmem_in(unsigned int taddr, unsigned int tmem_base, int cols, unsigned int* status) {
+// do the 32 (`width`) accumulator columns read at `taddr` lie inside the `cols` columns allocated at `tmem_base`?
+__device__ __forceinline__ bool tmem_in(unsigned int taddr, unsigned int tmem_base, int cols, unsigned int* status, int width = 32) {
   const int col = static_cast<int>(taddr & 0xFFFFu) - static_cast<int>(tmem_base & 0xFFFFu);
   const int lane = static_cast<int>(taddr >> 16) - static_cast<int>(tmem_base >> 16);
-  (void)col; (void)lane; (void)cols; (void)status;
-  return LUQ_IN_BOUNDS(col >= 0 && col + 32 <= cols && lane >= 0 && lane + 32 <= 128, status);
+  (void)col; (void)lane; (void)cols; (void)status; (void)width;
+  return LUQ_IN_BOUNDS(col >= 0 && col + width <= cols && lane >= 0 && lane + 32 <= 128, status);
 }
 
 // waits until the preceding kernel of the stream has completed and its memory is visible

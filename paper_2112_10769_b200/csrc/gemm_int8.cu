@@ -59,7 +59,15 @@ struct Int8Params {
   int early;                // everything but the tokens' codes and scales was there before the preceding kernel
   int z_tma;                // the output can be addressed by TMA
   long long tma_cols;       // a store copy writes whole 16-byte pieces: boxes up to this column end on one
+#ifdef LUQ_DEBUG
+  int slack;                // LUQ_OPT_CHECK_SLACK
+#endif
 };
+#ifdef LUQ_DEBUG
+#define LUQ_CHECKED_N(p) ((p).N - (p).slack)
+#else
+#define LUQ_CHECKED_N(p) ((p).N)
+#endif
 
 // One tile: kCh channels (twice that on a CTA pair) by up to BT tokens.  The epilogue's warps come in groups of
 // four (one per quarter of the lanes, 32 channels each); a group takes `span` tokens of the tile.
@@ -207,6 +215,11 @@ __device__ __forceinline__ void store_z(void* z, long long at, float v, bool bf1
   if (bf16) static_cast<__nv_bfloat16*>(z)[at] = __float2bfloat16_rn(v);
   else static_cast<float*>(z)[at] = v;
 }
+// is [row, ch] an output?  (always true outside the checking build)
+__device__ __forceinline__ bool z_in(const Int8Params& p, long long row, int ch) {
+  (void)p; (void)row; (void)ch;
+  return LUQ_IN_BOUNDS(row >= 0 && row < p.M && ch >= 0 && ch < LUQ_CHECKED_N(p), p.status);
+}
 // two products and two sums of neighbouring tokens: z = (acc * sw) * s + bias
 __device__ __forceinline__ float2 scale2(uint32_t a0, uint32_t a1, float2 sw, float2 s, float2 bias) {
   const float2 acc = make_float2(static_cast<float>(static_cast<int>(a0)), static_cast<float>(static_cast<int>(a1)));
@@ -220,8 +233,8 @@ __device__ __forceinline__ float2 scale2(uint32_t a0, uint32_t a1, float2 sw, fl
 // One fence serves all boxes a warp has (two of bf16, one of fp32).
 template <typename C, bool BF16>
 __device__ __forceinline__ void write_tile(const Int8Params& p, const void* tm_z, const Unit& v, float sw, float bias,
-                                           uint32_t taddr, int warp_e, int lane, uint32_t staging, uint8_t* gen,
-                                           const float* scales) {
+                                           uint32_t taddr, uint32_t tmem_base, int warp_e, int lane, uint32_t staging,
+                                           uint8_t* gen, const float* scales) {
   constexpr int CH = C::chunk, kSteps = C::span / CH, kPair = kSteps < 2 ? kSteps : 2;
   constexpr int kBoxes = BF16 ? 2 : 1, kBoxBytes = kWarpStaging / kBoxes;
   const int quarter = (warp_e + kFirstEpiWarp) & 3;
@@ -238,7 +251,9 @@ __device__ __forceinline__ void write_tile(const Int8Params& p, const void* tm_z
     fence_proxy_async();
     __syncwarp();
     if (lane == 0) {
-      for (int i = 0; i < staged; ++i) tma_store_2d(tm_z, staging + slot + i * kBoxBytes, ch_first, v.row0 + first_staged + 32 * i);
+      for (int i = 0; i < staged; ++i)
+        if (z_in(p, v.row0 + first_staged + 32 * i + 31, min(ch_first + 31, static_cast<int>(p.N) - 1)))
+          tma_store_2d(tm_z, staging + slot + i * kBoxBytes, ch_first, v.row0 + first_staged + 32 * i);
       bulk_commit();
     }
     staged = 0;
@@ -248,7 +263,8 @@ __device__ __forceinline__ void write_tile(const Int8Params& p, const void* tm_z
     uint32_t r[kPair][CH];
 #pragma unroll
     for (int i = 0; i < kPair; ++i)
-      if (c_first + (pair + i) * CH < v.rows) load_chunk<CH>(taddr + c_first + (pair + i) * CH, r[i]);
+      if (c_first + (pair + i) * CH < v.rows &&
+          tmem_in(taddr + c_first + (pair + i) * CH, tmem_base, C::tmem_cols, p.status, CH)) load_chunk<CH>(taddr + c_first + (pair + i) * CH, r[i]);
     tmem_ld_wait();
 #pragma unroll
     for (int step = 0; step < kPair; ++step) {
@@ -297,8 +313,8 @@ __device__ __forceinline__ void write_tile(const Int8Params& p, const void* tm_z
         for (int i = 0; i < CH; i += 2) {
           if (i < left) {
             const float2 z = scale2(r[step][i], r[step][i + 1], sw2, make_float2(scales[c0 + i], scales[c0 + i + 1]), bias2);
-            store_z(p.z, z0 + i * p.ld_z, z.x, BF16);
-            if (i + 1 < left) store_z(p.z, z0 + (i + 1) * p.ld_z, z.y, BF16);
+            if (z_in(p, v.row0 + c0 + i, ch)) store_z(p.z, z0 + i * p.ld_z, z.x, BF16);
+            if (i + 1 < left && z_in(p, v.row0 + c0 + i + 1, ch)) store_z(p.z, z0 + (i + 1) * p.ld_z, z.y, BF16);
           }
         }
       }
@@ -310,7 +326,7 @@ __device__ __forceinline__ void write_tile(const Int8Params& p, const void* tm_z
 // Adds a channel's partial sums of Q CTAs (of fewer, if the cluster has fewer) for every stride-th token and
 // writes the results; sixteen loads from the other CTAs are on their way at once.
 template <int Q>
-__device__ __forceinline__ void join(const Int8Params& p, const Unit& v, uint32_t column, int first_token, int stride, int ch,
+__device__ __forceinline__ void join(const Int8Params& p, const Unit& v, uint32_t column, uint32_t end, int first_token, int stride, int ch,
                                      float sw, float bias, const float* scales, bool bf16) {
   constexpr int U = 16 / Q;
   const int cluster = static_cast<int>(cluster_nctarank());
@@ -320,7 +336,8 @@ __device__ __forceinline__ void join(const Int8Params& p, const Unit& v, uint32_
     for (int u = 0; u < U; ++u) {
 #pragma unroll
       for (int q = 0; q < Q; ++q)
-        part[u][q] = q < cluster && t0 + u * stride < v.rows ? ld_shared_cluster(mapa_shared(column + (t0 + u * stride) * kCh * 4, q)) : 0;
+        part[u][q] = q < cluster && t0 + u * stride < v.rows &&
+                             LUQ_IN_BOUNDS(t0 >= 0 && column + (t0 + u * stride) * kCh * 4 + 4 <= end, p.status) ? ld_shared_cluster(mapa_shared(column + (t0 + u * stride) * kCh * 4, q)) : 0;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -328,7 +345,7 @@ __device__ __forceinline__ void join(const Int8Params& p, const Unit& v, uint32_
       int sum = 0;
 #pragma unroll
       for (int q = 0; q < Q; ++q) sum += part[u][q];
-      if (t < v.rows)
+      if (t < v.rows && z_in(p, v.row0 + t, ch))
         store_z(p.z, (static_cast<long long>(v.row0) + t) * p.ld_z + ch, fmaf(static_cast<float>(sum) * sw, scales[t], bias), bf16);
     }
   }
@@ -500,6 +517,7 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     const int ch = v.ch0 + (warp & 3) * 32 + lane;
     const bool ch_in = ch < p.N;
     const long long wi = static_cast<long long>(v.group) * p.N + ch;
+    (void)LUQ_IN_BOUNDS(v.group >= 0 && v.group < p.groups && v.row0 >= 0 && v.row0 + v.rows <= p.M && v.rows <= BT, p.status);
     sw_ahead = ch_in ? *(p.sw + wi) : 0.0f;
     bias_ahead = ch_in && p.bias ? *(p.bias + wi) : 0.0f;
     if (!waited) { pdl_wait(); waited = true; }
@@ -543,7 +561,7 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         ok = ok && mbar_wait(acc_full(buf), (it >> 1) & 1u, abort_flag);
         if (ok) {
           tc_fence_after();
-          write_tile<C, BF16>(p, &tm_z, v, sw, bias, lane_base + buf * BT, warp_e, lane, base + C::staging, gen, scales_of(it));
+          write_tile<C, BF16>(p, &tm_z, v, sw, bias, lane_base + buf * BT, tmem_base, warp_e, lane, base + C::staging, gen, scales_of(it));
         }
         tc_fence_before();
         __syncwarp();
@@ -574,6 +592,7 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         tc_fence_after();
         for (int c = (warp_e >> 2) * C::chunk; ok && c < v.rows; c += C::epi_warps / 4 * C::chunk) {
           uint32_t r[C::chunk];
+          if (!tmem_in(lane_base + buf * BT + c, tmem_base, C::tmem_cols, p.status, C::chunk)) continue;
           load_chunk<C::chunk>(lane_base + buf * BT + c, r);
           tmem_ld_wait();
 #pragma unroll
@@ -594,9 +613,9 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         const int stride = static_cast<int>(cluster) * (C::epi_warps / 4);
         const uint32_t column = smem_u32(partial + (warp & 3) * 32 + lane);
         if (ch < p.N) {                // every load below is used, and so has ended, before the meeting after it
-          if (cluster <= 2) join<2>(p, v, column, first_token, stride, ch, sw_ahead, bias_ahead, scales_of(it), BF16);
-          else if (cluster <= 4) join<4>(p, v, column, first_token, stride, ch, sw_ahead, bias_ahead, scales_of(it), BF16);
-          else join<8>(p, v, column, first_token, stride, ch, sw_ahead, bias_ahead, scales_of(it), BF16);
+          if (cluster <= 2) join<2>(p, v, column, base + C::staging, first_token, stride, ch, sw_ahead, bias_ahead, scales_of(it), BF16);
+          else if (cluster <= 4) join<4>(p, v, column, base + C::staging, first_token, stride, ch, sw_ahead, bias_ahead, scales_of(it), BF16);
+          else join<8>(p, v, column, base + C::staging, first_token, stride, ch, sw_ahead, bias_ahead, scales_of(it), BF16);
         }
         fence_proxy_async();           // the next tile's copies come after these reads
       }
@@ -716,6 +735,9 @@ int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, bool early, cudaS
   p.sx = a.sx; p.sw = a.sw; p.bias = a.bias; p.offsets = a.offsets; p.z = a.z; p.ld_z = a.ld_z; p.status = ctx->d_status;
   p.M = a.M; p.N = a.N; p.groups = a.groups; p.early = early;
   p.row0 = static_cast<int>(a.row0); p.all_rows = static_cast<int>(a.all_rows);
+#ifdef LUQ_DEBUG
+  p.slack = ctx->check_slack;
+#endif
   p.num_kb = static_cast<int>((a.K + kBk - 1) / kBk);
   const int64_t esize = a.out_bf16 ? 2 : 4;
   p.z_tma = (reinterpret_cast<uintptr_t>(a.z) & 15u) == 0 && (a.ld_z * esize) % 16 == 0;

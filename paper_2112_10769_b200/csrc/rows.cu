@@ -20,6 +20,18 @@ using namespace luqdev;
 
 constexpr int kNorm = 0, kNormInt8 = 1, kInt8 = 2;   // what a row kernel makes of a row
 
+// Checking build: where the checks take a row to end, and the shared memory of the launch.
+#ifdef LUQ_DEBUG
+#define LUQ_CHECKED_COLS(p) ((p).cols - (p).slack)
+__device__ __forceinline__ int dynamic_smem() {
+  int n;
+  asm volatile("mov.u32 %0, %%dynamic_smem_size;" : "=r"(n));
+  return n;
+}
+#else
+#define LUQ_CHECKED_COLS(p) ((p).cols)
+#endif
+
 struct RowParams {
   const void* x;
   long long rows, ld_x;
@@ -36,6 +48,9 @@ struct RowParams {
   float* scale;
   unsigned int* status;
   bool vec_params, vec_y;   // gamma and beta, and the rows of y, are 16-byte aligned
+#ifdef LUQ_DEBUG
+  int slack;                // LUQ_OPT_CHECK_SLACK
+#endif
 };
 
 __device__ __forceinline__ float load1(const float* p) { return *(p); }
@@ -112,6 +127,8 @@ __global__ void __launch_bounds__(512) row_loop_kernel(const RowParams p) {
   pdl_wait();
   pdl_trigger();
   const int C = p.cols;
+  // (every address below is a row's start and c < C)
+  auto in_row = [&](int c) { (void)c; return LUQ_IN_BOUNDS(c >= 0 && c < LUQ_CHECKED_COLS(p), p.status); };
   for (long long r = blockIdx.x; r < p.rows; r += gridDim.x) {
     const T* const x = static_cast<const T*>(p.x) + r * p.ld_x;
     float mean0 = 0.0f, shift = 0.0f, rstd = 1.0f;
@@ -138,7 +155,8 @@ __global__ void __launch_bounds__(512) row_loop_kernel(const RowParams p) {
     };
     if (MODE == kNorm) {
       T* const y = static_cast<T*>(p.y) + r * p.ld_y;
-      for (int c = threadIdx.x; c < C; c += blockDim.x) store1(y + c, value(c));
+      for (int c = threadIdx.x; c < C; c += blockDim.x)
+        if (in_row(c)) store1(y + c, value(c));
       if (threadIdx.x == 0) {
         if (p.mean) p.mean[r] = mean0 + shift;
         if (p.rstd) p.rstd[r] = rstd;
@@ -149,7 +167,8 @@ __global__ void __launch_bounds__(512) row_loop_kernel(const RowParams p) {
       top = block_max(top, reinterpret_cast<unsigned int*>(box));
       const float factor = row_factor(top);
       int8_t* const q = p.codes + r * p.ld_codes;
-      for (int c = threadIdx.x; c < C; c += blockDim.x) q[c] = factor == 0.0f ? 0 : static_cast<int8_t>(quantize1(value(c), factor));
+      for (int c = threadIdx.x; c < C; c += blockDim.x)
+        if (in_row(c)) q[c] = factor == 0.0f ? 0 : static_cast<int8_t>(quantize1(value(c), factor));
       if (threadIdx.x == 0) store_scale(top, p.scale + r, p.status);
     }
   }
@@ -216,11 +235,12 @@ __device__ __forceinline__ bool piece_exists(int c, int cols) {
 
 // V parameters, `other` where there are none, zero beyond the row's end; `vec`: 16-byte aligned
 template <int V, int FIT>
-__device__ __forceinline__ void load_params(const float* g, bool vec, int c, int cols, float other, float* v) {
+__device__ __forceinline__ void load_params(const float* g, bool vec, int c, int cols, float other, float* v, int limit, unsigned int* status) {
   if (FIT == kRagged && g == nullptr) {
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = other;
   } else if (piece_exists<FIT, V>(c, cols) && (FIT != kRagged || vec)) {
+    if (!LUQ_IN_BOUNDS(c >= 0 && c + V <= limit, status)) return;
 #pragma unroll
     for (int i = 0; i < V; i += 4) {
       const float4 f = *(reinterpret_cast<const float4*>(g + c + i));
@@ -228,7 +248,7 @@ __device__ __forceinline__ void load_params(const float* g, bool vec, int c, int
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = c + i < cols ? *(g + c + i) : 0.0f;
+    for (int i = 0; i < V; ++i) v[i] = c + i < cols && LUQ_IN_BOUNDS(c + i < limit, status) ? *(g + c + i) : 0.0f;
   }
 }
 
@@ -329,6 +349,9 @@ struct Rows {
   uint4 raw[TENSORS][LOAD == kDirect ? VPT : 1];
   T single[TENSORS][LOAD == kBounce ? EPT : 1];
   uint4* wbuf = nullptr;
+  // for the checks: where rows end
+  int limit;
+  unsigned int* status;
 
   static int ring_row_bytes(int cols) { return (cols * static_cast<int>(sizeof(T)) + 32 + 127) / 128 * 128; }
   // shared memory of a block's rings: [groups][depth] barriers, the abort word, then [groups][depth][TENSORS] rows
@@ -344,6 +367,7 @@ struct Rows {
     bars = smem_u32(smem) + group * depth * 8;
     abort_flag = reinterpret_cast<volatile uint32_t*>(smem + groups * depth * 8);
     held = smem + head + group * depth * TENSORS * row_bytes;
+    (void)LUQ_IN_BOUNDS(head + groups * depth * TENSORS * row_bytes <= dynamic_smem(), status);
     data = smem_u32(held);
     if (tid == 0)
       for (int s = 0; s < depth; ++s) mbar_init(bars + 8 * s, 1);
@@ -360,11 +384,16 @@ struct Rows {
       const uint32_t m = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base[t] + r * ld[t]) & 15u);
       lo[t] = r == 0 && m ? 16u : 0u;
       n[t] = (r + 1 < rows ? (m + bytes + 15u) & ~15u : (m + bytes) & ~15u) - lo[t];
+      // inside the tensor, and inside the stage
+      if (!LUQ_IN_BOUNDS((r > 0 || lo[t] >= m) && r >= 0 && r < rows && lo[t] + n[t] <= static_cast<uint32_t>(row_bytes) && s < depth &&
+                         r * ld[t] * static_cast<long long>(sizeof(T)) - m + lo[t] + n[t] <=
+                             ((rows - 1) * ld[t] + limit) * static_cast<long long>(sizeof(T)), status)) n[t] = 0u;
       total += n[t];
     }
     mbar_arrive_expect_tx(bars + 8 * s, total);
 #pragma unroll
     for (int t = 0; t < TENSORS; ++t) {
+      if (!LUQ_IN_BOUNDS(n[t] != 0u, status)) continue;
       const uintptr_t from = reinterpret_cast<uintptr_t>(base[t] + r * ld[t]) & ~static_cast<uintptr_t>(15);
       bulk_load(data + (s * TENSORS + t) * row_bytes + lo[t], reinterpret_cast<const void*>(from + lo[t]), n[t], bars + 8 * s);
     }
@@ -373,6 +402,11 @@ struct Rows {
   // elements c .. c + V - 1 of tensor t's row in the present stage, m = the row's address & 15
   template <bool ALIGNED>
   __device__ __forceinline__ void ring_piece(int t, uint32_t m, int c, float* v) const {
+    if (!LUQ_IN_BOUNDS(c >= 0 && c < cols && c / V * 16 + (ALIGNED ? 16 : 32) <= row_bytes && stage < depth, status)) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = 0.0f;
+      return;
+    }
     const uint4* const q = reinterpret_cast<const uint4*>(held + (stage * TENSORS + t) * row_bytes) + c / V;
     const uint4 a = q[0];
     if (ALIGNED) { unpack(a, base[0], v); return; }
@@ -406,8 +440,11 @@ struct Rows {
         const T* const row = base[t] + r * ld[t];
         const int m = static_cast<int>(skew(t, r)) / static_cast<int>(sizeof(T)), tail = (m + cols) % V;
         T* const to = reinterpret_cast<T*>(held + (stage * TENSORS + t) * row_bytes) + m;
-        if (r == 0 && m && tid < V - m && tid < cols) to[tid] = row[tid];
-        if (r + 1 == rows && tid < tail && tid < cols) to[cols - 1 - tid] = row[cols - 1 - tid];
+        auto patch = [&](int c) {
+          if (LUQ_IN_BOUNDS(c >= 0 && c < limit && (m + c + 1) * static_cast<int>(sizeof(T)) <= row_bytes, status)) to[c] = row[c];
+        };
+        if (r == 0 && m && tid < V - m && tid < cols) patch(tid);
+        if (r + 1 == rows && tid < tail && tid < cols) patch(cols - 1 - tid);
       }
       fence_proxy_async();               // before the stage's next copy
     }
@@ -424,11 +461,11 @@ struct Rows {
           raw[t][j] = make_uint4(0u, 0u, 0u, 0u);
           if (r < rows) {
             if (piece_exists<FIT, V>(c, cols)) {
-              raw[t][j] = *(reinterpret_cast<const uint4*>(row + c));
+              if (LUQ_IN_BOUNDS(c >= 0 && c + V <= limit && r >= 0, status)) raw[t][j] = *(reinterpret_cast<const uint4*>(row + c));
             } else if (FIT == kRagged) {
               float v[V];
 #pragma unroll
-              for (int i = 0; i < V; ++i) v[i] = c + i < cols ? load1(row + c + i) : 0.0f;
+              for (int i = 0; i < V; ++i) v[i] = c + i < cols && LUQ_IN_BOUNDS(c + i < limit, status) ? load1(row + c + i) : 0.0f;
               raw[t][j] = pack(v, row);                // exact: the values are of type T
             }
           }
@@ -441,7 +478,7 @@ struct Rows {
 #pragma unroll
           for (int i = 0; i < V; ++i) {
             const int c = c0 + i * width + l;
-            single[t][j * V + i] = r < rows && c < cols ? row[c] : zero_of(row);
+            single[t][j * V + i] = r < rows && c < cols && LUQ_IN_BOUNDS(c >= 0 && c < limit && r >= 0, status) ? row[c] : zero_of(row);
           }
         }
       }
@@ -500,7 +537,8 @@ struct Rows {
           for (int j = 0; j < kBouncePieces<T>; ++j)
             if (j0 + j < VPT) {
 #pragma unroll
-              for (int i = 0; i < V; ++i) b[j * 32 * V + i * width + l] = single[t][(j0 + j) * V + i];
+              for (int i = 0; i < V; ++i)
+                if (LUQ_IN_BOUNDS((lane - l) * V + i * width + l < 32 * V, status)) b[j * 32 * V + i * width + l] = single[t][(j0 + j) * V + i];
             }
           __syncwarp();
 #pragma unroll
@@ -533,7 +571,8 @@ struct Rows {
 // writes a thread's elements of a row; `vec`: the row starts at a multiple of 16 bytes (else through the warp's
 // shared memory, as kBounce reads)
 template <typename T, int EPT, int FIT, bool NARROW>
-__device__ __forceinline__ void store_row(T* row, bool exists, bool vec, int tid, int G, int cols, uint4* wbuf, const float* v) {
+__device__ __forceinline__ void store_row(T* row, bool exists, bool vec, int tid, int G, int cols, uint4* wbuf, const float* v, int limit,
+                                          unsigned int* status) {
   constexpr int V = Piece<T>::V, VPT = EPT / V;
   if (FIT != kRagged || vec) {
     if (!exists) return;
@@ -541,11 +580,11 @@ __device__ __forceinline__ void store_row(T* row, bool exists, bool vec, int tid
     for (int j = 0; j < VPT; ++j) {
       const int c = (tid + j * G) * V;
       if (piece_exists<FIT, V>(c, cols)) {
-        *reinterpret_cast<uint4*>(row + c) = pack(v + j * V, row);
+        if (LUQ_IN_BOUNDS(c >= 0 && c + V <= limit, status)) *reinterpret_cast<uint4*>(row + c) = pack(v + j * V, row);
       } else if (FIT == kRagged) {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-          if (c + i < cols) store1(row + c + i, v[j * V + i]);
+          if (c + i < cols && LUQ_IN_BOUNDS(c + i < limit, status)) store1(row + c + i, v[j * V + i]);
       }
     }
   } else {
@@ -564,7 +603,8 @@ __device__ __forceinline__ void store_row(T* row, bool exists, bool vec, int tid
         const int c0 = (tid - l + (j0 + j) * G) * V + l;
 #pragma unroll
         for (int i = 0; i < V; ++i)
-          if (exists && c0 + i * width < cols) row[c0 + i * width] = b[j * 32 * V + i * width + l];
+          if (exists && c0 + i * width < cols && LUQ_IN_BOUNDS(c0 >= 0 && c0 + i * width < limit && (lane - l) * V + i * width + l < 32 * V, status))
+            row[c0 + i * width] = b[j * 32 * V + i * width + l];
       }
       __syncwarp();
     }
@@ -601,6 +641,8 @@ row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
   in.base[0] = static_cast<const T*>(p.x); in.ld[0] = p.ld_x; in.rows = p.rows; in.cols = C; in.tid = tid; in.G = G;
   in.step = static_cast<long long>(gridDim.x) * groups;
   in.wbuf = wbuf;
+  in.limit = LUQ_CHECKED_COLS(p);
+  in.status = p.status;
   if constexpr (LOAD == kRing) {
     in.init_ring(ring_smem, groups, g.index, ring_depth);
     __syncthreads();
@@ -615,8 +657,8 @@ row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
   if constexpr (MODE != kInt8) {
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-      load_params<V, FIT>(p.gamma, p.vec_params, (tid + j * G) * V, C, 1.0f, w + j * V);
-      load_params<V, FIT>(p.beta, p.vec_params, (tid + j * G) * V, C, 0.0f, b + j * V);
+      load_params<V, FIT>(p.gamma, p.vec_params, (tid + j * G) * V, C, 1.0f, w + j * V, LUQ_CHECKED_COLS(p), p.status);
+      load_params<V, FIT>(p.beta, p.vec_params, (tid + j * G) * V, C, 0.0f, b + j * V, LUQ_CHECKED_COLS(p), p.status);
     }
   }
   const float inv_c = 1.0f / C;
@@ -660,14 +702,16 @@ row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
 #pragma unroll
         for (int i = 0; i < V; ++i) v[j * V + i] = fmaf(fmaf(v[j * V + i], rstd, minus), w[j * V + i], b[j * V + i]);
         // (a full row piece by piece: its stores leave while the next piece is computed)
-        if (MODE == kNorm && FIT != kRagged && exists && piece_exists<FIT, V>(c, C)) *reinterpret_cast<uint4*>(static_cast<T*>(p.y) + r * p.ld_y + c) = pack(v + j * V, static_cast<const T*>(nullptr));
+        if (MODE == kNorm && FIT != kRagged && exists && piece_exists<FIT, V>(c, C) && LUQ_IN_BOUNDS(c + V <= LUQ_CHECKED_COLS(p) && r < p.rows, p.status))
+          *reinterpret_cast<uint4*>(static_cast<T*>(p.y) + r * p.ld_y + c) = pack(v + j * V, static_cast<const T*>(nullptr));
         if (MODE != kNorm && FIT == kRagged && c + V > C) {
 #pragma unroll
           for (int i = 0; i < V; ++i)
             if (c + i >= C) v[j * V + i] = 0.0f;
         }
       }
-      if (MODE == kNorm && FIT == kRagged) store_row<T, EPT, FIT, NARROW>(static_cast<T*>(p.y) + r * p.ld_y, exists, p.vec_y, tid, G, C, wbuf, v);
+      if (MODE == kNorm && FIT == kRagged) store_row<T, EPT, FIT, NARROW>(static_cast<T*>(p.y) + r * p.ld_y, exists, p.vec_y, tid, G, C, wbuf, v,
+                                                                                  LUQ_CHECKED_COLS(p), p.status);
       if (MODE == kNorm && tid == 0 && exists) {
         if (p.mean) p.mean[r] = mean0 + shift;
         if (p.rstd) p.rstd[r] = rstd;
@@ -696,12 +740,13 @@ row_kernel(const RowParams p, int threads_per_row, int ring_depth) {
                                     0x5410);
         if (!exists) continue;
         if (piece_exists<FIT, V>(c, C)) {
+          if (!LUQ_IN_BOUNDS(c >= 0 && c + V <= LUQ_CHECKED_COLS(p) && r < p.rows, p.status)) continue;
           if constexpr (V == 8) *reinterpret_cast<uint2*>(q + c) = make_uint2(word[0], word[1]);
           else *reinterpret_cast<uint32_t*>(q + c) = word[0];
         } else if (FIT == kRagged) {
 #pragma unroll
           for (int i = 0; i < V; ++i)
-            if (c + i < C) q[c + i] = static_cast<int8_t>(word[i / 4] >> (8 * (i & 3)));
+            if (c + i < C && LUQ_IN_BOUNDS(c + i < LUQ_CHECKED_COLS(p) && r < p.rows, p.status)) q[c + i] = static_cast<int8_t>(word[i / 4] >> (8 * (i & 3)));
         }
       }
       if (tid == 0 && exists) store_scale(top, p.scale + r, p.status);
@@ -727,6 +772,9 @@ struct NormBwdParams {
   long long rows_per_chunk;
   unsigned int* status;
   bool vec_gamma, vec_dx;
+#ifdef LUQ_DEBUG
+  int slack;
+#endif
 };
 
 // mean_c(g) and mean_c(g xhat) of every row
@@ -770,11 +818,12 @@ __global__ void __launch_bounds__(256) norm_bwd_columns_kernel(const NormBwdPara
     const float xhat = (load1(static_cast<const T*>(p.x) + r * p.ld_x + c) - mean) * rstd;
     dgamma = fmaf(dy, xhat, dgamma);
     dbeta += dy;
-    if (p.dx) {
+    if (p.dx && LUQ_IN_BOUNDS(c >= 0 && c < LUQ_CHECKED_COLS(p) && r < p.rows, p.status)) {
       const float2 m = p.row_means[r];
       store1(static_cast<T*>(p.dx) + r * p.ld_dx + c, rstd * (fmaf(-xhat, m.y, dy * w) - m.x));
     }
   }
+  if (!LUQ_IN_BOUNDS(chunk >= 0 && chunk < p.chunks, p.status)) return;
   p.partial[(2 * chunk) * p.cols + c] = dgamma;
   p.partial[(2 * chunk + 1) * p.cols + c] = dbeta;
 }
@@ -803,6 +852,8 @@ __global__ void __launch_bounds__(bwd_threads(NARROW)) norm_bwd_kernel(const Nor
   in.base[0] = static_cast<const T*>(p.x); in.ld[0] = p.ld_x;
   in.base[1] = static_cast<const T*>(p.dy); in.ld[1] = p.ld_dy;
   in.rows = p.rows; in.cols = C; in.tid = tid; in.G = G; in.wbuf = wbuf;
+  in.limit = LUQ_CHECKED_COLS(p);
+  in.status = p.status;
   in.step = static_cast<long long>(gridDim.x) * groups;
   if constexpr (LOAD == kRing) {
     in.init_ring(ring_smem, groups, group, ring_depth);
@@ -817,7 +868,7 @@ __global__ void __launch_bounds__(bwd_threads(NARROW)) norm_bwd_kernel(const Nor
   float dgamma[EPT], dbeta[EPT], w[TWICE ? 1 : EPT];
   if constexpr (!TWICE) {
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) load_params<V, FIT>(p.gamma, p.vec_gamma, (tid + j * G) * V, C, 1.0f, w + j * V);
+    for (int j = 0; j < VPT; ++j) load_params<V, FIT>(p.gamma, p.vec_gamma, (tid + j * G) * V, C, 1.0f, w + j * V, LUQ_CHECKED_COLS(p), p.status);
   }
 #pragma unroll
   for (int i = 0; i < EPT; ++i) dgamma[i] = dbeta[i] = 0.0f;
@@ -852,7 +903,7 @@ __global__ void __launch_bounds__(bwd_threads(NARROW)) norm_bwd_kernel(const Nor
         const float m1 = -t.x * inv_c * rstd, m2 = t.y * inv_c;
 #pragma unroll
         for (int i = 0; i < EPT; ++i) dy[i] = fmaf(fmaf(-x[i], m2, dy[i]), rstd, m1);
-        store_row<T, EPT, FIT, NARROW>(dx, exists, p.vec_dx, tid, G, C, wbuf, dy);
+        store_row<T, EPT, FIT, NARROW>(dx, exists, p.vec_dx, tid, G, C, wbuf, dy, LUQ_CHECKED_COLS(p), p.status);
       } else if constexpr (LOAD == kRing) {
         g.sync();                                      // everyone has read the stage
         in.release(r);
@@ -876,7 +927,7 @@ __global__ void __launch_bounds__(bwd_threads(NARROW)) norm_bwd_kernel(const Nor
         float x[V], dy[V], weight[V];
         piece(0, c, x);
         piece(1, c, dy);
-        load_params<V, FIT>(p.gamma, p.vec_gamma, c, C, 1.0f, weight);
+        load_params<V, FIT>(p.gamma, p.vec_gamma, c, C, 1.0f, weight, LUQ_CHECKED_COLS(p), p.status);
 #pragma unroll
         for (int i = 0; i < V; ++i) gather(x[i], dy[i], weight[i], dgamma[j * V + i], dbeta[j * V + i], i);
       }
@@ -889,10 +940,11 @@ __global__ void __launch_bounds__(bwd_threads(NARROW)) norm_bwd_kernel(const Nor
           float x[V], dy[V], weight[V];
           piece(0, c, x);
           piece(1, c, dy);
-          load_params<V, FIT>(p.gamma, p.vec_gamma, c, C, 1.0f, weight);
+          load_params<V, FIT>(p.gamma, p.vec_gamma, c, C, 1.0f, weight, LUQ_CHECKED_COLS(p), p.status);
 #pragma unroll
           for (int i = 0; i < V; ++i) dy[i] = fmaf(fmaf(-((x[i] - mean) * rstd), m2, dy[i] * weight[i]), rstd, m1);
-          store_row<T, V, FIT, NARROW>(dx + j * G * V, in.ok(), p.vec_dx, tid, G, C - j * G * V, wbuf, dy);
+          store_row<T, V, FIT, NARROW>(dx + j * G * V, in.ok(), p.vec_dx, tid, G, C - j * G * V, wbuf, dy,
+                                    LUQ_CHECKED_COLS(p) - j * G * V, p.status);
         }
       }
       g.sync();                                        // everyone has read the stage
@@ -926,7 +978,7 @@ __global__ void __launch_bounds__(bwd_threads(NARROW)) norm_bwd_kernel(const Nor
 #pragma unroll
     for (int i = 0; i < EPT; i += 4) {
       const int c = (tid + i / V * G) * V + i % V;
-      if (c < Cp) {
+      if (c < Cp && LUQ_IN_BOUNDS(c >= 0 && ((2 * mine + 1) * Cp + c + 4) * 4 <= dynamic_smem() && mine < turns, p.status)) {
         *reinterpret_cast<float4*>(to + c) = make_float4(dgamma[i], dgamma[i + 1], dgamma[i + 2], dgamma[i + 3]);
         *reinterpret_cast<float4*>(to + Cp + c) = make_float4(dbeta[i], dbeta[i + 1], dbeta[i + 2], dbeta[i + 3]);
       }
@@ -934,6 +986,7 @@ __global__ void __launch_bounds__(bwd_threads(NARROW)) norm_bwd_kernel(const Nor
   }
   __syncthreads();
   for (int c = threadIdx.x; c < C; c += blockDim.x) {
+    if (!LUQ_IN_BOUNDS(((2 * turns - 1) * Cp + c + 1) * 4 <= dynamic_smem() && c < LUQ_CHECKED_COLS(p) && blockIdx.x < p.chunks, p.status)) continue;
     float sg = sums[c], sb = sums[Cp + c];
     for (int k = 1; k < turns; ++k) {
       sg += sums[2 * k * Cp + c];
@@ -1197,6 +1250,9 @@ int luq_launch_layer_norm(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows
   RowParams p{};
   p.x = d_x; p.rows = rows; p.ld_x = ld_x; p.cols = cols; p.gamma = d_gamma; p.beta = d_beta; p.eps = eps;
   p.y = d_y; p.ld_y = ld_y; p.mean = d_mean; p.rstd = d_rstd; p.status = ctx->d_status;
+#ifdef LUQ_DEBUG
+  p.slack = ctx->check_slack;
+#endif
   return dtype == LUQ_BF16 ? launch_rows<__nv_bfloat16, kNorm>(ctx, p, st) : launch_rows<float, kNorm>(ctx, p, st);
 }
 
@@ -1206,6 +1262,9 @@ int luq_launch_int8_rows(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows,
   RowParams p{};
   p.x = d_x; p.rows = rows; p.ld_x = ld_x; p.cols = cols; p.gamma = d_gamma; p.beta = d_beta; p.eps = eps;
   p.codes = d_codes; p.ld_codes = ld_codes; p.scale = d_scale; p.status = ctx->d_status;
+#ifdef LUQ_DEBUG
+  p.slack = ctx->check_slack;
+#endif
   if (norm) return dtype == LUQ_BF16 ? launch_rows<__nv_bfloat16, kNormInt8>(ctx, p, st) : launch_rows<float, kNormInt8>(ctx, p, st);
   return dtype == LUQ_BF16 ? launch_rows<__nv_bfloat16, kInt8>(ctx, p, st) : launch_rows<float, kInt8>(ctx, p, st);
 }
@@ -1216,6 +1275,9 @@ int luq_launch_layer_norm_bwd(luq_ctx* ctx, const void* d_dy, int64_t ld_dy, con
   NormBwdParams p{};
   p.dy = d_dy; p.x = d_x; p.rows = rows; p.cols = cols; p.ld_dy = ld_dy; p.ld_x = ld_x; p.ld_dx = ld_dx;
   p.gamma = d_gamma; p.mean = d_mean; p.rstd = d_rstd; p.dx = d_dx; p.status = ctx->d_status;
+#ifdef LUQ_DEBUG
+  p.slack = ctx->check_slack;
+#endif
   return dtype == LUQ_BF16 ? launch_norm_bwd<__nv_bfloat16>(ctx, p, d_dgamma, d_dbeta, st)
                            : launch_norm_bwd<float>(ctx, p, d_dgamma, d_dbeta, st);
 }
