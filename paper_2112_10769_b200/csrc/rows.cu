@@ -552,6 +552,8 @@ struct Rows {
   }
   __device__ __forceinline__ void release(long long r) {
     if constexpr (LOAD == kRing) {
+      // (a wide group's reductions have a barrier; the shuffles of a warp's order no memory)
+      if constexpr (NARROW) __syncwarp();
       const long long next = r + depth * step;
       if (tid == 0 && next < rows) fill(stage, next);
       if (++stage == depth) { stage = 0; phase ^= 1u; }
