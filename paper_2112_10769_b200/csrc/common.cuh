@@ -150,7 +150,9 @@ int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, bool early, cudaS
 // become resident and set up (barriers, tensor memory, descriptor prefetch) while its predecessor
 // in the stream drains, and waits in pdl_wait() until that predecessor has completed and its writes
 // are visible.  Every kernel of the library calls pdl_wait() before its first access to global
-// memory, and all but the cooperative ones are launched this way.  One trap, measured: a small
+// memory, and all but the cooperative ones are launched this way.  One exception: the int8 product that comes right
+// after its own call's row kernel reads weights, offsets and channel scales before it.  The row kernel waits before it
+// lets the product start, so everything that was launched earlier has ended by then.  One trap, measured: a small
 // streaming block that becomes resident beside a running GEMM block sits on an SM carved for
 // maximum shared memory and keeps that small L1 after the GEMM has gone (the 462 MB max reduction:
 // 68 -> 96 us).  The streaming kernels therefore state a preference for the largest L1 carve-out,

@@ -20,7 +20,7 @@
 // tensor memory and returns.
 //
 // What bounds it: many tokens, the L2's delivery of operands next to the tensor cores (16384x4096x4096 175 us, 3.1 POP/s;
-// 8192x4096x1024 32.8 us, 2.1 POP/s, where a tile's contraction is hardly longer than its epilogue); few tokens, the
+// 8192x4096x1024 32.8 us, 2.1 POP/s: a tile's epilogue, beside the next tile's contraction, takes longer than its eight stages); few tokens, the
 // weights' bytes (32 tokens over 64 experts of 2048x1024 14.2 us) or, for one layer, the latency of a launch and one
 // trip through memory (5 tokens, 4096x4096 6.0 us).
 #include <cuda.h>

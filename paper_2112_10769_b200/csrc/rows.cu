@@ -120,7 +120,8 @@ __device__ __forceinline__ uint32_t quantize1(float v, float factor) {
 }
 
 // Any width, any alignment: one block per row, the row is read again for every pass (from L2).  Serves the
-// rows that do not fit a block's registers (above 16384 elements).
+// rows that do not fit a block's registers (above 16384 elements).  Element by element in every pass: 2048 x 32768 bf16
+// norm 266 us, to codes 354, codes alone 189 (1.0, 0.8 and 1.1 TB/s of what has to move).
 template <typename T, int MODE>
 __global__ void __launch_bounds__(512) row_loop_kernel(const RowParams p) {
   __shared__ float2 box[32];
@@ -328,7 +329,7 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 // The rows of one to two tensors on their way into a group's registers.
 //   start(r)   before the first row, after the wait for the preceding kernel
 //   take(r, v) row r's elements, zero beyond its end; rows come in the order first, first + step, ...
-//   release(r) kRing: once every thread of the group has taken row r (a barrier lies between), the stage is
+//   release(r) kRing: once every thread of the group has taken row r (a barrier lies between or, of one warp, is made), the stage is
 //              filled again
 // kRing waits are bounded; when one runs out the group goes on without writing anything (ok() is false), so that
 // its barriers still meet, and finish() waits for the copies under way and raises the status.
@@ -779,7 +780,8 @@ struct NormBwdParams {
 #endif
 };
 
-// mean_c(g) and mean_c(g xhat) of every row
+// mean_c(g) and mean_c(g xhat) of every row (wider than 16384 elements: with the kernel below and the sum of the chunks
+// 2048 x 32768 bf16 410 us, 1.0 TB/s)
 template <typename T>
 __global__ void __launch_bounds__(512) norm_bwd_means_kernel(const NormBwdParams p) {
   __shared__ float2 box[32];

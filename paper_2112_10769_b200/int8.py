@@ -76,7 +76,7 @@ class Int8Linear(_Int8Module):
 
 class Int8Experts(_Int8Module):
     """One weight per expert, ``[E, N, K]``.  ``forward(x, offsets)``: rows ``offsets[e] .. offsets[e + 1] - 1`` of x
-    belong to expert e (``offsets``: int32 on the device, E + 1 numbers)."""
+    belong to expert e (``offsets``: int32 on the device, E + 1 numbers); rows that belong to none are not written."""
 
     def __init__(self, weight: torch.Tensor, bias: torch.Tensor | None = None):
         super().__init__()
