@@ -381,8 +381,8 @@ int luq_gemm_wgrad_static(const uint8_t* d_g_codes, const float* d_alpha, int n_
                           const uint8_t* d_a_codes, const float* d_sa,
                           float* d_dw, int64_t M, int64_t N, int64_t K, void* stream);
 
-/* Where layer norm's backward pass and the one-call 8-bit products take their workspace from: alloc(user, bytes, stream)
- * returns device memory of at least `bytes` bytes (at most 96 MiB; 256-byte aligned, on the context's device, which is
+/* Where layer norm's backward pass, the one-call 8-bit and e2m1 products and luq_expert_order take their workspace from: alloc(user, bytes, stream)
+ * returns device memory of at least `bytes` bytes (at most 96 MiB, but for the e2m1 products; 256-byte aligned, on the context's device, which is
  * current) whose earlier users on `stream` may still be running, NULL if there is none (the call then returns
  * LUQ_ERR_WORKSPACE); release(user, ptr, stream) takes it back while the call's kernels may still be running on `stream`:
  * the next user has to come after them in that stream.  Both are called on the thread of the call and must not
@@ -464,6 +464,99 @@ int luq_quant_int8_gemm_grouped(luq_ctx* ctx, const void* d_x, int dtype, int64_
                                 const int32_t* d_offsets, int groups,
                                 const int8_t* d_w_codes, int64_t ld_w, int64_t w_stride, const float* d_sw, const float* d_bias,
                                 void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream);
+
+/* ---- microscaled 4-bit floating point ------------------------------------------------------------------
+ * Numbers are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; sign, two exponent bits, one mantissa bit), packed two
+ * to a byte, the earlier one in the lower half, with a scale for each block of a row's numbers:
+ *   block 32   power-of-two scales (e8m0 bytes: 2^(byte - 127)), no other scale
+ *   block 16   e4m3 scales, and a binary32 scale for the row
+ * Both are formats that the tensor cores multiply as they are.  (The paper's [1,3,0] gradient format is another one.)
+ *
+ * Block scales lie in tiles of 512 bytes, 128 rows x 4 blocks: row r, block b of a tile at byte
+ * 16 (r mod 32) + 4 (r / 32) + b; tiles follow one another along a row (ceil(K / (4 block)) of them) and then by rows of
+ * tiles.  Rows of tiles: of a matrix ceil(rows / 128), matrices one after the other; of rows in groups (experts) with offsets,
+ * group e's rows start at row of tiles offsets[e] / 128 + e, and there are rows / 128 + groups.
+ * Scales of blocks that lie beyond K are written as zeros.  Codes need a 16-byte aligned base and a row stride ("ld_*", bytes)
+ * that is a multiple of 16, tiles a 16-byte aligned base.  K numbers of a row are ceil(K / 2) bytes; a last half is zero.
+ *
+ * Quantizer, every operation rounded to binary32 and to nearest, ties to even codes:
+ *   block 16   g = max|row| / 2688, s = e4m3(max|block| / (6 g)), q = e2m1(x * (1 / (s g)))
+ *   block 32   s = 2^(floor(log2 max|block|) - 2), not below 2^-127, q = e2m1(x / s)
+ * Inf or NaN: block 16, zero codes and a NaN row scale; block 32, zero codes and a NaN scale (255) for its block; what is made
+ * of the row is NaN, other rows are not; LUQ_STATUS_NONFINITE.  Block 16, a non-zero row maximum below 2^-100: zero codes and
+ * scale, LUQ_STATUS_RANGE.
+ *   planes            the rows are that many matrices of rows / planes rows each, whose tiles follow one another
+ *   d_offsets/groups  (or NULL) the rows of a group start a row of tiles of their own; planes is 1
+ *   d_position/copies (or NULL) row r's codes and scales go to rows d_position[r * copies + j] of rows * copies; a position
+ *                     that is none of them is left out, rows that no position names are not written.  Needs d_offsets.
+ *                     Positions are distinct.
+ * d_row_scale: one per written row (block 16; NULL with block 32). */
+int luq_quant_e2m1_rows(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int64_t cols, int64_t ld_x, int block, int64_t planes,
+                        const int32_t* d_offsets, int groups, const int32_t* d_position, int copies,
+                        uint8_t* d_codes, int64_t ld_codes, uint8_t* d_tiles, float* d_row_scale, void* stream);
+
+/* Z[t,n] = gx[t] gw[n] sum_b sx[t,b] sw[n,b] sum_(k in b) X[t,k] W[n,k] + bias[n], binary32 sums.  Scales and codes as
+ * above, any values; d_x_scale and d_w_scale are the rows' scales (block 16; NULL with block 32).  d_bias may be NULL.
+ * 1 <= K < 2^31. */
+int luq_gemm_e2m1(luq_ctx* ctx, const uint8_t* d_x_codes, int64_t ld_x, const uint8_t* d_x_tiles, const float* d_x_scale, int block,
+                  const uint8_t* d_w_codes, int64_t ld_w, const uint8_t* d_w_tiles, const float* d_w_scale, const float* d_bias,
+                  void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream);
+/* The same grouped by expert, as luq_gemm_int8_grouped: w_codes[e] w_stride bytes apart (a multiple of 16), w_tiles, w_scale and
+ * bias of the experts one after the other, the tokens' tiles by the same offsets. */
+int luq_gemm_e2m1_grouped(luq_ctx* ctx, const uint8_t* d_x_codes, int64_t ld_x, const uint8_t* d_x_tiles, const float* d_x_scale, int block,
+                          const int32_t* d_offsets, int groups, const uint8_t* d_w_codes, int64_t ld_w, int64_t w_stride,
+                          const uint8_t* d_w_tiles, const float* d_w_scale, const float* d_bias,
+                          void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream);
+/* Quantizer and product in one call, with the same results bit for bit.  M: rows of x.  Grouped, with d_position [M x copies]: token
+ * t's results are rows d_position[t * copies + j] of the M * copies rows of z; without (NULL): rows as they lie, copies 1.
+ * The tokens' codes and scales stay in a workspace, less than rows * (0.6 K + 32) + groups * (8 K + 512) bytes for K >= 256; where
+ * that is more than 96 MiB and no allocator is set, LUQ_ERR_WORKSPACE. */
+int luq_quant_e2m1_gemm(luq_ctx* ctx, const void* d_x, int dtype, int64_t ld_x, int block, const uint8_t* d_w_codes, int64_t ld_w,
+                        const uint8_t* d_w_tiles, const float* d_w_scale, const float* d_bias,
+                        void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream);
+int luq_quant_e2m1_gemm_grouped(luq_ctx* ctx, const void* d_x, int dtype, int64_t ld_x, int block, const int32_t* d_position, int copies,
+                                const int32_t* d_offsets, int groups, const uint8_t* d_w_codes, int64_t ld_w, int64_t w_stride,
+                                const uint8_t* d_w_tiles, const float* d_w_scale, const float* d_bias,
+                                void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream);
+
+/* ---- a layer of experts --------------------------------------------------------------------------------
+ * Which of `experts` experts a token goes to, and with what weights.  logits [rows x experts], fp32 or bf16, row stride
+ * ld in elements.  With s = softmax(l) (score 0) or sigmoid(l) (score 1) and c = s + d_bias[e] (d_bias NULL: the order of the
+ * logits): the experts are `groups` equal groups, a group's value is the sum of its group_top (1 or 2) best c, the top_groups
+ * best groups stay; of theirs the k largest c are chosen, in descending order, d_chosen [rows x k].  Ties go to the lowest
+ * index; values are compared as exact ones (in binary64 where binary32 is too close).  d_weights [rows x k] = scale * s,
+ * renormalize: scale * s / sum of the chosen s.  An expert whose logit or bias is -Inf is never chosen: places that are
+ * left over hold -1 and weight 0.  A row with NaN or +Inf (or any row, if a bias has) gets -1 and NaN weights and raises
+ * LUQ_STATUS_NONFINITE.
+ * experts <= LUQ_MAX_GROUPS; 1 <= k <= 32 and k <= experts of top_groups groups; groups <= 32 divides experts. */
+int luq_route(luq_ctx* ctx, const void* d_logits, int dtype, int64_t rows, int experts, int64_t ld, int k, int score, const float* d_bias,
+              int groups, int top_groups, int group_top, int renormalize, float scale, int32_t* d_chosen, float* d_weights, void* stream);
+/* Gradient of the logits from the weights' (the choice is piecewise constant and has none): with ds_j = scale dw_j, or
+ * scale / S (dw_j - sum_i dw_i s_i / S) where renormalized (S: sum of the chosen s),
+ *   softmax: dl_e = s_e (ds_e - sum_j s_j ds_j)      sigmoid: dl_e = ds_e s_e (1 - s_e).
+ * Places that hold no expert have no part; an expert in several places gets the sum of theirs.  dlogits has the logits' type. */
+int luq_route_bwd(luq_ctx* ctx, const float* d_dweights, const void* d_logits, int dtype, int64_t rows, int experts, int64_t ld,
+                  const int32_t* d_chosen, int k, int score, int renormalize, float scale, void* d_dlogits, int64_t ld_d, void* stream);
+
+/* The copies of the tokens in the experts' order: d_position [rows x k] is each assignment's row - by expert, then by token, then
+ * by place; -1 where d_chosen holds no expert of 0 .. groups - 1 - and d_offsets [groups + 1] the experts' first rows.  Rows from
+ * d_offsets[groups] on (of rows * k) belong to no copy.  Uses a workspace of at most 1 MiB. */
+int luq_expert_order(luq_ctx* ctx, const int32_t* d_chosen, int64_t rows, int k, int groups, int32_t* d_position, int32_t* d_offsets,
+                     void* stream);
+/* out[d_position[t, j]] = x[t], out [rows * k x cols]; rows from d_offsets[groups] on are zeros.  Positions are distinct and below
+ * d_offsets[groups]; others than 0 .. rows * k - 1 are left out. */
+int luq_dispatch(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int64_t cols, int64_t ld_x, const int32_t* d_position, int k,
+                 const int32_t* d_offsets, int groups, void* d_out, int64_t ld_out, void* stream);
+/* out[t] = residual[t] + sum_j w[t, j] y[d_position[t, j]] in binary32, rounded once; y [y_rows x cols].  d_weights NULL: ones (then
+ * this is luq_dispatch's backward pass); d_residual may be NULL.  A place without a position adds w * 0. */
+int luq_combine(luq_ctx* ctx, const void* d_y, int dtype, int64_t y_rows, int64_t cols, int64_t ld_y, const int32_t* d_position,
+                int64_t rows, int k, const float* d_weights, const void* d_residual, int64_t ld_residual, void* d_out, int64_t ld_out,
+                void* stream);
+/* dy[d_position[t, j]] = w[t, j] dout[t], rows from d_offsets[groups] on zeros; dweights[t, j] = sum_c dout[t, c] y[d_position[t, j], c],
+ * zero where there is no position.  d_dy, d_dweights: each may be NULL (not needed); d_y only for dweights, d_weights NULL: ones. */
+int luq_combine_bwd(luq_ctx* ctx, const void* d_dout, int64_t ld_dout, const void* d_y, int64_t ld_y, int dtype, int64_t y_rows,
+                    int64_t cols, const int32_t* d_position, int64_t rows, int k, const float* d_weights, const int32_t* d_offsets,
+                    int groups, void* d_dy, int64_t ld_dy, float* d_dweights, void* stream);
 
 /* 1 if this library was compiled with -DLUQ_DEBUG: every shared-memory, tensor-memory and global
  * address that the converters, epilogues, row kernels and streaming loops form is checked against its region

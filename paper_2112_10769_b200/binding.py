@@ -36,6 +36,8 @@ SYMBOLS = ("luq_create", "luq_destroy", "luq_set_option", "luq_kmax", "luq_debug
            "luq_quant_grad_hindsight", "luq_debug_quotient", "luq_debug_expire_wait", "luq_debug_bounds_probe", "luq_gemm_fwd", "luq_quant_int4_gemm_fwd", "luq_gemm_bwd", "luq_gemm_wgrad",
            "luq_layer_norm", "luq_layer_norm_bwd", "luq_layer_norm_int8", "luq_quant_int8_rows", "luq_gemm_int8",
            "luq_gemm_int8_grouped", "luq_quant_int8_gemm", "luq_layer_norm_int8_gemm", "luq_quant_int8_gemm_grouped", "luq_set_allocator",
+           "luq_quant_e2m1_rows", "luq_gemm_e2m1", "luq_gemm_e2m1_grouped", "luq_quant_e2m1_gemm", "luq_quant_e2m1_gemm_grouped",
+           "luq_route", "luq_route_bwd", "luq_expert_order", "luq_dispatch", "luq_combine", "luq_combine_bwd",
            "luq_gemm_wgrad_static", "luq_status", "luq_launch_count", "luq_strerror")
 
 _lib = None
@@ -96,6 +98,19 @@ def load() -> ctypes.CDLL:
         L.luq_layer_norm_int8_gemm.argtypes = [vp, vp, ci, i64, vp, vp, cf, vp, i64, vp, vp] + product
         L.luq_quant_int8_gemm_grouped.argtypes = [vp, vp, ci, i64, vp, ci, vp, i64, i64, vp, vp] + product
         L.luq_set_allocator.argtypes = [vp, vp, vp, vp]
+        weights = [vp, i64, vp, vp, vp]                                  # w_codes, ld_w, w_tiles, w_scale, bias
+        experts = [vp, ci, vp, i64, i64, vp, vp, vp]                     # offsets, groups, w_codes, ld_w, w_stride, w_tiles, w_scale, bias
+        L.luq_quant_e2m1_rows.argtypes = [vp, vp, ci, i64, i64, i64, ci, i64, vp, ci, vp, ci, vp, i64, vp, vp, vp]
+        L.luq_gemm_e2m1.argtypes = [vp, vp, i64, vp, vp, ci] + weights + product
+        L.luq_gemm_e2m1_grouped.argtypes = [vp, vp, i64, vp, vp, ci] + experts + product
+        L.luq_quant_e2m1_gemm.argtypes = [vp, vp, ci, i64, ci] + weights + product
+        L.luq_quant_e2m1_gemm_grouped.argtypes = [vp, vp, ci, i64, ci, vp, ci] + experts + product
+        L.luq_route.argtypes = [vp, vp, ci, i64, ci, i64, ci, ci, vp, ci, ci, ci, ci, cf, vp, vp, vp]
+        L.luq_route_bwd.argtypes = [vp, vp, vp, ci, i64, ci, i64, vp, ci, ci, ci, cf, vp, i64, vp]
+        L.luq_expert_order.argtypes = [vp, vp, i64, ci, ci, vp, vp, vp]
+        L.luq_dispatch.argtypes = [vp, vp, ci, i64, i64, i64, vp, ci, vp, ci, vp, i64, vp]
+        L.luq_combine.argtypes = [vp, vp, ci, i64, i64, i64, vp, i64, ci, vp, vp, i64, vp, i64, vp]
+        L.luq_combine_bwd.argtypes = [vp, vp, i64, vp, i64, ci, i64, i64, vp, i64, ci, vp, vp, ci, vp, i64, vp, vp]
         L.luq_status.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int)]
         L.luq_launch_count.argtypes = [vp]
         L.luq_launch_count.restype = i64
@@ -121,10 +136,18 @@ def _dtype_value(dtype: torch.dtype) -> int:
     raise TypeError("outputs are float32 or bfloat16")
 
 
+def _score(name: str) -> int:
+    if name not in ("softmax", "sigmoid"):
+        raise TypeError("score: 'softmax' or 'sigmoid' expected")
+    return int(name == "sigmoid")
+
+
 _native = None
 _NATIVE_ENTRIES = ("luq_layer_norm", "luq_layer_norm_bwd", "luq_layer_norm_int8", "luq_quant_int8_rows", "luq_gemm_int8",
                    "luq_gemm_int8_grouped", "luq_quant_int8_gemm", "luq_layer_norm_int8_gemm", "luq_quant_int8_gemm_grouped",
-                   "luq_set_allocator")
+                   "luq_set_allocator", "luq_quant_e2m1_rows", "luq_gemm_e2m1", "luq_gemm_e2m1_grouped", "luq_quant_e2m1_gemm",
+                   "luq_quant_e2m1_gemm_grouped", "luq_route", "luq_route_bwd", "luq_expert_order", "luq_dispatch", "luq_combine",
+                   "luq_combine_bwd")
 
 
 def native():
@@ -511,6 +534,80 @@ class Context:
         """quant_int8_rows(x) and gemm_int8_grouped in one call."""
         return self._native.quant_int8_gemm_grouped(self._address, self.device, x, offsets, w_codes, w_scale, bias, out,
                                                     -1 if out_dtype is None else _dtype_value(out_dtype))
+
+    # ---- microscaled 4-bit floating point ---------------------------------------------------------
+    # Numbers are e2m1, packed two to a byte (uint8 codes [rows, ceil(K / 2)] whose rows start at multiples of 16 bytes), with a
+    # scale for each block of 16 or 32.  Block scales lie in tiles (uint8 [rows of tiles, tiles along a row, 512], the layout
+    # e2m1.scale_tiles makes of plain ones); blocks of 16 have a float32 scale for each row besides, blocks of 32 None.
+    def quant_e2m1_rows(self, x: torch.Tensor, block: int = 16, planes: int = 1, offsets: torch.Tensor | None = None,
+                        position: torch.Tensor | None = None):
+        """(codes, tiles, row_scale) of rows - tokens, or the output channels of a weight.  ``planes``: the rows are so many
+        matrices, whose tiles follow one another.  ``offsets``: the rows of an expert, whose tiles start anew, too.
+        ``position`` [rows, k]: every row is written to k rows of rows * k, as gemm_e2m1_grouped reads them."""
+        return self._native.quant_e2m1_rows(self._address, self.device, x, block, planes, offsets, position)
+
+    def gemm_e2m1(self, codes: torch.Tensor, tiles: torch.Tensor, row_scale: torch.Tensor | None, w_codes: torch.Tensor,
+                  w_tiles: torch.Tensor, w_row_scale: torch.Tensor | None, bias: torch.Tensor | None = None, block: int = 16,
+                  out: torch.Tensor | None = None, out_dtype=torch.float32):
+        """Z[t, n] = sum over the blocks' products times all scales (+ bias[n])."""
+        return self._native.gemm_e2m1(self._address, self.device, codes, tiles, row_scale, w_codes, w_tiles, w_row_scale, bias, block, out,
+                                      _dtype_value(out_dtype))
+
+    def gemm_e2m1_grouped(self, codes: torch.Tensor, tiles: torch.Tensor, row_scale: torch.Tensor | None, offsets: torch.Tensor,
+                          w_codes: torch.Tensor, w_tiles: torch.Tensor, w_row_scale: torch.Tensor | None,
+                          bias: torch.Tensor | None = None, block: int = 16, out: torch.Tensor | None = None, out_dtype=torch.float32):
+        """gemm_e2m1 with one weight per expert (w_codes [experts, N, ceil(K / 2)]): rows offsets[e] .. offsets[e + 1] - 1 with
+        w_codes[e]; the tokens were quantized with the same offsets.  Rows that belong to no expert are not written."""
+        return self._native.gemm_e2m1_grouped(self._address, self.device, codes, tiles, row_scale, offsets, w_codes, w_tiles, w_row_scale,
+                                              bias, block, out, _dtype_value(out_dtype))
+
+    def quant_e2m1_gemm(self, x: torch.Tensor, w_codes: torch.Tensor, w_tiles: torch.Tensor, w_row_scale: torch.Tensor | None,
+                        bias: torch.Tensor | None = None, block: int = 16, out: torch.Tensor | None = None, out_dtype=None):
+        """quant_e2m1_rows(x) and gemm_e2m1 in one call; the result has the type of x unless said otherwise."""
+        return self._native.quant_e2m1_gemm(self._address, self.device, x, block, w_codes, w_tiles, w_row_scale, bias, out,
+                                            -1 if out_dtype is None else _dtype_value(out_dtype))
+
+    def quant_e2m1_gemm_grouped(self, x: torch.Tensor, offsets: torch.Tensor, w_codes: torch.Tensor, w_tiles: torch.Tensor,
+                                w_row_scale: torch.Tensor | None, bias: torch.Tensor | None = None, block: int = 16,
+                                position: torch.Tensor | None = None, out: torch.Tensor | None = None, out_dtype=None):
+        """quant_e2m1_rows(x) and gemm_e2m1_grouped in one call.  With ``position`` [rows, k] (expert_order) x holds each token once
+        and the result has its k rows where ``position`` says; without it x lies sorted by expert."""
+        return self._native.quant_e2m1_gemm_grouped(self._address, self.device, x, block, position, offsets, w_codes, w_tiles, w_row_scale,
+                                                    bias, out, -1 if out_dtype is None else _dtype_value(out_dtype))
+
+    # ---- a layer of experts ------------------------------------------------------------------------
+    def route(self, logits: torch.Tensor, k: int, score: str = "softmax", bias: torch.Tensor | None = None, groups: int = 1,
+              top_groups: int = 1, group_top: int = 2, renormalize: bool = True, scale: float = 1.0):
+        """(experts int32 [rows, k], weights float32 [rows, k]).  The k experts with the largest score (+ bias) among those of the
+        ``top_groups`` best of ``groups`` equal groups (by the sum of their ``group_top`` best), in descending order, ties to the
+        lowest index; weights are scale * score, divided by the chosen scores' sum if ``renormalize``.  Experts whose logit is
+        -inf are never chosen: places left over hold -1 and weight 0."""
+        return self._native.route(self._address, self.device, logits, k, _score(score), bias, groups, top_groups, group_top, renormalize,
+                                  scale)
+
+    def route_bwd(self, dweights: torch.Tensor, logits: torch.Tensor, experts: torch.Tensor, score: str = "softmax",
+                  renormalize: bool = True, scale: float = 1.0):
+        """Gradient of route's logits from that of its weights."""
+        return self._native.route_bwd(self._address, self.device, dweights, logits, experts, _score(score), renormalize, scale)
+
+    def expert_order(self, experts: torch.Tensor, groups: int):
+        """(offsets int32 [groups + 1], position int32 [rows, k]): where the copies of the tokens lie when they are sorted by
+        expert (stable), and every expert's first row.  Experts outside 0 .. groups - 1 get position -1."""
+        return self._native.expert_order(self._address, self.device, experts, groups)
+
+    def dispatch(self, x: torch.Tensor, position: torch.Tensor, offsets: torch.Tensor, out: torch.Tensor | None = None):
+        """Rows [rows * k, cols] with every token copied to its k positions; rows from offsets[-1] on are zeros."""
+        return self._native.dispatch(self._address, self.device, x, position, offsets, out)
+
+    def combine(self, y: torch.Tensor, position: torch.Tensor, weights: torch.Tensor | None = None,
+                residual: torch.Tensor | None = None, out: torch.Tensor | None = None):
+        """residual[t] + sum over j of weights[t, j] * y[position[t, j]], in 32 bits, rounded once to the type of y."""
+        return self._native.combine(self._address, self.device, y, position, weights, residual, out)
+
+    def combine_bwd(self, dout: torch.Tensor, y: torch.Tensor, position: torch.Tensor, weights: torch.Tensor | None,
+                    offsets: torch.Tensor, need_dy: bool = True, need_dweights: bool = True):
+        """(dy, dweights) of combine; rows of dy from offsets[-1] on are zeros.  What is not needed is None and not computed."""
+        return self._native.combine_bwd(self._address, self.device, dout, y, position, weights, offsets, need_dy, need_dweights)
 
     def status(self) -> int:
         """Synchronises the current stream; returns and clears the device status bits."""

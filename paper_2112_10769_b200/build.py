@@ -22,7 +22,8 @@ ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 COMMON = ["-std=c++17", "-O3", "-lineinfo", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"),
           "-I", CSRC, "--expt-relaxed-constexpr",
           "-diag-suppress", "177"]   # 177: a static member that one instantiation of a configuration struct does not use
-UNITS = {"quant.cu": ["-fmad=false"], "gemm.cu": [], "rows.cu": [], "gemm_int8.cu": [], "api.cu": []}
+UNITS = {"quant.cu": ["-fmad=false"], "gemm.cu": [], "rows.cu": [], "gemm_int8.cu": [], "e2m1.cu": [], "gemm_e2m1.cu": [],
+         "experts.cu": [], "api.cu": []}
 
 
 def _digest(paths, extra=()) -> str:
@@ -74,7 +75,8 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     nvcc = os.environ.get("NVCC", "nvcc")
     lib = LIB_DEBUG if debug else LIB
     suffix, define = (".dbg.o", ["-DLUQ_DEBUG"]) if debug else (".o", [])
-    headers = [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "int4_math.cuh"), os.path.join(ROOT, "include", "luq.h")]
+    headers = [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "int4_math.cuh"), os.path.join(CSRC, "product_tiles.cuh"),
+               os.path.join(ROOT, "include", "luq.h")]
     objs, digests, running = [], [], []
     for name, extra in UNITS.items():
         src = os.path.join(CSRC, name)

@@ -701,6 +701,231 @@ int luq_quant_int8_gemm_grouped(luq_ctx* ctx, const void* d_x, int dtype, int64_
                       z_dtype, true, d_x, dtype, ld_x, false, nullptr, nullptr, 0.0f, false, stream);
 }
 
+// ---- microscaled 4-bit floating point --------------------------------------------------------------------
+
+namespace {
+
+int64_t code_bytes(int64_t K) { return (K + 1) / 2; }
+bool tiles_ok(const void* p, bool needed) { return p ? aligned16(p) : !needed; }
+bool ints_ok(const void* p, bool needed) { return p ? (reinterpret_cast<uintptr_t>(p) & 3u) == 0 : !needed; }
+
+int e2m1_args_ok(const luq_e2m1_args& a, int z_dtype, bool grouped) {
+  if (!element_type(z_dtype) || !rows_ok(a.M, a.K) || a.N < 0 || a.N > kMaxExtent || (a.block != 16 && a.block != 32)) return LUQ_ERR_ARG;
+  if (grouped && (a.groups < 1 || a.groups > LUQ_MAX_GROUPS || !ints_ok(a.offsets, a.M && a.N))) return LUQ_ERR_ARG;
+  if (grouped && (a.w_stride % 16 || a.w_stride >= (1ll << 40) ||
+                  (a.groups > 1 && a.N && a.w_stride < (a.N - 1) * a.ld_w + code_bytes(a.K)))) return LUQ_ERR_ARG;
+  if (a.M == 0 || a.N == 0) return LUQ_OK;
+  if (!codes_ok(a.w_codes, a.N, code_bytes(a.K), a.ld_w) || !tiles_ok(a.w_tiles, true)) return LUQ_ERR_ARG;
+  if (!floats_ok(a.sw, a.block == 16) || !floats_ok(a.bias, false)) return LUQ_ERR_ARG;
+  return tensor_ok(a.z, z_dtype, a.M, a.N, a.ld_z, true) ? LUQ_OK : LUQ_ERR_ARG;
+}
+
+// the product from codes (x == null) or from high-precision rows, whose codes for a.M rows go to a workspace first
+int e2m1_product(luq_ctx* ctx, luq_e2m1_args a, int z_dtype, bool grouped, const void* x, int dtype, int64_t ld_x, int64_t x_rows,
+                 const int32_t* position, int copies, bool from_codes, void* stream) {
+  if (!ctx) return LUQ_ERR_ARG;
+  const int rc = e2m1_args_ok(a, z_dtype, grouped);
+  if (rc) return rc;
+  a.out_bf16 = z_dtype == LUQ_BF16;
+  if (!grouped) { a.offsets = nullptr; a.groups = 1; }
+  if (a.groups == 1) a.w_stride = a.ld_w * a.N;         // (there is nothing between one group and the next)
+  if (from_codes) {
+    if (!codes_ok(a.x_codes, a.M, code_bytes(a.K), a.ld_x) || !tiles_ok(a.x_tiles, a.M > 0) || !floats_ok(a.sx, a.block == 16 && a.M > 0))
+      return LUQ_ERR_ARG;
+  } else if (!element_type(dtype) || !tensor_ok(x, dtype, x_rows, a.K, ld_x, true) || !ints_ok(position, false)) {
+    return LUQ_ERR_ARG;
+  }
+  if (a.M == 0 || a.N == 0) return LUQ_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return LUQ_ERR_CUDA;
+  if (from_codes) return cuda_rc(luq_launch_gemm_e2m1(ctx, a, false, as_stream(stream)));
+  a.ld_x = (code_bytes(a.K) + 15) / 16 * 16;
+  const size_t codes = static_cast<size_t>(a.M) * a.ld_x;
+  const size_t tiles = static_cast<size_t>(luq_e2m1_tile_rows(a.M, grouped ? a.groups : 0)) * luq_e2m1_k_tiles(a.K, a.block) * 512;
+  const size_t bytes = codes + tiles + (a.block == 16 ? a.M * sizeof(float) : 0);
+  if (!ctx->alloc && bytes > ctx->workspace_bytes) return LUQ_ERR_WORKSPACE;
+  luq_call_workspace workspace(ctx, stream);
+  uint8_t* const q = static_cast<uint8_t*>(workspace.get(bytes));
+  if (!q) return LUQ_ERR_WORKSPACE;
+  luq_e2m1_rows_args r{};
+  r.x = x; r.dtype = dtype; r.rows = x_rows; r.cols = a.K; r.ld_x = ld_x; r.block = a.block; r.plane_rows = x_rows;
+  r.offsets = a.offsets; r.groups = a.groups; r.position = position; r.copies = position ? copies : 1; r.out_rows = a.M;
+  r.codes = q; r.ld_codes = a.ld_x; r.tiles = q + codes;
+  r.scale = a.block == 16 ? reinterpret_cast<float*>(q + codes + tiles) : nullptr;
+  a.x_codes = q; a.x_tiles = r.tiles; a.sx = r.scale;
+  const int e = cuda_rc(luq_launch_e2m1_rows(ctx, r, as_stream(stream)));
+  return e ? e : cuda_rc(luq_launch_gemm_e2m1(ctx, a, true, as_stream(stream)));
+}
+
+luq_e2m1_args e2m1_args(const uint8_t* x, int64_t ld_x, const uint8_t* x_tiles, const float* sx, int block, const int32_t* offsets, int groups,
+                        const uint8_t* w, int64_t ld_w, int64_t w_stride, const uint8_t* w_tiles, const float* sw, const float* bias,
+                        void* z, int64_t ld_z, int64_t M, int64_t N, int64_t K) {
+  luq_e2m1_args a{};
+  a.x_codes = x; a.ld_x = ld_x; a.x_tiles = x_tiles; a.sx = sx; a.offsets = offsets; a.groups = groups;
+  a.w_codes = w; a.ld_w = ld_w; a.w_stride = w_stride; a.w_tiles = w_tiles; a.sw = sw; a.bias = bias;
+  a.z = z; a.ld_z = ld_z; a.M = M; a.N = N; a.K = K; a.block = block;
+  return a;
+}
+
+}  // namespace
+
+int luq_quant_e2m1_rows(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int64_t cols, int64_t ld_x, int block, int64_t planes,
+                        const int32_t* d_offsets, int groups, const int32_t* d_position, int copies, uint8_t* d_codes, int64_t ld_codes,
+                        uint8_t* d_tiles, float* d_row_scale, void* stream) {
+  if (!ctx || !element_type(dtype) || !rows_ok(rows, cols) || (block != 16 && block != 32)) return LUQ_ERR_ARG;
+  if (planes < 1 || rows % planes || (d_offsets && (planes != 1 || groups < 1 || groups > LUQ_MAX_GROUPS))) return LUQ_ERR_ARG;
+  if (d_position && (!d_offsets || copies < 1 || rows * copies > kMaxExtent)) return LUQ_ERR_ARG;
+  const int64_t out_rows = d_position ? rows * copies : rows;
+  if (!tensor_ok(d_x, dtype, rows, cols, ld_x, true) || !codes_ok(d_codes, out_rows, code_bytes(cols), ld_codes)) return LUQ_ERR_ARG;
+  if (!tiles_ok(d_tiles, rows > 0) || !floats_ok(d_row_scale, block == 16 && rows > 0)) return LUQ_ERR_ARG;
+  if (!ints_ok(d_offsets, false) || !ints_ok(d_position, false)) return LUQ_ERR_ARG;
+  if (rows == 0) return LUQ_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return LUQ_ERR_CUDA;
+  luq_e2m1_rows_args r{};
+  r.x = d_x; r.dtype = dtype; r.rows = rows; r.cols = cols; r.ld_x = ld_x; r.block = block; r.plane_rows = rows / planes;
+  r.offsets = d_offsets; r.groups = groups; r.position = d_position; r.copies = d_position ? copies : 1; r.out_rows = out_rows;
+  r.codes = d_codes; r.ld_codes = ld_codes; r.tiles = d_tiles; r.scale = d_row_scale;
+  return cuda_rc(luq_launch_e2m1_rows(ctx, r, as_stream(stream)));
+}
+
+int luq_gemm_e2m1(luq_ctx* ctx, const uint8_t* d_x_codes, int64_t ld_x, const uint8_t* d_x_tiles, const float* d_x_scale, int block,
+                  const uint8_t* d_w_codes, int64_t ld_w, const uint8_t* d_w_tiles, const float* d_w_scale, const float* d_bias, void* d_z,
+                  int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream) {
+  return e2m1_product(ctx, e2m1_args(d_x_codes, ld_x, d_x_tiles, d_x_scale, block, nullptr, 1, d_w_codes, ld_w, 0, d_w_tiles, d_w_scale,
+                                     d_bias, d_z, ld_z, M, N, K), z_dtype, false, nullptr, 0, 0, 0, nullptr, 1, true, stream);
+}
+
+int luq_gemm_e2m1_grouped(luq_ctx* ctx, const uint8_t* d_x_codes, int64_t ld_x, const uint8_t* d_x_tiles, const float* d_x_scale, int block,
+                          const int32_t* d_offsets, int groups, const uint8_t* d_w_codes, int64_t ld_w, int64_t w_stride,
+                          const uint8_t* d_w_tiles, const float* d_w_scale, const float* d_bias, void* d_z, int z_dtype, int64_t ld_z,
+                          int64_t M, int64_t N, int64_t K, void* stream) {
+  return e2m1_product(ctx, e2m1_args(d_x_codes, ld_x, d_x_tiles, d_x_scale, block, d_offsets, groups, d_w_codes, ld_w, w_stride, d_w_tiles,
+                                     d_w_scale, d_bias, d_z, ld_z, M, N, K), z_dtype, true, nullptr, 0, 0, 0, nullptr, 1, true, stream);
+}
+
+int luq_quant_e2m1_gemm(luq_ctx* ctx, const void* d_x, int dtype, int64_t ld_x, int block, const uint8_t* d_w_codes, int64_t ld_w,
+                        const uint8_t* d_w_tiles, const float* d_w_scale, const float* d_bias, void* d_z, int z_dtype, int64_t ld_z,
+                        int64_t M, int64_t N, int64_t K, void* stream) {
+  return e2m1_product(ctx, e2m1_args(nullptr, 0, nullptr, nullptr, block, nullptr, 1, d_w_codes, ld_w, 0, d_w_tiles, d_w_scale, d_bias, d_z,
+                                     ld_z, M, N, K), z_dtype, false, d_x, dtype, ld_x, M, nullptr, 1, false, stream);
+}
+
+int luq_quant_e2m1_gemm_grouped(luq_ctx* ctx, const void* d_x, int dtype, int64_t ld_x, int block, const int32_t* d_position, int copies,
+                                const int32_t* d_offsets, int groups, const uint8_t* d_w_codes, int64_t ld_w, int64_t w_stride,
+                                const uint8_t* d_w_tiles, const float* d_w_scale, const float* d_bias, void* d_z, int z_dtype, int64_t ld_z,
+                                int64_t M, int64_t N, int64_t K, void* stream) {
+  if (copies < 1 || M < 0 || M > kMaxExtent / copies || (!d_position && copies != 1)) return LUQ_ERR_ARG;
+  return e2m1_product(ctx, e2m1_args(nullptr, 0, nullptr, nullptr, block, d_offsets, groups, d_w_codes, ld_w, w_stride, d_w_tiles, d_w_scale,
+                                     d_bias, d_z, ld_z, M * copies, N, K), z_dtype, true, d_x, dtype, ld_x, M, d_position, copies, false, stream);
+}
+
+// ---- a layer of experts ------------------------------------------------------------------------------------
+
+namespace {
+
+constexpr int kMostChosen = 32;
+
+bool route_ok(const luq_ctx* ctx, int dtype, int64_t rows, int experts, int k, int score) {
+  return ctx && element_type(dtype) && rows >= 0 && experts >= 1 && experts <= LUQ_MAX_GROUPS && k >= 1 && k <= kMostChosen && k <= experts &&
+         (score == 0 || score == 1) && rows <= kMaxExtent / k;
+}
+bool move_ok(const luq_ctx* ctx, int dtype, int64_t rows, int64_t cols, int k) {
+  return ctx && element_type(dtype) && rows_ok(rows, cols) && k >= 1 && rows <= kMaxExtent / k;
+}
+
+}  // namespace
+
+int luq_route(luq_ctx* ctx, const void* d_logits, int dtype, int64_t rows, int experts, int64_t ld, int k, int score, const float* d_bias,
+              int groups, int top_groups, int group_top, int renormalize, float scale, int32_t* d_chosen, float* d_weights, void* stream) {
+  if (!route_ok(ctx, dtype, rows, experts, k, score) || groups < 1 || groups > 32 || experts % groups || top_groups < 1 ||
+      top_groups > groups || (group_top != 1 && group_top != 2) || k > experts / groups * top_groups) return LUQ_ERR_ARG;
+  if (!tensor_ok(d_logits, dtype, rows, experts, ld, true) || !floats_ok(d_bias, false) || !ints_ok(d_chosen, rows > 0) ||
+      !floats_ok(d_weights, rows > 0)) return LUQ_ERR_ARG;
+  if (rows == 0) return LUQ_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return LUQ_ERR_CUDA;
+  luq_route_args a{d_logits, dtype, rows, experts, ld, k, score == 1, d_bias, groups, top_groups, group_top, renormalize != 0, scale, d_chosen,
+                   d_weights};
+  return cuda_rc(luq_launch_route(ctx, a, as_stream(stream)));
+}
+
+int luq_route_bwd(luq_ctx* ctx, const float* d_dweights, const void* d_logits, int dtype, int64_t rows, int experts, int64_t ld,
+                  const int32_t* d_chosen, int k, int score, int renormalize, float scale, void* d_dlogits, int64_t ld_d, void* stream) {
+  if (!route_ok(ctx, dtype, rows, experts, k, score)) return LUQ_ERR_ARG;
+  if (!tensor_ok(d_logits, dtype, rows, experts, ld, true) || !tensor_ok(d_dlogits, dtype, rows, experts, ld_d, true) ||
+      !ints_ok(d_chosen, rows > 0) || !floats_ok(d_dweights, rows > 0)) return LUQ_ERR_ARG;
+  if (rows == 0) return LUQ_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return LUQ_ERR_CUDA;
+  luq_route_args a{};
+  a.logits = d_logits; a.dtype = dtype; a.rows = rows; a.experts = experts; a.ld = ld; a.k = k; a.sigmoid = score == 1;
+  a.renormalize = renormalize != 0; a.scale = scale; a.chosen = const_cast<int32_t*>(d_chosen);
+  return cuda_rc(luq_launch_route_bwd(ctx, a, d_dweights, d_dlogits, ld_d, as_stream(stream)));
+}
+
+int luq_expert_order(luq_ctx* ctx, const int32_t* d_chosen, int64_t rows, int k, int groups, int32_t* d_position, int32_t* d_offsets,
+                     void* stream) {
+  if (!ctx || rows < 0 || k < 1 || rows > kMaxExtent / k || groups < 1 || groups > LUQ_MAX_GROUPS) return LUQ_ERR_ARG;
+  if (!ints_ok(d_chosen, rows > 0) || !ints_ok(d_position, rows > 0) || !ints_ok(d_offsets, true)) return LUQ_ERR_ARG;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return LUQ_ERR_CUDA;
+  luq_call_workspace workspace(ctx, stream);
+  int* counts = nullptr;
+  if (const size_t bytes = luq_order_workspace(rows * k, groups)) {
+    counts = static_cast<int*>(workspace.get(bytes));
+    if (!counts) return LUQ_ERR_WORKSPACE;
+  }
+  return cuda_rc(luq_launch_order(ctx, d_chosen, rows * k, groups, d_position, d_offsets, counts, as_stream(stream)));
+}
+
+int luq_dispatch(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, int64_t cols, int64_t ld_x, const int32_t* d_position, int k,
+                 const int32_t* d_offsets, int groups, void* d_out, int64_t ld_out, void* stream) {
+  if (!move_ok(ctx, dtype, rows, cols, k) || groups < 1 || groups > LUQ_MAX_GROUPS) return LUQ_ERR_ARG;
+  if (!tensor_ok(d_x, dtype, rows, cols, ld_x, true) || !tensor_ok(d_out, dtype, rows * k, cols, ld_out, true) ||
+      !ints_ok(d_position, rows > 0) || !ints_ok(d_offsets, rows > 0)) return LUQ_ERR_ARG;
+  if (rows == 0) return LUQ_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return LUQ_ERR_CUDA;
+  luq_move_args a{};
+  a.x = d_x; a.ld_x = ld_x; a.dtype = dtype; a.position = d_position; a.rows = rows; a.k = k; a.cols = cols; a.copies = rows * k;
+  a.offsets = d_offsets; a.groups = groups; a.out = d_out; a.ld_out = ld_out;
+  return cuda_rc(luq_launch_dispatch(ctx, a, as_stream(stream)));
+}
+
+int luq_combine(luq_ctx* ctx, const void* d_y, int dtype, int64_t y_rows, int64_t cols, int64_t ld_y, const int32_t* d_position,
+                int64_t rows, int k, const float* d_weights, const void* d_residual, int64_t ld_residual, void* d_out, int64_t ld_out,
+                void* stream) {
+  if (!move_ok(ctx, dtype, rows, cols, k) || y_rows < 0 || y_rows > kMaxExtent) return LUQ_ERR_ARG;
+  if (!tensor_ok(d_y, dtype, y_rows, cols, ld_y, true) || !tensor_ok(d_residual, dtype, rows, cols, ld_residual, false) ||
+      !tensor_ok(d_out, dtype, rows, cols, ld_out, true) || !ints_ok(d_position, rows > 0) || !floats_ok(d_weights, false)) return LUQ_ERR_ARG;
+  if (rows == 0) return LUQ_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return LUQ_ERR_CUDA;
+  luq_move_args a{};
+  a.x = d_y; a.ld_x = ld_y; a.more = d_residual; a.ld_more = ld_residual; a.dtype = dtype; a.position = d_position; a.rows = rows; a.k = k;
+  a.cols = cols; a.copies = y_rows; a.weights = d_weights; a.out = d_out; a.ld_out = ld_out;
+  return cuda_rc(luq_launch_combine(ctx, a, as_stream(stream)));
+}
+
+int luq_combine_bwd(luq_ctx* ctx, const void* d_dout, int64_t ld_dout, const void* d_y, int64_t ld_y, int dtype, int64_t y_rows,
+                    int64_t cols, const int32_t* d_position, int64_t rows, int k, const float* d_weights, const int32_t* d_offsets,
+                    int groups, void* d_dy, int64_t ld_dy, float* d_dweights, void* stream) {
+  if (!move_ok(ctx, dtype, rows, cols, k) || y_rows < 0 || y_rows > kMaxExtent || groups < 1 || groups > LUQ_MAX_GROUPS) return LUQ_ERR_ARG;
+  if (!tensor_ok(d_dout, dtype, rows, cols, ld_dout, true) || !tensor_ok(d_y, dtype, y_rows, cols, ld_y, d_dweights != nullptr) ||
+      !tensor_ok(d_dy, dtype, y_rows, cols, ld_dy, false) || !ints_ok(d_position, rows > 0) || !floats_ok(d_weights, false) ||
+      !ints_ok(d_offsets, d_dy != nullptr) || !floats_ok(d_dweights, false)) return LUQ_ERR_ARG;
+  if (!d_dy && !d_dweights) return LUQ_OK;
+  if (rows == 0 && y_rows == 0) return LUQ_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return LUQ_ERR_CUDA;
+  luq_move_args a{};
+  a.x = d_y; a.ld_x = ld_y; a.more = d_dout; a.ld_more = ld_dout; a.dtype = dtype; a.position = d_position; a.rows = rows; a.k = k;
+  a.cols = cols; a.copies = y_rows; a.weights = d_weights; a.offsets = d_offsets; a.groups = groups; a.out = d_dy; a.ld_out = ld_dy;
+  a.dweights = d_dweights;
+  return cuda_rc(luq_launch_combine_bwd(ctx, a, as_stream(stream)));
+}
+
 int luq_status(luq_ctx* ctx, void* stream, int* host_flags) {
   if (!ctx || !host_flags) return LUQ_ERR_ARG;
   DeviceGuard guard(ctx->device);

@@ -143,6 +143,53 @@ struct luq_int8_args {
 // early: the preceding kernel of the stream is this call's quantizer, which writes x_codes and sx only
 int luq_launch_gemm_int8(luq_ctx* ctx, const luq_int8_args& a, bool early, cudaStream_t st);
 
+// gemm_e2m1.cu: Z[t, n] = sx[t] sw[e, n] sum_b bx[t, b] bw[e, n, b] sum_(k in b) X[t, k] W[e, n, k] + bias[e, n]
+struct luq_e2m1_args {
+  const uint8_t* x_codes; int64_t ld_x; const uint8_t* x_tiles; const float* sx;      // ld_*: bytes
+  const int* offsets; int groups;                       // offsets null: one group
+  const uint8_t* w_codes; int64_t ld_w; int64_t w_stride; const uint8_t* w_tiles;
+  const float* sw; const float* bias;
+  void* z; int out_bf16; int64_t ld_z;
+  int64_t M, N, K; int block;
+};
+// early: the preceding kernel of the stream is this call's quantizer, which writes x_codes, x_tiles and sx only
+int luq_launch_gemm_e2m1(luq_ctx* ctx, const luq_e2m1_args& a, bool early, cudaStream_t st);
+// Tiles of 128 rows x 4 block scales: along a row, and rows of tiles (a group's rows start one of their own; groups 0: no groups)
+inline int64_t luq_e2m1_k_tiles(int64_t K, int block) { return (K + 4 * block - 1) / (4 * block); }
+inline int64_t luq_e2m1_tile_rows(int64_t rows, int64_t groups) { return groups ? rows / 128 + groups : (rows + 127) / 128; }
+
+// e2m1.cu: rows to packed e2m1 numbers, block scales in tiles, row scales (block 16)
+struct luq_e2m1_rows_args {
+  const void* x; int dtype; int64_t rows, cols, ld_x; int block;
+  int64_t plane_rows;                                   // the rows of a matrix, whose scales start a tile row of their own
+  const int* offsets; int groups;                       // or: the rows of a group do (null: no groups)
+  const int* position; int copies;                      // row r is written to rows position[r * copies ..] (null: to row r)
+  int64_t out_rows;
+  uint8_t* codes; int64_t ld_codes; uint8_t* tiles; float* scale;
+};
+int luq_launch_e2m1_rows(luq_ctx* ctx, const luq_e2m1_rows_args& a, cudaStream_t st);
+
+// experts.cu: routing, the copies' order, and rows on their way to the experts and back
+struct luq_route_args {
+  const void* logits; int dtype; int64_t rows; int experts; int64_t ld;
+  int k; bool sigmoid; const float* bias; int groups, top_groups, group_top; bool renormalize; float scale;
+  int* chosen; float* weights;
+};
+int luq_launch_route(luq_ctx* ctx, const luq_route_args& a, cudaStream_t st);
+int luq_launch_route_bwd(luq_ctx* ctx, const luq_route_args& a, const float* dweights, void* dlogits, int64_t ld_d, cudaStream_t st);
+size_t luq_order_workspace(int64_t total, int experts);
+int luq_launch_order(luq_ctx* ctx, const int* chosen, int64_t total, int experts, int* position, int* offsets, int* counts,
+                     cudaStream_t st);
+struct luq_move_args {
+  const void* x; int64_t ld_x; const void* more; int64_t ld_more; int dtype;
+  const int* position; int64_t rows; int k; int64_t cols; int64_t copies;
+  const float* weights; const int* offsets; int groups;
+  void* out; int64_t ld_out; float* dweights;
+};
+int luq_launch_dispatch(luq_ctx* ctx, const luq_move_args& a, cudaStream_t st);
+int luq_launch_combine(luq_ctx* ctx, const luq_move_args& a, cudaStream_t st);
+int luq_launch_combine_bwd(luq_ctx* ctx, const luq_move_args& a, cudaStream_t st);
+
 #ifdef __CUDACC__
 
 // Launch helper.  LUQ_LAUNCH_COOPERATIVE: all blocks of the grid are resident at once (the kernel

@@ -1,0 +1,309 @@
+// Quantizer of rows (tokens, or the output channels of a weight) to 4-bit floating point with a scale for each block of a row
+// (sm_100a).  Numbers are e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, packed two to a byte, the earlier one in the
+// lower half.  Every operation below is rounded to binary32, to nearest.
+//
+//   blocks of 16   g = max|row| / 2688       s = e4m3(max|block| / (6 g))              q = e2m1(x * (1 / (s g)))
+//   blocks of 32                             s = 2^(floor(log2 max|block|) - 2)        q = e2m1(x / s)
+//
+// 2688 = 6 * 448: the row's largest block gets the largest e4m3 number, its largest element the largest e2m1 number.  A block
+// that is less than 2^-10 of the row's scale has a zero scale and zero numbers.
+//
+// A thread holds 16 neighbouring elements in registers, so x is read once; the row's maximum meets in shared memory.  Block
+// scales leave in the tiles that the tensor cores copy (128 rows x 4 blocks, row r, block b at 16 (r mod 32) + 4 (r / 32) + b):
+// the threads of four blocks put their bytes together and one stores the word.  What bounds it is the memory's bytes.
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+
+namespace {
+
+using namespace luqdev;
+
+constexpr int kChunk = 16;                 // elements of a thread
+constexpr int kScaleTile = 512;
+
+struct RowsParams {
+  const void* x;
+  long long rows, ld_x;
+  int cols;
+  long long plane_rows;
+  const int* offsets;       // may be null
+  int groups;
+  const int* position;      // may be null
+  int copies;
+  long long out_rows;
+  uint8_t* codes;
+  long long ld_codes;
+  uint8_t* tiles;
+  float* scale;             // blocks of 16
+  int k_tiles;
+  unsigned int* status;
+  bool vec;                 // rows of x start at multiples of 16 bytes
+};
+
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+
+// 16 elements of a row from `c0` on, zeros beyond its end
+template <typename T>
+__device__ __forceinline__ void load_chunk16(const T* row, int c0, int cols, bool vec, float (&v)[kChunk]) {
+  if (vec && c0 + kChunk <= cols) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 f = reinterpret_cast<const float4*>(row + c0)[i];
+        v[4 * i] = f.x; v[4 * i + 1] = f.y; v[4 * i + 2] = f.z; v[4 * i + 3] = f.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint4 u = reinterpret_cast<const uint4*>(row + c0)[i];
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
+          v[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) v[i] = c0 + i < cols ? load1(row + c0 + i) : 0.0f;
+  }
+}
+// the largest pattern of |v|: of numbers the largest, Inf above every number, NaN above Inf
+__device__ __forceinline__ uint32_t top_of(const float (&v)[kChunk]) {
+  uint32_t t = 0;
+#pragma unroll
+  for (int i = 0; i < kChunk; ++i) t = max(t, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  return t;
+}
+// eight numbers, the first in the lowest four bits
+__device__ __forceinline__ uint32_t pack8(const float* v, float f) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(r)
+      : "f"(__fmul_rn(v[0], f)), "f"(__fmul_rn(v[1], f)), "f"(__fmul_rn(v[2], f)), "f"(__fmul_rn(v[3], f)),
+        "f"(__fmul_rn(v[4], f)), "f"(__fmul_rn(v[5], f)), "f"(__fmul_rn(v[6], f)), "f"(__fmul_rn(v[7], f)));
+  return r;
+}
+// the e4m3 number nearest to v >= 0 (at most 448), and its value
+__device__ __forceinline__ uint32_t to_e4m3(float v, float& value) {
+  uint16_t b;
+  uint32_t h;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(0.0f), "f"(v));
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(b));
+  asm("{\n\t.reg .f16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.f32.f16 %0, lo;\n\t}" : "=f"(value) : "r"(h));
+  return b & 0xFFu;
+}
+
+// What a row's elements are made of: the row's scale and six times it (blocks of 16), and whether it has numbers at all
+struct RowScale {
+  float g, six;
+  bool dead;             // Inf or NaN, or nothing to scale by: zero codes
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t top) {
+  RowScale s;
+  s.dead = top >= 0x7F800000u || top < 0x0D800000u;                 // 2^-100
+  s.g = s.dead ? (top >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : 0.0f) : __fdiv_rn(__uint_as_float(top), 2688.0f);
+  s.six = __fmul_rn(s.g, 6.0f);
+  return s;
+}
+// a block's scale byte and the factor of its elements
+template <int BLOCK>
+__device__ __forceinline__ uint32_t block_scale(uint32_t top, const RowScale& row, float& factor) {
+  if constexpr (BLOCK == 16) {
+    factor = 0.0f;
+    if (row.dead) return 0u;
+    float s;
+    const uint32_t byte = to_e4m3(__fdiv_rn(__uint_as_float(top), row.six), s);
+    if (s > 0.0f) factor = __frcp_rn(__fmul_rn(s, row.g));
+    return byte;
+  } else {
+    if (top >= 0x7F800000u) { factor = 0.0f; return 255u; }
+    const uint32_t byte = max(static_cast<int>(top >> 23) - 2, 0);
+    factor = __uint_as_float((254u - byte) << 23);
+    return byte;
+  }
+}
+
+// The group of a row and the row's number in it, by a whole warp; false: the row belongs to none.  Whatever the offsets
+// hold, start / 128 + group + in_group / 128 is below out_rows / 128 + groups.
+__device__ __forceinline__ bool group_of(const RowsParams& p, int row, int& tile_row, int& in_tile) {
+  const int lane = threadIdx.x & 31;
+  int before = 0;                              // offsets 1 .. groups that are at most `row`
+  for (int e0 = 1; e0 <= p.groups; e0 += 32) {
+    const int e = e0 + lane;
+    before += __popc(__ballot_sync(0xFFFFFFFFu, e <= p.groups && *(p.offsets + e) <= row));
+  }
+  if (before >= p.groups) return false;
+  const int start = max(*(p.offsets + before), 0);
+  if (start > row) return false;
+  tile_row = start / 128 + before + (row - start) / 128;
+  in_tile = (row - start) % 128;
+  return true;
+}
+
+template <int BLOCK>
+__device__ __forceinline__ void store_chunk(const RowsParams& p, long long out_row, long long tile_row, int in_tile, bool tiled, int chunk,
+                                            uint2 codes, uint32_t byte) {
+  const int lane = threadIdx.x & 31;
+  // the word of four blocks' scales (blocks of 32 are two threads)
+  constexpr int kThreads = BLOCK == 16 ? 4 : 8;
+  uint32_t word = byte << (8 * (BLOCK == 16 ? lane & 3 : (lane >> 1) & 3));
+  if (BLOCK == 32) word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
+  else word |= __shfl_xor_sync(0xFFFFFFFFu, word, 1);
+  word |= __shfl_xor_sync(0xFFFFFFFFu, word, 2);
+  const int kt = chunk / kThreads;
+  if (tiled && (lane & (kThreads - 1)) == 0 && kt < p.k_tiles &&
+      LUQ_IN_BOUNDS(tile_row >= 0 && in_tile >= 0 && in_tile < 128, p.status))
+    *reinterpret_cast<uint32_t*>(p.tiles + (tile_row * p.k_tiles + kt) * kScaleTile + (in_tile & 31) * 16 + (in_tile >> 5) * 4) = word;
+  const int first = chunk * (kChunk / 2), bytes = (p.cols + 1) / 2 - first;
+  if (bytes <= 0 || !LUQ_IN_BOUNDS(out_row >= 0 && out_row < p.out_rows, p.status)) return;
+  uint8_t* const to = p.codes + out_row * p.ld_codes + first;
+  if (bytes >= 8) {
+    *reinterpret_cast<uint2*>(to) = codes;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < bytes) to[i] = static_cast<uint8_t>((i < 4 ? codes.x : codes.y) >> (8 * (i & 3)));
+  }
+}
+
+// A chunk in registers -> its codes and scale byte -> every row it goes to
+template <int BLOCK>
+__device__ __forceinline__ void quantize_chunk(const float (&v)[kChunk], uint32_t top, const RowScale& row, uint2& codes, uint32_t& byte) {
+  float f;
+  byte = block_scale<BLOCK>(top, row, f);
+  // (a factor of zero would leave NaN where there is Inf)
+  codes = f > 0.0f ? make_uint2(pack8(v, f), pack8(v + 8, f)) : make_uint2(0u, 0u);
+}
+
+// WARPS warps share a row, a thread has CHUNKS of its chunks, every (32 * WARPS)-th.  CHUNKS = 0: any width, chunks are read
+// again for the second pass (from L2).
+template <typename T, int BLOCK, int WARPS, int CHUNKS>
+__global__ void __launch_bounds__(256) e2m1_rows_kernel(const RowsParams p) {
+  constexpr int kRowsPerBlock = 8 / WARPS;
+  __shared__ uint32_t box[8];
+  pdl_wait();
+  pdl_trigger();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int t = threadIdx.x % (32 * WARPS);
+  const long long r = static_cast<long long>(blockIdx.x) * kRowsPerBlock + warp / WARPS;
+  const bool there = r < p.rows;
+  const T* const x = static_cast<const T*>(p.x) + (there ? r : 0) * p.ld_x;
+  const int cols = there ? p.cols : 0;
+  const int chunks = p.k_tiles * (4 * BLOCK / kChunk);        // with the padding of the last tile of scales
+  constexpr int kHeld = CHUNKS > 0 ? CHUNKS : 1;
+  float v[kHeld][kChunk];
+  uint32_t top[kHeld], row_top = 0;
+  if constexpr (CHUNKS > 0) {
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) load_chunk16(x, (t + i * 32 * WARPS) * kChunk, cols, p.vec, v[i]);
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) { top[i] = top_of(v[i]); row_top = max(row_top, top[i]); }
+  } else {
+    for (int c = t; c * kChunk < cols; c += 32 * WARPS) {
+      load_chunk16(x, c * kChunk, cols, p.vec, v[0]);
+      row_top = max(row_top, top_of(v[0]));
+    }
+  }
+  row_top = __reduce_max_sync(0xFFFFFFFFu, row_top);
+  if (WARPS > 1 && (BLOCK == 16 || CHUNKS == 0)) {            // (blocks of 32 need no maximum of the row, only its status)
+    if (lane == 0) box[warp] = row_top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) row_top = max(row_top, box[warp / WARPS * WARPS + i]);
+  }
+  if (!there) return;                                          // (whole warps, and no meeting follows)
+  RowScale row{};
+  if constexpr (BLOCK == 16) row = row_scale(row_top);
+  if (lane == 0) {
+    const bool bad = row_top >= 0x7F800000u, tiny = BLOCK == 16 && row_top < 0x0D800000u && row_top > 0;
+    if (bad || tiny) atomicOr(p.status, bad ? LUQ_STATUS_NONFINITE : LUQ_STATUS_RANGE);
+  }
+  auto put = [&](int chunk, uint2 codes, uint32_t byte) {
+    // (shuffles inside: every lane of the warp calls)
+    if (p.position == nullptr && p.offsets == nullptr) {
+      const long long plane = r / p.plane_rows, in_plane = r - plane * p.plane_rows;
+      store_chunk<BLOCK>(p, r, plane * ((p.plane_rows + 127) / 128) + in_plane / 128, static_cast<int>(in_plane % 128), true, chunk, codes, byte);
+      return;
+    }
+    for (int j = 0; j < p.copies; ++j) {
+      const int to = p.position ? *(p.position + r * p.copies + j) : static_cast<int>(r);
+      if (to < 0 || to >= p.out_rows) continue;                // warp-uniform
+      int tile_row = 0, in_tile = 0;
+      const bool tiled = group_of(p, to, tile_row, in_tile);
+      store_chunk<BLOCK>(p, to, tile_row, in_tile, tiled, chunk, codes, byte);
+    }
+  };
+  if constexpr (CHUNKS > 0) {
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      uint32_t b = top[i], byte;
+      if (BLOCK == 32) b = max(b, __shfl_xor_sync(0xFFFFFFFFu, b, 1));
+      uint2 codes;
+      quantize_chunk<BLOCK>(v[i], b, row, codes, byte);
+      const int c = t + i * 32 * WARPS;
+      if (c - lane < chunks) put(c, codes, c < chunks ? byte : 0u);
+    }
+  } else {
+    for (int c = t; c - lane < chunks; c += 32 * WARPS) {
+      load_chunk16(x, c * kChunk, cols, p.vec, v[0]);
+      uint32_t b = top_of(v[0]), byte;
+      if (BLOCK == 32) b = max(b, __shfl_xor_sync(0xFFFFFFFFu, b, 1));
+      uint2 codes;
+      quantize_chunk<BLOCK>(v[0], b, row, codes, byte);
+      put(c, codes, c < chunks ? byte : 0u);
+    }
+  }
+  if (BLOCK == 16 && t == 0) {
+    if (p.position) {
+      for (int j = 0; j < p.copies; ++j) {
+        const int to = *(p.position + r * p.copies + j);
+        if (to >= 0 && to < p.out_rows) p.scale[to] = row.g;
+      }
+    } else {
+      p.scale[r] = row.g;
+    }
+  }
+}
+
+template <typename T, int BLOCK, int WARPS, int CHUNKS>
+int launch(luq_ctx* ctx, const RowsParams& p, cudaStream_t st) {
+  constexpr int kRowsPerBlock = 8 / WARPS;
+  const long long blocks = (p.rows + kRowsPerBlock - 1) / kRowsPerBlock;
+  const cudaError_t e = luq_launch_kernel(e2m1_rows_kernel<T, BLOCK, WARPS, CHUNKS>, static_cast<int>(blocks), 256, 0, st, LUQ_LAUNCH_EARLY, 1, p);
+  if (e == cudaSuccess) ctx->launches += 1;
+  return static_cast<int>(e);
+}
+template <typename T, int BLOCK>
+int launch_width(luq_ctx* ctx, const RowsParams& p, cudaStream_t st) {
+  const int chunks = p.k_tiles * (4 * BLOCK / kChunk);
+  if (chunks <= 32) return launch<T, BLOCK, 1, 1>(ctx, p, st);
+  if (chunks <= 64) return launch<T, BLOCK, 2, 1>(ctx, p, st);
+  if (chunks <= 128) return launch<T, BLOCK, 4, 1>(ctx, p, st);
+  if (chunks <= 256) return launch<T, BLOCK, 8, 1>(ctx, p, st);
+  if (chunks <= 512) return launch<T, BLOCK, 8, 2>(ctx, p, st);
+  if (chunks <= 1024) return launch<T, BLOCK, 8, 4>(ctx, p, st);
+  return launch<T, BLOCK, 8, 0>(ctx, p, st);
+}
+
+}  // namespace
+
+int luq_launch_e2m1_rows(luq_ctx* ctx, const luq_e2m1_rows_args& a, cudaStream_t st) {
+  RowsParams p{};
+  p.x = a.x; p.rows = a.rows; p.ld_x = a.ld_x; p.cols = static_cast<int>(a.cols);
+  p.plane_rows = a.plane_rows; p.offsets = a.offsets; p.groups = a.groups; p.position = a.position; p.copies = a.copies;
+  p.out_rows = a.out_rows; p.codes = a.codes; p.ld_codes = a.ld_codes; p.tiles = a.tiles; p.scale = a.scale;
+  p.k_tiles = static_cast<int>(luq_e2m1_k_tiles(a.cols, a.block));
+  p.status = ctx->d_status;
+  p.vec = (reinterpret_cast<uintptr_t>(a.x) & 15u) == 0 && (a.rows <= 1 || a.ld_x * (a.dtype == LUQ_BF16 ? 2 : 4) % 16 == 0);
+  if (a.dtype == LUQ_BF16) return a.block == 16 ? launch_width<__nv_bfloat16, 16>(ctx, p, st) : launch_width<__nv_bfloat16, 32>(ctx, p, st);
+  return a.block == 16 ? launch_width<float, 16>(ctx, p, st) : launch_width<float, 32>(ctx, p, st);
+}
