@@ -89,10 +89,12 @@ struct Cfg {
   static constexpr int per_sm = BT <= 64 ? 2 : 1;
   static constexpr int stages = BT <= 64 ? 3 : PAIR ? 4 : 5;
   static constexpr int chunk = 32;                                // tokens per epilogue step
-  // tensor memory: the accumulators of two tiles (one on a pair), then the stages' scales
-  static constexpr int accumulators = PAIR ? 1 : 2;
-  static constexpr int scale_cols = 4 * k_tiles * (1 + x_tile_rows);
-  static constexpr int used_cols = accumulators * BT + stages * scale_cols;
+  // Tensor memory: the accumulators of two tiles, then places for scales.  On a pair the accumulators share 96 columns,
+  // which are taken out of a tile first: 2 x 256 columns would leave none for the scales.
+  static constexpr int second = PAIR ? 160 : BT, shared_cols = PAIR ? BT - second : 0;
+  static constexpr int scale_cols = 4 * k_tiles * (1 + x_tile_rows), first_scale = second + BT;
+  static constexpr int places = PAIR && BLOCK == 16 ? 2 : stages;
+  static constexpr int used_cols = first_scale + places * scale_cols;
   static constexpr int tmem_cols = used_cols <= 128 ? 128 : used_cols <= 256 ? 256 : 512;
   static_assert(used_cols <= 512 / per_sm, "tensor memory has 512 columns");
   static constexpr int staging = stages * stage_bytes;            // store boxes
@@ -100,7 +102,7 @@ struct Cfg {
   // a split's partial tile lies where the stages were, which its contraction is done with
   static_assert(BT * kCh * 4 <= stages * stage_bytes, "a partial tile has to fit the stages");
   static constexpr int barriers = token_scales + 2 * BT * 4;
-  static constexpr int num_barriers = 2 * stages + 2 * accumulators;
+  static constexpr int num_barriers = 2 * stages + 4;
   static constexpr int tmem_slot = barriers + 8 * num_barriers;
   static constexpr int abort_flag = tmem_slot + 4;
   static constexpr int groups = abort_flag + 4;                   // group ends, then tile prefix: 2 x (groups + 1) ints
@@ -152,55 +154,66 @@ __device__ __forceinline__ float2 scale2(uint32_t a0, uint32_t a1, float2 sw, fl
 }
 
 // Takes a tile's accumulators out of tensor memory, scales them and writes them: this warp's quarter of the
-// lanes (32 channels) and its group's span of tokens, in steps of 32.
+// lanes (32 channels) and its group's tokens, in steps of 32, two steps' accumulators in registers at a time.
 // A full step goes through a staged box [token][channel] and a copy; a step that holds rows of another
 // group, or an output the copies cannot address, is written element by element (32 channels in a row).
 // One fence serves all boxes a warp has (two of bf16, one of fp32).
-template <typename C, bool BF16>
+// On a pair the two groups of warps take every other step, the steps that the next tile's accumulators share first;
+// `taken` is called once, when those (elsewhere all) are in registers.
+template <typename C, bool BF16, bool PAIR, typename Taken>
 __device__ __forceinline__ void write_tile(const E2m1Params& p, const void* tm_z, const Unit& v, float sw, float bias,
-                                           uint32_t taddr, uint32_t tmem_base, int warp_e, int lane, uint32_t staging,
-                                           uint8_t* gen, const float* scales) {
-  constexpr int CH = C::chunk, kSteps = C::span / CH, kPair = kSteps < 2 ? kSteps : 2;
+                                           uint32_t taddr, uint32_t buf, uint32_t tmem_base, int warp_e, int lane, uint32_t staging,
+                                           uint8_t* gen, const float* scales, Taken taken) {
+  constexpr int CH = C::chunk, kSteps = C::span / CH, kPair = 2;
+  static_assert(kSteps % kPair == 0);
   constexpr int kBoxes = BF16 ? 2 : 1, kBoxBytes = kWarpStaging / kBoxes;
-  const int quarter = (warp_e + kFirstEpiWarp) & 3;
+  const int quarter = (warp_e + kFirstEpiWarp) & 3, group = warp_e >> 2;
   const int ch_first = v.ch0 + quarter * 32, ch = ch_first + lane;
-  const int c_first = (warp_e >> 2) * C::span;
-  if (ch_first >= p.N || c_first >= v.rows) return;    // warp-uniform
-  const bool boxes = CH == 32 && p.z_tma && (ch_first + 32 <= p.N || p.tma_cols == p.N);
+  // columns 160 .. 255 of the first accumulators are 0 .. 95 of the second
+  auto first_token = [&](int step) { return PAIR ? (2 * step + group + (buf == 0 ? 4 : 0)) % 8 * CH : group * C::span + step * CH; };
+  static_assert(!PAIR || (C::second == 5 * CH && C::span == 4 * CH));
+  const bool channels = ch_first < p.N;                // warp-uniform
+  const bool boxes = p.z_tma && (ch_first + 32 <= p.N || p.tma_cols == p.N);
   const float2 sw2 = make_float2(sw, sw), bias2 = make_float2(bias, bias);
   const uint32_t slot = static_cast<uint32_t>(warp_e) * kWarpStaging;
   uint8_t* const box0 = gen + C::staging + slot;
 
-  int staged = 0, first_staged = c_first;
+  int staged = 0, staged_at[kBoxes];
   auto flush = [&]() {                                 // hands the staged boxes to the copy engine
     fence_proxy_async();
     __syncwarp();
     if (lane == 0) {
-      for (int i = 0; i < staged; ++i)
-        if (z_in(p, v.row0 + first_staged + 32 * i + 31, min(ch_first + 31, static_cast<int>(p.N) - 1)))
-          tma_store_2d(tm_z, staging + slot + i * kBoxBytes, ch_first, v.row0 + first_staged + 32 * i);
+#pragma unroll
+      for (int i = 0; i < kBoxes; ++i)
+        if (i < staged && z_in(p, v.row0 + staged_at[i] + 31, min(ch_first + 31, static_cast<int>(p.N) - 1)))
+          tma_store_2d(tm_z, staging + slot + i * kBoxBytes, ch_first, v.row0 + staged_at[i]);
       bulk_commit();
     }
     staged = 0;
   };
 #pragma unroll 1
-  for (int pair = 0; pair < kSteps && c_first + pair * CH < v.rows; pair += kPair) {
+  for (int pair = 0; pair < kSteps; pair += kPair) {
     uint32_t r[kPair][CH];
 #pragma unroll
-    for (int i = 0; i < kPair; ++i)
-      if (c_first + (pair + i) * CH < v.rows &&
-          tmem_in(taddr + c_first + (pair + i) * CH, tmem_base, C::tmem_cols, p.status, CH)) load_chunk<CH>(taddr + c_first + (pair + i) * CH, r[i]);
+    for (int i = 0; i < kPair; ++i) {
+      const int c0 = first_token(pair + i);
+      if (channels && c0 < v.rows && tmem_in(taddr + c0, tmem_base, C::first_scale, p.status, CH)) load_chunk<CH>(taddr + c0, r[i]);
+    }
     tmem_ld_wait();
+    if (pair == (PAIR ? 0 : kSteps - kPair)) taken();
+    if (!channels) continue;
 #pragma unroll
     for (int step = 0; step < kPair; ++step) {
-      const int c0 = c_first + (pair + step) * CH, left = v.rows - c0;
+      const int c0 = first_token(pair + step), left = v.rows - c0;
       if (boxes && left >= 32) {
         if (staged == 0) {                               // (first of its pair) the stores that last read this warp's boxes are done
           if (lane == 0) bulk_wait_read<0>();
           __syncwarp();
         }
-        if (staged == 0) first_staged = c0;
         uint8_t* const box = box0 + staged * kBoxBytes;
+#pragma unroll
+        for (int i = 0; i < kBoxes; ++i)
+          if (i == staged) staged_at[i] = c0;
         ++staged;
         // all scales first: between the stores below every load would wait for the last store
         float4 s_step[CH / 4];
@@ -297,13 +310,13 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   auto full = [&](uint32_t s) { return bar0 + 8u * s; };
   auto empty = [&](uint32_t s) { return bar0 + 8u * (ES + s); };
   auto acc_full = [&](uint32_t b) { return bar0 + 8u * (2 * ES + b); };
-  auto acc_empty = [&](uint32_t b) { return bar0 + 8u * (2 * ES + C::accumulators + b); };
+  auto acc_empty = [&](uint32_t b) { return bar0 + 8u * (2 * ES + 2 + b); };
   volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + C::tmem_slot);
   volatile uint32_t* const abort_flag = reinterpret_cast<volatile uint32_t*>(gen + C::abort_flag);
   int* const hi = reinterpret_cast<int*>(gen + C::groups);
   int* const first_tile = hi + p.groups + 1;
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = PAIR || SPLIT ? cluster_ctarank() : 0u;
   const uint32_t cluster = PAIR ? 2u : (SPLIT ? cluster_nctarank() : 1u);
   // this CTA's share of a tile's contraction
@@ -341,7 +354,7 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   if (threadIdx.x == 0) {
     // on a pair the leader's barriers count both CTAs
     for (int s = 0; s < ES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-    for (int b = 0; b < C::accumulators; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), (PAIR ? 2 : 1) * C::epi_warps); }
+    for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), (PAIR ? 2 : 1) * C::epi_warps); }
     *abort_flag = 0;
     fence_barrier_init();
     fence_proxy_async();
@@ -370,7 +383,9 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   uint32_t stage = 0, phase = 0, issued = 0, it = 0;
   bool ok = true, waited = !p.early;
 
-  // one thread fetches the weights, another the tokens (two threads pull more than one)
+  // One warp fetches the weights, another the tokens, a third multiplies.  A whole warp walks and waits and one of its
+  // threads issues: in a loop of one thread alone every issue takes some 50 cycles more (its operands are no longer known to
+  // be the warp's), which bound the kernel: 16384x4096x4096 202 -> 118 us.
   auto produce = [&](const Unit& v, bool tokens) {
     // token rows of this CTA: all of the tile's, or on a pair its half of the instruction's extent
     const int x_row0 = v.row0 + (PAIR ? static_cast<int>(rank) * ((v.rows + 31) / 32 * 16) : 0);
@@ -380,24 +395,27 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     const int x_tile_row = (v.row0 - v.in_group) / 128 + v.group + v.in_group / 128;
     for (int kb = kb_first; kb < kb_end; ++kb) {
       if (!mbar_wait(empty(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
-      if (!tokens) {
-        w_copy(v, kb, stage);
-      } else {
-        const uint32_t dst = base + stage * C::stage_bytes + C::at_x, scales = base + stage * C::stage_bytes + C::at_x_scales;
-        const uint32_t bar = PAIR ? mapa_shared(full(stage), 0) : full(stage);
-        if constexpr (PAIR) tma_pair_load_3d(scales, &tm_xs, bar, 0, kb * C::k_tiles, x_tile_row);
-        else tma_load_3d(scales, &tm_xs, bar, 0, kb * C::k_tiles, x_tile_row);
-        if (whole) {
-          if constexpr (PAIR) tma_pair_load_2d(dst, &tm_x, bar, kb * kBk, x_row0);
-          else tma_load_2d(dst, &tm_x, bar, kb * kBk, x_row0);
+      if (elect_one()) {
+        if (!tokens) {
+          w_copy(v, kb, stage);
         } else {
-          for (int b = 0; b < parts; ++b) {
-            const int off = b * C::part_rows;
-            if constexpr (PAIR) tma_pair_load_2d(dst + off * kBk, &tm_x_part, bar, kb * kBk, x_row0 + off);
-            else tma_load_2d(dst + off * kBk, &tm_x_part, bar, kb * kBk, x_row0 + off);
+          const uint32_t dst = base + stage * C::stage_bytes + C::at_x, scales = base + stage * C::stage_bytes + C::at_x_scales;
+          const uint32_t bar = PAIR ? mapa_shared(full(stage), 0) : full(stage);
+          if constexpr (PAIR) tma_pair_load_3d(scales, &tm_xs, bar, 0, kb * C::k_tiles, x_tile_row);
+          else tma_load_3d(scales, &tm_xs, bar, 0, kb * C::k_tiles, x_tile_row);
+          if (whole) {
+            if constexpr (PAIR) tma_pair_load_2d(dst, &tm_x, bar, kb * kBk, x_row0);
+            else tma_load_2d(dst, &tm_x, bar, kb * kBk, x_row0);
+          } else {
+            for (int b = 0; b < parts; ++b) {
+              const int off = b * C::part_rows;
+              if constexpr (PAIR) tma_pair_load_2d(dst + off * kBk, &tm_x_part, bar, kb * kBk, x_row0 + off);
+              else tma_load_2d(dst + off * kBk, &tm_x_part, bar, kb * kBk, x_row0 + off);
+            }
           }
         }
       }
+      __syncwarp();
       ++issued;
       if (++stage == static_cast<uint32_t>(ES)) { stage = 0; phase ^= 1u; }
     }
@@ -410,55 +428,68 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         else mbar_wait(full(s), ((issued - 1 - s) / ES) & 1u, abort_flag);
       }
   };
-  auto multiply = [&](const Unit& v) {                 // one thread (of the leader)
+  uint32_t place = 0, stages_done = 0;
+  auto multiply = [&](const Unit& v) {                 // one warp (of the leader)
     // e2m1 A and B, both K-major, binary32 accumulators; N covers the tile's tokens; the scales' type: e4m3 0, e8m0 1
     const uint32_t n8 = PAIR ? (v.rows + 31) / 32 * 4 : (v.rows + 15) / 16 * 2;
     const uint32_t idesc0 = (1u << 7) | (1u << 10) | (n8 << 17) | ((BLOCK == 32 ? 1u : 0u) << 23) | (static_cast<uint32_t>((PAIR ? 2 : 1) * kCh >> 7) << 27);
     const uint64_t da0 = umma_desc_sw128(base, 16, 1024), db0 = umma_desc_sw128(base + C::at_x, 16, 1024);
     const uint64_t dsa0 = scale_desc(base + C::at_w_scales), dsb0 = scale_desc(base + C::at_x_scales);
     constexpr uint64_t kStageStep = C::stage_bytes >> 4;
-    const uint32_t buf = it % C::accumulators, use = it / C::accumulators;
-    const bool free = PAIR ? mbar_wait_cluster(acc_empty(buf), (use & 1u) ^ 1u, abort_flag)
-                           : mbar_wait(acc_empty(buf), (use & 1u) ^ 1u, abort_flag);
+    const uint32_t buf = it & 1u;
+    // On a pair: the tile before has left the columns that the two share, and so the one before that all of its own
+    const bool free = PAIR ? it == 0 || mbar_wait_cluster(acc_empty(0), (it - 1) & 1u, abort_flag)
+                           : mbar_wait(acc_empty(buf), ((it >> 1) & 1u) ^ 1u, abort_flag);
     if (!free) { ok = false; return; }
     tc_fence_after();
-    const uint32_t tmem_d = tmem_base + buf * BT;
+    const uint32_t tmem_d = tmem_base + buf * C::second;
     // the tile's first token among the rows of its scales' tile: 32 rows are one column (the instruction takes the scales
     // from an even column on, so tiles are of 64 tokens at least)
     const uint32_t first_col = static_cast<uint32_t>(v.in_group % 128) / 32;
-    uint32_t accumulate = 0;
     for (int kb = kb_first; kb < kb_end; ++kb) {
-      const bool there = PAIR ? mbar_wait_cluster(full(stage), phase, abort_flag) : mbar_wait(full(stage), phase, abort_flag);
+      bool there = PAIR ? mbar_wait_cluster(full(stage), phase, abort_flag) : mbar_wait(full(stage), phase, abort_flag);
+      if (C::places < ES && stages_done >= C::places) {          // the products that used these scales' place are done
+        const uint32_t before = stage >= C::places ? stage - C::places : stage + ES - C::places;
+        there = there && mbar_wait(empty(before), stage >= C::places ? phase : phase ^ 1u, abort_flag);
+      }
       if (!there) { ok = false; return; }
       tc_fence_after();
-      // scales: [k tile][4 columns] of the channels, then [k tile][tile row][4 columns] of the tokens
-      const uint32_t sa = tmem_base + C::accumulators * BT + stage * C::scale_cols, sb = sa + 4 * C::k_tiles;
+      if (elect_one()) {
+        // scales: [k tile][4 columns] of the channels, then [k tile][tile row][4 columns] of the tokens
+        const uint32_t sa = tmem_base + C::first_scale + place * C::scale_cols, sb = sa + 4 * C::k_tiles;
 #pragma unroll
-      for (int t = 0; t < C::k_tiles; ++t) {
-        tc_copy_scales<PAIR>(sa + 4 * t, dsa0 + stage * kStageStep + t * (kScaleTile >> 4));
+        for (int t = 0; t < C::k_tiles; ++t) {
+          tc_copy_scales<PAIR>(sa + 4 * t, dsa0 + stage * kStageStep + t * (kScaleTile >> 4));
 #pragma unroll
-        for (int r = 0; r < C::x_tile_rows; ++r)
-          tc_copy_scales<PAIR>(sb + 4 * (t * C::x_tile_rows + r), dsb0 + stage * kStageStep + (r * C::k_tiles + t) * (kScaleTile >> 4));
-      }
-      const uint64_t da = da0 + stage * kStageStep, db = db0 + stage * kStageStep;
-      const int steps = min(kSteps4, p.k_steps - kb * kSteps4);
-#pragma unroll
-      for (int kk = 0; kk < kSteps4; ++kk) {
-        if (kk < steps) {
-          // blocks of 16: an instruction's four scales are a column; of 32: its two are half of one
-          const int t = BLOCK == 16 ? kk : kk / 2;
-          const uint32_t half = BLOCK == 16 ? 0u : 2u * (kk & 1);
-          const uint32_t idesc = idesc0 | (half << 4) | (half << 29);
-          tc_mma_scaled<BLOCK, PAIR>(tmem_d, da + kk * 2, db + kk * 2, idesc, sa + 4 * t, sb + 4 * C::x_tile_rows * t + first_col, accumulate);
-          accumulate = 1;
+          for (int r = 0; r < C::x_tile_rows; ++r)
+            tc_copy_scales<PAIR>(sb + 4 * (t * C::x_tile_rows + r), dsb0 + stage * kStageStep + (r * C::k_tiles + t) * (kScaleTile >> 4));
         }
+        const uint64_t da = da0 + stage * kStageStep, db = db0 + stage * kStageStep;
+        const int steps = min(kSteps4, p.k_steps - kb * kSteps4);
+#pragma unroll
+        for (int kk = 0; kk < kSteps4; ++kk) {
+          if (kk < steps) {
+            // blocks of 16: an instruction's four scales are a column; of 32: its two are half of one
+            const int t = BLOCK == 16 ? kk : kk / 2;
+            const uint32_t half = BLOCK == 16 ? 0u : 2u * (kk & 1);
+            const uint32_t idesc = idesc0 | (half << 4) | (half << 29);
+            tc_mma_scaled<BLOCK, PAIR>(tmem_d, da + kk * 2, db + kk * 2, idesc, sa + 4 * t, sb + 4 * C::x_tile_rows * t + first_col,
+                                       kb > kb_first || kk > 0);
+          }
+        }
+        if constexpr (PAIR) tc_commit_pair(empty(stage));
+        else tc_commit(empty(stage));
       }
-      if constexpr (PAIR) tc_commit_pair(empty(stage));
-      else tc_commit(empty(stage));
+      __syncwarp();
+      ++stages_done;
+      if (++place == static_cast<uint32_t>(C::places)) place = 0;
       if (++stage == static_cast<uint32_t>(ES)) { stage = 0; phase ^= 1u; }
     }
-    if constexpr (PAIR) tc_commit_pair(acc_full(buf));
-    else tc_commit(acc_full(buf));
+    if (elect_one()) {
+      if constexpr (PAIR) tc_commit_pair(acc_full(buf));
+      else tc_commit(acc_full(buf));
+    }
+    __syncwarp();
   };
 
   const int warp_e = warp - kFirstEpiWarp;
@@ -488,13 +519,11 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
 
   if constexpr (!SPLIT) {
     if (warp == 0 || warp == kXWarp) {
-      if (lane == 0) {
-        if (warp == kXWarp && !waited) pdl_wait();
-        for (; ok && walk.more(); walk.next()) produce(unit_of(walk), warp == kXWarp);
-        if (warp == 0) drain();
-      }
+      if (warp == kXWarp && !waited) pdl_wait();
+      for (; ok && walk.more(); walk.next()) produce(unit_of(walk), warp == kXWarp);
+      if (warp == 0) drain();
     } else if (warp == 1) {
-      if (lane == 0 && rank == 0)
+      if (rank == 0)
         for (; ok && walk.more(); walk.next(), ++it) multiply(unit_of(walk));
     } else {
       Unit next{};
@@ -510,18 +539,24 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         share_scales();
         walk.next();
         if (walk.more()) ahead();
-        const uint32_t buf = it % C::accumulators;
+        const uint32_t buf = it & 1u;
         // after a wait that ran out the loop goes on without touching the tile: the warps keep meeting
-        ok = ok && mbar_wait(acc_full(buf), (it / C::accumulators) & 1u, abort_flag);
+        ok = ok && mbar_wait(acc_full(buf), (it >> 1) & 1u, abort_flag);
+        // this warp's columns (on a pair: those that the next tile needs) are in registers
+        auto taken = [&]() {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (PAIR) mbar_arrive_leader(mapa_shared(acc_empty(0), 0));
+            else mbar_arrive(acc_empty(buf));
+          }
+        };
         if (ok) {
           tc_fence_after();
-          write_tile<C, BF16>(p, &tm_z, v, sw, bias, lane_base + buf * BT, tmem_base, warp_e, lane, base + C::staging, gen, scales_of(it));
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          if constexpr (PAIR) mbar_arrive_leader(mapa_shared(acc_empty(buf), 0));
-          else mbar_arrive(acc_empty(buf));
+          write_tile<C, BF16, PAIR>(p, &tm_z, v, sw, bias, lane_base + buf * C::second, buf, tmem_base, warp_e, lane, base + C::staging, gen,
+                                    scales_of(it), taken);
+        } else {
+          taken();
         }
         ++it;
       }
@@ -532,17 +567,17 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     for (; walk.more(); walk.next(), ++it) {
       const Unit v = unit_of(walk);
       if (warp == 0 || warp == kXWarp) {
-        if (lane == 0 && ok) {
+        if (ok) {
           if (warp == kXWarp && !waited) { pdl_wait(); waited = true; }
           produce(v, warp == kXWarp);
         }
       } else if (warp == 1) {
-        if (lane == 0 && ok) multiply(v);
+        if (ok) multiply(v);
       } else {
         look_ahead(v);
         share_scales();
-        const uint32_t buf = it % C::accumulators;
-        ok = ok && mbar_wait(acc_full(buf), (it / C::accumulators) & 1u, abort_flag);
+        const uint32_t buf = it & 1u;
+        ok = ok && mbar_wait(acc_full(buf), (it >> 1) & 1u, abort_flag);
         tc_fence_after();
         for (int c = (warp_e >> 2) * C::chunk; ok && c < v.rows; c += C::epi_warps / 4 * C::chunk) {
           uint32_t r[C::chunk];
@@ -576,7 +611,7 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
       __syncwarp();
       cluster_sync_relaxed();          // and has been read by all
     }
-    if (warp == 0 && lane == 0) drain();
+    if (warp == 0) drain();
   }
 
   // a CTA without tiles has waited for nothing yet: what comes after this kernel relies on the preceding one
