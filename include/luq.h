@@ -521,14 +521,15 @@ int luq_quant_e2m1_gemm_grouped(luq_ctx* ctx, const void* d_x, int dtype, int64_
 
 /* ---- a layer of experts --------------------------------------------------------------------------------
  * Which of `experts` experts a token goes to, and with what weights.  logits [rows x experts], fp32 or bf16, row stride
- * ld in elements.  With s = softmax(l) (score 0) or sigmoid(l) (score 1) and c = s + d_bias[e] (d_bias NULL: the order of the
- * logits): the experts are `groups` equal groups, a group's value is the sum of its group_top (1 or 2) best c, the top_groups
+ * ld in elements.  With s = softmax(l) (score 0) or sigmoid(l) (score 1) and c = s + d_bias[e] (d_bias NULL: s, or with one group
+ * the logits themselves): the experts are `groups` equal groups, a group's value is the sum of its group_top (1 or 2) best c, the top_groups
  * best groups stay; of theirs the k largest c are chosen, in descending order, d_chosen [rows x k].  Ties go to the lowest
  * index; values are compared as exact ones (in binary64 where binary32 is too close).  d_weights [rows x k] = scale * s,
  * renormalize: scale * s / sum of the chosen s.  An expert whose logit or bias is -Inf is never chosen: places that are
  * left over hold -1 and weight 0.  A row with NaN or +Inf (or any row, if a bias has) gets -1 and NaN weights and raises
  * LUQ_STATUS_NONFINITE.
- * experts <= LUQ_MAX_GROUPS; 1 <= k <= 32 and k <= experts of top_groups groups; groups <= 32 divides experts. */
+ * experts <= LUQ_MAX_GROUPS; 1 <= k <= 32 and k <= experts of top_groups groups; groups is a power of two up to 32 and divides
+ * experts. */
 int luq_route(luq_ctx* ctx, const void* d_logits, int dtype, int64_t rows, int experts, int64_t ld, int k, int score, const float* d_bias,
               int groups, int top_groups, int group_top, int renormalize, float scale, int32_t* d_chosen, float* d_weights, void* stream);
 /* Gradient of the logits from the weights' (the choice is piecewise constant and has none): with ds_j = scale dw_j, or

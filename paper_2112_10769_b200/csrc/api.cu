@@ -838,7 +838,7 @@ bool move_ok(const luq_ctx* ctx, int dtype, int64_t rows, int64_t cols, int k) {
 
 int luq_route(luq_ctx* ctx, const void* d_logits, int dtype, int64_t rows, int experts, int64_t ld, int k, int score, const float* d_bias,
               int groups, int top_groups, int group_top, int renormalize, float scale, int32_t* d_chosen, float* d_weights, void* stream) {
-  if (!route_ok(ctx, dtype, rows, experts, k, score) || groups < 1 || groups > 32 || experts % groups || top_groups < 1 ||
+  if (!route_ok(ctx, dtype, rows, experts, k, score) || groups < 1 || groups > 32 || (groups & (groups - 1)) || experts % groups || top_groups < 1 ||
       top_groups > groups || (group_top != 1 && group_top != 2) || k > experts / groups * top_groups) return LUQ_ERR_ARG;
   if (!tensor_ok(d_logits, dtype, rows, experts, ld, true) || !floats_ok(d_bias, false) || !ints_ok(d_chosen, rows > 0) ||
       !floats_ok(d_weights, rows > 0)) return LUQ_ERR_ARG;

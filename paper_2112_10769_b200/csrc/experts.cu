@@ -12,6 +12,7 @@
 
 #include <climits>
 #include <type_traits>
+#include <utility>
 
 #include "common.cuh"
 
@@ -39,7 +40,7 @@ __device__ __forceinline__ double warp_sum(double v) {
 // ---- keys: whole numbers in the order of the values they stand for ------------------------------------------------------
 __device__ __forceinline__ uint32_t key_of(float v) {
   const uint32_t b = __float_as_uint(v + 0.0f);                        // (-0 is 0)
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
 __device__ __forceinline__ unsigned long long key_of(double v) {
@@ -49,15 +50,11 @@ __device__ __forceinline__ unsigned long long key_of(double v) {
 __device__ __forceinline__ double value_of(unsigned long long k) {
   return __longlong_as_double(static_cast<long long>(k >> 63 ? k & ~(1ull << 63) : ~k));
 }
-__device__ __forceinline__ uint32_t warp_max(uint32_t k) { return __reduce_max_sync(kFull, k); }
 __device__ __forceinline__ unsigned long long warp_max(unsigned long long k) {
   const uint32_t hi = __reduce_max_sync(kFull, static_cast<uint32_t>(k >> 32));
   const uint32_t lo = __reduce_max_sync(kFull, static_cast<uint32_t>(k >> 32) == hi ? static_cast<uint32_t>(k) : 0u);
   return static_cast<unsigned long long>(hi) << 32 | lo;
 }
-template <typename V> struct KeyOf;
-template <> struct KeyOf<float> { using type = uint32_t; };
-template <> struct KeyOf<double> { using type = unsigned long long; };
 
 // ---- route ---------------------------------------------------------------------------------------------------------------
 struct RouteParams {
@@ -72,200 +69,430 @@ struct RouteParams {
   int* chosen;
   float* weights;
   unsigned int* status;
+  bool vec;                 // a lane's logits are whole pieces of 16 bytes
+  int size, log_groups;     // experts of a group, log2(groups)
+  bool vec_bias;            // so are its biases
 };
 
-__device__ __forceinline__ float minus_inf() { return __int_as_float(0xFF800000u); }
-// scores in 32 and in 64 bits
-__device__ __forceinline__ float sigmoid_of(float l) { return __fdividef(1.0f, 1.0f + expf(-l)); }
-__device__ __forceinline__ double sigmoid_of(double l) { return 1.0 / (1.0 + exp(-l)); }
-
-// Chooses: lane j gets the j-th expert (-1: none was left) and its logit.  Lane L holds the logits of experts L, L + 32, ...
-// Values are of type V; with float the result is the exact one only if true is returned (no two values that decide lie closer
-// than their error).
-template <int VPL, typename V>
-__device__ __forceinline__ bool choose(const RouteParams& p, const float (&l)[VPL], float row_max, int lane, int& mine, float& my_logit) {
-  using Key = typename KeyOf<V>::type;
-  const bool scored = p.bias || p.groups > 1;       // else the logits' order decides, which is exact
-  V s[VPL];                                         // scores plus bias, or logits
-  V err = 0;                                        // what a value may be off by
-  if (!scored) {
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) s[i] = l[i];
+// LANES neighbouring lanes have a row; their maximum, sum, and the mask of those for which `b` holds
+template <int LANES>
+__device__ __forceinline__ uint32_t seg_max(uint32_t v) {
+  if constexpr (LANES == 32) {
+    return __reduce_max_sync(kFull, v);
   } else {
-    V factor = 1;
-    if (!p.sigmoid) {
-      V sum = 0;
 #pragma unroll
-      for (int i = 0; i < VPL; ++i) {
-        if constexpr (std::is_same_v<V, float>) s[i] = expf(l[i] - row_max);
-        else s[i] = exp(static_cast<double>(l[i]) - static_cast<double>(row_max));
-        sum += s[i];
-      }
-      sum = warp_sum(sum);
-      factor = V(1) / sum;
-    }
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      if (p.sigmoid) s[i] = sigmoid_of(static_cast<V>(l[i]));
-      else s[i] *= factor;
-    }
-    if constexpr (std::is_same_v<V, float>) {
-      // Of scores up to s: sigmoid, the exponential's 2 ulp, a sum and a quotient (2 ulp): 6 half steps of 2^-24 s at most, s < 1.
-      // Softmax: the difference of two logits is off by half a step of itself, which moves s by at most 0.37 2^-24 of the
-      // row's largest; the exponential, VPL + 5 sums, quotient, product: VPL + 12 half steps.  The bias adds half a step of
-      // the sum.  Twice that is taken.
-      float largest = 0.0f;
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) largest = fmaxf(largest, s[i]);
-      err = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(largest))) * (p.sigmoid ? 12.0f : 2.0f * (VPL + 13)) * 0x1p-24f;
-    }
-    float bias_top = 0.0f;
-    if (p.bias) {
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) {
-        const int e = lane + 32 * i;
-        if (e < p.experts) { const float b = *(p.bias + e); s[i] += static_cast<V>(b); bias_top = fmaxf(bias_top, fabsf(b) > 3e38f ? 0.0f : fabsf(b)); }
-      }
-    }
-    if constexpr (std::is_same_v<V, float>) err += (1.0f + __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(bias_top)))) * 0x1p-24f;
-#pragma unroll
-    for (int i = 0; i < VPL; ++i)
-      if (lane + 32 * i >= p.experts || l[i] == minus_inf()) s[i] = minus_inf();
+    for (int o = LANES / 2; o; o >>= 1) v = max(v, __shfl_xor_sync(kFull, v, o));
+    return v;
   }
-  uint32_t gone = 0;                                // bit i: expert lane + 32 i cannot be chosen (any more)
-  bool sure = true;
-  // the best of the values for which `take` holds: its key and index
-  auto best_of = [&](auto take, Key& key, int& index) {
-    Key k = key_of(static_cast<V>(minus_inf()));
-    int at = INT_MAX;
+}
+template <int LANES>
+__device__ __forceinline__ float seg_sum(float v) {
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      const Key ki = key_of(s[i]);
-      if (take(i) && ki > k) { k = ki; at = lane + 32 * i; }
-    }
-    key = warp_max(k);
-    index = static_cast<int>(__reduce_min_sync(kFull, static_cast<unsigned>(k == key ? at : INT_MAX)));
-  };
-  if (p.groups > 1) {
-    // lane g keeps group g's value, its key
-    const int size = p.experts / p.groups;
-    V value = minus_inf();
-    for (int g = 0; g < p.groups; ++g) {
-      Key k1;
-      int at;
-      best_of([&](int i) { return (lane + 32 * i) / size == g; }, k1, at);
-      V sum = value_of(k1);
-      if (p.group_top == 2 && at != INT_MAX) {
-        Key k2;
-        int at2;
-        best_of([&](int i) { return (lane + 32 * i) / size == g && lane + 32 * i != at; }, k2, at2);
-        if (at2 != INT_MAX) sum += value_of(k2);
-      }
-      if (lane == g) value = sum;
-    }
-    uint32_t stay = 0;
-    bool out = false;
-    V last = 0;
-    for (int h = 0; h <= p.top_groups && h < p.groups; ++h) {
-      const Key k = lane < p.groups && !out ? key_of(value) : 0;
-      const Key best = warp_max(k);
-      const int g = static_cast<int>(__reduce_min_sync(kFull, static_cast<unsigned>(k == best && lane < p.groups && !out ? lane : INT_MAX)));
-      const V v = value_of(best);
-      if (h == p.top_groups) {
-        // the first group that goes: is it clear of the last one that stays?
-        if (std::is_same_v<V, float> && v > minus_inf() && !(last - v > 4 * err + (fabs(last) + 1) * V(0x1p-22f))) sure = false;
-      } else {
-        last = v;
-        stay |= 1u << g;
-        if (lane == g) out = true;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < VPL; ++i)
-      if (!(stay >> min((lane + 32 * i) / size, 31) & 1)) gone |= 1u << i;
-    if (!p.bias) {                                  // scores are in the order of the logits
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) s[i] = l[i];
-    }
-  }
-  mine = -1;
-  my_logit = minus_inf();
-  V before = 0;
-  float before_logit = 0.0f, before_bias = 0.0f;
-  for (int j = 0; j <= p.k; ++j) {
-    if (j == p.k && !(std::is_same_v<V, float> && p.bias)) break;      // one more, to see how close it is
-    Key key;
-    int e;
-    best_of([&](int i) { return !(gone >> i & 1); }, key, e);
-    if (e == INT_MAX) break;
-    float le = 0.0f;
-#pragma unroll
-    for (int i = 0; i < VPL; ++i)
-      if (e >> 5 == i) le = l[i];
-    le = __shfl_sync(kFull, le, e & 31);
-    if (std::is_same_v<V, float> && p.bias) {
-      const float be = *(p.bias + e);
-      const V v = value_of(key);
-      // (equal logits and biases have equal values, of which the lower index comes first)
-      if (j > 0 && !(before - v > 2 * err) && !(le == before_logit && be == before_bias)) sure = false;
-      before = v; before_logit = le; before_bias = be;
-    }
-    if (j < p.k) {
-      if (lane == j) { mine = e; my_logit = le; }
-      if (lane == (e & 31)) gone |= 1u << (e >> 5);
-    }
-  }
-  return sure;
+  for (int o = LANES / 2; o; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+  return v;
+}
+template <int LANES>
+__device__ __forceinline__ uint32_t seg_ballot(bool b, int lane) {
+  const uint32_t all = __ballot_sync(kFull, b);
+  if constexpr (LANES == 32) return all;
+  else return all >> (lane / LANES * LANES) & ((1u << LANES) - 1u);
 }
 
+__device__ __forceinline__ float minus_inf() { return __int_as_float(0xFF800000u); }
+__device__ __forceinline__ bool unusable(float v) { return !(v <= 3.402823466e38f); }       // NaN or +Inf
+__device__ __forceinline__ float sigmoid_of(float l) { return __fdiv_rn(1.0f, 1.0f + expf(-l)); }
+
+// VPL neighbouring elements of a row from `e0` on, of which the first n are there; -Inf for the others
 template <typename T, int VPL>
+__device__ __forceinline__ void load_lane(const T* row, int e0, int n, bool vec, float (&l)[VPL]) {
+  constexpr int kPiece = 16 / static_cast<int>(sizeof(T));
+  if constexpr (VPL >= kPiece) {
+    if (vec) {
+#pragma unroll
+      for (int i = 0; i < VPL; i += kPiece) {
+        uint4 u = make_uint4(0, 0, 0, 0);
+        const bool in = i < n;
+        if (in) u = *reinterpret_cast<const uint4*>(row + e0 + i);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (sizeof(T) == 4) {
+            l[i + j] = in ? __uint_as_float(w[j]) : minus_inf();
+          } else {
+            l[i + 2 * j] = in ? __uint_as_float(w[j] << 16) : minus_inf();
+            l[i + 2 * j + 1] = in ? __uint_as_float(w[j] & 0xFFFF0000u) : minus_inf();
+          }
+        }
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < VPL; ++i) l[i] = i < n ? load1(row + e0 + i) : minus_inf();
+}
+
+// Batcher's odd-even merge sort, largest first.  Its exchanges are a table made by the compiler and written out one by one: as nested
+// loops they were not all unrolled, and the keys lay in local memory.
+template <int N>
+struct Network {
+  int low[N * N / 2 + 1] = {}, high[N * N / 2 + 1] = {}, count = 0;
+  constexpr Network() {
+    for (int p = 1; p < N; p *= 2)
+      for (int k = p; k >= 1; k /= 2)
+        for (int j = k % p; j + k < N; j += 2 * k)
+          for (int i = 0; i < k; ++i)
+            if (i + j + k < N && (i + j) / (2 * p) == (i + j + k) / (2 * p)) { low[count] = i + j; high[count++] = i + j + k; }
+  }
+};
+template <int N>
+__device__ constexpr Network<N> kNetwork{};
+template <int N, int... I>
+__device__ __forceinline__ void sort_keys(uint32_t (&v)[N], std::integer_sequence<int, I...>) {
+  auto exchange = [](uint32_t& a, uint32_t& b) {
+    const uint32_t most = max(a, b);
+    b = min(a, b);
+    a = most;
+  };
+  (exchange(v[std::integral_constant<int, kNetwork<N>.low[I]>::value], v[std::integral_constant<int, kNetwork<N>.high[I]>::value]), ...);
+}
+template <int N>
+__device__ __forceinline__ void sort_keys(uint32_t (&v)[N]) {
+  sort_keys(v, std::make_integer_sequence<int, Network<N>{}.count>{});
+}
+
+// Where binary32 leaves a choice open (two values that decide lie closer than their errors: some rows in a thousand), it is made
+// again in binary64, by three functions that a warp's rows enter together; each reads the logits again, so that nothing is held for
+// their sake.  One such row at a launch's end is all of its tail, so the frequent ones are quick: the groups' values from a lane's
+// own experts, and the order of the places from the chosen experts' values, a lane each.  The third makes the whole choice.
+
+// exp(l - top) of a row, summed
+template <typename T, int LANES>
+__device__ __forceinline__ double exact_sum(const RouteParams& p, const T* row, int ls, double& top) {
+  double most = -INFINITY, sum = 0.0;
+  for (int e = ls; e < p.experts; e += LANES) most = fmax(most, static_cast<double>(load1(row + e)));
+#pragma unroll
+  for (int o = LANES / 2; o; o >>= 1) most = fmax(most, __shfl_xor_sync(kFull, most, o));
+  for (int e = ls; e < p.experts; e += LANES) sum += exp(static_cast<double>(load1(row + e)) - most);
+#pragma unroll
+  for (int o = LANES / 2; o; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
+  top = most;
+  return sum;
+}
+__device__ __forceinline__ double exact_value(const RouteParams& p, double l, int e, double top, double sum) {
+  if (l == -INFINITY) return l;
+  const double s = p.sigmoid ? 1.0 / (1.0 + exp(-l)) : exp(l - top) / sum;
+  return p.bias ? s + static_cast<double>(*(p.bias + e)) : s;
+}
+
+// does this lane's group stay?
+template <typename T, int LANES, int VPL>
+__device__ __noinline__ bool exact_groups(const RouteParams& p, const T* row, int e0, int n, int per_group) {
+  const int ls = threadIdx.x & (LANES - 1);
+  double top = 0.0, sum = 1.0, first = -INFINITY, second = -INFINITY;
+  if (!p.sigmoid) sum = exact_sum<T, LANES>(p, row, ls, top);
+#pragma unroll 4
+  for (int i = 0; i < VPL; ++i) {
+    const double c = i < n ? exact_value(p, load1(row + e0 + i), e0 + i, top, sum) : -INFINITY;
+    second = fmax(second, fmin(first, c));
+    first = fmax(first, c);
+  }
+  for (int o = 1; o < per_group; o *= 2) {
+    const double f = __shfl_xor_sync(kFull, first, o), g = __shfl_xor_sync(kFull, second, o);
+    second = fmax(fmin(first, f), fmax(second, g));
+    first = fmax(first, f);
+  }
+  const double mine = p.group_top == 2 && second > -INFINITY ? first + second : first;
+  int better = 0;
+  for (int g = 0; g < p.groups; ++g) {
+    const double other = __shfl_sync(kFull, mine, g * per_group, LANES);
+    better += other > mine || (other == mine && g < ls / per_group);
+  }
+  return better < p.top_groups;
+}
+
+// the experts found (lane j has the j-th, -1: none; every lane the one beyond them, -1: it plays no part) in exact order
+template <typename T, int LANES>
+__device__ __noinline__ int exact_places(const RouteParams& p, const T* row, int mine, int extra) {
+  const int ls = threadIdx.x & (LANES - 1);
+  double top = 0.0, sum = 1.0;
+  const bool scored = p.bias || p.groups > 1;
+  if (scored && !p.sigmoid) sum = exact_sum<T, LANES>(p, row, ls, top);
+  auto value = [&](int e) {
+    const double l = e >= 0 ? static_cast<double>(load1(row + e)) : -INFINITY;
+    return scored ? exact_value(p, l, e, top, sum) : l;
+  };
+  const double c = value(mine), cx = value(extra);
+  auto before = [](double ca, int ea, double cb, int eb) { return ea >= 0 && (ca > cb || (ca == cb && ea < eb)); };
+  int rank = before(cx, extra, c, mine), rank_x = 0, at = -1;
+  for (int i = 0; i < LANES; ++i) {
+    const double ci = __shfl_sync(kFull, c, i, LANES);
+    const int ei = __shfl_sync(kFull, mine, i, LANES);
+    rank += before(ci, ei, c, mine);
+    rank_x += before(ci, ei, cx, extra);
+  }
+  for (int i = 0; i < LANES; ++i) {
+    const int ei = __shfl_sync(kFull, mine, i, LANES), ri = __shfl_sync(kFull, rank, i, LANES);
+    if (ei >= 0 && ri == ls) at = ei;
+  }
+  return extra >= 0 && rank_x == ls ? extra : at;
+}
+
+// the choice by a whole warp for one row: lane j gets the j-th expert or -1
+template <typename T>
+__device__ __noinline__ int choose_exact(const RouteParams& p, const T* row) {
+  const int lane = threadIdx.x & 31;
+  const bool scored = p.bias || p.groups > 1;
+  const double none = -INFINITY;
+  double top = 0.0, sum = 1.0, values[LUQ_MAX_GROUPS / 32];      // of experts `lane`, `lane` + 32, ...
+  if (scored && !p.sigmoid) sum = exact_sum<T, 32>(p, row, lane, top);
+#pragma unroll 4
+  for (int i = 0; i < (p.experts + 31) / 32; ++i) {
+    const int e = lane + 32 * i;
+    const double l = e < p.experts ? static_cast<double>(load1(row + e)) : none;
+    values[i] = scored ? exact_value(p, l, e, top, sum) : l;
+  }
+  // the best of experts `from` .. `to` - 1 in the groups of `stay` that comes after (v, e) in the order; e = -1: there is none
+  const int size = p.experts / p.groups;
+  auto next = [&](int from, int to, uint32_t stay, double& v, int& e) {
+    unsigned long long best = key_of(none);
+    int at = INT_MAX;
+    for (int i = from + ((lane - from) & 31); i < to; i += 32) {
+      const double vi = values[i >> 5];
+      const unsigned long long ki = key_of(vi);
+      if (ki > best && (vi < v || (vi == v && i > e)) && stay >> (i / size) & 1) { best = ki; at = i; }
+    }
+    const unsigned long long all = warp_max(best);
+    const int index = static_cast<int>(__reduce_min_sync(kFull, static_cast<unsigned>(best == all ? at : INT_MAX)));
+    v = value_of(all);
+    e = index == INT_MAX ? -1 : index;
+  };
+  uint32_t stay = kFull;
+  if (p.groups > 1) {
+    double mine = none;
+    for (int g = 0; g < p.groups; ++g) {
+      double v = INFINITY, w;
+      int e = -1;
+      next(g * size, (g + 1) * size, kFull, v, e);
+      w = v;
+      if (p.group_top == 2 && e >= 0) {
+        next(g * size, (g + 1) * size, kFull, w, e);
+        w = e >= 0 ? v + w : v;
+      }
+      if (lane == g) mine = w;
+    }
+    stay = 0;
+    unsigned long long k = lane < p.groups ? key_of(mine) : 0ull;
+    for (int h = 0; h < p.top_groups; ++h) {
+      const int g = __ffs(__ballot_sync(kFull, warp_max(k) == k && k > 0)) - 1;
+      if (g < 0) break;
+      stay |= 1u << g;
+      if (lane == g) k = 0;
+    }
+  }
+  double v = INFINITY;
+  int e = -1, mine = -1;
+  for (int j = 0; j < p.k; ++j) {
+    next(0, p.experts, stay, v, e);
+    if (e < 0) break;
+    if (lane == j) mine = e;
+  }
+  return mine;
+}
+
+// LANES lanes have a row, a lane VPL neighbouring experts of a group, groups the same number of lanes each: so a lower lane has
+// lower experts.  A lane sorts its keys, whose lowest bits are the expert's place in the lane; the k rounds then are a maximum
+// over the lanes' first keys, the lowest lane that has it, and that lane's shift.  What bounds it is instructions.
+template <typename T, int LANES, int VPL>
 __global__ void __launch_bounds__(128) route_kernel(const RouteParams p) {
+  constexpr uint32_t kPlace = VPL - 1;
+  constexpr int kLogLanes = LANES == 32 ? 5 : LANES == 16 ? 4 : 3;
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const long long r = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-  if (r >= p.rows) return;
+  const int lane = threadIdx.x & 31, ls = lane % LANES;
+  const long long given = (static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 5)) * (32 / LANES) + lane / LANES;
+  if (given - lane / LANES >= p.rows) return;                  // (a whole warp)
+  const long long r = given < p.rows ? given : p.rows - 1;     // (the lanes of rows that are not there take part)
   const T* const row = static_cast<const T*>(p.logits) + r * p.ld;
-  float l[VPL], top = minus_inf();
+  const int size = p.size, per_group = LANES >> p.log_groups;
+  const int in_group = (ls & (per_group - 1)) * VPL, group = ls >> (kLogLanes - p.log_groups);
+  const int e0 = group * size + in_group, n = min(max(size - in_group, 0), VPL);
+  float l[VPL];
+  load_lane<T, VPL>(row, e0, n, p.vec, l);
   bool bad = false;
 #pragma unroll
-  for (int i = 0; i < VPL; ++i) {
-    const int e = lane + 32 * i;
-    l[i] = e < p.experts ? load1(row + e) : minus_inf();
-    bad |= !(l[i] <= 3.402823466e38f);
-    if (p.bias && e < p.experts) bad |= !(*(p.bias + e) <= 3.402823466e38f);
-    top = fmaxf(top, l[i]);
-  }
-  top = value_of(warp_max(key_of(top)));
-  int mine = -1;
-  float logit = minus_inf(), w = 0.0f;
-  if (__any_sync(kFull, bad)) {
-    w = __int_as_float(0x7FC00000);
-    if (lane == 0) atomicOr(p.status, LUQ_STATUS_NONFINITE);
-  } else if (top > minus_inf()) {
-    if (!choose<VPL, float>(p, l, top, lane, mine, logit)) choose<VPL, double>(p, l, top, lane, mine, logit);
-    if (p.sigmoid) {
-      w = mine >= 0 ? sigmoid_of(logit) : 0.0f;
-    } else {
-      // renormalised: relative to the largest chosen logit, so that they cannot all vanish
-      const float shift = p.renormalize ? value_of(warp_max(key_of(mine >= 0 ? logit : minus_inf()))) : top;
-      w = mine >= 0 ? expf(logit - shift) : 0.0f;
-      if (!p.renormalize) {
-        float sum = 0.0f;
+  for (int i = 0; i < VPL; ++i) bad |= unusable(l[i]);
+  const bool scored = p.bias || p.groups > 1;
+  // softmax: the row's largest logit, and the sum of the exponentials where it plays a part
+  float top = minus_inf(), sum = 0.0f;
+  float c[VPL];
+  if (!p.sigmoid) {
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) sum += expf(l[i] - top);
-        w /= warp_sum(sum);
+    for (int i = 0; i < VPL; ++i) top = fmaxf(top, l[i]);
+    top = value_of(seg_max<LANES>(key_of(top)));
+    if (scored || !p.renormalize) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) {
+        c[i] = l[i] > minus_inf() ? expf(l[i] - top) : 0.0f;
+        sum += c[i];
       }
+      sum = seg_sum<LANES>(sum);
     }
-    if (p.renormalize) {
-      const float sum = warp_sum(w);
-      w = sum > 0.0f ? w / sum : 0.0f;
-    }
-    w *= p.scale;
   }
-  if (lane < p.k) {
-    p.chosen[r * p.k + lane] = mine;
-    p.weights[r * p.k + lane] = w;
+  float err = 0.0f;                                    // what a value may be off by
+  uint32_t keys[VPL];
+  if (!scored) {
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) keys[i] = l[i] > minus_inf() ? (key_of(l[i]) & ~kPlace) | (kPlace - i) : 0u;
+  } else {
+    if (p.sigmoid) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) c[i] = __fdividef(1.0f, 1.0f + __expf(-l[i]));
+      // The exponential is off by (|l| + 4) half steps of itself, which moves s by s (1 - s) (|l| + 4) <= 1.3 of them, sum and
+      // quotient add 3; taken twice
+      err = 9.0f * 0x1p-24f;
+    } else {
+      const float factor = sum > 0.0f ? __fdividef(1.0f, sum) : 0.0f;
+      float largest = 0.0f;
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) {
+        c[i] *= factor;
+        largest = fmaxf(largest, c[i]);
+      }
+      // The exponential of d = l - top is off by (|d| + 4) half steps, and |d| exp(d) <= 0.37: 5 of the row's largest; the sum
+      // VPL + 5, quotient and product 4; taken twice
+      err = __uint_as_float(seg_max<LANES>(__float_as_uint(largest))) * (2.0f * (VPL + 14)) * 0x1p-24f;
+    }
+    if (p.bias) {
+      float b[VPL];
+      load_lane<float, VPL>(p.bias, e0, n, p.vec_bias, b);
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) c[i] += b[i];
+      // (a sum of finite numbers is a number; where the bias is not finite, neither is the sum)
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) bad |= unusable(c[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) keys[i] = fminf(l[i], c[i]) > minus_inf() ? (key_of(c[i]) & ~kPlace) | (kPlace - i) : 0u;
+  }
+  sort_keys<VPL>(keys);
+  // how far apart two values have to be: their errors, the bias's rounding, and the bits that hold the place
+  auto clear = [&](float more, float less, float errors) {
+    return more - less > errors * err + (fabsf(more) + fabsf(less)) * (VPL + 1) * 0x1p-23f;
+  };
+  bool open = false;                                   // (of this lane's row)
+  bad = seg_ballot<LANES>(bad, lane) != 0;
+  if (p.groups > 1) {
+    uint32_t first = keys[0], second = VPL > 1 ? keys[VPL > 1 ? 1 : 0] : 0u;
+    for (int o = 1; o < per_group; o *= 2) {
+      const uint32_t f = __shfl_xor_sync(kFull, first, o), g = __shfl_xor_sync(kFull, second, o);
+      second = max(min(first, f), max(second, g));
+      first = max(first, f);
+    }
+    const float both = (first ? value_of(first & ~kPlace) : minus_inf()) + (p.group_top == 2 && second ? value_of(second & ~kPlace) : 0.0f);
+    const uint32_t mine = key_of(both);
+    int better = 0;
+    for (int g = 0; g < p.groups; ++g) {
+      const uint32_t other = __shfl_sync(kFull, mine, g * per_group, LANES);
+      better += other > mine || (other == mine && g < group);
+    }
+    bool stays = better < p.top_groups;
+    // (a complement's maximum is the minimum)
+    const float least = value_of(~seg_max<LANES>(stays ? ~mine : 0u)), most = value_of(seg_max<LANES>(stays ? key_of(minus_inf()) : mine));
+    const bool close = most > minus_inf() && !clear(least, most, 4.0f) && !bad;
+    if (__any_sync(kFull, close)) {
+      const bool exact = exact_groups<T, LANES, VPL>(p, row, e0, n, per_group);
+      if (close) stays = exact;
+    }
+    if (!stays) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) keys[i] = 0u;
+    }
+  }
+  int mine = -1, extra = -1;
+  uint32_t mine_key = 0, last = 0;                     // the value of my place, and of the one after the last
+  auto round = [&](uint32_t& best, int& e) {
+    const uint32_t head = keys[0] & ~kPlace;           // (the places of different lanes do not compare)
+    best = seg_max<LANES>(head);
+    const int from = __ffs(seg_ballot<LANES>(head == best, lane)) - 1;
+    e = __shfl_sync(kFull, e0 + static_cast<int>(kPlace - (keys[0] & kPlace)), from, LANES);
+    if (ls == from) {
+#pragma unroll
+      for (int i = 0; i + 1 < VPL; ++i) keys[i] = keys[i + 1];
+      keys[VPL - 1] = 0u;
+    }
+  };
+  for (int j = 0; j < p.k; ++j) {
+    uint32_t best;
+    int e;
+    round(best, e);
+    if (ls == j) { mine_key = best; mine = best ? e : -1; }
+  }
+  round(last, extra);                                  // one more than wanted, to see how close it is
+  // Is a place close to the next?  Equal logits and biases have equal values, of which the lower index comes first.
+  auto close = [&](uint32_t a, uint32_t b) { return b && !(scored ? clear(value_of(a), value_of(b), 2.0f) : a > b); };
+  auto same = [&](int a, int b) { return load1(row + a) == load1(row + b) && (!p.bias || *(p.bias + a) == *(p.bias + b)); };
+  const uint32_t down_key = __shfl_down_sync(kFull, mine_key, 1, LANES);
+  const int down = __shfl_down_sync(kFull, mine, 1, LANES);
+  const bool end = ls == p.k - 1;
+  const bool near = ls < p.k && close(mine_key, end ? last : down_key);
+  bool beyond = false;
+  if (__any_sync(kFull, near)) {
+    bool differs = near && !same(mine, end ? extra : down);
+    open |= seg_ballot<LANES>(differs, lane) != 0;
+    // the last place is not clear of what comes next: it plays a part, or, equal, leads to what comes after it
+    bool more = seg_ballot<LANES>(near && end, lane) != 0;
+    const bool part = seg_ballot<LANES>(differs && end, lane) != 0;
+    uint32_t from_key = last;
+    int from = extra;
+    while (__any_sync(kFull, more)) {
+      uint32_t best;
+      int e;
+      round(best, e);
+      more = more && close(from_key, best);
+      if (more && (part || !same(from, e))) { open = beyond = true; more = false; }
+      from_key = best;
+      from = e;
+    }
+    if (!part) extra = -1;
+  }
+  open &= !bad;
+  if (__any_sync(kFull, open)) {
+    const int exact = exact_places<T, LANES>(p, row, mine, extra);
+    if (open) mine = exact;
+    uint32_t left = __ballot_sync(kFull, open && beyond);       // more values in a row that binary32 does not tell apart
+    while (left) {
+      const int first = (__ffs(left) - 1) / LANES * LANES;     // its row's first lane
+      const long long row_at = __shfl_sync(kFull, r, first);
+      const int all = choose_exact<T>(p, static_cast<const T*>(p.logits) + row_at * p.ld);
+      const int at = __shfl_sync(kFull, all, ls);
+      if (lane / LANES * LANES == first) mine = at;
+      left &= LANES == 32 ? 0u : ~(((1u << (LANES & 31)) - 1u) << first);
+    }
+  }
+  if (ls >= p.k) mine = -1;
+  const float logit = mine >= 0 ? load1(row + mine) : minus_inf();
+  float w;
+  if (p.sigmoid) {
+    w = mine >= 0 ? sigmoid_of(logit) : 0.0f;
+  } else {
+    // renormalised: relative to the largest chosen logit, so that they cannot all vanish
+    const float shift = p.renormalize ? value_of(seg_max<LANES>(key_of(logit))) : top;
+    w = mine >= 0 ? expf(logit - shift) : 0.0f;
+    if (!p.renormalize) w = mine >= 0 ? w / sum : 0.0f;
+  }
+  if (p.renormalize) {
+    const float chosen = seg_sum<LANES>(w);
+    w = chosen > 0.0f ? w / chosen : 0.0f;
+  }
+  w *= p.scale;
+  if (bad) {
+    mine = -1;
+    w = __int_as_float(0x7FC00000);
+    if (ls == 0) atomicOr(p.status, LUQ_STATUS_NONFINITE);
+  }
+  if (ls < p.k && given < p.rows) {
+    p.chosen[r * p.k + ls] = mine;
+    p.weights[r * p.k + ls] = w;
   }
 }
 
@@ -279,59 +506,102 @@ struct RouteBwdParams {
   const int* chosen;
   void* dlogits;
   long long ld_d;
+  bool vec;
 };
 
-// A warp has a row.  Renormalised scores and sigmoids have gradients at the chosen experts only; the softmax's other experts
-// get -s_e sum_j s_j ds_j.
-template <typename T>
+template <typename T, int VPL>
+__device__ __forceinline__ void store_lane(T* row, int e0, int n, bool vec, const float (&v)[VPL]) {
+  constexpr int kPiece = 16 / static_cast<int>(sizeof(T));
+  if constexpr (VPL >= kPiece) {
+    if (vec) {
+#pragma unroll
+      for (int i = 0; i < VPL; i += kPiece) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (sizeof(T) == 4) {
+            w[j] = __float_as_uint(v[i + j]);
+          } else {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[i + 2 * j], v[i + 2 * j + 1]);
+            w[j] = *reinterpret_cast<const uint32_t*>(&h);
+          }
+        }
+        if (i < n) *reinterpret_cast<uint4*>(row + e0 + i) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < VPL; ++i)
+    if (i < n) store1(row + e0 + i, v[i]);
+}
+
+// LANES lanes have a row, a lane VPL neighbouring experts.  Renormalised scores and sigmoids have gradients at the chosen experts
+// only; the softmax's other experts get -s_e sum_j s_j ds_j.
+template <typename T, int LANES, int VPL>
 __global__ void __launch_bounds__(128) route_bwd_kernel(const RouteBwdParams p) {
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const long long r = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-  if (r >= p.rows) return;
+  const int lane = threadIdx.x & 31, ls = lane % LANES;
+  const long long given = (static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 5)) * (32 / LANES) + lane / LANES;
+  if (given - lane / LANES >= p.rows) return;                  // (a whole warp)
+  const bool there = given < p.rows;
+  const long long r = there ? given : p.rows - 1;
   const T* const row = static_cast<const T*>(p.logits) + r * p.ld;
   T* const out = static_cast<T*>(p.dlogits) + r * p.ld_d;
-  int e = lane < p.k ? p.chosen[r * p.k + lane] : -1;
+  const int e0 = ls * VPL, n = min(max(p.experts - e0, 0), VPL);
+  int e = ls < p.k ? p.chosen[r * p.k + ls] : -1;
   if (e >= p.experts) e = -1;
-  const float dw = e >= 0 ? p.dweights[r * p.k + lane] : 0.0f;
+  const float dw = e >= 0 ? p.dweights[r * p.k + ls] : 0.0f;
   const float l = e >= 0 ? load1(row + e) : minus_inf();
   const bool whole = !p.sigmoid && !p.renormalize;       // every logit has a gradient
-  float top = minus_inf(), sum = 0.0f;
+  float v[VPL], top = minus_inf(), sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < VPL; ++i) v[i] = 0.0f;
   if (whole) {
-    for (int c = lane; c < p.experts; c += 32) top = fmaxf(top, load1(row + c));
-    top = value_of(warp_max(key_of(top)));
-    if (top > minus_inf())
-      for (int c = lane; c < p.experts; c += 32) sum += expf(load1(row + c) - top);
-    sum = warp_sum(sum);
+    load_lane<T, VPL>(row, e0, n, p.vec, v);
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) top = fmaxf(top, v[i]);
+    top = value_of(seg_max<LANES>(key_of(top)));
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+      v[i] = v[i] == minus_inf() ? 0.0f : expf(v[i] - top);
+      sum += v[i];
+    }
+    sum = seg_sum<LANES>(sum);
   } else if (!p.sigmoid) {
-    top = value_of(warp_max(key_of(l)));
+    top = value_of(seg_max<LANES>(key_of(l)));
   }
   float s = 0.0f;                                        // my score, or its share of the chosen ones' sum
-  if (e >= 0 && l > minus_inf()) s = p.sigmoid ? sigmoid_of(l) : expf(l - top);
-  if (whole && sum > 0.0f) s /= sum;
+  if (e >= 0 && l != minus_inf()) s = p.sigmoid ? sigmoid_of(l) : expf(l - top);
+  const float inverse = sum > 0.0f ? 1.0f / sum : sum;   // (NaN stays)
+  if (whole) s *= inverse;
   float d = p.scale * dw;
   if (p.renormalize) {
-    const float total = warp_sum(s);
-    s = total > 0.0f ? s / total : 0.0f;
-    d -= warp_sum(d * s);
+    const float total = seg_sum<LANES>(s);
+    s = total == 0.0f ? 0.0f : s / total;
+    d -= seg_sum<LANES>(d * s);
   }
-  const float along = whole ? warp_sum(s * d) : 0.0f;
-  const float term = p.sigmoid ? d * s * (l > minus_inf() ? sigmoid_of(-l) : 0.0f) : s * d;
+  const float along = whole ? seg_sum<LANES>(s * d) : 0.0f;
+  const float term = p.sigmoid ? d * s * (l != minus_inf() ? sigmoid_of(-l) : 0.0f) : s * d;
   // an expert that stands in several places gets the sum of theirs
   float mine = 0.0f;
   bool first = e >= 0;
   for (int j = 0; j < p.k; ++j) {
-    const int ej = __shfl_sync(kFull, e, j);
-    const float tj = __shfl_sync(kFull, term, j);
+    const int ej = __shfl_sync(kFull, e, j, LANES);
+    const float tj = __shfl_sync(kFull, term, j, LANES);
     if (ej == e) {
       mine += tj;
-      first &= j >= lane;
+      first &= j >= ls;
     }
   }
-  for (int c = lane; c < p.experts; c += 32) store1(out + c, whole && sum > 0.0f ? -along * (expf(load1(row + c) - top) / sum) : 0.0f);
+  if (whole) {
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) v[i] *= -along * inverse;
+  }
+  if (there) store_lane<T, VPL>(out, e0, n, p.vec, v);
   __syncwarp();
-  if (first) store1(out + e, whole ? mine - s * along : mine);
+  if (there && first) store1(out + e, whole ? mine - s * along : mine);
 }
 
 // ---- order ---------------------------------------------------------------------------------------------------------------
@@ -605,18 +875,35 @@ int done(luq_ctx* ctx, cudaError_t e) {
   return static_cast<int>(e);
 }
 
-template <typename T, int VPL>
-int launch_route(luq_ctx* ctx, const RouteParams& p, cudaStream_t st) {
-  return done(ctx, luq_launch_kernel(route_kernel<T, VPL>, static_cast<int>((p.rows + 3) / 4), 128, 0, st, LUQ_LAUNCH_EARLY, 1, p));
+// The lanes that share a row: as few as hold its experts 8 each, its places and groups.  (16 experts a lane: as quick for many rows,
+// slower for one.)
+int route_lanes(int experts, int k, int groups) {
+  const int least = k > groups ? k : groups;
+  return experts <= 64 && least <= 8 ? 8 : experts <= 128 && least <= 16 ? 16 : 32;
 }
-template <typename T>
-int launch_route_width(luq_ctx* ctx, const RouteParams& p, cudaStream_t st) {
-  if (p.experts <= 32) return launch_route<T, 1>(ctx, p, st);
-  if (p.experts <= 64) return launch_route<T, 2>(ctx, p, st);
-  if (p.experts <= 128) return launch_route<T, 4>(ctx, p, st);
-  if (p.experts <= 256) return launch_route<T, 8>(ctx, p, st);
-  if (p.experts <= 512) return launch_route<T, 16>(ctx, p, st);
-  return launch_route<T, 32>(ctx, p, st);
+template <typename T, int LANES, int VPL, typename P>
+int launch_route(luq_ctx* ctx, P p, cudaStream_t st) {
+  const int blocks = static_cast<int>((p.rows * LANES + 127) / 128);
+  if constexpr (std::is_same_v<P, RouteParams>) return done(ctx, luq_launch_kernel(route_kernel<T, LANES, VPL>, blocks, 128, 0, st, LUQ_LAUNCH_EARLY, 1, p));
+  else return done(ctx, luq_launch_kernel(route_bwd_kernel<T, LANES, VPL>, blocks, 128, 0, st, LUQ_LAUNCH_EARLY, 1, p));
+}
+// per_lane: experts that a lane has to hold
+template <typename T, typename P>
+int launch_route_lanes(luq_ctx* ctx, const P& p, int lanes, int per_lane, cudaStream_t st) {
+  if (lanes == 8) {
+    if (per_lane <= 1) return launch_route<T, 8, 1>(ctx, p, st);
+    if (per_lane <= 2) return launch_route<T, 8, 2>(ctx, p, st);
+    if (per_lane <= 4) return launch_route<T, 8, 4>(ctx, p, st);
+    return launch_route<T, 8, 8>(ctx, p, st);
+  }
+  if (lanes == 16) {
+    if (per_lane <= 4) return launch_route<T, 16, 4>(ctx, p, st);
+    return launch_route<T, 16, 8>(ctx, p, st);
+  }
+  if (per_lane <= 2) return launch_route<T, 32, 2>(ctx, p, st);
+  if (per_lane <= 8) return launch_route<T, 32, 8>(ctx, p, st);
+  if (per_lane <= 16) return launch_route<T, 32, 16>(ctx, p, st);
+  return launch_route<T, 32, 32>(ctx, p, st);
 }
 
 MoveParams move_params(const luq_ctx* ctx, const luq_move_args& a, bool& vec) {
@@ -639,17 +926,26 @@ MoveParams move_params(const luq_ctx* ctx, const luq_move_args& a, bool& vec) {
 
 }  // namespace
 
+// rows whose lanes' elements are whole pieces of 16 bytes: `size` elements from one lane's group to the next
+static bool route_vec(const void* p, int64_t ld, int size, int esize) {
+  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * esize % 16 == 0 && size * esize % 16 == 0;
+}
+
 int luq_launch_route(luq_ctx* ctx, const luq_route_args& a, cudaStream_t st) {
-  RouteParams p{a.logits, a.rows, a.ld, a.experts, a.k, a.sigmoid, a.bias, a.groups, a.top_groups, a.group_top, a.renormalize, a.scale,
-                a.chosen, a.weights, ctx->d_status};
-  return a.dtype == LUQ_BF16 ? launch_route_width<__nv_bfloat16>(ctx, p, st) : launch_route_width<float>(ctx, p, st);
+  const int esize = a.dtype == LUQ_BF16 ? 2 : 4, size = a.experts / a.groups;
+  const RouteParams p{a.logits, a.rows, a.ld, a.experts, a.k, a.sigmoid, a.bias, a.groups, a.top_groups, a.group_top, a.renormalize, a.scale,
+                      a.chosen, a.weights, ctx->d_status, route_vec(a.logits, a.ld, size, esize), size, __builtin_ctz(a.groups),
+                      a.bias && (reinterpret_cast<uintptr_t>(a.bias) & 15u) == 0 && size % 4 == 0};
+  const int lanes = route_lanes(a.experts, a.k, a.groups), per_group = lanes / a.groups, held = (size + per_group - 1) / per_group;
+  return a.dtype == LUQ_BF16 ? launch_route_lanes<__nv_bfloat16>(ctx, p, lanes, held, st) : launch_route_lanes<float>(ctx, p, lanes, held, st);
 }
 
 int luq_launch_route_bwd(luq_ctx* ctx, const luq_route_args& a, const float* dweights, void* dlogits, int64_t ld_d, cudaStream_t st) {
-  RouteBwdParams p{dweights, a.logits, a.rows, a.ld, a.experts, a.k, a.sigmoid, a.renormalize, a.scale, a.chosen, dlogits, ld_d};
-  const int blocks = static_cast<int>((a.rows + 3) / 4);
-  return done(ctx, luq_launch_kernel(a.dtype == LUQ_BF16 ? route_bwd_kernel<__nv_bfloat16> : route_bwd_kernel<float>, blocks, 128, 0, st,
-                                     LUQ_LAUNCH_EARLY, 1, p));
+  const int esize = a.dtype == LUQ_BF16 ? 2 : 4;
+  const RouteBwdParams p{dweights, a.logits, a.rows, a.ld, a.experts, a.k, a.sigmoid, a.renormalize, a.scale, a.chosen, dlogits, ld_d,
+                         route_vec(a.logits, a.ld, a.experts, esize) && route_vec(dlogits, ld_d, a.experts, esize)};
+  const int lanes = route_lanes(a.experts, a.k, 1), held = (a.experts + lanes - 1) / lanes;
+  return a.dtype == LUQ_BF16 ? launch_route_lanes<__nv_bfloat16>(ctx, p, lanes, held, st) : launch_route_lanes<float>(ctx, p, lanes, held, st);
 }
 
 // bytes of workspace that the order of `total` assignments needs
