@@ -607,7 +607,8 @@ __global__ void __launch_bounds__(128) route_bwd_kernel(const RouteBwdParams p) 
 // ---- order ---------------------------------------------------------------------------------------------------------------
 // A stable counting sort.  A block has a segment of the assignments, a warp a run of it; runs are counted, the counts are
 // summed over the runs before, and every run is walked once more, 32 assignments at a time: a lane's place is the number of
-// lanes below it with the same expert.  More than one segment: a kernel counts them first.
+// lanes below it with the same expert.  More than one segment: a kernel counts them first, and every block adds the segments'
+// counts up for itself.  What bounds it is the latency of its steps, so a run of several segments is one step of a warp.
 struct OrderParams {
   const int* chosen;
   long long total;          // assignments
@@ -619,56 +620,63 @@ struct OrderParams {
 };
 constexpr int kOrderWarps = 32;
 
-// counts of a warp's run into `hist` (cleared)
-__device__ __forceinline__ void count_run(const OrderParams& p, long long from, long long to, int* hist, int lane) {
-  for (long long a = from; a < to; a += 32) {
-    const int e = a + lane < to ? p.chosen[a + lane] : -1;
-    const unsigned same = __match_any_sync(kFull, e);
-    if (e >= 0 && e < p.experts && lane == __ffs(same) - 1) hist[e] += __popc(same);
-    __syncwarp();
-  }
-}
-
 __global__ void __launch_bounds__(32 * kOrderWarps) order_count_kernel(const OrderParams p) {
-  extern __shared__ int hist[];                         // [warps][experts]
+  __shared__ int hist[LUQ_MAX_GROUPS];
   pdl_wait();
   pdl_trigger();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int i = threadIdx.x; i < kOrderWarps * p.experts; i += blockDim.x) hist[i] = 0;
+  for (int i = threadIdx.x; i < p.experts; i += blockDim.x) hist[i] = 0;
   __syncthreads();
-  const long long run = p.segment / kOrderWarps, from = blockIdx.x * p.segment + warp * run;
-  count_run(p, from, min(from + run, p.total), hist + warp * p.experts, lane);
-  __syncthreads();
-  for (int e = threadIdx.x; e < p.experts; e += blockDim.x) {
-    int n = 0;
-    for (int w = 0; w < kOrderWarps; ++w) n += hist[w * p.experts + e];
-    p.counts[static_cast<long long>(blockIdx.x) * p.experts + e] = n;
+  const long long from = blockIdx.x * p.segment, to = min(from + p.segment, p.total);
+  for (long long a = from + threadIdx.x; a < to; a += blockDim.x) {
+    const int e = p.chosen[a];
+    if (e >= 0 && e < p.experts) atomicAdd(hist + e, 1);           // (whole numbers: in any order the same)
   }
+  __syncthreads();
+  for (int e = threadIdx.x; e < p.experts; e += blockDim.x) p.counts[static_cast<long long>(blockIdx.x) * p.experts + e] = hist[e];
 }
 
 __global__ void __launch_bounds__(32 * kOrderWarps) order_kernel(const OrderParams p) {
   extern __shared__ int hist[];                         // [warps][experts]: counts, then the next position of each
-  __shared__ int sums[kOrderWarps];
+  __shared__ int sums[kOrderWarps], parts[2][32 * kOrderWarps];
   pdl_wait();
   pdl_trigger();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = threadIdx.x; i < kOrderWarps * p.experts; i += blockDim.x) hist[i] = 0;
+  // a warp has 32 experts and a part of the segments: their copies before this block's segment, and in all
+  const int experts32 = (p.experts + 31) / 32, share = kOrderWarps / experts32;
+  const int segments = static_cast<int>(gridDim.x), here = static_cast<int>(blockIdx.x);
+  if (segments > 1 && warp < share * experts32) {
+    const int e = warp % experts32 * 32 + lane, part = warp / experts32;
+    int before = 0, all = 0;
+    if (e < p.experts) {
+#pragma unroll 8
+      for (int b = part; b < segments; b += share) {
+        const int n = p.counts[static_cast<long long>(b) * p.experts + e];
+        all += n;
+        before += b < here ? n : 0;
+      }
+    }
+    parts[0][warp * 32 + lane] = before;
+    parts[1][warp * 32 + lane] = all;
+  }
   __syncthreads();
-  const long long run = p.segment / kOrderWarps, from = blockIdx.x * p.segment + warp * run, to = min(from + run, p.total);
+  const long long run = p.segment / kOrderWarps, from = here * p.segment + warp * run, to = min(from + run, p.total);
   int* const own = hist + warp * p.experts;
-  count_run(p, from, to, own, lane);
+  for (long long a = from; a < to; a += 32) {
+    const int e = a + lane < to ? p.chosen[a + lane] : -1;
+    const unsigned same = __match_any_sync(kFull, e);
+    if (e >= 0 && e < p.experts && lane == __ffs(same) - 1) own[e] += __popc(same);
+    __syncwarp();
+  }
   __syncthreads();
-  // a thread has an expert (there are at most as many): its copies before this block's segment, and in all segments
+  // a thread has an expert (there are at most as many)
   const int e = threadIdx.x;
   int before = 0, all = 0;
   if (e < p.experts) {
-    if (gridDim.x > 1) {
-      for (unsigned b = 0; b < gridDim.x; ++b) {
-        const int n = p.counts[static_cast<long long>(b) * p.experts + e];
-        all += n;
-        if (b < blockIdx.x) before += n;
-      }
+    if (segments > 1) {
+      for (int i = 0; i < share; ++i) { before += parts[0][i * experts32 * 32 + e]; all += parts[1][i * experts32 * 32 + e]; }
     } else {
+#pragma unroll
       for (int w = 0; w < kOrderWarps; ++w) all += hist[w * p.experts + e];
     }
   }
@@ -680,17 +688,19 @@ __global__ void __launch_bounds__(32 * kOrderWarps) order_kernel(const OrderPara
   }
   if (lane == 31) sums[warp] = start;
   __syncthreads();
-  for (int w = 0; w < warp; ++w) start += sums[w];
+  start += static_cast<int>(__reduce_add_sync(kFull, static_cast<unsigned>(lane < warp ? sums[lane] : 0)));
   if (e < p.experts) {
-    if (blockIdx.x == 0) p.offsets[e + 1] = start;
-    int next = start - all + before;
+    if (here == 0) p.offsets[e + 1] = start;
+    int n[kOrderWarps], next = start - all + before;
+#pragma unroll
+    for (int w = 0; w < kOrderWarps; ++w) n[w] = hist[w * p.experts + e];
+#pragma unroll
     for (int w = 0; w < kOrderWarps; ++w) {
-      const int n = hist[w * p.experts + e];
       hist[w * p.experts + e] = next;
-      next += n;
+      next += n[w];
     }
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) p.offsets[0] = 0;
+  if (here == 0 && threadIdx.x == 0) p.offsets[0] = 0;
   __syncthreads();
   for (long long a = from; a < to; a += 32) {
     const int x = a + lane < to ? p.chosen[a + lane] : -1;
@@ -706,44 +716,92 @@ __global__ void __launch_bounds__(32 * kOrderWarps) order_kernel(const OrderPara
 }
 
 // ---- dispatch and combine --------------------------------------------------------------------------------------------------
-// Rows in pieces of 16 bytes where every row starts at a multiple of them, else element by element.  A warp has a token's
-// segment of 32 pieces.
-template <typename T, bool VEC>
+// Rows go in pieces.  kWhole: 16 bytes, all rows start at multiples of them.  Where they do not, fp32 goes element by element
+// (kSingle; 32 lanes are 128 bytes all the same), bf16 in pieces that are aligned in the row that is written (kShifted): what is read
+// is put together from the two aligned pieces that it lies in, and a row's first and last piece are written element by element.  An
+// aligned piece is read only if it holds an element of the row.  (bf16, 4000 x 1001, four copies summed: 25.6 us element by element, 15.4
+// shifted; fp32, 4099 x 771, three copies' gradients: 26.8 us shifted, 21.0 element by element.)
+constexpr int kWhole = 0, kSingle = 1, kShifted = 2;
+template <typename T, int MODE>
 struct Piece {
-  static constexpr int n = VEC ? 16 / static_cast<int>(sizeof(T)) : 1;
-  float v[n];
-  __device__ __forceinline__ void load(const T* p) {
-    if constexpr (!VEC) {
-      v[0] = load1(p);
-    } else if constexpr (sizeof(T) == 4) {
-      const float4 f = *reinterpret_cast<const float4*>(p);
-      v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
-    } else {
-      const uint4 u = *reinterpret_cast<const uint4*>(p);
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-      }
-    }
+  static constexpr int n = MODE == kSingle ? 1 : 16 / static_cast<int>(sizeof(T)), words = MODE == kSingle ? 1 : 4;
+  uint32_t w[words];
+  __device__ __forceinline__ float get(int i) const {       // (i is known when this is compiled)
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
   }
-  __device__ __forceinline__ void store(T* p) const {
-    if constexpr (!VEC) {
-      store1(p, v[0]);
-    } else if constexpr (sizeof(T) == 4) {
-      *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    } else {
-      uint32_t w[4];
+  __device__ __forceinline__ void set(const float (&v)[n]) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < words; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        w[i] = __float_as_uint(v[i]);
+      } else {
         const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
         w[i] = *reinterpret_cast<const uint32_t*>(&h);
       }
-      *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < words; ++i) w[i] = 0u;
+  }
+  // elements c .. c + n - 1 of a row of `cols` (at least one of them there), zeros where there are none
+  __device__ __forceinline__ void load(const T* row, int c, int cols) {
+    if constexpr (MODE == kSingle) {
+      w[0] = *reinterpret_cast<const uint32_t*>(row + c);
+    } else if constexpr (MODE == kWhole) {
+      const uint4 u = *reinterpret_cast<const uint4*>(row + c);
+      w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+    } else {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(row) + static_cast<long long>(c) * static_cast<int>(sizeof(T));
+      const uintptr_t low = at & ~static_cast<uintptr_t>(15);
+      const int shift = static_cast<int>(at & 15u);
+      const bool inside = c >= 0 && c + n <= cols;
+      uint4 a = make_uint4(0, 0, 0, 0), b = a;
+      if (inside) {
+        a = *reinterpret_cast<const uint4*>(low);
+        if (shift) b = *reinterpret_cast<const uint4*>(low + 16);
+      } else {
+        const uintptr_t first = reinterpret_cast<uintptr_t>(row + max(c, 0)), end = reinterpret_cast<uintptr_t>(row + min(c + n, cols));
+        if (low + 16 > first && low < end) a = *reinterpret_cast<const uint4*>(low);
+        if (shift && low + 16 < end && low + 32 > first) b = *reinterpret_cast<const uint4*>(low + 16);
+      }
+      uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      if (shift & 8) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) v[i] = v[i + 2];
+      }
+      if (shift & 4) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) v[i] = v[i + 1];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(v[i], v[i + 1], 8 * (shift & 3));
+      // what lies before the row's first element or behind its last plays no part in a sum
+      if (!inside) {
+#pragma unroll
+        for (int i = 0; i < n; ++i)
+          if (c + i < 0 || c + i >= cols) w[i / 2] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* row, int c, int cols) const {
+    if constexpr (MODE == kSingle) {
+      *reinterpret_cast<uint32_t*>(row + c) = w[0];
+    } else if (MODE == kWhole || (c >= 0 && c + n <= cols)) {
+      *reinterpret_cast<uint4*>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < n; ++i)
+        if (c + i >= 0 && c + i < cols) reinterpret_cast<uint16_t*>(row)[c + i] = static_cast<uint16_t>(i & 1 ? w[i / 2] >> 16 : w[i / 2]);
     }
   }
 };
+// a row's first piece starts so many elements before it
+template <typename T, int MODE>
+__device__ __forceinline__ int lead(const T* row) {
+  return MODE == kShifted ? static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T)) : 0;
+}
 
 struct MoveParams {
   const void* x;            // dispatch: tokens; combine: results; combine_bwd: results
@@ -752,7 +810,7 @@ struct MoveParams {
   long long ld_more;
   const int* position;
   long long rows;           // tokens
-  int k, cols, segments;
+  int k, cols, segments;    // segments: parts of a row that a warp takes at a time
   long long copies;         // rows of the copies' tensor
   const float* weights;     // may be null: ones
   const int* offsets;       // dispatch, combine_bwd: rows from offsets[groups] on are zeroed
@@ -762,78 +820,140 @@ struct MoveParams {
   float* dweights;
   unsigned int* status;
 };
+template <int MODE> constexpr int kPieces = MODE == kSingle ? 8 : 4;       // pieces of a lane at a time
+// those that it sums copies of (16384 x 2048 bf16, two copies: 45 us, with two pieces 50; 4000 x 1001, four copies: 19 us with four, 14 with two)
+template <int MODE> constexpr int kSumPieces = MODE == kSingle ? 8 : MODE == kWhole ? 4 : 2;
+constexpr int kMoveWarps = 4;                   // warps of a block
 
+// row `to` of the copies, if it is one
 __device__ __forceinline__ bool copy_in(const MoveParams& p, int to) { return to >= 0 && to < p.copies; }
 
 // rows of the copies that no token has
-template <typename T, bool VEC>
+template <typename T, int MODE>
 __device__ __forceinline__ void zero_rest(const MoveParams& p, long long warp, long long warps, int lane) {
   const int used = min(max(*(p.offsets + p.groups), 0), static_cast<int>(p.copies));
-  Piece<T, VEC> zero;
-#pragma unroll
-  for (int i = 0; i < zero.n; ++i) zero.v[i] = 0.0f;
-  for (long long r = used + warp; r < p.copies; r += warps)
-    for (int c = lane * zero.n; c < p.cols; c += 32 * zero.n) zero.store(static_cast<T*>(p.out) + r * p.ld_out + c);
-}
-
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) dispatch_kernel(const MoveParams p) {
-  using P = Piece<T, VEC>;
-  pdl_wait();
-  pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const long long warp = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5), warps = static_cast<long long>(gridDim.x) * 8;
-  for (long long i = warp; i < p.rows * p.segments; i += warps) {
-    const long long t = i / p.segments;
-    const int c = (static_cast<int>(i - t * p.segments) * 32 + lane) * P::n;
-    const int* const to = p.position + t * p.k;
-    if (c >= p.cols) continue;
-    P v;
-    v.load(static_cast<const T*>(p.x) + t * p.ld_x + c);
-    for (int j = 0; j < p.k; ++j)
-      if (copy_in(p, to[j])) v.store(static_cast<T*>(p.out) + to[j] * p.ld_out + c);
+  Piece<T, MODE> zero;
+  zero.zero();
+  for (long long r = used + warp; r < p.copies; r += warps) {
+    T* const row = static_cast<T*>(p.out) + r * p.ld_out;
+    for (int c = lane * zero.n - lead<T, MODE>(row); c < p.cols; c += 32 * zero.n) zero.store(row, c, p.cols);
   }
-  zero_rest<T, VEC>(p, warp, warps, lane);
 }
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) combine_kernel(const MoveParams p) {
-  using P = Piece<T, VEC>;
+// A warp has a token's segment.  With aligned rows it holds the segment in registers and writes it k times; else every copy has
+// an alignment of its own and the token's pieces are read again for it (from L1).
+template <typename T, int MODE>
+__global__ void __launch_bounds__(32 * kMoveWarps) dispatch_kernel(const MoveParams p) {
+  using P = Piece<T, MODE>;
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31;
-  const long long warp = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5), warps = static_cast<long long>(gridDim.x) * 8;
+  const long long warp = static_cast<long long>(blockIdx.x) * kMoveWarps + (threadIdx.x >> 5), warps = static_cast<long long>(gridDim.x) * kMoveWarps;
   for (long long i = warp; i < p.rows * p.segments; i += warps) {
     const long long t = i / p.segments;
-    const int c = (static_cast<int>(i - t * p.segments) * 32 + lane) * P::n;
-    if (c >= p.cols) continue;
-    P sum;
-    if (p.more) sum.load(static_cast<const T*>(p.more) + t * p.ld_more + c);
-    else
+    const int first = (static_cast<int>(i - t * p.segments) * 32 * kPieces<MODE> + lane) * P::n;
+    const T* const row = static_cast<const T*>(p.x) + t * p.ld_x;
+    P v[kPieces<MODE>];
+    if constexpr (MODE != kShifted) {
 #pragma unroll
-      for (int q = 0; q < P::n; ++q) sum.v[q] = 0.0f;
-    for (int j = 0; j < p.k; ++j) {
-      const int at = p.position[t * p.k + j];
-      const float w = p.weights ? p.weights[t * p.k + j] : 1.0f;
-      P v;
-#pragma unroll
-      for (int q = 0; q < P::n; ++q) v.v[q] = 0.0f;
-      if (copy_in(p, at)) v.load(static_cast<const T*>(p.x) + at * p.ld_x + c);
-#pragma unroll
-      for (int q = 0; q < P::n; ++q) sum.v[q] = fmaf(w, v.v[q], sum.v[q]);
+      for (int u = 0; u < kPieces<MODE>; ++u)
+        if (first + u * 32 * P::n < p.cols) v[u].load(row, first + u * 32 * P::n, p.cols);
     }
-    sum.store(static_cast<T*>(p.out) + t * p.ld_out + c);
+    for (int j0 = 0; j0 < p.k; j0 += 32) {
+      const int mine = j0 + lane < p.k ? p.position[t * p.k + j0 + lane] : -1;
+      for (int j = 0; j < min(p.k - j0, 32); ++j) {
+        const int to = __shfl_sync(kFull, mine, j);
+        if (!copy_in(p, to)) continue;
+        T* const out = static_cast<T*>(p.out) + to * p.ld_out;
+        const int c0 = first - lead<T, MODE>(out);
+        if constexpr (MODE == kShifted) {
+#pragma unroll
+          for (int u = 0; u < kPieces<MODE>; ++u)
+            if (c0 + u * 32 * P::n < p.cols) v[u].load(row, c0 + u * 32 * P::n, p.cols);
+        }
+#pragma unroll
+        for (int u = 0; u < kPieces<MODE>; ++u)
+          if (c0 + u * 32 * P::n < p.cols) v[u].store(out, c0 + u * 32 * P::n, p.cols);
+      }
+    }
   }
+  zero_rest<T, MODE>(p, warp, warps, lane);
 }
 
-// dy[position] = w dout, dw = dout . y[position]: a warp has a copy
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) combine_bwd_kernel(const MoveParams p) {
-  using P = Piece<T, VEC>;
+// A warp sums a token's segment.  The next segment's positions and weights are on their way meanwhile.
+template <typename T, int MODE>
+__global__ void __launch_bounds__(32 * kMoveWarps) combine_kernel(const MoveParams p) {
+  using P = Piece<T, MODE>;
+  constexpr int kAt = kSumPieces<MODE>;
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31;
-  const long long warp = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5), warps = static_cast<long long>(gridDim.x) * 8;
+  const long long warp = static_cast<long long>(blockIdx.x) * kMoveWarps + (threadIdx.x >> 5), warps = static_cast<long long>(gridDim.x) * kMoveWarps;
+  const long long end = p.rows * p.segments;
+  auto places = [&](long long t, int j0, int& at, float& w) {
+    const bool in = t < p.rows && j0 + lane < p.k;
+    at = in ? p.position[t * p.k + j0 + lane] : -1;
+    w = in && p.weights ? p.weights[t * p.k + j0 + lane] : 1.0f;
+  };
+  int next_at;
+  float next_w;
+  places(warp / p.segments, 0, next_at, next_w);
+  for (long long i = warp; i < end; i += warps) {
+    const long long t = i / p.segments;
+    T* const out = static_cast<T*>(p.out) + t * p.ld_out;
+    const int first = (static_cast<int>(i - t * p.segments) * 32 * kAt + lane) * P::n - lead<T, MODE>(out);
+    P r[kAt];
+#pragma unroll
+    for (int u = 0; u < kAt; ++u) {
+      const int c = first + u * 32 * P::n;
+      r[u].zero();
+      if (p.more && c < p.cols) r[u].load(static_cast<const T*>(p.more) + t * p.ld_more, c, p.cols);
+    }
+    int mine = next_at;
+    float weight = next_w;
+    places((i + warps) / p.segments, 0, next_at, next_w);
+    float sum[kAt][P::n];
+#pragma unroll
+    for (int u = 0; u < kAt; ++u)
+#pragma unroll
+      for (int q = 0; q < P::n; ++q) sum[u][q] = r[u].get(q);
+    for (int j0 = 0; j0 < p.k; j0 += 32) {
+      if (j0) places(t, j0, mine, weight);
+      const int count = min(p.k - j0, 32);
+#pragma unroll 2
+      for (int j = 0; j < count; ++j) {
+        const int at = __shfl_sync(kFull, mine, j);
+        const float w = __shfl_sync(kFull, weight, j);
+        P v[kAt];
+#pragma unroll
+        for (int u = 0; u < kAt; ++u) {
+          const int c = first + u * 32 * P::n;
+          v[u].zero();
+          if (copy_in(p, at) && c < p.cols) v[u].load(static_cast<const T*>(p.x) + at * p.ld_x, c, p.cols);
+        }
+#pragma unroll
+        for (int u = 0; u < kAt; ++u)
+#pragma unroll
+          for (int q = 0; q < P::n; ++q) sum[u][q] = fmaf(w, v[u].get(q), sum[u][q]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kAt; ++u) {
+      const int c = first + u * 32 * P::n;
+      r[u].set(sum[u]);
+      if (c < p.cols) r[u].store(out, c, p.cols);
+    }
+  }
+}
+
+// dy[position] = w dout, dw = dout . y[position]: a warp has a copy; a token's copies are neighbours and read its dout from L1
+template <typename T, int MODE>
+__global__ void __launch_bounds__(32 * kMoveWarps) combine_bwd_kernel(const MoveParams p) {
+  using P = Piece<T, MODE>;
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31;
+  const long long warp = static_cast<long long>(blockIdx.x) * kMoveWarps + (threadIdx.x >> 5), warps = static_cast<long long>(gridDim.x) * kMoveWarps;
   for (long long i = warp; i < p.rows * p.k; i += warps) {
     const int at = p.position[i];
     if (!copy_in(p, at)) {
@@ -842,32 +962,48 @@ __global__ void __launch_bounds__(256) combine_bwd_kernel(const MoveParams p) {
     }
     const long long t = i / p.k;
     const float w = p.weights ? p.weights[i] : 1.0f;
+    const T* const d_row = static_cast<const T*>(p.more) + t * p.ld_more;
+    const T* const y_row = static_cast<const T*>(p.x) + at * p.ld_x;
+    T* const out = static_cast<T*>(p.out) + at * p.ld_out;
     float dot = 0.0f;
-    for (int c = lane * P::n; c < p.cols; c += 32 * P::n) {
-      P d, y;
-      d.load(static_cast<const T*>(p.more) + t * p.ld_more + c);
-      if (p.dweights) {
-        y.load(static_cast<const T*>(p.x) + at * p.ld_x + c);
+    for (int first = lane * P::n - (p.out ? lead<T, MODE>(out) : 0); first - lane * P::n < p.cols; first += 32 * P::n * kPieces<MODE>) {
+      P d[kPieces<MODE>], y[kPieces<MODE>];
 #pragma unroll
-        for (int q = 0; q < P::n; ++q) dot = fmaf(d.v[q], y.v[q], dot);
+      for (int u = 0; u < kPieces<MODE>; ++u) {
+        const int c = first + u * 32 * P::n;
+        d[u].zero();
+        y[u].zero();
+        if (c < p.cols) {
+          d[u].load(d_row, c, p.cols);
+          if (p.dweights) y[u].load(y_row, c, p.cols);
+        }
       }
-      if (p.out) {
 #pragma unroll
-        for (int q = 0; q < P::n; ++q) d.v[q] *= w;
-        d.store(static_cast<T*>(p.out) + at * p.ld_out + c);
+      for (int u = 0; u < kPieces<MODE>; ++u) {
+        const int c = first + u * 32 * P::n;
+        float g[P::n];
+#pragma unroll
+        for (int q = 0; q < P::n; ++q) {
+          g[q] = d[u].get(q);
+          dot = fmaf(g[q], y[u].get(q), dot);
+          g[q] *= w;
+        }
+        P r;
+        r.set(g);
+        if (p.out && c < p.cols) r.store(out, c, p.cols);
       }
     }
     dot = warp_sum(dot);
     if (lane == 0 && p.dweights) p.dweights[i] = dot;
   }
-  if (p.out) zero_rest<T, VEC>(p, warp, warps, lane);
+  if (p.out) zero_rest<T, MODE>(p, warp, warps, lane);
 }
 
 bool vec16(const void* p, long long ld, long long rows, int esize) {
   return !p || ((reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows <= 1 || ld * esize % 16 == 0));
 }
 int blocks_of(const luq_ctx* ctx, long long warps) {
-  const long long blocks = (warps + 7) / 8, most = ctx->sm_count * 32ll;
+  const long long blocks = (warps + kMoveWarps - 1) / kMoveWarps, most = static_cast<long long>(ctx->sm_count) * 64;
   return static_cast<int>(blocks < 1 ? 1 : blocks < most ? blocks : most);
 }
 int done(luq_ctx* ctx, cudaError_t e) {
@@ -906,23 +1042,42 @@ int launch_route_lanes(luq_ctx* ctx, const P& p, int lanes, int per_lane, cudaSt
   return launch_route<T, 32, 32>(ctx, p, st);
 }
 
-MoveParams move_params(const luq_ctx* ctx, const luq_move_args& a, bool& vec) {
+MoveParams move_params(const luq_ctx* ctx, const luq_move_args& a, bool& whole) {
   const int esize = a.dtype == LUQ_BF16 ? 2 : 4;
   MoveParams p{};
   p.x = a.x; p.ld_x = a.ld_x; p.more = a.more; p.ld_more = a.ld_more; p.position = a.position; p.rows = a.rows; p.k = a.k;
   p.cols = static_cast<int>(a.cols); p.copies = a.copies; p.weights = a.weights; p.offsets = a.offsets; p.groups = a.groups;
   p.out = a.out; p.ld_out = a.ld_out; p.dweights = a.dweights; p.status = ctx->d_status;
   // (row counts play no part: a row of one is as good as any)
-  vec = a.cols * esize % 16 == 0 && vec16(a.x, a.ld_x, 2, esize) && vec16(a.more, a.ld_more, 2, esize) && vec16(a.out, a.ld_out, 2, esize);
-  const int n = vec ? 16 / esize : 1;
-  p.segments = static_cast<int>((a.cols + 32 * n - 1) / (32 * n));
+  whole = a.cols * esize % 16 == 0 && vec16(a.x, a.ld_x, 2, esize) && vec16(a.more, a.ld_more, 2, esize) && vec16(a.out, a.ld_out, 2, esize);
   return p;
 }
-// chooses one of a kernel's four forms
-#define LUQ_MOVE(kernel, warps)                                                                                               \
-  (a.dtype == LUQ_BF16                                                                                                        \
-       ? done(ctx, luq_launch_kernel(vec ? kernel<__nv_bfloat16, true> : kernel<__nv_bfloat16, false>, blocks_of(ctx, warps), 256, 0, st, LUQ_LAUNCH_EARLY, 1, p)) \
-       : done(ctx, luq_launch_kernel(vec ? kernel<float, true> : kernel<float, false>, blocks_of(ctx, warps), 256, 0, st, LUQ_LAUNCH_EARLY, 1, p)))
+// parts of a row that a warp takes at a time
+template <typename T, int MODE>
+int segments_of(long long cols, int pieces) {
+  const int n = Piece<T, MODE>::n, lead = MODE == kShifted ? n - 1 : 0;   // (at most so many elements lie before a row's first piece's end)
+  return static_cast<int>((cols + lead + 32 * n * pieces - 1) / (32 * n * pieces));
+}
+template <typename T, int MODE>
+int launch_dispatch(luq_ctx* ctx, MoveParams p, cudaStream_t st) {
+  p.segments = segments_of<T, MODE>(p.cols, kPieces<MODE>);
+  return done(ctx, luq_launch_kernel(dispatch_kernel<T, MODE>, blocks_of(ctx, p.rows * p.segments), 32 * kMoveWarps, 0, st, LUQ_LAUNCH_EARLY, 1, p));
+}
+template <typename T, int MODE>
+int launch_combine(luq_ctx* ctx, MoveParams p, cudaStream_t st) {
+  p.segments = segments_of<T, MODE>(p.cols, kSumPieces<MODE>);
+  return done(ctx, luq_launch_kernel(combine_kernel<T, MODE>, blocks_of(ctx, p.rows * p.segments), 32 * kMoveWarps, 0, st, LUQ_LAUNCH_EARLY, 1, p));
+}
+template <typename T, int MODE>
+int launch_combine_bwd(luq_ctx* ctx, MoveParams p, cudaStream_t st) {
+  return done(ctx, luq_launch_kernel(combine_bwd_kernel<T, MODE>, blocks_of(ctx, p.rows * p.k), 32 * kMoveWarps, 0, st, LUQ_LAUNCH_EARLY, 1, p));
+}
+// chooses one of a move's four forms
+#define LUQ_MOVE(launch)                                                                                                             \
+  bool whole;                                                                                                                        \
+  const MoveParams p = move_params(ctx, a, whole);                                                                                   \
+  if (a.dtype == LUQ_BF16) return whole ? launch<__nv_bfloat16, kWhole>(ctx, p, st) : launch<__nv_bfloat16, kShifted>(ctx, p, st);  \
+  return whole ? launch<float, kWhole>(ctx, p, st) : launch<float, kSingle>(ctx, p, st);
 
 }  // namespace
 
@@ -950,9 +1105,10 @@ int luq_launch_route_bwd(luq_ctx* ctx, const luq_route_args& a, const float* dwe
 
 // bytes of workspace that the order of `total` assignments needs
 static int64_t order_segments(int64_t total, int64_t* segment) {
-  constexpr int64_t kLeast = 32 * kOrderWarps * 4, kMost = 256;
-  int64_t s = kLeast;
-  if (total > kLeast * kMost) s = ((total + kMost - 1) / kMost + 32 * kOrderWarps - 1) / (32 * kOrderWarps) * (32 * kOrderWarps);
+  constexpr int64_t kStep = 32 * kOrderWarps, kAlone = 2 * kStep, kMost = 256;
+  int64_t s = kStep;
+  if (total <= kAlone) s = kAlone;                      // one launch
+  else if (total > kStep * kMost) s = ((total + kMost - 1) / kMost + kStep - 1) / kStep * kStep;
   *segment = s;
   return (total + s - 1) / s;
 }
@@ -970,30 +1126,16 @@ int luq_launch_order(luq_ctx* ctx, const int* chosen, int64_t total, int experts
   const size_t smem = static_cast<size_t>(kOrderWarps) * experts * sizeof(int);
   static luq_once_per_device allowed;
   const cudaError_t attr = allowed([&] {
-    constexpr int most = kOrderWarps * LUQ_MAX_GROUPS * sizeof(int);
-    const cudaError_t e = cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-    return e != cudaSuccess ? e : cudaFuncSetAttribute(order_count_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    return cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kOrderWarps * LUQ_MAX_GROUPS * sizeof(int)));
   }, ctx->device);
   if (attr != cudaSuccess) return static_cast<int>(attr);
   if (blocks > 1) {
-    const int e = done(ctx, luq_launch_kernel(order_count_kernel, blocks, 32 * kOrderWarps, smem, st, LUQ_LAUNCH_EARLY, 1, p));
+    const int e = done(ctx, luq_launch_kernel(order_count_kernel, blocks, 32 * kOrderWarps, 0, st, LUQ_LAUNCH_EARLY, 1, p));
     if (e) return e;
   }
   return done(ctx, luq_launch_kernel(order_kernel, blocks, 32 * kOrderWarps, smem, st, LUQ_LAUNCH_EARLY, 1, p));
 }
 
-int luq_launch_dispatch(luq_ctx* ctx, const luq_move_args& a, cudaStream_t st) {
-  bool vec;
-  const MoveParams p = move_params(ctx, a, vec);
-  return LUQ_MOVE(dispatch_kernel, p.rows * p.segments);
-}
-int luq_launch_combine(luq_ctx* ctx, const luq_move_args& a, cudaStream_t st) {
-  bool vec;
-  const MoveParams p = move_params(ctx, a, vec);
-  return LUQ_MOVE(combine_kernel, p.rows * p.segments);
-}
-int luq_launch_combine_bwd(luq_ctx* ctx, const luq_move_args& a, cudaStream_t st) {
-  bool vec;
-  const MoveParams p = move_params(ctx, a, vec);
-  return LUQ_MOVE(combine_bwd_kernel, p.rows * p.k);
-}
+int luq_launch_dispatch(luq_ctx* ctx, const luq_move_args& a, cudaStream_t st) { LUQ_MOVE(launch_dispatch) }
+int luq_launch_combine(luq_ctx* ctx, const luq_move_args& a, cudaStream_t st) { LUQ_MOVE(launch_combine) }
+int luq_launch_combine_bwd(luq_ctx* ctx, const luq_move_args& a, cudaStream_t st) { LUQ_MOVE(launch_combine_bwd) }
