@@ -8,9 +8,10 @@
 // 2688 = 6 * 448: the row's largest block gets the largest e4m3 number, its largest element the largest e2m1 number.  A block
 // that is less than 2^-10 of the row's scale has a zero scale and zero numbers.
 //
-// A thread holds 16 neighbouring elements in registers, so x is read once; the row's maximum meets in shared memory.  Block
-// scales leave in the tiles that the tensor cores copy (128 rows x 4 blocks, row r, block b at 16 (r mod 32) + 4 (r / 32) + b):
-// the threads of four blocks put their bytes together and one stores the word.  What bounds it is the memory's bytes.
+// Warps that share a row walk over rows; a thread holds chunks of 16 neighbouring elements in registers, and the next row's are on
+// their way meanwhile, so x is read once; the row's maximum meets in shared memory.  Block scales leave in the tiles that the
+// tensor cores copy (128 rows x 4 blocks, row r, block b at 16 (r mod 32) + 4 (r / 32) + b): the threads of four blocks put
+// their bytes together and one stores the word.
 #include <cuda_bf16.h>
 
 #include "common.cuh"
@@ -41,45 +42,79 @@ struct RowsParams {
   bool vec;                 // rows of x start at multiples of 16 bytes
 };
 
-__device__ __forceinline__ float load1(const float* p) { return *p; }
-__device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-
-// 16 elements of a row from `c0` on, zeros beyond its end
+// The words of a thread's 16 elements, zeros beyond the row's end.  Where they do not lie in whole aligned pieces of 16 bytes they
+// are put together from the pieces that hold an element of theirs.
+template <typename T> constexpr int kWords = kChunk * static_cast<int>(sizeof(T)) / 4;
 template <typename T>
-__device__ __forceinline__ void load_chunk16(const T* row, int c0, int cols, bool vec, float (&v)[kChunk]) {
+__device__ __forceinline__ void load_chunk16(const T* row, int c0, int cols, bool vec, uint32_t (&w)[kWords<T>]) {
+  constexpr int W = kWords<T>;
   if (vec && c0 + kChunk <= cols) {
-    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 f = reinterpret_cast<const float4*>(row + c0)[i];
-        v[4 * i] = f.x; v[4 * i + 1] = f.y; v[4 * i + 2] = f.z; v[4 * i + 3] = f.w;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint4 u = reinterpret_cast<const uint4*>(row + c0)[i];
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
-          v[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-        }
-      }
+    for (int i = 0; i < W / 4; ++i) {
+      const uint4 u = reinterpret_cast<const uint4*>(row + c0)[i];
+      w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
     }
-  } else {
+    return;
+  }
+  if (c0 >= cols) {
 #pragma unroll
-    for (int i = 0; i < kChunk; ++i) v[i] = c0 + i < cols ? load1(row + c0 + i) : 0.0f;
+    for (int i = 0; i < W; ++i) w[i] = 0u;
+    return;
+  }
+  const uintptr_t at = reinterpret_cast<uintptr_t>(row + c0), end = reinterpret_cast<uintptr_t>(row + min(c0 + kChunk, cols));
+  const uintptr_t low = at & ~static_cast<uintptr_t>(15);
+  const int shift = static_cast<int>(at & 15u);
+  uint32_t v[W + 4];
+#pragma unroll
+  for (int i = 0; i <= W / 4; ++i) {
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (low + 16 * i < end) u = *reinterpret_cast<const uint4*>(low + 16 * i);
+    v[4 * i] = u.x; v[4 * i + 1] = u.y; v[4 * i + 2] = u.z; v[4 * i + 3] = u.w;
+  }
+  if (shift & 8) {
+#pragma unroll
+    for (int i = 0; i < W + 2; ++i) v[i] = v[i + 2];
+  }
+  if (shift & 4) {
+#pragma unroll
+    for (int i = 0; i < W + 1; ++i) v[i] = v[i + 1];
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) w[i] = sizeof(T) == 4 ? v[i] : __funnelshift_r(v[i], v[i + 1], 8 * (shift & 2));
+  if (c0 + kChunk > cols) {
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i)
+      if (c0 + i >= cols) {
+        if constexpr (sizeof(T) == 4) w[i] = 0u;
+        else w[i / 2] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+      }
   }
 }
-// the largest pattern of |v|: of numbers the largest, Inf above every number, NaN above Inf
-__device__ __forceinline__ uint32_t top_of(const float (&v)[kChunk]) {
+// the largest pattern of |x|, as a binary32 one: of numbers the largest, Inf above every number, NaN above Inf
+template <typename T>
+__device__ __forceinline__ uint32_t top_of(const uint32_t (&w)[kWords<T>]) {
   uint32_t t = 0;
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-  for (int i = 0; i < kChunk; ++i) t = max(t, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-  return t;
+    for (int i = 0; i < kWords<T>; ++i) t = max(t, w[i] & 0x7FFFFFFFu);
+    return t;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kWords<T>; ++i) asm("max.u16x2 %0, %0, %1;" : "+r"(t) : "r"(w[i] & 0x7FFF7FFFu));
+    return max(t << 16, t & 0xFFFF0000u);
+  }
 }
-// eight numbers, the first in the lowest four bits
-__device__ __forceinline__ uint32_t pack8(const float* v, float f) {
+template <typename T>
+__device__ __forceinline__ float2 pair_of(const uint32_t (&w)[kWords<T>], int i) {
+  if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+  else return make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+}
+// eight numbers from pairs `first` .. `first` + 3, the first in the lowest four bits
+template <typename T>
+__device__ __forceinline__ uint32_t pack8(const uint32_t (&w)[kWords<T>], int first, float f) {
+  float2 v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __fmul2_rn(pair_of<T>(w, first + i), make_float2(f, f));
   uint32_t r;
   asm("{\n\t.reg .b8 a, b, c, d;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
@@ -88,8 +123,7 @@ __device__ __forceinline__ uint32_t pack8(const float* v, float f) {
       "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
       "mov.b32 %0, {a, b, c, d};\n\t}"
       : "=r"(r)
-      : "f"(__fmul_rn(v[0], f)), "f"(__fmul_rn(v[1], f)), "f"(__fmul_rn(v[2], f)), "f"(__fmul_rn(v[3], f)),
-        "f"(__fmul_rn(v[4], f)), "f"(__fmul_rn(v[5], f)), "f"(__fmul_rn(v[6], f)), "f"(__fmul_rn(v[7], f)));
+      : "f"(v[0].x), "f"(v[0].y), "f"(v[1].x), "f"(v[1].y), "f"(v[2].x), "f"(v[2].y), "f"(v[3].x), "f"(v[3].y));
   return r;
 }
 // the e4m3 number nearest to v >= 0 (at most 448), and its value
@@ -175,123 +209,146 @@ __device__ __forceinline__ void store_chunk(const RowsParams& p, long long out_r
   }
 }
 
-// A chunk in registers -> its codes and scale byte -> every row it goes to
-template <int BLOCK>
-__device__ __forceinline__ void quantize_chunk(const float (&v)[kChunk], uint32_t top, const RowScale& row, uint2& codes, uint32_t& byte) {
+// A chunk in registers -> its codes and scale byte
+template <typename T, int BLOCK>
+__device__ __forceinline__ void quantize_chunk(const uint32_t (&w)[kWords<T>], uint32_t top, const RowScale& row, uint2& codes, uint32_t& byte) {
   float f;
   byte = block_scale<BLOCK>(top, row, f);
   // (a factor of zero would leave NaN where there is Inf)
-  codes = f > 0.0f ? make_uint2(pack8(v, f), pack8(v + 8, f)) : make_uint2(0u, 0u);
+  codes = f > 0.0f ? make_uint2(pack8<T>(w, 0, f), pack8<T>(w, 4, f)) : make_uint2(0u, 0u);
 }
 
-// WARPS warps share a row, a thread has CHUNKS of its chunks, every (32 * WARPS)-th.  CHUNKS = 0: any width, chunks are read
-// again for the second pass (from L2).
-template <typename T, int BLOCK, int WARPS, int CHUNKS>
-__global__ void __launch_bounds__(256) e2m1_rows_kernel(const RowsParams p) {
-  constexpr int kRowsPerBlock = 8 / WARPS;
-  __shared__ uint32_t box[8];
+// WARPS warps share a row; blocks walk over rows.  CHUNKS chunks of a thread, every (32 * WARPS)-th of the row; CHUNKS = 0: any width,
+// chunks are read again for the second pass (from L2).  PLAN: rows go where offsets and positions say.
+template <int WARPS> constexpr int kThreads = WARPS < 4 ? 128 : 32 * WARPS;
+template <typename T, int BLOCK, int WARPS, int CHUNKS, bool PLAN>
+__global__ void __launch_bounds__(kThreads<WARPS>) e2m1_rows_kernel(const RowsParams p) {
+  constexpr int kRowsPerBlock = kThreads<WARPS> / (32 * WARPS), kHeld = CHUNKS > 0 ? CHUNKS : 1;
+  __shared__ uint32_t box[2][kThreads<WARPS> / 32];
   pdl_wait();
   pdl_trigger();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int t = threadIdx.x % (32 * WARPS);
-  const long long r = static_cast<long long>(blockIdx.x) * kRowsPerBlock + warp / WARPS;
-  const bool there = r < p.rows;
-  const T* const x = static_cast<const T*>(p.x) + (there ? r : 0) * p.ld_x;
-  const int cols = there ? p.cols : 0;
   const int chunks = p.k_tiles * (4 * BLOCK / kChunk);        // with the padding of the last tile of scales
-  constexpr int kHeld = CHUNKS > 0 ? CHUNKS : 1;
-  float v[kHeld][kChunk];
-  uint32_t top[kHeld], row_top = 0;
-  if constexpr (CHUNKS > 0) {
+  const long long step = static_cast<long long>(gridDim.x) * kRowsPerBlock;
+  long long r = static_cast<long long>(blockIdx.x) * kRowsPerBlock + warp / WARPS;
+  uint32_t w[kHeld][kWords<T>], ahead[kHeld][kWords<T>];
+  auto fetch = [&](long long row) {
+    if constexpr (CHUNKS > 0) {
+      if (row < p.rows) {
 #pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) load_chunk16(x, (t + i * 32 * WARPS) * kChunk, cols, p.vec, v[i]);
-#pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) { top[i] = top_of(v[i]); row_top = max(row_top, top[i]); }
-  } else {
-    for (int c = t; c * kChunk < cols; c += 32 * WARPS) {
-      load_chunk16(x, c * kChunk, cols, p.vec, v[0]);
-      row_top = max(row_top, top_of(v[0]));
-    }
-  }
-  row_top = __reduce_max_sync(0xFFFFFFFFu, row_top);
-  if (WARPS > 1 && (BLOCK == 16 || CHUNKS == 0)) {            // (blocks of 32 need no maximum of the row, only its status)
-    if (lane == 0) box[warp] = row_top;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < WARPS; ++i) row_top = max(row_top, box[warp / WARPS * WARPS + i]);
-  }
-  if (!there) return;                                          // (whole warps, and no meeting follows)
-  RowScale row{};
-  if constexpr (BLOCK == 16) row = row_scale(row_top);
-  if (lane == 0) {
-    const bool bad = row_top >= 0x7F800000u, tiny = BLOCK == 16 && row_top < 0x0D800000u && row_top > 0;
-    if (bad || tiny) atomicOr(p.status, bad ? LUQ_STATUS_NONFINITE : LUQ_STATUS_RANGE);
-  }
-  auto put = [&](int chunk, uint2 codes, uint32_t byte) {
-    // (shuffles inside: every lane of the warp calls)
-    if (p.position == nullptr && p.offsets == nullptr) {
-      const long long plane = r / p.plane_rows, in_plane = r - plane * p.plane_rows;
-      store_chunk<BLOCK>(p, r, plane * ((p.plane_rows + 127) / 128) + in_plane / 128, static_cast<int>(in_plane % 128), true, chunk, codes, byte);
-      return;
-    }
-    for (int j = 0; j < p.copies; ++j) {
-      const int to = p.position ? *(p.position + r * p.copies + j) : static_cast<int>(r);
-      if (to < 0 || to >= p.out_rows) continue;                // warp-uniform
-      int tile_row = 0, in_tile = 0;
-      const bool tiled = group_of(p, to, tile_row, in_tile);
-      store_chunk<BLOCK>(p, to, tile_row, in_tile, tiled, chunk, codes, byte);
+        for (int i = 0; i < CHUNKS; ++i)
+          load_chunk16(static_cast<const T*>(p.x) + row * p.ld_x, (t + i * 32 * WARPS) * kChunk, p.cols, p.vec, ahead[i]);
+      }
     }
   };
-  if constexpr (CHUNKS > 0) {
+  fetch(r);
+  // (a block's warps stay together: rows that are not there are walked too)
+  for (int turn = 0; r - warp / WARPS < p.rows; r += step, ++turn) {
+    const bool there = r < p.rows;
+    const T* const x = static_cast<const T*>(p.x) + (there ? r : 0) * p.ld_x;
+    uint32_t top[kHeld] = {}, row_top = 0;
+    if constexpr (CHUNKS > 0) {
 #pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) {
-      uint32_t b = top[i], byte;
-      if (BLOCK == 32) b = max(b, __shfl_xor_sync(0xFFFFFFFFu, b, 1));
-      uint2 codes;
-      quantize_chunk<BLOCK>(v[i], b, row, codes, byte);
-      const int c = t + i * 32 * WARPS;
-      if (c - lane < chunks) put(c, codes, c < chunks ? byte : 0u);
-    }
-  } else {
-    for (int c = t; c - lane < chunks; c += 32 * WARPS) {
-      load_chunk16(x, c * kChunk, cols, p.vec, v[0]);
-      uint32_t b = top_of(v[0]), byte;
-      if (BLOCK == 32) b = max(b, __shfl_xor_sync(0xFFFFFFFFu, b, 1));
-      uint2 codes;
-      quantize_chunk<BLOCK>(v[0], b, row, codes, byte);
-      put(c, codes, c < chunks ? byte : 0u);
-    }
-  }
-  if (BLOCK == 16 && t == 0) {
-    if (p.position) {
-      for (int j = 0; j < p.copies; ++j) {
-        const int to = *(p.position + r * p.copies + j);
-        if (to >= 0 && to < p.out_rows) p.scale[to] = row.g;
-      }
+      for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+        for (int j = 0; j < kWords<T>; ++j) w[i][j] = ahead[i][j];
+      fetch(r + step);
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i) { top[i] = top_of<T>(w[i]); row_top = max(row_top, top[i]); }
     } else {
-      p.scale[r] = row.g;
+      for (int c = t; there && c * kChunk < p.cols; c += 32 * WARPS) {
+        load_chunk16(x, c * kChunk, p.cols, p.vec, w[0]);
+        row_top = max(row_top, top_of<T>(w[0]));
+      }
+    }
+    row_top = __reduce_max_sync(0xFFFFFFFFu, row_top);
+    if (WARPS > 1 && BLOCK == 16) {                            // (blocks of 32 need no maximum of the row: each warp reports its own)
+      if (lane == 0) box[turn & 1][warp] = row_top;
+      __syncthreads();                                         // (the box of the row before has been read by all: two are enough)
+      row_top = box[turn & 1][warp / WARPS * WARPS + lane % WARPS];
+      row_top = __reduce_max_sync(0xFFFFFFFFu, row_top);
+    }
+    if (!there) continue;                                      // (whole warps)
+    RowScale row{};
+    if constexpr (BLOCK == 16) row = row_scale(row_top);
+    if (row_top >= 0x7F800000u || (BLOCK == 16 && row_top < 0x0D800000u && row_top > 0)) {
+      if (lane == 0) atomicOr(p.status, row_top >= 0x7F800000u ? LUQ_STATUS_NONFINITE : LUQ_STATUS_RANGE);
+    }
+    long long tile_row = 0;
+    int in_tile = 0;
+    if constexpr (!PLAN) {
+      const long long plane = p.plane_rows == p.rows ? 0 : r / p.plane_rows, in_plane = r - plane * p.plane_rows;
+      tile_row = plane * ((p.plane_rows + 127) / 128) + in_plane / 128;
+      in_tile = static_cast<int>(in_plane % 128);
+    }
+    auto put = [&](int chunk, uint2 codes, uint32_t byte) {
+      // (shuffles inside: every lane of the warp calls)
+      if constexpr (!PLAN) {
+        store_chunk<BLOCK>(p, r, tile_row, in_tile, true, chunk, codes, byte);
+      } else {
+        for (int j = 0; j < p.copies; ++j) {
+          const int to = p.position ? *(p.position + r * p.copies + j) : static_cast<int>(r);
+          if (to < 0 || to >= p.out_rows) continue;            // warp-uniform
+          int group_row = 0, in_group = 0;
+          const bool tiled = group_of(p, to, group_row, in_group);
+          store_chunk<BLOCK>(p, to, group_row, in_group, tiled, chunk, codes, byte);
+        }
+      }
+    };
+    auto finish = [&](int i, int c) {
+      uint32_t b = CHUNKS > 0 ? top[i] : top_of<T>(w[i]), byte;
+      if (BLOCK == 32) b = max(b, __shfl_xor_sync(0xFFFFFFFFu, b, 1));
+      uint2 codes;
+      quantize_chunk<T, BLOCK>(w[i], b, row, codes, byte);
+      put(c, codes, c < chunks ? byte : 0u);
+    };
+    if constexpr (CHUNKS > 0) {
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i)
+        if (t - lane + i * 32 * WARPS < chunks) finish(i, t + i * 32 * WARPS);
+    } else {
+      for (int c = t; c - lane < chunks; c += 32 * WARPS) {
+        load_chunk16(x, c * kChunk, p.cols, p.vec, w[0]);
+        finish(0, c);
+      }
+    }
+    if (BLOCK == 16 && t == 0) {
+      if constexpr (PLAN) {
+        for (int j = 0; j < p.copies; ++j) {
+          const int to = p.position ? *(p.position + r * p.copies + j) : static_cast<int>(r);
+          if (to >= 0 && to < p.out_rows) p.scale[to] = row.g;
+        }
+      } else {
+        p.scale[r] = row.g;
+      }
     }
   }
 }
 
-template <typename T, int BLOCK, int WARPS, int CHUNKS>
+template <typename T, int BLOCK, int WARPS, int CHUNKS, bool PLAN>
 int launch(luq_ctx* ctx, const RowsParams& p, cudaStream_t st) {
-  constexpr int kRowsPerBlock = 8 / WARPS;
-  const long long blocks = (p.rows + kRowsPerBlock - 1) / kRowsPerBlock;
-  const cudaError_t e = luq_launch_kernel(e2m1_rows_kernel<T, BLOCK, WARPS, CHUNKS>, static_cast<int>(blocks), 256, 0, st, LUQ_LAUNCH_EARLY, 1, p);
+  constexpr int kRowsPerBlock = kThreads<WARPS> / (32 * WARPS);
+  const long long blocks = (p.rows + kRowsPerBlock - 1) / kRowsPerBlock, most = static_cast<long long>(ctx->sm_count) * (2048 / kThreads<WARPS>);
+  const cudaError_t e = luq_launch_kernel(e2m1_rows_kernel<T, BLOCK, WARPS, CHUNKS, PLAN>, static_cast<int>(blocks < most ? blocks : most),
+                                          kThreads<WARPS>, 0, st, LUQ_LAUNCH_EARLY, 1, p);
   if (e == cudaSuccess) ctx->launches += 1;
   return static_cast<int>(e);
 }
-template <typename T, int BLOCK>
+template <typename T, int BLOCK, bool PLAN>
 int launch_width(luq_ctx* ctx, const RowsParams& p, cudaStream_t st) {
   const int chunks = p.k_tiles * (4 * BLOCK / kChunk);
-  if (chunks <= 32) return launch<T, BLOCK, 1, 1>(ctx, p, st);
-  if (chunks <= 64) return launch<T, BLOCK, 2, 1>(ctx, p, st);
-  if (chunks <= 128) return launch<T, BLOCK, 4, 1>(ctx, p, st);
-  if (chunks <= 256) return launch<T, BLOCK, 8, 1>(ctx, p, st);
-  if (chunks <= 512) return launch<T, BLOCK, 8, 2>(ctx, p, st);
-  if (chunks <= 1024) return launch<T, BLOCK, 8, 4>(ctx, p, st);
-  return launch<T, BLOCK, 8, 0>(ctx, p, st);
+  if (chunks <= 32) return launch<T, BLOCK, 1, 1, PLAN>(ctx, p, st);
+  if (chunks <= 64) return launch<T, BLOCK, 2, 1, PLAN>(ctx, p, st);
+  if (chunks <= 128) return launch<T, BLOCK, 4, 1, PLAN>(ctx, p, st);
+  if (chunks <= 256) return launch<T, BLOCK, 8, 1, PLAN>(ctx, p, st);
+  if (chunks <= 512) return launch<T, BLOCK, 16, 1, PLAN>(ctx, p, st);
+  if (chunks <= 1024) return launch<T, BLOCK, 32, 1, PLAN>(ctx, p, st);
+  return launch<T, BLOCK, 32, 0, PLAN>(ctx, p, st);
+}
+template <typename T, int BLOCK>
+int launch_plan(luq_ctx* ctx, const RowsParams& p, cudaStream_t st) {
+  return p.offsets ? launch_width<T, BLOCK, true>(ctx, p, st) : launch_width<T, BLOCK, false>(ctx, p, st);
 }
 
 }  // namespace
@@ -304,6 +361,6 @@ int luq_launch_e2m1_rows(luq_ctx* ctx, const luq_e2m1_rows_args& a, cudaStream_t
   p.k_tiles = static_cast<int>(luq_e2m1_k_tiles(a.cols, a.block));
   p.status = ctx->d_status;
   p.vec = (reinterpret_cast<uintptr_t>(a.x) & 15u) == 0 && (a.rows <= 1 || a.ld_x * (a.dtype == LUQ_BF16 ? 2 : 4) % 16 == 0);
-  if (a.dtype == LUQ_BF16) return a.block == 16 ? launch_width<__nv_bfloat16, 16>(ctx, p, st) : launch_width<__nv_bfloat16, 32>(ctx, p, st);
-  return a.block == 16 ? launch_width<float, 16>(ctx, p, st) : launch_width<float, 32>(ctx, p, st);
+  if (a.dtype == LUQ_BF16) return a.block == 16 ? launch_plan<__nv_bfloat16, 16>(ctx, p, st) : launch_plan<__nv_bfloat16, 32>(ctx, p, st);
+  return a.block == 16 ? launch_plan<float, 16>(ctx, p, st) : launch_plan<float, 32>(ctx, p, st);
 }
