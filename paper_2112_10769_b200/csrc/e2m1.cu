@@ -8,8 +8,8 @@
 // 2688 = 6 * 448: the row's largest block gets the largest e4m3 number, its largest element the largest e2m1 number.  A block
 // that is less than 2^-10 of the row's scale has a zero scale and zero numbers.
 //
-// Warps that share a row walk over rows; a thread holds chunks of 16 neighbouring elements in registers, and the next row's are on
-// their way meanwhile, so x is read once; the row's maximum meets in shared memory.  Block scales leave in the tiles that the
+// Warps that share a row walk over rows; a thread holds chunks of 16 neighbouring elements in registers, so x is read once; the row's
+// maximum meets in shared memory.  Block scales leave in the tiles that the
 // tensor cores copy (128 rows x 4 blocks, row r, block b at 16 (r mod 32) + 4 (r / 32) + b): the threads of four blocks put
 // their bytes together and one stores the word.
 #include <cuda_bf16.h>
@@ -183,29 +183,43 @@ __device__ __forceinline__ bool group_of(const RowsParams& p, int row, int& tile
   return true;
 }
 
+// Where a thread's chunk lies in every row: nothing here depends on the row.
 template <int BLOCK>
-__device__ __forceinline__ void store_chunk(const RowsParams& p, long long out_row, long long tile_row, int in_tile, bool tiled, int chunk,
-                                            uint2 codes, uint32_t byte) {
-  const int lane = threadIdx.x & 31;
-  // the word of four blocks' scales (blocks of 32 are two threads)
-  constexpr int kThreads = BLOCK == 16 ? 4 : 8;
-  uint32_t word = byte << (8 * (BLOCK == 16 ? lane & 3 : (lane >> 1) & 3));
-  if (BLOCK == 32) word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
-  else word |= __shfl_xor_sync(0xFFFFFFFFu, word, 1);
-  word |= __shfl_xor_sync(0xFFFFFFFFu, word, 2);
-  const int kt = chunk / kThreads;
-  if (tiled && (lane & (kThreads - 1)) == 0 && kt < p.k_tiles &&
-      LUQ_IN_BOUNDS(tile_row >= 0 && in_tile >= 0 && in_tile < 128, p.status))
-    *reinterpret_cast<uint32_t*>(p.tiles + (tile_row * p.k_tiles + kt) * kScaleTile + (in_tile & 31) * 16 + (in_tile >> 5) * 4) = word;
-  const int first = chunk * (kChunk / 2), bytes = (p.cols + 1) / 2 - first;
-  if (bytes <= 0 || !LUQ_IN_BOUNDS(out_row >= 0 && out_row < p.out_rows, p.status)) return;
-  uint8_t* const to = p.codes + out_row * p.ld_codes + first;
-  if (bytes >= 8) {
+struct Place {
+  int bytes;             // of its codes that belong to the row, 8 at most
+  long long code, tile;  // offsets of its codes, and of the word of four blocks' scales (negative: another thread stores it)
+  int shift;             // its scale's place in that word
+  __device__ __forceinline__ Place(const RowsParams& p, int chunk) {
+    constexpr int kThreads4 = BLOCK == 16 ? 4 : 8;          // (blocks of 32 are two threads)
+    const int lane = threadIdx.x & 31, kt = chunk / kThreads4;
+    code = chunk * (kChunk / 2);
+    bytes = min(max((p.cols + 1) / 2 - chunk * (kChunk / 2), 0), 8);
+    tile = (lane & (kThreads4 - 1)) == 0 && kt < p.k_tiles ? static_cast<long long>(kt) * kScaleTile : -1;
+    shift = 8 * (BLOCK == 16 ? lane & 3 : (lane >> 1) & 3);
+  }
+};
+// the scales' bytes of four blocks in one word
+template <int BLOCK>
+__device__ __forceinline__ uint32_t scale_word(uint32_t byte, int shift) {
+  uint32_t word = byte << shift;
+  word |= __shfl_xor_sync(0xFFFFFFFFu, word, BLOCK == 16 ? 1 : 4);
+  return word | __shfl_xor_sync(0xFFFFFFFFu, word, 2);
+}
+__device__ __forceinline__ long long tile_offset(const RowsParams& p, int tile_row, int in_tile) {
+  return static_cast<long long>(tile_row) * (p.k_tiles * static_cast<long long>(kScaleTile)) + (in_tile & 31) * 16 + (in_tile >> 5) * 4;
+}
+template <int BLOCK>
+__device__ __forceinline__ void store_chunk(const RowsParams& p, const Place<BLOCK>& at, int out_row, long long tiles_from, bool tiled, uint2 codes,
+                                            uint32_t word) {
+  if (!LUQ_IN_BOUNDS(out_row >= 0 && out_row < p.out_rows, p.status)) return;
+  if (tiled && at.tile >= 0) *reinterpret_cast<uint32_t*>(p.tiles + tiles_from + at.tile) = word;
+  uint8_t* const to = p.codes + out_row * p.ld_codes + at.code;
+  if (at.bytes == 8) {
     *reinterpret_cast<uint2*>(to) = codes;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < bytes) to[i] = static_cast<uint8_t>((i < 4 ? codes.x : codes.y) >> (8 * (i & 3)));
+    for (int i = 0; i < 7; ++i)
+      if (i < at.bytes) to[i] = static_cast<uint8_t>((i < 4 ? codes.x : codes.y) >> (8 * (i & 3)));
   }
 }
 
@@ -218,105 +232,105 @@ __device__ __forceinline__ void quantize_chunk(const uint32_t (&w)[kWords<T>], u
   codes = f > 0.0f ? make_uint2(pack8<T>(w, 0, f), pack8<T>(w, 4, f)) : make_uint2(0u, 0u);
 }
 
-// WARPS warps share a row; blocks walk over rows.  CHUNKS chunks of a thread, every (32 * WARPS)-th of the row; CHUNKS = 0: any width,
-// chunks are read again for the second pass (from L2).  PLAN: rows go where offsets and positions say.
-template <int WARPS> constexpr int kThreads = WARPS < 4 ? 128 : 32 * WARPS;
-template <typename T, int BLOCK, int WARPS, int CHUNKS, bool PLAN>
-__global__ void __launch_bounds__(kThreads<WARPS>) e2m1_rows_kernel(const RowsParams p) {
-  constexpr int kRowsPerBlock = kThreads<WARPS> / (32 * WARPS), kHeld = CHUNKS > 0 ? CHUNKS : 1;
-  __shared__ uint32_t box[2][kThreads<WARPS> / 32];
+// LANES lanes (kBlockRow: a block, of any number of warps) share a row; blocks walk over rows.  CHUNKS chunks of a thread, every
+// LANES-th of the row; CHUNKS = 0: any width, chunks are read again for the second pass (from L2).  PLAN: rows go where offsets and
+// positions say.
+constexpr int kBlockRow = 0;
+template <typename T, int BLOCK, int LANES, int CHUNKS, bool PLAN>
+__global__ void __launch_bounds__(LANES == kBlockRow ? 1024 : 128) e2m1_rows_kernel(const RowsParams p) {
+  static_assert(!PLAN || LANES == kBlockRow || LANES == 32, "a plan is read by whole warps");
+  constexpr int kHeld = CHUNKS > 0 ? CHUNKS : 1;
+  __shared__ uint32_t box[2][32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int lanes = LANES == kBlockRow ? static_cast<int>(blockDim.x) : LANES, per_block = LANES == kBlockRow ? 1 : 128 / (LANES == kBlockRow ? 1 : LANES);
+  const int t = LANES == kBlockRow ? static_cast<int>(threadIdx.x) : static_cast<int>(threadIdx.x) % (LANES == kBlockRow ? 1 : LANES);
+  const int chunks = p.k_tiles * (4 * BLOCK / kChunk);        // with the padding of the last tile of scales
+  const int rows = static_cast<int>(p.rows), step = static_cast<int>(gridDim.x) * per_block;
+  const long long plane_tiles = (p.plane_rows + 127) / 128;
   pdl_wait();
   pdl_trigger();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int t = threadIdx.x % (32 * WARPS);
-  const int chunks = p.k_tiles * (4 * BLOCK / kChunk);        // with the padding of the last tile of scales
-  const long long step = static_cast<long long>(gridDim.x) * kRowsPerBlock;
-  long long r = static_cast<long long>(blockIdx.x) * kRowsPerBlock + warp / WARPS;
-  uint32_t w[kHeld][kWords<T>], ahead[kHeld][kWords<T>];
-  auto fetch = [&](long long row) {
-    if constexpr (CHUNKS > 0) {
-      if (row < p.rows) {
-#pragma unroll
-        for (int i = 0; i < CHUNKS; ++i)
-          load_chunk16(static_cast<const T*>(p.x) + row * p.ld_x, (t + i * 32 * WARPS) * kChunk, p.cols, p.vec, ahead[i]);
-      }
-    }
-  };
-  fetch(r);
-  // (a block's warps stay together: rows that are not there are walked too)
-  for (int turn = 0; r - warp / WARPS < p.rows; r += step, ++turn) {
-    const bool there = r < p.rows;
+  int turn = 0;
+  for (int first = static_cast<int>(blockIdx.x) * per_block; first < rows; first += step, turn ^= 1) {
+    const int r = first + (LANES == kBlockRow ? 0 : static_cast<int>(threadIdx.x) / (LANES == kBlockRow ? 1 : LANES));
+    const bool there = r < rows;
+    if (LANES == 32 && !there) break;                          // (a whole warp; nothing meets)
     const T* const x = static_cast<const T*>(p.x) + (there ? r : 0) * p.ld_x;
-    uint32_t top[kHeld] = {}, row_top = 0;
+    uint32_t w[kHeld][kWords<T>], top[kHeld] = {}, row_top = 0;
     if constexpr (CHUNKS > 0) {
 #pragma unroll
-      for (int i = 0; i < CHUNKS; ++i)
-#pragma unroll
-        for (int j = 0; j < kWords<T>; ++j) w[i][j] = ahead[i][j];
-      fetch(r + step);
+      for (int i = 0; i < CHUNKS; ++i) load_chunk16(x, (t + i * lanes) * kChunk, p.cols, p.vec, w[i]);
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) { top[i] = top_of<T>(w[i]); row_top = max(row_top, top[i]); }
     } else {
-      for (int c = t; there && c * kChunk < p.cols; c += 32 * WARPS) {
+      for (int c = t; c * kChunk < p.cols; c += lanes) {
         load_chunk16(x, c * kChunk, p.cols, p.vec, w[0]);
         row_top = max(row_top, top_of<T>(w[0]));
       }
     }
-    row_top = __reduce_max_sync(0xFFFFFFFFu, row_top);
-    if (WARPS > 1 && BLOCK == 16) {                            // (blocks of 32 need no maximum of the row: each warp reports its own)
-      if (lane == 0) box[turn & 1][warp] = row_top;
-      __syncthreads();                                         // (the box of the row before has been read by all: two are enough)
-      row_top = box[turn & 1][warp / WARPS * WARPS + lane % WARPS];
+    if constexpr (LANES == kBlockRow || LANES == 32) {
       row_top = __reduce_max_sync(0xFFFFFFFFu, row_top);
+    } else {
+#pragma unroll
+      for (int o = LANES / 2; o; o >>= 1) row_top = max(row_top, __shfl_xor_sync(0xFFFFFFFFu, row_top, o));
     }
-    if (!there) continue;                                      // (whole warps)
+    if (LANES == kBlockRow && BLOCK == 16) {                   // (blocks of 32 need no maximum of the row: each warp reports its own)
+      if (lane == 0) box[turn][warp] = row_top;
+      __syncthreads();                                         // (the box of the row before has been read by all: two are enough)
+      row_top = __reduce_max_sync(0xFFFFFFFFu, lane * 32 < lanes ? box[turn][lane] : 0u);
+    }
     RowScale row{};
     if constexpr (BLOCK == 16) row = row_scale(row_top);
     if (row_top >= 0x7F800000u || (BLOCK == 16 && row_top < 0x0D800000u && row_top > 0)) {
-      if (lane == 0) atomicOr(p.status, row_top >= 0x7F800000u ? LUQ_STATUS_NONFINITE : LUQ_STATUS_RANGE);
+      if ((LANES == kBlockRow ? lane : t) == 0 && there) atomicOr(p.status, row_top >= 0x7F800000u ? LUQ_STATUS_NONFINITE : LUQ_STATUS_RANGE);
     }
-    long long tile_row = 0;
-    int in_tile = 0;
-    if constexpr (!PLAN) {
-      const long long plane = p.plane_rows == p.rows ? 0 : r / p.plane_rows, in_plane = r - plane * p.plane_rows;
-      tile_row = plane * ((p.plane_rows + 127) / 128) + in_plane / 128;
-      in_tile = static_cast<int>(in_plane % 128);
-    }
-    auto put = [&](int chunk, uint2 codes, uint32_t byte) {
-      // (shuffles inside: every lane of the warp calls)
+    // calls f(row to write, offset of its scales' words, have they a place) for every place that the row goes to
+    auto places = [&](auto f) {
       if constexpr (!PLAN) {
-        store_chunk<BLOCK>(p, r, tile_row, in_tile, true, chunk, codes, byte);
+        if (!there) return;
+        if (p.plane_rows == p.rows) {
+          f(r, tile_offset(p, r / 128, r % 128), true);
+        } else {
+          const int plane = r / static_cast<int>(p.plane_rows), in_plane = r - plane * static_cast<int>(p.plane_rows);
+          f(r, tile_offset(p, static_cast<int>(plane * plane_tiles) + in_plane / 128, in_plane % 128), true);
+        }
       } else {
         for (int j = 0; j < p.copies; ++j) {
-          const int to = p.position ? *(p.position + r * p.copies + j) : static_cast<int>(r);
+          const int to = p.position ? *(p.position + static_cast<long long>(r) * p.copies + j) : r;
           if (to < 0 || to >= p.out_rows) continue;            // warp-uniform
-          int group_row = 0, in_group = 0;
-          const bool tiled = group_of(p, to, group_row, in_group);
-          store_chunk<BLOCK>(p, to, group_row, in_group, tiled, chunk, codes, byte);
+          int tile_row = 0, in_tile = 0;
+          const bool tiled = group_of(p, to, tile_row, in_tile);
+          f(to, tile_offset(p, tile_row, in_tile), tiled);
         }
       }
     };
-    auto finish = [&](int i, int c) {
-      uint32_t b = CHUNKS > 0 ? top[i] : top_of<T>(w[i]), byte;
+    auto finish = [&](const uint32_t (&v)[kWords<T>], uint32_t b, int c, uint2& codes) {        // codes, and the scales' word
+      uint32_t byte;
       if (BLOCK == 32) b = max(b, __shfl_xor_sync(0xFFFFFFFFu, b, 1));
-      uint2 codes;
-      quantize_chunk<T, BLOCK>(w[i], b, row, codes, byte);
-      put(c, codes, c < chunks ? byte : 0u);
+      quantize_chunk<T, BLOCK>(v, b, row, codes, byte);
+      return scale_word<BLOCK>(c < chunks ? byte : 0u, Place<BLOCK>(p, c).shift);
     };
     if constexpr (CHUNKS > 0) {
+      uint2 codes[kHeld];
+      uint32_t word[kHeld];
 #pragma unroll
-      for (int i = 0; i < CHUNKS; ++i)
-        if (t - lane + i * 32 * WARPS < chunks) finish(i, t + i * 32 * WARPS);
+      for (int i = 0; i < CHUNKS; ++i) word[i] = finish(w[i], top[i], t + i * lanes, codes[i]);
+      places([&](int to, long long tiles_from, bool tiled) {
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) store_chunk<BLOCK>(p, Place<BLOCK>(p, t + i * lanes), to, tiles_from, tiled, codes[i], word[i]);
+      });
     } else {
-      for (int c = t; c - lane < chunks; c += 32 * WARPS) {
+      for (int c = t; c - lane < chunks; c += lanes) {
         load_chunk16(x, c * kChunk, p.cols, p.vec, w[0]);
-        finish(0, c);
+        uint2 codes;
+        const uint32_t word = finish(w[0], top_of<T>(w[0]), c, codes);
+        const Place<BLOCK> at(p, c);
+        places([&](int to, long long tiles_from, bool tiled) { store_chunk<BLOCK>(p, at, to, tiles_from, tiled, codes, word); });
       }
     }
-    if (BLOCK == 16 && t == 0) {
+    if (BLOCK == 16 && t == 0 && there) {
       if constexpr (PLAN) {
         for (int j = 0; j < p.copies; ++j) {
-          const int to = p.position ? *(p.position + r * p.copies + j) : static_cast<int>(r);
+          const int to = p.position ? *(p.position + static_cast<long long>(r) * p.copies + j) : r;
           if (to >= 0 && to < p.out_rows) p.scale[to] = row.g;
         }
       } else {
@@ -326,25 +340,32 @@ __global__ void __launch_bounds__(kThreads<WARPS>) e2m1_rows_kernel(const RowsPa
   }
 }
 
-template <typename T, int BLOCK, int WARPS, int CHUNKS, bool PLAN>
-int launch(luq_ctx* ctx, const RowsParams& p, cudaStream_t st) {
-  constexpr int kRowsPerBlock = kThreads<WARPS> / (32 * WARPS);
-  const long long blocks = (p.rows + kRowsPerBlock - 1) / kRowsPerBlock, most = static_cast<long long>(ctx->sm_count) * (2048 / kThreads<WARPS>);
-  const cudaError_t e = luq_launch_kernel(e2m1_rows_kernel<T, BLOCK, WARPS, CHUNKS, PLAN>, static_cast<int>(blocks < most ? blocks : most),
-                                          kThreads<WARPS>, 0, st, LUQ_LAUNCH_EARLY, 1, p);
+template <typename T, int BLOCK, int LANES, int CHUNKS, bool PLAN>
+int launch(luq_ctx* ctx, const RowsParams& p, int threads, cudaStream_t st) {
+  const int per_block = LANES == kBlockRow ? 1 : 128 / (LANES == kBlockRow ? 1 : LANES);
+  // bf16: as many blocks as may be resident at once, which walk (16384 x 4096, blocks of 32: 27.8 us, 29.2 with a block for every
+  // row); fp32: a block for every row (44.8 us, walking 49.3)
+  const long long blocks = (p.rows + per_block - 1) / per_block, most = sizeof(T) == 2 ? static_cast<long long>(ctx->sm_count) * (2048 / threads) : blocks;
+  const cudaError_t e = luq_launch_kernel(e2m1_rows_kernel<T, BLOCK, LANES, CHUNKS, PLAN>, static_cast<int>(blocks < most ? blocks : most), threads, 0,
+                                          st, LUQ_LAUNCH_EARLY, 1, p);
   if (e == cudaSuccess) ctx->launches += 1;
   return static_cast<int>(e);
 }
+// Narrow rows share a warp.  A thread takes two chunks where there are rows enough to fill the card (the steps that a row costs are
+// shared: 16384 x 4096 bf16, blocks of 16: 33 us, with one chunk 44, with four 43), one where a few rows' latency counts.
 template <typename T, int BLOCK, bool PLAN>
 int launch_width(luq_ctx* ctx, const RowsParams& p, cudaStream_t st) {
   const int chunks = p.k_tiles * (4 * BLOCK / kChunk);
-  if (chunks <= 32) return launch<T, BLOCK, 1, 1, PLAN>(ctx, p, st);
-  if (chunks <= 64) return launch<T, BLOCK, 2, 1, PLAN>(ctx, p, st);
-  if (chunks <= 128) return launch<T, BLOCK, 4, 1, PLAN>(ctx, p, st);
-  if (chunks <= 256) return launch<T, BLOCK, 8, 1, PLAN>(ctx, p, st);
-  if (chunks <= 512) return launch<T, BLOCK, 16, 1, PLAN>(ctx, p, st);
-  if (chunks <= 1024) return launch<T, BLOCK, 32, 1, PLAN>(ctx, p, st);
-  return launch<T, BLOCK, 32, 0, PLAN>(ctx, p, st);
+  if constexpr (!PLAN) {
+    if (chunks <= 8) return launch<T, BLOCK, 8, 1, PLAN>(ctx, p, 128, st);
+    if (chunks <= 16) return launch<T, BLOCK, 16, 1, PLAN>(ctx, p, 128, st);
+  }
+  if (chunks <= 32) return launch<T, BLOCK, 32, 1, PLAN>(ctx, p, 128, st);
+  const bool many = p.rows >= 4ll * ctx->sm_count;
+  if (chunks <= 64 && many) return launch<T, BLOCK, 32, 2, PLAN>(ctx, p, 128, st);
+  if (chunks <= 1024 && !many) return launch<T, BLOCK, kBlockRow, 1, PLAN>(ctx, p, (chunks + 31) / 32 * 32, st);
+  if (chunks <= 2048) return launch<T, BLOCK, kBlockRow, 2, PLAN>(ctx, p, (chunks + 63) / 64 * 32, st);
+  return launch<T, BLOCK, kBlockRow, 0, PLAN>(ctx, p, 1024, st);
 }
 template <typename T, int BLOCK>
 int launch_plan(luq_ctx* ctx, const RowsParams& p, cudaStream_t st) {
