@@ -20,7 +20,7 @@
 //              owns the tensor-memory allocation: the accumulators, and a place for the scales of every stage, which is
 //              free when the stage is
 //   warp 2     TMA producer of the tile's token rows x 128 bytes and their scales
-//   warps 3..  epilogue: tcgen05.ld -> row scales, bias -> staged 32 x 32 boxes -> TMA store; token rows
+//   warps 3..  epilogue: tcgen05.ld -> row scales, bias -> staged boxes of 32 channels -> TMA store; token rows
 //              that share a box with another group's, and outputs TMA cannot address, are stored directly
 // All waits are bounded; on expiry the CTA flags LUQ_STATUS_TIMEOUT, drains its copies, frees its
 // tensor memory and returns.
@@ -39,7 +39,8 @@ constexpr int kSlab = kCh * kBk;          // bytes of W per stage
 constexpr int kScaleTile = 512;           // 128 rows x 4 block scales
 constexpr int kXWarp = 2;
 constexpr int kFirstEpiWarp = 3;
-constexpr int kWarpStaging = 32 * 32 * 4; // a warp's store boxes: one of 32 x 32 fp32, or two of bf16
+constexpr int kBox = 2048;                // a store box of 32 channels: 32 tokens bf16, 16 tokens fp32
+constexpr int kWarpStaging = 2 * kBox;    // a warp fills one while the other is read
 constexpr int kMaxSplit = 8;              // CTAs that share a tile's contraction (a portable cluster)
 
 struct E2m1Params {
@@ -140,6 +141,21 @@ __device__ __forceinline__ void tc_copy_scales(uint32_t taddr, uint64_t desc) {
 __device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
   return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | static_cast<uint64_t>(8) << 32 | static_cast<uint64_t>(1) << 46;
 }
+// 16 lanes x 32 columns of accumulators: thread t gets rows t / 4 (registers 4 i, 4 i + 1) and t / 4 + 8 (4 i + 2, 4 i + 3),
+// columns 8 i + 2 (t mod 4) and the next
+__device__ __forceinline__ void tmem_ld_16x32(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+// four 8 x 8 matrices of 16-bit numbers, transposed: thread t gives the address of row t mod 8 of matrix t / 8
+__device__ __forceinline__ void stmatrix_trans(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
 __device__ __forceinline__ float ld_shared_cluster_f32(uint32_t cluster_addr) { return __int_as_float(ld_shared_cluster(cluster_addr)); }
 
 // is [row, ch] an output?  (always true outside the checking build)
@@ -155,18 +171,19 @@ __device__ __forceinline__ float2 scale2(uint32_t a0, uint32_t a1, float2 sw, fl
 
 // Takes a tile's accumulators out of tensor memory, scales them and writes them: this warp's quarter of the
 // lanes (32 channels) and its group's tokens, in steps of 32, two steps' accumulators in registers at a time.
-// A full step goes through a staged box [token][channel] and a copy; a step that holds rows of another
-// group, or an output the copies cannot address, is written element by element (32 channels in a row).
-// One fence serves all boxes a warp has (two of bf16, one of fp32).
+// bf16: a thread gets two tokens of a channel, eight channels' words turn to eight tokens' on their way to a box (stmatrix), whose
+// 16-byte pieces are swizzled so that no two rows meet in a bank (with a lane for a channel, shuffles and word stores a tile took
+// 3.0 us).  A full box is handed to the copy engine, of one that holds rows of another group the warp stores its own.  fp32: as many
+// boxes of 16 tokens.  An output the copies cannot address is stored from registers, a lane for a channel (8192 x 4097 x 1024 bf16:
+// 32 us, 52 from boxes).
 // On a pair the two groups of warps take every other step, the steps that the next tile's accumulators share first;
-// `taken` is called once, when those (elsewhere all) are in registers.
+// `taken` is called once, when those (elsewhere all) are in registers.  `used` counts the boxes.
 template <typename C, bool BF16, bool PAIR, typename Taken>
 __device__ __forceinline__ void write_tile(const E2m1Params& p, const void* tm_z, const Unit& v, float sw, float bias,
                                            uint32_t taddr, uint32_t buf, uint32_t tmem_base, int warp_e, int lane, uint32_t staging,
-                                           uint8_t* gen, const float* scales, Taken taken) {
+                                           uint8_t* gen, const float* scales, uint32_t& used, Taken taken) {
   constexpr int CH = C::chunk, kSteps = C::span / CH, kPair = 2;
   static_assert(kSteps % kPair == 0);
-  constexpr int kBoxes = BF16 ? 2 : 1, kBoxBytes = kWarpStaging / kBoxes;
   const int quarter = (warp_e + kFirstEpiWarp) & 3, group = warp_e >> 2;
   const int ch_first = v.ch0 + quarter * 32, ch = ch_first + lane;
   // columns 160 .. 255 of the first accumulators are 0 .. 95 of the second
@@ -174,30 +191,45 @@ __device__ __forceinline__ void write_tile(const E2m1Params& p, const void* tm_z
   static_assert(!PAIR || (C::second == 5 * CH && C::span == 4 * CH));
   const bool channels = ch_first < p.N;                // warp-uniform
   const bool boxes = p.z_tma && (ch_first + 32 <= p.N || p.tma_cols == p.N);
-  const float2 sw2 = make_float2(sw, sw), bias2 = make_float2(bias, bias);
   const uint32_t slot = static_cast<uint32_t>(warp_e) * kWarpStaging;
-  uint8_t* const box0 = gen + C::staging + slot;
-
-  int staged = 0, staged_at[kBoxes];
-  auto flush = [&]() {                                 // hands the staged boxes to the copy engine
-    fence_proxy_async();
+  // the box to fill next: the copy that last read it has ended
+  auto open_box = [&]() {
+    if (lane == 0) bulk_wait_read<1>();
+    __syncwarp();
+    return slot + (used & 1u) * kBox;
+  };
+  auto close_box = [&](uint32_t at, int token, int tokens, bool copy) {          // (an empty group counts for a box without a copy)
+    if (copy) fence_proxy_async();
     __syncwarp();
     if (lane == 0) {
-#pragma unroll
-      for (int i = 0; i < kBoxes; ++i)
-        if (i < staged && z_in(p, v.row0 + staged_at[i] + 31, min(ch_first + 31, static_cast<int>(p.N) - 1)))
-          tma_store_2d(tm_z, staging + slot + i * kBoxBytes, ch_first, v.row0 + staged_at[i]);
+      if (copy && z_in(p, v.row0 + token + tokens - 1, min(ch_first + 31, static_cast<int>(p.N) - 1))) tma_store_2d(tm_z, staging + at, ch_first, v.row0 + token);
       bulk_commit();
     }
-    staged = 0;
+    ++used;
   };
+  float2 sw4[4], bias4[4];                             // bf16: of this thread's four channels, twice
+  if constexpr (BF16) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float a = __shfl_sync(0xFFFFFFFFu, sw, lane / 4 + 8 * j), b = __shfl_sync(0xFFFFFFFFu, bias, lane / 4 + 8 * j);
+      sw4[j] = make_float2(a, a);
+      bias4[j] = make_float2(b, b);
+    }
+  }
 #pragma unroll 1
   for (int pair = 0; pair < kSteps; pair += kPair) {
     uint32_t r[kPair][CH];
 #pragma unroll
     for (int i = 0; i < kPair; ++i) {
       const int c0 = first_token(pair + i);
-      if (channels && c0 < v.rows && tmem_in(taddr + c0, tmem_base, C::first_scale, p.status, CH)) load_chunk<CH>(taddr + c0, r[i]);
+      if (channels && c0 < v.rows && tmem_in(taddr + c0, tmem_base, C::first_scale, p.status, CH)) {
+        if (BF16 && boxes) {
+          tmem_ld_16x32(taddr + c0, r[i]);
+          tmem_ld_16x32(taddr + c0 + (16u << 16), r[i] + 16);
+        } else {
+          load_chunk<CH>(taddr + c0, r[i]);
+        }
+      }
     }
     tmem_ld_wait();
     if (pair == (PAIR ? 0 : kSteps - kPair)) taken();
@@ -205,59 +237,74 @@ __device__ __forceinline__ void write_tile(const E2m1Params& p, const void* tm_z
 #pragma unroll
     for (int step = 0; step < kPair; ++step) {
       const int c0 = first_token(pair + step), left = v.rows - c0;
-      if (boxes && left >= 32) {
-        if (staged == 0) {                               // (first of its pair) the stores that last read this warp's boxes are done
-          if (lane == 0) bulk_wait_read<0>();
-          __syncwarp();
+      if (left <= 0) continue;
+      if (BF16 && boxes) {
+        const uint32_t at = open_box();
+        const int row = lane & 7;
+        const uint32_t to = staging + at + row * 64 + (((lane >> 3) ^ (row >> 1)) << 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                  // eight tokens
+          const float2 s2 = *reinterpret_cast<const float2*>(scales + c0 + 8 * i + 2 * (lane & 3));
+          uint32_t word[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {                // eight channels
+            const uint32_t* const acc = r[step] + 16 * (j >> 1) + 4 * i + 2 * (j & 1);
+            const float2 z = scale2(acc[0], acc[1], sw4[j], s2, bias4[j]);
+            const __nv_bfloat162 h = __floats2bfloat162_rn(z.x, z.y);
+            word[j] = *reinterpret_cast<const uint32_t*>(&h);
+          }
+          if (smem_in(gen + (to - staging) + C::staging + i * 512, gen, C::staging, C::token_scales, 16, p.status))
+            stmatrix_trans(to + i * 512, word[0], word[1], word[2], word[3]);
         }
-        uint8_t* const box = box0 + staged * kBoxBytes;
+        const bool copy = left >= 32;
+        if (!copy) {
+          __syncwarp();
+          if (ch < p.N) {                              // a lane for a channel
+            uint16_t* z = static_cast<uint16_t*>(p.z) + (static_cast<long long>(v.row0) + c0) * p.ld_z + ch;
+#pragma unroll 4
+            for (int i = 0; i < left; ++i, z += p.ld_z) {
+              const uint8_t* const from = gen + C::staging + at + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + (lane & 7) * 2;
+              if (smem_in(from, gen, C::staging, C::token_scales, 2, p.status) && z_in(p, v.row0 + c0 + i, ch)) *z = *reinterpret_cast<const uint16_t*>(from);
+            }
+          }
+        }
+        close_box(at, c0, 32, copy);
+      } else {
+        const float2 sw2 = make_float2(sw, sw), bias2 = make_float2(bias, bias);
 #pragma unroll
-        for (int i = 0; i < kBoxes; ++i)
-          if (i == staged) staged_at[i] = c0;
-        ++staged;
-        // all scales first: between the stores below every load would wait for the last store
-        float4 s_step[CH / 4];
+        for (int half = 0; half < CH; half += 16) {
+          if (!BF16 && boxes && left >= half + 16) {
+            const uint32_t at = open_box();
+            uint8_t* const box = gen + C::staging + at;
+            // all scales first: between the stores below every load would wait for the last store
+            float4 s_step[4];
 #pragma unroll
-        for (int i = 0; i < CH / 4; ++i) s_step[i] = reinterpret_cast<const float4*>(scales + c0)[i];
+            for (int i = 0; i < 4; ++i) s_step[i] = reinterpret_cast<const float4*>(scales + c0 + half)[i];
 #pragma unroll
-        for (int i = 0; i < CH; i += 4) {
-          const float4 s4 = s_step[i / 4];
-          const float2 z[2] = {scale2(r[step][i], r[step][i + 1], sw2, make_float2(s4.x, s4.y), bias2),
-                               scale2(r[step][i + 2], r[step][i + 3], sw2, make_float2(s4.z, s4.w), bias2)};
+            for (int i = 0; i < 16; i += 2) {
+              const float4 s4 = s_step[i / 4];
+              const float2 z = scale2(r[step][half + i], r[step][half + i + 1], sw2, i % 4 ? make_float2(s4.z, s4.w) : make_float2(s4.x, s4.y), bias2);
+              uint8_t* const to = box + i * 128 + lane * 4;
+              if (smem_in(to, gen, C::staging, C::token_scales, 132, p.status)) {
+                *reinterpret_cast<float*>(to) = z.x;
+                *reinterpret_cast<float*>(to + 128) = z.y;
+              }
+            }
+            close_box(at, c0 + half, 16, true);
+          } else if (left > half && ch < p.N) {
+            const long long z0 = (static_cast<long long>(v.row0) + c0 + half) * p.ld_z + ch;
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            if constexpr (BF16) {
-              // a lane has one channel of two tokens, a word is two channels of one: neighbours swap halves, the
-              // even lane keeps the first token's word, the odd lane the second's
-              const __nv_bfloat162 h = __floats2bfloat162_rn(z[j].x, z[j].y);
-              const uint32_t own = *reinterpret_cast<const uint32_t*>(&h);
-              const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, own, 1);
-              const uint32_t word = __byte_perm(own, other, lane & 1 ? 0x3276 : 0x5410);
-              uint8_t* const at = box + (i + 2 * j + (lane & 1)) * 64 + (lane >> 1) * 4;
-              if (smem_in(at, gen, C::staging, C::token_scales, 4, p.status)) *reinterpret_cast<uint32_t*>(at) = word;
-            } else {
-              uint8_t* const at = box + (i + 2 * j) * 128 + lane * 4;
-              if (smem_in(at, gen, C::staging, C::token_scales, 132, p.status)) {
-                *reinterpret_cast<float*>(at) = z[j].x;
-                *reinterpret_cast<float*>(at + 128) = z[j].y;
+            for (int i = 0; i < 16; i += 2) {
+              if (half + i < left) {
+                const float2 z = scale2(r[step][half + i], r[step][half + i + 1], sw2, make_float2(scales[c0 + half + i], scales[c0 + half + i + 1]), bias2);
+                if (z_in(p, v.row0 + c0 + half + i, ch)) store_z(p.z, z0 + i * p.ld_z, z.x, BF16);
+                if (half + i + 1 < left && z_in(p, v.row0 + c0 + half + i + 1, ch)) store_z(p.z, z0 + (i + 1) * p.ld_z, z.y, BF16);
               }
             }
           }
         }
-        if (staged == kBoxes) flush();
-      } else if (left > 0 && ch < p.N) {
-        const long long z0 = (static_cast<long long>(v.row0) + c0) * p.ld_z + ch;
-#pragma unroll
-        for (int i = 0; i < CH; i += 2) {
-          if (i < left) {
-            const float2 z = scale2(r[step][i], r[step][i + 1], sw2, make_float2(scales[c0 + i], scales[c0 + i + 1]), bias2);
-            if (z_in(p, v.row0 + c0 + i, ch)) store_z(p.z, z0 + i * p.ld_z, z.x, BF16);
-            if (i + 1 < left && z_in(p, v.row0 + c0 + i + 1, ch)) store_z(p.z, z0 + (i + 1) * p.ld_z, z.y, BF16);
-          }
-        }
       }
     }
-    if (staged) flush();
   }
 }
 
@@ -494,6 +541,7 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
 
   const int warp_e = warp - kFirstEpiWarp;
   const uint32_t lane_base = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+  uint32_t boxes_used = 0;
   auto scales_of = [&](uint32_t i) { return reinterpret_cast<float*>(gen + C::token_scales) + (i & 1u) * BT; };
   // What a tile's epilogue needs from global memory, one tile ahead: this thread's token scale (the warps share
   // them through shared memory) and its channel's scale and bias.
@@ -554,7 +602,7 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         if (ok) {
           tc_fence_after();
           write_tile<C, BF16, PAIR>(p, &tm_z, v, sw, bias, lane_base + buf * C::second, buf, tmem_base, warp_e, lane, base + C::staging, gen,
-                                    scales_of(it), taken);
+                                    scales_of(it), boxes_used, taken);
         } else {
           taken();
         }
@@ -629,6 +677,17 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   }
 }
 
+// output [rows x cols]: boxes of 32 channels, of bf16 with their 16-byte pieces swizzled
+int encode_out(void* fn, CUtensorMap* map, void* ptr, int64_t cols, int64_t rows, int64_t ld, bool bf16) {
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * (bf16 ? 2 : 4)};
+  const cuuint32_t box[2] = {32, bf16 ? 32u : 16u};
+  const cuuint32_t estr[2] = {1, 1};
+  return reinterpret_cast<EncodeTiledFn>(fn)(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2,
+                                             ptr, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                             bf16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                                             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS;
+}
 // block scales: tiles of 512 bytes as [tile rows][k tiles]; a box is a stage's of `tile_rows` tile rows
 int encode_scales(void* fn, CUtensorMap* map, const uint8_t* ptr, int64_t k_tiles, int64_t tile_rows, int box_tiles, int box_rows) {
   const cuuint64_t dims[3] = {kScaleTile / 4, static_cast<cuuint64_t>(k_tiles), static_cast<cuuint64_t>(tile_rows)};
@@ -719,7 +778,7 @@ int luq_launch_gemm_e2m1(luq_ctx* ctx, const luq_e2m1_args& a, bool early, cudaS
   p.z_tma = (reinterpret_cast<uintptr_t>(a.z) & 15u) == 0 && (a.ld_z * esize) % 16 == 0;
   p.tma_cols = a.N / (16 / esize) * (16 / esize);
   CUtensorMap tz{};                                   // not used where copies cannot address the output
-  if (p.z_tma && encode_z(ctx->encode_tiled, &tz, a.z, a.N, a.M, a.ld_z, a.out_bf16 != 0)) return LUQ_ERR_CUDA;
+  if (p.z_tma && encode_out(ctx->encode_tiled, &tz, a.z, a.N, a.M, a.ld_z, a.out_bf16 != 0)) return LUQ_ERR_CUDA;
   // most tiles there can be: at most one partial token tile per group that has rows
   const long long used = p.groups < a.M ? p.groups : a.M;
   auto units = [&](int tile_rows, int tile_ch) {
