@@ -469,7 +469,7 @@ int luq_quant_int8_gemm_grouped(luq_ctx* ctx, const void* d_x, int dtype, int64_
  * Numbers are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; sign, two exponent bits, one mantissa bit), packed two
  * to a byte, the earlier one in the lower half, with a scale for each block of a row's numbers:
  *   block 32   power-of-two scales (e8m0 bytes: 2^(byte - 127)), no other scale
- *   block 16   e4m3 scales, and a binary32 scale for the row
+ *   block 16   e4m3 scales without a sign (the highest bit is not read), and a binary32 scale for the row, of either sign
  * Both are formats that the tensor cores multiply as they are.  (The paper's [1,3,0] gradient format is another one.)
  *
  * Block scales lie in tiles of 512 bytes, 128 rows x 4 blocks: row r, block b of a tile at byte

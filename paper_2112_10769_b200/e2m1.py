@@ -67,7 +67,7 @@ def values(codes: torch.Tensor, tiles: torch.Tensor, row_scale: torch.Tensor | N
     q = levels[torch.stack([codes & 15, codes >> 4], 2).view(rows, -1)[:, :cols].long()]
     s = scale_rows(tiles, rows, cols, block).contiguous()
     if block == 16:
-        s = s.view(torch.float8_e4m3fn).double() * row_scale.double()[:, None]
+        s = (s & 127).view(torch.float8_e4m3fn).double() * row_scale.double()[:, None]      # (scales have no sign)
     else:
         s = torch.where(s == 255, torch.nan, torch.exp2(s.double() - 127))
     return q * s.repeat_interleave(block, 1)[:, :cols]

@@ -1,0 +1,147 @@
+"""A layer of experts, around its products: which experts a token goes to, its copies in the experts' order, and their weighted sum.
+
+    experts, weights = route(logits, k)                  # differentiable in logits
+    offsets, position = order(experts, n_experts)
+    rows = dispatch(x, position, offsets)                # differentiable in x
+    ... products of rows offsets[e] .. offsets[e + 1] - 1 with expert e ...
+    out = combine(y, position, weights, offsets, residual=x)      # differentiable in y, weights and residual
+
+``int8.Int8Experts`` and ``e2m1.E2m1Experts`` are such products; ``E2m1Experts`` takes the tokens and ``position`` themselves and
+needs no ``dispatch``.  Nothing here waits for the device: the numbers of an expert's rows stay there.  Argument handling only: every step
+runs in the library's kernels.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import autograd
+
+
+class RouteFunction(torch.autograd.Function):
+    """``Context.route`` and its gradient.  There is no second derivative: asking for it raises."""
+
+    @staticmethod
+    def forward(ctx, logits, k, score, bias, groups, top_groups, group_top, renormalize, scale):
+        lib = autograd.context(logits.device)
+        experts, weights = lib.route(logits, k, score, bias, groups, top_groups, group_top, renormalize, scale)
+        ctx.save_for_backward(logits, experts)
+        ctx.form = (score, renormalize, scale)
+        ctx.mark_non_differentiable(experts)
+        return experts, weights
+
+    @staticmethod
+    def backward(ctx, _, dweights):
+        logits, experts = ctx.saved_tensors
+        grad = RouteGradient.apply if torch.is_grad_enabled() else autograd.context(logits.device).route_bwd
+        return grad(dweights.contiguous(), logits, experts, *ctx.form), None, None, None, None, None, None, None, None
+
+
+class RouteGradient(torch.autograd.Function):
+    """The backward pass where a graph of it is recorded: differentiating it raises instead of leaving it out."""
+
+    @staticmethod
+    def forward(ctx, dweights, logits, experts, *form):
+        return autograd.context(logits.device).route_bwd(dweights, logits, experts, *form)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("route is differentiable once: its backward pass has no derivative")
+
+
+def route(logits: torch.Tensor, k: int, score: str = "softmax", bias: torch.Tensor | None = None, groups: int = 1, top_groups: int = 1,
+          group_top: int = 2, renormalize: bool = True, scale: float = 1.0):
+    """(experts int32 [rows, k], weights float32 [rows, k]) as ``Context.route``; the weights are differentiable in the logits.  ``bias``
+    (float32, for balance) plays a part in the choice only and gets no gradient."""
+    return RouteFunction.apply(logits, k, score, None if bias is None else bias.detach(), groups, top_groups, group_top, renormalize, scale)
+
+
+def order(experts: torch.Tensor, n_experts: int):
+    """(offsets int32 [n_experts + 1], position int32 [rows, k]) as ``Context.expert_order``."""
+    return autograd.context(experts.device).expert_order(experts, n_experts)
+
+
+class DispatchFunction(torch.autograd.Function):
+    """Linear in x: its backward pass is the copies' sum, whose own is this again."""
+
+    @staticmethod
+    def forward(ctx, x, position, offsets):
+        ctx.save_for_backward(position, offsets)
+        ctx.shape = x.shape
+        return autograd.context(x.device).dispatch(x, position, offsets)
+
+    @staticmethod
+    def backward(ctx, drows):
+        position, offsets = ctx.saved_tensors
+        return CombineFunction.apply(drows, position, None, offsets, None).reshape(ctx.shape), None, None
+
+
+class CombineFunction(torch.autograd.Function):
+    """``Context.combine`` and its gradients.  With weights there is no second derivative: asking for it raises."""
+
+    @staticmethod
+    def forward(ctx, y, position, weights, offsets, residual):
+        ctx.save_for_backward(y if weights is not None else None, position, weights, offsets)
+        ctx.residual_shape = None if residual is None else residual.shape
+        return autograd.context(y.device).combine(y, position, weights, residual)
+
+    @staticmethod
+    def backward(ctx, dout):
+        y, position, weights, offsets = ctx.saved_tensors
+        need_dy, _, need_dw, _, need_dres = ctx.needs_input_grad
+        dy = dw = None
+        if weights is None:
+            dy = DispatchFunction.apply(dout, position, offsets) if need_dy else None
+        elif need_dy or need_dw:
+            grads = CombineGradient.apply if torch.is_grad_enabled() else autograd.context(dout.device).combine_bwd
+            dy, dw = grads(dout, y, position, weights, offsets, need_dy, need_dw)
+        return dy, None, dw, None, dout.reshape(ctx.residual_shape) if need_dres else None
+
+
+class CombineGradient(torch.autograd.Function):
+    """The backward pass where a graph of it is recorded: differentiating it raises instead of leaving it out."""
+
+    @staticmethod
+    def forward(ctx, dout, y, position, weights, offsets, need_dy, need_dw):
+        return autograd.context(dout.device).combine_bwd(dout, y, position, weights, offsets, need_dy, need_dw)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("combine with weights is differentiable once: its backward pass has no derivative")
+
+
+def dispatch(x: torch.Tensor, position: torch.Tensor, offsets: torch.Tensor) -> torch.Tensor:
+    """Rows [rows * k, cols]: every token at its k positions; rows from offsets[-1] on are zeros.  Differentiable in x."""
+    return DispatchFunction.apply(x, position, offsets)
+
+
+def combine(y: torch.Tensor, position: torch.Tensor, weights: torch.Tensor | None, offsets: torch.Tensor,
+            residual: torch.Tensor | None = None) -> torch.Tensor:
+    """residual[t] + sum over j of weights[t, j] * y[position[t, j]].  y has rows * k rows, as ``dispatch`` makes them; its gradient is zero
+    from row offsets[-1] on.  Differentiable in y, weights and residual."""
+    if y.dim() != 2 or y.shape[0] != position.numel():
+        raise TypeError(f"y: {position.numel()} rows expected")
+    out = CombineFunction.apply(y, position, weights, offsets, residual)
+    return out if residual is None else out.reshape(residual.shape)
+
+
+class Router(autograd.KeepsFloat32):
+    """Scores of all experts and the choice of k: ``forward(x)`` gives ``route``'s result for logits ``x @ weight.T`` in 32 bits.  ``balance``:
+    a bias for each expert that only the choice sees, moved by ``rebalance``."""
+
+    def __init__(self, features: int, n_experts: int, k: int, score: str = "softmax", groups: int = 1, top_groups: int = 1,
+                 group_top: int = 2, renormalize: bool = True, scale: float = 1.0, balance: bool = False, device=None):
+        super().__init__()
+        self.k, self.form = k, (score, groups, top_groups, group_top, renormalize, scale)
+        self.weight = torch.nn.Parameter(torch.randn(n_experts, features, device=device) * features ** -0.5)
+        self.register_buffer("bias", torch.zeros(n_experts, device=device) if balance else None)
+
+    def forward(self, x: torch.Tensor):
+        score, groups, top_groups, group_top, renormalize, scale = self.form
+        logits = x.reshape(-1, x.shape[-1]).float() @ self.weight.t()
+        return route(logits, self.k, score, self.bias, groups, top_groups, group_top, renormalize, scale)
+
+    @torch.no_grad()
+    def rebalance(self, offsets: torch.Tensor, rate: float = 1e-3) -> None:
+        """Raises the bias of experts with fewer rows than the mean and lowers that of the others, by ``rate``."""
+        load = (offsets[1:] - offsets[:-1]).float()
+        self.bias += rate * torch.sign(load.mean() - load)

@@ -89,11 +89,8 @@ class Int8Experts(_Int8Module):
         return autograd.context(x.device).quant_int8_gemm_grouped(x, offsets, self.codes, self.scale, self.bias)
 
     def route(self, x: torch.Tensor, expert: torch.Tensor) -> torch.Tensor:
-        """Rows in any order: ``expert`` [M] names each row's expert; the result comes in the order of x."""
-        order = torch.argsort(expert, stable=True)
-        counts = torch.bincount(expert, minlength=self.codes.shape[0])
-        offsets = torch.zeros(self.codes.shape[0] + 1, dtype=torch.int32, device=x.device)
-        offsets[1:] = counts.cumsum(0)
-        z = torch.empty(x.shape[0], self.codes.shape[1], dtype=x.dtype, device=x.device)
-        z[order] = self.forward(x[order], offsets)
-        return z
+        """Rows in any order: ``expert`` [M] names each row's expert; the result comes in the order of x (zeros for a row whose
+        expert is none of these)."""
+        lib = autograd.context(x.device)
+        offsets, position = lib.expert_order(expert.to(torch.int32).reshape(-1, 1).contiguous(), self.codes.shape[0])
+        return lib.combine(self.forward(lib.dispatch(x, position, offsets), offsets), position)

@@ -1,0 +1,302 @@
+"""Order, dispatch and combine, and the layers that use them, against plain indexing in 64 bits.  Positions, copies and the gradients of copies
+are exact; a sum of k products is off by at most k + 1 half steps of binary32 of its terms' magnitudes and half a step of its own
+type, a dot product over C columns by C of them."""
+import pytest
+import torch
+
+from paper_2112_10769_b200 import autograd, binding, e2m1, experts, int8
+
+pytestmark = pytest.mark.gpu
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = binding.Context(0)
+    yield c
+    c.close()
+
+
+def choice(T, k, E, drop=0.0, seed=0):
+    g = torch.Generator("cuda").manual_seed(T + 7 * k + E + seed)
+    e = torch.rand(T, E, device="cuda", generator=g).topk(k, 1).indices.to(torch.int32)
+    if drop:
+        e[torch.rand(T, k, device="cuda", generator=g) < drop] = -1
+        e[torch.rand(T, k, device="cuda", generator=g) < 0.02] = E + 3
+    return e
+
+
+def plain_order(chosen, E):
+    flat = chosen.flatten().long()
+    key = torch.where((flat < 0) | (flat >= E), E, flat)
+    by = torch.sort(key, stable=True).indices
+    position = torch.empty_like(by)
+    position[by] = torch.arange(by.numel(), device="cuda")
+    position[key == E] = -1
+    counts = torch.bincount(key, minlength=E + 1)[:E]
+    return torch.cat([counts.new_zeros(1), counts.cumsum(0)]).to(torch.int32), position.view(chosen.shape).to(torch.int32)
+
+
+@pytest.mark.parametrize("T,k,E", [(1, 1, 1), (1, 8, 256), (5, 2, 3), (31, 1, 1024), (1023, 1, 7), (1024, 2, 64), (1025, 2, 64), (700, 3, 33), (2049, 1, 2), (30000, 8, 256),
+                                   (300000, 1, 1000), (5000, 5, 100)])
+def test_order(ctx, T, k, E):
+    for drop in (0.0, 0.3):
+        chosen = choice(T, k, E, drop)
+        got, want = ctx.expert_order(chosen, E), plain_order(chosen, E)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    # all with one expert, the last, none
+    for e in (0, E - 1, -1, E):
+        chosen = torch.full((T, k), e, dtype=torch.int32, device="cuda")
+        got, want = ctx.expert_order(chosen, E), plain_order(chosen, E)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_order_of_nothing(ctx):
+    offsets, position = ctx.expert_order(torch.empty(0, 2, dtype=torch.int32, device="cuda"), 5)
+    assert torch.equal(offsets, torch.zeros_like(offsets)) and position.shape == (0, 2)
+    x = torch.empty(0, 16, device="cuda")
+    assert ctx.dispatch(x, position, offsets).shape == (0, 16) and ctx.combine(x, position).shape == (0, 16)
+    dy, dw = ctx.combine_bwd(x, x, position, None, offsets)
+    assert dy.shape == (0, 16) and dw.shape == (0, 2)
+
+
+MOVES = [(1, 1, 1, 0, 0), (1, 7, 8, 0, 0), (3, 16, 2, 0, 0), (40, 15, 3, 1, 1), (100, 64, 8, 0, 0), (65, 1000, 2, 8, 0), (30, 771, 3, 0, 0), (30, 1001, 4, 3, 3), (200, 2048, 1, 0, 0),
+         (5, 4100, 33, 0, 0), (1000, 8, 5, 0, 1), (2000, 257, 2, 0, 0), (7, 9001, 2, 1, 0)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,cols,k,pad,shift", MOVES)
+def test_moves(ctx, T, cols, k, pad, shift, dtype):
+    E = max(k, 16)
+    def rows(n, seed):
+        g = torch.Generator("cuda").manual_seed(seed)
+        return torch.randn(n * (cols + pad) + shift, device="cuda", generator=g).to(dtype)[shift:].view(n, cols + pad)[:, :cols]
+    for drop in (0.0, 0.3):
+        offsets, position = ctx.expert_order(choice(T, k, E, drop), E)
+        live, at = position >= 0, position.clamp_min(0).long()
+        token = torch.arange(T, device="cuda")[:, None].expand(T, k)
+        x, y, dout = rows(T, 1), rows(T * k, 2), rows(T, 3)
+        w = torch.rand(T, k, device="cuda")
+        want = torch.zeros(T * k, cols, dtype=dtype, device="cuda")
+        want[position[live].long()] = x[token[live]]
+        assert torch.equal(ctx.dispatch(x, position, offsets), want)
+        for weights in (w, None):
+            for residual in (x, None):
+                terms = torch.where(live[:, :, None], y.double()[at], 0.0) * (1.0 if weights is None else w.double()[:, :, None])
+                total, mag = terms.sum(1), terms.abs().sum(1)
+                if residual is not None:
+                    total, mag = total + x.double(), mag + x.double().abs()
+                bound = (k + 1) * 2.0 ** -24 * mag
+                bound = bound + HALF[dtype] * (total.abs() + bound)
+                assert ((ctx.combine(y, position, weights, residual).double() - total).abs() <= bound).all()
+            dy, dw = ctx.combine_bwd(dout, y, position, weights, offsets)
+            wdy = torch.zeros_like(want)
+            wdy[position[live].long()] = (dout.float()[:, None, :] * (1.0 if weights is None else w[:, :, None])).expand(T, k, cols)[live].to(dtype)
+            assert torch.equal(dy, wdy)
+            prod = torch.where(live[:, :, None], y.double()[at], 0.0) * dout.double()[:, None, :]
+            assert ((dw.double() - prod.sum(2)).abs() <= (cols + 1) * 2.0 ** -24 * prod.abs().sum(2)).all()
+        assert ctx.combine_bwd(dout, y, position, w, offsets, False, True)[0] is None
+        assert ctx.combine_bwd(dout, y, position, w, offsets, True, False)[1] is None
+    assert ctx.status() == 0
+
+
+def test_rows_that_no_position_names_play_no_part(ctx):
+    # Inf and NaN in rows of no copy, and a NaN weight of a token without experts
+    T, k, E, cols = 50, 2, 8, 40
+    chosen = choice(T, k, E)
+    chosen[10:20] = -1
+    offsets, position = ctx.expert_order(chosen, E)
+    y = torch.randn(T * k, cols, device="cuda")
+    y[int(offsets[-1]):] = float("nan")
+    w = torch.rand(T, k, device="cuda")
+    w[15, 0] = float("nan")
+    out = ctx.combine(y, position, w)
+    assert torch.isnan(out[15]).all() and torch.isfinite(out[torch.arange(T, device="cuda") != 15]).all()
+    assert (out[10:15] == 0).all()
+    # positions beyond the rows are left out
+    position[0, 0], position[1, 1] = T * k, -(1 << 31)
+    assert torch.isfinite(ctx.combine(y, position, w)[[0, 1]]).all()
+
+
+def test_out_arguments(ctx):
+    offsets, position = ctx.expert_order(choice(30, 2, 8), 8)
+    x = torch.randn(30, 50, device="cuda")
+    wide = torch.full((60, 57), 3.0, device="cuda")
+    rows = ctx.dispatch(x, position, offsets, out=wide[:, 3:53])
+    assert torch.equal(rows, ctx.dispatch(x, position, offsets)) and (wide[:, :3] == 3).all() and (wide[:, 53:] == 3).all()
+    wide = torch.full((30, 57), 3.0, device="cuda")
+    assert torch.equal(ctx.combine(rows, position, out=wide[:, :50]), ctx.combine(rows.clone(), position)) and (wide[:, 50:] == 3).all()
+
+
+def test_refusals(ctx):
+    offsets, position = ctx.expert_order(choice(30, 2, 8), 8)
+    x, y = torch.randn(30, 50, device="cuda"), torch.randn(60, 50, device="cuda")
+    w = torch.rand(30, 2, device="cuda")
+    for call in (lambda: ctx.expert_order(torch.zeros(3, 2, dtype=torch.int64, device="cuda"), 8), lambda: ctx.expert_order(torch.zeros(3, dtype=torch.int32, device="cuda"), 8),
+                 lambda: ctx.expert_order(choice(30, 2, 8), 0), lambda: ctx.expert_order(choice(30, 2, 8), 1025), lambda: ctx.expert_order(choice(30, 4, 8)[:, ::2], 8),
+                 lambda: ctx.dispatch(x[:29], position, offsets), lambda: ctx.dispatch(x, position.long(), offsets), lambda: ctx.dispatch(x, position, offsets.long()),
+                 lambda: ctx.dispatch(x.half(), position, offsets), lambda: ctx.dispatch(x, position, offsets, out=torch.empty(59, 50, device="cuda")),
+                 lambda: ctx.dispatch(x, position, offsets, out=torch.empty(60, 50, device="cuda").bfloat16()), lambda: ctx.combine(y, position, w[:29]),
+                 lambda: ctx.combine(y, position, w.double()), lambda: ctx.combine(y, position, w, x[:, :49]), lambda: ctx.combine(y, position, w, x.bfloat16()),
+                 lambda: ctx.combine_bwd(x.bfloat16(), y, position, w, offsets), lambda: ctx.combine_bwd(x[:, :49], y, position, w, offsets),
+                 lambda: ctx.dispatch(x.cpu(), position, offsets), lambda: experts.combine(y[:59], position, w, offsets)):
+        with pytest.raises(TypeError):
+            call()
+    assert ctx.status() == 0
+
+
+def test_gradients_of_the_whole_path():
+    # router, copies, a product of every expert, their sum: against the same in 64 bits.  Choices are those of the logits, given to both
+    T, C, E, k = 60, 24, 6, 2
+    g = torch.Generator("cuda").manual_seed(3)
+    x, logits, weight, res = (torch.randn(*s, device="cuda", generator=g) for s in ((T, C), (T, E), (E, C, C), (T, C)))
+    weight *= C ** -0.5
+    leaves = [t.clone().requires_grad_() for t in (x, logits, weight, res)]
+    chosen, w = experts.route(leaves[1], k, score="softmax", renormalize=False)
+    offsets, position = experts.order(chosen, E)
+    rows = experts.dispatch(leaves[0], position, offsets)
+    ends = offsets.tolist()
+    y = torch.cat([rows[a:b] @ leaves[2][e].t() for e, (a, b) in enumerate(zip(ends, ends[1:]))])
+    out = experts.combine(y, position, w, offsets, residual=leaves[3])
+    d = torch.randn(T, C, device="cuda", generator=g)
+    got = torch.autograd.grad((out * d).sum(), leaves)
+    l64 = [t.double().requires_grad_() for t in (x, logits, weight, res)]
+    p = torch.softmax(l64[1], 1).gather(1, chosen.long())
+    z = torch.einsum("tc,tknc->tkn", l64[0], l64[2][chosen.long()])
+    want_out = (p[:, :, None] * z).sum(1) + l64[3]
+    want = torch.autograd.grad((want_out * d.double()).sum(), l64)
+    # sums of at most T C terms in binary32, twice: against the largest of each
+    for a, b in zip([out, *got], [want_out, *want]):
+        assert ((a.double() - b).abs() <= 4 * C * 2.0 ** -23 * b.abs().max().clamp_min(1.0)).all()
+
+
+def test_gradients_of_broadcast_and_strided_tensors():
+    offsets, position = experts.order(choice(20, 2, 4), 4)
+    x = torch.randn(1, 16, device="cuda").requires_grad_()
+    rows = experts.dispatch(x.expand(20, 16), position, offsets)
+    rows.sum().backward()                                      # (a gradient that is one number, broadcast)
+    assert torch.equal(x.grad, torch.full_like(x, 40.0))
+    y, w = torch.randn(40, 16, device="cuda").requires_grad_(), torch.rand(20, 2, device="cuda").requires_grad_()
+    d = torch.randn(16, 20, device="cuda").t()                 # (columns contiguous)
+    out = experts.combine(y, position, w, offsets)
+    dy, dw = torch.autograd.grad(out, (y, w), d)
+    want = torch.autograd.grad(experts.combine(y, position, w, offsets), (y, w), d.contiguous())
+    assert torch.equal(dy, want[0]) and torch.equal(dw, want[1])
+    # tokens in more dimensions keep them
+    x3 = torch.randn(4, 5, 16, device="cuda").requires_grad_()
+    out = experts.combine(experts.dispatch(x3, position, offsets), position, None, offsets, residual=x3)
+    assert out.shape == x3.shape
+    out.sum().backward()
+    assert torch.equal(x3.grad, torch.full_like(x3, 3.0))
+
+
+def test_second_derivatives():
+    offsets, position = experts.order(choice(20, 2, 4), 4)
+    x = torch.randn(20, 8, device="cuda").requires_grad_()
+    f = lambda v: experts.combine(experts.dispatch(v, position, offsets) ** 3, position, None, offsets).sum()
+    grad, = torch.autograd.grad(f(x), x, create_graph=True)    # linear parts have one
+    torch.testing.assert_close(torch.autograd.grad(grad.sum(), x)[0], 12 * x.detach())
+    w = torch.rand(20, 2, device="cuda").requires_grad_()
+    grad, = torch.autograd.grad(experts.combine(experts.dispatch(x, position, offsets), position, w, offsets).sum(), w, create_graph=True)
+    with pytest.raises(RuntimeError, match="differentiable once"):
+        grad.sum().backward()
+
+
+def test_int8_experts_route():
+    torch.manual_seed(0)
+    layer = int8.Int8Experts(torch.randn(5, 40, 64, device="cuda"))
+    x, expert = torch.randn(300, 64, device="cuda"), torch.randint(5, (300,), device="cuda")
+    order = torch.argsort(expert, stable=True)
+    offsets = torch.zeros(6, dtype=torch.int32, device="cuda")
+    offsets[1:] = torch.bincount(expert, minlength=5).cumsum(0)
+    want = torch.empty(300, 40, device="cuda")
+    want[order] = layer(x[order], offsets)
+    assert torch.equal(layer.route(x, expert), want)
+    expert[7] = 9
+    got = layer.route(x, expert)
+    assert (got[7] == 0).all() and torch.equal(got[8:], want[8:])
+
+
+def answer(x, router, up, down):
+    chosen, w = router(x)
+    offsets, position = experts.order(chosen, up.codes.shape[0])
+    y = down(torch.relu(up(x, offsets, position)), offsets)
+    return experts.combine(y, position, w, offsets, residual=x)
+
+
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("T,dtype", [(1, torch.bfloat16), (33, torch.float32), (700, torch.bfloat16)])
+def test_a_layer_that_answers(T, dtype, block):
+    torch.manual_seed(T)
+    C, H, E, k = 96, 160, 12, 3
+    router = experts.Router(C, E, k, score="sigmoid", groups=4, top_groups=2, balance=True, device="cuda")
+    wu, wd = torch.randn(E, H, C, device="cuda") * C ** -0.5, torch.randn(E, C, H, device="cuda") * H ** -0.5
+    up, down = e2m1.E2m1Experts(wu, block=block), e2m1.E2m1Experts(wd, block=block)
+    x = torch.randn(T, C, device="cuda").to(dtype)
+    with torch.no_grad():
+        got = answer(x, router, up, down)
+        # the same with every expert on its own: products of the same codes, whose sums may be in another order
+        chosen, w = router(x)
+        want = x.double()
+        for e in range(E):
+            h = e2m1.E2m1Linear(wd[e], block=block)(torch.relu(e2m1.E2m1Linear(wu[e], block=block)(x)))
+            want = want + torch.where(chosen == e, w, 0.0).sum(1, keepdim=True).double() * h.double()
+    # a first product off by a step may be quantized to a neighbouring number, a sixth of a block's largest away: rare, and bounded by that
+    err = (got.double() - want).abs()
+    assert (err <= 2 * HALF[dtype] * (want.abs() + 1)).float().mean() > 0.97 and err.max() < 0.5
+    # captured and replayed with other tokens
+    if T > 1:
+        static, stream = x.clone(), torch.cuda.Stream()
+        with torch.no_grad(), torch.cuda.stream(stream):
+            answer(static, router, up, down)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                out = answer(static, router, up, down)
+        torch.cuda.synchronize()
+        for seed in range(3):
+            static.copy_(torch.randn(T, C, device="cuda", generator=torch.Generator("cuda").manual_seed(seed)).to(dtype))
+            graph.replay()
+            with torch.no_grad():
+                assert torch.equal(out, answer(static.clone(), router, up, down))
+    assert autograd.context(x.device).status() == 0
+
+
+def test_captured_training_step():
+    # (leaves are first used on the stream of the capture, as torch's graphs ask)
+    torch.manual_seed(0)
+    T, C, E, k = 64, 32, 8, 2
+    router = experts.Router(C, E, k, device="cuda")
+    x = torch.randn(T, C, device="cuda").requires_grad_()
+    def step(x, weight):
+        chosen, w = experts.route(x @ weight.t(), k)
+        offsets, position = experts.order(chosen, E)
+        out = experts.combine(experts.dispatch(x, position, offsets) * 2.0, position, w, offsets, residual=x)
+        return torch.autograd.grad((out * out).sum(), (x, weight))
+    want = step(x.detach().clone().requires_grad_(), router.weight.detach().clone().requires_grad_())
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        step(x, router.weight)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            got = step(x, router.weight)
+    torch.cuda.synchronize()
+    for g in got:
+        g.zero_()
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        torch.testing.assert_close(a, b)
+
+
+def test_rebalance_moves_towards_the_mean():
+    router = experts.Router(8, 4, 1, balance=True, device="cuda")
+    router.rebalance(torch.tensor([0, 10, 12, 20, 28], dtype=torch.int32, device="cuda"), 0.5)
+    assert router.bias.tolist() == [-0.5, 0.5, -0.5, -0.5]
+
+
+def test_example_runs():
+    from paper_2112_10769_b200 import example_experts
+    result = example_experts.main(width=64, tokens=256, n_experts=4, steps=3, verbose=False)
+    assert result["status"] == 0 and all(v == v for v in result.values())
