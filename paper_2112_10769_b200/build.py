@@ -75,7 +75,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     nvcc = os.environ.get("NVCC", "nvcc")
     lib = LIB_DEBUG if debug else LIB
     suffix, define = (".dbg.o", ["-DLUQ_DEBUG"]) if debug else (".o", [])
-    headers = [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "int4_math.cuh"), os.path.join(CSRC, "product_tiles.cuh"),
+    headers = [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "int4_math.cuh"), os.path.join(CSRC, "product_tiles.cuh"), os.path.join(CSRC, "e2m1_math.cuh"),
                os.path.join(ROOT, "include", "luq.h")]
     objs, digests, running = [], [], []
     for name, extra in UNITS.items():

@@ -739,6 +739,7 @@ int e2m1_product(luq_ctx* ctx, luq_e2m1_args a, int z_dtype, bool grouped, const
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return LUQ_ERR_CUDA;
   if (from_codes) return cuda_rc(luq_launch_gemm_e2m1(ctx, a, false, as_stream(stream)));
+  if (!grouped && luq_e2m1_is_few(ctx, a.M, a.N, a.K)) return cuda_rc(luq_launch_e2m1_few(ctx, a, x, dtype, ld_x, as_stream(stream)));
   a.ld_x = (code_bytes(a.K) + 15) / 16 * 16;
   const size_t codes = static_cast<size_t>(a.M) * a.ld_x;
   const size_t tiles = static_cast<size_t>(luq_e2m1_tile_rows(a.M, grouped ? a.groups : 0)) * luq_e2m1_k_tiles(a.K, a.block) * 512;

@@ -154,6 +154,9 @@ struct luq_e2m1_args {
 };
 // early: the preceding kernel of the stream is this call's quantizer, which writes x_codes, x_tiles and sx only
 int luq_launch_gemm_e2m1(luq_ctx* ctx, const luq_e2m1_args& a, bool early, cudaStream_t st);
+// quantizer and product of a few tokens in one launch, for the sizes that luq_e2m1_is_few says (no groups)
+bool luq_e2m1_is_few(const luq_ctx* ctx, int64_t M, int64_t N, int64_t K);
+int luq_launch_e2m1_few(luq_ctx* ctx, const luq_e2m1_args& a, const void* x, int dtype, int64_t ld_x, cudaStream_t st);
 // Tiles of 128 rows x 4 block scales: along a row, and rows of tiles (a group's rows start one of their own; groups 0: no groups)
 inline int64_t luq_e2m1_k_tiles(int64_t K, int block) { return (K + 4 * block - 1) / (4 * block); }
 inline int64_t luq_e2m1_tile_rows(int64_t rows, int64_t groups) { return groups ? rows / 128 + groups : (rows + 127) / 128; }

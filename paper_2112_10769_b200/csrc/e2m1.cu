@@ -12,16 +12,13 @@
 // maximum meets in shared memory.  Block scales leave in the tiles that the
 // tensor cores copy (128 rows x 4 blocks, row r, block b at 16 (r mod 32) + 4 (r / 32) + b): the threads of four blocks put
 // their bytes together and one stores the word.
-#include <cuda_bf16.h>
+#include <climits>
 
-#include "common.cuh"
+#include "e2m1_math.cuh"
 
 namespace {
 
 using namespace luqdev;
-
-constexpr int kChunk = 16;                 // elements of a thread
-constexpr int kScaleTile = 512;
 
 struct RowsParams {
   const void* x;
@@ -42,141 +39,40 @@ struct RowsParams {
   bool vec;                 // rows of x start at multiples of 16 bytes
 };
 
-// The words of a thread's 16 elements, zeros beyond the row's end.  Where they do not lie in whole aligned pieces of 16 bytes they
-// are put together from the pieces that hold an element of theirs.
-template <typename T> constexpr int kWords = kChunk * static_cast<int>(sizeof(T)) / 4;
-template <typename T>
-__device__ __forceinline__ void load_chunk16(const T* row, int c0, int cols, bool vec, uint32_t (&w)[kWords<T>]) {
-  constexpr int W = kWords<T>;
-  if (vec && c0 + kChunk <= cols) {
+// The offsets that a lane holds of up to kHeldGroups groups: offsets[1 + lane], offsets[33 + lane], ...; more are read for every row.
+constexpr int kHeldOffsets = 4, kHeldGroups = 32 * kHeldOffsets;
+struct Offsets {
+  int held[kHeldOffsets], first;
+  Offsets() = default;
+  __device__ __forceinline__ explicit Offsets(const RowsParams& p) {
+    const int lane = threadIdx.x & 31;
+    first = *p.offsets;
 #pragma unroll
-    for (int i = 0; i < W / 4; ++i) {
-      const uint4 u = reinterpret_cast<const uint4*>(row + c0)[i];
-      w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
-    }
-    return;
+    for (int i = 0; i < kHeldOffsets; ++i) held[i] = 32 * i + lane < p.groups ? *(p.offsets + 1 + 32 * i + lane) : INT_MAX;
   }
-  if (c0 >= cols) {
-#pragma unroll
-    for (int i = 0; i < W; ++i) w[i] = 0u;
-    return;
-  }
-  const uintptr_t at = reinterpret_cast<uintptr_t>(row + c0), end = reinterpret_cast<uintptr_t>(row + min(c0 + kChunk, cols));
-  const uintptr_t low = at & ~static_cast<uintptr_t>(15);
-  const int shift = static_cast<int>(at & 15u);
-  uint32_t v[W + 4];
-#pragma unroll
-  for (int i = 0; i <= W / 4; ++i) {
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (low + 16 * i < end) u = *reinterpret_cast<const uint4*>(low + 16 * i);
-    v[4 * i] = u.x; v[4 * i + 1] = u.y; v[4 * i + 2] = u.z; v[4 * i + 3] = u.w;
-  }
-  if (shift & 8) {
-#pragma unroll
-    for (int i = 0; i < W + 2; ++i) v[i] = v[i + 2];
-  }
-  if (shift & 4) {
-#pragma unroll
-    for (int i = 0; i < W + 1; ++i) v[i] = v[i + 1];
-  }
-#pragma unroll
-  for (int i = 0; i < W; ++i) w[i] = sizeof(T) == 4 ? v[i] : __funnelshift_r(v[i], v[i + 1], 8 * (shift & 2));
-  if (c0 + kChunk > cols) {
-#pragma unroll
-    for (int i = 0; i < kChunk; ++i)
-      if (c0 + i >= cols) {
-        if constexpr (sizeof(T) == 4) w[i] = 0u;
-        else w[i / 2] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-      }
-  }
-}
-// the largest pattern of |x|, as a binary32 one: of numbers the largest, Inf above every number, NaN above Inf
-template <typename T>
-__device__ __forceinline__ uint32_t top_of(const uint32_t (&w)[kWords<T>]) {
-  uint32_t t = 0;
-  if constexpr (sizeof(T) == 4) {
-#pragma unroll
-    for (int i = 0; i < kWords<T>; ++i) t = max(t, w[i] & 0x7FFFFFFFu);
-    return t;
-  } else {
-#pragma unroll
-    for (int i = 0; i < kWords<T>; ++i) asm("max.u16x2 %0, %0, %1;" : "+r"(t) : "r"(w[i] & 0x7FFF7FFFu));
-    return max(t << 16, t & 0xFFFF0000u);
-  }
-}
-template <typename T>
-__device__ __forceinline__ float2 pair_of(const uint32_t (&w)[kWords<T>], int i) {
-  if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
-  else return make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
-}
-// eight numbers from pairs `first` .. `first` + 3, the first in the lowest four bits
-template <typename T>
-__device__ __forceinline__ uint32_t pack8(const uint32_t (&w)[kWords<T>], int first, float f) {
-  float2 v[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = __fmul2_rn(pair_of<T>(w, first + i), make_float2(f, f));
-  uint32_t r;
-  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
-      "mov.b32 %0, {a, b, c, d};\n\t}"
-      : "=r"(r)
-      : "f"(v[0].x), "f"(v[0].y), "f"(v[1].x), "f"(v[1].y), "f"(v[2].x), "f"(v[2].y), "f"(v[3].x), "f"(v[3].y));
-  return r;
-}
-// the e4m3 number nearest to v >= 0 (at most 448), and its value
-__device__ __forceinline__ uint32_t to_e4m3(float v, float& value) {
-  uint16_t b;
-  uint32_t h;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(0.0f), "f"(v));
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(b));
-  asm("{\n\t.reg .f16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.f32.f16 %0, lo;\n\t}" : "=f"(value) : "r"(h));
-  return b & 0xFFu;
-}
-
-// What a row's elements are made of: the row's scale and six times it (blocks of 16), and whether it has numbers at all
-struct RowScale {
-  float g, six;
-  bool dead;             // Inf or NaN, or nothing to scale by: zero codes
 };
-__device__ __forceinline__ RowScale row_scale(uint32_t top) {
-  RowScale s;
-  s.dead = top >= 0x7F800000u || top < 0x0D800000u;                 // 2^-100
-  s.g = s.dead ? (top >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : 0.0f) : __fdiv_rn(__uint_as_float(top), 2688.0f);
-  s.six = __fmul_rn(s.g, 6.0f);
-  return s;
-}
-// a block's scale byte and the factor of its elements
-template <int BLOCK>
-__device__ __forceinline__ uint32_t block_scale(uint32_t top, const RowScale& row, float& factor) {
-  if constexpr (BLOCK == 16) {
-    factor = 0.0f;
-    if (row.dead) return 0u;
-    float s;
-    const uint32_t byte = to_e4m3(__fdiv_rn(__uint_as_float(top), row.six), s);
-    if (s > 0.0f) factor = __frcp_rn(__fmul_rn(s, row.g));
-    return byte;
-  } else {
-    if (top >= 0x7F800000u) { factor = 0.0f; return 255u; }
-    const uint32_t byte = max(static_cast<int>(top >> 23) - 2, 0);
-    factor = __uint_as_float((254u - byte) << 23);
-    return byte;
-  }
-}
-
 // The group of a row and the row's number in it, by a whole warp; false: the row belongs to none.  Whatever the offsets
 // hold, start / 128 + group + in_group / 128 is below out_rows / 128 + groups.
-__device__ __forceinline__ bool group_of(const RowsParams& p, int row, int& tile_row, int& in_tile) {
+__device__ __forceinline__ bool group_of(const RowsParams& p, const Offsets& offsets, int row, int& tile_row, int& in_tile) {
   const int lane = threadIdx.x & 31;
-  int before = 0;                              // offsets 1 .. groups that are at most `row`
-  for (int e0 = 1; e0 <= p.groups; e0 += 32) {
-    const int e = e0 + lane;
-    before += __popc(__ballot_sync(0xFFFFFFFFu, e <= p.groups && *(p.offsets + e) <= row));
+  int before = 0, start = offsets.first;       // offsets 1 .. groups that are at most `row`, and the last of them
+  if (p.groups <= kHeldGroups) {
+#pragma unroll
+    for (int i = 0; i < kHeldOffsets; ++i) {
+      if (32 * i >= p.groups) break;
+      const int n = __popc(__ballot_sync(0xFFFFFFFFu, offsets.held[i] <= row));
+      const int last = __shfl_sync(0xFFFFFFFFu, offsets.held[i], max(n - 1, 0));
+      if (n > 0) { before += n; start = last; }
+    }
+  } else {
+    for (int e0 = 1; e0 <= p.groups; e0 += 32) {
+      const int e = e0 + lane;
+      before += __popc(__ballot_sync(0xFFFFFFFFu, e <= p.groups && *(p.offsets + e) <= row));
+    }
+    if (before < p.groups) start = *(p.offsets + before);
   }
   if (before >= p.groups) return false;
-  const int start = max(*(p.offsets + before), 0);
+  start = max(start, 0);
   if (start > row) return false;
   tile_row = start / 128 + before + (row - start) / 128;
   in_tile = (row - start) % 128;
@@ -223,15 +119,6 @@ __device__ __forceinline__ void store_chunk(const RowsParams& p, const Place<BLO
   }
 }
 
-// A chunk in registers -> its codes and scale byte
-template <typename T, int BLOCK>
-__device__ __forceinline__ void quantize_chunk(const uint32_t (&w)[kWords<T>], uint32_t top, const RowScale& row, uint2& codes, uint32_t& byte) {
-  float f;
-  byte = block_scale<BLOCK>(top, row, f);
-  // (a factor of zero would leave NaN where there is Inf)
-  codes = f > 0.0f ? make_uint2(pack8<T>(w, 0, f), pack8<T>(w, 4, f)) : make_uint2(0u, 0u);
-}
-
 // LANES lanes (kBlockRow: a block, of any number of warps) share a row; blocks walk over rows.  CHUNKS chunks of a thread, every
 // LANES-th of the row; CHUNKS = 0: any width, chunks are read again for the second pass (from L2).  PLAN: rows go where offsets and
 // positions say.
@@ -249,6 +136,8 @@ __global__ void __launch_bounds__(LANES == kBlockRow ? 1024 : 128) e2m1_rows_ker
   const long long plane_tiles = (p.plane_rows + 127) / 128;
   pdl_wait();
   pdl_trigger();
+  // a plan's offsets are read once, a row's positions (the first 32) before its elements
+  const Offsets offsets = PLAN ? Offsets(p) : Offsets();
   int turn = 0;
   for (int first = static_cast<int>(blockIdx.x) * per_block; first < rows; first += step, turn ^= 1) {
     const int r = first + (LANES == kBlockRow ? 0 : static_cast<int>(threadIdx.x) / (LANES == kBlockRow ? 1 : LANES));
@@ -256,6 +145,8 @@ __global__ void __launch_bounds__(LANES == kBlockRow ? 1024 : 128) e2m1_rows_ker
     if (LANES == 32 && !there) break;                          // (a whole warp; nothing meets)
     const T* const x = static_cast<const T*>(p.x) + (there ? r : 0) * p.ld_x;
     uint32_t w[kHeld][kWords<T>], top[kHeld] = {}, row_top = 0;
+    int positions = -1;
+    if (PLAN && p.position && lane < p.copies) positions = *(p.position + static_cast<long long>(r) * p.copies + lane);
     if constexpr (CHUNKS > 0) {
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) load_chunk16(x, (t + i * lanes) * kChunk, p.cols, p.vec, w[i]);
@@ -283,6 +174,11 @@ __global__ void __launch_bounds__(LANES == kBlockRow ? 1024 : 128) e2m1_rows_ker
     if (row_top >= 0x7F800000u || (BLOCK == 16 && row_top < 0x0D800000u && row_top > 0)) {
       if ((LANES == kBlockRow ? lane : t) == 0 && there) atomicOr(p.status, row_top >= 0x7F800000u ? LUQ_STATUS_NONFINITE : LUQ_STATUS_RANGE);
     }
+    // the row that copy j goes to (every lane of the warp asks)
+    auto place = [&](int j) {
+      if (!p.position) return r;
+      return j < 32 ? __shfl_sync(0xFFFFFFFFu, positions, j) : *(p.position + static_cast<long long>(r) * p.copies + j);
+    };
     // calls f(row to write, offset of its scales' words, have they a place) for every place that the row goes to
     auto places = [&](auto f) {
       if constexpr (!PLAN) {
@@ -295,10 +191,10 @@ __global__ void __launch_bounds__(LANES == kBlockRow ? 1024 : 128) e2m1_rows_ker
         }
       } else {
         for (int j = 0; j < p.copies; ++j) {
-          const int to = p.position ? *(p.position + static_cast<long long>(r) * p.copies + j) : r;
+          const int to = place(j);
           if (to < 0 || to >= p.out_rows) continue;            // warp-uniform
           int tile_row = 0, in_tile = 0;
-          const bool tiled = group_of(p, to, tile_row, in_tile);
+          const bool tiled = group_of(p, offsets, to, tile_row, in_tile);
           f(to, tile_offset(p, tile_row, in_tile), tiled);
         }
       }
@@ -327,13 +223,15 @@ __global__ void __launch_bounds__(LANES == kBlockRow ? 1024 : 128) e2m1_rows_ker
         places([&](int to, long long tiles_from, bool tiled) { store_chunk<BLOCK>(p, at, to, tiles_from, tiled, codes, word); });
       }
     }
-    if (BLOCK == 16 && t == 0 && there) {
+    if (BLOCK == 16) {
       if constexpr (PLAN) {
-        for (int j = 0; j < p.copies; ++j) {
-          const int to = p.position ? *(p.position + static_cast<long long>(r) * p.copies + j) : r;
-          if (to >= 0 && to < p.out_rows) p.scale[to] = row.g;
+        if (warp == 0 || LANES == 32) {
+          for (int j = 0; j < p.copies; ++j) {
+            const int to = place(j);
+            if (t == 0 && to >= 0 && to < p.out_rows) p.scale[to] = row.g;
+          }
         }
-      } else {
+      } else if (t == 0 && there) {
         p.scale[r] = row.g;
       }
     }

@@ -26,6 +26,7 @@
 // tensor memory and returns.
 #include <climits>
 
+#include "e2m1_math.cuh"
 #include "product_tiles.cuh"
 
 namespace {
@@ -36,7 +37,6 @@ constexpr int kCh = 128;                  // output channels per tile (tensor-me
 constexpr int kBk = 128;                  // bytes of a row per stage: 256 contraction elements
 constexpr int kSteps4 = 4;                // instructions per stage, 64 elements each
 constexpr int kSlab = kCh * kBk;          // bytes of W per stage
-constexpr int kScaleTile = 512;           // 128 rows x 4 block scales
 constexpr int kXWarp = 2;
 constexpr int kFirstEpiWarp = 3;
 constexpr int kBox = 2048;                // a store box of 32 channels: 32 tokens bf16, 16 tokens fp32
@@ -677,6 +677,264 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   }
 }
 
+// ---- few tokens: quantizer and product in one launch --------------------------------------------------------------------
+// Z = gx gw X W^T + bias of at most kFew tokens, from high-precision tokens.  A cluster has 128 channels, its CTAs a share of the
+// contraction each, as in the kernel above with as many CTAs: the sums are made in the same order and the results are the same
+// bit for bit.  While the weights are on their way (warp 0), warps 2 to 5 find the tokens' maxima, quantize the CTA's share of them
+// into shared memory as a copy would have laid it there - eight tokens' rows of a stage in 1 KB, a line of scales for each of
+// eight rows - and take the epilogue afterwards.  A stage's instructions are told of 16 tokens: rows 8 to 15 and lines 8 to 31 are
+// whatever follows in shared memory, and make columns that nobody reads.
+// What bounds it is the latency of its steps (4096 x 4096, one token: 4.1 us, with a launch for the quantizer 6.1; two tokens of
+// 1000 x 1000: 4.6 and 5.6; three or four were no quicker, the CTAs each reading all of them).
+constexpr int kFew = 2, kFewStages = 4, kFewThreads = 192, kFewBlocks = 32;     // kFewBlocks: stages' worth of tokens a CTA can hold
+template <int BLOCK>
+struct FewCfg {
+  static constexpr int k_tiles = BLOCK == 16 ? 4 : 2, w_scales = k_tiles * kScaleTile, stage_bytes = kSlab + w_scales;
+  static constexpr int lines = 8 * 16;                            // of a tile of the tokens' scales
+  static constexpr int scale_cols = 8 * k_tiles, first_scale = 32, tmem_cols = 256;
+  static_assert(first_scale + kFewStages * scale_cols <= tmem_cols);
+  static constexpr int x_codes = kFewStages * stage_bytes;        // 1024-byte aligned, one more than the CTA's blocks
+  __host__ __device__ static constexpr int x_scales(int blocks) { return x_codes + (blocks + 1) * 1024; }
+  __host__ __device__ static constexpr int partial(int blocks) { return x_scales(blocks) + blocks * k_tiles * lines + kScaleTile; }
+  __host__ __device__ static constexpr int barriers(int blocks) { return partial(blocks) + kFew * kCh * 4; }
+  static constexpr int num_barriers = 2 * kFewStages + 2;
+  __host__ __device__ static constexpr int box(int blocks) { return barriers(blocks) + 8 * num_barriers; }      // tokens' maxima, 4 warps
+  __host__ __device__ static constexpr int tmem_slot(int blocks) { return box(blocks) + 4 * 4 * kFew; }
+  __host__ __device__ static constexpr int smem_bytes(int blocks) { return tmem_slot(blocks) + 8 + 1024; }
+  static_assert(x_codes % 1024 == 0);
+};
+struct FewParams {
+  const void* x;
+  long long ld_x;
+  bool vec;
+  int M, N, K, num_kb, k_steps, blocks;
+  const float* sw;
+  const float* bias;
+  void* z;
+  long long ld_z;
+  unsigned int* status;
+};
+
+template <typename T, bool BF16, int BLOCK, int TOKENS>
+__global__ void __launch_bounds__(kFewThreads, 2)
+e2m1_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_ws, const FewParams p) {
+  using C = FewCfg<BLOCK>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* const gen = smem_raw + (base - raw);
+  const uint32_t bar0 = base + C::barriers(p.blocks);
+  auto full = [&](uint32_t s) { return bar0 + 8u * s; };
+  auto empty = [&](uint32_t s) { return bar0 + 8u * (kFewStages + s); };
+  const uint32_t tokens_ready = bar0 + 8u * (2 * kFewStages), acc_full = tokens_ready + 8u;
+  volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + C::tmem_slot(p.blocks));
+  volatile uint32_t* const abort_flag = tmem_slot + 1;
+  float* const partial = reinterpret_cast<float*>(gen + C::partial(p.blocks));
+  const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank(), cluster = cluster_nctarank();
+  const int kb_first = static_cast<int>(static_cast<long long>(p.num_kb) * rank / cluster);
+  const int kb_end = static_cast<int>(static_cast<long long>(p.num_kb) * (rank + 1) / cluster);
+  const int ch0 = static_cast<int>(blockIdx.x / cluster) * kCh;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kFewStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+    mbar_init(tokens_ready, 4);
+    mbar_init(acc_full, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+    fence_proxy_async();
+    tma_prefetch_desc(&tm_w); tma_prefetch_desc(&tm_ws);
+  }
+  if (warp == 1) { tmem_alloc(base + C::tmem_slot(p.blocks), C::tmem_cols); tmem_relinquish(); }
+  pdl_wait();
+  pdl_trigger();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  bool ok = true;
+  uint32_t stage = 0, phase = 0;
+  float sw = 1.0f, bias = 0.0f, g[TOKENS];
+  const int ch = ch0 + (warp & 3) * 32 + lane;
+
+  if (warp == 0) {
+    uint32_t issued = 0;
+    for (int kb = kb_first; kb < kb_end && ok; ++kb) {
+      ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag);
+      if (!ok) break;
+      if (elect_one()) {
+        mbar_arrive_expect_tx(full(stage), C::stage_bytes);
+        tma_load_3d(base + stage * C::stage_bytes, &tm_w, full(stage), kb * kBk, ch0, 0);
+        tma_load_3d(base + stage * C::stage_bytes + kSlab, &tm_ws, full(stage), 0, kb * C::k_tiles, ch0 / kCh);
+      }
+      __syncwarp();
+      ++issued;
+      if (++stage == kFewStages) { stage = 0; phase ^= 1u; }
+    }
+    for (int s = 0; s < kFewStages; ++s)               // every copy must have landed before the CTA may exit
+      if (issued > static_cast<uint32_t>(s)) mbar_wait(full(s), ((issued - 1 - s) / kFewStages) & 1u, abort_flag);
+  } else if (warp == 1) {
+    ok = mbar_wait(tokens_ready, 0, abort_flag);
+    const uint32_t idesc0 = (1u << 7) | (1u << 10) | (2u << 17) | ((BLOCK == 32 ? 1u : 0u) << 23) | (1u << 27);
+    for (int kb = kb_first; kb < kb_end && ok; ++kb) {
+      ok = mbar_wait(full(stage), phase, abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+      if (elect_one()) {
+        const int own = kb - kb_first;
+        const uint32_t sa = tmem_base + C::first_scale + stage * C::scale_cols, sb = sa + 4 * C::k_tiles;
+        const uint64_t da = umma_desc_sw128(base + stage * C::stage_bytes, 16, 1024), db = umma_desc_sw128(base + C::x_codes + own * 1024, 16, 1024);
+        const uint64_t dsa = scale_desc(base + stage * C::stage_bytes + kSlab);
+        const uint64_t dsb = scale_desc(base + C::x_scales(p.blocks) + own * C::k_tiles * C::lines);
+#pragma unroll
+        for (int t = 0; t < C::k_tiles; ++t) {
+          tc_copy_scales<false>(sa + 4 * t, dsa + t * (kScaleTile >> 4));
+          tc_copy_scales<false>(sb + 4 * t, dsb + t * (C::lines >> 4));
+        }
+        const int steps = min(kSteps4, p.k_steps - kb * kSteps4);
+#pragma unroll
+        for (int kk = 0; kk < kSteps4; ++kk) {
+          if (kk < steps) {
+            const int t = BLOCK == 16 ? kk : kk / 2;
+            const uint32_t half = BLOCK == 16 ? 0u : 2u * (kk & 1);
+            tc_mma_scaled<BLOCK, false>(tmem_base, da + kk * 2, db + kk * 2, idesc0 | (half << 4) | (half << 29), sa + 4 * t, sb + 4 * t, own > 0 || kk > 0);
+          }
+        }
+        tc_commit(empty(stage));
+      }
+      __syncwarp();
+      if (++stage == kFewStages) { stage = 0; phase ^= 1u; }
+    }
+    if (ok && elect_one()) tc_commit(acc_full);
+    __syncwarp();
+  } else {
+    const int q = threadIdx.x - 64;
+    if (ch < p.N) {
+      if (BLOCK == 16) sw = *(p.sw + ch);
+      if (p.bias) bias = *(p.bias + ch);
+    }
+    const T* const x = static_cast<const T*>(p.x);
+    // this CTA's share of the tokens: chunks 0 .. own - 1 of each, dealt out over the threads (a block of 32 is two lanes, a warp stays
+    // together); the first ones' elements are on their way while the maxima are found
+    const int own = (kb_end - kb_first) * 16, first_chunk = kb_first * 16, tasks = p.M * own;
+    constexpr int kAhead = TOKENS == 1 ? 1 : 2;
+    uint32_t w[kAhead][kWords<T>];
+    auto fetch = [&](int task, uint32_t (&v)[kWords<T>]) {
+      const int m = TOKENS == 1 ? 0 : task / own;
+      load_chunk16(x + (task < tasks ? m : 0) * p.ld_x, (first_chunk + task - m * own) * kChunk, task < tasks ? p.K : 0, p.vec, v);
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) fetch(min(q + 128 * i, tasks), w[i]);
+    // the tokens' maxima, over the whole contraction (blocks of 32 need none)
+    uint32_t top[TOKENS] = {};
+    if constexpr (BLOCK == 16) {
+      uint32_t* const box = reinterpret_cast<uint32_t*>(gen + C::box(p.blocks));
+#pragma unroll 2
+      for (int c = q; c * kChunk < p.K; c += 128) {
+        uint32_t v[TOKENS][kWords<T>];
+#pragma unroll
+        for (int m = 0; m < TOKENS; ++m) load_chunk16(x + (m < p.M ? m : 0) * p.ld_x, c * kChunk, m < p.M ? p.K : 0, p.vec, v[m]);
+#pragma unroll
+        for (int m = 0; m < TOKENS; ++m) top[m] = max(top[m], top_of<T>(v[m]));
+      }
+#pragma unroll
+      for (int m = 0; m < TOKENS; ++m) {
+        top[m] = __reduce_max_sync(0xFFFFFFFFu, top[m]);
+        if (lane == 0) box[4 * m + warp - 2] = top[m];
+      }
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+      for (int m = 0; m < TOKENS; ++m) {
+        const uint4 t = *reinterpret_cast<const uint4*>(box + 4 * m);
+        top[m] = max(max(t.x, t.y), max(t.z, t.w));
+      }
+    }
+    uint32_t flags = 0;
+#pragma unroll
+    for (int m = 0; m < TOKENS; ++m) {
+      g[m] = 1.0f;
+      if (BLOCK == 16 && m < p.M) {
+        g[m] = row_scale(top[m]).g;
+        if (top[m] >= 0x7F800000u) flags |= LUQ_STATUS_NONFINITE;
+        else if (top[m] && top[m] < 0x0D800000u) flags |= LUQ_STATUS_RANGE;
+      }
+    }
+    auto put = [&](int task, const uint32_t (&v)[kWords<T>]) {
+      uint32_t t = top_of<T>(v), byte, row_top = 0;
+      if (BLOCK == 32) {
+        t = max(t, __shfl_xor_sync(0xFFFFFFFFu, t, 1));
+        if (t >= 0x7F800000u) flags |= LUQ_STATUS_NONFINITE;
+      }
+      const int m = TOKENS == 1 ? 0 : min(task / own, TOKENS - 1), c = TOKENS == 1 ? task : task - task / own * own;
+#pragma unroll
+      for (int i = 0; i < TOKENS; ++i) row_top = i == m ? top[i] : row_top;
+      uint2 codes;
+      quantize_chunk<T, BLOCK>(v, t, BLOCK == 16 ? row_scale(row_top) : RowScale{}, codes, byte);
+      if (task < tasks) {
+        const int block = c >> 4, in = c & 15;
+        uint8_t* const to = gen + C::x_codes + block * 1024 + m * 128 + (((in >> 1) ^ m) << 4) + (in & 1) * 8;
+        if (smem_in(to, gen, C::x_codes, C::x_scales(p.blocks), 8, p.status)) *reinterpret_cast<uint2*>(to) = codes;
+        const int b = BLOCK == 16 ? in : in >> 1;
+        uint8_t* const s = gen + C::x_scales(p.blocks) + (block * C::k_tiles + (b >> 2)) * C::lines + m * 16 + (b & 3);
+        if ((BLOCK == 16 || (in & 1) == 0) && smem_in(s, gen, C::x_scales(p.blocks), C::partial(p.blocks), 1, p.status)) *s = static_cast<uint8_t>(byte);
+      }
+    };
+    for (int first = 0; first < tasks; first += 128 * kAhead) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (first > 0) fetch(min(first + q + 128 * i, tasks), w[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) put(first + q + 128 * i, w[i]);
+    }
+    if (flags && ch0 == 0) atomicOr(p.status, flags);
+    fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(tokens_ready);
+
+    ok = mbar_wait(acc_full, 0, abort_flag);
+    uint32_t r[16];
+    if (ok) {
+      tc_fence_after();
+      tmem_ld_32x16(tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16), r);
+      tmem_ld_wait();
+      tc_fence_before();
+      const bool alone = cluster == 1;
+#pragma unroll
+      for (int m = 0; m < TOKENS; ++m) {
+        const float acc = __uint_as_float(r[m]);
+        if (!alone) partial[m * kCh + (warp & 3) * 32 + lane] = acc;
+        else if (m < p.M && ch < p.N) store_z(p.z, m * p.ld_z + ch, fmaf(acc * sw, g[m], bias), BF16);
+      }
+    }
+  }
+  __syncwarp();
+  if (cluster > 1) {
+    cluster_sync_all();                                // every CTA's partial sums are there
+    if (warp >= 2 && ch < p.N) {
+      const uint32_t column = smem_u32(partial + (warp & 3) * 32 + lane);
+#pragma unroll
+      for (int m = 0; m < TOKENS; ++m) {
+        if (m < p.M && m % cluster == rank) {          // tokens dealt out over the CTAs, summed in the CTAs' order
+          float part[kMaxSplit], sum = 0.0f;
+#pragma unroll
+          for (uint32_t c = 0; c < kMaxSplit; ++c) part[c] = c < cluster ? ld_shared_cluster_f32(mapa_shared(column + m * kCh * 4, c)) : 0.0f;
+#pragma unroll
+          for (uint32_t c = 0; c < kMaxSplit; ++c) sum += part[c];
+          if (ok) store_z(p.z, m * p.ld_z + ch, fmaf(sum * sw, g[m], bias), BF16);
+        }
+      }
+    }
+    __syncwarp();
+    cluster_sync_relaxed();                            // and have been read by all
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, LUQ_STATUS_TIMEOUT);
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, C::tmem_cols);
+  }
+}
+
 // output [rows x cols]: boxes of 32 channels, of bf16 with their 16-byte pieces swizzled
 int encode_out(void* fn, CUtensorMap* map, void* ptr, int64_t cols, int64_t rows, int64_t ld, bool bf16) {
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
@@ -699,6 +957,31 @@ int encode_scales(void* fn, CUtensorMap* map, const uint8_t* ptr, int64_t k_tile
                                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS;
 }
 
+// The CTAs that share a tile's contraction where there are few tokens: as many as leave a CTA an SM of its own
+int few_split(long long tiles, int sms, int num_kb) {
+  int split = 1;
+  while (split < kMaxSplit && tiles * split * 2 <= sms && split * 2 <= num_kb) split *= 2;
+  return split;
+}
+int used_sms(const luq_ctx* ctx) { return ctx->sm_limit > 0 && ctx->sm_limit < ctx->sm_count ? ctx->sm_limit : ctx->sm_count; }
+
+template <typename T, bool BF16, int BLOCK, int TOKENS>
+int launch_few(luq_ctx* ctx, const luq_e2m1_args& a, const FewParams& p, long long tiles, int split, cudaStream_t st) {
+  using C = FewCfg<BLOCK>;
+  CUtensorMap tw, tws;
+  if (encode_codes(ctx->encode_tiled, &tw, a.w_codes, (a.K + 1) / 2, a.N, a.ld_w, 1, a.w_stride, kCh)) return LUQ_ERR_CUDA;
+  if (encode_scales(ctx->encode_tiled, &tws, a.w_tiles, luq_e2m1_k_tiles(a.K, BLOCK), tiles, C::k_tiles, 1)) return LUQ_ERR_CUDA;
+  auto kernel = e2m1_few_kernel<T, BF16, BLOCK, TOKENS>;
+  static luq_once_per_device allowed;
+  const cudaError_t attr = allowed([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem_bytes(kFewBlocks)); },
+                                   ctx->device);
+  if (attr != cudaSuccess) return static_cast<int>(attr);
+  const cudaError_t e = luq_launch_kernel(kernel, static_cast<int>(tiles) * split, kFewThreads, static_cast<size_t>(C::smem_bytes(p.blocks)), st,
+                                          LUQ_LAUNCH_EARLY, static_cast<unsigned>(split), tw, tws, p);
+  if (e == cudaSuccess) ctx->launches += 1;
+  return static_cast<int>(e);
+}
+
 template <int BT, bool PAIR, bool SPLIT, bool BF16, int BLOCK>
 int launch(luq_ctx* ctx, const luq_e2m1_args& a, const E2m1Params& p, long long units, int cluster,
            const CUtensorMap& tz, cudaStream_t st) {
@@ -718,7 +1001,7 @@ int launch(luq_ctx* ctx, const luq_e2m1_args& a, const E2m1Params& p, long long 
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem_bytes(LUQ_MAX_GROUPS));
   }, ctx->device);
   if (attr != cudaSuccess) return static_cast<int>(attr);
-  const int sms = (ctx->sm_limit > 0 && ctx->sm_limit < ctx->sm_count) ? ctx->sm_limit : ctx->sm_count;
+  const int sms = used_sms(ctx);
   const long long most = sms * C::per_sm / cluster > 0 ? sms * C::per_sm / cluster : 1;
   const int grid = static_cast<int>(units < most ? units : most) * cluster;
   const cudaError_t e = luq_launch_kernel(kernel, grid, C::threads, static_cast<size_t>(C::smem_bytes(p.groups)), st,
@@ -785,7 +1068,7 @@ int luq_launch_gemm_e2m1(luq_ctx* ctx, const luq_e2m1_args& a, bool early, cudaS
     p.tiles_n = static_cast<int>((a.N + tile_ch - 1) / tile_ch);
     return (p.groups == 1 ? (a.M + tile_rows - 1) / tile_rows : a.M / tile_rows + used) * p.tiles_n;
   };
-  const int sms = (ctx->sm_limit > 0 && ctx->sm_limit < ctx->sm_count) ? ctx->sm_limit : ctx->sm_count;
+  const int sms = used_sms(ctx);
   const long long mean_rows = (a.M + used - 1) / used;
   if (mean_rows > 64) {
     const Choice best = choose_tile(sms, p.num_kb, mean_rows, units);
@@ -796,7 +1079,31 @@ int luq_launch_gemm_e2m1(luq_ctx* ctx, const luq_e2m1_args& a, bool early, cudaS
     return best.split > 1 ? launch_out<64, false, true>(ctx, a, p, n, best.split, tz, st) : launch_out<64, false, false>(ctx, a, p, n, 1, tz, st);
   }
   const long long n = units(64, kCh);
-  int split = 1;
-  while (split < kMaxSplit && n * split * 2 <= sms && split * 2 <= p.num_kb) split *= 2;
+  const int split = few_split(n, sms, p.num_kb);
   return split > 1 ? launch_out<64, false, true>(ctx, a, p, n, split, tz, st) : launch_out<64, false, false>(ctx, a, p, n, 1, tz, st);
+}
+
+bool luq_e2m1_is_few(const luq_ctx* ctx, int64_t M, int64_t N, int64_t K) {
+  const long long tiles = (N + kCh - 1) / kCh;
+  const int num_kb = static_cast<int>((K + 2 * kBk - 1) / (2 * kBk)), split = few_split(tiles, used_sms(ctx), num_kb);
+  return M <= kFew && (num_kb + split - 1) / split <= kFewBlocks && tiles * split <= INT_MAX;
+}
+int luq_launch_e2m1_few(luq_ctx* ctx, const luq_e2m1_args& a, const void* x, int dtype, int64_t ld_x, cudaStream_t st) {
+  FewParams p{};
+  p.x = x; p.ld_x = ld_x; p.M = static_cast<int>(a.M); p.N = static_cast<int>(a.N); p.K = static_cast<int>(a.K);
+  p.vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && (a.M <= 1 || ld_x * (dtype == LUQ_BF16 ? 2 : 4) % 16 == 0);
+  p.num_kb = static_cast<int>((a.K + 2 * kBk - 1) / (2 * kBk));
+  p.k_steps = static_cast<int>((a.K + 63) / 64);
+  p.sw = a.sw; p.bias = a.bias; p.z = a.z; p.ld_z = a.ld_z; p.status = ctx->d_status;
+  const long long tiles = (a.N + kCh - 1) / kCh;
+  const int split = few_split(tiles, used_sms(ctx), p.num_kb);
+  p.blocks = (p.num_kb + split - 1) / split;
+#define LUQ_FEW_TOKENS(T, BF16, BLOCK)                                                                                            \
+  (a.M == 1 ? launch_few<T, BF16, BLOCK, 1>(ctx, a, p, tiles, split, st)                                                          \
+            : launch_few<T, BF16, BLOCK, 2>(ctx, a, p, tiles, split, st))
+#define LUQ_FEW(T, BLOCK) (a.out_bf16 ? LUQ_FEW_TOKENS(T, true, BLOCK) : LUQ_FEW_TOKENS(T, false, BLOCK))
+  if (dtype == LUQ_BF16) return a.block == 16 ? LUQ_FEW(__nv_bfloat16, 16) : LUQ_FEW(__nv_bfloat16, 32);
+  return a.block == 16 ? LUQ_FEW(float, 16) : LUQ_FEW(float, 32);
+#undef LUQ_FEW
+#undef LUQ_FEW_TOKENS
 }
