@@ -106,8 +106,8 @@ extern "C" {
                               return it too.  Set it on the quantizing and on the multiplying context alike.
                               0 (default): one plane per sample.  The paper states SMP as repeated products;
                               it has no counterpart of this shortcut. */
-#define LUQ_OPT_CHECK_SLACK 10 /* checking build only (LUQ_ERR_UNSUPPORTED in the normal one): the checks of layer norm and the
-                              8-bit kernels take rows as n elements (0..64) shorter than they are, so that accesses
+#define LUQ_OPT_CHECK_SLACK 10 /* checking build only (LUQ_ERR_UNSUPPORTED in the normal one): the checks of layer norm, the 8-bit,
+                              e2m1 and expert kernels take rows as n elements (0..64) shorter than they are, so that accesses
                               to the last n, which are sound, are reported and skipped: a test of the checks.  0 (default) */
 #define LUQ_OPT_LEVELS 4   /* kmax of the gradient quantizers, 1..6 (default luq_kmax() = 4): levels
                               alpha * 2^0 .. alpha * 2^kmax with alpha = max / 2^kmax, codes 0..kmax+1.  The

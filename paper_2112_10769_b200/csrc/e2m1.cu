@@ -37,7 +37,15 @@ struct RowsParams {
   int k_tiles;
   unsigned int* status;
   bool vec;                 // rows of x start at multiples of 16 bytes
+#ifdef LUQ_DEBUG
+  int slack;                // LUQ_OPT_CHECK_SLACK
+#endif
 };
+#ifdef LUQ_DEBUG
+#define LUQ_CHECKED_COLS(p) ((p).cols - (p).slack)
+#else
+#define LUQ_CHECKED_COLS(p) ((p).cols)
+#endif
 
 // The offsets that a lane holds of up to kHeldGroups groups: offsets[1 + lane], offsets[33 + lane], ...; more are read for every row.
 constexpr int kHeldOffsets = 4, kHeldGroups = 32 * kHeldOffsets;
@@ -107,7 +115,8 @@ __device__ __forceinline__ long long tile_offset(const RowsParams& p, int tile_r
 template <int BLOCK>
 __device__ __forceinline__ void store_chunk(const RowsParams& p, const Place<BLOCK>& at, int out_row, long long tiles_from, bool tiled, uint2 codes,
                                             uint32_t word) {
-  if (!LUQ_IN_BOUNDS(out_row >= 0 && out_row < p.out_rows, p.status)) return;
+  if (!LUQ_IN_BOUNDS(out_row >= 0 && out_row < p.out_rows && at.code + at.bytes <= max((LUQ_CHECKED_COLS(p) + 1) / 2, static_cast<int>(at.code)), p.status))
+    return;
   if (tiled && at.tile >= 0) *reinterpret_cast<uint32_t*>(p.tiles + tiles_from + at.tile) = word;
   uint8_t* const to = p.codes + out_row * p.ld_codes + at.code;
   if (at.bytes == 8) {
@@ -144,17 +153,18 @@ __global__ void __launch_bounds__(LANES == kBlockRow ? 1024 : 128) e2m1_rows_ker
     const bool there = r < rows;
     if (LANES == 32 && !there) break;                          // (a whole warp; nothing meets)
     const T* const x = static_cast<const T*>(p.x) + (there ? r : 0) * p.ld_x;
+    const int cols = LUQ_IN_BOUNDS(p.cols <= LUQ_CHECKED_COLS(p), p.status) ? p.cols : LUQ_CHECKED_COLS(p);
     uint32_t w[kHeld][kWords<T>], top[kHeld] = {}, row_top = 0;
     int positions = -1;
     if (PLAN && p.position && lane < p.copies) positions = *(p.position + static_cast<long long>(r) * p.copies + lane);
     if constexpr (CHUNKS > 0) {
 #pragma unroll
-      for (int i = 0; i < CHUNKS; ++i) load_chunk16(x, (t + i * lanes) * kChunk, p.cols, p.vec, w[i]);
+      for (int i = 0; i < CHUNKS; ++i) load_chunk16(x, (t + i * lanes) * kChunk, cols, p.vec, w[i]);
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) { top[i] = top_of<T>(w[i]); row_top = max(row_top, top[i]); }
     } else {
       for (int c = t; c * kChunk < p.cols; c += lanes) {
-        load_chunk16(x, c * kChunk, p.cols, p.vec, w[0]);
+        load_chunk16(x, c * kChunk, cols, p.vec, w[0]);
         row_top = max(row_top, top_of<T>(w[0]));
       }
     }
@@ -216,7 +226,7 @@ __global__ void __launch_bounds__(LANES == kBlockRow ? 1024 : 128) e2m1_rows_ker
       });
     } else {
       for (int c = t; c - lane < chunks; c += lanes) {
-        load_chunk16(x, c * kChunk, p.cols, p.vec, w[0]);
+        load_chunk16(x, c * kChunk, cols, p.vec, w[0]);
         uint2 codes;
         const uint32_t word = finish(w[0], top_of<T>(w[0]), c, codes);
         const Place<BLOCK> at(p, c);
@@ -279,6 +289,9 @@ int luq_launch_e2m1_rows(luq_ctx* ctx, const luq_e2m1_rows_args& a, cudaStream_t
   p.out_rows = a.out_rows; p.codes = a.codes; p.ld_codes = a.ld_codes; p.tiles = a.tiles; p.scale = a.scale;
   p.k_tiles = static_cast<int>(luq_e2m1_k_tiles(a.cols, a.block));
   p.status = ctx->d_status;
+#ifdef LUQ_DEBUG
+  p.slack = ctx->check_slack;
+#endif
   p.vec = (reinterpret_cast<uintptr_t>(a.x) & 15u) == 0 && (a.rows <= 1 || a.ld_x * (a.dtype == LUQ_BF16 ? 2 : 4) % 16 == 0);
   if (a.dtype == LUQ_BF16) return a.block == 16 ? launch_plan<__nv_bfloat16, 16>(ctx, p, st) : launch_plan<__nv_bfloat16, 32>(ctx, p, st);
   return a.block == 16 ? launch_plan<float, 16>(ctx, p, st) : launch_plan<float, 32>(ctx, p, st);

@@ -22,6 +22,13 @@ using namespace luqdev;
 
 constexpr uint32_t kFull = 0xFFFFFFFFu;
 
+// Checking build: where the checks take a row (of `n` elements) to end.
+#ifdef LUQ_DEBUG
+#define LUQ_CHECKED(p, n) ((n) - (p).slack)
+#else
+#define LUQ_CHECKED(p, n) (n)
+#endif
+
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
@@ -72,6 +79,9 @@ struct RouteParams {
   bool vec;                 // a lane's logits are whole pieces of 16 bytes
   int size, log_groups;     // experts of a group, log2(groups)
   bool vec_bias;            // so are its biases
+#ifdef LUQ_DEBUG
+  int slack;                // LUQ_OPT_CHECK_SLACK
+#endif
 };
 
 // LANES neighbouring lanes have a row; their maximum, sum, and the mask of those for which `b` holds
@@ -315,7 +325,8 @@ __global__ void __launch_bounds__(128) route_kernel(const RouteParams p) {
   const T* const row = static_cast<const T*>(p.logits) + r * p.ld;
   const int size = p.size, per_group = LANES >> p.log_groups;
   const int in_group = (ls & (per_group - 1)) * VPL, group = ls >> (kLogLanes - p.log_groups);
-  const int e0 = group * size + in_group, n = min(max(size - in_group, 0), VPL);
+  const int e0 = group * size + in_group, held = min(max(size - in_group, 0), VPL);
+  const int n = LUQ_IN_BOUNDS(held == 0 || e0 + held <= LUQ_CHECKED(p, p.experts), p.status) ? held : 0;
   float l[VPL];
   load_lane<T, VPL>(row, e0, n, p.vec, l);
   bool bad = false;
@@ -507,6 +518,10 @@ struct RouteBwdParams {
   void* dlogits;
   long long ld_d;
   bool vec;
+  unsigned int* status;
+#ifdef LUQ_DEBUG
+  int slack;                // LUQ_OPT_CHECK_SLACK
+#endif
 };
 
 template <typename T, int VPL>
@@ -549,7 +564,8 @@ __global__ void __launch_bounds__(128) route_bwd_kernel(const RouteBwdParams p) 
   const long long r = there ? given : p.rows - 1;
   const T* const row = static_cast<const T*>(p.logits) + r * p.ld;
   T* const out = static_cast<T*>(p.dlogits) + r * p.ld_d;
-  const int e0 = ls * VPL, n = min(max(p.experts - e0, 0), VPL);
+  const int e0 = ls * VPL, held = min(max(p.experts - e0, 0), VPL);
+  const int n = LUQ_IN_BOUNDS(held == 0 || e0 + held <= LUQ_CHECKED(p, p.experts), p.status) ? held : 0;
   int e = ls < p.k ? p.chosen[r * p.k + ls] : -1;
   if (e >= p.experts) e = -1;
   const float dw = e >= 0 ? p.dweights[r * p.k + ls] : 0.0f;
@@ -617,6 +633,10 @@ struct OrderParams {
   int* counts;              // [segments][experts], more than one segment
   int* position;
   int* offsets;
+  unsigned int* status;
+#ifdef LUQ_DEBUG
+  int slack;                // LUQ_OPT_CHECK_SLACK
+#endif
 };
 constexpr int kOrderWarps = 32;
 
@@ -711,7 +731,7 @@ __global__ void __launch_bounds__(32 * kOrderWarps) order_kernel(const OrderPara
     __syncwarp();
     if (valid && lane == __ffs(same) - 1) own[x] += __popc(same);
     __syncwarp();
-    if (a + lane < to) p.position[a + lane] = at;
+    if (a + lane < to && LUQ_IN_BOUNDS(a + lane < LUQ_CHECKED(p, p.total), p.status)) p.position[a + lane] = at;
   }
 }
 
@@ -819,12 +839,21 @@ struct MoveParams {
   long long ld_out;
   float* dweights;
   unsigned int* status;
+#ifdef LUQ_DEBUG
+  int slack;                // LUQ_OPT_CHECK_SLACK
+#endif
 };
 template <int MODE> constexpr int kPieces = MODE == kSingle ? 8 : 4;       // pieces of a lane at a time
 // those that it sums copies of (16384 x 2048 bf16, two copies: 45 us, with two pieces 50; 4000 x 1001, four copies: 19 us with four, 14 with two)
 template <int MODE> constexpr int kSumPieces = MODE == kSingle ? 8 : MODE == kWhole ? 4 : 2;
 constexpr int kMoveWarps = 4;                   // warps of a block
 
+// do the elements of a row that a piece from `c` on holds lie in it?  (always true outside the checking build)
+template <int N>
+__device__ __forceinline__ bool piece_in(const MoveParams& p, int c) {
+  (void)p; (void)c;
+  return LUQ_IN_BOUNDS(min(c + N, p.cols) <= LUQ_CHECKED(p, p.cols), p.status);
+}
 // row `to` of the copies, if it is one
 __device__ __forceinline__ bool copy_in(const MoveParams& p, int to) { return to >= 0 && to < p.copies; }
 
@@ -836,7 +865,7 @@ __device__ __forceinline__ void zero_rest(const MoveParams& p, long long warp, l
   zero.zero();
   for (long long r = used + warp; r < p.copies; r += warps) {
     T* const row = static_cast<T*>(p.out) + r * p.ld_out;
-    for (int c = lane * zero.n - lead<T, MODE>(row); c < p.cols; c += 32 * zero.n) zero.store(row, c, p.cols);
+    for (int c = lane * zero.n - lead<T, MODE>(row); c < p.cols; c += 32 * zero.n) if (piece_in<zero.n>(p, c)) zero.store(row, c, p.cols);
   }
 }
 
@@ -857,7 +886,7 @@ __global__ void __launch_bounds__(32 * kMoveWarps) dispatch_kernel(const MovePar
     if constexpr (MODE != kShifted) {
 #pragma unroll
       for (int u = 0; u < kPieces<MODE>; ++u)
-        if (first + u * 32 * P::n < p.cols) v[u].load(row, first + u * 32 * P::n, p.cols);
+        if (first + u * 32 * P::n < p.cols && piece_in<P::n>(p, first + u * 32 * P::n)) v[u].load(row, first + u * 32 * P::n, p.cols);
     }
     for (int j0 = 0; j0 < p.k; j0 += 32) {
       const int mine = j0 + lane < p.k ? p.position[t * p.k + j0 + lane] : -1;
@@ -869,11 +898,11 @@ __global__ void __launch_bounds__(32 * kMoveWarps) dispatch_kernel(const MovePar
         if constexpr (MODE == kShifted) {
 #pragma unroll
           for (int u = 0; u < kPieces<MODE>; ++u)
-            if (c0 + u * 32 * P::n < p.cols) v[u].load(row, c0 + u * 32 * P::n, p.cols);
+            if (c0 + u * 32 * P::n < p.cols && piece_in<P::n>(p, c0 + u * 32 * P::n)) v[u].load(row, c0 + u * 32 * P::n, p.cols);
         }
 #pragma unroll
         for (int u = 0; u < kPieces<MODE>; ++u)
-          if (c0 + u * 32 * P::n < p.cols) v[u].store(out, c0 + u * 32 * P::n, p.cols);
+          if (c0 + u * 32 * P::n < p.cols && piece_in<P::n>(p, c0 + u * 32 * P::n)) v[u].store(out, c0 + u * 32 * P::n, p.cols);
       }
     }
   }
@@ -907,7 +936,7 @@ __global__ void __launch_bounds__(32 * kMoveWarps) combine_kernel(const MovePara
     for (int u = 0; u < kAt; ++u) {
       const int c = first + u * 32 * P::n;
       r[u].zero();
-      if (p.more && c < p.cols) r[u].load(static_cast<const T*>(p.more) + t * p.ld_more, c, p.cols);
+      if (p.more && c < p.cols && piece_in<P::n>(p, c)) r[u].load(static_cast<const T*>(p.more) + t * p.ld_more, c, p.cols);
     }
     int mine = next_at;
     float weight = next_w;
@@ -929,7 +958,7 @@ __global__ void __launch_bounds__(32 * kMoveWarps) combine_kernel(const MovePara
         for (int u = 0; u < kAt; ++u) {
           const int c = first + u * 32 * P::n;
           v[u].zero();
-          if (copy_in(p, at) && c < p.cols) v[u].load(static_cast<const T*>(p.x) + at * p.ld_x, c, p.cols);
+          if (copy_in(p, at) && c < p.cols && piece_in<P::n>(p, c)) v[u].load(static_cast<const T*>(p.x) + at * p.ld_x, c, p.cols);
         }
 #pragma unroll
         for (int u = 0; u < kAt; ++u)
@@ -941,7 +970,7 @@ __global__ void __launch_bounds__(32 * kMoveWarps) combine_kernel(const MovePara
     for (int u = 0; u < kAt; ++u) {
       const int c = first + u * 32 * P::n;
       r[u].set(sum[u]);
-      if (c < p.cols) r[u].store(out, c, p.cols);
+      if (c < p.cols && piece_in<P::n>(p, c)) r[u].store(out, c, p.cols);
     }
   }
 }
@@ -973,7 +1002,7 @@ __global__ void __launch_bounds__(32 * kMoveWarps) combine_bwd_kernel(const Move
         const int c = first + u * 32 * P::n;
         d[u].zero();
         y[u].zero();
-        if (c < p.cols) {
+        if (c < p.cols && piece_in<P::n>(p, c)) {
           d[u].load(d_row, c, p.cols);
           if (p.dweights) y[u].load(y_row, c, p.cols);
         }
@@ -990,7 +1019,7 @@ __global__ void __launch_bounds__(32 * kMoveWarps) combine_bwd_kernel(const Move
         }
         P r;
         r.set(g);
-        if (p.out && c < p.cols) r.store(out, c, p.cols);
+        if (p.out && c < p.cols && piece_in<P::n>(p, c)) r.store(out, c, p.cols);
       }
     }
     dot = warp_sum(dot);
@@ -1048,6 +1077,9 @@ MoveParams move_params(const luq_ctx* ctx, const luq_move_args& a, bool& whole) 
   p.x = a.x; p.ld_x = a.ld_x; p.more = a.more; p.ld_more = a.ld_more; p.position = a.position; p.rows = a.rows; p.k = a.k;
   p.cols = static_cast<int>(a.cols); p.copies = a.copies; p.weights = a.weights; p.offsets = a.offsets; p.groups = a.groups;
   p.out = a.out; p.ld_out = a.ld_out; p.dweights = a.dweights; p.status = ctx->d_status;
+#ifdef LUQ_DEBUG
+  p.slack = ctx->check_slack;
+#endif
   // (row counts play no part: a row of one is as good as any)
   whole = a.cols * esize % 16 == 0 && vec16(a.x, a.ld_x, 2, esize) && vec16(a.more, a.ld_more, 2, esize) && vec16(a.out, a.ld_out, 2, esize);
   return p;
@@ -1088,17 +1120,23 @@ static bool route_vec(const void* p, int64_t ld, int size, int esize) {
 
 int luq_launch_route(luq_ctx* ctx, const luq_route_args& a, cudaStream_t st) {
   const int esize = a.dtype == LUQ_BF16 ? 2 : 4, size = a.experts / a.groups;
-  const RouteParams p{a.logits, a.rows, a.ld, a.experts, a.k, a.sigmoid, a.bias, a.groups, a.top_groups, a.group_top, a.renormalize, a.scale,
+  RouteParams p{a.logits, a.rows, a.ld, a.experts, a.k, a.sigmoid, a.bias, a.groups, a.top_groups, a.group_top, a.renormalize, a.scale,
                       a.chosen, a.weights, ctx->d_status, route_vec(a.logits, a.ld, size, esize), size, __builtin_ctz(a.groups),
                       a.bias && (reinterpret_cast<uintptr_t>(a.bias) & 15u) == 0 && size % 4 == 0};
+#ifdef LUQ_DEBUG
+  p.slack = ctx->check_slack;
+#endif
   const int lanes = route_lanes(a.experts, a.k, a.groups), per_group = lanes / a.groups, held = (size + per_group - 1) / per_group;
   return a.dtype == LUQ_BF16 ? launch_route_lanes<__nv_bfloat16>(ctx, p, lanes, held, st) : launch_route_lanes<float>(ctx, p, lanes, held, st);
 }
 
 int luq_launch_route_bwd(luq_ctx* ctx, const luq_route_args& a, const float* dweights, void* dlogits, int64_t ld_d, cudaStream_t st) {
   const int esize = a.dtype == LUQ_BF16 ? 2 : 4;
-  const RouteBwdParams p{dweights, a.logits, a.rows, a.ld, a.experts, a.k, a.sigmoid, a.renormalize, a.scale, a.chosen, dlogits, ld_d,
-                         route_vec(a.logits, a.ld, a.experts, esize) && route_vec(dlogits, ld_d, a.experts, esize)};
+  RouteBwdParams p{dweights, a.logits, a.rows, a.ld, a.experts, a.k, a.sigmoid, a.renormalize, a.scale, a.chosen, dlogits, ld_d,
+                         route_vec(a.logits, a.ld, a.experts, esize) && route_vec(dlogits, ld_d, a.experts, esize), ctx->d_status};
+#ifdef LUQ_DEBUG
+  p.slack = ctx->check_slack;
+#endif
   const int lanes = route_lanes(a.experts, a.k, 1), held = (a.experts + lanes - 1) / lanes;
   return a.dtype == LUQ_BF16 ? launch_route_lanes<__nv_bfloat16>(ctx, p, lanes, held, st) : launch_route_lanes<float>(ctx, p, lanes, held, st);
 }
@@ -1118,7 +1156,10 @@ size_t luq_order_workspace(int64_t total, int experts) {
   return n > 1 ? static_cast<size_t>(n) * experts * sizeof(int) : 0;
 }
 int luq_launch_order(luq_ctx* ctx, const int* chosen, int64_t total, int experts, int* position, int* offsets, int* counts, cudaStream_t st) {
-  OrderParams p{chosen, total, experts, 0, counts, position, offsets};
+  OrderParams p{chosen, total, experts, 0, counts, position, offsets, ctx->d_status};
+#ifdef LUQ_DEBUG
+  p.slack = ctx->check_slack;
+#endif
   int64_t segment;
   const int blocks = total > 0 ? static_cast<int>(order_segments(total, &segment)) : 1;
   if (total == 0) segment = 32 * kOrderWarps;

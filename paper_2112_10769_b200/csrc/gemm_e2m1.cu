@@ -713,6 +713,9 @@ struct FewParams {
   void* z;
   long long ld_z;
   unsigned int* status;
+#ifdef LUQ_DEBUG
+  int slack;                // LUQ_OPT_CHECK_SLACK
+#endif
 };
 
 template <typename T, bool BF16, int BLOCK, int TOKENS>
@@ -902,7 +905,7 @@ e2m1_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
       for (int m = 0; m < TOKENS; ++m) {
         const float acc = __uint_as_float(r[m]);
         if (!alone) partial[m * kCh + (warp & 3) * 32 + lane] = acc;
-        else if (m < p.M && ch < p.N) store_z(p.z, m * p.ld_z + ch, fmaf(acc * sw, g[m], bias), BF16);
+        else if (m < p.M && ch < p.N && LUQ_IN_BOUNDS(ch < LUQ_CHECKED_N(p), p.status)) store_z(p.z, m * p.ld_z + ch, fmaf(acc * sw, g[m], bias), BF16);
       }
     }
   }
@@ -919,7 +922,7 @@ e2m1_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
           for (uint32_t c = 0; c < kMaxSplit; ++c) part[c] = c < cluster ? ld_shared_cluster_f32(mapa_shared(column + m * kCh * 4, c)) : 0.0f;
 #pragma unroll
           for (uint32_t c = 0; c < kMaxSplit; ++c) sum += part[c];
-          if (ok) store_z(p.z, m * p.ld_z + ch, fmaf(sum * sw, g[m], bias), BF16);
+          if (ok && LUQ_IN_BOUNDS(ch < LUQ_CHECKED_N(p), p.status)) store_z(p.z, m * p.ld_z + ch, fmaf(sum * sw, g[m], bias), BF16);
         }
       }
     }
@@ -1095,6 +1098,9 @@ int luq_launch_e2m1_few(luq_ctx* ctx, const luq_e2m1_args& a, const void* x, int
   p.num_kb = static_cast<int>((a.K + 2 * kBk - 1) / (2 * kBk));
   p.k_steps = static_cast<int>((a.K + 63) / 64);
   p.sw = a.sw; p.bias = a.bias; p.z = a.z; p.ld_z = a.ld_z; p.status = ctx->d_status;
+#ifdef LUQ_DEBUG
+  p.slack = ctx->check_slack;
+#endif
   const long long tiles = (a.N + kCh - 1) / kCh;
   const int split = few_split(tiles, used_sms(ctx), p.num_kb);
   p.blocks = (p.num_kb + split - 1) / split;
