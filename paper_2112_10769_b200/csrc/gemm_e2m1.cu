@@ -60,6 +60,7 @@ struct E2m1Params {
   int tiles_n;              // channel tiles
   int early;                // everything but the tokens' codes and scales was there before the preceding kernel
   int z_tma;                // the output can be addressed by TMA
+  int z_fours;              // four neighbouring channels from a multiple of four on can be stored at once
   long long tma_cols;       // a store copy writes whole 16-byte pieces: boxes up to this column end on one
 #ifdef LUQ_DEBUG
   int slack;                // LUQ_OPT_CHECK_SLACK
@@ -155,6 +156,11 @@ __device__ __forceinline__ void tmem_ld_16x32(uint32_t taddr, uint32_t* r) {
 // four 8 x 8 matrices of 16-bit numbers, transposed: thread t gives the address of row t mod 8 of matrix t / 8
 __device__ __forceinline__ void stmatrix_trans(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ float4 ld_shared_cluster_f32x4(uint32_t cluster_addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
+  return v;
 }
 __device__ __forceinline__ float ld_shared_cluster_f32(uint32_t cluster_addr) { return __int_as_float(ld_shared_cluster(cluster_addr)); }
 
@@ -308,30 +314,57 @@ __device__ __forceinline__ void write_tile(const E2m1Params& p, const void* tm_z
   }
 }
 
-// Adds a channel's partial sums of Q CTAs (of fewer, if the cluster has fewer) for every stride-th token and
-// writes the results; sixteen loads from the other CTAs are on their way at once.
+// Adds the partial sums of Q CTAs (of fewer, if the cluster has fewer) in the CTAs' order and writes the results: a warp takes every
+// stride-th token, a lane four neighbouring channels.  Eight loads from the CTAs are on their way at once.
 template <int Q>
-__device__ __forceinline__ void join(const E2m1Params& p, const Unit& v, uint32_t column, uint32_t end, int first_token, int stride, int ch,
-                                     float sw, float bias, const float* scales, bool bf16) {
-  constexpr int U = 16 / Q;
-  const int cluster = static_cast<int>(cluster_nctarank());
+__device__ __forceinline__ void join(const E2m1Params& p, const Unit& v, uint32_t partial, uint32_t end, int first_token, int stride, int lane,
+                                     const float* scales, bool block16, bool bf16) {
+  constexpr int U = 8 / Q;
+  const int cluster = static_cast<int>(cluster_nctarank()), ch = v.ch0 + 4 * lane;
+  const long long wi = static_cast<long long>(v.group) * p.N + ch;
+  float sw[4], bias[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    sw[i] = block16 && ch + i < p.N ? *(p.sw + wi + i) : 1.0f;
+    bias[i] = p.bias && ch + i < p.N ? *(p.bias + wi + i) : 0.0f;
+  }
   for (int t0 = first_token; t0 < v.rows; t0 += U * stride) {
-    float part[U][Q];
+    float4 part[U][Q];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      const uint32_t at = partial + (min(t0 + u * stride, v.rows - 1) * kCh + 4 * lane) * 4;
 #pragma unroll
       for (int q = 0; q < Q; ++q)
-        part[u][q] = q < cluster && t0 + u * stride < v.rows &&
-                             LUQ_IN_BOUNDS(t0 >= 0 && column + (t0 + u * stride) * kCh * 4 + 4 <= end, p.status) ? ld_shared_cluster_f32(mapa_shared(column + (t0 + u * stride) * kCh * 4, q)) : 0.0f;
+        if (LUQ_IN_BOUNDS(at + 16 <= end, p.status)) part[u][q] = ld_shared_cluster_f32x4(mapa_shared(at, min(q, cluster - 1)));
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int t = t0 + u * stride;
-      float sum = 0.0f;                  // in the CTAs' order: a call repeats bit for bit
+      float sum[4] = {};
 #pragma unroll
-      for (int q = 0; q < Q; ++q) sum += part[u][q];
-      if (t < v.rows && z_in(p, v.row0 + t, ch))
-        store_z(p.z, (static_cast<long long>(v.row0) + t) * p.ld_z + ch, fmaf(sum * sw, scales[t], bias), bf16);
+      for (int q = 0; q < Q; ++q) {
+        if (q < cluster) {
+          sum[0] += part[u][q].x; sum[1] += part[u][q].y; sum[2] += part[u][q].z; sum[3] += part[u][q].w;
+        }
+      }
+      if (t >= v.rows) break;
+      float z[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[i] = fmaf(sum[i] * sw[i], scales[t], bias[i]);
+      const long long at = (static_cast<long long>(v.row0) + t) * p.ld_z + ch;
+      if (p.z_fours && ch + 3 < p.N && z_in(p, v.row0 + t, ch + 3)) {
+        if (bf16) {
+          const __nv_bfloat162 a = __floats2bfloat162_rn(z[0], z[1]), b = __floats2bfloat162_rn(z[2], z[3]);
+          *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.z) + at) =
+              make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+        } else {
+          *reinterpret_cast<float4*>(static_cast<float*>(p.z) + at) = make_float4(z[0], z[1], z[2], z[3]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (ch + i < p.N && z_in(p, v.row0 + t, ch + i)) store_z(p.z, at + i, z[i], bf16);
+      }
     }
   }
 }
@@ -644,16 +677,12 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
       __syncwarp();
       cluster_sync_all();              // every CTA's partial tile is there
       if (warp >= kFirstEpiWarp) {
-        // a token's 128 channels at a time, tokens dealt out over the CTAs
-        const int ch = v.ch0 + (warp & 3) * 32 + lane;
-        const int first_token = static_cast<int>(rank) + (warp_e >> 2) * static_cast<int>(cluster);
-        const int stride = static_cast<int>(cluster) * (C::epi_warps / 4);
-        const uint32_t column = smem_u32(partial + (warp & 3) * 32 + lane);
-        if (ch < p.N) {                // every load below is used, and so has ended, before the meeting after it
-          if (cluster <= 2) join<2>(p, v, column, base + C::staging, first_token, stride, ch, sw_ahead, bias_ahead, scales_of(it), BF16);
-          else if (cluster <= 4) join<4>(p, v, column, base + C::staging, first_token, stride, ch, sw_ahead, bias_ahead, scales_of(it), BF16);
-          else join<8>(p, v, column, base + C::staging, first_token, stride, ch, sw_ahead, bias_ahead, scales_of(it), BF16);
-        }
+        // tokens dealt out over the warps and CTAs; every load below is used, and so has ended, before the meeting after it
+        const int first_token = warp_e * static_cast<int>(cluster) + static_cast<int>(rank), stride = static_cast<int>(cluster) * C::epi_warps;
+        const uint32_t from = smem_u32(partial), end = base + C::staging;
+        if (cluster <= 2) join<2>(p, v, from, end, first_token, stride, lane, scales_of(it), BLOCK == 16, BF16);
+        else if (cluster <= 4) join<4>(p, v, from, end, first_token, stride, lane, scales_of(it), BLOCK == 16, BF16);
+        else join<8>(p, v, from, end, first_token, stride, lane, scales_of(it), BLOCK == 16, BF16);
         fence_proxy_async();           // the next tile's copies come after these reads
       }
       __syncwarp();
@@ -960,11 +989,39 @@ int encode_scales(void* fn, CUtensorMap* map, const uint8_t* ptr, int64_t k_tile
                                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS;
 }
 
-// The CTAs that share a tile's contraction where there are few tokens: as many as leave a CTA an SM of its own
-int few_split(long long tiles, int sms, int num_kb) {
-  int split = 1;
-  while (split < kMaxSplit && tiles * split * 2 <= sms && split * 2 <= num_kb) split *= 2;
-  return split;
+// How long the product takes with each tile and split, in microseconds: a start, and for every round over the SMs the stages of a
+// CTA's share and what a tile costs at its ends.  64-token tiles come two to an SM: where they do, a stage takes longer, and so do
+// their ends.  A split pays its meeting and the sums over the other CTAs' memory, and is taken in a single round only.  Fitted to 300
+// products of 1 to 16384 tokens, 64 to 8192 channels and contraction elements, each timed with every tile and split: the choice was the
+// best one or 1.7% from it on average, a tenth of them 7% and more, at worst 5055 x 128 x 4288 9.2 us where 7.2 would do.
+struct Choice { int tokens, split; };
+template <class Units>
+Choice choose_tile(int sms, int num_kb, long long mean_rows, Units units) {
+  struct Tile { int tokens, channels, ctas; float start, stage, ends; };        // ctas: that one tile occupies
+  constexpr Tile tiles[] = {{64, kCh, 1, 3.0f, 0.205f, 0.0f}, {128, kCh, 1, 2.2f, 0.264f, 1.16f}, {256, 2 * kCh, 2, 3.2f, 0.335f, 2.0f}};
+  Choice best{64, 1};
+  float best_time = 3.4e38f;
+  for (const Tile& t : tiles) {
+    if ((t.tokens == 256 && sms < 2) || (t.tokens > 64 && mean_rows * 2 <= t.tokens)) continue;
+    const long long n = units(t.tokens, t.channels), slots = t.tokens == 64 ? 2 * sms : sms / t.ctas;
+    const float rows = static_cast<float>(mean_rows < t.tokens ? mean_rows : t.tokens);
+    for (int split = 1; split <= kMaxSplit; split *= 2) {
+      if (split > 1 && (t.tokens == 256 || n * split > slots || split > num_kb)) break;
+      const float share = static_cast<float>((num_kb + split - 1) / split);
+      auto round = [&](long long ctas) {                 // of so many CTAs
+        const float second = t.tokens == 64 && ctas > sms ? static_cast<float>(ctas - sms) / sms : 0.0f;      // SMs that have two
+        return share * t.stage * (1.0f + 1.28f * second) + t.ends + 1.5f * second;
+      };
+      const long long rest = n * split % slots;
+      const float time = t.start + static_cast<float>(n * split / slots) * round(slots) + (rest ? round(rest) : 0.0f) + (split > 1 ? 0.38f + 0.015f * rows : 0.0f);
+      if (time < best_time) { best_time = time; best = {t.tokens, split}; }
+    }
+  }
+  return best;
+}
+// (the one or two tokens of the launch above have 64-token tiles too: the same split, and so the same sums)
+int few_split(long long tiles, int sms, int num_kb, int M) {
+  return choose_tile(sms, num_kb, M, [&](int, int) { return tiles; }).split;
 }
 int used_sms(const luq_ctx* ctx) { return ctx->sm_limit > 0 && ctx->sm_limit < ctx->sm_count ? ctx->sm_limit : ctx->sm_count; }
 
@@ -1022,31 +1079,6 @@ int launch_out(luq_ctx* ctx, const luq_e2m1_args& a, const E2m1Params& p, long l
                     : launch<BT, PAIR, SPLIT, false, 32>(ctx, a, p, units, cluster, tz, st);
 }
 
-// How long the product takes with each tile, in hundredths of a microsecond past the launch: rounds over the SMs
-// x (stages x the time of one + what a tile costs at its ends).  A split pays its meeting and the sums over the other CTAs'
-// memory; it is taken in a single round only.
-struct Choice { int tokens, split; };
-template <class Units>
-Choice choose_tile(int sms, int num_kb, long long mean_rows, Units units) {
-  struct Tile { int tokens, channels, ctas, stage, ends, meeting; };        // ctas: that one tile occupies
-  constexpr Tile tiles[] = {{256, 2 * kCh, 2, 48, 150, 0}, {128, kCh, 1, 42, 50, 210}, {64, kCh, 1, 32, 50, 140}};
-  Choice best{64, 1};
-  long long best_time = LLONG_MAX;
-  for (const Tile& t : tiles) {
-    if (t.tokens == 256 && (sms < 2 || mean_rows <= 128)) continue;
-    const long long n = units(t.tokens, t.channels);
-    for (int split = 1; split <= kMaxSplit; split *= 2) {
-      // clusters of four and eight do not fill the SMs: a group of SMs that share clusters has 16 to 20
-      const long long slots = split > 2 ? sms - sms / 8 : sms;
-      if (split > 1 && (t.tokens == 256 || n * split > slots || split > num_kb)) break;
-      const long long rounds = (n + sms / t.ctas - 1) / (sms / t.ctas);
-      const long long time = rounds * ((num_kb + split - 1) / split * t.stage + t.ends) + (split > 1 ? t.meeting : 0);
-      if (time < best_time) { best_time = time; best = {t.tokens, split}; }
-    }
-  }
-  return best;
-}
-
 }  // namespace
 
 int luq_launch_gemm_e2m1(luq_ctx* ctx, const luq_e2m1_args& a, bool early, cudaStream_t st) {
@@ -1063,6 +1095,7 @@ int luq_launch_gemm_e2m1(luq_ctx* ctx, const luq_e2m1_args& a, bool early, cudaS
   const int64_t esize = a.out_bf16 ? 2 : 4;
   p.z_tma = (reinterpret_cast<uintptr_t>(a.z) & 15u) == 0 && (a.ld_z * esize) % 16 == 0;
   p.tma_cols = a.N / (16 / esize) * (16 / esize);
+  p.z_fours = reinterpret_cast<uintptr_t>(a.z) % (4 * esize) == 0 && a.ld_z % 4 == 0;
   CUtensorMap tz{};                                   // not used where copies cannot address the output
   if (p.z_tma && encode_out(ctx->encode_tiled, &tz, a.z, a.N, a.M, a.ld_z, a.out_bf16 != 0)) return LUQ_ERR_CUDA;
   // most tiles there can be: at most one partial token tile per group that has rows
@@ -1073,23 +1106,19 @@ int luq_launch_gemm_e2m1(luq_ctx* ctx, const luq_e2m1_args& a, bool early, cudaS
   };
   const int sms = used_sms(ctx);
   const long long mean_rows = (a.M + used - 1) / used;
-  if (mean_rows > 64) {
-    const Choice best = choose_tile(sms, p.num_kb, mean_rows, units);
-    const long long n = units(best.tokens, best.tokens == 256 ? 2 * kCh : kCh);
-    if (best.tokens == 256) return launch_out<256, true, false>(ctx, a, p, n, 2, tz, st);
-    if (best.tokens == 128)
-      return best.split > 1 ? launch_out<128, false, true>(ctx, a, p, n, best.split, tz, st) : launch_out<128, false, false>(ctx, a, p, n, 1, tz, st);
-    return best.split > 1 ? launch_out<64, false, true>(ctx, a, p, n, best.split, tz, st) : launch_out<64, false, false>(ctx, a, p, n, 1, tz, st);
-  }
-  const long long n = units(64, kCh);
-  const int split = few_split(n, sms, p.num_kb);
-  return split > 1 ? launch_out<64, false, true>(ctx, a, p, n, split, tz, st) : launch_out<64, false, false>(ctx, a, p, n, 1, tz, st);
+  const Choice best = choose_tile(sms, p.num_kb, mean_rows, units);
+  const long long n = units(best.tokens, best.tokens == 256 ? 2 * kCh : kCh);
+  if (best.tokens == 256) return launch_out<256, true, false>(ctx, a, p, n, 2, tz, st);
+  if (best.tokens == 128)
+    return best.split > 1 ? launch_out<128, false, true>(ctx, a, p, n, best.split, tz, st) : launch_out<128, false, false>(ctx, a, p, n, 1, tz, st);
+  return best.split > 1 ? launch_out<64, false, true>(ctx, a, p, n, best.split, tz, st) : launch_out<64, false, false>(ctx, a, p, n, 1, tz, st);
 }
 
 bool luq_e2m1_is_few(const luq_ctx* ctx, int64_t M, int64_t N, int64_t K) {
+  if (M > kFew) return false;
   const long long tiles = (N + kCh - 1) / kCh;
-  const int num_kb = static_cast<int>((K + 2 * kBk - 1) / (2 * kBk)), split = few_split(tiles, used_sms(ctx), num_kb);
-  return M <= kFew && (num_kb + split - 1) / split <= kFewBlocks && tiles * split <= INT_MAX;
+  const int num_kb = static_cast<int>((K + 2 * kBk - 1) / (2 * kBk)), split = few_split(tiles, used_sms(ctx), num_kb, static_cast<int>(M));
+  return (num_kb + split - 1) / split <= kFewBlocks && tiles * split <= INT_MAX;
 }
 int luq_launch_e2m1_few(luq_ctx* ctx, const luq_e2m1_args& a, const void* x, int dtype, int64_t ld_x, cudaStream_t st) {
   FewParams p{};
@@ -1102,7 +1131,7 @@ int luq_launch_e2m1_few(luq_ctx* ctx, const luq_e2m1_args& a, const void* x, int
   p.slack = ctx->check_slack;
 #endif
   const long long tiles = (a.N + kCh - 1) / kCh;
-  const int split = few_split(tiles, used_sms(ctx), p.num_kb);
+  const int split = few_split(tiles, used_sms(ctx), p.num_kb, p.M);
   p.blocks = (p.num_kb + split - 1) / split;
 #define LUQ_FEW_TOKENS(T, BF16, BLOCK)                                                                                            \
   (a.M == 1 ? launch_few<T, BF16, BLOCK, 1>(ctx, a, p, tiles, split, st)                                                          \
