@@ -1156,7 +1156,7 @@ int luq_launch_route_bwd(luq_ctx* ctx, const luq_route_args& a, const float* dwe
 static int64_t order_segments(int64_t total, int64_t* segment) {
   constexpr int64_t kStep = 32 * kOrderWarps, kAlone = 2 * kStep, kMost = 256;
   int64_t s = kStep;
-  if (total <= kAlone) s = (total + kStep - 1) / kStep * kStep;      // one launch (4096 assignments: 5.7 us in one block, 5.2 in two launches)
+  if (total <= kAlone) s = total > kStep ? kAlone : kStep;      // one launch (4096 assignments: 5.7 us in one block, 5.2 in two launches)
   else if (total > kStep * kMost) s = ((total + kMost - 1) / kMost + kStep - 1) / kStep * kStep;
   *segment = s;
   return (total + s - 1) / s;
