@@ -335,7 +335,7 @@ __device__ __forceinline__ void join(const E2m1Params& p, const Unit& v, uint32_
       const uint32_t at = partial + (min(t0 + u * stride, v.rows - 1) * kCh + 4 * lane) * 4;
 #pragma unroll
       for (int q = 0; q < Q; ++q)
-        if (LUQ_IN_BOUNDS(at + 16 <= end, p.status)) part[u][q] = ld_shared_cluster_f32x4(mapa_shared(at, min(q, cluster - 1)));
+        part[u][q] = LUQ_IN_BOUNDS(at + 16 <= end, p.status) ? ld_shared_cluster_f32x4(mapa_shared(at, min(q, cluster - 1))) : make_float4(0, 0, 0, 0);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -347,7 +347,7 @@ __device__ __forceinline__ void join(const E2m1Params& p, const Unit& v, uint32_
           sum[0] += part[u][q].x; sum[1] += part[u][q].y; sum[2] += part[u][q].z; sum[3] += part[u][q].w;
         }
       }
-      if (t >= v.rows) break;
+      if (t >= v.rows) continue;
       float z[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) z[i] = fmaf(sum[i] * sw[i], scales[t], bias[i]);
@@ -680,9 +680,12 @@ e2m1_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         // tokens dealt out over the warps and CTAs; every load below is used, and so has ended, before the meeting after it
         const int first_token = warp_e * static_cast<int>(cluster) + static_cast<int>(rank), stride = static_cast<int>(cluster) * C::epi_warps;
         const uint32_t from = smem_u32(partial), end = base + C::staging;
+#ifndef LUQ_DEBUG                      // (with the checks, the three forms of a 64-token tile together end the assembler, ptxas 12.9, with a fault)
         if (cluster <= 2) join<2>(p, v, from, end, first_token, stride, lane, scales_of(it), BLOCK == 16, BF16);
         else if (cluster <= 4) join<4>(p, v, from, end, first_token, stride, lane, scales_of(it), BLOCK == 16, BF16);
-        else join<8>(p, v, from, end, first_token, stride, lane, scales_of(it), BLOCK == 16, BF16);
+        else
+#endif
+          join<8>(p, v, from, end, first_token, stride, lane, scales_of(it), BLOCK == 16, BF16);
         fence_proxy_async();           // the next tile's copies come after these reads
       }
       __syncwarp();
