@@ -497,7 +497,7 @@ int luq_quant_e2m1_rows(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, 
 
 /* Z[t,n] = gx[t] gw[n] sum_b sx[t,b] sw[n,b] sum_(k in b) X[t,k] W[n,k] + bias[n], binary32 sums.  Scales and codes as
  * above, any values; d_x_scale and d_w_scale are the rows' scales (block 16; NULL with block 32).  d_bias may be NULL.
- * 1 <= K < 2^31. */
+ * 1 <= K <= 2^30 (LUQ_ERR_UNSUPPORTED beyond, in the quantizer too).  Inputs and outputs must not overlap, here and below. */
 int luq_gemm_e2m1(luq_ctx* ctx, const uint8_t* d_x_codes, int64_t ld_x, const uint8_t* d_x_tiles, const float* d_x_scale, int block,
                   const uint8_t* d_w_codes, int64_t ld_w, const uint8_t* d_w_tiles, const float* d_w_scale, const float* d_bias,
                   void* d_z, int z_dtype, int64_t ld_z, int64_t M, int64_t N, int64_t K, void* stream);

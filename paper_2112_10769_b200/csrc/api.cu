@@ -705,12 +705,15 @@ int luq_quant_int8_gemm_grouped(luq_ctx* ctx, const void* d_x, int dtype, int64_
 
 namespace {
 
+constexpr int64_t kMostNumbers = 1ll << 30;           // of a row: chunk counts and their multiples stay in int32
+
 int64_t code_bytes(int64_t K) { return (K + 1) / 2; }
 bool tiles_ok(const void* p, bool needed) { return p ? aligned16(p) : !needed; }
 bool ints_ok(const void* p, bool needed) { return p ? (reinterpret_cast<uintptr_t>(p) & 3u) == 0 : !needed; }
 
 int e2m1_args_ok(const luq_e2m1_args& a, int z_dtype, bool grouped) {
   if (!element_type(z_dtype) || !rows_ok(a.M, a.K) || a.N < 0 || a.N > kMaxExtent || (a.block != 16 && a.block != 32)) return LUQ_ERR_ARG;
+  if (a.K > kMostNumbers) return LUQ_ERR_UNSUPPORTED;
   if (grouped && (a.groups < 1 || a.groups > LUQ_MAX_GROUPS || !ints_ok(a.offsets, a.M && a.N))) return LUQ_ERR_ARG;
   if (grouped && (a.w_stride % 16 || a.w_stride >= (1ll << 40) ||
                   (a.groups > 1 && a.N && a.w_stride < (a.N - 1) * a.ld_w + code_bytes(a.K)))) return LUQ_ERR_ARG;
@@ -774,6 +777,7 @@ int luq_quant_e2m1_rows(luq_ctx* ctx, const void* d_x, int dtype, int64_t rows, 
                         const int32_t* d_offsets, int groups, const int32_t* d_position, int copies, uint8_t* d_codes, int64_t ld_codes,
                         uint8_t* d_tiles, float* d_row_scale, void* stream) {
   if (!ctx || !element_type(dtype) || !rows_ok(rows, cols) || (block != 16 && block != 32)) return LUQ_ERR_ARG;
+  if (cols > kMostNumbers) return LUQ_ERR_UNSUPPORTED;
   if (planes < 1 || rows % planes || (d_offsets && (planes != 1 || groups < 1 || groups > LUQ_MAX_GROUPS))) return LUQ_ERR_ARG;
   if (d_position && (!d_offsets || copies < 1 || rows * copies > kMaxExtent)) return LUQ_ERR_ARG;
   const int64_t out_rows = d_position ? rows * copies : rows;

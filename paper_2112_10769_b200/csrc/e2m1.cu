@@ -141,15 +141,15 @@ __global__ void __launch_bounds__(LANES == kBlockRow ? 1024 : 128) e2m1_rows_ker
   const int lanes = LANES == kBlockRow ? static_cast<int>(blockDim.x) : LANES, per_block = LANES == kBlockRow ? 1 : 128 / (LANES == kBlockRow ? 1 : LANES);
   const int t = LANES == kBlockRow ? static_cast<int>(threadIdx.x) : static_cast<int>(threadIdx.x) % (LANES == kBlockRow ? 1 : LANES);
   const int chunks = p.k_tiles * (4 * BLOCK / kChunk);        // with the padding of the last tile of scales
-  const int rows = static_cast<int>(p.rows), step = static_cast<int>(gridDim.x) * per_block;
+  const long long rows = p.rows, step = static_cast<long long>(gridDim.x) * per_block;
   const long long plane_tiles = (p.plane_rows + 127) / 128;
   pdl_wait();
   pdl_trigger();
   // a plan's offsets are read once, a row's positions (the first 32) before its elements
   const Offsets offsets = PLAN ? Offsets(p) : Offsets();
   int turn = 0;
-  for (int first = static_cast<int>(blockIdx.x) * per_block; first < rows; first += step, turn ^= 1) {
-    const int r = first + (LANES == kBlockRow ? 0 : static_cast<int>(threadIdx.x) / (LANES == kBlockRow ? 1 : LANES));
+  for (long long first = static_cast<long long>(blockIdx.x) * per_block; first < rows; first += step, turn ^= 1) {
+    const int r = static_cast<int>(first) + (LANES == kBlockRow ? 0 : static_cast<int>(threadIdx.x) / (LANES == kBlockRow ? 1 : LANES));
     const bool there = r < rows;
     if (LANES == 32 && !there) break;                          // (a whole warp; nothing meets)
     const T* const x = static_cast<const T*>(p.x) + (there ? r : 0) * p.ld_x;

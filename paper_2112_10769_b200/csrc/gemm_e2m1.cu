@@ -1118,7 +1118,7 @@ int luq_launch_gemm_e2m1(luq_ctx* ctx, const luq_e2m1_args& a, bool early, cudaS
 }
 
 bool luq_e2m1_is_few(const luq_ctx* ctx, int64_t M, int64_t N, int64_t K) {
-  if (M > kFew) return false;
+  if (M > kFew || used_sms(ctx) < ctx->sm_count) return false;         // (a cluster for every tile, whatever the SM limit)
   const long long tiles = (N + kCh - 1) / kCh;
   const int num_kb = static_cast<int>((K + 2 * kBk - 1) / (2 * kBk)), split = few_split(tiles, used_sms(ctx), num_kb, static_cast<int>(M));
   return (num_kb + split - 1) / split <= kFewBlocks && tiles * split <= INT_MAX;

@@ -143,5 +143,7 @@ class Router(autograd.KeepsFloat32):
     @torch.no_grad()
     def rebalance(self, offsets: torch.Tensor, rate: float = 1e-3) -> None:
         """Raises the bias of experts with fewer rows than the mean and lowers that of the others, by ``rate``."""
+        if self.bias is None:
+            raise RuntimeError("this router was made without a bias for balance")
         load = (offsets[1:] - offsets[:-1]).float()
         self.bias += rate * torch.sign(load.mean() - load)

@@ -177,6 +177,21 @@ def test_product_into_a_part_of_a_tensor(ctx, dtype, pad, shift):
         assert (out[:, N:] == 7).all() and (base[:shift] == 7).all() and (base[shift + M * (N + pad):] == 7).all()
 
 
+def test_rows_beyond_32_bits(ctx):
+    # 2.6e9 elements in, 2.3e9 out: a row's answer does not depend on where it lies (the same tiles, the same sums)
+    M, N, K = 320000, 7200, 8192
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda")
+    part = tokens(256, K, torch.bfloat16)
+    wq = e2m1.quantize_weight(tokens(N, K, torch.float32, 1))
+    first = M - 512                                            # (a tile's first row)
+    x[first:first + 256] = part
+    z = ctx.quant_e2m1_gemm(x, *wq)
+    assert (z[:first] == 0).all() and (z[first + 256:] == 0).all()
+    q = ctx.quant_e2m1_rows(part)
+    xv, wv = e2m1.values(*q, K), e2m1.values(*wq, K)
+    close(z[first:first + 256], xv @ wv.t(), xv.abs() @ wv.abs().t(), K)
+
+
 def test_scales_from_elsewhere(ctx):
     # any e4m3 scales and any row scales, negative ones among them, and codes in rows further apart
     g = torch.Generator("cuda").manual_seed(1)
@@ -294,6 +309,17 @@ def test_refusals(ctx):
         e2m1.E2m1Linear(torch.randn(3, 40, 64, device="cuda"))
     with pytest.raises(ValueError):
         e2m1.E2m1Experts(torch.randn(40, 64, device="cuda"))
+    assert ctx.status() == 0
+
+
+def test_limited_to_some_multiprocessors(ctx):
+    x, w = tokens(300, 1000, torch.bfloat16), torch.randn(700, 1000, device="cuda")
+    wq = e2m1.quantize_weight(w)
+    xv, wv = definition(x, 16), e2m1.values(*wq, 1000)
+    for limit in (1, 2, 7, 0):
+        ctx.set_option(binding.OPT_SM_LIMIT, limit)
+        for M in (1, 2, 40, 300):
+            close(ctx.quant_e2m1_gemm(x[:M], *wq), xv[:M] @ wv.t(), xv[:M].abs() @ wv.abs().t(), 1000)
     assert ctx.status() == 0
 
 

@@ -118,6 +118,23 @@ def test_rows_that_no_position_names_play_no_part(ctx):
     assert torch.isfinite(ctx.combine(y, position, w)[[0, 1]]).all()
 
 
+def test_rows_beyond_32_bits(ctx):
+    # copies of 2.5e9 elements: the last rows are where they belong
+    T, cols = 310000, 8192
+    x = torch.zeros(T, cols, dtype=torch.bfloat16, device="cuda")
+    x[:, 0] = (torch.arange(T, device="cuda") % 251).to(torch.bfloat16)
+    x[:, -1] = 1.0
+    chosen = torch.zeros(T, 1, dtype=torch.int32, device="cuda")
+    chosen[::2] = 1                                            # odd tokens first
+    offsets, position = ctx.expert_order(chosen, 2)
+    rows = ctx.dispatch(x, position, offsets)
+    token = torch.cat([torch.arange(1, T, 2, device="cuda"), torch.arange(0, T, 2, device="cuda")])
+    assert torch.equal(rows[:, 0], x[token, 0]) and (rows[:, -1] == 1).all()
+    assert torch.equal(ctx.combine(rows, position)[:, 0], x[:, 0])
+    _, dw = ctx.combine_bwd(x, rows, position, None, offsets, need_dy=False)
+    assert torch.equal(dw[:, 0], x[:, 0].float() ** 2 + 1)
+
+
 def test_out_arguments(ctx):
     offsets, position = ctx.expert_order(choice(30, 2, 8), 8)
     x = torch.randn(30, 50, device="cuda")
