@@ -132,8 +132,14 @@ __device__ __forceinline__ void store_chunk(const RowsParams& p, const Place<BLO
 // LANES-th of the row; CHUNKS = 0: any width, chunks are read again for the second pass (from L2).  PLAN: rows go where offsets and
 // positions say.
 constexpr int kBlockRow = 0;
+constexpr int most_threads(int lanes, int chunks) { return lanes != kBlockRow ? 128 : chunks == 4 ? 256 : 1024; }
+// Blocks that an SM has to hold, and so the registers a thread may have: left alone, the compiler keeps all chunks' steps in flight at
+// once (16384 x 1024 bf16, two chunks, 10 blocks: 7.9 us, unbound 10.0; 32768 x 2048, four chunks, 8 blocks: 29.2 us, with 6 31).
+constexpr int least_blocks(int lanes, int chunks, bool half) {
+  return chunks == 4 ? (lanes == kBlockRow ? 4 : 8) : chunks == 2 && lanes == 32 && half ? 10 : 1;
+}
 template <typename T, int BLOCK, int LANES, int CHUNKS, bool PLAN>
-__global__ void __launch_bounds__(LANES == kBlockRow ? 1024 : 128) e2m1_rows_kernel(const RowsParams p) {
+__global__ void __launch_bounds__(most_threads(LANES, CHUNKS), least_blocks(LANES, CHUNKS, sizeof(T) == 2)) e2m1_rows_kernel(const RowsParams p) {
   static_assert(!PLAN || LANES == kBlockRow || LANES == 32, "a plan is read by whole warps");
   constexpr int kHeld = CHUNKS > 0 ? CHUNKS : 1;
   __shared__ uint32_t box[2][32];
@@ -215,7 +221,17 @@ __global__ void __launch_bounds__(LANES == kBlockRow ? 1024 : 128) e2m1_rows_ker
       quantize_chunk<T, BLOCK>(v, b, row, codes, byte);
       return scale_word<BLOCK>(c < chunks ? byte : 0u, Place<BLOCK>(p, c).shift);
     };
-    if constexpr (CHUNKS > 0) {
+    // one place: a chunk's codes leave as they are made, in few registers (two chunks have enough: 16384 x 4096 33.9 us, 34.8 so)
+    if constexpr (!PLAN && (CHUNKS == 4 || LANES == 32)) {
+      places([&](int to, long long tiles_from, bool tiled) {
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) {
+          uint2 codes;
+          const uint32_t word = finish(w[i], top[i], t + i * lanes, codes);
+          store_chunk<BLOCK>(p, Place<BLOCK>(p, t + i * lanes), to, tiles_from, tiled, codes, word);
+        }
+      });
+    } else if constexpr (CHUNKS > 0) {
       uint2 codes[kHeld];
       uint32_t word[kHeld];
 #pragma unroll
@@ -251,16 +267,20 @@ __global__ void __launch_bounds__(LANES == kBlockRow ? 1024 : 128) e2m1_rows_ker
 template <typename T, int BLOCK, int LANES, int CHUNKS, bool PLAN>
 int launch(luq_ctx* ctx, const RowsParams& p, int threads, cudaStream_t st) {
   const int per_block = LANES == kBlockRow ? 1 : 128 / (LANES == kBlockRow ? 1 : LANES);
-  // bf16: as many blocks as may be resident at once, which walk (16384 x 4096, blocks of 32: 27.8 us, 29.2 with a block for every
-  // row); fp32: a block for every row (44.8 us, walking 49.3)
-  const long long blocks = (p.rows + per_block - 1) / per_block, most = sizeof(T) == 2 ? static_cast<long long>(ctx->sm_count) * (2048 / threads) : blocks;
+  // bf16, up to two chunks: blocks for 2048 threads an SM, which walk (16384 x 1024: 12.5 us with one chunk, 17.5 with blocks for all
+  // rows; two chunks 9.3 and 10.0); four chunks and fp32: blocks for all rows (16384 x 4096 bf16 33.3 us, walking 35.2; fp32 45 and 47)
+  const long long blocks = (p.rows + per_block - 1) / per_block;
+  const long long most = sizeof(T) == 2 && CHUNKS < 4 ? static_cast<long long>(ctx->sm_count) * (2048 / threads) : blocks;
   const cudaError_t e = luq_launch_kernel(e2m1_rows_kernel<T, BLOCK, LANES, CHUNKS, PLAN>, static_cast<int>(blocks < most ? blocks : most), threads, 0,
                                           st, LUQ_LAUNCH_EARLY, 1, p);
   if (e == cudaSuccess) ctx->launches += 1;
   return static_cast<int>(e);
 }
-// Narrow rows share a warp.  A thread takes two chunks where there are rows enough to fill the card (the steps that a row costs are
-// shared: 16384 x 4096 bf16, blocks of 16: 33 us, with one chunk 44, with four 43), one where a few rows' latency counts.
+// Narrow rows share a warp.  A thread takes one chunk where a few rows' latency counts, two where there are rows enough to fill the
+// card and four bf16 ones where they fill it more than once (the steps that a row costs are shared: 16384 x 2048 bf16, blocks of 16:
+// 20.9, 17.9, 14.4 us with one, two, four; 4800 rows 6.9, 6.1, 6.1; 2400 rows 4.2, 3.8, 5.1).  Warps that have to meet fill it later,
+// and win less: 16384 x 8192 68.9 -> 62.5 us, two copies of 8192 x 4096 28.7 -> 25.1; 16384 x 4096 33.9 -> 33.3 alone, but 162.9 -> 164.4
+// before a product at the power cap, so two there.  Four fp32 chunks leave too few warps (16384 x 2048: 24.1 us with two, 28).
 template <typename T, int BLOCK, bool PLAN>
 int launch_width(luq_ctx* ctx, const RowsParams& p, cudaStream_t st) {
   const int chunks = p.k_tiles * (4 * BLOCK / kChunk);
@@ -271,6 +291,11 @@ int launch_width(luq_ctx* ctx, const RowsParams& p, cudaStream_t st) {
   if (chunks <= 32) return launch<T, BLOCK, 32, 1, PLAN>(ctx, p, 128, st);
   const bool many = p.rows >= 4ll * ctx->sm_count;
   if (chunks <= 64 && many) return launch<T, BLOCK, 32, 2, PLAN>(ctx, p, 128, st);
+  if constexpr (sizeof(T) == 2) {
+    const long long filled = 4096ll * ctx->sm_count;             // chunks that all resident warps hold at four a thread
+    if (chunks <= 128 && p.rows * chunks >= filled) return launch<T, BLOCK, 32, 4, PLAN>(ctx, p, 128, st);
+    if (chunks > (PLAN ? 128 : 256) && chunks <= 1024 && p.rows * chunks >= 3 * filled) return launch<T, BLOCK, kBlockRow, 4, PLAN>(ctx, p, (chunks + 127) / 128 * 32, st);
+  }
   if (chunks <= 1024 && !many) return launch<T, BLOCK, kBlockRow, 1, PLAN>(ctx, p, (chunks + 31) / 32 * 32, st);
   if (chunks <= 2048) return launch<T, BLOCK, kBlockRow, 2, PLAN>(ctx, p, (chunks + 63) / 64 * 32, st);
   return launch<T, BLOCK, kBlockRow, 0, PLAN>(ctx, p, 1024, st);

@@ -84,6 +84,56 @@ def test_quantizer(ctx, rows, cols, pad, shift, dtype, block):
     assert (beyond == 0).all() and ctx.status() == 0
 
 
+# so many rows that a thread takes several pieces of each: rows of a warp and of a block, whole and ragged, aligned and not
+MANY = [(4801, 2000, 0, 0), (9500, 1041, 1, 1), (5000, 1025, 7, 0), (18500, 2065, 0, 0), (9500, 4096, 0, 0), (9500, 4097, 1, 3), (2400, 16384, 0, 0)]
+
+
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("rows,cols,pad,shift", MANY)
+def test_quantizer_of_many_rows(ctx, rows, cols, pad, shift, block):
+    x = tokens(rows, cols, torch.bfloat16, 0, pad, shift)
+    x[rows // 2, cols // 3] = 0.0
+    x[rows - 1] = 0.0
+    codes, tiles, scale = ctx.quant_e2m1_rows(x, block)
+    assert torch.equal(e2m1.values(codes, tiles, scale, cols, block), definition(x, block))
+    beyond = e2m1.scale_rows(tiles, rows, tiles.shape[1] * 4 * block, block)[:, -(-cols // block):]
+    assert (beyond == 0).all() and ctx.status() == 0
+    x[7, cols - 1], x[rows - 2, 0] = NAN, INF                 # two rows of neither numbers nor a scale leave the others as they are
+    again, tiles2, scale2 = ctx.quant_e2m1_rows(x, block)
+    others = torch.ones(rows, dtype=torch.bool, device="cuda")
+    others[7] = others[rows - 2] = False
+    assert torch.equal(again[others], codes[others]) and ctx.status() == binding.STATUS_NONFINITE
+    a, b = e2m1.scale_rows(tiles, rows, cols, block), e2m1.scale_rows(tiles2, rows, cols, block)
+    assert torch.equal(a[others].view(torch.uint8), b[others].view(torch.uint8))
+
+
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("rows,cols,pad,shift", [(5000, 1999, 1, 0), (9500, 4096, 0, 0)])
+def test_quantizer_of_many_copies(ctx, rows, cols, pad, shift, block):
+    x = tokens(rows, cols, torch.bfloat16, 0, pad, shift)
+    g = torch.Generator("cuda").manual_seed(rows)
+    chosen = torch.rand(rows, 7, device="cuda", generator=g).topk(2, dim=1).indices.int()
+    chosen[::5, 1] = -1
+    offsets, position = ctx.expert_order(chosen, 7)
+    codes, tiles, scale = ctx.quant_e2m1_rows(x, block)
+    at, tiles_at, scale_at = ctx.quant_e2m1_rows(x, block, offsets=offsets, position=position)
+    there = position >= 0
+    token = torch.arange(rows, device="cuda")[:, None].expand(-1, 2)[there]
+    to = position[there].long()
+    assert torch.equal(at[to], codes[token])
+    if block == 16:
+        assert torch.equal(scale_at[to], scale[token])
+    plain = e2m1.scale_rows(tiles, rows, cols, block).view(torch.uint8)
+    source = torch.empty(int(there.sum()), dtype=torch.long, device="cuda")
+    source[to] = token
+    ends = offsets.tolist()
+    for e in range(7):
+        n = ends[e + 1] - ends[e]
+        got = e2m1.scale_rows(tiles_at[ends[e] // 128 + e:], n, cols, block).view(torch.uint8)
+        assert torch.equal(got, plain[source[ends[e]:ends[e + 1]]])
+    assert ctx.status() == 0
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_quantizer_at_the_borders(ctx, dtype):
     # every border between two numbers, and the patterns next to it, with scales that are powers of two; the first element is the largest
