@@ -172,39 +172,44 @@ __device__ __forceinline__ void sort_keys(uint32_t (&v)[N]) {
 
 // Where binary32 leaves a choice open (two values that decide lie closer than their errors: some rows in a thousand), it is made
 // again in binary64, by three functions that a warp's rows enter together; each reads the logits again, so that nothing is held for
-// their sake.  One such row at a launch's end is all of its tail, so the frequent ones are quick: the groups' values from a lane's
-// own experts, and the order of the places from the chosen experts' values, a lane each.  The third makes the whole choice.
+// their sake.  One such row at a launch's end is all of its tail (16384 x 256 sigmoids, groups and bias: 17.3 us without any, 22 where
+// all experts' values were computed again, 20.0 now), so the frequent ones are quick: the groups' values from the experts that may
+// decide them, and the order of the places from the chosen experts' values, a lane each.  The third makes the whole choice (8192 x
+// 512 with one such row: 32 us; 46 when every place was looked for among all experts).  Their code is never in the instruction
+// cache when it is needed, so the exponential is one function, and loops are not unrolled (20.3 and 20.9 us otherwise).
 
-// exp(l - top) of a row, summed
+__device__ __noinline__ double exact_exp(double v) { return exp(v); }
+// the sum of exp(l - top) of a row, where it plays a part: without a bias the exponentials compare as the scores do
 template <typename T, int LANES>
-__device__ __forceinline__ double exact_sum(const RouteParams& p, const T* row, int ls, double& top) {
-  double most = -INFINITY, sum = 0.0;
-  for (int e = ls; e < p.experts; e += LANES) most = fmax(most, static_cast<double>(load1(row + e)));
-#pragma unroll
-  for (int o = LANES / 2; o; o >>= 1) most = fmax(most, __shfl_xor_sync(kFull, most, o));
-  for (int e = ls; e < p.experts; e += LANES) sum += exp(static_cast<double>(load1(row + e)) - most);
+__device__ __forceinline__ double exact_sum(const RouteParams& p, const T* row, int ls, float top) {
+  if (p.sigmoid || !p.bias) return 1.0;
+  double sum = 0.0;
+  for (int e = ls; e < p.experts; e += LANES) sum += exact_exp(static_cast<double>(load1(row + e)) - top);
 #pragma unroll
   for (int o = LANES / 2; o; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
-  top = most;
   return sum;
 }
-__device__ __forceinline__ double exact_value(const RouteParams& p, double l, int e, double top, double sum) {
+__device__ __forceinline__ double exact_value(const RouteParams& p, double l, int e, float top, double sum) {
   if (l == -INFINITY) return l;
-  const double s = p.sigmoid ? 1.0 / (1.0 + exp(-l)) : exp(l - top) / sum;
-  return p.bias ? s + static_cast<double>(*(p.bias + e)) : s;
+  double s = exact_exp(p.sigmoid ? -l : l - top);
+  if (p.sigmoid) s = 1.0 / (1.0 + s);
+  return p.bias ? (p.sigmoid ? s : s / sum) + static_cast<double>(*(p.bias + e)) : s;
 }
 
-// does this lane's group stay?
-template <typename T, int LANES, int VPL>
-__device__ __noinline__ bool exact_groups(const RouteParams& p, const T* row, int e0, int n, int per_group) {
+// does this lane's group stay?  `may`: the places of this lane's experts that may be one of the group's best two
+template <typename T, int LANES>
+__device__ __noinline__ bool exact_groups(const RouteParams& p, const T* row, int e0, uint32_t may, int per_group, float top) {
   const int ls = threadIdx.x & (LANES - 1);
-  double top = 0.0, sum = 1.0, first = -INFINITY, second = -INFINITY;
-  if (!p.sigmoid) sum = exact_sum<T, LANES>(p, row, ls, top);
-#pragma unroll 4
-  for (int i = 0; i < VPL; ++i) {
-    const double c = i < n ? exact_value(p, load1(row + e0 + i), e0 + i, top, sum) : -INFINITY;
-    second = fmax(second, fmin(first, c));
-    first = fmax(first, c);
+  const double sum = exact_sum<T, LANES>(p, row, ls, top);
+  double first = -INFINITY, second = -INFINITY;
+  while (__any_sync(kFull, may != 0u)) {
+    if (may) {
+      const int e = e0 + __ffs(may) - 1;
+      may &= may - 1;
+      const double c = exact_value(p, load1(row + e), e, top, sum);
+      second = fmax(second, fmin(first, c));
+      first = fmax(first, c);
+    }
   }
   for (int o = 1; o < per_group; o *= 2) {
     const double f = __shfl_xor_sync(kFull, first, o), g = __shfl_xor_sync(kFull, second, o);
@@ -222,89 +227,104 @@ __device__ __noinline__ bool exact_groups(const RouteParams& p, const T* row, in
 
 // the experts found (lane j has the j-th, -1: none; every lane the one beyond them, -1: it plays no part) in exact order
 template <typename T, int LANES>
-__device__ __noinline__ int exact_places(const RouteParams& p, const T* row, int mine, int extra) {
-  const int ls = threadIdx.x & (LANES - 1);
-  double top = 0.0, sum = 1.0;
+__device__ __noinline__ int exact_places(const RouteParams& p, const T* row, int mine, int extra, float top) {
+  const int ls = threadIdx.x & (LANES - 1), places = min(p.k + 1, LANES);
   const bool scored = p.bias || p.groups > 1;
-  if (scored && !p.sigmoid) sum = exact_sum<T, LANES>(p, row, ls, top);
-  auto value = [&](int e) {
-    const double l = e >= 0 ? static_cast<double>(load1(row + e)) : -INFINITY;
-    return scored ? exact_value(p, l, e, top, sum) : l;
-  };
-  const double c = value(mine), cx = value(extra);
-  auto before = [](double ca, int ea, double cb, int eb) { return ea >= 0 && (ca > cb || (ca == cb && ea < eb)); };
-  int rank = before(cx, extra, c, mine), rank_x = 0, at = -1;
-  for (int i = 0; i < LANES; ++i) {
-    const double ci = __shfl_sync(kFull, c, i, LANES);
-    const int ei = __shfl_sync(kFull, mine, i, LANES);
-    rank += before(ci, ei, c, mine);
-    rank_x += before(ci, ei, cx, extra);
+  const double sum = scored ? exact_sum<T, LANES>(p, row, ls, top) : 1.0;
+  double cx = -INFINITY;
+  int e = ls < p.k ? mine : -1, ex = -1;
+  double c = -INFINITY;
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {               // the one beyond: the next lane's, or of all lanes where there is none left
+    const int at = pass ? extra : ls == p.k ? extra : e;
+    const double l = at >= 0 ? static_cast<double>(load1(row + at)) : -INFINITY;
+    const double v = scored ? exact_value(p, l, at, top, sum) : l;
+    if (pass) { cx = v; ex = at; }
+    else { c = v; e = at; }
+    if (p.k < LANES) break;
   }
-  for (int i = 0; i < LANES; ++i) {
-    const int ei = __shfl_sync(kFull, mine, i, LANES), ri = __shfl_sync(kFull, rank, i, LANES);
+  auto before = [](double ca, int ea, double cb, int eb) { return ea >= 0 && (ca > cb || (ca == cb && ea < eb)); };
+  int rank = before(cx, ex, c, e), rank_x = 0, at = -1;
+  for (int i = 0; i < places; ++i) {
+    const double ci = __shfl_sync(kFull, c, i, LANES);
+    const int ei = __shfl_sync(kFull, e, i, LANES);
+    rank += before(ci, ei, c, e);
+    rank_x += before(ci, ei, cx, ex);
+  }
+  for (int i = 0; i < places; ++i) {
+    const int ei = __shfl_sync(kFull, e, i, LANES), ri = __shfl_sync(kFull, rank, i, LANES);
     if (ei >= 0 && ri == ls) at = ei;
   }
-  return extra >= 0 && rank_x == ls ? extra : at;
+  return ex >= 0 && rank_x == ls ? ex : at;
 }
 
 // the choice by a whole warp for one row: lane j gets the j-th expert or -1
 template <typename T>
-__device__ __noinline__ int choose_exact(const RouteParams& p, const T* row) {
+__device__ __noinline__ int choose_exact(const RouteParams& p, const T* row, float top) {
   const int lane = threadIdx.x & 31;
   const bool scored = p.bias || p.groups > 1;
   const double none = -INFINITY;
-  double top = 0.0, sum = 1.0, values[LUQ_MAX_GROUPS / 32];      // of experts `lane`, `lane` + 32, ...
-  if (scored && !p.sigmoid) sum = exact_sum<T, 32>(p, row, lane, top);
-#pragma unroll 4
+  const double sum = scored ? exact_sum<T, 32>(p, row, lane, top) : 1.0;
+  double values[LUQ_MAX_GROUPS / 32];                  // of experts `lane`, `lane` + 32, ...
+  uint32_t rest = 0;                                   // those that may be chosen yet
+#pragma unroll 1
   for (int i = 0; i < (p.experts + 31) / 32; ++i) {
     const int e = lane + 32 * i;
     const double l = e < p.experts ? static_cast<double>(load1(row + e)) : none;
     values[i] = scored ? exact_value(p, l, e, top, sum) : l;
+    if (values[i] > none) rest |= 1u << i;
   }
-  // the best of experts `from` .. `to` - 1 in the groups of `stay` that comes after (v, e) in the order; e = -1: there is none
-  const int size = p.experts / p.groups;
-  auto next = [&](int from, int to, uint32_t stay, double& v, int& e) {
-    unsigned long long best = key_of(none);
-    int at = INT_MAX;
-    for (int i = from + ((lane - from) & 31); i < to; i += 32) {
-      const double vi = values[i >> 5];
-      const unsigned long long ki = key_of(vi);
-      if (ki > best && (vi < v || (vi == v && i > e)) && stay >> (i / size) & 1) { best = ki; at = i; }
-    }
-    const unsigned long long all = warp_max(best);
-    const int index = static_cast<int>(__reduce_min_sync(kFull, static_cast<unsigned>(best == all ? at : INT_MAX)));
-    v = value_of(all);
-    e = index == INT_MAX ? -1 : index;
-  };
-  uint32_t stay = kFull;
   if (p.groups > 1) {
+    const int size = p.experts / p.groups;
+    auto of_group = [&](int g) {                       // this lane's experts of a group
+      const int from = (g * size + 31 - lane) >> 5, to = ((g + 1) * size + 31 - lane) >> 5;      // (of 32 places at most)
+      return static_cast<uint32_t>((1ull << to) - (1ull << from)) & rest;
+    };
     double mine = none;
     for (int g = 0; g < p.groups; ++g) {
-      double v = INFINITY, w;
-      int e = -1;
-      next(g * size, (g + 1) * size, kFull, v, e);
-      w = v;
-      if (p.group_top == 2 && e >= 0) {
-        next(g * size, (g + 1) * size, kFull, w, e);
-        w = e >= 0 ? v + w : v;
+      double first = none, second = none;
+      for (uint32_t m = of_group(g); m; m &= m - 1) {
+        const double c = values[__ffs(m) - 1];
+        second = fmax(second, fmin(first, c));
+        first = fmax(first, c);
       }
-      if (lane == g) mine = w;
+      const unsigned long long best = warp_max(key_of(first));
+      if (lane == __ffs(__ballot_sync(kFull, key_of(first) == best)) - 1) first = second;
+      const double next = value_of(warp_max(key_of(first))), w = value_of(best);
+      if (lane == g) mine = p.group_top == 2 && next > none ? w + next : w;
     }
-    stay = 0;
+    uint32_t stay = 0;
     unsigned long long k = lane < p.groups ? key_of(mine) : 0ull;
     for (int h = 0; h < p.top_groups; ++h) {
       const int g = __ffs(__ballot_sync(kFull, warp_max(k) == k && k > 0)) - 1;
       if (g < 0) break;
-      stay |= 1u << g;
+      stay |= of_group(g);
       if (lane == g) k = 0;
     }
+    rest = stay;
   }
-  double v = INFINITY;
-  int e = -1, mine = -1;
+  // a lane's best, which it looks for again once that is taken
+  unsigned long long best;
+  int at;
+  auto look = [&]() {
+    best = key_of(none);
+    at = 0;
+    for (uint32_t m = rest; m; m &= m - 1) {
+      const unsigned long long k = key_of(values[__ffs(m) - 1]);
+      if (k > best) { best = k; at = __ffs(m) - 1; }
+    }
+  };
+  look();
+  int mine = -1;
   for (int j = 0; j < p.k; ++j) {
-    next(0, p.experts, stay, v, e);
-    if (e < 0) break;
+    const unsigned long long all = warp_max(best);
+    if (all == key_of(none)) break;
+    const int e = static_cast<int>(__reduce_min_sync(kFull, best == all ? static_cast<unsigned>(lane + 32 * at) : 0xFFFFFFFFu));
     if (lane == j) mine = e;
+    if (lane == (e & 31)) {
+      rest &= ~(1u << at);
+      look();
+    }
   }
   return mine;
 }
@@ -411,7 +431,12 @@ __global__ void __launch_bounds__(128) route_kernel(const RouteParams p) {
     const float least = value_of(~seg_max<LANES>(stays ? ~mine : 0u)), most = value_of(seg_max<LANES>(stays ? key_of(minus_inf()) : mine));
     const bool close = most > minus_inf() && !clear(least, most, 4.0f) && !bad;
     if (__any_sync(kFull, close)) {
-      const bool exact = exact_groups<T, LANES, VPL>(p, row, e0, n, per_group);
+      // an expert clear of the group's second (where it has one) is not among its two
+      uint32_t may = 0;
+#pragma unroll
+      for (int i = 0; i < VPL; ++i)
+        if (close && keys[i] && !(second && clear(value_of(second & ~kPlace), value_of(keys[i] & ~kPlace), 2.0f))) may |= 1u << (kPlace - (keys[i] & kPlace));
+      const bool exact = exact_groups<T, LANES>(p, row, e0, may, per_group, top);
       if (close) stays = exact;
     }
     if (!stays) {
@@ -468,13 +493,13 @@ __global__ void __launch_bounds__(128) route_kernel(const RouteParams p) {
   }
   open &= !bad;
   if (__any_sync(kFull, open)) {
-    const int exact = exact_places<T, LANES>(p, row, mine, extra);
+    const int exact = exact_places<T, LANES>(p, row, mine, extra, top);
     if (open) mine = exact;
     uint32_t left = __ballot_sync(kFull, open && beyond);       // more values in a row that binary32 does not tell apart
     while (left) {
       const int first = (__ffs(left) - 1) / LANES * LANES;     // its row's first lane
       const long long row_at = __shfl_sync(kFull, r, first);
-      const int all = choose_exact<T>(p, static_cast<const T*>(p.logits) + row_at * p.ld);
+      const int all = choose_exact<T>(p, static_cast<const T*>(p.logits) + row_at * p.ld, __shfl_sync(kFull, top, first));
       const int at = __shfl_sync(kFull, all, ls);
       if (lane / LANES * LANES == first) mine = at;
       left &= LANES == 32 ? 0u : ~(((1u << (LANES & 31)) - 1u) << first);
