@@ -214,3 +214,21 @@ def test_refusals(ctx):
             call()
         assert e.value.code == binding.ERR_ARG
     assert ctx.route(x[:0], 2)[0].shape == (0, 2) and ctx.status() == 0
+
+
+# many rows, so that groups, places and whole rows that binary32 leaves open are among them; as many places as lanes have a row; rows
+# that share a warp with open ones
+@pytest.mark.parametrize("T,E,k,groups,top_groups,kind", [(20000, 512, 8, 4, 2, "plain"), (20000, 160, 6, 8, 3, "plain"), (6000, 1000, 32, 8, 4, "plain"), (20000, 64, 8, 8, 4, "plain"),
+                                                          (3001, 64, 8, 8, 5, "close"), (3001, 128, 16, 4, 2, "close"), (2000, 1024, 32, 32, 20, "close"), (3001, 60, 8, 1, 1, "close")])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_many_rows_left_open(ctx, T, E, k, groups, top_groups, kind, score):
+    g = torch.Generator("cuda").manual_seed(T + E)
+    bias = (0.05 if kind == "plain" else 5e-8) * torch.randn(E, device="cuda", generator=g)
+    x = logits(T, E, torch.float32, kind, 9)
+    if kind == "close":                                     # every other row is clear of it all
+        x[1::2] += 0.01 * torch.randperm(E, device="cuda", generator=g)
+    for group_top in (1, 2):
+        for b in (bias, None):
+            form = dict(score=score, bias=b, groups=groups, top_groups=top_groups, group_top=group_top)
+            assert torch.equal(ctx.route(x, k, **form)[0], reference(x, k, **form)[0])
+    assert ctx.status() == 0
